@@ -303,6 +303,86 @@ int ppu_attention_bwd_static(const void* qkv, const void* U, const float* lse, c
                              void* dqkv, int batch, int seq, int n_head, int d_head, int backend,
                              void* cuda_stream);
 
+/* ---- losses of hidden states against the vocabulary ---------------------------
+ *
+ * Softmax cross entropy, and distillation from a teacher's top logits, of hidden states X[T,d]
+ * (bf16, row stride ldx) against a vocabulary matrix E[V,d] (bf16, row stride lde; the tied
+ * embedding of this library's models), without holding the logits [T,V]: rows are worked in chunks
+ * of chunk_rows, and a chunk's softmax is kept (bf16) only until its gradients are formed.  With
+ * s = X E^T / temperature, lse_t = log sum_v exp s_tv and p = softmax(s):
+ *   row_loss_t = sum_j q_tj (log q_tj - s_t,id(j) + lse_t),   loss = sum_t w_t row_loss_t
+ *   dX = ds E / temperature, dE = ds^T X / temperature, ds_tv = w_t (Q_t p_tv - sum_{id(j)=v} q_tj)
+ * with Q_t = sum_j q_tj.
+ *   xent:    one entry a row, id = target[t], q = 1, temperature 1: the negative log-likelihood.
+ *   distill: up to k entries a row, (teacher_ids, teacher_logits)[t, 0..k).  q is the softmax of
+ *            teacher_logits / temperature over the row's entries, or, where teacher_lse[T] is given (the
+ *            log-sum-exp of all of the teacher's logits / temperature), exp(logit / temperature -
+ *            teacher_lse).  An entry whose id is negative or whose logit is -inf is absent; an id
+ *            given several times counts once for each.
+ * A row without a present entry (target < 0) has no loss and no gradient; its lse is still written.
+ * Ids >= V are left out in the same way and set flags[0].  row_weight: fp32 [T] (w), or null: w = 1 /
+ * (rows that have an entry), a mean; 0 over no rows at all.
+ *
+ * loss: fp32 [1].  row_loss, lse: fp32 [T] or null.  dX: bf16 [T,d] (row stride lddx) or null; dE: bf16
+ * [V,d] (row stride ldde) or null; both are written, not added to, and overlap no input.  d is a
+ * multiple of 8 up to 16384, row strides multiples of 8, X, E, dX, dE 16-byte aligned; T <= 2^20,
+ * V <= 2^22, any values within.  chunk_rows: 0 = as many as keep 256 MiB of softmax, else rows of a
+ * chunk (rounded up to a multiple of 256); larger chunks are faster.  workspace: DEVICE, 256-byte
+ * aligned, of the size ppu_head_query_bytes gives for the same T, d, V, gradients (1: dX, 2: dE) and
+ * chunk_rows; calls that may overlap on the GPU need one each.  flags: DEVICE int32 [8], zeroed by the
+ * caller once, or null (nothing is reported); read by ppu_op_status.  All other pointers DEVICE.
+ * Asynchronous on the stream; results do not depend on timing.  Sizes that are not 0 must not exceed
+ * the buffers; the calls may be captured. */
+#define PPU_MAX_TEACHER_ENTRIES 128
+int ppu_head_query_bytes(int T, int d, int V, int grads, int chunk_rows, size_t* bytes);
+int ppu_head_xent(const void* X, int64_t ldx, const void* E, int64_t lde, const int32_t* target,
+                  const float* row_weight, int T, int d, int V, float* loss, float* row_loss,
+                  float* lse, void* dX, int64_t lddx, void* dE, int64_t ldde, int chunk_rows,
+                  void* workspace, size_t workspace_bytes, int32_t* flags, void* cuda_stream);
+/* ld_ids, ld_logits: row strides of teacher_ids (int32) and teacher_logits (fp32), at least k;
+ * 1 <= k <= PPU_MAX_TEACHER_ENTRIES; teacher_lse may be null. */
+int ppu_head_distill(const void* X, int64_t ldx, const void* E, int64_t lde,
+                     const int32_t* teacher_ids, int64_t ld_ids, const float* teacher_logits,
+                     int64_t ld_logits, int k, const float* teacher_lse, float temperature,
+                     const float* row_weight, int T, int d, int V, float* loss, float* row_loss,
+                     float* lse, void* dX, int64_t lddx, void* dE, int64_t ldde, int chunk_rows,
+                     void* workspace, size_t workspace_bytes, int32_t* flags, void* cuda_stream);
+/* Waits for the stream and reads the error words that calls given `flags` may have set: PPU_ETOKEN
+ * (an id >= V was left out), PPU_ETIMEOUT (a bounded wait inside a kernel expired: the results are
+ * not valid), else PPU_OK.  Clears them. */
+int ppu_op_status(int32_t* flags, void* cuda_stream);
+
+/* ---- norms before and after a block, with its gate and the residual scale ---------
+ *
+ *   n = N(y) post_gain + post_shift;  r_out = res_scale r + gate n;  h = N(r_out) pre_gain + pre_shift
+ * for a block's output y[T,d] (bf16) and the residual stream r[T,d] (fp32): the norm after the block,
+ * its gate, the residual addition and the norm before the next block (or the head) in one pass.
+ * kind: N is LayerNorm or RMSNorm (no mean taken off), with eps added to the mean square.
+ * Gains: fp32 [d]; shifts: fp32 [d] or null.  gate: fp32 [ceil(T / gate_rows), d], a row for every gate_rows
+ * consecutive rows of y (T: one for all, a sequence's length: one each, 1: one per token), or null.
+ * r_out: fp32 [T,d], may be r itself; h: bf16 [T,d]; stats: fp32 [T,4], both norms' mean and 1 / deviation.
+ *
+ * Backward: from dh (bf16), dr_out (fp32, the gradient that reaches r_out through the residual stream,
+ * or null), y, the saved r_out and stats: dy (bf16), dr (fp32, may be dr_out itself), and summed over
+ * the rows dpost_gain, dpost_shift, dpre_gain, dpre_shift (fp32 [d]; the shifts' may be null) and dgate
+ * (shape of gate; given if and only if gate is).  post_shift is needed where the forward pass had
+ * one.  Sums have a fixed order.  All are written, not added to.
+ * d is a multiple of 8 up to 4096; rows are contiguous; every operand 16-byte aligned.  workspace:
+ * DEVICE, the size ppu_norm_gate_query_bytes gives (gate_rows 0 without a gate); calls that may overlap
+ * on the GPU need one each.  All pointers DEVICE.  Asynchronous on the stream; the calls may be captured. */
+enum { PPU_NORM_LAYER = 0, PPU_NORM_RMS = 1 };
+int ppu_norm_gate_fwd(const void* y, const float* r, const float* gate, int gate_rows,
+                      const float* post_gain, const float* post_shift, const float* pre_gain,
+                      const float* pre_shift, int kind, float res_scale, float eps, float* r_out,
+                      void* h, float* stats, int T, int d, void* cuda_stream);
+int ppu_norm_gate_query_bytes(int T, int d, int gate_rows, size_t* bytes);
+int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void* y, const float* r_out,
+                      const float* stats, const float* gate, int gate_rows, const float* post_gain,
+                      const float* post_shift, const float* pre_gain, int kind, float res_scale,
+                      void* dy, float* dr, float* dpost_gain, float* dpost_shift, float* dpre_gain,
+                      float* dpre_shift, float* dgate, int T, int d, void* workspace,
+                      size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,8 +20,13 @@ enum GemmEpilogue {
   // C bf16 = acc (the attention output's gradient dU), and per (token, head)
   // C3 fp32 [batch, heads, rope_S] = sum over the head's rope_dh columns of C * aux (aux = U bf16):
   // the row term of the softmax backward, formed while dU is still in registers
-  EPI_DELTA_BF16 = 6
+  EPI_DELTA_BF16 = 6,
+  // softmax pieces (launch_gemm_tc_pieces only): per row and 64 columns, C bf16 = 2^(x - max) with
+  // x = acc * piece_scale, and piece_stats = {max, sum of the unrounded powers}
+  EPI_PIECES = 7,
+  EPI_RESID_BF16 = 8   // C bf16 = aux fp32 + acc (launch_gemm_tc_resid_bf16 only)
 };
+constexpr int PIECE = 64;   // columns of one softmax piece
 
 struct GemmArgs {
   const bf16* A; int64_t lda; int a_kmajor;  // a_kmajor: A[m*lda+k], else A[k*lda+m]
@@ -44,10 +49,17 @@ struct GemmArgs {
   // per 256 x 256 tile, 3 an SM pair per 256 x 128 tile, 4 as 2 without cutting the tiles of a
   // half-empty last wave in two (tests force each)
   int tile_shape = 0;
+  // EPI_PIECES: piece_stats [M][ld_pieces]; C (leading dimension a multiple of PIECE) may be null,
+  // columns of C from N up to the next multiple of PIECE are written as zeros
+  float piece_scale = 1.f; float2* piece_stats = nullptr; int64_t ld_pieces = 0;
+  // operands that come and go (a caller's tensors): their tensor maps are encoded for this launch
+  bool transient = false;
 };
 
 int launch_gemm_simt(const GemmArgs& g, cudaStream_t st);
 int launch_gemm_tc(const GemmArgs& g, cudaStream_t st);   // tcgen05 / TMEM / TMA
+int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st);      // EPI_PIECES, both operands K-major, any N
+int launch_gemm_tc_resid_bf16(const GemmArgs& g, cudaStream_t st);  // EPI_RESID_BF16, both operands MN-major
 // whether launch_gemm_tc accepts EPI_DELTA_BF16 for this product (tile shape and alignment allow
 // a thread to own whole heads of its row); otherwise the caller runs launch_attn_delta
 bool gemm_tc_fuses_delta(const GemmArgs& g);

@@ -80,12 +80,20 @@ struct TcParams {
   int wide;   // every output / auxiliary row start is 32-byte aligned: use 32-byte accesses
   int rope_S, rope_dh, rope_cols;
   void* C3; long long ldc3; int c3_lo, c3_hi;
+  float piece_scale; float2* piece_stats; long long ld_pieces;
 };
 
+// what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of the
+// two that have instantiations of their own so that drain_cols keeps its registers
+enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_RESID_BF16 = 2 };
+
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
-bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows);
+bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows,
+                bool transient = false);
 TcParams make_params(const GemmArgs& g);
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st);   // bn: 256 or 128
+int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st);
+int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
 
 // Drains rows [m0 + 32 quarter, +32) x columns [n0 + half BN/2, + BN/2) of the accumulator at
 // TMEM column t_acc through registers into global memory, applying the epilogue p.epilogue.
@@ -284,10 +292,105 @@ __device__ __forceinline__ void drain_cols(const TcParams& p, int m0, int n0, in
   }
 }
 
-template <int BN>
-__device__ __forceinline__ void drain_tile(const TcParams& p, int m0, int n0, int sp, uint32_t t_acc,
-                                           int quarter, int half, int lane) {
-  drain_cols(p, m0, n0, sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+__device__ __forceinline__ float ex2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// EPI_PIECES.  A lane holds 64 logits of its row at a time: x = acc * piece_scale (the scale holds
+// log2(e) and the temperature), m = max x, e = 2^(x - m).  The powers are stored in bf16 - a relative
+// rounding of half a step (2^-8) whatever the logit, where a bf16 logit of 16 would be off by 2^-4 absolutely -
+// and {m, sum e} in fp32, the sum over the unrounded powers, so the log-sum-exp keeps fp32 accuracy.
+// The exponent is one fused multiply-add on the accumulator; m is the rounded product used in it,
+// so its rounding cancels between the sum and the maximum.
+__device__ __forceinline__ void drain_pieces(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
+                                             int c_begin, int c_end, int lane) {
+  const int m = m0 + quarter * 32 + lane;
+  const bool row_ok = m < p.M;
+  const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += PIECE) {
+    const int nb = n0 + c0;
+    if (nb >= p.N) break;                  // warp-uniform
+    uint32_t r[PIECE];
+    tmem_ld32(t_row + c0, r);
+    tmem_ld32(t_row + c0 + 32, r + 32);
+    tmem_ld_wait();
+    if (nb + PIECE > p.N) {                // columns past the vocabulary: nothing
+#pragma unroll
+      for (int j = 0; j < PIECE; ++j)
+        if (nb + j >= p.N) r[j] = 0xff800000u;
+    }
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < PIECE; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
+    float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.piece_scale;
+    if (top == -INFINITY) top = 0.f;       // (a piece of -inf logits: all powers are 0)
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < PIECE; ++j) {
+      const float e = ex2_fast(fmaf(__uint_as_float(r[j]), p.piece_scale, -top));
+      sum[j & 3] += e;
+      r[j] = __float_as_uint(e);
+    }
+    if (row_ok) {
+      p.piece_stats[(long long)m * p.ld_pieces + nb / PIECE] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+      if (p.C) {
+        bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t o[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) o[q] = pack2_bf16(__uint_as_float(r[16 * j + 2 * q]), __uint_as_float(r[16 * j + 2 * q + 1]));
+          st_v8(dst + 16 * j, o);
+        }
+      }
+    }
+  }
+}
+
+// EPI_RESID_BF16: the last partial sum of an fp32 running total, rounded once.  N is a multiple of 8,
+// aux rows are 32-byte aligned, output rows 16-byte aligned.
+__device__ __forceinline__ void drain_resid_bf16(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
+                                                 int c_begin, int c_end, int lane) {
+  const int m = m0 + quarter * 32 + lane;
+  const bool row_ok = m < p.M;
+  const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+    const int nb = n0 + c0;
+    if (nb >= p.N) break;                  // warp-uniform
+    uint32_t r[32], x[32];
+    tmem_ld32(t_row + c0, r);
+    const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb;
+    if (row_ok) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (nb + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
+    }
+    tmem_ld_wait();
+    if (row_ok) {
+      bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (nb + 8 * j < p.N) {
+          float f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(x[8 * j + q]) + __uint_as_float(r[8 * j + q]);
+          *reinterpret_cast<uint4*>(dst + 8 * j) = pack8_bf16(f);
+        }
+      }
+    }
+  }
+}
+
+template <int MODE>
+__device__ __forceinline__ void drain_mode(const TcParams& p, int m0, int n0, int sp, uint32_t t_acc, int quarter,
+                                           int c_begin, int c_end, int lane) {
+  if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else if constexpr (MODE == DRAIN_RESID_BF16) drain_resid_bf16(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
 
 }  // namespace gemm_tc_detail

@@ -31,7 +31,7 @@ template <int BN> struct Cfg {
   static constexpr int TMEM_COLS = 2 * BN;
 };
 
-template <int BN, bool A_K, bool B_K>
+template <int BN, bool A_K, bool B_K, int MODE>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const TcParams p) {
@@ -154,7 +154,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
       const int m0 = (t2 % p.tiles_m) * BM, n0 = (t2 / p.tiles_m) * BN;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_tile<BN>(p, m0, n0, sp, tmem_base + (uint32_t)(acc * BN), quarter, half, lane);
+      drain_mode<MODE>(p, m0, n0, sp, tmem_base + (uint32_t)(acc * BN), quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
@@ -202,9 +202,9 @@ constexpr size_t MAP_CACHE_LIMIT = 1 << 16;
 using namespace mapcache;
 
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K,
-                int box_rows) {
+                int box_rows, bool transient) {
   const MapKey key{base, ld, kmajor ? 1 : 0, rows, K, box_rows};
-  {
+  if (!transient) {
     std::lock_guard<std::mutex> lk(g_maps_lock);
     auto it = g_maps.find(key);
     if (it != g_maps.end()) { *map = it->second; return true; }
@@ -225,6 +225,7 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
                         estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return false;
+  if (transient) return true;
   std::lock_guard<std::mutex> lk(g_maps_lock);
   if (g_maps.size() >= MAP_CACHE_LIMIT) g_maps.clear();
   g_maps.emplace(key, *map);
@@ -238,6 +239,7 @@ TcParams make_params(const GemmArgs& g) {
   p.C = g.C; p.ldc = g.ldc; p.C2 = g.C2; p.aux = g.aux; p.ldaux = g.ldaux; p.flags = g.flags;
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
+  p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes
@@ -253,14 +255,14 @@ TcParams make_params(const GemmArgs& g) {
 }  // namespace gemm_tc_detail
 
 namespace {
-template <int BN, bool A_K, bool B_K>
+template <int BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_t(const GemmArgs& g, cudaStream_t st) {
   using C = Cfg<BN>;
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K>, C::SMEM)) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM)) return -1;
   CUtensorMap mapA, mapB;
-  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, BM)) return -2;
-  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN)) return -2;
+  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, BM, g.transient)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN, g.transient)) return -2;
   TcParams p = make_params(g);
   p.tiles_m = (g.M + BM - 1) / BM;
   p.tiles_n = (g.N + BN - 1) / BN;
@@ -270,7 +272,7 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
   const int n_sm = ppu_sm_count();
   const int grid = tiles < n_sm ? tiles : n_sm;
-  gemm_tc_kernel<BN, A_K, B_K><<<grid, GEMM_THREADS, C::SMEM, st>>>(mapA, mapB, p);
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, C::SMEM, st>>>(mapA, mapB, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -339,4 +341,33 @@ int launch_gemm_tc(const GemmArgs& g, cudaStream_t st) {
   const long long tiles256 = (long long)((g.M + BM - 1) / BM) * ((g.N + 255) / 256) * (g.splits > 1 ? g.splits : 1);
   if (g.N > 128 && tiles256 >= ppu_sm_count()) return launch_bn<256>(g, st);
   return launch_bn<128>(g, st);
+}
+
+namespace {
+bool operands_ok(const GemmArgs& g) {
+  return !((g.lda % 8) || (g.ldb % 8) || (reinterpret_cast<uintptr_t>(g.A) & 15) || (reinterpret_cast<uintptr_t>(g.B) & 15));
+}
+}  // namespace
+
+int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st) {
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
+  if (gemm_tc_init() != 0) return -1;
+  if (!operands_ok(g) || !g.a_kmajor || !g.b_kmajor || g.splits > 1 || !g.piece_stats ||
+      (g.C && ((g.ldc % PIECE) || (reinterpret_cast<uintptr_t>(g.C) & 31))))
+    return -4;
+  const TcParams p = make_params(g);
+  if (picks_pair256(g)) return launch_gemm_tc_pair_pieces(g, p, st);
+  const long long tiles256 = (long long)((g.M + BM - 1) / BM) * ((g.N + 255) / 256);
+  if (g.N > 128 && tiles256 >= ppu_sm_count()) return launch_t<256, true, true, DRAIN_PIECES>(g, st);
+  return launch_t<128, true, true, DRAIN_PIECES>(g, st);
+}
+
+int launch_gemm_tc_resid_bf16(const GemmArgs& g, cudaStream_t st) {
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
+  if (gemm_tc_init() != 0) return -1;
+  if (!operands_ok(g) || g.a_kmajor || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || (g.ldaux % 8) || !g.aux ||
+      (reinterpret_cast<uintptr_t>(g.C) & 15) || (reinterpret_cast<uintptr_t>(g.aux) & 31))
+    return -4;
+  if (picks_pair256(g)) return launch_gemm_tc_pair_resid_bf16(g, make_params(g), st);
+  return launch_t<128, false, false, DRAIN_RESID_BF16>(g, st);
 }

@@ -113,7 +113,7 @@ __device__ __forceinline__ PairUnit pair_unit(const TcParams& p, int u, int num_
 }
 
 // mapB2: B with a box of 64 rows (the narrow units of a K-major B); otherwise a copy of mapB
-template <int PAIR_BN, bool A_K, bool B_K>
+template <int PAIR_BN, bool A_K, bool B_K, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                     const __grid_constant__ CUtensorMap mapB2, const TcParams p) {
@@ -248,8 +248,8 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_cols(p, m0, w.n0, w.sp, tmem_base + (uint32_t)(acc * PAIR_BN), quarter, half * (w.bn / 2),
-                 (half + 1) * (w.bn / 2), lane);
+      drain_mode<MODE>(p, m0, w.n0, w.sp, tmem_base + (uint32_t)(acc * PAIR_BN), quarter, half * (w.bn / 2),
+                       (half + 1) * (w.bn / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
@@ -270,13 +270,13 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   }
 }
 
-template <int PAIR_BN, bool A_K, bool B_K>
+template <int PAIR_BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K>, PairCfg<PAIR_BN>::SMEM)) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM)) return -1;
   CUtensorMap mapA, mapB, mapB2;
-  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128)) return -2;
-  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2)) return -2;
+  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient)) return -2;
   TcParams p = p0;
   p.tiles_m = (g.M + 255) / 256;
   p.tiles_n = (g.N + PAIR_BN - 1) / PAIR_BN;
@@ -308,8 +308,8 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
     pairs = max_pairs;
   }
   mapB2 = mapB;
-  if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64)) return -2;
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K><<<2 * pairs, GEMM_THREADS, PairCfg<PAIR_BN>::SMEM, st>>>(mapA, mapB, mapB2, p);
+  if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, PairCfg<PAIR_BN>::SMEM, st>>>(mapA, mapB, mapB2, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -328,5 +328,11 @@ int launch_pair_bn(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
 namespace gemm_tc_detail {
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st) {
   return bn == 128 ? launch_pair_bn<128>(g, p, st) : launch_pair_bn<256>(g, p, st);
+}
+int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
+  return launch_pair_t<256, true, true, DRAIN_PIECES>(g, p, st);
+}
+int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
+  return launch_pair_t<256, false, false, DRAIN_RESID_BF16>(g, p, st);
 }
 }  // namespace gemm_tc_detail

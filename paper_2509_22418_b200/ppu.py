@@ -344,3 +344,191 @@ def ppu_attention_bwd_static(qkv, U, lse, dU, batch, seq, n_head, d_head, backen
                                           C.c_void_p(dqkv.data_ptr()), batch, seq, n_head, d_head,
                                           backend, C.c_void_p(st)))
     return dqkv
+
+
+# ---- losses of hidden states against the vocabulary ------------------------------------------
+MAX_TEACHER_ENTRIES = 128
+NORM_LAYER, NORM_RMS = 0, 1
+
+
+def _need(ok, what):
+    if not ok:
+        raise PpuError(-1, what)
+
+
+def _tensor(t, name, dtype, shape, like=None, rows=False):
+    """Checks a device tensor; rows: the rows may be strided, otherwise it is contiguous."""
+    import torch
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
+    _need(t.dtype == dtype, f"{name} must be {dtype}, got {t.dtype}")
+    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    _need(like is None or t.device == like.device, f"{name} is on {t.device}, the others on {None if like is None else like.device}")
+    if not rows:
+        _need(t.is_contiguous(), f"{name} must be contiguous")
+    elif t.numel():
+        _need(t.shape[1] == 1 or t.stride(1) == 1, f"{name}: the values of a row must be adjacent")
+        _need(t.shape[0] == 1 or t.stride(0) >= t.shape[1], f"{name}: rows overlap")
+    return t
+
+
+def _ptr(t):
+    return C.c_void_p(None if t is None or t.numel() == 0 else t.data_ptr())
+
+
+def _row_stride(t):
+    return C.c_int64(t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _workspace(nbytes, device, given):
+    import torch
+    if given is not None:
+        _need(given.is_cuda and given.device == device and given.dtype == torch.uint8 and given.is_contiguous(),
+              "workspace must be a contiguous uint8 tensor on the operands' device")
+        return given
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
+    """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE)."""
+    n = C.c_size_t(0)
+    _check(lib().ppu_head_query_bytes(T, d, V, grads, chunk_rows, C.byref(n)))
+    return n.value
+
+
+def _head(call, X, E, row_weight, grad, chunk_rows, workspace, flags, targets):
+    """Outputs, workspace and the call of a head loss.  targets(T): its middle arguments."""
+    import torch
+    _need(isinstance(X, torch.Tensor) and X.is_cuda and X.dim() == 2, "X must be a CUDA tensor [T, d]")
+    _need(isinstance(E, torch.Tensor) and E.dim() == 2, "E must be a CUDA tensor [V, d]")
+    T, d, V = X.shape[0], X.shape[1], E.shape[0]
+    _tensor(X, "X", torch.bfloat16, (T, d), rows=True)
+    _tensor(E, "E", torch.bfloat16, (V, d), X, rows=True)
+    if row_weight is not None:
+        _tensor(row_weight, "row_weight", torch.float32, (T,), X)
+    if flags is not None:
+        _tensor(flags, "flags", torch.int32, (8,), X)
+    want_x, want_e = (bool(grad), bool(grad)) if not isinstance(grad, str) else ("x" in grad, "e" in grad)
+    middle = targets(T, X)
+    with torch.cuda.device(X.device):
+        nbytes = ppu_head_query_bytes(T, d, V, want_x + 2 * want_e, chunk_rows)
+        ws = _workspace(nbytes, X.device, workspace)
+        f32 = dict(dtype=torch.float32, device=X.device)
+        loss, row_loss, lse = torch.empty((), **f32), torch.empty(T, **f32), torch.empty(T, **f32)
+        dX = torch.empty((T, d), dtype=torch.bfloat16, device=X.device) if want_x else None
+        dE = torch.empty((V, d), dtype=torch.bfloat16, device=X.device) if want_e else None
+        st = torch.cuda.current_stream(X.device).cuda_stream
+        _check(call(_ptr(X), _row_stride(X), _ptr(E), _row_stride(E), *middle, _ptr(row_weight), T, d, V, _ptr(loss),
+                    _ptr(row_loss), _ptr(lse), _ptr(dX), C.c_int64(d), _ptr(dE), C.c_int64(d), chunk_rows,
+                    C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), _ptr(flags), C.c_void_p(st)))
+    return loss, row_loss, lse, dX, dE
+
+
+def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, workspace=None, flags=None):
+    """Softmax cross entropy of hidden states X [T, d] against the vocabulary matrix E [V, d] (bf16;
+    rows may be strided), without the logits.  target: int32 [T], negative: the row does not
+    count.  row_weight: fp32 [T], or None for the mean over the rows that count.  grad: True, False, or "x" /
+    "e" for one gradient only (E frozen, X frozen).  Returns (loss, row_loss [T], lse [T], dX, dE).
+    flags: int32 [8] zeros for ppu_op_status."""
+    import torch
+
+    def targets(T, like):
+        return (_ptr(_tensor(target, "target", torch.int32, (T,), like)),)
+    return _head(lib().ppu_head_xent, X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+
+
+def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher_lse=None, row_weight=None,
+                     grad=True, chunk_rows=0, workspace=None, flags=None):
+    """Distillation of X [T, d], E [V, d] (bf16) from a teacher's top logits: teacher_ids int32 [T, k]
+    (negative: absent) and teacher_logits fp32 [T, k]; teacher_lse fp32 [T]: the log-sum-exp of all of the
+    teacher's logits / temperature, or None for the softmax over the k entries.  Loss and gradients are those of
+    sum_j q_j (log q_j - log p_j); multiply row_weight by temperature ** 2 for gradients of the
+    same size at every temperature.  The rest as ppu_head_xent."""
+    import torch
+
+    def targets(T, like):
+        _need(isinstance(teacher_ids, torch.Tensor) and teacher_ids.dim() == 2, "teacher_ids must be a CUDA tensor [T, k]")
+        k = teacher_ids.shape[1]
+        _tensor(teacher_ids, "teacher_ids", torch.int32, (T, k), like, rows=True)
+        _tensor(teacher_logits, "teacher_logits", torch.float32, (T, k), like, rows=True)
+        if teacher_lse is not None:
+            _tensor(teacher_lse, "teacher_lse", torch.float32, (T,), like)
+        return (_ptr(teacher_ids), _row_stride(teacher_ids), _ptr(teacher_logits), _row_stride(teacher_logits), k,
+                _ptr(teacher_lse), C.c_float(temperature))
+    return _head(lib().ppu_head_distill, X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+
+
+def ppu_op_status(flags) -> None:
+    """Waits for the current stream; raises what a call given `flags` (int32 [8], zeros at first) reported."""
+    import torch
+    _tensor(flags, "flags", torch.int32, (8,))
+    with torch.cuda.device(flags.device):
+        _check(lib().ppu_op_status(_ptr(flags), C.c_void_p(torch.cuda.current_stream(flags.device).cuda_stream)))
+
+
+# ---- norms before and after a block, with its gate and the residual scale --------------------
+_KINDS = {"layer": NORM_LAYER, "rms": NORM_RMS}
+
+
+def _norm_operands(y, r, gate, gate_rows, vectors, kind):
+    import torch
+    _need(isinstance(y, torch.Tensor) and y.is_cuda and y.dim() == 2, "y must be a CUDA tensor [T, d]")
+    _need(kind in _KINDS, f"kind must be one of {sorted(_KINDS)}")
+    T, d = y.shape
+    _tensor(y, "y", torch.bfloat16, (T, d))
+    _tensor(r, "r", torch.float32, (T, d), y)
+    for name, v in vectors.items():
+        if v is not None:
+            _tensor(v, name, torch.float32, (d,), y)
+    if gate is not None:
+        gate_rows = gate_rows or max(T, 1)
+        _need(gate_rows >= 1, "gate_rows must be positive")
+        _tensor(gate, "gate", torch.float32, (-(-T // gate_rows), d), y)
+    return T, d, gate_rows if gate is not None else 0
+
+
+def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None, gate=None, gate_rows=0,
+                      kind="layer", res_scale=1.0, eps=1e-5, in_place=False):
+    """n = N(y) post_gain + post_shift; r_out = res_scale r + gate n; h = N(r_out) pre_gain + pre_shift for
+    a block's output y [T, d] (bf16) and the residual stream r [T, d] (fp32); kind "layer" or "rms";
+    gate fp32 [ceil(T / gate_rows), d] (gate_rows 0: one row for all).  in_place: r_out is r.
+    Returns (r_out fp32, h bf16, stats fp32 [T, 4])."""
+    import torch
+    T, d, gate_rows = _norm_operands(y, r, gate, gate_rows, {"post_gain": post_gain, "pre_gain": pre_gain, "post_shift": post_shift,
+                                                             "pre_shift": pre_shift}, kind)
+    with torch.cuda.device(y.device):
+        r_out = r if in_place else torch.empty_like(r)
+        h = torch.empty_like(y)
+        stats = torch.empty((T, 4), dtype=torch.float32, device=y.device)
+        st = torch.cuda.current_stream(y.device).cuda_stream
+        _check(lib().ppu_norm_gate_fwd(_ptr(y), _ptr(r), _ptr(gate), gate_rows, _ptr(post_gain), _ptr(post_shift),
+                                       _ptr(pre_gain), _ptr(pre_shift), _KINDS[kind], C.c_float(res_scale), C.c_float(eps),
+                                       _ptr(r_out), _ptr(h), _ptr(stats), T, d, C.c_void_p(st)))
+    return r_out, h, stats
+
+
+def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift=None, pre_shift=None, gate=None,
+                      gate_rows=0, kind="layer", res_scale=1.0, workspace=None):
+    """Gradients of ppu_norm_gate_fwd from dh [T, d] (bf16) and dr_out [T, d] (fp32, or None), with the saved
+    r_out and stats.  Returns (dy bf16, dr fp32, dpost_gain, dpost_shift, dpre_gain, dpre_shift,
+    dgate); those of absent operands are None."""
+    import torch
+    T, d, gate_rows = _norm_operands(y, r_out, gate, gate_rows, {"post_gain": post_gain, "pre_gain": pre_gain, "post_shift": post_shift,
+                                                                 "pre_shift": pre_shift}, kind)
+    _tensor(dh, "dh", torch.bfloat16, (T, d), y)
+    if dr_out is not None:
+        _tensor(dr_out, "dr_out", torch.float32, (T, d), y)
+    _tensor(stats, "stats", torch.float32, (T, 4), y)
+    with torch.cuda.device(y.device):
+        n = C.c_size_t(0)
+        _check(lib().ppu_norm_gate_query_bytes(T, d, gate_rows, C.byref(n)))
+        ws = _workspace(n.value, y.device, workspace)
+        dy, dr = torch.empty_like(y), torch.empty_like(r_out)
+        vec = lambda like: None if like is None else torch.empty(d, dtype=torch.float32, device=y.device)  # noqa: E731
+        dg1, db1, dg2, db2 = vec(post_gain), vec(post_shift), vec(pre_gain), vec(pre_shift)
+        dgate = None if gate is None else torch.empty_like(gate)
+        st = torch.cuda.current_stream(y.device).cuda_stream
+        _check(lib().ppu_norm_gate_bwd(_ptr(dh), _ptr(dr_out), _ptr(y), _ptr(r_out), _ptr(stats), _ptr(gate), gate_rows,
+                                       _ptr(post_gain), _ptr(post_shift), _ptr(pre_gain), _KINDS[kind], C.c_float(res_scale),
+                                       _ptr(dy), _ptr(dr), _ptr(dg1), _ptr(db1), _ptr(dg2), _ptr(db2), _ptr(dgate), T, d,
+                                       C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), C.c_void_p(st)))
+    return dy, dr, dg1, db1, dg2, db2, dgate
