@@ -11,12 +11,14 @@
 //   dgate = sum G n   dg1 = sum gate G yhat   db1 = sum gate G   dg2 = sum dh rhat   db2 = sum dh
 //
 // Both passes read each input once and write each output once: 12 and 18 bytes per element, so HBM
-// bounds them.  A "unit" of 8 to 512 threads owns a contiguous range of rows; a thread owns 8 columns
-// of all of them.  So gains, shifts and gate stay in registers over the rows, and the five parameter
-// sums of the backward pass are running sums in registers, written once per unit and added in a fixed
-// order by a second small kernel (no atomics).  Rows arrive through a ring of cp.async copies in shared
-// memory, three rows ahead: a unit works on one row at a time and would otherwise wait for each.
-// A unit's threads meet at a barrier of their own, so a block may hold several units (short rows).
+// bounds them.  A "unit" of LANES threads owns a contiguous range of rows; a thread owns CH chunks of 4
+// columns of all of them (16 bytes of fp32, 8 of bf16: neighbours are adjacent in both).  So gains,
+// shifts and gate stay in registers over the rows, and the parameter sums of the backward pass are
+// running sums in registers, written once per unit and added in a fixed order by a second small kernel
+// (no atomics).  Rows arrive through a ring of cp.async copies in shared memory: a unit works on one row at a
+// time, two to four sums over its threads one after the other, and loads for it would wait as long again.
+// LANES is a compile-time constant: with the loops over lanes and warps left to run time the same
+// kernel issued 675 instructions per warp and row and took 84 us where it now takes FWD_US (8192 x 2048).
 #include <algorithm>
 #include "../../include/ppu.h"
 #include "common.cuh"
@@ -26,11 +28,7 @@ int ppu_fail(int code, const char* fmt, ...);
 namespace {
 
 constexpr int MAX_D = 4096;
-// rows in flight of a unit: with two blocks of 256 threads on an SM (one of 512) what fits its shared memory
-template <bool BWD, int GATE> struct Ring {
-  static constexpr int BYTES = (BWD ? 96 : 48) + (GATE == 2 ? 32 : 0);   // per thread and row
-  static constexpr int STAGES = BWD && GATE == 2 ? 3 : 4;
-};
+constexpr int FWD_CH = 4, BWD_CH = 2;         // the backward pass has its running sums beside the row
 
 struct NormArgs {
   const bf16 *y, *dh;
@@ -39,340 +37,395 @@ struct NormArgs {
   float* r_out; bf16 *h, *dy; float* dr_out;
   float4* stats;                     // {mean1, rstd1, mean2, rstd2} per row
   float scale, eps;
-  int T, d, gate_rows;
+  int T, d, gate_rows, layer;
   int deal_rows;                     // rows dealt to the units as one (1, or the rows of a group)
-  int tpr;                           // threads of a unit
   int units;
   int per_group;                     // units that share a group of gate rows (0: units own whole groups / plain rows)
   float* partial;                    // [5][units][d]: dg1, db1, dg2, db2, dgate
   float* dgate;
 };
 
-__device__ __forceinline__ void cp16(void* smem, const void* gmem) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem)
-               : "memory");
+__device__ __forceinline__ void cp16(uint32_t smem, const void* gmem) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
+}
+__device__ __forceinline__ void cp8(uint32_t smem, const void* gmem) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem), "l"(gmem) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ void bf8(const void* p, float* f) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const __nv_bfloat162* q = reinterpret_cast<const __nv_bfloat162*>(&u);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 t = __bfloat1622float2(q[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
+__device__ __forceinline__ void from_bf4(const uint2& u, float* f) {
+  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
+  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
+  f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
 }
-__device__ __forceinline__ void put_bf8(bf16* p, const float* f) {
-  uint4 u;
-  __nv_bfloat162* q = reinterpret_cast<__nv_bfloat162*>(&u);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-  *reinterpret_cast<uint4*>(p) = u;
+__device__ __forceinline__ uint2 to_bf4(const float* f) {
+  __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+  return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
-__device__ __forceinline__ void f8(const float* p, float* f) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void put_f8(float* p, const float* f) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
+__device__ __forceinline__ void from_f4(const float4& v, float* f) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+__device__ __forceinline__ float4 to_f4(const float* f) { return make_float4(f[0], f[1], f[2], f[3]); }
+
+// how the threads of a block make up units
+template <int LANES> struct Layout {
+  static constexpr int UNITS = LANES <= 32 ? 128 / LANES : LANES <= 128 ? (LANES == 96 ? 1 : 128 / LANES) : 1;   // units in a block
+  static constexpr int BLOCK = LANES * UNITS;
+  static constexpr int WARPS = LANES > 32 ? LANES / 32 : 1;
+};
 
 // Sums of a unit's threads.  Within a warp by shuffles; a unit of several warps then through shared
 // memory and the unit's own named barrier.  Two buffers in turn: a thread that is back for the next sum
 // writes the other one, and the one after that lies behind a barrier that all readers of this have passed.
-struct UnitSum {
-  float2* buf;                      // [2][16] of this unit
-  int tpr, bar, lane, warp, turn;
-  __device__ float2 operator()(float2 v) {
+template <int LANES, int N> struct UnitSum {
+  static constexpr int W = Layout<LANES>::WARPS;
+  float* buf;                       // [2][W][N] of this unit
+  int bar, lane, warp, turn;
+  __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      if (o < tpr) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-      }
-    if (tpr <= 32) return v;
-    float2* b = buf + 16 * turn;
-    turn ^= 1;
-    if (lane == 0) b[warp] = v;
-    asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(tpr) : "memory");
-    float2 s = b[0];
-    for (int w = 1; w < (tpr >> 5); ++w) { s.x += b[w].x; s.y += b[w].y; }
-    return s;
+    for (int o = LANES < 32 ? LANES / 2 : 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if constexpr (W > 1) {
+      float* b = buf + turn;
+      turn ^= W * N;
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) b[warp * N + i] = v[i];
+      asm volatile("bar.sync %0, %1;" ::"r"(bar), "n"(LANES) : "memory");
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += b[w * N + i];
+    }
   }
 };
 
 // where a unit's threads stand and which rows are its own
 struct Unit {
   int tid, unit;                    // thread of the unit, index of the unit
-  int64_t lo, hi;                   // rows
+  int lo, hi;                       // rows
   int group;                        // gate row of all of them (units that share a group)
 };
+template <int LANES>
 __device__ __forceinline__ Unit my_unit(const NormArgs& a) {
   Unit u;
-  u.tid = threadIdx.x % a.tpr;
-  u.unit = blockIdx.x * (blockDim.x / a.tpr) + threadIdx.x / a.tpr;
-  u.group = 0;
-  if (u.unit >= a.units) { u.lo = u.hi = 0; return u; }
+  u.tid = threadIdx.x % LANES;
+  u.unit = blockIdx.x * Layout<LANES>::UNITS + threadIdx.x / LANES;
+  u.group = u.lo = u.hi = 0;
+  if (u.unit >= a.units) return u;
   if (a.per_group > 0) {            // a share of one group's rows
     u.group = u.unit / a.per_group;
-    const int part = u.unit % a.per_group;
-    const int64_t g0 = (int64_t)u.group * a.gate_rows, n = min((int64_t)a.gate_rows, a.T - g0);
-    u.lo = g0 + n * part / a.per_group;
-    u.hi = g0 + n * (part + 1) / a.per_group;
+    const int part = u.unit % a.per_group, g0 = u.group * a.gate_rows;
+    const int64_t n = min(a.gate_rows, a.T - g0);
+    u.lo = g0 + (int)(n * part / a.per_group);
+    u.hi = g0 + (int)(n * (part + 1) / a.per_group);
   } else {                          // whole groups (of one row where there is no sum over a group)
     const int64_t rows = a.deal_rows, groups = (a.T + rows - 1) / rows;
-    u.lo = groups * u.unit / a.units * rows;
-    u.hi = min(groups * (u.unit + 1) / a.units * rows, (int64_t)a.T);
+    u.lo = (int)(groups * u.unit / a.units * rows);
+    u.hi = (int)min(groups * (u.unit + 1) / a.units * rows, (int64_t)a.T);
   }
   return u;
 }
+// rows that a unit's turns cover: threads of several units in a warp go on together, shuffles need all lanes
+template <int LANES> __device__ __forceinline__ int turns_of(const Unit& u) {
+  if constexpr (LANES < 32) return __reduce_max_sync(0xffffffffu, u.hi - u.lo);
+  return u.hi - u.lo;
+}
 
-// GATE: 0 none, 1 one row for all of the unit's rows, 2 read with each row
-template <bool LAYER, int GATE>
-__global__ void __launch_bounds__(MAX_D / 8) norm_gate_fwd_kernel(const NormArgs a) {
+// a vector's chunks of this thread
+template <int LANES, int CH>
+__device__ __forceinline__ void load_vector(const float* p, int tid, int d, float (&f)[CH][4]) {
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = 4 * (tid + LANES * c);
+    if (col < d) from_f4(*reinterpret_cast<const float4*>(p + col), f[c]);
+  }
+}
+
+// A row in flight: per thread and chunk 8 bytes of each bf16 and 16 of each fp32 operand.  A thread
+// copies and reads its own columns alone, so there is no barrier.
+template <bool BWD, int GATE, int CH> struct Ring {
+  static constexpr int NB = BWD ? 2 : 1, NF = (BWD ? 2 : 1) + (GATE == 2 ? 1 : 0);
+  static constexpr int BYTES = CH * (8 * NB + 16 * NF);      // per thread
+  static constexpr int STAGES = BWD && GATE == 2 ? 3 : 4;
+};
+
+// GATE: 0 none, 1 one row for all rows, 2 read with each row
+template <int LANES, int GATE>
+__global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
+  constexpr int CH = FWD_CH, BLOCK = Layout<LANES>::BLOCK;
+  using R = Ring<false, GATE, CH>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 s_sum[4][2 * 16];
-  const Unit u = my_unit(a);
-  const int lane = threadIdx.x & 31, slot = threadIdx.x / a.tpr;
-  UnitSum sum{s_sum[a.tpr > 32 ? slot : 0], a.tpr, 1 + slot, lane, (int)u.tid >> 5, 0};
-  const int col = u.tid * 8;
-  const bool on = col < a.d;
-  constexpr int BYTES = Ring<false, GATE>::BYTES, STAGES = Ring<false, GATE>::STAGES;   // y, r, gate
-  // a thread copies and reads its own 8 columns: no other thread's data, so no barrier
-  auto at = [&](int s, int off) { return smem + ((size_t)(s * BYTES + off) * blockDim.x); };
-  auto fetch = [&](int64_t t, int s) {
-    if (t < u.hi && on) {
-      const int64_t e = t * a.d + col;
-      cp16(at(s, 0) + 16 * threadIdx.x, a.y + e);
-      cp16(at(s, 16) + 16 * threadIdx.x, a.r + e);
-      cp16(at(s, 32) + 16 * threadIdx.x, a.r + e + 4);
+  __shared__ float s_sum[Layout<LANES>::UNITS][2 * Layout<LANES>::WARPS];
+  const Unit u = my_unit<LANES>(a);
+  const int slot = threadIdx.x / LANES;
+  UnitSum<LANES, 1> sum{s_sum[slot], 1 + slot, (int)threadIdx.x & 31, u.tid >> 5, 0};
+  bool on[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) on[c] = 4 * (u.tid + LANES * c) < a.d;
+  // stage s: [NF * CH][BLOCK] of 16 bytes (r, then the gate), then [CH][BLOCK] of 8 bytes (y)
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem);
+  auto f_off = [&](int s, int i) { return s * (R::BYTES * BLOCK) + (i * BLOCK + (int)threadIdx.x) * 16; };
+  auto b_off = [&](int s, int i) { return s * (R::BYTES * BLOCK) + R::NF * CH * BLOCK * 16 + (i * BLOCK + (int)threadIdx.x) * 8; };
+  auto fetch = [&](int t, int s) {
+    if (t < u.hi) {
+      const int64_t e = (int64_t)t * a.d + 4 * u.tid;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (on[c]) {
+          cp8(ring + b_off(s, c), a.y + e + 4 * LANES * c);
+          cp16(ring + f_off(s, c), a.r + e + 4 * LANES * c);
+        }
       if (GATE == 2) {
-        const float* g = a.gate + t / a.gate_rows * a.d + col;
-        cp16(at(s, 48) + 16 * threadIdx.x, g);
-        cp16(at(s, 64) + 16 * threadIdx.x, g + 4);
+        const float* g = a.gate + (int64_t)(t / a.gate_rows) * a.d + 4 * u.tid;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) if (on[c]) cp16(ring + f_off(s, CH + c), g + 4 * LANES * c);
       }
     }
     cp_commit();
   };
-  for (int s = 0; s < STAGES - 1; ++s) fetch(u.lo + s, s);
-  float g1[8] = {}, b1[8] = {}, g2[8] = {}, b2[8] = {};
-  if (on && u.lo < u.hi) {
-    f8(a.g1 + col, g1);
-    if (a.b1) f8(a.b1 + col, b1);
-    f8(a.g2 + col, g2);
-    if (a.b2) f8(a.b2 + col, b2);
-    if (GATE == 1) {
-      float gt[8];
-      f8(a.gate + col, gt);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { g1[j] *= gt[j]; b1[j] *= gt[j]; }
+  for (int s = 0; s < R::STAGES - 1; ++s) fetch(u.lo + s, s);
+  float g1[CH][4] = {}, b1[CH][4] = {}, g2[CH][4] = {}, b2[CH][4] = {};
+  if (u.lo < u.hi) {
+    load_vector<LANES>(a.g1, u.tid, a.d, g1);
+    if (a.b1) load_vector<LANES>(a.b1, u.tid, a.d, b1);
+    load_vector<LANES>(a.g2, u.tid, a.d, g2);
+    if (a.b2) load_vector<LANES>(a.b2, u.tid, a.d, b2);
+    if (GATE == 1) {
+      float gt[CH][4] = {};
+      load_vector<LANES>(a.gate, u.tid, a.d, gt);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { g1[c][j] *= gt[c][j]; b1[c][j] *= gt[c][j]; }
     }
   }
   const float inv_d = 1.f / a.d;
-  int s = 0;
-  // (units of one warp or less run as many turns as the longest of their warp: shuffles need all lanes)
-  int64_t turns = u.hi - u.lo;
-  if (a.tpr < 32) turns = __reduce_max_sync(0xffffffffu, (int)turns);
-  for (int64_t i = 0; i < turns; ++i) {
-    const int64_t t = u.lo + i;
-    const bool row = on && t < u.hi;
-    cp_wait<STAGES - 2>();
-    float y[8] = {}, r[8] = {}, gt[8];
-    if (row) {
-      bf8(at(s, 0) + 16 * threadIdx.x, y);
-      const float4 p = *reinterpret_cast<const float4*>(at(s, 16) + 16 * threadIdx.x);
-      const float4 q = *reinterpret_cast<const float4*>(at(s, 32) + 16 * threadIdx.x);
-      r[0] = p.x; r[1] = p.y; r[2] = p.z; r[3] = p.w; r[4] = q.x; r[5] = q.y; r[6] = q.z; r[7] = q.w;
-      if (GATE == 2) {
-        const float4 v = *reinterpret_cast<const float4*>(at(s, 48) + 16 * threadIdx.x);
-        const float4 w = *reinterpret_cast<const float4*>(at(s, 64) + 16 * threadIdx.x);
-        gt[0] = v.x; gt[1] = v.y; gt[2] = v.z; gt[3] = v.w; gt[4] = w.x; gt[5] = w.y; gt[6] = w.z; gt[7] = w.w;
-      }
+  // mean, then the squares about it: one pass over the squares alone would lose digits where the mean is large
+  auto moments = [&](const float (&x)[CH][4], float& mean, float& rstd) {
+    mean = 0.f;
+    if (a.layer) {
+      float v[1] = {0.f};
+#pragma unroll
+      for (int c = 0; c < CH; ++c) v[0] += (x[c][0] + x[c][1]) + (x[c][2] + x[c][3]);
+      sum(v);
+      mean = v[0] * inv_d;
     }
-    fetch(t + STAGES - 1, (s + STAGES - 1) % STAGES);
-    s = (s + 1) % STAGES;
-    // mean, then the squares about it: one pass over the squares alone would lose digits where the mean is large
-    auto moments = [&](const float* x, float& mean, float& rstd) {
-      mean = 0.f;
-      if (LAYER) {
-        float v = 0.f;
+    float v[1] = {0.f};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v += x[j];
-        mean = sum(make_float2(v, 0.f)).x * inv_d;
+    for (int c = 0; c < CH; ++c) {
+      float q = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { const float e = x[c][j] - mean; q = fmaf(e, e, q); }
+      if (on[c]) v[0] += q;
+    }
+    sum(v);
+    rstd = rsqrtf(v[0] * inv_d + a.eps);
+  };
+  const int turns = turns_of<LANES>(u);
+  int s = 0;
+  for (int i = 0; i < turns; ++i) {
+    const int t = u.lo + i;
+    const bool row = t < u.hi;
+    cp_wait<R::STAGES - 2>();
+    float y[CH][4] = {}, r[CH][4] = {}, gt[CH][4] = {};
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (on[c] && row) {
+        from_bf4(*reinterpret_cast<const uint2*>(smem + b_off(s, c)), y[c]);
+        from_f4(*reinterpret_cast<const float4*>(smem + f_off(s, c)), r[c]);
+        if (GATE == 2) from_f4(*reinterpret_cast<const float4*>(smem + f_off(s, CH + c)), gt[c]);
       }
-      float v = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) { const float e = x[j] - mean; v += e * e; }
-      rstd = rsqrtf(sum(make_float2(row ? v : 0.f, 0.f)).x * inv_d + a.eps);
-    };
+    fetch(t + R::STAGES - 1, s == 0 ? R::STAGES - 1 : s - 1);
+    s = s == R::STAGES - 1 ? 0 : s + 1;
     float m1, r1, m2, r2;
     moments(y, m1, r1);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float n = (y[j] - m1) * r1 * g1[j] + b1[j];
-      if (GATE == 2) n *= row ? gt[j] : 0.f;
-      r[j] = row ? fmaf(a.scale, r[j], n) : 0.f;
-    }
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float n = fmaf((y[c][j] - m1) * r1, g1[c][j], b1[c][j]);
+        if (GATE == 2) n *= gt[c][j];
+        r[c][j] = fmaf(a.scale, r[c][j], n);
+      }
+    // (columns past the row's end have zero gains and shifts: r' = 0 there)
     moments(r, m2, r2);
     if (row) {
-      const int64_t e = t * a.d + col;
-      put_f8(a.r_out + e, r);
+      const int64_t e = (int64_t)t * a.d + 4 * u.tid;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] = (r[j] - m2) * r2 * g2[j] + b2[j];
-      put_bf8(a.h + e, r);
+      for (int c = 0; c < CH; ++c)
+        if (on[c]) {
+          *reinterpret_cast<float4*>(a.r_out + e + 4 * LANES * c) = to_f4(r[c]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) r[c][j] = fmaf((r[c][j] - m2) * r2, g2[c][j], b2[c][j]);
+          *reinterpret_cast<uint2*>(a.h + e + 4 * LANES * c) = to_bf4(r[c]);
+        }
       if (u.tid == 0) a.stats[t] = make_float4(m1, r1, m2, r2);
     }
   }
 }
 
 // GATE: 0 none, 1 one row for all of the unit's rows, 2 read with each row, its gradient written at the end of each group
-template <bool LAYER, int GATE>
-__global__ void __launch_bounds__(MAX_D / 8) norm_gate_bwd_kernel(const NormArgs a) {
+template <int LANES, int GATE>
+__global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
+  constexpr int CH = BWD_CH, BLOCK = Layout<LANES>::BLOCK;
+  using R = Ring<true, GATE, CH>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float2 s_sum[4][2 * 16];
-  const Unit u = my_unit(a);
-  const int lane = threadIdx.x & 31, slot = threadIdx.x / a.tpr;
-  UnitSum sum{s_sum[a.tpr > 32 ? slot : 0], a.tpr, 1 + slot, lane, (int)u.tid >> 5, 0};
-  const int col = u.tid * 8;
-  const bool on = col < a.d;
-  constexpr int BYTES = Ring<true, GATE>::BYTES, STAGES = Ring<true, GATE>::STAGES;     // dh, y, r', dr', gate
-  auto at = [&](int s, int off) { return smem + ((size_t)(s * BYTES + off) * blockDim.x) + 16 * threadIdx.x; };
-  auto fetch = [&](int64_t t, int s) {
-    if (t < u.hi && on) {
-      const int64_t e = t * a.d + col;
-      cp16(at(s, 0), a.dh + e);
-      cp16(at(s, 16), a.y + e);
-      cp16(at(s, 32), a.r + e);
-      cp16(at(s, 48), a.r + e + 4);
-      if (a.dr) { cp16(at(s, 64), a.dr + e); cp16(at(s, 80), a.dr + e + 4); }
+  __shared__ float s_sum[Layout<LANES>::UNITS][2 * 2 * Layout<LANES>::WARPS];
+  const Unit u = my_unit<LANES>(a);
+  const int slot = threadIdx.x / LANES;
+  UnitSum<LANES, 2> sum{s_sum[slot], 1 + slot, (int)threadIdx.x & 31, u.tid >> 5, 0};
+  bool on[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) on[c] = 4 * (u.tid + LANES * c) < a.d;
+  // stage s: [NF * CH][BLOCK] of 16 bytes (r', dr', the gate), then [2 CH][BLOCK] of 8 bytes (dh, y)
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem);
+  auto f_off = [&](int s, int i) { return s * (R::BYTES * BLOCK) + (i * BLOCK + (int)threadIdx.x) * 16; };
+  auto b_off = [&](int s, int i) { return s * (R::BYTES * BLOCK) + R::NF * CH * BLOCK * 16 + (i * BLOCK + (int)threadIdx.x) * 8; };
+  auto fetch = [&](int t, int s) {
+    if (t < u.hi) {
+      const int64_t e = (int64_t)t * a.d + 4 * u.tid;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (on[c]) {
+          cp8(ring + b_off(s, c), a.dh + e + 4 * LANES * c);
+          cp8(ring + b_off(s, CH + c), a.y + e + 4 * LANES * c);
+          cp16(ring + f_off(s, c), a.r + e + 4 * LANES * c);
+          if (a.dr) cp16(ring + f_off(s, CH + c), a.dr + e + 4 * LANES * c);
+        }
       if (GATE == 2) {
-        const float* g = a.gate + t / a.gate_rows * a.d + col;
-        cp16(at(s, 96), g);
-        cp16(at(s, 112), g + 4);
+        const float* g = a.gate + (int64_t)(t / a.gate_rows) * a.d + 4 * u.tid;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) if (on[c]) cp16(ring + f_off(s, 2 * CH + c), g + 4 * LANES * c);
       }
     }
     cp_commit();
   };
-  auto get = [&](int s, int off, float* f) {
-    const float4 p = *reinterpret_cast<const float4*>(at(s, off)), q = *reinterpret_cast<const float4*>(at(s, off + 16));
-    f[0] = p.x; f[1] = p.y; f[2] = p.z; f[3] = p.w; f[4] = q.x; f[5] = q.y; f[6] = q.z; f[7] = q.w;
-  };
-  for (int s = 0; s < STAGES - 1; ++s) fetch(u.lo + s, s);
-  float gg[8] = {}, g2[8] = {};                              // gate g1 (g1 where the gate comes with each row)
-  if (on && u.lo < u.hi) {
-    f8(a.g1 + col, gg);
-    f8(a.g2 + col, g2);
-    if (GATE == 1) {
-      float gt[8];
-      f8(a.gate + (int64_t)u.group * a.d + col, gt);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) gg[j] *= gt[j];
+  for (int s = 0; s < R::STAGES - 1; ++s) fetch(u.lo + s, s);
+  float gg[CH][4] = {}, g2[CH][4] = {};                      // gate g1 (g1 where the gate comes with each row)
+  if (u.lo < u.hi) {
+    load_vector<LANES>(a.g1, u.tid, a.d, gg);
+    load_vector<LANES>(a.g2, u.tid, a.d, g2);
+    if (GATE == 1) {
+      float gt[CH][4] = {};
+      load_vector<LANES>(a.gate + (int64_t)u.group * a.d, u.tid, a.d, gt);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) gg[c][j] *= gt[c][j];
     }
   }
   // running sums: A = sum G yhat, B = sum G (of the group, where the gate comes with each row),
   // C = sum dh rhat, D = sum dh, and there PA, PB = sums of gate G yhat, gate G
-  float A[8] = {}, B[8] = {}, C[8] = {}, D[8] = {}, PA[8] = {}, PB[8] = {};
+  float A[CH][4] = {}, B[CH][4] = {}, C[CH][4] = {}, D[CH][4] = {}, PA[CH][4] = {}, PB[CH][4] = {};
   const float inv_d = 1.f / a.d;
+  const int turns = turns_of<LANES>(u);
   int s = 0;
-  int64_t turns = u.hi - u.lo;
-  if (a.tpr < 32) turns = __reduce_max_sync(0xffffffffu, (int)turns);
   float4 st = u.lo < u.hi ? a.stats[u.lo] : make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int64_t i = 0; i < turns; ++i) {
-    const int64_t t = u.lo + i;
-    const bool row = on && t < u.hi;
-    cp_wait<STAGES - 2>();
-    float dh[8] = {}, y[8] = {}, r[8] = {}, G[8] = {}, gt[8] = {};
-    if (row) {
-      bf8(at(s, 0), dh);
-      bf8(at(s, 16), y);
-      get(s, 32, r);
-      if (a.dr) get(s, 64, G);
-      if (GATE == 2) get(s, 96, gt);
-    }
-    fetch(t + STAGES - 1, (s + STAGES - 1) % STAGES);
-    s = (s + 1) % STAGES;
-    const float4 now = st;
+  for (int i = 0; i < turns; ++i) {
+    const int t = u.lo + i;
+    const bool row = t < u.hi;
+    cp_wait<R::STAGES - 2>();
+    // columns past the row's end, and turns past the unit's rows: zeros throughout
+    float dh[CH][4] = {}, y[CH][4] = {}, r[CH][4] = {}, G[CH][4] = {}, gt[CH][4] = {};
+    const float4 now = row ? st : make_float4(0.f, 0.f, 0.f, 0.f);
     if (t + 1 < u.hi) st = a.stats[t + 1];
-    float2 v = make_float2(0.f, 0.f);
+    float v[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      r[j] = (r[j] - now.z) * now.w;                          // rhat
-      if (row) { C[j] = fmaf(dh[j], r[j], C[j]); D[j] += dh[j]; }
-      dh[j] *= g2[j];
-      if (LAYER) v.x += dh[j];
-      v.y = fmaf(dh[j], r[j], v.y);
-    }
-    v = sum(v);
-    v.x *= inv_d; v.y *= inv_d;
-    float2 w = make_float2(0.f, 0.f);
+    for (int c = 0; c < CH; ++c)
+      if (on[c] && row) {
+        from_bf4(*reinterpret_cast<const uint2*>(smem + b_off(s, c)), dh[c]);
+        from_bf4(*reinterpret_cast<const uint2*>(smem + b_off(s, CH + c)), y[c]);
+        from_f4(*reinterpret_cast<const float4*>(smem + f_off(s, c)), r[c]);
+        if (a.dr) from_f4(*reinterpret_cast<const float4*>(smem + f_off(s, CH + c)), G[c]);
+        if (GATE == 2) from_f4(*reinterpret_cast<const float4*>(smem + f_off(s, 2 * CH + c)), gt[c]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x = fmaf(-r[j], v.y, dh[j]);
-      if (LAYER) x -= v.x;
-      G[j] = row ? fmaf(now.w, x, G[j]) : 0.f;
-      y[j] = (y[j] - now.x) * now.y;                          // yhat
-      A[j] = fmaf(G[j], y[j], A[j]);
-      B[j] += G[j];
-      float q = G[j] * gg[j];
-      if (GATE == 2) q *= gt[j];
-      if (LAYER) w.x += q;
-      w.y = fmaf(q, y[j], w.y);
-    }
-    w = sum(w);
-    w.x *= inv_d; w.y *= inv_d;
-    if (row) {
-      const int64_t e = t * a.d + col;
-      float o[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = a.scale * G[j];
-      put_f8(a.dr_out + e, o);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float q = G[j] * gg[j];
-        if (GATE == 2) q *= gt[j];
-        q = fmaf(-y[j], w.y, q);
-        if (LAYER) q -= w.x;
-        o[j] = now.y * q;
-      }
-      put_bf8(a.dy + e, o);
-      if (GATE == 2 && ((t + 1) % a.gate_rows == 0 || t + 1 == a.T)) {   // the group's last row
-        float b1[8] = {};
-        if (a.b1) f8(a.b1 + col, b1);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          o[j] = fmaf(gg[j], A[j], b1[j] * B[j]);
-          PA[j] = fmaf(gt[j], A[j], PA[j]);
-          PB[j] = fmaf(gt[j], B[j], PB[j]);
-          A[j] = B[j] = 0.f;
+        for (int j = 0; j < 4; ++j) {
+          r[c][j] = (r[c][j] - now.z) * now.w;                // rhat
+          y[c][j] = (y[c][j] - now.x) * now.y;                // yhat
+          C[c][j] = fmaf(dh[c][j], r[c][j], C[c][j]);
+          D[c][j] += dh[c][j];
+          dh[c][j] *= g2[c][j];
+          v[0] += dh[c][j];
+          v[1] = fmaf(dh[c][j], r[c][j], v[1]);
         }
-        put_f8(a.dgate + t / a.gate_rows * a.d + col, o);
       }
-    }
-  }
-  if (on && u.unit < a.units) {
-    const int64_t plane = (int64_t)a.units * a.d, e = (int64_t)u.unit * a.d + col;
-    if (GATE == 2) {
-      put_f8(a.partial + e, PA);
-      put_f8(a.partial + plane + e, PB);
-    } else if (GATE == 1) {
-      float gt[8], o[8], b1[8] = {};
-      f8(a.gate + (int64_t)u.group * a.d + col, gt);
-      f8(a.g1 + col, gg);
-      if (a.b1) f8(a.b1 + col, b1);
+    fetch(t + R::STAGES - 1, s == 0 ? R::STAGES - 1 : s - 1);
+    s = s == R::STAGES - 1 ? 0 : s + 1;
+    sum(v);
+    const float mean = a.layer ? v[0] * inv_d : 0.f, dot = v[1] * inv_d;
+    float w[2] = {0.f, 0.f};
+    const int64_t e = (int64_t)t * a.d + 4 * u.tid;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        o[j] = fmaf(gg[j], A[j], b1[j] * B[j]);
-        A[j] *= gt[j]; B[j] *= gt[j];
+    for (int c = 0; c < CH; ++c)
+      if (on[c] && row) {
+        float o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          G[c][j] = fmaf(now.w, fmaf(-r[c][j], dot, dh[c][j] - mean), G[c][j]);
+          o[j] = a.scale * G[c][j];
+          A[c][j] = fmaf(G[c][j], y[c][j], A[c][j]);
+          B[c][j] += G[c][j];
+          G[c][j] *= gg[c][j];
+          if (GATE == 2) G[c][j] *= gt[c][j];
+          w[0] += G[c][j];
+          w[1] = fmaf(G[c][j], y[c][j], w[1]);
+        }
+        *reinterpret_cast<float4*>(a.dr_out + e + 4 * LANES * c) = to_f4(o);
       }
-      put_f8(a.partial + e, A);
-      put_f8(a.partial + plane + e, B);
-      put_f8(a.partial + 4 * plane + e, o);
-    } else {
-      put_f8(a.partial + e, A);
-      put_f8(a.partial + plane + e, B);
+    sum(w);
+    const float mean1 = a.layer ? w[0] * inv_d : 0.f, dot1 = w[1] * inv_d;
+    const bool last = GATE == 2 && row && ((t + 1) % a.gate_rows == 0 || t + 1 == a.T);      // the group's last row
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (on[c] && row) {
+        float o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = now.y * fmaf(-y[c][j], dot1, G[c][j] - mean1);
+        *reinterpret_cast<uint2*>(a.dy + e + 4 * LANES * c) = to_bf4(o);
+        if (last) {
+          const int col = 4 * (u.tid + LANES * c);
+          float b1[4] = {};
+          if (a.b1) from_f4(*reinterpret_cast<const float4*>(a.b1 + col), b1);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            o[j] = fmaf(gg[c][j], A[c][j], b1[j] * B[c][j]);
+            PA[c][j] = fmaf(gt[c][j], A[c][j], PA[c][j]);
+            PB[c][j] = fmaf(gt[c][j], B[c][j], PB[c][j]);
+            A[c][j] = B[c][j] = 0.f;
+          }
+          *reinterpret_cast<float4*>(a.dgate + (int64_t)(t / a.gate_rows) * a.d + col) = to_f4(o);
+        }
+      }
+  }
+  if (u.unit >= a.units) return;
+  const int64_t plane = (int64_t)a.units * a.d;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if (!on[c]) continue;
+    const int col = 4 * (u.tid + LANES * c);
+    float* p = a.partial + (int64_t)u.unit * a.d + col;
+    if (GATE == 1) {
+      float gt[4], g1[4], b1[4] = {}, o[4];
+      from_f4(*reinterpret_cast<const float4*>(a.gate + (int64_t)u.group * a.d + col), gt);
+      from_f4(*reinterpret_cast<const float4*>(a.g1 + col), g1);
+      if (a.b1) from_f4(*reinterpret_cast<const float4*>(a.b1 + col), b1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[j] = fmaf(g1[j], A[c][j], b1[j] * B[c][j]);
+        A[c][j] *= gt[j];
+        B[c][j] *= gt[j];
+      }
+      *reinterpret_cast<float4*>(p + 4 * plane) = to_f4(o);
     }
-    put_f8(a.partial + 2 * plane + e, C);
-    put_f8(a.partial + 3 * plane + e, D);
+    *reinterpret_cast<float4*>(p) = to_f4(GATE == 2 ? PA[c] : A[c]);
+    *reinterpret_cast<float4*>(p + plane) = to_f4(GATE == 2 ? PB[c] : B[c]);
+    *reinterpret_cast<float4*>(p + 2 * plane) = to_f4(C[c]);
+    *reinterpret_cast<float4*>(p + 3 * plane) = to_f4(D[c]);
   }
 }
 
@@ -408,15 +461,19 @@ __global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* par
 // ---- host ---------------------------------------------------------------------------------------
 constexpr int SMS = 148;                      // work is split for a B200 (also where sizes are asked without a device)
 
-struct Shape { int tpr, block, units, per_group, blocks, gate_mode; size_t partial; };
-// threads per row, rows dealt to about 512 threads per SM (two blocks of 256)
+struct Shape { int lanes, units, per_group, gate_mode; size_t partial; };
+
+// threads of a unit: the fewest that hold a row, of the sizes that are compiled
+int lanes_for(int d, int ch) {
+  for (int l : {4, 8, 16, 32, 64, 96, 128, 192, 256}) if (4 * ch * l >= d) return l;
+  return 512;
+}
+// rows are dealt to about `threads` threads per SM
 Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
   Shape s;
-  const int need = d / 8;
-  s.tpr = 8;
-  if (need <= 32) while (s.tpr < need) s.tpr *= 2;
-  else s.tpr = (need + 31) / 32 * 32;
-  const int64_t target = std::min<int64_t>(16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * 512 / s.tpr));
+  s.lanes = lanes_for(d, backward ? BWD_CH : FWD_CH);
+  const int threads = backward ? 512 : 768;
+  const int64_t target = std::min<int64_t>(16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (threads / s.lanes)));
   const int64_t groups = has_gate ? ((int64_t)T + gate_rows - 1) / gate_rows : 1;
   s.per_group = 0;
   s.gate_mode = !has_gate ? 0 : groups == 1 ? 1 : 2;
@@ -429,9 +486,6 @@ Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
     // whole groups (backward, more groups than units) or plain rows
     s.units = (int)std::min<int64_t>(target, backward && has_gate ? groups : T);
   }
-  const int fit = s.tpr <= 32 ? 128 / s.tpr : std::max(1, 256 / s.tpr);
-  s.block = s.tpr * fit;
-  s.blocks = (s.units + fit - 1) / fit;
   s.partial = backward ? 5 * (size_t)s.units * d * 4 : 0;
   return s;
 }
@@ -457,24 +511,38 @@ bool misaligned(std::initializer_list<const void*> ps) {
       return ppu_fail(PPU_ECUDA, "%s failed: %s", #call, cudaGetErrorString(e_));        \
   } while (0)
 
-template <bool LAYER, int GATE, bool BWD>
-int launch_norm(const NormArgs& a, const Shape& s, cudaStream_t st) {
-  constexpr int per_thread = Ring<BWD, GATE>::BYTES * Ring<BWD, GATE>::STAGES;
+template <int LANES, int GATE, bool BWD>
+int launch_norm(const NormArgs& a, cudaStream_t st) {
+  using L = Layout<LANES>;
+  using R = Ring<BWD, GATE, BWD ? BWD_CH : FWD_CH>;
+  constexpr int bytes = R::BYTES * R::STAGES * L::BLOCK;
+  static_assert(bytes <= 220 * 1024, "shared memory of a block");
   static PerDeviceFlag attr;
-  auto kernel = BWD ? norm_gate_bwd_kernel<LAYER, GATE> : norm_gate_fwd_kernel<LAYER, GATE>;
-  if (!ppu_set_smem_once(attr, kernel, per_thread * (MAX_D / 8))) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
-  kernel<<<s.blocks, s.block, per_thread * s.block, st>>>(a);
+  void (*kernel)(NormArgs);
+  if constexpr (BWD) kernel = norm_gate_bwd_kernel<LANES, GATE>;
+  else kernel = norm_gate_fwd_kernel<LANES, GATE>;
+  if (!ppu_set_smem_once(attr, kernel, bytes)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  kernel<<<(a.units + L::UNITS - 1) / L::UNITS, L::BLOCK, bytes, st>>>(a);
   CUDA_OK(cudaGetLastError());
   return PPU_OK;
 }
+template <int LANES, bool BWD>
+int launch_gate(const NormArgs& a, int gate_mode, cudaStream_t st) {
+  if (gate_mode == 0) return launch_norm<LANES, 0, BWD>(a, st);
+  if (gate_mode == 1) return launch_norm<LANES, 1, BWD>(a, st);
+  return launch_norm<LANES, 2, BWD>(a, st);
+}
 template <bool BWD>
-int dispatch(const NormArgs& a, const Shape& s, int kind, cudaStream_t st) {
-  const bool layer = kind == PPU_NORM_LAYER;
-  switch (s.gate_mode) {
-    case 0: return layer ? launch_norm<true, 0, BWD>(a, s, st) : launch_norm<false, 0, BWD>(a, s, st);
-    case 1: return layer ? launch_norm<true, 1, BWD>(a, s, st) : launch_norm<false, 1, BWD>(a, s, st);
-    default: return layer ? launch_norm<true, 2, BWD>(a, s, st) : launch_norm<false, 2, BWD>(a, s, st);
+int dispatch(const NormArgs& a, const Shape& s, cudaStream_t st) {
+  switch (s.lanes) {
+#define LANES_CASE(L) case L: return launch_gate<L, BWD>(a, s.gate_mode, st);
+    LANES_CASE(4) LANES_CASE(8) LANES_CASE(16) LANES_CASE(32) LANES_CASE(64) LANES_CASE(96) LANES_CASE(128) LANES_CASE(192)
+    LANES_CASE(256)
+#undef LANES_CASE
+    default: break;
   }
+  if constexpr (BWD) return launch_gate<512, BWD>(a, s.gate_mode, st);
+  return ppu_fail(PPU_ESHAPE, "row too long");
 }
 
 }  // namespace
@@ -493,9 +561,9 @@ extern "C" int ppu_norm_gate_fwd(const void* y, const float* r, const float* gat
   NormArgs a = {};
   a.y = (const bf16*)y; a.r = r; a.gate = gate; a.g1 = post_gain; a.b1 = post_shift; a.g2 = pre_gain; a.b2 = pre_shift;
   a.r_out = r_out; a.h = (bf16*)h; a.stats = (float4*)stats; a.scale = res_scale; a.eps = eps;
-  a.T = T; a.d = d; a.gate_rows = gate ? gate_rows : 1; a.tpr = s.tpr; a.units = s.units; a.per_group = 0;
+  a.T = T; a.d = d; a.gate_rows = gate ? gate_rows : 1; a.layer = kind == PPU_NORM_LAYER; a.units = s.units; a.per_group = 0;
   a.deal_rows = 1;                             // (no sums over a group)
-  return dispatch<false>(a, s, kind, (cudaStream_t)cuda_stream);
+  return dispatch<false>(a, s, (cudaStream_t)cuda_stream);
 }
 
 extern "C" int ppu_norm_gate_query_bytes(int T, int d, int gate_rows, size_t* bytes) {
@@ -531,9 +599,9 @@ extern "C" int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void
   NormArgs a = {};
   a.dh = (const bf16*)dh; a.dr = dr_out; a.y = (const bf16*)y; a.r = r_out; a.stats = (float4*)stats;
   a.gate = gate; a.g1 = post_gain; a.b1 = post_shift; a.g2 = pre_gain; a.dy = (bf16*)dy; a.dr_out = dr;
-  a.scale = res_scale; a.T = T; a.d = d; a.gate_rows = gate ? gate_rows : 1; a.tpr = s.tpr; a.units = s.units;
+  a.scale = res_scale; a.T = T; a.d = d; a.gate_rows = gate ? gate_rows : 1; a.layer = kind == PPU_NORM_LAYER; a.units = s.units;
   a.deal_rows = s.gate_mode == 2 ? gate_rows : 1; a.per_group = s.per_group; a.partial = (float*)workspace; a.dgate = dgate;
-  const int rc2 = dispatch<true>(a, s, kind, st);
+  const int rc2 = dispatch<true>(a, s, st);
   if (rc2) return rc2;
   const int groups = s.gate_mode == 1 ? s.units / s.per_group : 0;      // gate rows still to be summed
   const ParamOut po = {{dpost_gain, dpost_shift, dpre_gain, dpre_shift}, dgate};

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 
 import numpy as np
 
@@ -356,38 +357,87 @@ def _need(ok, what):
         raise PpuError(-1, what)
 
 
-def _tensor(t, name, dtype, shape, like=None, rows=False):
-    """Checks a device tensor; rows: the rows may be strided, otherwise it is contiguous."""
+def _is_dense(t, dtype, shape, device):
+    """A contiguous CUDA tensor of this type and shape on this device.  (These operators take
+    microseconds on small inputs, so their checks are few calls; _refuse finds the words.)"""
+    return t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
+
+
+def _is_rows(t, dtype, shape, device):
+    """The same for a matrix whose rows may be strided."""
+    if not (t.dtype is dtype and t.get_device() == device and t.shape == shape):
+        return False
+    if t.is_contiguous():
+        return True
+    return (shape[1] == 1 or t.stride(1) == 1) and (shape[0] == 1 or t.stride(0) >= shape[1])
+
+
+def _refuse(t, name, dtype, shape, device):
+    """Raises what is wrong with a tensor that _is_dense or _is_rows did not accept."""
     import torch
     _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
-    _need(t.dtype == dtype, f"{name} must be {dtype}, got {t.dtype}")
-    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    _need(like is None or t.device == like.device, f"{name} is on {t.device}, the others on {None if like is None else like.device}")
-    if not rows:
-        _need(t.is_contiguous(), f"{name} must be contiguous")
-    elif t.numel():
-        _need(t.shape[1] == 1 or t.stride(1) == 1, f"{name}: the values of a row must be adjacent")
-        _need(t.shape[0] == 1 or t.stride(0) >= t.shape[1], f"{name}: rows overlap")
-    return t
+    _need(t.dtype is dtype, f"{name} must be {dtype}, got {t.dtype}")
+    _need(t.shape == shape, f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    _need(t.get_device() == device, f"{name} is on {t.device}, other operands on cuda:{device}")
+    _need(False, f"{name}: values must be adjacent and rows must not overlap")
 
 
-def _ptr(t):
-    return C.c_void_p(None if t is None or t.numel() == 0 else t.data_ptr())
+def _dense(t, name, dtype, shape, device):
+    import torch
+    if not isinstance(t, torch.Tensor) or not _is_dense(t, dtype, shape, device):
+        _refuse(t, name, dtype, shape, device)
+    return t.data_ptr()
 
 
-def _row_stride(t):
-    return C.c_int64(t.stride(0) if t.shape[0] > 1 else t.shape[1])
+def _rows(t, name, dtype, shape, device):
+    import torch
+    if not isinstance(t, torch.Tensor) or not _is_rows(t, dtype, shape, device):
+        _refuse(t, name, dtype, shape, device)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _matrix(t, name):
+    import torch
+    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2, f"{name} must be a CUDA tensor of two dimensions")
+    return t.shape
 
 
 def _workspace(nbytes, device, given):
     import torch
     if given is not None:
-        _need(given.is_cuda and given.device == device and given.dtype == torch.uint8 and given.is_contiguous(),
+        _need(isinstance(given, torch.Tensor) and given.get_device() == device and given.dtype is torch.uint8 and given.is_contiguous(),
               "workspace must be a contiguous uint8 tensor on the operands' device")
         return given
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+def _on_device(device, call):
+    """Runs call(stream) with the operands' device current, on its current stream."""
+    import torch
+    if torch.cuda.current_device() == device:
+        return call(torch.cuda.current_stream(device).cuda_stream)
+    with torch.cuda.device(device):
+        return call(torch.cuda.current_stream(device).cuda_stream)
+
+
+_VP, _I, _I64, _F, _SZ = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
+_ARGTYPES = {
+    "ppu_head_xent": [_VP, _I64, _VP, _I64, _VP, _VP, _I, _I, _I, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _I, _VP, _SZ, _VP, _VP],
+    "ppu_head_distill": [_VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _I, _VP, _F, _VP, _I, _I, _I, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _I, _VP, _SZ,
+                         _VP, _VP],
+    "ppu_norm_gate_fwd": [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _I, _F, _F, _VP, _VP, _VP, _I, _I, _VP],
+    "ppu_norm_gate_bwd": [_VP, _VP, _VP, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _VP, _SZ, _VP],
+}
+
+
+def _entry(name):
+    fn = getattr(lib(), name)
+    if fn.argtypes is None:
+        fn.argtypes = _ARGTYPES[name]
+    return fn
+
+
+@lru_cache(maxsize=None)
 def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
     """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE)."""
     n = C.c_size_t(0)
@@ -395,32 +445,32 @@ def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
     return n.value
 
 
-def _head(call, X, E, row_weight, grad, chunk_rows, workspace, flags, targets):
-    """Outputs, workspace and the call of a head loss.  targets(T): its middle arguments."""
+def _head(name, X, E, row_weight, grad, chunk_rows, workspace, flags, targets):
+    """Outputs, workspace and the call of a head loss.  targets(T, device): its arguments between E and
+    row_weight."""
     import torch
-    _need(isinstance(X, torch.Tensor) and X.is_cuda and X.dim() == 2, "X must be a CUDA tensor [T, d]")
-    _need(isinstance(E, torch.Tensor) and E.dim() == 2, "E must be a CUDA tensor [V, d]")
-    T, d, V = X.shape[0], X.shape[1], E.shape[0]
-    _tensor(X, "X", torch.bfloat16, (T, d), rows=True)
-    _tensor(E, "E", torch.bfloat16, (V, d), X, rows=True)
-    if row_weight is not None:
-        _tensor(row_weight, "row_weight", torch.float32, (T,), X)
-    if flags is not None:
-        _tensor(flags, "flags", torch.int32, (8,), X)
-    want_x, want_e = (bool(grad), bool(grad)) if not isinstance(grad, str) else ("x" in grad, "e" in grad)
-    middle = targets(T, X)
-    with torch.cuda.device(X.device):
-        nbytes = ppu_head_query_bytes(T, d, V, want_x + 2 * want_e, chunk_rows)
-        ws = _workspace(nbytes, X.device, workspace)
-        f32 = dict(dtype=torch.float32, device=X.device)
-        loss, row_loss, lse = torch.empty((), **f32), torch.empty(T, **f32), torch.empty(T, **f32)
-        dX = torch.empty((T, d), dtype=torch.bfloat16, device=X.device) if want_x else None
-        dE = torch.empty((V, d), dtype=torch.bfloat16, device=X.device) if want_e else None
-        st = torch.cuda.current_stream(X.device).cuda_stream
-        _check(call(_ptr(X), _row_stride(X), _ptr(E), _row_stride(E), *middle, _ptr(row_weight), T, d, V, _ptr(loss),
-                    _ptr(row_loss), _ptr(lse), _ptr(dX), C.c_int64(d), _ptr(dE), C.c_int64(d), chunk_rows,
-                    C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), _ptr(flags), C.c_void_p(st)))
-    return loss, row_loss, lse, dX, dE
+    (T, d), V = _matrix(X, "X"), _matrix(E, "E")[0]
+    dev = X.get_device()
+    bf, f32 = torch.bfloat16, torch.float32
+    x, ldx = _rows(X, "X", bf, (T, d), dev)
+    e, lde = _rows(E, "E", bf, (V, d), dev)
+    w = None if row_weight is None else _dense(row_weight, "row_weight", f32, (T,), dev)
+    fl = None if flags is None else _dense(flags, "flags", torch.int32, (8,), dev)
+    want_x, want_e = ("x" in grad, "e" in grad) if isinstance(grad, str) else (bool(grad), bool(grad))
+    middle = targets(T, dev)
+    entry = _entry(name)
+
+    def call(stream):
+        ws = _workspace(ppu_head_query_bytes(T, d, V, want_x + 2 * want_e, chunk_rows), dev, workspace)
+        rows = torch.empty(2 * T + 1, dtype=f32, device=X.device)
+        loss, row_loss, lse = rows[2 * T], rows[:T], rows[T:2 * T]
+        dX = torch.empty((T, d), dtype=bf, device=X.device) if want_x else None
+        dE = torch.empty((V, d), dtype=bf, device=X.device) if want_e else None
+        p = rows.data_ptr()
+        _check(entry(x, ldx, e, lde, *middle, w, T, d, V, p + 8 * T, p, p + 4 * T, dX.data_ptr() if want_x else None, d,
+                     dE.data_ptr() if want_e else None, d, chunk_rows, ws.data_ptr(), ws.numel(), fl, stream))
+        return loss, row_loss, lse, dX, dE
+    return _on_device(dev, call)
 
 
 def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, workspace=None, flags=None):
@@ -431,9 +481,9 @@ def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, worksp
     flags: int32 [8] zeros for ppu_op_status."""
     import torch
 
-    def targets(T, like):
-        return (_ptr(_tensor(target, "target", torch.int32, (T,), like)),)
-    return _head(lib().ppu_head_xent, X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+    def targets(T, dev):
+        return (_dense(target, "target", torch.int32, (T,), dev),)
+    return _head("ppu_head_xent", X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
 
 
 def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher_lse=None, row_weight=None,
@@ -445,45 +495,44 @@ def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher
     same size at every temperature.  The rest as ppu_head_xent."""
     import torch
 
-    def targets(T, like):
-        _need(isinstance(teacher_ids, torch.Tensor) and teacher_ids.dim() == 2, "teacher_ids must be a CUDA tensor [T, k]")
-        k = teacher_ids.shape[1]
-        _tensor(teacher_ids, "teacher_ids", torch.int32, (T, k), like, rows=True)
-        _tensor(teacher_logits, "teacher_logits", torch.float32, (T, k), like, rows=True)
-        if teacher_lse is not None:
-            _tensor(teacher_lse, "teacher_lse", torch.float32, (T,), like)
-        return (_ptr(teacher_ids), _row_stride(teacher_ids), _ptr(teacher_logits), _row_stride(teacher_logits), k,
-                _ptr(teacher_lse), C.c_float(temperature))
-    return _head(lib().ppu_head_distill, X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+    def targets(T, dev):
+        k = _matrix(teacher_ids, "teacher_ids")[1]
+        i, ldi = _rows(teacher_ids, "teacher_ids", torch.int32, (T, k), dev)
+        z, ldz = _rows(teacher_logits, "teacher_logits", torch.float32, (T, k), dev)
+        return i, ldi, z, ldz, k, None if teacher_lse is None else _dense(teacher_lse, "teacher_lse", torch.float32, (T,), dev), temperature
+    return _head("ppu_head_distill", X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
 
 
 def ppu_op_status(flags) -> None:
     """Waits for the current stream; raises what a call given `flags` (int32 [8], zeros at first) reported."""
     import torch
-    _tensor(flags, "flags", torch.int32, (8,))
-    with torch.cuda.device(flags.device):
-        _check(lib().ppu_op_status(_ptr(flags), C.c_void_p(torch.cuda.current_stream(flags.device).cuda_stream)))
+    _need(isinstance(flags, torch.Tensor) and flags.is_cuda, "flags must be a CUDA tensor")
+    p = _dense(flags, "flags", torch.int32, (8,), flags.get_device())
+    _on_device(flags.get_device(), lambda stream: _check(lib().ppu_op_status(C.c_void_p(p), C.c_void_p(stream))))
 
 
 # ---- norms before and after a block, with its gate and the residual scale --------------------
 _KINDS = {"layer": NORM_LAYER, "rms": NORM_RMS}
 
 
-def _norm_operands(y, r, gate, gate_rows, vectors, kind):
+def _norm_operands(y, r, gate, gate_rows, kind, vectors):
+    """Device, sizes and addresses of what both passes take: y, r, the gate, the norms' vectors."""
     import torch
-    _need(isinstance(y, torch.Tensor) and y.is_cuda and y.dim() == 2, "y must be a CUDA tensor [T, d]")
+    T, d = _matrix(y, "y")
     _need(kind in _KINDS, f"kind must be one of {sorted(_KINDS)}")
-    T, d = y.shape
-    _tensor(y, "y", torch.bfloat16, (T, d))
-    _tensor(r, "r", torch.float32, (T, d), y)
-    for name, v in vectors.items():
-        if v is not None:
-            _tensor(v, name, torch.float32, (d,), y)
-    if gate is not None:
+    dev = y.get_device()
+    f32 = torch.float32
+    p = [_dense(y, "y", torch.bfloat16, (T, d), dev), _dense(r, "r", f32, (T, d), dev)]
+    if gate is None:
+        gate_rows = 0
+        p.append(None)
+    else:
+        _need(gate_rows >= 0, "gate_rows must not be negative")
         gate_rows = gate_rows or max(T, 1)
-        _need(gate_rows >= 1, "gate_rows must be positive")
-        _tensor(gate, "gate", torch.float32, (-(-T // gate_rows), d), y)
-    return T, d, gate_rows if gate is not None else 0
+        p.append(_dense(gate, "gate", f32, (-(-T // gate_rows), d), dev))
+    for name, v in zip(("post_gain", "post_shift", "pre_gain", "pre_shift"), vectors):
+        p.append(None if v is None and name.endswith("shift") else _dense(v, name, f32, (d,), dev))
+    return dev, T, d, gate_rows, p
 
 
 def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None, gate=None, gate_rows=0,
@@ -493,17 +542,24 @@ def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None
     gate fp32 [ceil(T / gate_rows), d] (gate_rows 0: one row for all).  in_place: r_out is r.
     Returns (r_out fp32, h bf16, stats fp32 [T, 4])."""
     import torch
-    T, d, gate_rows = _norm_operands(y, r, gate, gate_rows, {"post_gain": post_gain, "pre_gain": pre_gain, "post_shift": post_shift,
-                                                             "pre_shift": pre_shift}, kind)
-    with torch.cuda.device(y.device):
+    dev, T, d, gate_rows, (py, pr, pg, g1, b1, g2, b2) = _norm_operands(y, r, gate, gate_rows, kind, (post_gain, post_shift, pre_gain, pre_shift))
+    entry = _entry("ppu_norm_gate_fwd")
+
+    def call(stream):
         r_out = r if in_place else torch.empty_like(r)
         h = torch.empty_like(y)
-        stats = torch.empty((T, 4), dtype=torch.float32, device=y.device)
-        st = torch.cuda.current_stream(y.device).cuda_stream
-        _check(lib().ppu_norm_gate_fwd(_ptr(y), _ptr(r), _ptr(gate), gate_rows, _ptr(post_gain), _ptr(post_shift),
-                                       _ptr(pre_gain), _ptr(pre_shift), _KINDS[kind], C.c_float(res_scale), C.c_float(eps),
-                                       _ptr(r_out), _ptr(h), _ptr(stats), T, d, C.c_void_p(st)))
-    return r_out, h, stats
+        stats = torch.empty((T, 4), dtype=torch.float32, device=r.device)
+        _check(entry(py, pr, pg, gate_rows, g1, b1, g2, b2, _KINDS[kind], res_scale, eps, r_out.data_ptr(), h.data_ptr(), stats.data_ptr(), T, d, stream))
+        return r_out, h, stats
+    return _on_device(dev, call)
+
+
+@lru_cache(maxsize=None)
+def ppu_norm_gate_query_bytes(T, d, gate_rows=0) -> int:
+    """Bytes of workspace of ppu_norm_gate_bwd (gate_rows 0: no gate)."""
+    n = C.c_size_t(0)
+    _check(lib().ppu_norm_gate_query_bytes(T, d, gate_rows, C.byref(n)))
+    return n.value
 
 
 def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift=None, pre_shift=None, gate=None,
@@ -512,23 +568,21 @@ def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shi
     r_out and stats.  Returns (dy bf16, dr fp32, dpost_gain, dpost_shift, dpre_gain, dpre_shift,
     dgate); those of absent operands are None."""
     import torch
-    T, d, gate_rows = _norm_operands(y, r_out, gate, gate_rows, {"post_gain": post_gain, "pre_gain": pre_gain, "post_shift": post_shift,
-                                                                 "pre_shift": pre_shift}, kind)
-    _tensor(dh, "dh", torch.bfloat16, (T, d), y)
-    if dr_out is not None:
-        _tensor(dr_out, "dr_out", torch.float32, (T, d), y)
-    _tensor(stats, "stats", torch.float32, (T, 4), y)
-    with torch.cuda.device(y.device):
-        n = C.c_size_t(0)
-        _check(lib().ppu_norm_gate_query_bytes(T, d, gate_rows, C.byref(n)))
-        ws = _workspace(n.value, y.device, workspace)
+    dev, T, d, gate_rows, (py, pr, pg, g1, b1, g2, b2) = _norm_operands(y, r_out, gate, gate_rows, kind, (post_gain, post_shift, pre_gain, pre_shift))
+    f32 = torch.float32
+    pdh = _dense(dh, "dh", torch.bfloat16, (T, d), dev)
+    pdr = None if dr_out is None else _dense(dr_out, "dr_out", f32, (T, d), dev)
+    ps = _dense(stats, "stats", f32, (T, 4), dev)
+    entry = _entry("ppu_norm_gate_bwd")
+
+    def call(stream):
+        ws = _workspace(ppu_norm_gate_query_bytes(T, d, gate_rows), dev, workspace)
         dy, dr = torch.empty_like(y), torch.empty_like(r_out)
-        vec = lambda like: None if like is None else torch.empty(d, dtype=torch.float32, device=y.device)  # noqa: E731
-        dg1, db1, dg2, db2 = vec(post_gain), vec(post_shift), vec(pre_gain), vec(pre_shift)
+        sums = torch.empty((4, d), dtype=f32, device=dy.device)
         dgate = None if gate is None else torch.empty_like(gate)
-        st = torch.cuda.current_stream(y.device).cuda_stream
-        _check(lib().ppu_norm_gate_bwd(_ptr(dh), _ptr(dr_out), _ptr(y), _ptr(r_out), _ptr(stats), _ptr(gate), gate_rows,
-                                       _ptr(post_gain), _ptr(post_shift), _ptr(pre_gain), _KINDS[kind], C.c_float(res_scale),
-                                       _ptr(dy), _ptr(dr), _ptr(dg1), _ptr(db1), _ptr(dg2), _ptr(db2), _ptr(dgate), T, d,
-                                       C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), C.c_void_p(st)))
-    return dy, dr, dg1, db1, dg2, db2, dgate
+        s = sums.data_ptr()
+        _check(entry(pdh, pdr, py, pr, ps, pg, gate_rows, g1, b1, g2, _KINDS[kind], res_scale, dy.data_ptr(), dr.data_ptr(), s,
+                     None if b1 is None else s + 4 * d, s + 8 * d, None if b2 is None else s + 12 * d,
+                     None if gate is None else dgate.data_ptr(), T, d, ws.data_ptr(), ws.numel(), stream))
+        return (dy, dr, sums[0], None if b1 is None else sums[1], sums[2], None if b2 is None else sums[3], dgate)
+    return _on_device(dev, call)
