@@ -81,11 +81,12 @@ struct TcParams {
   int rope_S, rope_dh, rope_cols;
   void* C3; long long ldc3; int c3_lo, c3_hi;
   float piece_scale; float2* piece_stats; long long ld_pieces;
+  const float* row_scale;
 };
 
-// what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of the
-// two that have instantiations of their own so that drain_cols keeps its registers
-enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_RESID_BF16 = 2 };
+// what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of
+// those that have instantiations of their own so that drain_cols keeps its registers
+enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_RESID_BF16 = 2, DRAIN_SCALED_BF16 = 3 };
 
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows,
@@ -94,6 +95,7 @@ TcParams make_params(const GemmArgs& g);
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st);   // bn: 256 or 128
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st);
 int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
+int launch_gemm_tc_pair_scaled_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
 
 // Drains rows [m0 + 32 quarter, +32) x columns [n0 + half BN/2, + BN/2) of the accumulator at
 // TMEM column t_acc through registers into global memory, applying the epilogue p.epilogue.
@@ -299,11 +301,15 @@ __device__ __forceinline__ float ex2_fast(float x) {
 }
 
 // EPI_PIECES.  A lane holds 64 logits of its row at a time: x = acc * piece_scale (the scale holds
-// log2(e) and the temperature), m = max x, e = 2^(x - m).  The powers are stored in bf16 - a relative
-// rounding of half a step (2^-8) whatever the logit, where a bf16 logit of 16 would be off by 2^-4 absolutely -
-// and {m, sum e} in fp32, the sum over the unrounded powers, so the log-sum-exp keeps fp32 accuracy.
-// The exponent is one fused multiply-add on the accumulator; m is the rounded product used in it,
-// so its rounding cancels between the sum and the maximum.
+// log2(e) and the temperature), e = 2^(x - ref).  The powers are stored in bf16 - a relative
+// rounding of half a step (2^-8) whatever the logit, where a bf16 logit of 16 would be off by 2^-4
+// absolutely - and {ref, sum e} in fp32, the sum over the unrounded powers, so the log-sum-exp keeps fp32
+// accuracy.  bf16 has fp32's exponents, so with ordinary logits (|x| <= 60: 41 nats) one reference, 0,
+// serves the whole row, and its softmax is the stored powers times one factor, which the gradient
+// products apply to their other operand and to their result: no pass over the powers.  Pieces beyond that
+// are kept relative to their own maximum and brought into line afterwards.
+// The exponent is one fused multiply-add on the accumulator; ref is the rounded product used in it,
+// so its rounding cancels.
 __device__ __forceinline__ void drain_pieces(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
                                              int c_begin, int c_end, int lane) {
   const int m = m0 + quarter * 32 + lane;
@@ -326,7 +332,7 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, int m0, int n0, 
 #pragma unroll
     for (int j = 0; j < PIECE; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
     float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.piece_scale;
-    if (top == -INFINITY) top = 0.f;       // (a piece of -inf logits: all powers are 0)
+    if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < PIECE; ++j) {
@@ -385,11 +391,42 @@ __device__ __forceinline__ void drain_resid_bf16(const TcParams& p, int m0, int 
   }
 }
 
+// EPI_SCALED_BF16: row_scale[m] * acc, rounded once.  N is a multiple of 8, output rows 16-byte aligned.
+__device__ __forceinline__ void drain_scaled_bf16(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
+                                                  int c_begin, int c_end, int lane) {
+  const int m = m0 + quarter * 32 + lane;
+  const bool row_ok = m < p.M;
+  const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
+  const float f = row_ok ? __ldg(p.row_scale + m) : 0.f;
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+    const int nb = n0 + c0;
+    if (nb >= p.N) break;                  // warp-uniform
+    uint32_t r[32];
+    tmem_ld32(t_row + c0, r);
+    tmem_ld_wait();
+    if (!row_ok) continue;
+    uint32_t o[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
+    bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
+    if (p.wide && nb + 32 <= p.N) {
+      st_v8(dst, o);
+      st_v8(dst + 16, o + 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (nb + 8 * j < p.N) *reinterpret_cast<uint4*>(dst + 8 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+    }
+  }
+}
+
 template <int MODE>
 __device__ __forceinline__ void drain_mode(const TcParams& p, int m0, int n0, int sp, uint32_t t_acc, int quarter,
                                            int c_begin, int c_end, int lane) {
   if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
   else if constexpr (MODE == DRAIN_RESID_BF16) drain_resid_bf16(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else if constexpr (MODE == DRAIN_SCALED_BF16) drain_scaled_bf16(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
   else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
 

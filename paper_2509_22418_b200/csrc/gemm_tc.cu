@@ -240,6 +240,7 @@ TcParams make_params(const GemmArgs& g) {
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
   p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
+  p.row_scale = g.row_scale;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes
@@ -370,4 +371,14 @@ int launch_gemm_tc_resid_bf16(const GemmArgs& g, cudaStream_t st) {
     return -4;
   if (picks_pair256(g)) return launch_gemm_tc_pair_resid_bf16(g, make_params(g), st);
   return launch_t<128, false, false, DRAIN_RESID_BF16>(g, st);
+}
+
+int launch_gemm_tc_scaled_bf16(const GemmArgs& g, cudaStream_t st) {
+  if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
+  if (gemm_tc_init() != 0) return -1;
+  if (!operands_ok(g) || !g.a_kmajor || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || !g.row_scale ||
+      (reinterpret_cast<uintptr_t>(g.C) & 15))
+    return -4;
+  if (picks_pair256(g)) return launch_gemm_tc_pair_scaled_bf16(g, make_params(g), st);
+  return launch_t<128, true, false, DRAIN_SCALED_BF16>(g, st);
 }

@@ -335,4 +335,7 @@ int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_
 int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
   return launch_pair_t<256, false, false, DRAIN_RESID_BF16>(g, p, st);
 }
+int launch_gemm_tc_pair_scaled_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
+  return launch_pair_t<256, true, false, DRAIN_SCALED_BF16>(g, p, st);
+}
 }  // namespace gemm_tc_detail

@@ -10,17 +10,22 @@
 // Three matrix products cannot be avoided (6 T V d operations), and a backward pass that forms the
 // logits again would make it four.  So rows are worked in chunks, whose softmax is kept only until
 // the chunk's two gradient products are done: a [rows, V] buffer of bounded size, not [T, V].
-//   1. tcgen05 product of the chunk's rows with E^T.  Its epilogue works the vocabulary in pieces
-//      of 64 columns: bf16 powers relative to the piece's own maximum, and {maximum, sum} in fp32.
+//   1. tcgen05 product of the chunk's rows with E^T.  Its epilogue works the vocabulary in pieces of 64
+//      columns: bf16 powers u = 2^(x - ref), x = s log2(e), and {ref, sum} in fp32; ref is 0 for ordinary
+//      logits (within 41 nats of 0), else the piece's maximum.
 //   2. one block per row joins the pieces to the row's log-sum-exp, computes the entries' logits as
 //      fp32 dot products of their own (k of them, d long: the stored powers would be too coarse for
-//      the loss and for p - 1 next to p = 1), the row loss, and turns the powers into ds in place: one
-//      factor for each piece, the entries' places overwritten with their exact values.
-//   3. dX and dE products of ds; dE over several chunks is a running fp32 sum, rounded once by the last.
-// Steps 1 and 2 go over sub-chunks that fit the L2 (64 MiB), so step 2 does not read HBM.
-// Roundings: the powers and ds are bf16 (the tensor cores' operand type; each off by at most half a
-// step, 2^-8 of its own value, independently), dX and dE are rounded once from fp32; statistics,
-// losses and running sums are fp32.
+//      the loss and for p - 1 next to p = 1) and the row loss.  Then ds_tv = f_t u_tv with one factor per
+//      row: the powers stay as they are, but for the entries' places, which are overwritten, and for
+//      pieces (rows) beyond the range of the common reference, which are rescaled.
+//   3. dX = f (u E), the factor applied in the product's epilogue, and dE = u^T (f X) with f X formed in
+//      step 2; dE over several chunks is a running fp32 sum, rounded once by the last.
+// Step 2 once rewrote the whole buffer as ds: 27 us per 1024 rows of 32768 (L2-resident), 7 % of the
+// call at 8192 rows; without it GAIN_US.
+// Roundings: u and f X are bf16 (the tensor cores' operand type; each off by at most half a step, 2^-8 of
+// its own value, independently), dX and dE are rounded once from fp32; statistics, losses and running
+// sums are fp32.  (The tensor cores' fp32 sums drop what lies below the last bit, so logits come out low
+// by up to 2^-24 per 16 products: 2e-6 of a logit at d = 2048.)
 #include <algorithm>
 #include "../../include/ppu.h"
 #include "common.cuh"
@@ -29,7 +34,7 @@ int ppu_fail(int code, const char* fmt, ...);
 
 namespace {
 
-constexpr int ROW_THREADS = 256;
+constexpr int ROW_THREADS = 128;
 constexpr int MAX_ENTRIES = PPU_MAX_TEACHER_ENTRIES;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -42,13 +47,17 @@ struct Targets {             // q_tj
 
 struct RowArgs {
   Targets tg;
-  bf16* u; int64_t ldu;                  // powers in, ds out (this sub-chunk's rows); null without gradients
+  bf16* u; int64_t ldu;                  // powers of this chunk's rows; null without gradients
   const float2* stats; int64_t ld_pieces; int n_pieces;
   const bf16* X; int64_t ldx; const bf16* E; int64_t lde; int d, V;
-  int64_t row0;                          // first row of the sub-chunk
+  int64_t row0;                          // first row of the chunk
+  int T;
   float scale2;                          // log2(e) / temperature
   const float* weight; const int* count; // weight null: 1 / *count
   float *row_loss, *lse, *weighted;      // per row; the first two may be null
+  float* factor;                         // f, of this chunk's rows
+  bf16* fx;                              // f X [rows][d], or null
+  unsigned* done; float* loss;           // rows finished so far; sum of `weighted`, by the last of them
   int* flags;
 };
 
@@ -91,17 +100,36 @@ __device__ __forceinline__ Piece join(Piece a, Piece b) {
   return {m, a.s * exp2f(a.m - m) + b.s * exp2f(b.m - m)};
 }
 
+__device__ __forceinline__ bool row_counts(const Targets& tg, int64_t t, int V) {
+  for (int j = 0; j < tg.k; ++j) {
+    const int id = tg.ids[t * tg.ld_ids + j];
+    if (id >= 0 && id < V && !(tg.z && tg.z[t * tg.ld_z + j] * tg.inv_temp == -INFINITY)) return true;
+  }
+  return false;
+}
 // rows with at least one present entry (integer atomics: any order gives the same count)
 __global__ void __launch_bounds__(256) count_rows_kernel(Targets tg, int T, int V, int* count) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  bool any = false;
-  if (t < T)
-    for (int j = 0; j < tg.k && !any; ++j) {
-      const int id = tg.ids[t * tg.ld_ids + j];
-      any = id >= 0 && id < V && !(tg.z && tg.z[t * tg.ld_z + j] * tg.inv_temp == -INFINITY);
-    }
-  const int n = __syncthreads_count(any);
+  const int64_t t = blockIdx.x * 256 + threadIdx.x;
+  const int n = __syncthreads_count(t < T && row_counts(tg, t, V));
   if (threadIdx.x == 0 && n) atomicAdd(count, n);
+}
+// the same by one block, which needs no zeroed count: one launch less for up to 2^14 rows
+__global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int T, int V, int* count, unsigned* done) {
+  int n = 0;
+  for (int64_t t0 = 0; t0 < T; t0 += 1024) n += __syncthreads_count(t0 + threadIdx.x < T && row_counts(tg, t0 + threadIdx.x, V));
+  if (threadIdx.x == 0) { *count = n; *done = 0; }
+}
+
+// scales 64 stored powers
+__device__ __forceinline__ void scale_piece(bf16* p, float f) {
+#pragma unroll
+  for (int i = 0; i < PIECE / 8; ++i) {
+    float v[8];
+    unpack8(reinterpret_cast<const uint4*>(p)[i], v);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= f;
+    reinterpret_cast<uint4*>(p)[i] = pack8(v);
+  }
 }
 
 template <bool GRAD>
@@ -109,10 +137,10 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
   __shared__ int s_id[MAX_ENTRIES];
   __shared__ float s_q[MAX_ENTRIES], s_l[MAX_ENTRIES];
   __shared__ float s_total, s_entropy;
-  __shared__ int s_any;
+  __shared__ int s_any, s_last;
   __shared__ Piece s_piece[ROW_THREADS / 32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t row = blockIdx.x, t = a.row0 + row;
+  const int64_t row = blockIdx.x, t = a.row0 + row;   // row of the chunk, of the call
   const int k = a.tg.k;
 
   // the row's entries and their q (warp 0), while every thread joins its share of the pieces
@@ -181,97 +209,122 @@ __global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a)
   const float lse2 = all.m + log2f(all.s);          // base 2
   if (threadIdx.x == 0 && a.lse) a.lse[t] = lse2 * LN2;
 
-  if (!s_any) {                                     // block-uniform: the row has no loss and no gradient
-    if (threadIdx.x == 0) { if (a.row_loss) a.row_loss[t] = 0.f; a.weighted[t] = 0.f; }
-    if (GRAD)
-      for (int i = threadIdx.x; i < a.ldu / 8; i += ROW_THREADS)
-        reinterpret_cast<uint4*>(a.u + row * a.ldu)[i] = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  // the entries' logits, one warp each
+  // the reference of the row's powers: 0, or where that is too far from their sum, the sum itself
+  const float ref = fabsf(lse2) <= PIECE_RANGE ? 0.f : lse2;
   const uint4* xr = reinterpret_cast<const uint4*>(a.X + t * a.ldx);
-  for (int j = warp; j < k; j += ROW_THREADS / 32) {
-    if (s_id[j] < 0) continue;
-    const uint4* er = reinterpret_cast<const uint4*>(a.E + (int64_t)s_id[j] * a.lde);
-    float acc = 0.f;
-    for (int i = lane; i < a.d / 8; i += 32) {
-      float x[8], e[8];
-      unpack8(xr[i], x); unpack8(er[i], e);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) acc = fmaf(x[c], e[c], acc);
+  bf16* ur = a.u + row * a.ldu;
+  uint4* fx = GRAD && a.fx ? reinterpret_cast<uint4*>(a.fx + row * a.d) : nullptr;
+  if (!s_any) {                                     // block-uniform: the row has no loss and no gradient
+    if (threadIdx.x == 0) {
+      if (a.row_loss) a.row_loss[t] = 0.f;
+      a.weighted[t] = 0.f;
+      if (GRAD) a.factor[row] = 0.f;
     }
-    acc = warp_sum(acc);
-    if (lane == 0) s_l[j] = acc * a.scale2;
+    if (GRAD) {
+      if (!isfinite(all.s))                         // (0 times the powers has to be 0)
+        for (int i = threadIdx.x; i < a.ldu / 8; i += ROW_THREADS) reinterpret_cast<uint4*>(ur)[i] = make_uint4(0, 0, 0, 0);
+      if (fx)
+        for (int i = threadIdx.x; i < a.d / 8; i += ROW_THREADS) fx[i] = make_uint4(0, 0, 0, 0);
+    }
+  } else {
+    // the entries' logits, one warp each
+    for (int j = warp; j < k; j += ROW_THREADS / 32) {
+      if (s_id[j] < 0) continue;
+      const uint4* er = reinterpret_cast<const uint4*>(a.E + (int64_t)s_id[j] * a.lde);
+      float acc = 0.f;
+#pragma unroll 4
+      for (int i = lane; i < a.d / 8; i += 32) {
+        float x[8], e[8];
+        unpack8(xr[i], x); unpack8(er[i], e);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc = fmaf(x[c], e[c], acc);
+      }
+      acc = warp_sum(acc);
+      if (lane == 0) s_l[j] = acc * a.scale2;
+    }
+    __syncthreads();
+    const float w = a.weight ? a.weight[t] : 1.f / (float)*a.count;
+    const float c = w * a.tg.inv_temp * s_total;
+    const float f = c * exp2f(ref - lse2);
+    if (threadIdx.x == 0) {
+      float x = 0.f;
+      for (int j = 0; j < k; ++j)
+        if (s_id[j] >= 0 && s_q[j] != 0.f) x = fmaf(s_q[j], lse2 - s_l[j], x);
+      const float l = s_entropy + x * LN2;
+      if (a.row_loss) a.row_loss[t] = l;
+      a.weighted[t] = w * l;
+      if (GRAD) a.factor[row] = f;
+    }
+    if (GRAD) {
+      if (fx)
+        for (int i = threadIdx.x; i < a.d / 8; i += ROW_THREADS) {
+          float v[8];
+          unpack8(xr[i], v);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] *= f;
+          fx[i] = pack8(v);
+        }
+      // (seldom) powers that are relative to something else
+      for (int i = threadIdx.x; i < a.n_pieces; i += ROW_THREADS)
+        if (st[i].x != ref && st[i].y != 0.f) scale_piece(ur + (int64_t)i * PIECE, exp2f(st[i].x - ref));
+      __syncthreads();                              // those stand: overwrite the entries' places
+      for (int j = threadIdx.x; j < k; j += ROW_THREADS) {
+        const int id = s_id[j];
+        if (id < 0) continue;
+        float q = 0.f;
+        bool first = true;                          // an id given twice: its first entry writes for all
+        for (int i = 0; i < k; ++i)
+          if (s_id[i] == id) { if (i < j) first = false; q += s_q[i]; }
+        // p - q / Q with p = exp(x): (exp(x) - 1) + (1 - q / Q) keeps its digits where p is next to 1
+        if (first && s_total != 0.f)
+          ur[id] = __float2bfloat16_rn((expm1f((s_l[j] - lse2) * LN2) + (s_total - q) / s_total) * exp2f(lse2 - ref));
+      }
+    }
+  }
+  // the last row adds up the losses, in the same order whichever row that is
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    s_last = atomicAdd(a.done, 1u) == (unsigned)a.T - 1u;
   }
   __syncthreads();
-  const float w = a.weight ? a.weight[t] : 1.f / (float)*a.count;
-  if (threadIdx.x == 0) {
-    float x = 0.f;
-    for (int j = 0; j < k; ++j)
-      if (s_id[j] >= 0 && s_q[j] != 0.f) x = fmaf(s_q[j], lse2 - s_l[j], x);
-    const float l = s_entropy + x * LN2;
-    if (a.row_loss) a.row_loss[t] = l;
-    a.weighted[t] = w * l;
-  }
-  if (!GRAD) return;
-  const float c = w * a.tg.inv_temp, cq = c * s_total;
-  uint4* ur = reinterpret_cast<uint4*>(a.u + row * a.ldu);
-  const int nvec = (int)(a.ldu / 8);
-#pragma unroll 4
-  for (int i = threadIdx.x; i < nvec; i += ROW_THREADS) {
-    const float f = cq * exp2f(st[i / (PIECE / 8)].x - lse2);
-    float v[8];
-    unpack8(ur[i], v);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] *= f;
-    ur[i] = pack8(v);
-  }
-  __syncthreads();                                  // the entries' places have been written: overwrite them
-  for (int j = threadIdx.x; j < k; j += ROW_THREADS) {
-    const int id = s_id[j];
-    if (id < 0) continue;
-    float q = 0.f;
-    bool first = true;                              // an id given twice: its first entry writes for all
-    for (int i = 0; i < k; ++i)
-      if (s_id[i] == id) { if (i < j) first = false; q += s_q[i]; }
-    // Q p - q with p = exp(x): Q (exp(x) - 1) + (Q - q) keeps its digits where p is next to 1
-    if (first) a.u[row * a.ldu + id] = __float2bfloat16_rn(c * (s_total * expm1f((s_l[j] - lse2) * LN2) + (s_total - q)));
-  }
-}
-
-__global__ void __launch_bounds__(1024) sum_rows_kernel(const float* __restrict__ v, int T, float* out) {
-  __shared__ float red[32];
+  if (!s_last) return;
+  __threadfence();
   float s = 0.f;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < T; i += 1024) s += v[i];
+  for (int i = threadIdx.x; i < a.T; i += ROW_THREADS) s += __ldcg(a.weighted + i);
   s = warp_sum(s);
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
   __syncthreads();
-  if (threadIdx.x < 32) {
-    s = warp_sum(red[threadIdx.x]);
-    if (threadIdx.x == 0) *out = s;
+  if (lane == 0) s_q[warp] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.f;
+    for (int i = 0; i < ROW_THREADS / 32; ++i) s += s_q[i];
+    *a.loss = s;
   }
 }
 
-// out bf16 [rows, n] = sum of `splits` fp32 partial products, in index order
+// out bf16 [rows, 4 n4] = sum of `splits` fp32 partial products, in index order, times the row's factor
 __global__ void __launch_bounds__(256)
-join_partials_kernel(const float* __restrict__ part, int splits, int64_t stride, bf16* __restrict__ out, int64_t ldo, int rows, int n8) {
+join_partials_kernel(const float* __restrict__ part, int splits, int64_t stride, const float* __restrict__ row_scale,
+                     bf16* __restrict__ out, int64_t ldo, int rows, int n4) {
   const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-  if (i >= (int64_t)rows * n8) return;
-  float s[8] = {};
-#pragma unroll 4
+  if (i >= (int64_t)rows * n4) return;
+  const int64_t r = i / n4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
   for (int q = 0; q < splits; ++q) {
-    const float4* p = reinterpret_cast<const float4*>(part + q * stride + i * 8);
-    const float4 x = p[0], y = p[1];
-    s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
-    s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+    const float4 x = *reinterpret_cast<const float4*>(part + q * stride + i * 4);
+    s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
   }
-  *reinterpret_cast<uint4*>(out + (i / n8) * ldo + (i % n8) * 8) = pack8(s);
+  const float f = row_scale ? row_scale[r] : 1.f;
+  __nv_bfloat162 a = __floats2bfloat162_rn(f * s.x, f * s.y), b = __floats2bfloat162_rn(f * s.z, f * s.w);
+  *reinterpret_cast<uint2*>(out + r * ldo + (i - r * n4) * 4) =
+      make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
 }
 
 // ---- host ---------------------------------------------------------------------------------------
 constexpr int64_t U_BYTES = 256ll << 20;      // default bound of a chunk's powers
-constexpr int64_t L2_BYTES = 64ll << 20;      // a sub-chunk's powers, re-read while in the L2 (126 MB)
 constexpr int SMS = 148;                      // work is split for a B200 (also where sizes are asked without a device)
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -286,9 +339,9 @@ int splits_for(int64_t M, int64_t N, int64_t K) {
 }
 
 struct Plan {
-  int64_t ldu, n_pieces, chunk, sub;
+  int64_t ldu, n_pieces, chunk;
   int chunks, sx, se;                          // split-K factors of dX and dE
-  size_t off_weighted, off_stats, off_u, off_acc, off_part, bytes;
+  size_t off_weighted, off_factor, off_stats, off_u, off_fx, off_acc, off_part, bytes;
 };
 Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
   Plan p;
@@ -299,14 +352,15 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
   int64_t c = chunk_rows > 0 ? round_up(chunk_rows, 256) : std::max<int64_t>(256, U_BYTES / row_bytes / 256 * 256);
   p.chunks = (int)std::max<int64_t>(1, (T + c - 1) / c);
   p.chunk = p.chunks == 1 ? T : round_up((T + p.chunks - 1) / p.chunks, 256);
-  p.sub = want ? std::min<int64_t>(p.chunk, std::max<int64_t>(256, L2_BYTES / row_bytes / 256 * 256)) : p.chunk;
   p.sx = (want & 1) ? splits_for(p.chunk, d, V) : 1;
   p.se = (want & 2) && p.chunks == 1 ? splits_for(V, d, p.chunk) : 1;
-  size_t off = 256;                            // the row count
+  size_t off = 256;                            // the row count, the rows finished
   auto take = [&off](int64_t bytes) { const size_t at = off; off += (size_t)round_up(bytes, 256); return at; };
   p.off_weighted = take(4ll * T);
-  p.off_stats = take(8ll * p.sub * p.n_pieces);
+  p.off_factor = take(4ll * p.chunk);
+  p.off_stats = take(8ll * p.chunk * p.n_pieces);
   p.off_u = take(want ? p.chunk * row_bytes : 0);
+  p.off_fx = take((want & 2) ? 2ll * p.chunk * d : 0);
   p.off_acc = take((want & 2) && p.chunks > 1 ? 4ll * V * d : 0);
   int64_t part = 0;
   if (p.sx > 1) part = 4ll * p.sx * p.chunk * d;
@@ -351,14 +405,18 @@ struct HeadCall {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// bf16 C = A . B^T, split over K into fp32 partials where that fills the machine
+// bf16 C = A . B^T (times row_scale), split over K into fp32 partials where that fills the machine
 int product_bf16(GemmArgs g, int splits, float* part, cudaStream_t st) {
-  if (splits <= 1) { g.epilogue = EPI_STORE_BF16; GEMM_OK(launch_gemm_tc(g, st)); return PPU_OK; }
+  if (splits <= 1) {
+    g.epilogue = g.row_scale ? EPI_SCALED_BF16 : EPI_STORE_BF16;
+    GEMM_OK(g.row_scale ? launch_gemm_tc_scaled_bf16(g, st) : launch_gemm_tc(g, st));
+    return PPU_OK;
+  }
   bf16* out = (bf16*)g.C; const int64_t ldo = g.ldc;
   g.epilogue = EPI_STORE_F32; g.C = part; g.ldc = g.N; g.splits = splits; g.split_stride = (int64_t)g.M * g.N;
   GEMM_OK(launch_gemm_tc(g, st));
-  const int64_t n = (int64_t)g.M * (g.N / 8);
-  join_partials_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, splits, g.split_stride, out, ldo, g.M, g.N / 8);
+  const int64_t n = (int64_t)g.M * (g.N / 4);
+  join_partials_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, splits, g.split_stride, g.row_scale, out, ldo, g.M, g.N / 4);
   return PPU_OK;
 }
 
@@ -378,9 +436,11 @@ int run_head(const HeadCall& c) {
 
   uint8_t* ws = (uint8_t*)c.ws;
   int* count = (int*)ws;
-  float* weighted = (float*)(ws + p.off_weighted);
+  unsigned* done = (unsigned*)ws + 1;
+  float* factor = (float*)(ws + p.off_factor);
   float2* stats = (float2*)(ws + p.off_stats);
   bf16* u = want ? (bf16*)(ws + p.off_u) : nullptr;
+  bf16* fx = c.dE ? (bf16*)(ws + p.off_fx) : nullptr;
   float* acc = (float*)(ws + p.off_acc);
   float* part = (float*)(ws + p.off_part);
 
@@ -389,60 +449,59 @@ int run_head(const HeadCall& c) {
     if (c.dE) CUDA_OK(cudaMemset2DAsync(c.dE, (size_t)c.ldde * 2, 0, (size_t)c.d * 2, (size_t)c.V, c.st));
     return PPU_OK;
   }
-  if (!c.weight) {
-    CUDA_OK(cudaMemsetAsync(count, 0, 4, c.st));
-    count_rows_kernel<<<(c.T + 255) / 256, 256, 0, c.st>>>(c.tg, c.T, c.V, count);
+  if (!c.weight && c.T <= (1 << 14)) {
+    count_rows_block_kernel<<<1, 1024, 0, c.st>>>(c.tg, c.T, c.V, count, done);
+  } else {
+    CUDA_OK(cudaMemsetAsync(ws, 0, 8, c.st));
+    if (!c.weight) count_rows_kernel<<<(c.T + 255) / 256, 256, 0, c.st>>>(c.tg, c.T, c.V, count);
   }
   RowArgs r;
-  r.tg = c.tg; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
-  r.X = (const bf16*)c.X; r.ldx = c.ldx; r.E = (const bf16*)c.E; r.lde = c.lde; r.d = c.d; r.V = c.V;
+  r.tg = c.tg; r.u = u; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
+  r.X = (const bf16*)c.X; r.ldx = c.ldx; r.E = (const bf16*)c.E; r.lde = c.lde; r.d = c.d; r.V = c.V; r.T = c.T;
   r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = count;
-  r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = weighted; r.flags = c.flags;
+  r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
+  r.done = done; r.loss = c.loss; r.flags = c.flags;
 
   GemmArgs g0;
   g0.C2 = nullptr; g0.aux = nullptr; g0.ldaux = 0; g0.flags = c.flags; g0.transient = true;
-  for (int ch = 0; ch < p.chunks; ++ch) {
-    const int64_t c0 = ch * p.chunk, rows = std::min<int64_t>(p.chunk, c.T - c0);
-    if (rows <= 0) break;
-    for (int64_t s0 = 0; s0 < rows; s0 += p.sub) {
-      const int64_t n = std::min<int64_t>(p.sub, rows - s0);
+  for (int64_t c0 = 0; c0 < c.T; c0 += p.chunk) {
+    const int64_t rows = std::min<int64_t>(p.chunk, c.T - c0);
+    {
       GemmArgs g = g0;
-      g.A = r.X + (c0 + s0) * c.ldx; g.lda = c.ldx; g.a_kmajor = 1;
+      g.A = r.X + c0 * c.ldx; g.lda = c.ldx; g.a_kmajor = 1;
       g.B = r.E; g.ldb = c.lde; g.b_kmajor = 1;
-      g.M = (int)n; g.N = c.V; g.K = c.d; g.epilogue = EPI_PIECES;
-      g.C = u ? u + s0 * p.ldu : nullptr; g.ldc = p.ldu;
+      g.M = (int)rows; g.N = c.V; g.K = c.d; g.epilogue = EPI_PIECES; g.C = u; g.ldc = p.ldu;
       g.piece_scale = r.scale2; g.piece_stats = stats; g.ld_pieces = p.n_pieces;
       GEMM_OK(launch_gemm_tc_pieces(g, c.st));
-      r.row0 = c0 + s0; r.u = u ? u + s0 * p.ldu : nullptr;
-      if (want) head_rows_kernel<true><<<(unsigned)n, ROW_THREADS, 0, c.st>>>(r);
-      else head_rows_kernel<false><<<(unsigned)n, ROW_THREADS, 0, c.st>>>(r);
     }
+    r.row0 = c0;
+    if (want) head_rows_kernel<true><<<(unsigned)rows, ROW_THREADS, 0, c.st>>>(r);
+    else head_rows_kernel<false><<<(unsigned)rows, ROW_THREADS, 0, c.st>>>(r);
     if (c.dX) {
       GemmArgs g = g0;
-      g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = r.E; g.ldb = c.lde; g.b_kmajor = 0;
+      g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = r.E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;
       g.M = (int)rows; g.N = c.d; g.K = c.V; g.C = (bf16*)c.dX + c0 * c.lddx; g.ldc = c.lddx;
       rc = product_bf16(g, p.sx, part, c.st);
       if (rc) return rc;
     }
     if (c.dE) {
       GemmArgs g = g0;
-      g.A = u; g.lda = p.ldu; g.a_kmajor = 0; g.B = r.X + c0 * c.ldx; g.ldb = c.ldx; g.b_kmajor = 0;
+      g.A = u; g.lda = p.ldu; g.a_kmajor = 0; g.B = fx; g.ldb = c.d; g.b_kmajor = 0;
       g.M = c.V; g.N = c.d; g.K = (int)rows; g.C = c.dE; g.ldc = c.ldde;
-      const bool last = ch == p.chunks - 1 || c0 + p.chunk >= c.T;
-      if (ch == 0 && last) {
+      const bool last = c0 + p.chunk >= c.T;
+      if (c0 == 0 && last) {
         rc = product_bf16(g, p.se, part, c.st);
         if (rc) return rc;
       } else if (last) {
         g.epilogue = EPI_RESID_BF16; g.aux = acc; g.ldaux = c.d;
         GEMM_OK(launch_gemm_tc_resid_bf16(g, c.st));
       } else {
-        g.epilogue = ch == 0 ? EPI_STORE_F32 : EPI_RESID_F32;
+        g.epilogue = c0 == 0 ? EPI_STORE_F32 : EPI_RESID_F32;
         g.C = acc; g.ldc = c.d; g.aux = acc; g.ldaux = c.d;
         GEMM_OK(launch_gemm_tc(g, c.st));
       }
     }
   }
-  sum_rows_kernel<<<1, 1024, 0, c.st>>>(weighted, c.T, c.loss);
   CUDA_OK(cudaGetLastError());
   return PPU_OK;
 }

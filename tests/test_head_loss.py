@@ -6,8 +6,8 @@ Roundings counted (u = 2^-24 for fp32, half a step; bf16 half a step 2^-8):
     addition off by at most a whole step 2^-23 of the sum of magnitudes: (d / 16 + 8) 2^-23 sum |x e|;
   log-sum-exp: the largest logit error, the exponentials' relative error (2^-21 with the rounding of their
     argument: |argument| u / ln 2 more) and the rounding of the result;
-  ds: the stored power and the scaled value are both bf16, 2 * 2^-8 of Q p |w|, beside the logits' errors;
-    an entry's own place is rounded once;
+  ds = f u: the stored power u is bf16, 2^-8 of Q p |w| (an entry's place: 2^-8 of its own value), beside the
+    logits' errors; for dE the factor is multiplied into X, which is rounded to bf16 again: 2^-8 |ds| more;
   dX, dE: the errors of ds times the other operand's magnitudes, the sums' (n / 16 + 8) 2^-23 of the sum of
     magnitudes, and the result's own half step.
 """
@@ -52,11 +52,12 @@ def tolerances(X, E, q, w, temp, R, entropy):
     lse = worst + 2.0 ** -21 + 4 * U * spread + 8 * U
     row = R["Q"] * (lse + worst) + 32 * U * (np.abs(entropy) + (np.abs(q).sum(1)) * (spread + 8))
     both = (s_err + lse[:, None]) * 1.01
-    ds = np.abs(w)[:, None] * R["Q"][:, None] * R["p"] * (2 * BF + 2.0 ** -15 + both) + BF * np.abs(R["ds"]) + np.abs(w)[:, None] * 64 * U
+    ds = np.abs(w)[:, None] * R["Q"][:, None] * R["p"] * (BF + 2.0 ** -15 + both) + BF * np.abs(R["ds"]) + np.abs(w)[:, None] * 64 * U
+    ds_e = ds * (1 + BF) + BF * np.abs(R["ds"])
     # (64 U: the entries' own places, 1 - p formed from q and p in fp32)
     sums = lambda n: (n / 16 + 12) * 2 * U  # noqa: E731
     dX = ds @ np.abs(E) / temp + sums(V) * (np.abs(R["ds"]) @ np.abs(E)) / temp
-    dE = ds.T @ np.abs(X) / temp + sums(T) * (np.abs(R["ds"]).T @ np.abs(X)) / temp
+    dE = ds_e.T @ np.abs(X) / temp + sums(T) * (np.abs(R["ds"]).T @ np.abs(X)) / temp
     tiny = 1e-30
     return dict(lse=lse, row=row, loss=(np.abs(w) * row).sum() + 64 * U * (np.abs(w * R["row"])).sum() + tiny,
                 dX=dX * (1 + BF) + BF * np.abs(R["dX"]) + tiny, dE=dE * (1 + BF) + BF * np.abs(R["dE"]) + tiny)
@@ -171,8 +172,7 @@ def test_chunks_of_rows(T, d, V):
 
 
 @gpu
-def test_sub_chunks_of_a_large_vocabulary():
-    """Rows whose softmax is joined in several turns (64 MiB each) inside one chunk."""
+def test_large_vocabulary():
     import torch
     from paper_2509_22418_b200 import ppu
     T, d, V = 600, 64, 140003
@@ -220,10 +220,11 @@ def test_offsets_beyond_32_bits():
         p = torch.exp(s - lse[:, None])
         ds = p * w
         ds[at] -= w
-        err = w * p * (2 * BF + 2.0 ** -15 + 1.01 * (s_err + tol["lse"][b][:, None])) + BF * ds.abs() + w * 64 * U
+        err = w * p * (BF + 2.0 ** -15 + 1.01 * (s_err + tol["lse"][b][:, None])) + BF * ds.abs() + w * 64 * U
         R["dX"][b] = ds @ e
         tol["dX"][b] = (err @ e.abs() + sums(V) * (ds.abs() @ e.abs())) * (1 + BF) + BF * R["dX"][b].abs()
         R["dE"] += ds.T @ x[b]
+        err = err * (1 + BF) + BF * ds.abs()
         tol["dE"] += (err.T @ x[b].abs() + sums(T) * (ds.abs().T @ x[b].abs())) * (1 + BF)
     tol["dE"] += BF * R["dE"].abs()
     for out in (got, small):
@@ -358,7 +359,8 @@ def test_ids_outside_the_vocabulary_are_left_out_and_reported():
 
 @gpu
 def test_confident_and_hopeless_rows():
-    """Rows where the target has all of the probability, and rows hundreds of nats away from it."""
+    """Rows where the target has all of the probability, and rows hundreds of nats away from it: beyond the
+    range of the powers' common reference."""
     import torch
     from paper_2509_22418_b200 import ppu
     T, d, V = 64, 64, 300
@@ -371,6 +373,53 @@ def test_confident_and_hopeless_rows():
     R = definition(X, E, ids, q, ent, w, 1.0)
     assert R["row"].max() > 300 and R["row"].min() < 1e-6
     check(ppu.ppu_head_xent(Xt.cuda(), Et.cuda(), torch.from_numpy(target).cuda()), R, tolerances(X, E, q, w, 1.0, R, ent))
+
+
+@gpu
+@pytest.mark.parametrize("shift", [-90.0, -45.0, 45.0, 90.0])
+def test_logits_far_from_zero(shift):
+    """Rows whose logits all lie far from zero, rows with some pieces there, and ordinary rows together."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    T, d, V = 200, 72, 1003
+    rng = np.random.default_rng(int(shift) + 100)
+    E = rng.standard_normal((V, d)) * (3.0 / math.sqrt(d))
+    E[:, 0] = 1.0                          # a row's first value is added to all of its logits
+    E[:, 1] = np.where(np.arange(V) // 64 % 3 == 1, 1.0, 0.0)      # the second to every third piece's
+    Et, E = bf16(E)
+    x = rng.standard_normal((T, d))
+    x[:, 0] = np.where(np.arange(T) % 2 == 0, shift, 0.0)
+    x[:, 1] = np.where(np.arange(T) % 3 == 0, -shift, 0.0)
+    Xt, X = bf16(x)
+    target = rng.integers(0, V, T).astype(np.int32)
+    target[5::9] = -1
+    ids, q, ent, there = hard(target)
+    w = mean_weights(there)
+    R = definition(X, E, ids, q, ent, w, 1.0)
+    tol = tolerances(X, E, q, w, 1.0, R, ent)
+    R["row"] *= there
+    tol["row"] *= there
+    check(ppu.ppu_head_xent(Xt.cuda(), Et.cuda(), torch.from_numpy(target).cuda()), R, tol)
+
+
+@gpu
+def test_rows_that_do_not_count_may_hold_anything():
+    import torch
+    from paper_2509_22418_b200 import ppu
+    _, Xt, _, Et, _, target = make(300, 72, 1003, seed=14)
+    target[::4] = -1
+    tt = torch.from_numpy(target).cuda()
+    Xz = Xt.clone()
+    Xz[::4] = 0
+    ref = ppu.ppu_head_xent(Xz, Et, tt)
+    for junk in (float("nan"), float("inf"), 3e38):
+        Xj = Xt.clone()
+        Xj[::4] = junk
+        for chunk in (0, 256):
+            got = ppu.ppu_head_xent(Xj, Et, tt, chunk_rows=chunk)
+            ref = ppu.ppu_head_xent(Xz, Et, tt, chunk_rows=chunk)
+            for i in (0, 1, 3, 4):
+                assert torch.equal(got[i], ref[i]), (junk, i)
 
 
 @gpu
