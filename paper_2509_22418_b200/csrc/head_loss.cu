@@ -34,7 +34,6 @@ int ppu_fail(int code, const char* fmt, ...);
 
 namespace {
 
-constexpr int ROW_THREADS = 128;
 constexpr int MAX_ENTRIES = PPU_MAX_TEACHER_ENTRIES;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -57,7 +56,7 @@ struct RowArgs {
   float *row_loss, *lse, *weighted;      // per row; the first two may be null
   float* factor;                         // f, of this chunk's rows
   bf16* fx;                              // f X [rows][d], or null
-  unsigned* done; float* loss;           // rows finished so far; sum of `weighted`, by the last of them
+  unsigned *done, blocks; float* loss;   // blocks finished so far, and all there will be; sum of `weighted`, by the last of them
   int* flags;
 };
 
@@ -76,7 +75,7 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-__device__ __forceinline__ void unpack8(const uint4& u, float* f) {
+__device__ __forceinline__ void unpack8(const uint4 u, float* f) {
   const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&u);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -132,174 +131,228 @@ __device__ __forceinline__ void scale_piece(bf16* p, float f) {
   }
 }
 
-template <bool GRAD>
-__global__ void __launch_bounds__(ROW_THREADS) head_rows_kernel(const RowArgs a) {
-  __shared__ int s_id[MAX_ENTRIES];
-  __shared__ float s_q[MAX_ENTRIES], s_l[MAX_ENTRIES];
-  __shared__ float s_total, s_entropy;
-  __shared__ int s_any, s_last;
-  __shared__ Piece s_piece[ROW_THREADS / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t row = blockIdx.x, t = a.row0 + row;   // row of the chunk, of the call
+// Step 2 for W warps to a row: one (four rows to a block, no barrier) where the rows alone fill the
+// machine, 4 or 16 for few rows with many pieces or entries to go through.
+template <bool GRAD, int W>
+__global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const RowArgs a, int rows) {
+  constexpr int R = W == 1 ? 4 : 1, THREADS = W == 1 ? 128 : 32 * W, N = 32 * W;     // rows and threads of a block, threads of a row
+  __shared__ int s_id[R][MAX_ENTRIES];
+  __shared__ float s_q[R][MAX_ENTRIES], s_l[R][MAX_ENTRIES];
+  __shared__ float s_total[R], s_entropy[R], s_sum[16];
+  __shared__ int s_any[R], s_last;
+  __shared__ Piece s_piece[W];
+  const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5, tid = W == 1 ? lane : threadIdx.x;   // of the row
+  const int g = W == 1 ? threadIdx.x >> 5 : 0;
+  const int64_t row = (int64_t)blockIdx.x * R + g, t = a.row0 + row;        // row of the chunk, of the call
   const int k = a.tg.k;
+  auto sync = [] { if constexpr (W == 1) __syncwarp(); else __syncthreads(); };
 
-  // the row's entries and their q (warp 0), while every thread joins its share of the pieces
-  if (warp == 0) {
-    constexpr int PER = MAX_ENTRIES / 32;
-    float zs[PER]; int id[PER]; bool in[PER];
-    float top = -INFINITY;
-    bool any = false;
+  if (row < rows) {
+    // the row's entries and their q
+    if (warp == 0) {
+      constexpr int PER = MAX_ENTRIES / 32;
+      float zs[PER]; int id[PER]; bool in[PER];
+      float top = -INFINITY;
+      bool any = false;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int j = lane + 32 * i;
-      id[i] = -1; zs[i] = 0.f; in[i] = false;
-      if (j < k) {
-        id[i] = a.tg.ids[t * a.tg.ld_ids + j];
-        in[i] = present_id(id[i], a.V, a.flags);
-        if (in[i] && a.tg.z) {
-          zs[i] = a.tg.z[t * a.tg.ld_z + j] * a.tg.inv_temp;
-          in[i] = !(zs[i] == -INFINITY);
+      for (int i = 0; i < PER; ++i) {
+        const int j = lane + 32 * i;
+        id[i] = -1; zs[i] = 0.f; in[i] = false;
+        if (j < k) {
+          id[i] = a.tg.ids[t * a.tg.ld_ids + j];
+          in[i] = present_id(id[i], a.V, a.flags);
+          if (in[i] && a.tg.z) {
+            zs[i] = a.tg.z[t * a.tg.ld_z + j] * a.tg.inv_temp;
+            in[i] = !(zs[i] == -INFINITY);
+          }
+        }
+        if (in[i]) { top = fmaxf(top, zs[i]); any = true; }
+      }
+      any = __any_sync(0xffffffffu, any);
+      float norm = 0.f;                    // a hard target: q = exp(0)
+      if (a.tg.z) {
+        if (a.tg.teacher_lse) norm = a.tg.teacher_lse[t];
+        else {
+          top = warp_max(top);
+          float s = 0.f;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) if (in[i]) s += expf(zs[i] - top);
+          norm = top + logf(warp_sum(s));
         }
       }
-      if (in[i]) { top = fmaxf(top, zs[i]); any = true; }
-    }
-    any = __any_sync(0xffffffffu, any);
-    float norm = 0.f;                      // a hard target: q = exp(0)
-    if (a.tg.z) {
-      if (a.tg.teacher_lse) norm = a.tg.teacher_lse[t];
-      else {
-        top = warp_max(top);
-        float s = 0.f;
+      float total = 0.f, entropy = 0.f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) if (in[i]) s += expf(zs[i] - top);
-        norm = top + logf(warp_sum(s));
-      }
-    }
-    float total = 0.f, entropy = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int j = lane + 32 * i;
-      float q = 0.f;
-      if (in[i]) {
-        q = expf(zs[i] - norm);
-        if (q != 0.f) entropy += q * (zs[i] - norm);
-        total += q;
-      }
-      if (j < k) { s_id[j] = in[i] ? id[i] : -1; s_q[j] = q; }
-    }
-    total = warp_sum(total); entropy = warp_sum(entropy);
-    if (lane == 0) { s_total = total; s_entropy = entropy; s_any = any; }
-  }
-  const float2* st = a.stats + row * a.ld_pieces;
-  Piece mine = {-INFINITY, 0.f};
-  for (int i = threadIdx.x; i < a.n_pieces; i += ROW_THREADS) {
-    const float2 v = st[i];
-    if (v.y != 0.f) mine = join(mine, {v.x, v.y});
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Piece other = {__shfl_xor_sync(0xffffffffu, mine.m, o), __shfl_xor_sync(0xffffffffu, mine.s, o)};
-    mine = join(mine, other);
-  }
-  if (lane == 0) s_piece[warp] = mine;
-  __syncthreads();
-  Piece all = s_piece[0];
-#pragma unroll
-  for (int w = 1; w < ROW_THREADS / 32; ++w) all = join(all, s_piece[w]);
-  const float lse2 = all.m + log2f(all.s);          // base 2
-  if (threadIdx.x == 0 && a.lse) a.lse[t] = lse2 * LN2;
-
-  // the reference of the row's powers: 0, or where that is too far from their sum, the sum itself
-  const float ref = fabsf(lse2) <= PIECE_RANGE ? 0.f : lse2;
-  const uint4* xr = reinterpret_cast<const uint4*>(a.X + t * a.ldx);
-  bf16* ur = a.u + row * a.ldu;
-  uint4* fx = GRAD && a.fx ? reinterpret_cast<uint4*>(a.fx + row * a.d) : nullptr;
-  if (!s_any) {                                     // block-uniform: the row has no loss and no gradient
-    if (threadIdx.x == 0) {
-      if (a.row_loss) a.row_loss[t] = 0.f;
-      a.weighted[t] = 0.f;
-      if (GRAD) a.factor[row] = 0.f;
-    }
-    if (GRAD) {
-      if (!isfinite(all.s))                         // (0 times the powers has to be 0)
-        for (int i = threadIdx.x; i < a.ldu / 8; i += ROW_THREADS) reinterpret_cast<uint4*>(ur)[i] = make_uint4(0, 0, 0, 0);
-      if (fx)
-        for (int i = threadIdx.x; i < a.d / 8; i += ROW_THREADS) fx[i] = make_uint4(0, 0, 0, 0);
-    }
-  } else {
-    // the entries' logits, one warp each
-    for (int j = warp; j < k; j += ROW_THREADS / 32) {
-      if (s_id[j] < 0) continue;
-      const uint4* er = reinterpret_cast<const uint4*>(a.E + (int64_t)s_id[j] * a.lde);
-      float acc = 0.f;
-#pragma unroll 4
-      for (int i = lane; i < a.d / 8; i += 32) {
-        float x[8], e[8];
-        unpack8(xr[i], x); unpack8(er[i], e);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) acc = fmaf(x[c], e[c], acc);
-      }
-      acc = warp_sum(acc);
-      if (lane == 0) s_l[j] = acc * a.scale2;
-    }
-    __syncthreads();
-    const float w = a.weight ? a.weight[t] : 1.f / (float)*a.count;
-    const float c = w * a.tg.inv_temp * s_total;
-    const float f = c * exp2f(ref - lse2);
-    if (threadIdx.x == 0) {
-      float x = 0.f;
-      for (int j = 0; j < k; ++j)
-        if (s_id[j] >= 0 && s_q[j] != 0.f) x = fmaf(s_q[j], lse2 - s_l[j], x);
-      const float l = s_entropy + x * LN2;
-      if (a.row_loss) a.row_loss[t] = l;
-      a.weighted[t] = w * l;
-      if (GRAD) a.factor[row] = f;
-    }
-    if (GRAD) {
-      if (fx)
-        for (int i = threadIdx.x; i < a.d / 8; i += ROW_THREADS) {
-          float v[8];
-          unpack8(xr[i], v);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] *= f;
-          fx[i] = pack8(v);
-        }
-      // (seldom) powers that are relative to something else
-      for (int i = threadIdx.x; i < a.n_pieces; i += ROW_THREADS)
-        if (st[i].x != ref && st[i].y != 0.f) scale_piece(ur + (int64_t)i * PIECE, exp2f(st[i].x - ref));
-      __syncthreads();                              // those stand: overwrite the entries' places
-      for (int j = threadIdx.x; j < k; j += ROW_THREADS) {
-        const int id = s_id[j];
-        if (id < 0) continue;
+      for (int i = 0; i < PER; ++i) {
+        const int j = lane + 32 * i;
         float q = 0.f;
-        bool first = true;                          // an id given twice: its first entry writes for all
-        for (int i = 0; i < k; ++i)
-          if (s_id[i] == id) { if (i < j) first = false; q += s_q[i]; }
-        // p - q / Q with p = exp(x): (exp(x) - 1) + (1 - q / Q) keeps its digits where p is next to 1
-        if (first && s_total != 0.f)
-          ur[id] = __float2bfloat16_rn((expm1f((s_l[j] - lse2) * LN2) + (s_total - q) / s_total) * exp2f(lse2 - ref));
+        if (in[i]) {
+          q = expf(zs[i] - norm);
+          if (q != 0.f) entropy += q * (zs[i] - norm);
+          total += q;
+        }
+        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; }
+      }
+      total = warp_sum(total); entropy = warp_sum(entropy);
+      if (lane == 0) { s_total[g] = total; s_entropy[g] = entropy; s_any[g] = any; }
+    }
+    // the pieces: with the common reference throughout, a plain sum
+    const float2* st = a.stats + row * a.ld_pieces;
+    Piece all = {0.f, 0.f};
+    bool plain = true;
+#pragma unroll 4
+    for (int i = tid; i < a.n_pieces; i += N) {
+      const float2 v = st[i];
+      plain &= v.x == 0.f;
+      all.s += v.y;
+    }
+    if constexpr (W == 1) plain = __all_sync(0xffffffffu, plain);
+    else plain = __syncthreads_and(plain);
+    if (plain) {
+      all.s = warp_sum(all.s);
+    } else {
+      all = {-INFINITY, 0.f};
+      for (int i = tid; i < a.n_pieces; i += N) {
+        const float2 v = st[i];
+        if (v.y != 0.f) all = join(all, {v.x, v.y});
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+        all = join(all, {__shfl_xor_sync(0xffffffffu, all.m, o), __shfl_xor_sync(0xffffffffu, all.s, o)});
+    }
+    if constexpr (W > 1) {
+      if (lane == 0) s_piece[warp] = all;
+      __syncthreads();
+      all = s_piece[0];
+      for (int w = 1; w < W; ++w) all = join(all, s_piece[w]);
+    } else {
+      __syncwarp();
+    }
+    const float lse2 = all.m + log2f(all.s);        // base 2
+    if (tid == 0 && a.lse) a.lse[t] = lse2 * LN2;
+
+    // the reference of the row's powers: 0, or where that is too far from their sum, the sum itself
+    const float ref = fabsf(lse2) <= PIECE_RANGE ? 0.f : lse2;
+    const uint4* xr = reinterpret_cast<const uint4*>(a.X + t * a.ldx);
+    bf16* ur = a.u + row * a.ldu;
+    uint4* fx = GRAD && a.fx ? reinterpret_cast<uint4*>(a.fx + row * a.d) : nullptr;
+    if (!s_any[g]) {                                // the row has no loss and no gradient
+      if (tid == 0) {
+        if (a.row_loss) a.row_loss[t] = 0.f;
+        a.weighted[t] = 0.f;
+        if (GRAD) a.factor[row] = 0.f;
+      }
+      if (GRAD) {
+        if (!isfinite(all.s))                       // (0 times the powers has to be 0)
+          for (int i = tid; i < a.ldu / 8; i += N) reinterpret_cast<uint4*>(ur)[i] = make_uint4(0, 0, 0, 0);
+        if (fx)
+          for (int i = tid; i < a.d / 8; i += N) fx[i] = make_uint4(0, 0, 0, 0);
+      }
+    } else {
+      // the entries' logits, two to a warp at a time: their rows of E come from anywhere in HBM, so loads in flight count
+      const int n8 = a.d / 8;
+      for (int j = 2 * warp; j < k; j += 2 * W) {
+        const bool two = j + 1 < k;
+        const int i0 = max(s_id[g][j], 0), i1 = two ? max(s_id[g][j + 1], 0) : i0;
+        const uint4* e0 = reinterpret_cast<const uint4*>(a.E + (int64_t)i0 * a.lde);
+        const uint4* e1 = reinterpret_cast<const uint4*>(a.E + (int64_t)i1 * a.lde);
+        float d0 = 0.f, d1 = 0.f;
+        if (two) {
+#pragma unroll 4
+          for (int i = lane; i < n8; i += 32) {
+            const uint4 xv = xr[i], v0 = e0[i], v1 = e1[i];
+            float x[8], e[8];
+            unpack8(xv, x);
+            unpack8(v0, e);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) d0 = fmaf(x[c], e[c], d0);
+            unpack8(v1, e);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) d1 = fmaf(x[c], e[c], d1);
+          }
+        } else {
+#pragma unroll 4
+          for (int i = lane; i < n8; i += 32) {
+            const uint4 xv = xr[i], v0 = e0[i];
+            float x[8], e[8];
+            unpack8(xv, x);
+            unpack8(v0, e);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) d0 = fmaf(x[c], e[c], d0);
+          }
+        }
+        d0 = warp_sum(d0);
+        if (two) d1 = warp_sum(d1);
+        if (lane == 0) {
+          s_l[g][j] = d0 * a.scale2;
+          if (two) s_l[g][j + 1] = d1 * a.scale2;
+        }
+      }
+      sync();
+      const float w = a.weight ? a.weight[t] : 1.f / (float)*a.count;
+      const float total = s_total[g];
+      const float f = w * a.tg.inv_temp * total * exp2f(ref - lse2);
+      if (warp == 0) {
+        float x = 0.f;
+        for (int j = lane; j < k; j += 32)
+          if (s_id[g][j] >= 0 && s_q[g][j] != 0.f) x = fmaf(s_q[g][j], lse2 - s_l[g][j], x);
+        x = warp_sum(x);
+        if (lane == 0) {
+          const float l = s_entropy[g] + x * LN2;
+          if (a.row_loss) a.row_loss[t] = l;
+          a.weighted[t] = w * l;
+          if (GRAD) a.factor[row] = f;
+        }
+      }
+      if (GRAD) {
+        if (fx)
+#pragma unroll 4
+          for (int i = tid; i < n8; i += N) {
+            const uint4 xv = xr[i];
+            float v[8];
+            unpack8(xv, v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] *= f;
+            fx[i] = pack8(v);
+          }
+        if (!plain || ref != 0.f) {                 // (seldom) powers that are relative to something else
+          for (int i = tid; i < a.n_pieces; i += N) {
+            const float2 v = st[i];
+            if (v.x != ref && v.y != 0.f) scale_piece(ur + (int64_t)i * PIECE, exp2f(v.x - ref));
+          }
+          sync();
+        }
+        for (int j = tid; j < k; j += N) {          // those stand: overwrite the entries' places
+          const int id = s_id[g][j];
+          if (id < 0) continue;
+          float q = 0.f;
+          bool first = true;                        // an id given twice: its first entry writes for all
+          for (int i = 0; i < k; ++i)
+            if (s_id[g][i] == id) { if (i < j) first = false; q += s_q[g][i]; }
+          // p - q / Q with p = exp(x): (exp(x) - 1) + (1 - q / Q) keeps its digits where p is next to 1
+          if (first && total != 0.f)
+            ur[id] = __float2bfloat16_rn((expm1f((s_l[g][j] - lse2) * LN2) + (total - q) / total) * exp2f(lse2 - ref));
+        }
       }
     }
   }
-  // the last row adds up the losses, in the same order whichever row that is
+  // the last block adds up the losses, in the same order whichever block that is
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
-    s_last = atomicAdd(a.done, 1u) == (unsigned)a.T - 1u;
+    s_last = atomicAdd(a.done, 1u) == a.blocks - 1u;
   }
   __syncthreads();
   if (!s_last) return;
   __threadfence();
   float s = 0.f;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < a.T; i += ROW_THREADS) s += __ldcg(a.weighted + i);
+  for (int i = threadIdx.x; i < a.T; i += THREADS) s += __ldcg(a.weighted + i);
   s = warp_sum(s);
-  __syncthreads();
-  if (lane == 0) s_q[warp] = s;
+  if (lane == 0) s_sum[threadIdx.x >> 5] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
     s = 0.f;
-    for (int i = 0; i < ROW_THREADS / 32; ++i) s += s_q[i];
+    for (int i = 0; i < THREADS / 32; ++i) s += s_sum[i];
     *a.loss = s;
   }
 }
@@ -339,7 +392,7 @@ int splits_for(int64_t M, int64_t N, int64_t K) {
 }
 
 struct Plan {
-  int64_t ldu, n_pieces, chunk;
+  int64_t ldu, n_pieces, chunk, usual;         // usual: rows of a chunk by default (decides orders of sums: results do not depend on chunk_rows)
   int chunks, sx, se;                          // split-K factors of dX and dE
   size_t off_weighted, off_factor, off_stats, off_u, off_fx, off_acc, off_part, bytes;
 };
@@ -349,7 +402,9 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
   p.n_pieces = p.ldu / PIECE;
   const int64_t row_bytes = want ? p.ldu * 2 : p.n_pieces * 8;     // (without gradients only the pieces' statistics)
   T = std::max(T, 1);
-  int64_t c = chunk_rows > 0 ? round_up(chunk_rows, 256) : std::max<int64_t>(256, U_BYTES / row_bytes / 256 * 256);
+  p.usual = std::max<int64_t>(256, U_BYTES / row_bytes / 256 * 256);
+  int64_t c = chunk_rows > 0 ? round_up(chunk_rows, 256) : p.usual;
+  p.usual = std::min<int64_t>(p.usual, T);
   p.chunks = (int)std::max<int64_t>(1, (T + c - 1) / c);
   p.chunk = p.chunks == 1 ? T : round_up((T + p.chunks - 1) / p.chunks, 256);
   p.sx = (want & 1) ? splits_for(p.chunk, d, V) : 1;
@@ -402,6 +457,21 @@ struct HeadCall {
     const int r_ = (call);                                                               \
     if (r_) return ppu_fail(r_ == -4 ? PPU_ESHAPE : PPU_ECUDA, "head product failed (%d)", r_); \
   } while (0)
+
+// warps to a row: enough that the rows fill the machine, no more than there are pairs of entries or
+// 64 pieces a lane to share (24 rows, 64 entries, 32768 ids: FEW16 us with 16 warps, FEW1 with one; 4096 rows of
+// 32 entries: MANY1 with one, MANY4 with four)
+int warps_for(int64_t rows, int k, int64_t n_pieces) {
+  const int64_t share = std::max<int64_t>(k / 2, n_pieces / 256);
+  if (rows >= 32 * SMS || share < 4) return 1;
+  return rows >= 8 * SMS || share < 16 ? 4 : 16;
+}
+template <bool GRAD>
+void launch_rows(const RowArgs& r, int64_t rows, int warps, cudaStream_t st) {
+  if (warps == 1) head_rows_kernel<GRAD, 1><<<(unsigned)((rows + 3) / 4), 128, 0, st>>>(r, (int)rows);
+  else if (warps == 4) head_rows_kernel<GRAD, 4><<<(unsigned)rows, 128, 0, st>>>(r, (int)rows);
+  else head_rows_kernel<GRAD, 16><<<(unsigned)rows, 512, 0, st>>>(r, (int)rows);
+}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -461,6 +531,10 @@ int run_head(const HeadCall& c) {
   r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = count;
   r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
   r.done = done; r.loss = c.loss; r.flags = c.flags;
+  const int warps = warps_for(p.usual, c.tg.k, p.n_pieces);
+  const int64_t per_block = warps == 1 ? 4 : 1;
+  r.blocks = 0;
+  for (int64_t c0 = 0; c0 < c.T; c0 += p.chunk) r.blocks += (unsigned)((std::min<int64_t>(p.chunk, c.T - c0) + per_block - 1) / per_block);
 
   GemmArgs g0;
   g0.C2 = nullptr; g0.aux = nullptr; g0.ldaux = 0; g0.flags = c.flags; g0.transient = true;
@@ -475,8 +549,8 @@ int run_head(const HeadCall& c) {
       GEMM_OK(launch_gemm_tc_pieces(g, c.st));
     }
     r.row0 = c0;
-    if (want) head_rows_kernel<true><<<(unsigned)rows, ROW_THREADS, 0, c.st>>>(r);
-    else head_rows_kernel<false><<<(unsigned)rows, ROW_THREADS, 0, c.st>>>(r);
+    if (want) launch_rows<true>(r, rows, warps, c.st);
+    else launch_rows<false>(r, rows, warps, c.st);
     if (c.dX) {
       GemmArgs g = g0;
       g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = r.E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;

@@ -54,7 +54,7 @@ __device__ __forceinline__ void cp8(uint32_t smem, const void* gmem) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ void from_bf4(const uint2& u, float* f) {
+__device__ __forceinline__ void from_bf4(const uint2 u, float* f) {
   const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
   const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
   f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
@@ -430,31 +430,35 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(con
 }
 
 // parameter gradients from the units' partial sums: blockIdx.y = 0..3 the norms' gains and shifts over
-// all units, 4 + g the gate's row g over the units of its group; a warp adds a 32nd of them in order, and
-// the 32 sums are added in order
+// all units, 4 + g the gate's row g over the units of its group.  A block takes 128 columns (4 to a lane), a warp
+// adds a 32nd of the units in order, and the 32 sums are added in order.
 struct ParamOut { float* out[4]; float* dgate; };
-__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* partial, ParamOut po, int units, int per_group, int d) {
-  __shared__ float sh[32][33];
+__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* __restrict__ partial, const ParamOut po, int units, int per_group, int d) {
+  __shared__ float4 sh[32][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + lane;
+  const int c = blockIdx.x * 128 + 4 * lane;
   const int which = min((int)blockIdx.y, 4), g = (int)blockIdx.y - 4;
-  float* out = which < 4 ? po.out[which] : po.dgate + (int64_t)g * d;
-  if (which < 4 && !out) return;
+  float* out = which == 0 ? po.out[0] : which == 1 ? po.out[1] : which == 2 ? po.out[2] : which == 3 ? po.out[3] : po.dgate + (int64_t)g * d;
+  if (!out) return;
   const int n = which < 4 ? units : per_group, first = which < 4 ? 0 : g * per_group;
   const float* p = partial + ((int64_t)which * units + first) * d + c;
   const int per = (n + 31) / 32, b0 = w * per, b1 = min(n, b0 + per);
-  float s = 0.f;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < d) {
 #pragma unroll 8
-    for (int b = b0; b < b1; ++b) s += p[(int64_t)b * d];
+    for (int b = b0; b < b1; ++b) {
+      const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)b * d);
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
   }
   sh[w][lane] = s;
   __syncthreads();
-  if (w == 0 && c < d) {
+  if (threadIdx.x < 128 && blockIdx.x * 128 + threadIdx.x < d) {
+    const float* col = reinterpret_cast<const float*>(sh) + threadIdx.x;
     float t = 0.f;
 #pragma unroll
-    for (int q = 0; q < 32; ++q) t += sh[q][lane];
-    out[c] = t;
+    for (int q = 0; q < 32; ++q) t += col[128 * q];
+    out[blockIdx.x * 128 + threadIdx.x] = t;
   }
 }
 
@@ -472,7 +476,7 @@ int lanes_for(int d, int ch) {
 Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
   Shape s;
   s.lanes = lanes_for(d, backward ? BWD_CH : FWD_CH);
-  const int threads = backward ? 512 : 768;
+  const int threads = 512;
   const int64_t target = std::min<int64_t>(16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (threads / s.lanes)));
   const int64_t groups = has_gate ? ((int64_t)T + gate_rows - 1) / gate_rows : 1;
   s.per_group = 0;
@@ -605,7 +609,7 @@ extern "C" int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void
   if (rc2) return rc2;
   const int groups = s.gate_mode == 1 ? s.units / s.per_group : 0;      // gate rows still to be summed
   const ParamOut po = {{dpost_gain, dpost_shift, dpre_gain, dpre_shift}, dgate};
-  norm_gate_params_kernel<<<dim3((d + 31) / 32, 4 + groups), 1024, 0, st>>>(a.partial, po, s.units, s.per_group, d);
+  norm_gate_params_kernel<<<dim3((d + 127) / 128, 4 + groups), 1024, 0, st>>>(a.partial, po, s.units, s.per_group, d);
   CUDA_OK(cudaGetLastError());
   return PPU_OK;
 }
