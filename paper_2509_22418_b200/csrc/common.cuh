@@ -25,8 +25,8 @@ enum GemmEpilogue {
   // x = acc * piece_scale, and piece_stats = {ref, sum of the unrounded powers}; ref is 0 where the
   // piece's largest x lies within +-PIECE_RANGE, else that largest x
   EPI_PIECES = 7,
-  EPI_RESID_BF16 = 8,  // C bf16 = aux fp32 + acc (launch_gemm_tc_resid_bf16 only)
-  EPI_SCALED_BF16 = 9  // C bf16 = row_scale[m] * acc (launch_gemm_tc_scaled_bf16 only)
+  // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_out_bf16 only)
+  EPI_OUT_BF16 = 8
 };
 constexpr int PIECE = 64;               // columns of one softmax piece
 constexpr float PIECE_RANGE = 60.f;
@@ -55,7 +55,7 @@ struct GemmArgs {
   // EPI_PIECES: piece_stats [M][ld_pieces]; C (leading dimension a multiple of PIECE) may be null,
   // columns of C from N up to the next multiple of PIECE are written as zeros
   float piece_scale = 1.f; float2* piece_stats = nullptr; int64_t ld_pieces = 0;
-  const float* row_scale = nullptr;  // EPI_SCALED_BF16: fp32 [M]
+  const float* row_scale = nullptr;  // EPI_OUT_BF16: fp32 [M]
   // operands that come and go (a caller's tensors): their tensor maps are encoded for this launch
   bool transient = false;
 };
@@ -63,8 +63,7 @@ struct GemmArgs {
 int launch_gemm_simt(const GemmArgs& g, cudaStream_t st);
 int launch_gemm_tc(const GemmArgs& g, cudaStream_t st);   // tcgen05 / TMEM / TMA
 int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st);      // EPI_PIECES, both operands K-major, any N
-int launch_gemm_tc_resid_bf16(const GemmArgs& g, cudaStream_t st);  // EPI_RESID_BF16, both operands MN-major
-int launch_gemm_tc_scaled_bf16(const GemmArgs& g, cudaStream_t st); // EPI_SCALED_BF16, A K-major, B MN-major
+int launch_gemm_tc_out_bf16(const GemmArgs& g, cudaStream_t st);    // EPI_OUT_BF16, B MN-major
 // whether launch_gemm_tc accepts EPI_DELTA_BF16 for this product (tile shape and alignment allow
 // a thread to own whole heads of its row); otherwise the caller runs launch_attn_delta
 bool gemm_tc_fuses_delta(const GemmArgs& g);

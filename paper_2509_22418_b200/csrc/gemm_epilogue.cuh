@@ -85,8 +85,13 @@ struct TcParams {
 };
 
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of
-// those that have instantiations of their own so that drain_cols keeps its registers
-enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_RESID_BF16 = 2, DRAIN_SCALED_BF16 = 3 };
+// those that have instantiations of their own: drain_cols keeps its registers, and these have 32 KB of
+// shared memory behind the operand stages, through which they store 64-column groups by TMA
+enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_OUT_BF16 = 2 };
+constexpr int STORE_BYTES = 32 * 128;                      // a warp's 32 rows x 64 bf16 columns
+template <int MODE> struct OutMap { CUtensorMap c; };
+template <> struct OutMap<DRAIN_COLS> {};
+template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : EPI_WARPS * STORE_BYTES; }
 
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows,
@@ -94,8 +99,8 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
 TcParams make_params(const GemmArgs& g);
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st);   // bn: 256 or 128
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st);
-int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
-int launch_gemm_tc_pair_scaled_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
+int launch_gemm_tc_pair_out_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
+bool encode_out_map(CUtensorMap* map, void* base, long long ld, int rows, int cols);   // for 32 x 64 boxes
 
 // Drains rows [m0 + 32 quarter, +32) x columns [n0 + half BN/2, + BN/2) of the accumulator at
 // TMEM column t_acc through registers into global memory, applying the epilogue p.epilogue.
@@ -300,6 +305,23 @@ __device__ __forceinline__ float ex2_fast(float x) {
   return y;
 }
 
+// A warp's 32 rows x 64 columns, packed by its lanes (one row each, 32 words), to global memory through
+// its 4 KB of shared memory.  Stored from the registers instead, a lane's 32 bytes of its own row at a
+// time, a warp's store touches 32 lines: 2304 x 32000 x 768 took 95 us against 70 without the store
+// (65 us for the store alone, 2.3 TB/s); so TMA_STORE_US.
+__device__ __forceinline__ void store_group(const CUtensorMap* map, uint32_t buf, const uint32_t* o, int x, int y, int lane) {
+  if (lane == 0) tma_store_wait_read();
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 8; ++j)       // the 16-byte pieces of a 128-byte row swap places as the swizzle has it
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(o[4 * j]),
+                 "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
+                 : "memory");
+  fence_async_smem();
+  __syncwarp();
+  if (lane == 0) tma_store_2d(map, buf, x, y);
+}
+
 // EPI_PIECES.  A lane holds 64 logits of its row at a time: x = acc * piece_scale (the scale holds
 // log2(e) and the temperature), e = 2^(x - ref).  The powers are stored in bf16 - a relative
 // rounding of half a step (2^-8) whatever the logit, where a bf16 logit of 16 would be off by 2^-4
@@ -310,15 +332,14 @@ __device__ __forceinline__ float ex2_fast(float x) {
 // are kept relative to their own maximum and brought into line afterwards.
 // The exponent is one fused multiply-add on the accumulator; ref is the rounded product used in it,
 // so its rounding cancels.
-__device__ __forceinline__ void drain_pieces(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
-                                             int c_begin, int c_end, int lane) {
-  const int m = m0 + quarter * 32 + lane;
-  const bool row_ok = m < p.M;
+__device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0,
+                                             uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
+  const int mw = m0 + quarter * 32, m = mw + lane;
   const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += PIECE) {
     const int nb = n0 + c0;
-    if (nb >= p.N) break;                  // warp-uniform
+    if (nb >= p.N || mw >= p.M) break;     // warp-uniform
     uint32_t r[PIECE];
     tmem_ld32(t_row + c0, r);
     tmem_ld32(t_row + c0 + 32, r + 32);
@@ -334,99 +355,61 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, int m0, int n0, 
     float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.piece_scale;
     if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t o[PIECE / 2];
 #pragma unroll
-    for (int j = 0; j < PIECE; ++j) {
-      const float e = ex2_fast(fmaf(__uint_as_float(r[j]), p.piece_scale, -top));
-      sum[j & 3] += e;
-      r[j] = __float_as_uint(e);
+    for (int j = 0; j < PIECE / 2; ++j) {
+      const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -top));
+      const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -top));
+      sum[(2 * j) & 3] += e0;
+      sum[(2 * j + 1) & 3] += e1;
+      o[j] = pack2_bf16(e0, e1);
     }
-    if (row_ok) {
+    if (m < p.M)
       p.piece_stats[(long long)m * p.ld_pieces + nb / PIECE] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-      if (p.C) {
-        bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t o[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) o[q] = pack2_bf16(__uint_as_float(r[16 * j + 2 * q]), __uint_as_float(r[16 * j + 2 * q + 1]));
-          st_v8(dst + 16 * j, o);
-        }
-      }
-    }
+    if (p.C) store_group(out, buf, o, nb, mw, lane);
   }
 }
 
-// EPI_RESID_BF16: the last partial sum of an fp32 running total, rounded once.  N is a multiple of 8,
-// aux rows are 32-byte aligned, output rows 16-byte aligned.
-__device__ __forceinline__ void drain_resid_bf16(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
-                                                 int c_begin, int c_end, int lane) {
-  const int m = m0 + quarter * 32 + lane;
+// EPI_OUT_BF16: row_scale * (aux + acc), rounded once.  aux: fp32 partial sums, rows 32-byte aligned;
+// N is a multiple of 8.
+__device__ __forceinline__ void drain_out_bf16(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0,
+                                               uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
+  const int mw = m0 + quarter * 32, m = mw + lane;
   const bool row_ok = m < p.M;
   const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
+  const float f = p.row_scale && row_ok ? __ldg(p.row_scale + m) : 1.f;
 #pragma unroll 1
-  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+  for (int c0 = c_begin; c0 < c_end; c0 += 64) {
     const int nb = n0 + c0;
-    if (nb >= p.N) break;                  // warp-uniform
-    uint32_t r[32], x[32];
+    if (nb >= p.N || mw >= p.M) break;     // warp-uniform
+    uint32_t r[64];
     tmem_ld32(t_row + c0, r);
-    const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb;
-    if (row_ok) {
+    tmem_ld32(t_row + c0 + 32, r + 32);
+    if (p.aux) {
+      const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb;
+      uint32_t x[64];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (nb + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
-    }
-    tmem_ld_wait();
-    if (row_ok) {
-      bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
+      for (int j = 0; j < 8; ++j)
+        if (row_ok && nb + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
+      tmem_ld_wait();
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (nb + 8 * j < p.N) {
-          float f[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] = __uint_as_float(x[8 * j + q]) + __uint_as_float(r[8 * j + q]);
-          *reinterpret_cast<uint4*>(dst + 8 * j) = pack8_bf16(f);
-        }
-      }
-    }
-  }
-}
-
-// EPI_SCALED_BF16: row_scale[m] * acc, rounded once.  N is a multiple of 8, output rows 16-byte aligned.
-__device__ __forceinline__ void drain_scaled_bf16(const TcParams& p, int m0, int n0, uint32_t t_acc, int quarter,
-                                                  int c_begin, int c_end, int lane) {
-  const int m = m0 + quarter * 32 + lane;
-  const bool row_ok = m < p.M;
-  const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
-  const float f = row_ok ? __ldg(p.row_scale + m) : 0.f;
-#pragma unroll 1
-  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
-    const int nb = n0 + c0;
-    if (nb >= p.N) break;                  // warp-uniform
-    uint32_t r[32];
-    tmem_ld32(t_row + c0, r);
-    tmem_ld_wait();
-    if (!row_ok) continue;
-    uint32_t o[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) o[j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
-    bf16* dst = (bf16*)p.C + (long long)m * p.ldc + nb;
-    if (p.wide && nb + 32 <= p.N) {
-      st_v8(dst, o);
-      st_v8(dst + 16, o + 8);
+      for (int j = 0; j < 64; ++j)
+        if (row_ok && nb + (j & ~7) < p.N) r[j] = __float_as_uint(__uint_as_float(x[j]) + __uint_as_float(r[j]));
     } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (nb + 8 * j < p.N) *reinterpret_cast<uint4*>(dst + 8 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+      tmem_ld_wait();
     }
+    uint32_t o[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) o[j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
+    store_group(out, buf, o, nb, mw, lane);
   }
 }
 
 template <int MODE>
-__device__ __forceinline__ void drain_mode(const TcParams& p, int m0, int n0, int sp, uint32_t t_acc, int quarter,
-                                           int c_begin, int c_end, int lane) {
-  if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
-  else if constexpr (MODE == DRAIN_RESID_BF16) drain_resid_bf16(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
-  else if constexpr (MODE == DRAIN_SCALED_BF16) drain_scaled_bf16(p, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+__device__ __forceinline__ void drain_mode(const TcParams& p, const OutMap<MODE>& out, uint32_t buf, int m0, int n0, int sp,
+                                           uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
+  if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, &out.c, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else if constexpr (MODE == DRAIN_OUT_BF16) drain_out_bf16(p, &out.c, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
   else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
 

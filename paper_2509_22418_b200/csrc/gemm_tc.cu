@@ -34,12 +34,12 @@ template <int BN> struct Cfg {
 template <int BN, bool A_K, bool B_K, int MODE>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-               const TcParams p) {
+               const __grid_constant__ OutMap<MODE> mapC, const TcParams p) {
   using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE_BYTES);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE_BYTES + store_smem<MODE>());
   // bars[0..ST): full, [ST..2ST): empty, [2ST..2ST+2): tmem_full, [2ST+2..2ST+4): tmem_empty
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -148,18 +148,21 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     // ---------------- epilogue warps ----------------
     const int quarter = warp & 3;              // TMEM lanes [32 q, 32 q + 32) belong to this warp
     const int half = (warp - 2) >> 2;          // which half of the tile's columns
+    const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
     for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
       const int sp = tile / tiles_mn, t2 = tile - sp * tiles_mn;
       const int m0 = (t2 % p.tiles_m) * BM, n0 = (t2 / p.tiles_m) * BN;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_mode<MODE>(p, m0, n0, sp, tmem_base + (uint32_t)(acc * BN), quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+      drain_mode<MODE>(p, mapC, store_buf, m0, n0, sp, tmem_base + (uint32_t)(acc * BN), quarter, half * (BN / 2),
+                       (half + 1) * (BN / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
+    if (MODE != DRAIN_COLS && lane == 0) tma_store_wait();
   }
 
   // ---------------- common exit ----------------
@@ -232,6 +235,14 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
   return true;
 }
 
+// output [rows, cols] bf16 with leading dimension ld, stored in boxes of 32 rows x 64 columns
+bool encode_out_map(CUtensorMap* map, void* base, long long ld, int rows, int cols) {
+  cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)ld * 2};
+  cuuint32_t box[2] = {64, 32}, estr[2] = {1, 1};
+  return tc::g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // launch parameters common to every tile shape (tile counts and split-K are set by the launcher)
 TcParams make_params(const GemmArgs& g) {
   TcParams p;
@@ -260,7 +271,7 @@ template <int BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_t(const GemmArgs& g, cudaStream_t st) {
   using C = Cfg<BN>;
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM)) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB;
   if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, BM, g.transient)) return -2;
   if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN, g.transient)) return -2;
@@ -273,7 +284,12 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
   const int n_sm = ppu_sm_count();
   const int grid = tiles < n_sm ? tiles : n_sm;
-  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, C::SMEM, st>>>(mapA, mapB, p);
+  OutMap<MODE> mapC;
+  if constexpr (MODE != DRAIN_COLS) {
+    mapC = {};
+    if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
+  }
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, C::SMEM + store_smem<MODE>(), st>>>(mapA, mapB, mapC, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -363,22 +379,12 @@ int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st) {
   return launch_t<128, true, true, DRAIN_PIECES>(g, st);
 }
 
-int launch_gemm_tc_resid_bf16(const GemmArgs& g, cudaStream_t st) {
+int launch_gemm_tc_out_bf16(const GemmArgs& g, cudaStream_t st) {
   if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
   if (gemm_tc_init() != 0) return -1;
-  if (!operands_ok(g) || g.a_kmajor || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || (g.ldaux % 8) || !g.aux ||
+  if (!operands_ok(g) || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || (g.aux && (g.ldaux % 8)) ||
       (reinterpret_cast<uintptr_t>(g.C) & 15) || (reinterpret_cast<uintptr_t>(g.aux) & 31))
     return -4;
-  if (picks_pair256(g)) return launch_gemm_tc_pair_resid_bf16(g, make_params(g), st);
-  return launch_t<128, false, false, DRAIN_RESID_BF16>(g, st);
-}
-
-int launch_gemm_tc_scaled_bf16(const GemmArgs& g, cudaStream_t st) {
-  if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
-  if (gemm_tc_init() != 0) return -1;
-  if (!operands_ok(g) || !g.a_kmajor || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || !g.row_scale ||
-      (reinterpret_cast<uintptr_t>(g.C) & 15))
-    return -4;
-  if (picks_pair256(g)) return launch_gemm_tc_pair_scaled_bf16(g, make_params(g), st);
-  return launch_t<128, true, false, DRAIN_SCALED_BF16>(g, st);
+  if (picks_pair256(g)) return launch_gemm_tc_pair_out_bf16(g, make_params(g), st);
+  return g.a_kmajor ? launch_t<128, true, false, DRAIN_OUT_BF16>(g, st) : launch_t<128, false, false, DRAIN_OUT_BF16>(g, st);
 }

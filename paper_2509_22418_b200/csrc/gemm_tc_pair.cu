@@ -116,13 +116,14 @@ __device__ __forceinline__ PairUnit pair_unit(const TcParams& p, int u, int num_
 template <int PAIR_BN, bool A_K, bool B_K, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-                    const __grid_constant__ CUtensorMap mapB2, const TcParams p) {
+                    const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ OutMap<MODE> mapC,
+                    const TcParams p) {
   using PC = PairCfg<PAIR_BN>;
   constexpr int ST = PC::STAGES, PAIR_STAGE_BYTES = PC::STAGE_BYTES, HALF_BYTES = PC::A_HALF, B_SLAB = PC::B_SLAB;
   extern __shared__ uint8_t smem_raw[];
   // the dynamic window starts at the same offset in both CTAs, so aligned offsets match too
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ST * PAIR_STAGE_BYTES);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ST * PAIR_STAGE_BYTES + store_smem<MODE>());
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * ST + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -242,19 +243,21 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     // ---------------- epilogue warps (both CTAs, 128 rows each) ----------------
     const int quarter = warp & 3;
     const int half = (warp - 2) >> 2;
+    const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
     for (int u = pair; u < num_units; u += n_pairs) {
       const PairUnit w = pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_mode<MODE>(p, m0, w.n0, w.sp, tmem_base + (uint32_t)(acc * PAIR_BN), quarter, half * (w.bn / 2),
-                       (half + 1) * (w.bn / 2), lane);
+      drain_mode<MODE>(p, mapC, store_buf, m0, w.n0, w.sp, tmem_base + (uint32_t)(acc * PAIR_BN), quarter,
+                       half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
+    if (MODE != DRAIN_COLS && lane == 0) tma_store_wait();
   }
 
   // ---------------- common exit ----------------
@@ -273,7 +276,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 template <int PAIR_BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM)) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB, mapB2;
   if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient)) return -2;
   if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient)) return -2;
@@ -309,7 +312,13 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   }
   mapB2 = mapB;
   if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, PairCfg<PAIR_BN>::SMEM, st>>>(mapA, mapB, mapB2, p);
+  OutMap<MODE> mapC;
+  if constexpr (MODE != DRAIN_COLS) {
+    mapC = {};
+    if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
+  }
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>
+      <<<2 * pairs, GEMM_THREADS, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>(), st>>>(mapA, mapB, mapB2, mapC, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -332,10 +341,8 @@ int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
   return launch_pair_t<256, true, true, DRAIN_PIECES>(g, p, st);
 }
-int launch_gemm_tc_pair_resid_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
-  return launch_pair_t<256, false, false, DRAIN_RESID_BF16>(g, p, st);
-}
-int launch_gemm_tc_pair_scaled_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
-  return launch_pair_t<256, true, false, DRAIN_SCALED_BF16>(g, p, st);
+int launch_gemm_tc_pair_out_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
+  return g.a_kmajor ? launch_pair_t<256, true, false, DRAIN_OUT_BF16>(g, p, st)
+                    : launch_pair_t<256, false, false, DRAIN_OUT_BF16>(g, p, st);
 }
 }  // namespace gemm_tc_detail

@@ -383,12 +383,12 @@ constexpr int SMS = 148;                      // work is split for a B200 (also 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // slices of the reduction for a [M, N] product over K: as many as bring the output's tiles near one
-// wave, each at least 256 long
+// wave, each at least 1024 long (the partial products cost a launch of their own)
 int splits_for(int64_t M, int64_t N, int64_t K) {
   const int64_t pair = ((M + 255) / 256) * ((N + 255) / 256);
   int64_t tiles = pair, units = SMS / 2;
   if (M <= 128 || N <= 128 || pair < 16) { tiles = ((M + 127) / 128) * ((N + 127) / 128); units = SMS; }
-  return (int)std::max<int64_t>(1, std::min<int64_t>(units / tiles, K / 256));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(units / tiles, K / 1024));
 }
 
 struct Plan {
@@ -478,8 +478,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 // bf16 C = A . B^T (times row_scale), split over K into fp32 partials where that fills the machine
 int product_bf16(GemmArgs g, int splits, float* part, cudaStream_t st) {
   if (splits <= 1) {
-    g.epilogue = g.row_scale ? EPI_SCALED_BF16 : EPI_STORE_BF16;
-    GEMM_OK(g.row_scale ? launch_gemm_tc_scaled_bf16(g, st) : launch_gemm_tc(g, st));
+    g.epilogue = EPI_OUT_BF16;
+    GEMM_OK(launch_gemm_tc_out_bf16(g, st));
     return PPU_OK;
   }
   bf16* out = (bf16*)g.C; const int64_t ldo = g.ldc;
@@ -567,8 +567,8 @@ int run_head(const HeadCall& c) {
         rc = product_bf16(g, p.se, part, c.st);
         if (rc) return rc;
       } else if (last) {
-        g.epilogue = EPI_RESID_BF16; g.aux = acc; g.ldaux = c.d;
-        GEMM_OK(launch_gemm_tc_resid_bf16(g, c.st));
+        g.epilogue = EPI_OUT_BF16; g.aux = acc; g.ldaux = c.d;
+        GEMM_OK(launch_gemm_tc_out_bf16(g, c.st));
       } else {
         g.epilogue = c0 == 0 ? EPI_STORE_F32 : EPI_RESID_F32;
         g.C = acc; g.ldc = c.d; g.aux = acc; g.ldaux = c.d;
