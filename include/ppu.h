@@ -326,8 +326,8 @@ int ppu_attention_bwd_static(const void* qkv, const void* U, const float* lse, c
  * loss: fp32 [1].  row_loss, lse: fp32 [T] or null.  dX: bf16 [T,d] (row stride lddx) or null; dE: bf16
  * [V,d] (row stride ldde) or null; both are written, not added to, and overlap no input.  d is a
  * multiple of 8 up to 16384, row strides multiples of 8, X, E, dX, dE 16-byte aligned; T <= 2^20,
- * V <= 2^22, any values within.  chunk_rows: 0 = as many as keep 256 MiB of softmax, else rows of a
- * chunk (rounded up to a multiple of 256); larger chunks are faster.  workspace: DEVICE, 256-byte
+ * V <= 2^22, any values within.  chunk_rows: 0 = up to 6144, as many as keep 1 GiB of softmax,
+ * else the rows of a chunk (rounded up to a multiple of 256); chunks below 4096 rows are slower.  workspace: DEVICE, 256-byte
  * aligned, of the size ppu_head_query_bytes gives for the same T, d, V, gradients (1: dX, 2: dE) and
  * chunk_rows; calls that may overlap on the GPU need one each.  flags: DEVICE int32 [8], zeroed by the
  * caller once, or null (nothing is reported); read by ppu_op_status.  All other pointers DEVICE.

@@ -55,6 +55,7 @@ struct GemmArgs {
   // EPI_PIECES: piece_stats [M][ld_pieces]; C (leading dimension a multiple of PIECE) may be null,
   // columns of C from N up to the next multiple of PIECE are written as zeros
   float piece_scale = 1.f; float2* piece_stats = nullptr; int64_t ld_pieces = 0;
+  unsigned* zero_word = nullptr;     // EPI_PIECES: a word that the launch sets to 0 (a counter of the kernel after it), or null
   const float* row_scale = nullptr;  // EPI_OUT_BF16: fp32 [M]
   // operands that come and go (a caller's tensors): their tensor maps are encoded for this launch
   bool transient = false;

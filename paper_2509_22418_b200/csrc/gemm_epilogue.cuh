@@ -77,11 +77,16 @@ struct TcParams {
   int tail_from;   // SM-pair kernel: tiles from this index on are worked as two 128-column halves
   int n_fastest;   // SM-pair kernel: consecutive tile indices walk along N (else along M)
   int splits; long long split_stride;
+  // Boxes no larger than the operands need: rows of A (K-major, one CTA to a tile: M below 128), k rows of MN-major
+  // operands and products along k (K below 64).  Rows outside a tensor cost the TMA unit more than rows inside:
+  // 24 x 32768 x 2048 took 42 us with 104 of 128 rows filled in, 36 us with 128 real rows,
+  // 34 us with a box of 24.
+  int a_rows, k_rows;
   int wide;   // every output / auxiliary row start is 32-byte aligned: use 32-byte accesses
   int rope_S, rope_dh, rope_cols;
   void* C3; long long ldc3; int c3_lo, c3_hi;
   float piece_scale; float2* piece_stats; long long ld_pieces;
-  const float* row_scale;
+  const float* row_scale; unsigned* zero_word;
 };
 
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of
@@ -95,7 +100,7 @@ template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 :
 
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows,
-                bool transient = false);
+                bool transient = false, int k_rows = BK);
 TcParams make_params(const GemmArgs& g);
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st);   // bn: 256 or 128
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st);

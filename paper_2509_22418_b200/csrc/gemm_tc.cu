@@ -55,6 +55,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
     *abort_flag = 0;
+    if (MODE == DRAIN_PIECES && blockIdx.x == 0 && p.zero_word) *p.zero_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -73,6 +74,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer ----------------
+      const uint32_t a_bytes = A_K ? p.a_rows * 128 : (BM / 64) * p.k_rows * 128;
+      const uint32_t b_bytes = B_K ? C::B_BYTES : (BN / 64) * p.k_rows * 128;
       int s = 0; uint32_t ph = 0;
       for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
         const int sp = tile / tiles_mn, t2 = tile - sp * tiles_mn;
@@ -85,7 +88,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
           if (!ok) break;
           const uint32_t a_dst = smem_u32(smem + s * C::STAGE_BYTES);
           const uint32_t b_dst = a_dst + C::A_BYTES;
-          mbar_expect_tx(full_bar(s), C::STAGE_BYTES);
+          mbar_expect_tx(full_bar(s), a_bytes + b_bytes);
           if (A_K) {
             tma_load_2d(a_dst, &mapA, full_bar(s), kb * BK, m0);
           } else {
@@ -126,10 +129,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
           ok = mbar_wait(full_bar(s), ph, abort_flag, p.flags);
           if (!ok) break;
           tc_fence_after();
+          // (rows of A past a smaller box are what was there before: rows of the accumulator that are not stored)
           const uint32_t a_addr = smem_u32(smem + s * C::STAGE_BYTES);
           const uint32_t b_addr = a_addr + C::A_BYTES;
 #pragma unroll
           for (int k = 0; k < BK / UMMA_K; ++k) {
+            if (k * UMMA_K >= p.k_rows) break;
             const uint64_t adesc = A_K ? make_desc(a_addr + k * 32, 16, 1024)
                                        : make_desc(a_addr + k * 2048, 8192, 1024);
             const uint64_t bdesc = B_K ? make_desc(b_addr + k * 32, 16, 1024)
@@ -205,7 +210,7 @@ constexpr size_t MAP_CACHE_LIMIT = 1 << 16;
 using namespace mapcache;
 
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K,
-                int box_rows, bool transient) {
+                int box_rows, bool transient, int k_rows) {
   const MapKey key{base, ld, kmajor ? 1 : 0, rows, K, box_rows};
   if (!transient) {
     std::lock_guard<std::mutex> lk(g_maps_lock);
@@ -222,7 +227,7 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
     box[0] = BK; box[1] = (cuuint32_t)box_rows;
   } else {
     gdim[0] = (cuuint64_t)rows; gdim[1] = (cuuint64_t)K;
-    box[0] = 64; box[1] = BK;
+    box[0] = 64; box[1] = (cuuint32_t)k_rows;
   }
   CUresult r = tc::g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)base, gdim, gstride, box,
                         estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -248,10 +253,12 @@ TcParams make_params(const GemmArgs& g) {
   TcParams p;
   p.M = g.M; p.N = g.N; p.K = g.K; p.epilogue = g.epilogue;
   p.C = g.C; p.ldc = g.ldc; p.C2 = g.C2; p.aux = g.aux; p.ldaux = g.ldaux; p.flags = g.flags;
+  p.a_rows = BM;
+  p.k_rows = g.K < BK && !(g.a_kmajor && g.b_kmajor) ? (g.K + UMMA_K - 1) / UMMA_K * UMMA_K : BK;
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
   p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
-  p.row_scale = g.row_scale;
+  p.row_scale = g.row_scale; p.zero_word = g.zero_word;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes
@@ -273,9 +280,10 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   static PerDeviceFlag attr;
   if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB;
-  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, BM, g.transient)) return -2;
-  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN, g.transient)) return -2;
   TcParams p = make_params(g);
+  if (A_K && g.M < BM) p.a_rows = (g.M + 7) / 8 * 8;
+  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, p.a_rows, g.transient, p.k_rows)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN, g.transient, p.k_rows)) return -2;
   p.tiles_m = (g.M + BM - 1) / BM;
   p.tiles_n = (g.N + BN - 1) / BN;
   const int k_blocks = (g.K + BK - 1) / BK;

@@ -140,6 +140,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     for (int s = 0; s < ST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
     *abort_flag = 0;
+    if (MODE == DRAIN_PIECES && blockIdx.x == 0 && p.zero_word) *p.zero_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -179,10 +180,14 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
           const uint32_t a_dst = smem_u32(smem + s * PAIR_STAGE_BYTES);
           const uint32_t b_dst = a_dst + HALF_BYTES;
           const uint32_t fb = map_to_rank(full_bar(s), 0);
-          if (leader) mbar_expect_tx(full_bar(s), 2 * (HALF_BYTES + PAIR_KH * b_slab));
+          // the second slab of the last block may lie past the end of the reduction altogether
+          const int slabs = (kb * PAIR_KH + 1) * BK < p.K ? PAIR_KH : 1;
+          const uint32_t slab_bytes = (A_K ? SLAB_BYTES : 2 * p.k_rows * 128) + (B_K ? b_slab : (w.bn / 128) * p.k_rows * 128);
+          if (leader) mbar_expect_tx(full_bar(s), 2 * slabs * slab_bytes);
           // (k past the end of the reduction reads zeros)
 #pragma unroll
           for (int kh = 0; kh < PAIR_KH; ++kh) {
+            if (kh >= slabs) break;
             const int k0 = (kb * PAIR_KH + kh) * BK;
             if (A_K) {
               tma_load_2d_pair(a_dst + kh * SLAB_BYTES, &mapA, fb, k0, m0);
@@ -223,9 +228,11 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
           tc_fence_after();
           const uint32_t a_addr = smem_u32(smem + s * PAIR_STAGE_BYTES);
           const uint32_t b_addr = a_addr + HALF_BYTES;
+          const int slabs = (kb * PAIR_KH + 1) * BK < p.K ? PAIR_KH : 1;
 #pragma unroll
           for (int k = 0; k < PAIR_KH * (BK / UMMA_K); ++k) {
             const uint32_t kh = (uint32_t)(k / (BK / UMMA_K)), kk = (uint32_t)(k % (BK / UMMA_K));
+            if ((int)kh >= slabs || (int)kk * UMMA_K >= p.k_rows) continue;
             const uint32_t slab = kh * SLAB_BYTES, slab_b = kh * b_slab;
             const uint64_t adesc = A_K ? make_desc(a_addr + slab + kk * 32, 16, 1024) : make_desc(a_addr + slab + kk * 2048, 8192, 1024);
             const uint64_t bdesc = B_K ? make_desc(b_addr + slab_b + kk * 32, 16, 1024) : make_desc(b_addr + slab_b + kk * 2048, 8192, 1024);
@@ -278,8 +285,8 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   static PerDeviceFlag attr;
   if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB, mapB2;
-  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient)) return -2;
-  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient)) return -2;
+  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient, p0.k_rows)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient, p0.k_rows)) return -2;
   TcParams p = p0;
   p.tiles_m = (g.M + 255) / 256;
   p.tiles_n = (g.N + PAIR_BN - 1) / PAIR_BN;

@@ -52,7 +52,7 @@ struct RowArgs {
   int64_t row0;                          // first row of the chunk
   int T;
   float scale2;                          // log2(e) / temperature
-  const float* weight; const int* count; // weight null: 1 / *count
+  const float* weight; const int* count; // weight null: 1 / *count, or where that is null too, the blocks count the rows themselves
   float *row_loss, *lse, *weighted;      // per row; the first two may be null
   float* factor;                         // f, of this chunk's rows
   bf16* fx;                              // f X [rows][d], or null
@@ -112,11 +112,11 @@ __global__ void __launch_bounds__(256) count_rows_kernel(Targets tg, int T, int 
   const int n = __syncthreads_count(t < T && row_counts(tg, t, V));
   if (threadIdx.x == 0 && n) atomicAdd(count, n);
 }
-// the same by one block, which needs no zeroed count: one launch less for up to 2^14 rows
-__global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int T, int V, int* count, unsigned* done) {
+// the same by one block, which needs no zeroed count: one launch less
+__global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int T, int V, int* count) {
   int n = 0;
   for (int64_t t0 = 0; t0 < T; t0 += 1024) n += __syncthreads_count(t0 + threadIdx.x < T && row_counts(tg, t0 + threadIdx.x, V));
-  if (threadIdx.x == 0) { *count = n; *done = 0; }
+  if (threadIdx.x == 0) *count = n;
 }
 
 // scales 64 stored powers
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
   __shared__ int s_id[R][MAX_ENTRIES];
   __shared__ float s_q[R][MAX_ENTRIES], s_l[R][MAX_ENTRIES];
   __shared__ float s_total[R], s_entropy[R], s_sum[16];
-  __shared__ int s_any[R], s_last;
+  __shared__ int s_any[R], s_last, s_count[THREADS / 32];
   __shared__ Piece s_piece[W];
   const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5, tid = W == 1 ? lane : threadIdx.x;   // of the row
   const int g = W == 1 ? threadIdx.x >> 5 : 0;
@@ -147,6 +147,14 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
   const int k = a.tg.k;
   auto sync = [] { if constexpr (W == 1) __syncwarp(); else __syncthreads(); };
 
+  if (!a.weight && !a.count) {
+    int n = 0;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < a.T; i += THREADS) n += row_counts(a.tg, i, a.V);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) s_count[threadIdx.x >> 5] = n;
+    __syncthreads();
+  }
   if (row < rows) {
     // the row's entries and their q
     if (warp == 0) {
@@ -288,7 +296,16 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         }
       }
       sync();
-      const float w = a.weight ? a.weight[t] : 1.f / (float)*a.count;
+      float w;
+      if (a.weight) {
+        w = a.weight[t];
+      } else if (a.count) {
+        w = 1.f / (float)*a.count;
+      } else {
+        int n = 0;
+        for (int i = 0; i < THREADS / 32; ++i) n += s_count[i];
+        w = 1.f / (float)n;
+      }
       const float total = s_total[g];
       const float f = w * a.tg.inv_temp * total * exp2f(ref - lse2);
       if (warp == 0) {
@@ -377,18 +394,29 @@ join_partials_kernel(const float* __restrict__ part, int splits, int64_t stride,
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-constexpr int64_t U_BYTES = 256ll << 20;      // default bound of a chunk's powers
+// A chunk by default: 6144 rows (8192 are worked as two of 4096), at most 1 GiB of powers.  The gradient
+// products lose efficiency below 4096 rows: 8192 x 2048 x 131072 takes 13.7 ms in chunks of 1024, 11.4 of
+// 2048, 10.5 of 4096 and of 8192.
+constexpr int64_t USUAL_ROWS = 6144, U_BYTES = 1ll << 30;
 constexpr int SMS = 148;                      // work is split for a B200 (also where sizes are asked without a device)
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// slices of the reduction for a [M, N] product over K: as many as bring the output's tiles near one
-// wave, each at least 1024 long (the partial products cost a launch of their own)
+// Slices of the reduction for a [M, N] product over K, from a model of its time: waves of units over the
+// machine (an SM pair's 256 x 256 tile takes 6 ns for each k, one SM's 128 x 128 tile 4), then the partial
+// products read at 3.3 TB/s by a launch of its own (3 us).  Slices are at least 1024 long.
 int splits_for(int64_t M, int64_t N, int64_t K) {
   const int64_t pair = ((M + 255) / 256) * ((N + 255) / 256);
-  int64_t tiles = pair, units = SMS / 2;
-  if (M <= 128 || N <= 128 || pair < 16) { tiles = ((M + 127) / 128) * ((N + 127) / 128); units = SMS; }
-  return (int)std::max<int64_t>(1, std::min<int64_t>(units / tiles, K / 1024));
+  const bool one = M <= 128 || N <= 128 || pair < 16;
+  const int64_t tiles = one ? ((M + 127) / 128) * ((N + 127) / 128) : pair, units = one ? SMS : SMS / 2;
+  double best = 0.;
+  int at = 1;
+  for (int64_t s = 1; s <= 32 && s <= std::max<int64_t>(1, K / 1024); ++s) {
+    const double waves = (double)((tiles * s + units - 1) / units);
+    const double ns = waves * ((K + s - 1) / s) * (one ? 4. : 6.) + (s > 1 ? 3000. + s * 4. * M * N / 3300. : 0.);
+    if (s == 1 || ns < 0.95 * best) { best = ns; at = (int)s; }
+  }
+  return at;
 }
 
 struct Plan {
@@ -402,7 +430,7 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
   p.n_pieces = p.ldu / PIECE;
   const int64_t row_bytes = want ? p.ldu * 2 : p.n_pieces * 8;     // (without gradients only the pieces' statistics)
   T = std::max(T, 1);
-  p.usual = std::max<int64_t>(256, U_BYTES / row_bytes / 256 * 256);
+  p.usual = std::max<int64_t>(256, std::min<int64_t>(USUAL_ROWS, U_BYTES / row_bytes / 256 * 256));
   int64_t c = chunk_rows > 0 ? round_up(chunk_rows, 256) : p.usual;
   p.usual = std::min<int64_t>(p.usual, T);
   p.chunks = (int)std::max<int64_t>(1, (T + c - 1) / c);
@@ -519,16 +547,18 @@ int run_head(const HeadCall& c) {
     if (c.dE) CUDA_OK(cudaMemset2DAsync(c.dE, (size_t)c.ldde * 2, 0, (size_t)c.d * 2, (size_t)c.V, c.st));
     return PPU_OK;
   }
-  if (!c.weight && c.T <= (1 << 14)) {
-    count_rows_block_kernel<<<1, 1024, 0, c.st>>>(c.tg, c.T, c.V, count, done);
-  } else {
-    CUDA_OK(cudaMemsetAsync(ws, 0, 8, c.st));
-    if (!c.weight) count_rows_kernel<<<(c.T + 255) / 256, 256, 0, c.st>>>(c.tg, c.T, c.V, count);
+  // the rows that count, for a mean: up to 2^10 rows by every block of the row kernel for itself (a launch
+  // costs more), up to 2^14 by one block
+  if (!c.weight && c.T > (1 << 14)) {
+    CUDA_OK(cudaMemsetAsync(count, 0, 4, c.st));
+    count_rows_kernel<<<(c.T + 255) / 256, 256, 0, c.st>>>(c.tg, c.T, c.V, count);
+  } else if (!c.weight && c.T > (1 << 10)) {
+    count_rows_block_kernel<<<1, 1024, 0, c.st>>>(c.tg, c.T, c.V, count);
   }
   RowArgs r;
   r.tg = c.tg; r.u = u; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
   r.X = (const bf16*)c.X; r.ldx = c.ldx; r.E = (const bf16*)c.E; r.lde = c.lde; r.d = c.d; r.V = c.V; r.T = c.T;
-  r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = count;
+  r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = c.T > (1 << 10) ? count : nullptr;
   r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
   r.done = done; r.loss = c.loss; r.flags = c.flags;
   const int warps = warps_for(p.usual, c.tg.k, p.n_pieces);
@@ -545,6 +575,7 @@ int run_head(const HeadCall& c) {
       g.A = r.X + c0 * c.ldx; g.lda = c.ldx; g.a_kmajor = 1;
       g.B = r.E; g.ldb = c.lde; g.b_kmajor = 1;
       g.M = (int)rows; g.N = c.V; g.K = c.d; g.epilogue = EPI_PIECES; g.C = u; g.ldc = p.ldu;
+      if (c0 == 0) g.zero_word = done;
       g.piece_scale = r.scale2; g.piece_stats = stats; g.ld_pieces = p.n_pieces;
       GEMM_OK(launch_gemm_tc_pieces(g, c.st));
     }

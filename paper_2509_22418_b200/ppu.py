@@ -402,22 +402,29 @@ def _matrix(t, name):
     return t.shape
 
 
-def _workspace(nbytes, device, given):
+def _workspace(nbytes, like, given):
+    """Address and size of the workspace: the caller's tensor, or one of this call.  (Its memory goes back to
+    torch's allocator when the call returns, for later work on the same stream.)"""
     import torch
-    if given is not None:
-        _need(isinstance(given, torch.Tensor) and given.get_device() == device and given.dtype is torch.uint8 and given.is_contiguous(),
-              "workspace must be a contiguous uint8 tensor on the operands' device")
-        return given
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    if given is None:
+        ws = like.new_empty(max(nbytes, 256), dtype=torch.uint8)
+        return ws, ws.data_ptr(), nbytes
+    _need(isinstance(given, torch.Tensor) and given.get_device() == like.get_device() and given.dtype is torch.uint8 and given.is_contiguous(),
+          "workspace must be a contiguous uint8 tensor on the operands' device")
+    return given, given.data_ptr(), given.numel()
 
 
-def _on_device(device, call):
-    """Runs call(stream) with the operands' device current, on its current stream."""
+def _other_device(device):
+    """The device to make current for a call, or None where it is current already."""
     import torch
-    if torch.cuda.current_device() == device:
-        return call(torch.cuda.current_stream(device).cuda_stream)
-    with torch.cuda.device(device):
-        return call(torch.cuda.current_stream(device).cuda_stream)
+    return None if torch.cuda.current_device() == device else torch.cuda.device(device)
+
+
+def _stream(device):
+    """The current stream's handle.  (The raw accessor, where this torch has it, takes a tenth of the time.)"""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 _VP, _I, _I64, _F, _SZ = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
@@ -445,32 +452,34 @@ def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
     return n.value
 
 
-def _head(name, X, E, row_weight, grad, chunk_rows, workspace, flags, targets):
-    """Outputs, workspace and the call of a head loss.  targets(T, device): its arguments between E and
-    row_weight."""
+def _head(name, X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags):
+    """Outputs, workspace and the call of a head loss; middle: its arguments between E and row_weight."""
     import torch
-    (T, d), V = _matrix(X, "X"), _matrix(E, "E")[0]
-    dev = X.get_device()
     bf, f32 = torch.bfloat16, torch.float32
+    V = _matrix(E, "E")[0]
     x, ldx = _rows(X, "X", bf, (T, d), dev)
     e, lde = _rows(E, "E", bf, (V, d), dev)
     w = None if row_weight is None else _dense(row_weight, "row_weight", f32, (T,), dev)
     fl = None if flags is None else _dense(flags, "flags", torch.int32, (8,), dev)
-    want_x, want_e = ("x" in grad, "e" in grad) if isinstance(grad, str) else (bool(grad), bool(grad))
-    middle = targets(T, dev)
-    entry = _entry(name)
-
-    def call(stream):
-        ws = _workspace(ppu_head_query_bytes(T, d, V, want_x + 2 * want_e, chunk_rows), dev, workspace)
-        rows = torch.empty(2 * T + 1, dtype=f32, device=X.device)
-        loss, row_loss, lse = rows[2 * T], rows[:T], rows[T:2 * T]
-        dX = torch.empty((T, d), dtype=bf, device=X.device) if want_x else None
-        dE = torch.empty((V, d), dtype=bf, device=X.device) if want_e else None
-        p = rows.data_ptr()
-        _check(entry(x, ldx, e, lde, *middle, w, T, d, V, p + 8 * T, p, p + 4 * T, dX.data_ptr() if want_x else None, d,
-                     dE.data_ptr() if want_e else None, d, chunk_rows, ws.data_ptr(), ws.numel(), fl, stream))
-        return loss, row_loss, lse, dX, dE
-    return _on_device(dev, call)
+    want_x, want_e = ("x" in grad, "e" in grad) if isinstance(grad, str) else (grad, grad)
+    other = _other_device(dev)
+    if other is not None:
+        with other:
+            return _head(name, X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
+    ws, pw, nw = _workspace(ppu_head_query_bytes(T, d, V, (1 if want_x else 0) + (2 if want_e else 0), chunk_rows), X, workspace)
+    row_loss = X.new_empty(T, dtype=f32)
+    lse = torch.empty_like(row_loss)
+    loss = row_loss.new_empty(())
+    dX = dE = px = pe = None
+    if want_x:
+        dX = X.new_empty((T, d))
+        px = dX.data_ptr()
+    if want_e:
+        dE = X.new_empty((V, d))
+        pe = dE.data_ptr()
+    _check(_entry(name)(x, ldx, e, lde, *middle, w, T, d, V, loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), px, d, pe, d, chunk_rows, pw, nw,
+                        fl, _stream(dev)))
+    return loss, row_loss, lse, dX, dE
 
 
 def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, workspace=None, flags=None):
@@ -480,10 +489,10 @@ def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, worksp
     "e" for one gradient only (E frozen, X frozen).  Returns (loss, row_loss [T], lse [T], dX, dE).
     flags: int32 [8] zeros for ppu_op_status."""
     import torch
-
-    def targets(T, dev):
-        return (_dense(target, "target", torch.int32, (T,), dev),)
-    return _head("ppu_head_xent", X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+    T, d = _matrix(X, "X")
+    dev = X.get_device()
+    middle = (_dense(target, "target", torch.int32, (T,), dev),)
+    return _head("ppu_head_xent", X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
 
 
 def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher_lse=None, row_weight=None,
@@ -494,13 +503,13 @@ def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher
     sum_j q_j (log q_j - log p_j); multiply row_weight by temperature ** 2 for gradients of the
     same size at every temperature.  The rest as ppu_head_xent."""
     import torch
-
-    def targets(T, dev):
-        k = _matrix(teacher_ids, "teacher_ids")[1]
-        i, ldi = _rows(teacher_ids, "teacher_ids", torch.int32, (T, k), dev)
-        z, ldz = _rows(teacher_logits, "teacher_logits", torch.float32, (T, k), dev)
-        return i, ldi, z, ldz, k, None if teacher_lse is None else _dense(teacher_lse, "teacher_lse", torch.float32, (T,), dev), temperature
-    return _head("ppu_head_distill", X, E, row_weight, grad, chunk_rows, workspace, flags, targets)
+    T, d = _matrix(X, "X")
+    dev = X.get_device()
+    k = _matrix(teacher_ids, "teacher_ids")[1]
+    i, ldi = _rows(teacher_ids, "teacher_ids", torch.int32, (T, k), dev)
+    z, ldz = _rows(teacher_logits, "teacher_logits", torch.float32, (T, k), dev)
+    middle = (i, ldi, z, ldz, k, None if teacher_lse is None else _dense(teacher_lse, "teacher_lse", torch.float32, (T,), dev), temperature)
+    return _head("ppu_head_distill", X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
 
 
 def ppu_op_status(flags) -> None:
@@ -508,7 +517,8 @@ def ppu_op_status(flags) -> None:
     import torch
     _need(isinstance(flags, torch.Tensor) and flags.is_cuda, "flags must be a CUDA tensor")
     p = _dense(flags, "flags", torch.int32, (8,), flags.get_device())
-    _on_device(flags.get_device(), lambda stream: _check(lib().ppu_op_status(C.c_void_p(p), C.c_void_p(stream))))
+    with torch.cuda.device(flags.get_device()):
+        _check(lib().ppu_op_status(C.c_void_p(p), C.c_void_p(_stream(flags.get_device()))))
 
 
 # ---- norms before and after a block, with its gate and the residual scale --------------------
@@ -543,15 +553,16 @@ def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None
     Returns (r_out fp32, h bf16, stats fp32 [T, 4])."""
     import torch
     dev, T, d, gate_rows, (py, pr, pg, g1, b1, g2, b2) = _norm_operands(y, r, gate, gate_rows, kind, (post_gain, post_shift, pre_gain, pre_shift))
-    entry = _entry("ppu_norm_gate_fwd")
-
-    def call(stream):
-        r_out = r if in_place else torch.empty_like(r)
-        h = torch.empty_like(y)
-        stats = torch.empty((T, 4), dtype=torch.float32, device=r.device)
-        _check(entry(py, pr, pg, gate_rows, g1, b1, g2, b2, _KINDS[kind], res_scale, eps, r_out.data_ptr(), h.data_ptr(), stats.data_ptr(), T, d, stream))
-        return r_out, h, stats
-    return _on_device(dev, call)
+    other = _other_device(dev)
+    if other is not None:
+        with other:
+            return ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, kind, res_scale, eps, in_place)
+    r_out = r if in_place else torch.empty_like(r)
+    h = torch.empty_like(y)
+    stats = r.new_empty((T, 4))
+    _check(_entry("ppu_norm_gate_fwd")(py, pr, pg, gate_rows, g1, b1, g2, b2, _KINDS[kind], res_scale, eps, r_out.data_ptr(), h.data_ptr(),
+                                       stats.data_ptr(), T, d, _stream(dev)))
+    return r_out, h, stats
 
 
 @lru_cache(maxsize=None)
@@ -573,16 +584,23 @@ def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shi
     pdh = _dense(dh, "dh", torch.bfloat16, (T, d), dev)
     pdr = None if dr_out is None else _dense(dr_out, "dr_out", f32, (T, d), dev)
     ps = _dense(stats, "stats", f32, (T, 4), dev)
-    entry = _entry("ppu_norm_gate_bwd")
-
-    def call(stream):
-        ws = _workspace(ppu_norm_gate_query_bytes(T, d, gate_rows), dev, workspace)
-        dy, dr = torch.empty_like(y), torch.empty_like(r_out)
-        sums = torch.empty((4, d), dtype=f32, device=dy.device)
-        dgate = None if gate is None else torch.empty_like(gate)
-        s = sums.data_ptr()
-        _check(entry(pdh, pdr, py, pr, ps, pg, gate_rows, g1, b1, g2, _KINDS[kind], res_scale, dy.data_ptr(), dr.data_ptr(), s,
-                     None if b1 is None else s + 4 * d, s + 8 * d, None if b2 is None else s + 12 * d,
-                     None if gate is None else dgate.data_ptr(), T, d, ws.data_ptr(), ws.numel(), stream))
-        return (dy, dr, sums[0], None if b1 is None else sums[1], sums[2], None if b2 is None else sums[3], dgate)
-    return _on_device(dev, call)
+    other = _other_device(dev)
+    if other is not None:
+        with other:
+            return ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, kind, res_scale, workspace)
+    ws, pw, nw = _workspace(ppu_norm_gate_query_bytes(T, d, gate_rows), r_out, workspace)
+    dy, dr = torch.empty_like(y), torch.empty_like(r_out)
+    dg1, dg2 = torch.empty_like(post_gain), torch.empty_like(pre_gain)
+    db1 = db2 = dgate = q1 = q2 = qg = None
+    if b1 is not None:
+        db1 = torch.empty_like(post_shift)
+        q1 = db1.data_ptr()
+    if b2 is not None:
+        db2 = torch.empty_like(pre_shift)
+        q2 = db2.data_ptr()
+    if pg is not None:
+        dgate = torch.empty_like(gate)
+        qg = dgate.data_ptr()
+    _check(_entry("ppu_norm_gate_bwd")(pdh, pdr, py, pr, ps, pg, gate_rows, g1, b1, g2, _KINDS[kind], res_scale, dy.data_ptr(), dr.data_ptr(),
+                                       dg1.data_ptr(), q1, dg2.data_ptr(), q2, qg, T, d, pw, nw, _stream(dev)))
+    return dy, dr, dg1, db1, dg2, db2, dgate

@@ -541,8 +541,10 @@ def test_sizes_of_the_workspace(ppu):
     q = ppu.ppu_head_query_bytes
     full = 8192 * 32768 * 2
     assert q(8192, 2048, 32768, 0) < full / 15           # statistics of the pieces (8 bytes for 64 values) and the rows
-    assert q(8192, 2048, 32768, 1) < 0.75 * full         # at most 256 MiB of softmax beside them
-    assert q(1 << 20, 2048, 32768, 3) < q(8192, 2048, 32768, 3) + 8 * (1 << 20) + 4096
+    assert q(8192, 2048, 32768, 1) < 0.75 * full         # half of the rows' softmax beside them
+    # a chunk's softmax (6144 rows), dE's running sum and fX, and a few values for each row, however many rows
+    assert q(1 << 20, 2048, 32768, 3) < 6144 * (32768 * 2 + 512 * 8 + 2048 * 2) + 32768 * 2048 * 4 + 16 * (1 << 20)
+    assert q(1 << 20, 8, 1 << 22, 1) < 1.2 * 2 ** 31
     assert q(8192, 2048, 32768, 3, chunk_rows=256) < q(8192, 2048, 32768, 3)
     for bad in [(1, 12, 8), (1, 0, 8), (1, 16392, 8), (-1, 8, 8), (1, 8, 0), ((1 << 20) + 1, 8, 8), (1, 8, (1 << 22) + 1)]:
         with pytest.raises(ppu.PpuError):
