@@ -1,13 +1,17 @@
-"""Builds libppu.so (sm_100a) next to this file with nvcc.  No GPU is needed to build."""
+"""Builds libppu.so (sm_100a, nvcc) and _ops.so (the compiled torch binding of the operators, g++) next to this
+file.  No GPU is needed to build."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libppu.so")
+OPS = os.path.join(HERE, "_ops.so")
 SOURCES = ["ppu_api.cu", "ppu_step.cu", "elementwise.cu", "optim.cu", "gemm_simt.cu",
            "gemm_tc.cu", "gemm_tc_pair.cu", "attention_simt.cu", "attention_tc.cu", "attention_static.cu", "wait_probe.cu",
            "head_loss.cu", "norm_gate.cu"]
@@ -16,12 +20,26 @@ FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-li
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(OPS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(OPS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "ppu.h"))
     return any(os.path.getmtime(p) > t for p in deps)
+
+
+OPS_OBJ = os.path.join(HERE, "_build", "bind.o")
+
+
+def _torch_dir() -> str:
+    return os.path.dirname(importlib.util.find_spec("torch").origin)     # without importing it
+
+
+def _ops_compile():
+    inc = os.path.join(_torch_dir(), "include")
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=1", "-I" + inc, "-I" + os.path.join(inc, "torch", "csrc", "api", "include"),
+            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(cuda, "include"), "-c", os.path.join(CSRC, "bind.cpp"), "-o", OPS_OBJ]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -37,6 +55,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose:
             cmd.insert(1, "-Xptxas=-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    procs.append(("bind.cpp", subprocess.Popen(_ops_compile(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = False
     for src, p in procs:
         out = p.communicate()[0].decode()
@@ -44,9 +63,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(f"--- {src}\n{out}\n")
         failed |= p.returncode != 0
     if failed:
-        raise RuntimeError("nvcc failed")
+        raise RuntimeError("compilation failed")
     subprocess.check_call([nvcc, "-shared", "-o", LIB, *objs, "-gencode",
                            "arch=compute_100a,code=sm_100a"])
+    torch_lib = os.path.join(_torch_dir(), "lib")
+    subprocess.check_call(["g++", "-shared", "-o", OPS, OPS_OBJ, "-L" + HERE, "-l:libppu.so", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-ltorch_python", "-ltorch",
+                           "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     return LIB
 
 

@@ -9,7 +9,6 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from functools import lru_cache
 
 import numpy as np
 
@@ -350,101 +349,24 @@ def ppu_attention_bwd_static(qkv, U, lse, dU, batch, seq, n_head, d_head, backen
 # ---- losses of hidden states against the vocabulary ------------------------------------------
 MAX_TEACHER_ENTRIES = 128
 NORM_LAYER, NORM_RMS = 0, 1
+_ops = None
 
 
-def _need(ok, what):
-    if not ok:
-        raise PpuError(-1, what)
+def _binding():
+    """The compiled binding (_ops.so): checks, outputs, workspaces, streams and the C calls."""
+    global _ops
+    if _ops is None:
+        import torch  # noqa: F401  (its libraries have to be loaded first)
+        lib()
+        try:
+            from . import _ops as m
+        except ImportError as e:
+            raise PpuError(-6, f"_ops.so does not load ({e}): run paper_2509_22418_b200/build.py") from e
+        m.set_error(PpuError)
+        _ops = m
+    return _ops
 
 
-def _is_dense(t, dtype, shape, device):
-    """A contiguous CUDA tensor of this type and shape on this device.  (These operators take
-    microseconds on small inputs, so their checks are few calls; _refuse finds the words.)"""
-    return t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
-
-
-def _is_rows(t, dtype, shape, device):
-    """The same for a matrix whose rows may be strided."""
-    if not (t.dtype is dtype and t.get_device() == device and t.shape == shape):
-        return False
-    if t.is_contiguous():
-        return True
-    return (shape[1] == 1 or t.stride(1) == 1) and (shape[0] == 1 or t.stride(0) >= shape[1])
-
-
-def _refuse(t, name, dtype, shape, device):
-    """Raises what is wrong with a tensor that _is_dense or _is_rows did not accept."""
-    import torch
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
-    _need(t.dtype is dtype, f"{name} must be {dtype}, got {t.dtype}")
-    _need(t.shape == shape, f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    _need(t.get_device() == device, f"{name} is on {t.device}, other operands on cuda:{device}")
-    _need(False, f"{name}: values must be adjacent and rows must not overlap")
-
-
-def _dense(t, name, dtype, shape, device):
-    import torch
-    if not isinstance(t, torch.Tensor) or not _is_dense(t, dtype, shape, device):
-        _refuse(t, name, dtype, shape, device)
-    return t.data_ptr()
-
-
-def _rows(t, name, dtype, shape, device):
-    import torch
-    if not isinstance(t, torch.Tensor) or not _is_rows(t, dtype, shape, device):
-        _refuse(t, name, dtype, shape, device)
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
-
-
-def _matrix(t, name):
-    import torch
-    _need(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2, f"{name} must be a CUDA tensor of two dimensions")
-    return t.shape
-
-
-def _workspace(nbytes, like, given):
-    """Address and size of the workspace: the caller's tensor, or one of this call.  (Its memory goes back to
-    torch's allocator when the call returns, for later work on the same stream.)"""
-    import torch
-    if given is None:
-        ws = like.new_empty(max(nbytes, 256), dtype=torch.uint8)
-        return ws, ws.data_ptr(), nbytes
-    _need(isinstance(given, torch.Tensor) and given.get_device() == like.get_device() and given.dtype is torch.uint8 and given.is_contiguous(),
-          "workspace must be a contiguous uint8 tensor on the operands' device")
-    return given, given.data_ptr(), given.numel()
-
-
-def _other_device(device):
-    """The device to make current for a call, or None where it is current already."""
-    import torch
-    return None if torch.cuda.current_device() == device else torch.cuda.device(device)
-
-
-def _stream(device):
-    """The current stream's handle.  (The raw accessor, where this torch has it, takes a tenth of the time.)"""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
-
-
-_VP, _I, _I64, _F, _SZ = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
-_ARGTYPES = {
-    "ppu_head_xent": [_VP, _I64, _VP, _I64, _VP, _VP, _I, _I, _I, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _I, _VP, _SZ, _VP, _VP],
-    "ppu_head_distill": [_VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _I, _VP, _F, _VP, _I, _I, _I, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _I, _VP, _SZ,
-                         _VP, _VP],
-    "ppu_norm_gate_fwd": [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _I, _F, _F, _VP, _VP, _VP, _I, _I, _VP],
-    "ppu_norm_gate_bwd": [_VP, _VP, _VP, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _VP, _SZ, _VP],
-}
-
-
-def _entry(name):
-    fn = getattr(lib(), name)
-    if fn.argtypes is None:
-        fn.argtypes = _ARGTYPES[name]
-    return fn
-
-
-@lru_cache(maxsize=None)
 def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
     """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE)."""
     n = C.c_size_t(0)
@@ -452,47 +374,19 @@ def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
     return n.value
 
 
-def _head(name, X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags):
-    """Outputs, workspace and the call of a head loss; middle: its arguments between E and row_weight."""
-    import torch
-    bf, f32 = torch.bfloat16, torch.float32
-    V = _matrix(E, "E")[0]
-    x, ldx = _rows(X, "X", bf, (T, d), dev)
-    e, lde = _rows(E, "E", bf, (V, d), dev)
-    w = None if row_weight is None else _dense(row_weight, "row_weight", f32, (T,), dev)
-    fl = None if flags is None else _dense(flags, "flags", torch.int32, (8,), dev)
-    want_x, want_e = ("x" in grad, "e" in grad) if isinstance(grad, str) else (grad, grad)
-    other = _other_device(dev)
-    if other is not None:
-        with other:
-            return _head(name, X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
-    ws, pw, nw = _workspace(ppu_head_query_bytes(T, d, V, (1 if want_x else 0) + (2 if want_e else 0), chunk_rows), X, workspace)
-    row_loss = X.new_empty(T, dtype=f32)
-    lse = torch.empty_like(row_loss)
-    loss = row_loss.new_empty(())
-    dX = dE = px = pe = None
-    if want_x:
-        dX = X.new_empty((T, d))
-        px = dX.data_ptr()
-    if want_e:
-        dE = X.new_empty((V, d))
-        pe = dE.data_ptr()
-    _check(_entry(name)(x, ldx, e, lde, *middle, w, T, d, V, loss.data_ptr(), row_loss.data_ptr(), lse.data_ptr(), px, d, pe, d, chunk_rows, pw, nw,
-                        fl, _stream(dev)))
-    return loss, row_loss, lse, dX, dE
+def _grads(grad):
+    if isinstance(grad, str):
+        return ("x" in grad) + 2 * ("e" in grad)
+    return 3 if grad else 0
 
 
 def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, workspace=None, flags=None):
     """Softmax cross entropy of hidden states X [T, d] against the vocabulary matrix E [V, d] (bf16;
     rows may be strided), without the logits.  target: int32 [T], negative: the row does not
     count.  row_weight: fp32 [T], or None for the mean over the rows that count.  grad: True, False, or "x" /
-    "e" for one gradient only (E frozen, X frozen).  Returns (loss, row_loss [T], lse [T], dX, dE).
-    flags: int32 [8] zeros for ppu_op_status."""
-    import torch
-    T, d = _matrix(X, "X")
-    dev = X.get_device()
-    middle = (_dense(target, "target", torch.int32, (T,), dev),)
-    return _head("ppu_head_xent", X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
+    "e" for one gradient only (E frozen, X frozen).  workspace: uint8 tensor of ppu_head_query_bytes, or None.
+    Returns (loss, row_loss [T], lse [T], dX, dE).  flags: int32 [8] zeros for ppu_op_status."""
+    return (_ops or _binding()).head_xent(X, E, target, row_weight, _grads(grad), chunk_rows, workspace, flags)
 
 
 def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher_lse=None, row_weight=None,
@@ -502,47 +396,27 @@ def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher
     teacher's logits / temperature, or None for the softmax over the k entries.  Loss and gradients are those of
     sum_j q_j (log q_j - log p_j); multiply row_weight by temperature ** 2 for gradients of the
     same size at every temperature.  The rest as ppu_head_xent."""
-    import torch
-    T, d = _matrix(X, "X")
-    dev = X.get_device()
-    k = _matrix(teacher_ids, "teacher_ids")[1]
-    i, ldi = _rows(teacher_ids, "teacher_ids", torch.int32, (T, k), dev)
-    z, ldz = _rows(teacher_logits, "teacher_logits", torch.float32, (T, k), dev)
-    middle = (i, ldi, z, ldz, k, None if teacher_lse is None else _dense(teacher_lse, "teacher_lse", torch.float32, (T,), dev), temperature)
-    return _head("ppu_head_distill", X, E, T, d, dev, middle, row_weight, grad, chunk_rows, workspace, flags)
+    return (_ops or _binding()).head_distill(X, E, teacher_ids, teacher_logits, temperature, teacher_lse, row_weight, _grads(grad), chunk_rows,
+                                             workspace, flags)
 
 
 def ppu_op_status(flags) -> None:
     """Waits for the current stream; raises what a call given `flags` (int32 [8], zeros at first) reported."""
     import torch
-    _need(isinstance(flags, torch.Tensor) and flags.is_cuda, "flags must be a CUDA tensor")
-    p = _dense(flags, "flags", torch.int32, (8,), flags.get_device())
-    with torch.cuda.device(flags.get_device()):
-        _check(lib().ppu_op_status(C.c_void_p(p), C.c_void_p(_stream(flags.get_device()))))
+    if not (isinstance(flags, torch.Tensor) and flags.is_cuda and flags.dtype == torch.int32 and flags.shape == (8,) and flags.is_contiguous()):
+        raise PpuError(-1, "flags must be a contiguous int32 CUDA tensor of 8 values")
+    with torch.cuda.device(flags.device):
+        _check(lib().ppu_op_status(C.c_void_p(flags.data_ptr()), C.c_void_p(torch.cuda.current_stream(flags.device).cuda_stream)))
 
 
 # ---- norms before and after a block, with its gate and the residual scale --------------------
 _KINDS = {"layer": NORM_LAYER, "rms": NORM_RMS}
 
 
-def _norm_operands(y, r, gate, gate_rows, kind, vectors):
-    """Device, sizes and addresses of what both passes take: y, r, the gate, the norms' vectors."""
-    import torch
-    T, d = _matrix(y, "y")
-    _need(kind in _KINDS, f"kind must be one of {sorted(_KINDS)}")
-    dev = y.get_device()
-    f32 = torch.float32
-    p = [_dense(y, "y", torch.bfloat16, (T, d), dev), _dense(r, "r", f32, (T, d), dev)]
-    if gate is None:
-        gate_rows = 0
-        p.append(None)
-    else:
-        _need(gate_rows >= 0, "gate_rows must not be negative")
-        gate_rows = gate_rows or max(T, 1)
-        p.append(_dense(gate, "gate", f32, (-(-T // gate_rows), d), dev))
-    for name, v in zip(("post_gain", "post_shift", "pre_gain", "pre_shift"), vectors):
-        p.append(None if v is None and name.endswith("shift") else _dense(v, name, f32, (d,), dev))
-    return dev, T, d, gate_rows, p
+def _kind(kind):
+    if kind not in _KINDS:
+        raise PpuError(-1, f"kind must be one of {sorted(_KINDS)}")
+    return _KINDS[kind]
 
 
 def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None, gate=None, gate_rows=0,
@@ -551,21 +425,9 @@ def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None
     a block's output y [T, d] (bf16) and the residual stream r [T, d] (fp32); kind "layer" or "rms";
     gate fp32 [ceil(T / gate_rows), d] (gate_rows 0: one row for all).  in_place: r_out is r.
     Returns (r_out fp32, h bf16, stats fp32 [T, 4])."""
-    import torch
-    dev, T, d, gate_rows, (py, pr, pg, g1, b1, g2, b2) = _norm_operands(y, r, gate, gate_rows, kind, (post_gain, post_shift, pre_gain, pre_shift))
-    other = _other_device(dev)
-    if other is not None:
-        with other:
-            return ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, kind, res_scale, eps, in_place)
-    r_out = r if in_place else torch.empty_like(r)
-    h = torch.empty_like(y)
-    stats = r.new_empty((T, 4))
-    _check(_entry("ppu_norm_gate_fwd")(py, pr, pg, gate_rows, g1, b1, g2, b2, _KINDS[kind], res_scale, eps, r_out.data_ptr(), h.data_ptr(),
-                                       stats.data_ptr(), T, d, _stream(dev)))
-    return r_out, h, stats
+    return (_ops or _binding()).norm_gate_fwd(y, r, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, _kind(kind), res_scale, eps, in_place)
 
 
-@lru_cache(maxsize=None)
 def ppu_norm_gate_query_bytes(T, d, gate_rows=0) -> int:
     """Bytes of workspace of ppu_norm_gate_bwd (gate_rows 0: no gate)."""
     n = C.c_size_t(0)
@@ -578,29 +440,5 @@ def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shi
     """Gradients of ppu_norm_gate_fwd from dh [T, d] (bf16) and dr_out [T, d] (fp32, or None), with the saved
     r_out and stats.  Returns (dy bf16, dr fp32, dpost_gain, dpost_shift, dpre_gain, dpre_shift,
     dgate); those of absent operands are None."""
-    import torch
-    dev, T, d, gate_rows, (py, pr, pg, g1, b1, g2, b2) = _norm_operands(y, r_out, gate, gate_rows, kind, (post_gain, post_shift, pre_gain, pre_shift))
-    f32 = torch.float32
-    pdh = _dense(dh, "dh", torch.bfloat16, (T, d), dev)
-    pdr = None if dr_out is None else _dense(dr_out, "dr_out", f32, (T, d), dev)
-    ps = _dense(stats, "stats", f32, (T, 4), dev)
-    other = _other_device(dev)
-    if other is not None:
-        with other:
-            return ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, kind, res_scale, workspace)
-    ws, pw, nw = _workspace(ppu_norm_gate_query_bytes(T, d, gate_rows), r_out, workspace)
-    dy, dr = torch.empty_like(y), torch.empty_like(r_out)
-    dg1, dg2 = torch.empty_like(post_gain), torch.empty_like(pre_gain)
-    db1 = db2 = dgate = q1 = q2 = qg = None
-    if b1 is not None:
-        db1 = torch.empty_like(post_shift)
-        q1 = db1.data_ptr()
-    if b2 is not None:
-        db2 = torch.empty_like(pre_shift)
-        q2 = db2.data_ptr()
-    if pg is not None:
-        dgate = torch.empty_like(gate)
-        qg = dgate.data_ptr()
-    _check(_entry("ppu_norm_gate_bwd")(pdh, pdr, py, pr, ps, pg, gate_rows, g1, b1, g2, _KINDS[kind], res_scale, dy.data_ptr(), dr.data_ptr(),
-                                       dg1.data_ptr(), q1, dg2.data_ptr(), q2, qg, T, d, pw, nw, _stream(dev)))
-    return dy, dr, dg1, db1, dg2, db2, dgate
+    return (_ops or _binding()).norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, _kind(kind),
+                                              res_scale, workspace)
