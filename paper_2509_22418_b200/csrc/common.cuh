@@ -9,6 +9,24 @@ typedef __nv_bfloat16 bf16;
 // Device-side error word indices (one int32 each, in the context's flag block).
 enum { PPU_FLAG_TOKEN = 0, PPU_FLAG_TIMEOUT = 1, PPU_FLAG_COUNT = 8 };
 
+// ---- dependent launches ----------------------------------------------------------
+// The kernels of one operator follow one another within microseconds.  Launched as programmatic
+// dependents, a kernel's blocks are placed and set up (barriers, tensor memory, descriptors) while the one before
+// it still runs; pdl_wait() returns when that one has finished and its writes are visible, so everything
+// that touches global memory comes after it.  Without the launch attribute both are no-ops.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... P, typename... A>
+inline cudaError_t ppu_launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 // ---- GEMM: C[M,N] (+epilogue) = A . B^T, bf16 operands, fp32 accumulation ----
 enum GemmEpilogue {
   EPI_STORE_BF16 = 0,  // C bf16
@@ -57,7 +75,7 @@ struct GemmArgs {
   float piece_scale = 1.f; float2* piece_stats = nullptr; int64_t ld_pieces = 0;
   unsigned* zero_word = nullptr;     // EPI_PIECES: a word that the launch sets to 0 (a counter of the kernel after it), or null
   const float* row_scale = nullptr;  // EPI_OUT_BF16: fp32 [M]
-  // operands that come and go (a caller's tensors): their tensor maps are encoded for this launch
+  // part of an operator on a caller's tensors: tensor maps are encoded for this launch, which is a dependent one
   bool transient = false;
 };
 

@@ -87,6 +87,7 @@ struct TcParams {
   void* C3; long long ldc3; int c3_lo, c3_hi;
   float piece_scale; float2* piece_stats; long long ld_pieces;
   const float* row_scale; unsigned* zero_word;
+  int dependent;   // launched as a programmatic dependent
 };
 
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of

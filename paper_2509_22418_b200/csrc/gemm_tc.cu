@@ -55,7 +55,6 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
     *abort_flag = 0;
-    if (MODE == DRAIN_PIECES && blockIdx.x == 0 && p.zero_word) *p.zero_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -66,6 +65,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  if (p.dependent) { pdl_wait(); pdl_trigger(); }
+  if (MODE == DRAIN_PIECES && blockIdx.x == 0 && threadIdx.x == 0 && p.zero_word) *p.zero_word = 0;
 
   const int tiles_mn = p.tiles_m * p.tiles_n;
   const int num_tiles = tiles_mn * p.splits;
@@ -258,7 +259,7 @@ TcParams make_params(const GemmArgs& g) {
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
   p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
-  p.row_scale = g.row_scale; p.zero_word = g.zero_word;
+  p.row_scale = g.row_scale; p.zero_word = g.zero_word; p.dependent = g.transient ? 1 : 0;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes
@@ -297,7 +298,10 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
     mapC = {};
     if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
   }
-  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, C::SMEM + store_smem<MODE>(), st>>>(mapA, mapB, mapC, p);
+  constexpr int smem = C::SMEM + store_smem<MODE>();
+  if (g.transient)
+    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, GEMM_THREADS, smem, st, mapA, mapB, mapC, p) == cudaSuccess ? 0 : -3;
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, smem, st>>>(mapA, mapB, mapC, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 

@@ -140,7 +140,6 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     for (int s = 0; s < ST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
     *abort_flag = 0;
-    if (MODE == DRAIN_PIECES && blockIdx.x == 0 && p.zero_word) *p.zero_word = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -155,6 +154,8 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   cluster_sync_all();          // the peer's barriers are initialised before anything signals them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  if (p.dependent) { pdl_wait(); pdl_trigger(); }
+  if (MODE == DRAIN_PIECES && blockIdx.x == 0 && threadIdx.x == 0 && p.zero_word) *p.zero_word = 0;
 
   const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   const int num_tiles = p.tiles_m * p.tiles_n;
@@ -324,8 +325,11 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
     mapC = {};
     if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
   }
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>
-      <<<2 * pairs, GEMM_THREADS, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>(), st>>>(mapA, mapB, mapB2, mapC, p);
+  constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE>();
+  if (g.transient)
+    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB2, mapC, p) ==
+                   cudaSuccess ? 0 : -3;
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, smem, st>>>(mapA, mapB, mapB2, mapC, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 

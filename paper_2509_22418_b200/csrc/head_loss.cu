@@ -108,12 +108,14 @@ __device__ __forceinline__ bool row_counts(const Targets& tg, int64_t t, int V) 
 }
 // rows with at least one present entry (integer atomics: any order gives the same count)
 __global__ void __launch_bounds__(256) count_rows_kernel(Targets tg, int T, int V, int* count) {
+  pdl_wait(); pdl_trigger();
   const int64_t t = blockIdx.x * 256 + threadIdx.x;
   const int n = __syncthreads_count(t < T && row_counts(tg, t, V));
   if (threadIdx.x == 0 && n) atomicAdd(count, n);
 }
 // the same by one block, which needs no zeroed count: one launch less
 __global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int T, int V, int* count) {
+  pdl_wait(); pdl_trigger();
   int n = 0;
   for (int64_t t0 = 0; t0 < T; t0 += 1024) n += __syncthreads_count(t0 + threadIdx.x < T && row_counts(tg, t0 + threadIdx.x, V));
   if (threadIdx.x == 0) *count = n;
@@ -147,6 +149,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
   const int k = a.tg.k;
   auto sync = [] { if constexpr (W == 1) __syncwarp(); else __syncthreads(); };
 
+  pdl_wait(); pdl_trigger();
   if (!a.weight && !a.count) {
     int n = 0;
 #pragma unroll 4
@@ -378,6 +381,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
 __global__ void __launch_bounds__(256)
 join_partials_kernel(const float* __restrict__ part, int splits, int64_t stride, const float* __restrict__ row_scale,
                      bf16* __restrict__ out, int64_t ldo, int rows, int n4) {
+  pdl_wait(); pdl_trigger();
   const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
   if (i >= (int64_t)rows * n4) return;
   const int64_t r = i / n4;
@@ -495,10 +499,10 @@ int warps_for(int64_t rows, int k, int64_t n_pieces) {
   return rows >= 8 * SMS || share < 16 ? 4 : 16;
 }
 template <bool GRAD>
-void launch_rows(const RowArgs& r, int64_t rows, int warps, cudaStream_t st) {
-  if (warps == 1) head_rows_kernel<GRAD, 1><<<(unsigned)((rows + 3) / 4), 128, 0, st>>>(r, (int)rows);
-  else if (warps == 4) head_rows_kernel<GRAD, 4><<<(unsigned)rows, 128, 0, st>>>(r, (int)rows);
-  else head_rows_kernel<GRAD, 16><<<(unsigned)rows, 512, 0, st>>>(r, (int)rows);
+cudaError_t launch_rows(const RowArgs& r, int64_t rows, int warps, cudaStream_t st) {
+  if (warps == 1) return ppu_launch_dependent(head_rows_kernel<GRAD, 1>, (unsigned)((rows + 3) / 4), 128, 0, st, r, (int)rows);
+  if (warps == 4) return ppu_launch_dependent(head_rows_kernel<GRAD, 4>, (unsigned)rows, 128, 0, st, r, (int)rows);
+  return ppu_launch_dependent(head_rows_kernel<GRAD, 16>, (unsigned)rows, 512, 0, st, r, (int)rows);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -514,7 +518,8 @@ int product_bf16(GemmArgs g, int splits, float* part, cudaStream_t st) {
   g.epilogue = EPI_STORE_F32; g.C = part; g.ldc = g.N; g.splits = splits; g.split_stride = (int64_t)g.M * g.N;
   GEMM_OK(launch_gemm_tc(g, st));
   const int64_t n = (int64_t)g.M * (g.N / 4);
-  join_partials_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, splits, g.split_stride, g.row_scale, out, ldo, g.M, g.N / 4);
+  CUDA_OK(ppu_launch_dependent(join_partials_kernel, (unsigned)((n + 255) / 256), 256, 0, st, part, splits, g.split_stride, g.row_scale, out, ldo,
+                               g.M, g.N / 4));
   return PPU_OK;
 }
 
@@ -551,9 +556,9 @@ int run_head(const HeadCall& c) {
   // costs more), up to 2^14 by one block
   if (!c.weight && c.T > (1 << 14)) {
     CUDA_OK(cudaMemsetAsync(count, 0, 4, c.st));
-    count_rows_kernel<<<(c.T + 255) / 256, 256, 0, c.st>>>(c.tg, c.T, c.V, count);
+    CUDA_OK(ppu_launch_dependent(count_rows_kernel, (c.T + 255) / 256, 256, 0, c.st, c.tg, c.T, c.V, count));
   } else if (!c.weight && c.T > (1 << 10)) {
-    count_rows_block_kernel<<<1, 1024, 0, c.st>>>(c.tg, c.T, c.V, count);
+    CUDA_OK(ppu_launch_dependent(count_rows_block_kernel, 1, 1024, 0, c.st, c.tg, c.T, c.V, count));
   }
   RowArgs r;
   r.tg = c.tg; r.u = u; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
@@ -580,8 +585,7 @@ int run_head(const HeadCall& c) {
       GEMM_OK(launch_gemm_tc_pieces(g, c.st));
     }
     r.row0 = c0;
-    if (want) launch_rows<true>(r, rows, warps, c.st);
-    else launch_rows<false>(r, rows, warps, c.st);
+    CUDA_OK(want ? launch_rows<true>(r, rows, warps, c.st) : launch_rows<false>(r, rows, warps, c.st));
     if (c.dX) {
       GemmArgs g = g0;
       g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = r.E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;

@@ -155,6 +155,7 @@ template <bool BWD, int GATE, int CH> struct Ring {
 // GATE: 0 none, 1 one row for all rows, 2 read with each row
 template <int LANES, int GATE>
 __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
+  pdl_wait(); pdl_trigger();
   constexpr int CH = FWD_CH, BLOCK = Layout<LANES>::BLOCK;
   using R = Ring<false, GATE, CH>;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -271,6 +272,7 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_fwd_kernel(con
 // GATE: 0 none, 1 one row for all of the unit's rows, 2 read with each row, its gradient written at the end of each group
 template <int LANES, int GATE>
 __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
+  pdl_wait(); pdl_trigger();
   constexpr int CH = BWD_CH, BLOCK = Layout<LANES>::BLOCK;
   using R = Ring<true, GATE, CH>;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -434,6 +436,7 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(con
 // adds a 32nd of the units in order, and the 32 sums are added in order.
 struct ParamOut { float* out[4]; float* dgate; };
 __global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* __restrict__ partial, const ParamOut po, int units, int per_group, int d) {
+  pdl_wait(); pdl_trigger();
   __shared__ float4 sh[32][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int c = blockIdx.x * 128 + 4 * lane;
@@ -526,8 +529,7 @@ int launch_norm(const NormArgs& a, cudaStream_t st) {
   if constexpr (BWD) kernel = norm_gate_bwd_kernel<LANES, GATE>;
   else kernel = norm_gate_fwd_kernel<LANES, GATE>;
   if (!ppu_set_smem_once(attr, kernel, bytes)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
-  kernel<<<(a.units + L::UNITS - 1) / L::UNITS, L::BLOCK, bytes, st>>>(a);
-  CUDA_OK(cudaGetLastError());
+  CUDA_OK(ppu_launch_dependent(kernel, (a.units + L::UNITS - 1) / L::UNITS, L::BLOCK, bytes, st, a));
   return PPU_OK;
 }
 template <int LANES, bool BWD>
@@ -609,7 +611,6 @@ extern "C" int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void
   if (rc2) return rc2;
   const int groups = s.gate_mode == 1 ? s.units / s.per_group : 0;      // gate rows still to be summed
   const ParamOut po = {{dpost_gain, dpost_shift, dpre_gain, dpre_shift}, dgate};
-  norm_gate_params_kernel<<<dim3((d + 127) / 128, 4 + groups), 1024, 0, st>>>(a.partial, po, s.units, s.per_group, d);
-  CUDA_OK(cudaGetLastError());
+  CUDA_OK(ppu_launch_dependent(norm_gate_params_kernel, dim3((d + 127) / 128, 4 + groups), 1024, 0, st, a.partial, po, s.units, s.per_group, d));
   return PPU_OK;
 }
