@@ -328,13 +328,13 @@ int ppu_attention_bwd_static(const void* qkv, const void* U, const float* lse, c
  * multiple of 8 up to 16384, row strides multiples of 8, X, E, dX, dE 16-byte aligned; T <= 2^20,
  * V <= 2^22, any values within.  chunk_rows: 0 = up to 6144, as many as keep 1 GiB of softmax,
  * else the rows of a chunk (rounded up to a multiple of 256); chunks below 4096 rows are slower.  workspace: DEVICE, 256-byte
- * aligned, of the size ppu_head_query_bytes gives for the same T, d, V, gradients (1: dX, 2: dE) and
- * chunk_rows; calls that may overlap on the GPU need one each.  flags: DEVICE int32 [8], zeroed by the
+ * aligned, of the size ppu_head_query_bytes gives for the same T, d, V, gradients (1: dX, 2: dE),
+ * chunk_rows and k (entries a row; 1 for xent); calls that may overlap on the GPU need one each.  flags: DEVICE int32 [8], zeroed by the
  * caller once, or null (nothing is reported); read by ppu_op_status.  All other pointers DEVICE.
  * Asynchronous on the stream; results do not depend on timing.  Sizes that are not 0 must not exceed
  * the buffers; the calls may be captured. */
 #define PPU_MAX_TEACHER_ENTRIES 128
-int ppu_head_query_bytes(int T, int d, int V, int grads, int chunk_rows, size_t* bytes);
+int ppu_head_query_bytes(int T, int d, int V, int grads, int chunk_rows, int k, size_t* bytes);
 int ppu_head_xent(const void* X, int64_t ldx, const void* E, int64_t lde, const int32_t* target,
                   const float* row_weight, int T, int d, int V, float* loss, float* row_loss,
                   float* lse, void* dX, int64_t lddx, void* dE, int64_t ldde, int chunk_rows,

@@ -140,10 +140,10 @@ Head head_operands(PyObject* x, PyObject* e) {
 }
 // outputs and workspace of a head loss; call(loss, row_loss, lse, dX, dE, workspace, bytes, stream)
 template <typename F>
-PyObject* head_call(const Head& h, int grads, int chunk_rows, PyObject* ws_given, F call) {
+PyObject* head_call(const Head& h, int k, int grads, int chunk_rows, PyObject* ws_given, F call) {
   const c10::cuda::CUDAGuard guard((c10::DeviceIndex)h.dev);
   size_t bytes = 0;
-  check(ppu_head_query_bytes(h.T, h.d, h.V, grads, chunk_rows, &bytes));
+  check(ppu_head_query_bytes(h.T, h.d, h.V, grads, chunk_rows, k, &bytes));
   const at::Tensor ws = workspace(ws_given, bytes, h.dev);
   at::Tensor out[5] = {make({}, at::kFloat, h.dev), make({h.T}, at::kFloat, h.dev), make({h.T}, at::kFloat, h.dev), at::Tensor(), at::Tensor()};
   if (grads & 1) out[3] = make({h.T, h.d}, at::kBFloat16, h.dev);
@@ -169,7 +169,7 @@ PyObject* head_xent(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float* w = (const float*)optional(a[3], "row_weight", at::kFloat, {h.T}, h.dev);
     const int grads = int_arg(a[4], "grad"), chunk = int_arg(a[5], "chunk_rows");
     int32_t* flags = (int32_t*)optional(a[7], "flags", at::kInt, {8}, h.dev);
-    return head_call(h, grads, chunk, a[6], [&](float* loss, float* row, float* lse, void* dX, void* dE, void* ws, size_t nb, void* st) {
+    return head_call(h, 1, grads, chunk, a[6], [&](float* loss, float* row, float* lse, void* dX, void* dE, void* ws, size_t nb, void* st) {
       return ppu_head_xent(h.X.p, h.X.ld, h.E.p, h.E.ld, target, w, h.T, h.d, h.V, loss, row, lse, dX, h.d, dE, h.d, chunk, ws, nb, flags, st);
     });
   });
@@ -186,7 +186,7 @@ PyObject* head_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float* w = (const float*)optional(a[6], "row_weight", at::kFloat, {h.T}, h.dev);
     const int grads = int_arg(a[7], "grad"), chunk = int_arg(a[8], "chunk_rows");
     int32_t* flags = (int32_t*)optional(a[10], "flags", at::kInt, {8}, h.dev);
-    return head_call(h, grads, chunk, a[9], [&](float* loss, float* row, float* lse, void* dX, void* dE, void* ws, size_t nb, void* st) {
+    return head_call(h, k, grads, chunk, a[9], [&](float* loss, float* row, float* lse, void* dX, void* dE, void* ws, size_t nb, void* st) {
       return ppu_head_distill(h.X.p, h.X.ld, h.E.p, h.E.ld, (const int32_t*)ids.p, ids.ld, (const float*)z.p, z.ld, k, tl, temp, w, h.T, h.d, h.V,
                               loss, row, lse, dX, h.d, dE, h.d, chunk, ws, nb, flags, st);
     });

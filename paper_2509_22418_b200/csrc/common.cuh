@@ -46,6 +46,13 @@ enum GemmEpilogue {
   // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_out_bf16 only)
   EPI_OUT_BF16 = 8
 };
+// the columns of each row whose x is wanted itself (EPI_PIECES): ids [M][ld] ascending, k of them, behind them or
+// elsewhere negative; with k > 1, off [M][ld_off] = how many of a row's ids lie before each piece
+struct PieceEntries {
+  const int32_t* ids; int64_t ld; int k;
+  const uint8_t* off; int64_t ld_off;
+  float* x;                              // out [M][k]
+};
 constexpr int PIECE = 64;               // columns of one softmax piece
 constexpr float PIECE_RANGE = 60.f;
 
@@ -74,6 +81,7 @@ struct GemmArgs {
   // columns of C from N up to the next multiple of PIECE are written as zeros
   float piece_scale = 1.f; float2* piece_stats = nullptr; int64_t ld_pieces = 0;
   unsigned* zero_word = nullptr;     // EPI_PIECES: a word that the launch sets to 0 (a counter of the kernel after it), or null
+  PieceEntries entries = {};
   const float* row_scale = nullptr;  // EPI_OUT_BF16: fp32 [M]
   // part of an operator on a caller's tensors: tensor maps are encoded for this launch, which is a dependent one
   bool transient = false;

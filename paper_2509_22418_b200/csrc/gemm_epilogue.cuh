@@ -86,6 +86,7 @@ struct TcParams {
   int rope_S, rope_dh, rope_cols;
   void* C3; long long ldc3; int c3_lo, c3_hi;
   float piece_scale; float2* piece_stats; long long ld_pieces;
+  PieceEntries entries;
   const float* row_scale; unsigned* zero_word;
   int dependent;   // launched as a programmatic dependent
 };
@@ -338,6 +339,9 @@ __device__ __forceinline__ void store_group(const CUtensorMap* map, uint32_t buf
 // are kept relative to their own maximum and brought into line afterwards.
 // The exponent is one fused multiply-add on the accumulator; ref is the rounded product used in it,
 // so its rounding cancels.
+// The entries' own x are taken from tensor memory a column at a time: a warp's 32 rows have two in a
+// piece with 32 entries in 32768 columns.  (As dot products in the row kernel they were a gather of 4 KB of E
+// for each entry: 106 of 1200 us at 4096 x 2048 x 32768.)
 __device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0,
                                              uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
   const int mw = m0 + quarter * 32, m = mw + lane;
@@ -349,7 +353,28 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMa
     uint32_t r[PIECE];
     tmem_ld32(t_row + c0, r);
     tmem_ld32(t_row + c0 + 32, r + 32);
+    int at = 0, end = 0, id = -1;          // this row's entries in the piece, and the first one's column
+    if (m < p.M) {
+      if (p.entries.k > 1) {
+        const uint8_t* off = p.entries.off + (long long)m * p.entries.ld_off + nb / PIECE;
+        at = off[0]; end = off[1];
+      } else {
+        end = 1;
+      }
+      if (at < end) id = __ldg(p.entries.ids + (long long)m * p.entries.ld + at);
+      if (id < nb || id >= nb + PIECE) id = -1;
+    }
     tmem_ld_wait();
+    for (unsigned any = __ballot_sync(0xffffffffu, id >= 0); any; any = __ballot_sync(0xffffffffu, id >= 0)) {
+      const int col = __shfl_sync(0xffffffffu, id, __ffs(any) - 1);
+      const float x = __uint_as_float(tmem_ld1(t_row + c0 + (col - nb))) * p.piece_scale;
+      while (id == col) {                  // an id may be given several times
+        p.entries.x[(long long)m * p.entries.k + at] = x;
+        ++at;
+        id = at < end ? __ldg(p.entries.ids + (long long)m * p.entries.ld + at) : -1;
+      }
+      __syncwarp();
+    }
     if (nb + PIECE > p.N) {                // columns past the vocabulary: nothing
 #pragma unroll
       for (int j = 0; j < PIECE; ++j)

@@ -259,7 +259,7 @@ TcParams make_params(const GemmArgs& g) {
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
   p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
-  p.row_scale = g.row_scale; p.zero_word = g.zero_word; p.dependent = g.transient ? 1 : 0;
+  p.entries = g.entries; p.row_scale = g.row_scale; p.zero_word = g.zero_word; p.dependent = g.transient ? 1 : 0;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes

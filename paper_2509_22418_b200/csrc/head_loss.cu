@@ -12,10 +12,10 @@
 // the chunk's two gradient products are done: a [rows, V] buffer of bounded size, not [T, V].
 //   1. tcgen05 product of the chunk's rows with E^T.  Its epilogue works the vocabulary in pieces of 64
 //      columns: bf16 powers u = 2^(x - ref), x = s log2(e), and {ref, sum} in fp32; ref is 0 for ordinary
-//      logits (within 41 nats of 0), else the piece's maximum.
-//   2. one block per row joins the pieces to the row's log-sum-exp, computes the entries' logits as
-//      fp32 dot products of their own (k of them, d long: the stored powers would be too coarse for
-//      the loss and for p - 1 next to p = 1) and the row loss.  Then ds_tv = f_t u_tv with one factor per
+//      logits (within 41 nats of 0), else the piece's maximum.  The entries' own x are kept in fp32 (the powers
+//      would be too coarse for the loss and for p - 1 next to p = 1); for that a kernel before it has
+//      sorted each row's entries and counted how many lie before each piece (not needed for one entry a row).
+//   2. a warp or a block per row joins the pieces to the row's log-sum-exp and forms the row loss.  Then ds_tv = f_t u_tv with one factor per
 //      row: the powers stay as they are, but for the entries' places, which are overwritten, and for
 //      pieces (rows) beyond the range of the common reference, which are rescaled.
 //   3. dX = f (u E), the factor applied in the product's epilogue, and dE = u^T (f X) with f X formed in
@@ -27,6 +27,7 @@
 // sums are fp32.  (The tensor cores' fp32 sums drop what lies below the last bit, so logits come out low
 // by up to 2^-24 per 16 products: 2e-6 of a logit at d = 2048.)
 #include <algorithm>
+#include <climits>
 #include "../../include/ppu.h"
 #include "common.cuh"
 
@@ -48,7 +49,9 @@ struct RowArgs {
   Targets tg;
   bf16* u; int64_t ldu;                  // powers of this chunk's rows; null without gradients
   const float2* stats; int64_t ld_pieces; int n_pieces;
-  const bf16* X; int64_t ldx; const bf16* E; int64_t lde; int d, V;
+  const bf16* X; int64_t ldx; int d, V;
+  const float* x;                        // the entries' x [rows][k]
+  int sorted;                            // tg is the chunk's own (sorted) copy: its rows are the chunk's
   int64_t row0;                          // first row of the chunk
   int T;
   float scale2;                          // log2(e) / temperature
@@ -133,6 +136,65 @@ __device__ __forceinline__ void scale_piece(bf16* p, float f) {
   }
 }
 
+// A chunk's entries, each row's in ascending order of id (the rank of each by comparing it with all: k is at most
+// 128), absent ones as -1 behind them; and off[p] = entries before piece p.  One warp to a row.
+__global__ void __launch_bounds__(128) sort_entries_kernel(Targets tg, int64_t row0, int rows, int V, int n_pieces, int32_t* ids, float* zs, uint8_t* off,
+                                                           int64_t ld_off, int* flags) {
+  __shared__ int s_key[4][MAX_ENTRIES], s_id[4][MAX_ENTRIES];
+  pdl_wait(); pdl_trigger();
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * 4 + g, t = row0 + row;
+  if (row >= rows) return;
+  constexpr int PER = MAX_ENTRIES / 32;
+  float z[PER];
+  int key[PER], present = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = lane + 32 * i;
+    key[i] = INT_MAX; z[i] = 0.f;
+    if (j < tg.k) {
+      const int id = tg.ids[t * tg.ld_ids + j];
+      z[i] = tg.z[t * tg.ld_z + j];
+      if (present_id(id, V, flags) && !(z[i] * tg.inv_temp == -INFINITY)) { key[i] = id; ++present; }
+      s_key[g][j] = key[i];
+    }
+  }
+  present = __reduce_add_sync(0xffffffffu, present);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = lane + 32 * i;
+    if (j >= tg.k) continue;
+    int rank = 0;
+    for (int q = 0; q < tg.k; ++q) rank += s_key[g][q] < key[i] || (s_key[g][q] == key[i] && q < j);
+    const int id = key[i] == INT_MAX ? -1 : key[i];
+    s_id[g][rank] = id;
+    ids[row * tg.k + rank] = id;
+    zs[row * tg.k + rank] = z[i];
+  }
+  __syncwarp();
+  // a lane goes through a 32nd of the pieces, four to a store; where it starts it searches
+  const int n4 = (int)(ld_off / 4), per = (n4 + 31) / 32;
+  int at = 0;
+  {
+    int hi = present;
+    const int first = 4 * per * lane * PIECE;
+    while (at < hi) {
+      const int mid = (at + hi) / 2;
+      if (s_id[g][mid] < first) at = mid + 1; else hi = mid;
+    }
+  }
+  for (int w = per * lane; w < min(n4, per * (lane + 1)); ++w) {
+    uint32_t word = 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      while (at < present && s_id[g][at] < (4 * w + b) * PIECE) ++at;
+      word |= (uint32_t)at << (8 * b);
+    }
+    *reinterpret_cast<uint32_t*>(off + row * ld_off + 4 * w) = word;
+  }
+}
+
 // Step 2 for W warps to a row: one (four rows to a block, no barrier) where the rows alone fill the
 // machine, 4 or 16 for few rows with many pieces or entries to go through.
 template <bool GRAD, int W>
@@ -147,6 +209,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
   const int g = W == 1 ? threadIdx.x >> 5 : 0;
   const int64_t row = (int64_t)blockIdx.x * R + g, t = a.row0 + row;        // row of the chunk, of the call
   const int k = a.tg.k;
+  const int64_t te = a.sorted ? row : t;                                     // row of the entries
   auto sync = [] { if constexpr (W == 1) __syncwarp(); else __syncthreads(); };
 
   pdl_wait(); pdl_trigger();
@@ -170,10 +233,10 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         const int j = lane + 32 * i;
         id[i] = -1; zs[i] = 0.f; in[i] = false;
         if (j < k) {
-          id[i] = a.tg.ids[t * a.tg.ld_ids + j];
+          id[i] = a.tg.ids[te * a.tg.ld_ids + j];
           in[i] = present_id(id[i], a.V, a.flags);
           if (in[i] && a.tg.z) {
-            zs[i] = a.tg.z[t * a.tg.ld_z + j] * a.tg.inv_temp;
+            zs[i] = a.tg.z[te * a.tg.ld_z + j] * a.tg.inv_temp;
             in[i] = !(zs[i] == -INFINITY);
           }
         }
@@ -201,7 +264,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           if (q != 0.f) entropy += q * (zs[i] - norm);
           total += q;
         }
-        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; }
+        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; s_l[g][j] = in[i] ? a.x[row * k + j] : 0.f; }
       }
       total = warp_sum(total); entropy = warp_sum(entropy);
       if (lane == 0) { s_total[g] = total; s_entropy[g] = entropy; s_any[g] = any; }
@@ -259,46 +322,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           for (int i = tid; i < a.d / 8; i += N) fx[i] = make_uint4(0, 0, 0, 0);
       }
     } else {
-      // the entries' logits, two to a warp at a time: their rows of E come from anywhere in HBM, so loads in flight count
       const int n8 = a.d / 8;
-      for (int j = 2 * warp; j < k; j += 2 * W) {
-        const bool two = j + 1 < k;
-        const int i0 = max(s_id[g][j], 0), i1 = two ? max(s_id[g][j + 1], 0) : i0;
-        const uint4* e0 = reinterpret_cast<const uint4*>(a.E + (int64_t)i0 * a.lde);
-        const uint4* e1 = reinterpret_cast<const uint4*>(a.E + (int64_t)i1 * a.lde);
-        float d0 = 0.f, d1 = 0.f;
-        if (two) {
-#pragma unroll 4
-          for (int i = lane; i < n8; i += 32) {
-            const uint4 xv = xr[i], v0 = e0[i], v1 = e1[i];
-            float x[8], e[8];
-            unpack8(xv, x);
-            unpack8(v0, e);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) d0 = fmaf(x[c], e[c], d0);
-            unpack8(v1, e);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) d1 = fmaf(x[c], e[c], d1);
-          }
-        } else {
-#pragma unroll 4
-          for (int i = lane; i < n8; i += 32) {
-            const uint4 xv = xr[i], v0 = e0[i];
-            float x[8], e[8];
-            unpack8(xv, x);
-            unpack8(v0, e);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) d0 = fmaf(x[c], e[c], d0);
-          }
-        }
-        d0 = warp_sum(d0);
-        if (two) d1 = warp_sum(d1);
-        if (lane == 0) {
-          s_l[g][j] = d0 * a.scale2;
-          if (two) s_l[g][j + 1] = d1 * a.scale2;
-        }
-      }
-      sync();
       float w;
       if (a.weight) {
         w = a.weight[t];
@@ -344,12 +368,11 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         for (int j = tid; j < k; j += N) {          // those stand: overwrite the entries' places
           const int id = s_id[g][j];
           if (id < 0) continue;
+          if (j > 0 && s_id[g][j - 1] == id) continue;          // an id given twice: its first entry writes for all
           float q = 0.f;
-          bool first = true;                        // an id given twice: its first entry writes for all
-          for (int i = 0; i < k; ++i)
-            if (s_id[g][i] == id) { if (i < j) first = false; q += s_q[g][i]; }
+          for (int i = j; i < k && s_id[g][i] == id; ++i) q += s_q[g][i];
           // p - q / Q with p = exp(x): (exp(x) - 1) + (1 - q / Q) keeps its digits where p is next to 1
-          if (first && total != 0.f)
+          if (total != 0.f)
             ur[id] = __float2bfloat16_rn((expm1f((s_l[g][j] - lse2) * LN2) + (total - q) / total) * exp2f(lse2 - ref));
         }
       }
@@ -426,9 +449,10 @@ int splits_for(int64_t M, int64_t N, int64_t K) {
 struct Plan {
   int64_t ldu, n_pieces, chunk, usual;         // usual: rows of a chunk by default (decides orders of sums: results do not depend on chunk_rows)
   int chunks, sx, se;                          // split-K factors of dX and dE
-  size_t off_weighted, off_factor, off_stats, off_u, off_fx, off_acc, off_part, bytes;
+  int64_t ld_off;
+  size_t off_weighted, off_factor, off_stats, off_x, off_ids, off_z, off_before, off_u, off_fx, off_acc, off_part, bytes;
 };
-Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
+Plan make_plan(int T, int d, int V, int want, int chunk_rows, int k) {
   Plan p;
   p.ldu = round_up(V, PIECE);
   p.n_pieces = p.ldu / PIECE;
@@ -446,6 +470,11 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows) {
   p.off_weighted = take(4ll * T);
   p.off_factor = take(4ll * p.chunk);
   p.off_stats = take(8ll * p.chunk * p.n_pieces);
+  p.ld_off = round_up(p.n_pieces + 1, 4);
+  p.off_x = take(4ll * p.chunk * k);
+  p.off_ids = take(k > 1 ? 4ll * p.chunk * k : 0);
+  p.off_z = take(k > 1 ? 4ll * p.chunk * k : 0);
+  p.off_before = take(k > 1 ? p.chunk * p.ld_off : 0);
   p.off_u = take(want ? p.chunk * row_bytes : 0);
   p.off_fx = take((want & 2) ? 2ll * p.chunk * d : 0);
   p.off_acc = take((want & 2) && p.chunks > 1 ? 4ll * V * d : 0);
@@ -490,13 +519,11 @@ struct HeadCall {
     if (r_) return ppu_fail(r_ == -4 ? PPU_ESHAPE : PPU_ECUDA, "head product failed (%d)", r_); \
   } while (0)
 
-// warps to a row: enough that the rows fill the machine, no more than there are pairs of entries or
-// 64 pieces a lane to share (24 rows, 64 entries, 32768 ids: FEW16 us with 16 warps, FEW1 with one; 4096 rows of
-// 32 entries: MANY1 with one, MANY4 with four)
-int warps_for(int64_t rows, int k, int64_t n_pieces) {
-  const int64_t share = std::max<int64_t>(k / 2, n_pieces / 256);
-  if (rows >= 32 * SMS || share < 4) return 1;
-  return rows >= 8 * SMS || share < 16 ? 4 : 16;
+// warps to a row: one where the rows fill the machine or have little to go through (64 pieces are two a lane)
+int warps_for(int64_t rows, int64_t n_pieces) {
+  const int64_t share = n_pieces / 64;
+  if (rows >= 16 * SMS || share < 4) return 1;
+  return rows >= 2 * SMS || share < 16 ? 4 : 16;
 }
 template <bool GRAD>
 cudaError_t launch_rows(const RowArgs& r, int64_t rows, int warps, cudaStream_t st) {
@@ -534,7 +561,8 @@ int run_head(const HeadCall& c) {
   if (!aligned16(c.X) || !aligned16(c.E) || !aligned16(c.dX) || !aligned16(c.dE))
     return ppu_fail(PPU_EINVAL, "operands must be 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(c.ws) & 255) return ppu_fail(PPU_EINVAL, "workspace not 256-byte aligned");
-  const Plan p = make_plan(c.T, c.d, c.V, want, c.chunk_rows);
+  const int k = c.tg.k;
+  const Plan p = make_plan(c.T, c.d, c.V, want, c.chunk_rows, k);
   if (c.ws_bytes < p.bytes) return ppu_fail(PPU_ENOMEM, "workspace has %zu bytes, %zu needed", c.ws_bytes, p.bytes);
 
   uint8_t* ws = (uint8_t*)c.ws;
@@ -562,11 +590,18 @@ int run_head(const HeadCall& c) {
   }
   RowArgs r;
   r.tg = c.tg; r.u = u; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
-  r.X = (const bf16*)c.X; r.ldx = c.ldx; r.E = (const bf16*)c.E; r.lde = c.lde; r.d = c.d; r.V = c.V; r.T = c.T;
+  r.X = (const bf16*)c.X; r.ldx = c.ldx; r.d = c.d; r.V = c.V; r.T = c.T;
   r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = c.T > (1 << 10) ? count : nullptr;
   r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
   r.done = done; r.loss = c.loss; r.flags = c.flags;
-  const int warps = warps_for(p.usual, c.tg.k, p.n_pieces);
+  float* ex = (float*)(ws + p.off_x);
+  int32_t* sorted_ids = (int32_t*)(ws + p.off_ids);
+  float* sorted_z = (float*)(ws + p.off_z);
+  uint8_t* before = ws + p.off_before;
+  r.x = ex; r.sorted = k > 1;
+  if (k > 1) { r.tg.ids = sorted_ids; r.tg.ld_ids = k; r.tg.z = sorted_z; r.tg.ld_z = k; }
+  const bf16* E = (const bf16*)c.E;
+  const int warps = warps_for(p.usual, p.n_pieces);
   const int64_t per_block = warps == 1 ? 4 : 1;
   r.blocks = 0;
   for (int64_t c0 = 0; c0 < c.T; c0 += p.chunk) r.blocks += (unsigned)((std::min<int64_t>(p.chunk, c.T - c0) + per_block - 1) / per_block);
@@ -575,12 +610,17 @@ int run_head(const HeadCall& c) {
   g0.C2 = nullptr; g0.aux = nullptr; g0.ldaux = 0; g0.flags = c.flags; g0.transient = true;
   for (int64_t c0 = 0; c0 < c.T; c0 += p.chunk) {
     const int64_t rows = std::min<int64_t>(p.chunk, c.T - c0);
+    if (k > 1)
+      CUDA_OK(ppu_launch_dependent(sort_entries_kernel, (unsigned)((rows + 3) / 4), 128, 0, c.st, c.tg, c0, (int)rows, c.V, (int)p.n_pieces, sorted_ids,
+                                   sorted_z, before, p.ld_off, c.flags));
     {
       GemmArgs g = g0;
       g.A = r.X + c0 * c.ldx; g.lda = c.ldx; g.a_kmajor = 1;
-      g.B = r.E; g.ldb = c.lde; g.b_kmajor = 1;
+      g.B = E; g.ldb = c.lde; g.b_kmajor = 1;
       g.M = (int)rows; g.N = c.V; g.K = c.d; g.epilogue = EPI_PIECES; g.C = u; g.ldc = p.ldu;
       if (c0 == 0) g.zero_word = done;
+      if (k > 1) g.entries = {sorted_ids, k, k, before, p.ld_off, ex};
+      else g.entries = {c.tg.ids + c0 * c.tg.ld_ids, c.tg.ld_ids, 1, nullptr, 0, ex};
       g.piece_scale = r.scale2; g.piece_stats = stats; g.ld_pieces = p.n_pieces;
       GEMM_OK(launch_gemm_tc_pieces(g, c.st));
     }
@@ -588,7 +628,7 @@ int run_head(const HeadCall& c) {
     CUDA_OK(want ? launch_rows<true>(r, rows, warps, c.st) : launch_rows<false>(r, rows, warps, c.st));
     if (c.dX) {
       GemmArgs g = g0;
-      g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = r.E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;
+      g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;
       g.M = (int)rows; g.N = c.d; g.K = c.V; g.C = (bf16*)c.dX + c0 * c.lddx; g.ldc = c.lddx;
       rc = product_bf16(g, p.sx, part, c.st);
       if (rc) return rc;
@@ -617,12 +657,14 @@ int run_head(const HeadCall& c) {
 
 }  // namespace
 
-extern "C" int ppu_head_query_bytes(int T, int d, int V, int grads, int chunk_rows, size_t* bytes) {
+extern "C" int ppu_head_query_bytes(int T, int d, int V, int grads, int chunk_rows, int k, size_t* bytes) {
   if (!bytes) return ppu_fail(PPU_EINVAL, "bytes is null");
   if (grads < 0 || grads > 3) return ppu_fail(PPU_EINVAL, "grads is a sum of 1 (dX) and 2 (dE)");
   const int rc = check_sizes(T, d, V, chunk_rows);
   if (rc) return rc;
-  *bytes = make_plan(T, d, V, grads, chunk_rows).bytes;
+  if (k < 1 || k > PPU_MAX_TEACHER_ENTRIES)
+    return ppu_fail(PPU_ESHAPE, "k must lie in 1..%d (got %d)", PPU_MAX_TEACHER_ENTRIES, k);
+  *bytes = make_plan(T, d, V, grads, chunk_rows, k).bytes;
   return PPU_OK;
 }
 

@@ -367,10 +367,10 @@ def _binding():
     return _ops
 
 
-def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0) -> int:
-    """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE)."""
+def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0, k=1) -> int:
+    """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE); k: entries a row (1 for xent)."""
     n = C.c_size_t(0)
-    _check(lib().ppu_head_query_bytes(T, d, V, grads, chunk_rows, C.byref(n)))
+    _check(lib().ppu_head_query_bytes(T, d, V, grads, chunk_rows, k, C.byref(n)))
     return n.value
 
 

@@ -477,7 +477,7 @@ def test_strided_operands_and_untouched_surroundings():
     # the C call with strided outputs
     dX = torch.full((T + 1, d + 16), 5.0, dtype=torch.bfloat16, device="cuda")
     dE = torch.full((V + 1, d + 8), 5.0, dtype=torch.bfloat16, device="cuda")
-    nb = ppu.ppu_head_query_bytes(T, d, V)
+    nb = ppu.ppu_head_query_bytes(T, d, V, k=k)
     ws = torch.full((nb + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
     out = torch.full((2 * T + 1 + 8,), 9.0, device="cuda")
     p = lambda t: C.c_void_p(t.data_ptr())  # noqa: E731
@@ -549,7 +549,7 @@ def test_sizes_of_the_workspace(ppu):
     for bad in [(1, 12, 8), (1, 0, 8), (1, 16392, 8), (-1, 8, 8), (1, 8, 0), ((1 << 20) + 1, 8, 8), (1, 8, (1 << 22) + 1)]:
         with pytest.raises(ppu.PpuError):
             q(*bad)
-    for kw in (dict(grads=4), dict(grads=-1), dict(chunk_rows=-1)):
+    for kw in (dict(grads=4), dict(grads=-1), dict(chunk_rows=-1), dict(k=0), dict(k=129)):
         with pytest.raises(ppu.PpuError):
             q(8, 8, 8, **kw)
 
