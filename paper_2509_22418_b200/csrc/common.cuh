@@ -13,7 +13,9 @@ enum { PPU_FLAG_TOKEN = 0, PPU_FLAG_TIMEOUT = 1, PPU_FLAG_COUNT = 8 };
 // The kernels of one operator follow one another within microseconds.  Launched as programmatic
 // dependents, a kernel's blocks are placed and set up (barriers, tensor memory, descriptors) while the one before
 // it still runs; pdl_wait() returns when that one has finished and its writes are visible, so everything
-// that touches global memory comes after it.  Without the launch attribute both are no-ops.
+// that touches global memory comes after it - and what an earlier kernel of the operator wrote is read
+// by plain loads, not as read-only data (__ldg, const __restrict__), which may be moved ahead of the wait.
+// Without the launch attribute both are no-ops.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... P, typename... A>

@@ -361,7 +361,7 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMa
       } else {
         end = 1;
       }
-      if (at < end) id = __ldg(p.entries.ids + (long long)m * p.entries.ld + at);
+      if (at < end) id = p.entries.ids[(long long)m * p.entries.ld + at];
       if (id < nb || id >= nb + PIECE) id = -1;
     }
     tmem_ld_wait();
@@ -371,7 +371,7 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMa
       while (id == col) {                  // an id may be given several times
         p.entries.x[(long long)m * p.entries.k + at] = x;
         ++at;
-        id = at < end ? __ldg(p.entries.ids + (long long)m * p.entries.ld + at) : -1;
+        id = at < end ? p.entries.ids[(long long)m * p.entries.ld + at] : -1;
       }
       __syncwarp();
     }
@@ -408,7 +408,7 @@ __device__ __forceinline__ void drain_out_bf16(const TcParams& p, const CUtensor
   const int mw = m0 + quarter * 32, m = mw + lane;
   const bool row_ok = m < p.M;
   const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
-  const float f = p.row_scale && row_ok ? __ldg(p.row_scale + m) : 1.f;
+  const float f = p.row_scale && row_ok ? p.row_scale[m] : 1.f;
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += 64) {
     const int nb = n0 + c0;

@@ -222,24 +222,32 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
     __syncthreads();
   }
   if (row < rows) {
+    // what the row needs from global memory is asked for first: the rest is a chain of short steps
+    const float2* st = a.stats + row * a.ld_pieces;
+    const uint4* xr = reinterpret_cast<const uint4*>(a.X + t * a.ldx);
+    const float2 st0 = tid < a.n_pieces ? st[tid] : make_float2(0.f, 0.f);
+    uint4 x0 = make_uint4(0, 0, 0, 0);
+    if (GRAD && a.fx && tid < a.d / 8) x0 = xr[tid];
+    const float row_weight = a.weight ? a.weight[t] : 0.f;
     // the row's entries and their q
     if (warp == 0) {
       constexpr int PER = MAX_ENTRIES / 32;
-      float zs[PER]; int id[PER]; bool in[PER];
+      float zs[PER], ex[PER]; int id[PER]; bool in[PER];
       float top = -INFINITY;
       bool any = false;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int j = lane + 32 * i;
-        id[i] = -1; zs[i] = 0.f; in[i] = false;
+        id[i] = -1; zs[i] = ex[i] = 0.f; in[i] = false;
         if (j < k) {
           id[i] = a.tg.ids[te * a.tg.ld_ids + j];
-          in[i] = present_id(id[i], a.V, a.flags);
-          if (in[i] && a.tg.z) {
-            zs[i] = a.tg.z[te * a.tg.ld_z + j] * a.tg.inv_temp;
-            in[i] = !(zs[i] == -INFINITY);
-          }
+          ex[i] = a.x[row * k + j];                 // (of an absent entry: whatever is there, and not used)
+          if (a.tg.z) zs[i] = a.tg.z[te * a.tg.ld_z + j] * a.tg.inv_temp;
         }
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        if (lane + 32 * i < k) in[i] = present_id(id[i], a.V, a.flags) && !(zs[i] == -INFINITY);
         if (in[i]) { top = fmaxf(top, zs[i]); any = true; }
       }
       any = __any_sync(0xffffffffu, any);
@@ -264,17 +272,16 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           if (q != 0.f) entropy += q * (zs[i] - norm);
           total += q;
         }
-        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; s_l[g][j] = in[i] ? a.x[row * k + j] : 0.f; }
+        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; s_l[g][j] = ex[i]; }
       }
       total = warp_sum(total); entropy = warp_sum(entropy);
       if (lane == 0) { s_total[g] = total; s_entropy[g] = entropy; s_any[g] = any; }
     }
     // the pieces: with the common reference throughout, a plain sum
-    const float2* st = a.stats + row * a.ld_pieces;
-    Piece all = {0.f, 0.f};
-    bool plain = true;
+    Piece all = {0.f, st0.y};
+    bool plain = st0.x == 0.f;
 #pragma unroll 4
-    for (int i = tid; i < a.n_pieces; i += N) {
+    for (int i = tid + N; i < a.n_pieces; i += N) {
       const float2 v = st[i];
       plain &= v.x == 0.f;
       all.s += v.y;
@@ -306,7 +313,6 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
 
     // the reference of the row's powers: 0, or where that is too far from their sum, the sum itself
     const float ref = fabsf(lse2) <= PIECE_RANGE ? 0.f : lse2;
-    const uint4* xr = reinterpret_cast<const uint4*>(a.X + t * a.ldx);
     bf16* ur = a.u + row * a.ldu;
     uint4* fx = GRAD && a.fx ? reinterpret_cast<uint4*>(a.fx + row * a.d) : nullptr;
     if (!s_any[g]) {                                // the row has no loss and no gradient
@@ -325,7 +331,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
       const int n8 = a.d / 8;
       float w;
       if (a.weight) {
-        w = a.weight[t];
+        w = row_weight;
       } else if (a.count) {
         w = 1.f / (float)*a.count;
       } else {
@@ -351,7 +357,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         if (fx)
 #pragma unroll 4
           for (int i = tid; i < n8; i += N) {
-            const uint4 xv = xr[i];
+            const uint4 xv = i == tid ? x0 : xr[i];
             float v[8];
             unpack8(xv, v);
 #pragma unroll
@@ -402,8 +408,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
 
 // out bf16 [rows, 4 n4] = sum of `splits` fp32 partial products, in index order, times the row's factor
 __global__ void __launch_bounds__(256)
-join_partials_kernel(const float* __restrict__ part, int splits, int64_t stride, const float* __restrict__ row_scale,
-                     bf16* __restrict__ out, int64_t ldo, int rows, int n4) {
+join_partials_kernel(const float* part, int splits, int64_t stride, const float* row_scale, bf16* out, int64_t ldo, int rows, int n4) {
   pdl_wait(); pdl_trigger();
   const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
   if (i >= (int64_t)rows * n4) return;

@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(con
 // all units, 4 + g the gate's row g over the units of its group.  A block takes 128 columns (4 to a lane), a warp
 // adds a 32nd of the units in order, and the 32 sums are added in order.
 struct ParamOut { float* out[4]; float* dgate; };
-__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* __restrict__ partial, const ParamOut po, int units, int per_group, int d) {
+__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* partial, const ParamOut po, int units, int per_group, int d) {
   pdl_wait(); pdl_trigger();
   __shared__ float4 sh[32][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
