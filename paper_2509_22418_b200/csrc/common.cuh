@@ -45,7 +45,7 @@ enum GemmEpilogue {
   // x = acc * piece_scale, and piece_stats = {ref, sum of the unrounded powers}; ref is 0 where the
   // piece's largest x lies within +-PIECE_RANGE, else that largest x
   EPI_PIECES = 7,
-  // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_out_bf16 only)
+  // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_two only)
   EPI_OUT_BF16 = 8
 };
 // the columns of each row whose x is wanted itself (EPI_PIECES): ids [M][ld] ascending, k of them, behind them or
@@ -92,7 +92,10 @@ struct GemmArgs {
 int launch_gemm_simt(const GemmArgs& g, cudaStream_t st);
 int launch_gemm_tc(const GemmArgs& g, cudaStream_t st);   // tcgen05 / TMEM / TMA
 int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st);      // EPI_PIECES, both operands K-major, any N
-int launch_gemm_tc_out_bf16(const GemmArgs& g, cudaStream_t st);    // EPI_OUT_BF16, B MN-major
+// Two products in one launch (the second may be null): EPI_OUT_BF16, EPI_STORE_F32 (possibly split) or
+// EPI_RESID_F32, B MN-major, A in either order.  gemm_tc_pairs_two: whether SM pairs on 256 x 256 tiles would work them
+int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st);
+bool gemm_tc_pairs_two(const GemmArgs& g, const GemmArgs* g2);
 // whether launch_gemm_tc accepts EPI_DELTA_BF16 for this product (tile shape and alignment allow
 // a thread to own whole heads of its row); otherwise the caller runs launch_attn_delta
 bool gemm_tc_fuses_delta(const GemmArgs& g);

@@ -94,10 +94,34 @@ struct TcParams {
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of
 // those that have instantiations of their own: drain_cols keeps its registers, and these have 32 KB of
 // shared memory behind the operand stages, through which they store 64-column groups by TMA
-enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_OUT_BF16 = 2 };
+enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_TWO = 2 };
 constexpr int STORE_BYTES = 32 * 128;                      // a warp's 32 rows x 64 bf16 columns
 template <int MODE> struct OutMap { CUtensorMap c; };
 template <> struct OutMap<DRAIN_COLS> {};
+// DRAIN_TWO: a launch works the units of two products (launch_gemm_tc_two), the one with the longer units
+// first; A's order may differ between the two.  This holds the second product.
+template <> struct OutMap<DRAIN_TWO> { CUtensorMap c, a2, b2, c2; TcParams p2; int a_k, a_k2, units, units2, fill; };
+// The i-th unit of block (pair) b of n: the first product's are dealt round; blocks that got one less then
+// have `fill` of the second's, as many as make up for it; the rest are dealt round again.
+__device__ __forceinline__ int two_unit(int i, int b, int n, int units, int units2, int fill) {
+  constexpr int NONE = 0x7fffffff;
+  const int own = units > b ? (units - b - 1) / n + 1 : 0;
+  if (i < own) return b + i * n;
+  i -= own;
+  const int heavy = units % n;
+  int v = 0;
+  if (heavy > 0) {
+    const int light = n - heavy;
+    if (b >= heavy) {
+      if (i < fill) { v = b - heavy + i * light; return v < units2 ? units + v : NONE; }
+      i -= fill;
+    }
+    v = light * fill;
+  }
+  v += n - 1 - b + i * n;
+  return v < units2 ? units + v : NONE;
+}
+
 template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : EPI_WARPS * STORE_BYTES; }
 
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
@@ -106,7 +130,12 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
 TcParams make_params(const GemmArgs& g);
 int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream_t st);   // bn: 256 or 128
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st);
-int launch_gemm_tc_pair_out_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st);
+int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st);
+// units of the second product that take the time of one of the first (overhead: of a unit, in k)
+inline int two_fill(const GemmArgs& g, const GemmArgs& g2, int overhead) {
+  const int k1 = g.K / (g.splits > 1 ? g.splits : 1), k2 = g2.K / (g2.splits > 1 ? g2.splits : 1);
+  return (k1 + overhead) / (k2 + overhead);
+}
 bool encode_out_map(CUtensorMap* map, void* base, long long ld, int rows, int cols);   // for 32 x 64 boxes
 
 // Drains rows [m0 + 32 quarter, +32) x columns [n0 + half BN/2, + BN/2) of the accumulator at
@@ -413,25 +442,27 @@ __device__ __forceinline__ void drain_out_bf16(const TcParams& p, const CUtensor
   for (int c0 = c_begin; c0 < c_end; c0 += 64) {
     const int nb = n0 + c0;
     if (nb >= p.N || mw >= p.M) break;     // warp-uniform
-    uint32_t r[64];
-    tmem_ld32(t_row + c0, r);
-    tmem_ld32(t_row + c0 + 32, r + 32);
-    if (p.aux) {
-      const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb;
-      uint32_t x[64];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (row_ok && nb + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
-      tmem_ld_wait();
-#pragma unroll
-      for (int j = 0; j < 64; ++j)
-        if (row_ok && nb + (j & ~7) < p.N) r[j] = __float_as_uint(__uint_as_float(x[j]) + __uint_as_float(r[j]));
-    } else {
-      tmem_ld_wait();
-    }
     uint32_t o[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) o[j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
+    for (int h = 0; h < 2; ++h) {          // 32 columns at a time: with the partial sums, 64 do not fit the registers
+      uint32_t r[32];
+      tmem_ld32(t_row + c0 + 32 * h, r);
+      if (p.aux) {
+        const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb + 32 * h;
+        uint32_t x[32];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (row_ok && nb + 32 * h + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (row_ok && nb + 32 * h + (j & ~7) < p.N) r[j] = __float_as_uint(__uint_as_float(x[j]) + __uint_as_float(r[j]));
+      } else {
+        tmem_ld_wait();
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[16 * h + j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
+    }
     store_group(out, buf, o, nb, mw, lane);
   }
 }
@@ -440,7 +471,12 @@ template <int MODE>
 __device__ __forceinline__ void drain_mode(const TcParams& p, const OutMap<MODE>& out, uint32_t buf, int m0, int n0, int sp,
                                            uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
   if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, &out.c, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
-  else if constexpr (MODE == DRAIN_OUT_BF16) drain_out_bf16(p, &out.c, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
+}
+// DRAIN_TWO: bf16 results, or fp32 partial sums (of a split product; of several chunks)
+__device__ __forceinline__ void drain_two(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0, int sp, uint32_t t_acc,
+                                          int quarter, int c_begin, int c_end, int lane) {
+  if (p.epilogue == EPI_OUT_BF16) drain_out_bf16(p, out, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
   else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
 

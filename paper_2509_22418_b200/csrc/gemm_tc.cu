@@ -34,7 +34,7 @@ template <int BN> struct Cfg {
 template <int BN, bool A_K, bool B_K, int MODE>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-               const __grid_constant__ OutMap<MODE> mapC, const TcParams p) {
+               const __grid_constant__ OutMap<MODE> mapC, const __grid_constant__ TcParams p) {
   using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -69,40 +69,68 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   if (MODE == DRAIN_PIECES && blockIdx.x == 0 && threadIdx.x == 0 && p.zero_word) *p.zero_word = 0;
 
   const int tiles_mn = p.tiles_m * p.tiles_n;
-  const int num_tiles = tiles_mn * p.splits;
+  int num_tiles = tiles_mn * p.splits;
   const int k_blocks = (p.K + BK - 1) / BK;
+  // units of a DRAIN_TWO launch: those of p, then those of mapC.p2
+  constexpr bool TWO = MODE == DRAIN_TWO, FIT = MODE != DRAIN_COLS;   // FIT: boxes may be smaller than a stage
+  if constexpr (TWO) num_tiles = mapC.units + mapC.units2;
+  auto unit_of = [&](int i) {
+    if constexpr (TWO) return two_unit(i, blockIdx.x, gridDim.x, mapC.units, mapC.units2, mapC.fill);
+    else return (int)(blockIdx.x + i * gridDim.x);
+  };
+  auto second = [&](int u) { if constexpr (TWO) return u >= mapC.units; else return false; };
+  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &mapC.p2 : &p; else return &p; };
+  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? mapC.a_k2 : mapC.a_k) != 0; else return A_K; };
+  struct Place { int sp, m0, n0, kb0, kb1; };
+  auto locate = [&](int u, bool sec) {
+    const TcParams& q = *params(sec);
+    int per = tiles_mn, kbs = k_blocks;
+    if constexpr (TWO) {
+      per = q.tiles_m * q.tiles_n; kbs = (q.K + BK - 1) / BK;
+      if (sec) u -= mapC.units;
+    }
+    Place w;
+    w.sp = u / per;
+    const int t2 = u - w.sp * per;
+    w.m0 = (t2 % q.tiles_m) * BM; w.n0 = (t2 / q.tiles_m) * BN;
+    w.kb0 = (int)((long long)w.sp * kbs / q.splits);
+    w.kb1 = (int)((long long)(w.sp + 1) * kbs / q.splits);
+    return w;
+  };
 
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer ----------------
-      const uint32_t a_bytes = A_K ? p.a_rows * 128 : (BM / 64) * p.k_rows * 128;
-      const uint32_t b_bytes = B_K ? C::B_BYTES : (BN / 64) * p.k_rows * 128;
       int s = 0; uint32_t ph = 0;
-      for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-        const int sp = tile / tiles_mn, t2 = tile - sp * tiles_mn;
-        const int m0 = (t2 % p.tiles_m) * BM, n0 = (t2 / p.tiles_m) * BN;
-        const int kb0 = (int)((long long)sp * k_blocks / p.splits);
-        const int kb1 = (int)((long long)(sp + 1) * k_blocks / p.splits);
+      for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
+        const bool sec = second(u), ak = a_kmajor(sec);
+        const Place w = locate(u, sec);
+        uint32_t stage_bytes = C::STAGE_BYTES;
+        if constexpr (FIT)
+          stage_bytes = (ak ? params(sec)->a_rows * 128 : (BM / 64) * params(sec)->k_rows * 128) +
+                        (B_K ? C::B_BYTES : (BN / 64) * params(sec)->k_rows * 128);
+        const CUtensorMap *mA = &mapA, *mB = &mapB;
+        if constexpr (TWO) if (sec) { mA = &mapC.a2; mB = &mapC.b2; }
         bool ok = true;
-        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+        for (int kb = w.kb0; kb < w.kb1 && ok; ++kb) {
           ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.flags);
           if (!ok) break;
           const uint32_t a_dst = smem_u32(smem + s * C::STAGE_BYTES);
           const uint32_t b_dst = a_dst + C::A_BYTES;
-          mbar_expect_tx(full_bar(s), a_bytes + b_bytes);
-          if (A_K) {
-            tma_load_2d(a_dst, &mapA, full_bar(s), kb * BK, m0);
+          mbar_expect_tx(full_bar(s), stage_bytes);
+          if (ak) {
+            tma_load_2d(a_dst, mA, full_bar(s), kb * BK, w.m0);
           } else {
 #pragma unroll
-            for (int i = 0; i < BM / 64; ++i)
-              tma_load_2d(a_dst + i * 8192, &mapA, full_bar(s), m0 + 64 * i, kb * BK);
+            for (int j = 0; j < BM / 64; ++j)
+              tma_load_2d(a_dst + j * 8192, mA, full_bar(s), w.m0 + 64 * j, kb * BK);
           }
           if (B_K) {
-            tma_load_2d(b_dst, &mapB, full_bar(s), kb * BK, n0);
+            tma_load_2d(b_dst, mB, full_bar(s), kb * BK, w.n0);
           } else {
 #pragma unroll
-            for (int i = 0; i < BN / 64; ++i)
-              tma_load_2d(b_dst + i * 8192, &mapB, full_bar(s), n0 + 64 * i, kb * BK);
+            for (int j = 0; j < BN / 64; ++j)
+              tma_load_2d(b_dst + j * 8192, mB, full_bar(s), w.n0 + 64 * j, kb * BK);
           }
           if (++s == C::STAGES) { s = 0; ph ^= 1u; }
         }
@@ -113,34 +141,39 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     if (lane == 0) {
       // ---------------- MMA issuer ----------------
       // instruction descriptor: D fp32, A/B bf16, majors, N >> 3, M >> 4
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_K ? 0u : 1u) << 15) |
-                             ((B_K ? 0u : 1u) << 16) | ((uint32_t)(BN >> 3) << 17) |
-                             ((uint32_t)(BM >> 4) << 24);
+      const uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((B_K ? 0u : 1u) << 16) | ((uint32_t)(BN >> 3) << 17) |
+                              ((uint32_t)(BM >> 4) << 24);
       int s = 0; uint32_t ph = 0;
       int acc = 0; uint32_t acc_ph = 0;
-      for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-        const int sp = tile / tiles_mn;
-        const int kb0 = (int)((long long)sp * k_blocks / p.splits);
-        const int kb1 = (int)((long long)(sp + 1) * k_blocks / p.splits);
+      for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
+        const bool sec = second(u), ak = a_kmajor(sec);
+        const int k_rows = FIT ? params(sec)->k_rows : BK;
+        const Place w = locate(u, sec);
+        const uint32_t idesc = idesc0 | ((ak ? 0u : 1u) << 15);
         if (!mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.flags)) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
         bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
           ok = mbar_wait(full_bar(s), ph, abort_flag, p.flags);
           if (!ok) break;
           tc_fence_after();
           // (rows of A past a smaller box are what was there before: rows of the accumulator that are not stored)
           const uint32_t a_addr = smem_u32(smem + s * C::STAGE_BYTES);
           const uint32_t b_addr = a_addr + C::A_BYTES;
-#pragma unroll
-          for (int k = 0; k < BK / UMMA_K; ++k) {
-            if (k * UMMA_K >= p.k_rows) break;
-            const uint64_t adesc = A_K ? make_desc(a_addr + k * 32, 16, 1024)
-                                       : make_desc(a_addr + k * 2048, 8192, 1024);
+          auto product = [&](int k) {
+            const uint64_t adesc = ak ? make_desc(a_addr + k * 32, 16, 1024)
+                                      : make_desc(a_addr + k * 2048, 8192, 1024);
             const uint64_t bdesc = B_K ? make_desc(b_addr + k * 32, 16, 1024)
                                        : make_desc(b_addr + k * 2048, 8192, 1024);
-            umma_bf16(d_tmem, adesc, bdesc, idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+            umma_bf16(d_tmem, adesc, bdesc, idesc, (kb > w.kb0 || k > 0) ? 1u : 0u);
+          };
+          if (k_rows == BK) {
+#pragma unroll
+            for (int k = 0; k < BK / UMMA_K; ++k) product(k);
+          } else {
+#pragma unroll 1
+            for (int k = 0; k * UMMA_K < k_rows; ++k) product(k);
           }
           umma_commit(empty_bar(s));           // slot is free once these MMAs have read it
           if (++s == C::STAGES) { s = 0; ph ^= 1u; }
@@ -156,13 +189,16 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     const int half = (warp - 2) >> 2;          // which half of the tile's columns
     const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
-    for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x) {
-      const int sp = tile / tiles_mn, t2 = tile - sp * tiles_mn;
-      const int m0 = (t2 % p.tiles_m) * BM, n0 = (t2 / p.tiles_m) * BN;
+    for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
+      const bool sec = second(u);
+      const Place w = locate(u, sec);
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_mode<MODE>(p, mapC, store_buf, m0, n0, sp, tmem_base + (uint32_t)(acc * BN), quarter, half * (BN / 2),
-                       (half + 1) * (BN / 2), lane);
+      const uint32_t t_acc = tmem_base + (uint32_t)(acc * BN);
+      if constexpr (TWO)
+        drain_two(*params(sec), sec ? &mapC.c2 : &mapC.c, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+      else
+        drain_mode<MODE>(p, mapC, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
@@ -282,7 +318,8 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB;
   TcParams p = make_params(g);
-  if (A_K && g.M < BM) p.a_rows = (g.M + 7) / 8 * 8;
+  if (MODE == DRAIN_COLS) p.k_rows = BK;
+  else if (A_K && g.M < BM) p.a_rows = (g.M + 7) / 8 * 8;
   if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, p.a_rows, g.transient, p.k_rows)) return -2;
   if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, BN, g.transient, p.k_rows)) return -2;
   p.tiles_m = (g.M + BM - 1) / BM;
@@ -391,12 +428,60 @@ int launch_gemm_tc_pieces(const GemmArgs& g, cudaStream_t st) {
   return launch_t<128, true, true, DRAIN_PIECES>(g, st);
 }
 
-int launch_gemm_tc_out_bf16(const GemmArgs& g, cudaStream_t st) {
-  if (g.M <= 0 || g.N <= 0 || g.K <= 0) return 0;
+bool gemm_tc_pairs_two(const GemmArgs& g, const GemmArgs* g2) {
+  // SM pairs where neither product is narrower than a tile half and there are 16 units or more between them
+  const GemmArgs& h = g2 ? *g2 : g;
+  const long long tiles = (long long)((g.M + 255) / 256) * ((g.N + 255) / 256) + (g2 ? (long long)((h.M + 255) / 256) * ((h.N + 255) / 256) : 0);
+  return g.M > 128 && g.N > 128 && h.M > 128 && h.N > 128 && tiles >= 16;
+}
+
+namespace {
+int one_units(const GemmArgs& g, TcParams& p) {
+  p = make_params(g);
+  if (g.a_kmajor && g.M < BM) p.a_rows = (g.M + 7) / 8 * 8;
+  p.tiles_m = (g.M + BM - 1) / BM;
+  p.tiles_n = (g.N + 127) / 128;
+  const int k_blocks = (g.K + BK - 1) / BK;
+  p.splits = g.splits < 1 ? 1 : (g.splits > k_blocks ? k_blocks : g.splits);
+  p.split_stride = g.split_stride;
+  return p.tiles_m * p.tiles_n * p.splits;
+}
+bool two_ok(const GemmArgs& g) {
+  const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
+  return operands_ok(g) && g.transient && !g.b_kmajor && (f32 || g.epilogue == EPI_OUT_BF16) && (g.splits <= 1 || g.epilogue == EPI_STORE_F32) &&
+         !(g.N % 8) && !(g.ldc % 8) && !(g.aux && (g.ldaux % 8)) && !(reinterpret_cast<uintptr_t>(g.C) & 15) &&
+         !(reinterpret_cast<uintptr_t>(g.aux) & 31) && g.M > 0 && g.N > 0 && g.K > 0;
+}
+}  // namespace
+
+int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   if (gemm_tc_init() != 0) return -1;
-  if (!operands_ok(g) || g.b_kmajor || g.splits > 1 || (g.N % 8) || (g.ldc % 8) || (g.aux && (g.ldaux % 8)) ||
-      (reinterpret_cast<uintptr_t>(g.C) & 15) || (reinterpret_cast<uintptr_t>(g.aux) & 31))
-    return -4;
-  if (picks_pair256(g)) return launch_gemm_tc_pair_out_bf16(g, make_params(g), st);
-  return g.a_kmajor ? launch_t<128, true, false, DRAIN_OUT_BF16>(g, st) : launch_t<128, false, false, DRAIN_OUT_BF16>(g, st);
+  if (!two_ok(g) || (g2 && !two_ok(*g2))) return -4;
+  // the product with the longer units first
+  const int k1 = g.K / (g.splits > 1 ? g.splits : 1), k2 = g2 ? g2->K / (g2->splits > 1 ? g2->splits : 1) : 0;
+  if (k2 > k1) return launch_gemm_tc_two(*g2, &g, st);
+  if (gemm_tc_pairs_two(g, g2)) return launch_gemm_tc_pair_two(g, g2, st);
+  using C = Cfg<128>;
+  static PerDeviceFlag attr;
+  constexpr int smem = C::SMEM + store_smem<DRAIN_TWO>();
+  auto kernel = gemm_tc_kernel<128, true, false, DRAIN_TWO>;
+  if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
+  CUtensorMap mapA, mapB;
+  OutMap<DRAIN_TWO> m = {};
+  TcParams p;
+  m.units = one_units(g, p);
+  m.a_k = g.a_kmajor;
+  if (!encode_map(&mapA, g.A, g.lda, g.a_kmajor, g.M, g.K, p.a_rows, true, p.k_rows)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, false, g.N, g.K, 128, true, p.k_rows)) return -2;
+  if (g.epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c, g.C, g.ldc, g.M, g.N)) return -2;
+  if (g2) {
+    m.units2 = one_units(*g2, m.p2);
+    m.a_k2 = g2->a_kmajor;
+    if (!encode_map(&m.a2, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, m.p2.a_rows, true, m.p2.k_rows)) return -2;
+    if (!encode_map(&m.b2, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p2.k_rows)) return -2;
+    if (g2->epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c2, g2->C, g2->ldc, g2->M, g2->N)) return -2;
+  }
+  m.fill = g2 ? two_fill(g, *g2, 190) : 0;
+  const int units = m.units + m.units2, n_sm = ppu_sm_count();
+  return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, GEMM_THREADS, smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
 }

@@ -117,7 +117,7 @@ template <int PAIR_BN, bool A_K, bool B_K, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                     const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ OutMap<MODE> mapC,
-                    const TcParams p) {
+                    const __grid_constant__ TcParams p) {
   using PC = PairCfg<PAIR_BN>;
   constexpr int ST = PC::STAGES, PAIR_STAGE_BYTES = PC::STAGE_BYTES, HALF_BYTES = PC::A_HALF, B_SLAB = PC::B_SLAB;
   extern __shared__ uint8_t smem_raw[];
@@ -160,21 +160,42 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   const int num_tiles = p.tiles_m * p.tiles_n;
   const int k_blocks = (p.K + PAIR_KH * BK - 1) / (PAIR_KH * BK);
-  const int num_units = p.splits > 1 ? num_tiles * p.splits
-                                     : num_tiles + (PAIR_BN == 256 && num_tiles > p.tail_from ? num_tiles - p.tail_from : 0);
+  int num_units = p.splits > 1 ? num_tiles * p.splits
+                               : num_tiles + (PAIR_BN == 256 && num_tiles > p.tail_from ? num_tiles - p.tail_from : 0);
+  // units of a DRAIN_TWO launch: those of p, then those of mapC.p2
+  constexpr bool TWO = MODE == DRAIN_TWO, FIT = MODE != DRAIN_COLS;   // FIT: boxes may be smaller than a stage
+  if constexpr (TWO) num_units = mapC.units + mapC.units2;
+  auto unit_of = [&](int i) {
+    if constexpr (TWO) return two_unit(i, pair, n_pairs, mapC.units, mapC.units2, mapC.fill);
+    else return pair + i * n_pairs;
+  };
+  auto second = [&](int u) { if constexpr (TWO) return u >= mapC.units; else return false; };
+  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &mapC.p2 : &p; else return &p; };
+  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? mapC.a_k2 : mapC.a_k) != 0; else return A_K; };
+  auto locate = [&](int u, bool sec) {
+    if constexpr (TWO) {
+      const TcParams& q = *params(sec);
+      return pair_unit<PAIR_BN>(q, sec ? u - mapC.units : u, q.tiles_m * q.tiles_n, (q.K + PAIR_KH * BK - 1) / (PAIR_KH * BK));
+    } else {
+      return pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
+    }
+  };
 
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer (both CTAs) ----------------
       int s = 0; uint32_t ph = 0;
       bool ok = true;
-      for (int u = pair; u < num_units && ok; u += n_pairs) {
-        const PairUnit w = pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
+      for (int i = 0, u = unit_of(0); u < num_units && ok; u = unit_of(++i)) {
+        const bool sec = second(u), ak = a_kmajor(sec);
+        const int K = params(sec)->K, k_rows = FIT ? params(sec)->k_rows : BK;
+        const PairUnit w = locate(u, sec);
         const int m0 = w.m0 + (int)rank * 128;
         const int n0 = w.n0 + (int)rank * (w.bn / 2);
         const bool narrow = w.bn != PAIR_BN;
         const int b_slab = narrow ? B_SLAB / 2 : B_SLAB;          // this CTA's bn/2 rows of B, 64 k
-        const CUtensorMap* mB = narrow ? &mapB2 : &mapB;
+        const CUtensorMap *mA = &mapA, *mB = narrow ? &mapB2 : &mapB;
+        if constexpr (TWO) if (sec) { mA = &mapC.a2; mB = &mapC.b2; }
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.flags);
           if (!ok) break;
@@ -182,26 +203,26 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
           const uint32_t b_dst = a_dst + HALF_BYTES;
           const uint32_t fb = map_to_rank(full_bar(s), 0);
           // the second slab of the last block may lie past the end of the reduction altogether
-          const int slabs = (kb * PAIR_KH + 1) * BK < p.K ? PAIR_KH : 1;
-          const uint32_t slab_bytes = (A_K ? SLAB_BYTES : 2 * p.k_rows * 128) + (B_K ? b_slab : (w.bn / 128) * p.k_rows * 128);
+          const int slabs = !FIT || (kb * PAIR_KH + 1) * BK < K ? PAIR_KH : 1;
+          const uint32_t slab_bytes = (ak ? SLAB_BYTES : 2 * k_rows * 128) + (B_K ? b_slab : (w.bn / 128) * k_rows * 128);
           if (leader) mbar_expect_tx(full_bar(s), 2 * slabs * slab_bytes);
           // (k past the end of the reduction reads zeros)
 #pragma unroll
           for (int kh = 0; kh < PAIR_KH; ++kh) {
             if (kh >= slabs) break;
             const int k0 = (kb * PAIR_KH + kh) * BK;
-            if (A_K) {
-              tma_load_2d_pair(a_dst + kh * SLAB_BYTES, &mapA, fb, k0, m0);
+            if (ak) {
+              tma_load_2d_pair(a_dst + kh * SLAB_BYTES, mA, fb, k0, m0);
             } else {
-              tma_load_2d_pair(a_dst + kh * SLAB_BYTES, &mapA, fb, m0, k0);
-              tma_load_2d_pair(a_dst + kh * SLAB_BYTES + 8192, &mapA, fb, m0 + 64, k0);
+              tma_load_2d_pair(a_dst + kh * SLAB_BYTES, mA, fb, m0, k0);
+              tma_load_2d_pair(a_dst + kh * SLAB_BYTES + 8192, mA, fb, m0 + 64, k0);
             }
             if (B_K) {
               tma_load_2d_pair(b_dst + kh * b_slab, mB, fb, k0, n0);
             } else {
 #pragma unroll
-              for (int i = 0; i < PAIR_BN / 128; ++i)
-                if (i < w.bn / 128) tma_load_2d_pair(b_dst + kh * b_slab + i * 8192, &mapB, fb, n0 + 64 * i, k0);
+              for (int j = 0; j < PAIR_BN / 128; ++j)
+                if (j < w.bn / 128) tma_load_2d_pair(b_dst + kh * b_slab + j * 8192, mB, fb, n0 + 64 * j, k0);
             }
           }
           if (++s == ST) { s = 0; ph ^= 1u; }
@@ -211,13 +232,14 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   } else if (warp == 1) {
     if (lane == 0 && leader) {
       // ---------------- MMA issuer (leader CTA only) ----------------
-      const uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((A_K ? 0u : 1u) << 15) |
-                              ((B_K ? 0u : 1u) << 16) | ((uint32_t)(256 >> 4) << 24);
+      const uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((B_K ? 0u : 1u) << 16) | ((uint32_t)(256 >> 4) << 24);
       int s = 0; uint32_t ph = 0;
       int acc = 0; uint32_t acc_ph = 0;
-      for (int u = pair; u < num_units; u += n_pairs) {
-        const PairUnit w = pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
-        const uint32_t idesc = idesc0 | ((uint32_t)(w.bn >> 3) << 17);
+      for (int i = 0, u = unit_of(0); u < num_units; u = unit_of(++i)) {
+        const bool sec = second(u), ak = a_kmajor(sec);
+        const int K = params(sec)->K, k_rows = FIT ? params(sec)->k_rows : BK;
+        const PairUnit w = locate(u, sec);
+        const uint32_t idesc = idesc0 | ((ak ? 0u : 1u) << 15) | ((uint32_t)(w.bn >> 3) << 17);
         const uint32_t b_slab = w.bn != PAIR_BN ? B_SLAB / 2 : B_SLAB;
         if (!mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.flags)) break;
         tc_fence_after();
@@ -229,15 +251,21 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
           tc_fence_after();
           const uint32_t a_addr = smem_u32(smem + s * PAIR_STAGE_BYTES);
           const uint32_t b_addr = a_addr + HALF_BYTES;
-          const int slabs = (kb * PAIR_KH + 1) * BK < p.K ? PAIR_KH : 1;
-#pragma unroll
-          for (int k = 0; k < PAIR_KH * (BK / UMMA_K); ++k) {
+          const int slabs = !FIT || (kb * PAIR_KH + 1) * BK < K ? PAIR_KH : 1;
+          auto product = [&](int k) {
             const uint32_t kh = (uint32_t)(k / (BK / UMMA_K)), kk = (uint32_t)(k % (BK / UMMA_K));
-            if ((int)kh >= slabs || (int)kk * UMMA_K >= p.k_rows) continue;
             const uint32_t slab = kh * SLAB_BYTES, slab_b = kh * b_slab;
-            const uint64_t adesc = A_K ? make_desc(a_addr + slab + kk * 32, 16, 1024) : make_desc(a_addr + slab + kk * 2048, 8192, 1024);
+            const uint64_t adesc = ak ? make_desc(a_addr + slab + kk * 32, 16, 1024) : make_desc(a_addr + slab + kk * 2048, 8192, 1024);
             const uint64_t bdesc = B_K ? make_desc(b_addr + slab_b + kk * 32, 16, 1024) : make_desc(b_addr + slab_b + kk * 2048, 8192, 1024);
             umma_bf16_pair(d_tmem, adesc, bdesc, idesc, (kb > w.kb0 || k > 0) ? 1u : 0u);
+          };
+          if (slabs == PAIR_KH && k_rows == BK) {
+#pragma unroll
+            for (int k = 0; k < PAIR_KH * (BK / UMMA_K); ++k) product(k);
+          } else {                               // the end of the reduction
+#pragma unroll 1
+            for (int k = 0; k < slabs * (BK / UMMA_K); ++k)
+              if ((k % (BK / UMMA_K)) * UMMA_K < k_rows) product(k);
           }
           umma_commit_pair(empty_bar(s));        // both CTAs' slots are free once these MMAs have read them
           if (++s == ST) { s = 0; ph ^= 1u; }
@@ -253,13 +281,17 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     const int half = (warp - 2) >> 2;
     const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
-    for (int u = pair; u < num_units; u += n_pairs) {
-      const PairUnit w = pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
+    for (int i = 0, u = unit_of(0); u < num_units; u = unit_of(++i)) {
+      const bool sec = second(u);
+      const PairUnit w = locate(u, sec);
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
-      drain_mode<MODE>(p, mapC, store_buf, m0, w.n0, w.sp, tmem_base + (uint32_t)(acc * PAIR_BN), quarter,
-                       half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+      const uint32_t t_acc = tmem_base + (uint32_t)(acc * PAIR_BN);
+      if constexpr (TWO)
+        drain_two(*params(sec), sec ? &mapC.c2 : &mapC.c, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+      else
+        drain_mode<MODE>(p, mapC, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
@@ -286,9 +318,10 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   static PerDeviceFlag attr;
   if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>())) return -1;
   CUtensorMap mapA, mapB, mapB2;
-  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient, p0.k_rows)) return -2;
-  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient, p0.k_rows)) return -2;
   TcParams p = p0;
+  if (MODE == DRAIN_COLS) p.k_rows = BK;
+  if (!encode_map(&mapA, g.A, g.lda, A_K, g.M, g.K, 128, g.transient, p.k_rows)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, B_K, g.N, g.K, PAIR_BN / 2, g.transient, p.k_rows)) return -2;
   p.tiles_m = (g.M + 255) / 256;
   p.tiles_n = (g.N + PAIR_BN - 1) / PAIR_BN;
   // split-K (fp32 partial outputs sp * split_stride apart, summed by the consumer): each unit of
@@ -352,8 +385,41 @@ int launch_gemm_tc_pair(const GemmArgs& g, const TcParams& p, int bn, cudaStream
 int launch_gemm_tc_pair_pieces(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
   return launch_pair_t<256, true, true, DRAIN_PIECES>(g, p, st);
 }
-int launch_gemm_tc_pair_out_bf16(const GemmArgs& g, const TcParams& p, cudaStream_t st) {
-  return g.a_kmajor ? launch_pair_t<256, true, false, DRAIN_OUT_BF16>(g, p, st)
-                    : launch_pair_t<256, false, false, DRAIN_OUT_BF16>(g, p, st);
+// tiles, split-K and unit counts of one of two products
+static int two_units(const GemmArgs& g, TcParams& p) {
+  p = make_params(g);
+  p.tiles_m = (g.M + 255) / 256;
+  p.tiles_n = (g.N + 255) / 256;
+  const int k_blocks = (g.K + PAIR_KH * BK - 1) / (PAIR_KH * BK);
+  p.splits = g.splits < 1 ? 1 : (g.splits > k_blocks ? k_blocks : g.splits);
+  p.split_stride = g.split_stride;
+  p.n_fastest = g.M > g.N ? 1 : 0;
+  return p.tiles_m * p.tiles_n * p.splits;
+}
+int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
+  static PerDeviceFlag attr;
+  constexpr int smem = PairCfg<256>::SMEM + store_smem<DRAIN_TWO>();
+  auto kernel = gemm_tc_pair_kernel<256, true, false, DRAIN_TWO>;
+  if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
+  CUtensorMap mapA, mapB;
+  OutMap<DRAIN_TWO> m = {};
+  TcParams p;
+  m.units = two_units(g, p);
+  m.a_k = g.a_kmajor;
+  if (!encode_map(&mapA, g.A, g.lda, g.a_kmajor, g.M, g.K, 128, true, p.k_rows)) return -2;
+  if (!encode_map(&mapB, g.B, g.ldb, false, g.N, g.K, 128, true, p.k_rows)) return -2;
+  if (g.epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c, g.C, g.ldc, g.M, g.N)) return -2;
+  if (g2) {
+    m.units2 = two_units(*g2, m.p2);
+    m.a_k2 = g2->a_kmajor;
+    if (!encode_map(&m.a2, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, 128, true, m.p2.k_rows)) return -2;
+    if (!encode_map(&m.b2, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p2.k_rows)) return -2;
+    if (g2->epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c2, g2->C, g2->ldc, g2->M, g2->N)) return -2;
+  }
+  const int units = m.units + m.units2, max_pairs = ppu_sm_count() / 2, waves = (units + max_pairs - 1) / max_pairs;
+  m.fill = g2 ? two_fill(g, *g2, 330) : 0;
+  // (one product alone: as many pairs as give each the same number of tiles)
+  const int pairs = g2 ? (units < max_pairs ? units : max_pairs) : (units + waves - 1) / waves;
+  return ppu_launch_dependent(kernel, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
 }
 }  // namespace gemm_tc_detail

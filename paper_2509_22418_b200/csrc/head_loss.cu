@@ -434,28 +434,37 @@ constexpr int SMS = 148;                      // work is split for a B200 (also 
 
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// Slices of the reduction for a [M, N] product over K, from a model of its time: waves of units over the
-// machine (an SM pair's 256 x 256 tile takes 6 ns for each k, one SM's 128 x 128 tile 4), then the partial
-// products read at 3.3 TB/s by a launch of its own (3 us).  Slices are at least 1024 long.
-int splits_for(int64_t M, int64_t N, int64_t K) {
-  const int64_t pair = ((M + 255) / 256) * ((N + 255) / 256);
-  const bool one = M <= 128 || N <= 128 || pair < 16;
-  const int64_t tiles = one ? ((M + 127) / 128) * ((N + 127) / 128) : pair, units = one ? SMS : SMS / 2;
-  double best = 0.;
-  int at = 1;
-  for (int64_t s = 1; s <= 32 && s <= std::max<int64_t>(1, K / 1024); ++s) {
-    const double waves = (double)((tiles * s + units - 1) / units);
-    const double ns = waves * ((K + s - 1) / s) * (one ? 4. : 6.) + (s > 1 ? 3000. + s * 4. * M * N / 3300. : 0.);
-    if (s == 1 || ns < 0.95 * best) { best = ns; at = (int)s; }
-  }
-  return at;
+// Slices of the reductions of dX [rows, d] over V and dE [V, d] over the rows, which one launch works, from a
+// model of its time: units of (k + overhead), 6 ns for each k (an SM pair's 256 x 256 tile; one SM's 128 x 128
+// tile takes the same), shared out evenly or as long as the longest unit; then for a split product its
+// partial sums, read at 3.3 TB/s by a launch of its own (3 us).  Slices are at least 1024 long.
+void choose_splits(int64_t rows, int64_t d, int64_t V, int want, bool split_e, int* sx, int* se) {
+  GemmArgs gx, ge;
+  gx.M = (int)rows; gx.N = (int)d; ge.M = (int)V; ge.N = (int)d;
+  const bool pairs = want == 3 ? gemm_tc_pairs_two(gx, &ge) : gemm_tc_pairs_two(want & 1 ? gx : ge, nullptr);
+  const int64_t tile = pairs ? 256 : 128, units = pairs ? SMS / 2 : SMS;
+  const double overhead = pairs ? 330. : 190.;
+  const int64_t tx = (want & 1) ? ((rows + tile - 1) / tile) * ((d + tile - 1) / tile) : 0;
+  const int64_t te = (want & 2) ? ((V + tile - 1) / tile) * ((d + tile - 1) / tile) : 0;
+  auto ns = [&](int a, int b) {
+    const double ux = (double)V / a + overhead, ue = (double)rows / b + overhead;
+    const double work = (tx * a * ux + te * b * ue) / units;
+    const double longest = std::max(tx ? ux : 0., te ? ue : 0.);
+    return 6. * std::max(work, longest) + (a > 1 ? 3000. + a * 4. * rows * d / 3300. : 0.) + (b > 1 ? 3000. + b * 4. * V * d / 3300. : 0.);
+  };
+  *sx = *se = 1;
+  double best = ns(1, 1);
+  for (int s = 2; tx && s <= 32 && s <= V / 1024; ++s)
+    if (const double t = ns(s, 1); t < 0.95 * best) { best = t; *sx = s; }
+  for (int s = 2; te && split_e && s <= 32 && s <= rows / 1024; ++s)
+    if (const double t = ns(*sx, s); t < 0.95 * best) { best = t; *se = s; }
 }
 
 struct Plan {
   int64_t ldu, n_pieces, chunk, usual;         // usual: rows of a chunk by default (decides orders of sums: results do not depend on chunk_rows)
   int chunks, sx, se;                          // split-K factors of dX and dE
   int64_t ld_off;
-  size_t off_weighted, off_factor, off_stats, off_x, off_ids, off_z, off_before, off_u, off_fx, off_acc, off_part, bytes;
+  size_t off_weighted, off_factor, off_stats, off_x, off_ids, off_z, off_before, off_u, off_fx, off_acc, off_part_x, off_part_e, bytes;
 };
 Plan make_plan(int T, int d, int V, int want, int chunk_rows, int k) {
   Plan p;
@@ -468,8 +477,7 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows, int k) {
   p.usual = std::min<int64_t>(p.usual, T);
   p.chunks = (int)std::max<int64_t>(1, (T + c - 1) / c);
   p.chunk = p.chunks == 1 ? T : round_up((T + p.chunks - 1) / p.chunks, 256);
-  p.sx = (want & 1) ? splits_for(p.chunk, d, V) : 1;
-  p.se = (want & 2) && p.chunks == 1 ? splits_for(V, d, p.chunk) : 1;
+  choose_splits(p.chunk, d, V, want, p.chunks == 1, &p.sx, &p.se);
   size_t off = 256;                            // the row count, the rows finished
   auto take = [&off](int64_t bytes) { const size_t at = off; off += (size_t)round_up(bytes, 256); return at; };
   p.off_weighted = take(4ll * T);
@@ -483,10 +491,8 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows, int k) {
   p.off_u = take(want ? p.chunk * row_bytes : 0);
   p.off_fx = take((want & 2) ? 2ll * p.chunk * d : 0);
   p.off_acc = take((want & 2) && p.chunks > 1 ? 4ll * V * d : 0);
-  int64_t part = 0;
-  if (p.sx > 1) part = 4ll * p.sx * p.chunk * d;
-  if (p.se > 1) part = std::max<int64_t>(part, 4ll * p.se * V * d);
-  p.off_part = take(part);
+  p.off_part_x = take(p.sx > 1 ? 4ll * p.sx * p.chunk * d : 0);
+  p.off_part_e = take(p.se > 1 ? 4ll * p.se * V * d : 0);
   p.bytes = off;
   return p;
 }
@@ -539,20 +545,14 @@ cudaError_t launch_rows(const RowArgs& r, int64_t rows, int warps, cudaStream_t 
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// bf16 C = A . B^T (times row_scale), split over K into fp32 partials where that fills the machine
-int product_bf16(GemmArgs g, int splits, float* part, cudaStream_t st) {
-  if (splits <= 1) {
-    g.epilogue = EPI_OUT_BF16;
-    GEMM_OK(launch_gemm_tc_out_bf16(g, st));
-    return PPU_OK;
-  }
-  bf16* out = (bf16*)g.C; const int64_t ldo = g.ldc;
+// a split product's epilogue: fp32 partial sums, which join() adds up after the launch
+void split_product(GemmArgs& g, int splits, float* part) {
   g.epilogue = EPI_STORE_F32; g.C = part; g.ldc = g.N; g.splits = splits; g.split_stride = (int64_t)g.M * g.N;
-  GEMM_OK(launch_gemm_tc(g, st));
+}
+cudaError_t join(const GemmArgs& g, void* out, int64_t ldo, cudaStream_t st) {
   const int64_t n = (int64_t)g.M * (g.N / 4);
-  CUDA_OK(ppu_launch_dependent(join_partials_kernel, (unsigned)((n + 255) / 256), 256, 0, st, part, splits, g.split_stride, g.row_scale, out, ldo,
-                               g.M, g.N / 4));
-  return PPU_OK;
+  return ppu_launch_dependent(join_partials_kernel, (unsigned)((n + 255) / 256), 256, 0, st, (const float*)g.C, g.splits, g.split_stride, g.row_scale,
+                              (bf16*)out, ldo, g.M, g.N / 4);
 }
 
 int run_head(const HeadCall& c) {
@@ -578,7 +578,7 @@ int run_head(const HeadCall& c) {
   bf16* u = want ? (bf16*)(ws + p.off_u) : nullptr;
   bf16* fx = c.dE ? (bf16*)(ws + p.off_fx) : nullptr;
   float* acc = (float*)(ws + p.off_acc);
-  float* part = (float*)(ws + p.off_part);
+  float *part_x = (float*)(ws + p.off_part_x), *part_e = (float*)(ws + p.off_part_e);
 
   if (c.T == 0) {                              // a mean over nothing: no loss, no gradient
     CUDA_OK(cudaMemsetAsync(c.loss, 0, 4, c.st));
@@ -631,30 +631,25 @@ int run_head(const HeadCall& c) {
     }
     r.row0 = c0;
     CUDA_OK(want ? launch_rows<true>(r, rows, warps, c.st) : launch_rows<false>(r, rows, warps, c.st));
+    // both gradient products in one launch
+    GemmArgs gx = g0, ge = g0;
+    bf16* dX = c.dX ? (bf16*)c.dX + c0 * c.lddx : nullptr;
     if (c.dX) {
-      GemmArgs g = g0;
-      g.A = u; g.lda = p.ldu; g.a_kmajor = 1; g.B = E; g.ldb = c.lde; g.b_kmajor = 0; g.row_scale = factor;
-      g.M = (int)rows; g.N = c.d; g.K = c.V; g.C = (bf16*)c.dX + c0 * c.lddx; g.ldc = c.lddx;
-      rc = product_bf16(g, p.sx, part, c.st);
-      if (rc) return rc;
+      gx.A = u; gx.lda = p.ldu; gx.a_kmajor = 1; gx.B = E; gx.ldb = c.lde; gx.b_kmajor = 0; gx.row_scale = factor;
+      gx.M = (int)rows; gx.N = c.d; gx.K = c.V; gx.epilogue = EPI_OUT_BF16; gx.C = dX; gx.ldc = c.lddx;
+      if (p.sx > 1) split_product(gx, p.sx, part_x);
     }
     if (c.dE) {
-      GemmArgs g = g0;
-      g.A = u; g.lda = p.ldu; g.a_kmajor = 0; g.B = fx; g.ldb = c.d; g.b_kmajor = 0;
-      g.M = c.V; g.N = c.d; g.K = (int)rows; g.C = c.dE; g.ldc = c.ldde;
-      const bool last = c0 + p.chunk >= c.T;
-      if (c0 == 0 && last) {
-        rc = product_bf16(g, p.se, part, c.st);
-        if (rc) return rc;
-      } else if (last) {
-        g.epilogue = EPI_OUT_BF16; g.aux = acc; g.ldaux = c.d;
-        GEMM_OK(launch_gemm_tc_out_bf16(g, c.st));
-      } else {
-        g.epilogue = c0 == 0 ? EPI_STORE_F32 : EPI_RESID_F32;
-        g.C = acc; g.ldc = c.d; g.aux = acc; g.ldaux = c.d;
-        GEMM_OK(launch_gemm_tc(g, c.st));
-      }
+      const bool first = c0 == 0, last = c0 + p.chunk >= c.T;
+      ge.A = u; ge.lda = p.ldu; ge.a_kmajor = 0; ge.B = fx; ge.ldb = c.d; ge.b_kmajor = 0;
+      ge.M = c.V; ge.N = c.d; ge.K = (int)rows; ge.epilogue = EPI_OUT_BF16; ge.C = c.dE; ge.ldc = c.ldde;
+      if (p.se > 1) split_product(ge, p.se, part_e);
+      if (!first) { ge.aux = acc; ge.ldaux = c.d; }
+      if (!last) { ge.epilogue = first ? EPI_STORE_F32 : EPI_RESID_F32; ge.C = acc; ge.ldc = c.d; }
     }
+    if (want) GEMM_OK(launch_gemm_tc_two(c.dX ? gx : ge, want == 3 ? &ge : nullptr, c.st));
+    if (c.dX && p.sx > 1) CUDA_OK(join(gx, dX, c.lddx, c.st));
+    if (c.dE && p.se > 1) CUDA_OK(join(ge, c.dE, c.ldde, c.st));
   }
   CUDA_OK(cudaGetLastError());
   return PPU_OK;
