@@ -93,14 +93,13 @@ struct TcParams {
 
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of
 // those that have instantiations of their own: drain_cols keeps its registers, and these have 32 KB of
-// shared memory behind the operand stages, through which they store 64-column groups by TMA
+// shared memory behind the operand stages, through which they store 64-column groups
 enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_TWO = 2 };
 constexpr int STORE_BYTES = 32 * 128;                      // a warp's 32 rows x 64 bf16 columns
-template <int MODE> struct OutMap { CUtensorMap c; };
-template <> struct OutMap<DRAIN_COLS> {};
+template <int MODE> struct Second {};
 // DRAIN_TWO: a launch works the units of two products (launch_gemm_tc_two), the one with the longer units
 // first; A's order may differ between the two.  This holds the second product.
-template <> struct OutMap<DRAIN_TWO> { CUtensorMap c, a2, b2, c2; TcParams p2; int a_k, a_k2, units, units2, fill; };
+template <> struct Second<DRAIN_TWO> { CUtensorMap a, b; TcParams p; int a_k, a_k2, units, units2, fill; };
 // The i-th unit of block (pair) b of n: the first product's are dealt round; blocks that got one less then
 // have `fill` of the second's, as many as make up for it; the rest are dealt round again.
 __device__ __forceinline__ int two_unit(int i, int b, int n, int units, int units2, int fill) {
@@ -136,7 +135,6 @@ inline int two_fill(const GemmArgs& g, const GemmArgs& g2, int overhead) {
   const int k1 = g.K / (g.splits > 1 ? g.splits : 1), k2 = g2.K / (g2.splits > 1 ? g2.splits : 1);
   return (k1 + overhead) / (k2 + overhead);
 }
-bool encode_out_map(CUtensorMap* map, void* base, long long ld, int rows, int cols);   // for 32 x 64 boxes
 
 // Drains rows [m0 + 32 quarter, +32) x columns [n0 + half BN/2, + BN/2) of the accumulator at
 // TMEM column t_acc through registers into global memory, applying the epilogue p.epilogue.
@@ -342,20 +340,27 @@ __device__ __forceinline__ float ex2_fast(float x) {
 }
 
 // A warp's 32 rows x 64 columns, packed by its lanes (one row each, 32 words), to global memory through
-// its 4 KB of shared memory.  Stored from the registers instead, a lane's 32 bytes of its own row at a
-// time, a warp's store touches 32 lines: 2304 x 32000 x 768 took 95 us against 70 without the store
-// (65 us for the store alone, 2.3 TB/s); so TMA_STORE_US.
-__device__ __forceinline__ void store_group(const CUtensorMap* map, uint32_t buf, const uint32_t* o, int x, int y, int lane) {
-  if (lane == 0) tma_store_wait_read();
-  __syncwarp();
+// its 4 KB of shared memory, so that a store covers four rows' whole 128-byte lines.  (From the registers, a lane
+// 32 bytes of its own row at a time, a store touches 32 lines: 2304 x 32000 x 768 took 95 us against 70 without
+// the store.  By TMA from the same shared memory it took 90: the buffer is free again only when the copy has
+// read it.  This way STORE_US.)  Row r of the buffer has its 16-byte pieces in the places j ^ (r & 7): no bank conflicts
+// either way.  rows, cols: of the output, from here on.
+__device__ __forceinline__ void store_group(bf16* out, long long ld, uint32_t buf, const uint32_t* o, int rows, int cols, int lane) {
+  __syncwarp();                     // (the group before has been read)
 #pragma unroll
-  for (int j = 0; j < 8; ++j)       // the 16-byte pieces of a 128-byte row swap places as the swizzle has it
+  for (int j = 0; j < 8; ++j)
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(o[4 * j]),
                  "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
                  : "memory");
-  fence_async_smem();
   __syncwarp();
-  if (lane == 0) tma_store_2d(map, buf, x, y);
+  const int piece = lane & 7;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = 4 * i + (lane >> 3);
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(buf + r * 128 + ((piece ^ (r & 7)) << 4)) : "memory");
+    if (r < rows && 8 * piece < cols) *reinterpret_cast<uint4*>(out + r * ld + 8 * piece) = v;
+  }
 }
 
 // EPI_PIECES.  A lane holds 64 logits of its row at a time: x = acc * piece_scale (the scale holds
@@ -371,7 +376,7 @@ __device__ __forceinline__ void store_group(const CUtensorMap* map, uint32_t buf
 // The entries' own x are taken from tensor memory a column at a time: a warp's 32 rows have two in a
 // piece with 32 entries in 32768 columns.  (As dot products in the row kernel they were a gather of 4 KB of E
 // for each entry: 106 of 1200 us at 4096 x 2048 x 32768.)
-__device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0,
+__device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, int m0, int n0,
                                              uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
   const int mw = m0 + quarter * 32, m = mw + lane;
   const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
@@ -426,13 +431,14 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, const CUtensorMa
     }
     if (m < p.M)
       p.piece_stats[(long long)m * p.ld_pieces + nb / PIECE] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-    if (p.C) store_group(out, buf, o, nb, mw, lane);
+    // (columns up to the next multiple of 64 belong to the row too)
+    if (p.C) store_group((bf16*)p.C + (long long)mw * p.ldc + nb, p.ldc, buf, o, p.M - mw, PIECE, lane);
   }
 }
 
 // EPI_OUT_BF16: row_scale * (aux + acc), rounded once.  aux: fp32 partial sums, rows 32-byte aligned;
 // N is a multiple of 8.
-__device__ __forceinline__ void drain_out_bf16(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0,
+__device__ __forceinline__ void drain_out_bf16(const TcParams& p, uint32_t buf, int m0, int n0,
                                                uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
   const int mw = m0 + quarter * 32, m = mw + lane;
   const bool row_ok = m < p.M;
@@ -463,21 +469,52 @@ __device__ __forceinline__ void drain_out_bf16(const TcParams& p, const CUtensor
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[16 * h + j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
     }
-    store_group(out, buf, o, nb, mw, lane);
+    store_group((bf16*)p.C + (long long)mw * p.ldc + nb, p.ldc, buf, o, p.M - mw, p.N - nb, lane);
   }
 }
 
 template <int MODE>
-__device__ __forceinline__ void drain_mode(const TcParams& p, const OutMap<MODE>& out, uint32_t buf, int m0, int n0, int sp,
+__device__ __forceinline__ void drain_mode(const TcParams& p, uint32_t buf, int m0, int n0, int sp,
                                            uint32_t t_acc, int quarter, int c_begin, int c_end, int lane) {
-  if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, &out.c, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  if constexpr (MODE == DRAIN_PIECES) drain_pieces(p, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
   else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
-// DRAIN_TWO: bf16 results, or fp32 partial sums (of a split product; of several chunks)
-__device__ __forceinline__ void drain_two(const TcParams& p, const CUtensorMap* out, uint32_t buf, int m0, int n0, int sp, uint32_t t_acc,
-                                          int quarter, int c_begin, int c_end, int lane) {
-  if (p.epilogue == EPI_OUT_BF16) drain_out_bf16(p, out, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
-  else drain_cols(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
+// fp32 partial sums of a split product, or the running sum of several chunks (EPI_RESID_F32, aux may be C): N is
+// a multiple of 8, rows are 32-byte aligned
+__device__ __forceinline__ void drain_f32(const TcParams& p, int m0, int n0, int sp, uint32_t t_acc, int quarter, int c_begin, int c_end,
+                                          int lane) {
+  const int m = m0 + quarter * 32 + lane;
+  const bool row_ok = m < p.M;
+  const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
+  const bool add = p.epilogue == EPI_RESID_F32;
+#pragma unroll 1
+  for (int c0 = c_begin; c0 < c_end; c0 += 32) {
+    const int nb = n0 + c0;
+    if (nb >= p.N) break;                  // warp-uniform
+    uint32_t r[32], x[32];
+    tmem_ld32(t_row + c0, r);
+    float* dst = (float*)p.C + (long long)sp * p.split_stride + (long long)m * p.ldc + nb;
+    const float* src = (const float*)p.aux + (long long)m * p.ldaux + nb;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (add && row_ok && nb + 8 * j < p.N) ld_v8(x + 8 * j, src + 8 * j);
+    tmem_ld_wait();
+    if (!row_ok) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (nb + 8 * j >= p.N) break;
+      if (add) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) r[8 * j + q] = __float_as_uint(__uint_as_float(r[8 * j + q]) + __uint_as_float(x[8 * j + q]));
+      }
+      st_v8(dst + 8 * j, r + 8 * j);
+    }
+  }
+}
+__device__ __forceinline__ void drain_two(const TcParams& p, uint32_t buf, int m0, int n0, int sp, uint32_t t_acc, int quarter,
+                                          int c_begin, int c_end, int lane) {
+  if (p.epilogue == EPI_OUT_BF16) drain_out_bf16(p, buf, m0, n0, t_acc, quarter, c_begin, c_end, lane);
+  else drain_f32(p, m0, n0, sp, t_acc, quarter, c_begin, c_end, lane);
 }
 
 }  // namespace gemm_tc_detail

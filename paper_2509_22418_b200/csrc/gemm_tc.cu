@@ -34,7 +34,7 @@ template <int BN> struct Cfg {
 template <int BN, bool A_K, bool B_K, int MODE>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-               const __grid_constant__ OutMap<MODE> mapC, const __grid_constant__ TcParams p) {
+               const __grid_constant__ Second<MODE> two, const __grid_constant__ TcParams p) {
   using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -71,23 +71,23 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   const int tiles_mn = p.tiles_m * p.tiles_n;
   int num_tiles = tiles_mn * p.splits;
   const int k_blocks = (p.K + BK - 1) / BK;
-  // units of a DRAIN_TWO launch: those of p, then those of mapC.p2
+  // units of a DRAIN_TWO launch: those of p, then those of two.p
   constexpr bool TWO = MODE == DRAIN_TWO, FIT = MODE != DRAIN_COLS;   // FIT: boxes may be smaller than a stage
-  if constexpr (TWO) num_tiles = mapC.units + mapC.units2;
+  if constexpr (TWO) num_tiles = two.units + two.units2;
   auto unit_of = [&](int i) {
-    if constexpr (TWO) return two_unit(i, blockIdx.x, gridDim.x, mapC.units, mapC.units2, mapC.fill);
+    if constexpr (TWO) return two_unit(i, blockIdx.x, gridDim.x, two.units, two.units2, two.fill);
     else return (int)(blockIdx.x + i * gridDim.x);
   };
-  auto second = [&](int u) { if constexpr (TWO) return u >= mapC.units; else return false; };
-  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &mapC.p2 : &p; else return &p; };
-  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? mapC.a_k2 : mapC.a_k) != 0; else return A_K; };
+  auto second = [&](int u) { if constexpr (TWO) return u >= two.units; else return false; };
+  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &two.p : &p; else return &p; };
+  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? two.a_k2 : two.a_k) != 0; else return A_K; };
   struct Place { int sp, m0, n0, kb0, kb1; };
   auto locate = [&](int u, bool sec) {
     const TcParams& q = *params(sec);
     int per = tiles_mn, kbs = k_blocks;
     if constexpr (TWO) {
       per = q.tiles_m * q.tiles_n; kbs = (q.K + BK - 1) / BK;
-      if (sec) u -= mapC.units;
+      if (sec) u -= two.units;
     }
     Place w;
     w.sp = u / per;
@@ -110,7 +110,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
           stage_bytes = (ak ? params(sec)->a_rows * 128 : (BM / 64) * params(sec)->k_rows * 128) +
                         (B_K ? C::B_BYTES : (BN / 64) * params(sec)->k_rows * 128);
         const CUtensorMap *mA = &mapA, *mB = &mapB;
-        if constexpr (TWO) if (sec) { mA = &mapC.a2; mB = &mapC.b2; }
+        if constexpr (TWO) if (sec) { mA = &two.a; mB = &two.b; }
         bool ok = true;
         for (int kb = w.kb0; kb < w.kb1 && ok; ++kb) {
           ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.flags);
@@ -196,15 +196,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * BN);
       if constexpr (TWO)
-        drain_two(*params(sec), sec ? &mapC.c2 : &mapC.c, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+        drain_two(*params(sec), store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
       else
-        drain_mode<MODE>(p, mapC, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+        drain_mode<MODE>(p, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
-    if (MODE != DRAIN_COLS && lane == 0) tma_store_wait();
   }
 
   // ---------------- common exit ----------------
@@ -277,14 +276,6 @@ bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, i
   return true;
 }
 
-// output [rows, cols] bf16 with leading dimension ld, stored in boxes of 32 rows x 64 columns
-bool encode_out_map(CUtensorMap* map, void* base, long long ld, int rows, int cols) {
-  cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {64, 32}, estr[2] = {1, 1};
-  return tc::g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // launch parameters common to every tile shape (tile counts and split-K are set by the launcher)
 TcParams make_params(const GemmArgs& g) {
   TcParams p;
@@ -330,15 +321,10 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
   const int n_sm = ppu_sm_count();
   const int grid = tiles < n_sm ? tiles : n_sm;
-  OutMap<MODE> mapC;
-  if constexpr (MODE != DRAIN_COLS) {
-    mapC = {};
-    if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
-  }
   constexpr int smem = C::SMEM + store_smem<MODE>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, GEMM_THREADS, smem, st, mapA, mapB, mapC, p) == cudaSuccess ? 0 : -3;
-  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, smem, st>>>(mapA, mapB, mapC, p);
+    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, GEMM_THREADS, smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, smem, st>>>(mapA, mapB, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -449,7 +435,7 @@ int one_units(const GemmArgs& g, TcParams& p) {
 bool two_ok(const GemmArgs& g) {
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   return operands_ok(g) && g.transient && !g.b_kmajor && (f32 || g.epilogue == EPI_OUT_BF16) && (g.splits <= 1 || g.epilogue == EPI_STORE_F32) &&
-         !(g.N % 8) && !(g.ldc % 8) && !(g.aux && (g.ldaux % 8)) && !(reinterpret_cast<uintptr_t>(g.C) & 15) &&
+         !(g.N % 8) && !(g.ldc % 8) && !(g.aux && (g.ldaux % 8)) && !(reinterpret_cast<uintptr_t>(g.C) & (f32 ? 31 : 15)) &&
          !(reinterpret_cast<uintptr_t>(g.aux) & 31) && g.M > 0 && g.N > 0 && g.K > 0;
 }
 }  // namespace
@@ -467,19 +453,17 @@ int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   auto kernel = gemm_tc_kernel<128, true, false, DRAIN_TWO>;
   if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
   CUtensorMap mapA, mapB;
-  OutMap<DRAIN_TWO> m = {};
+  Second<DRAIN_TWO> m = {};
   TcParams p;
   m.units = one_units(g, p);
   m.a_k = g.a_kmajor;
   if (!encode_map(&mapA, g.A, g.lda, g.a_kmajor, g.M, g.K, p.a_rows, true, p.k_rows)) return -2;
   if (!encode_map(&mapB, g.B, g.ldb, false, g.N, g.K, 128, true, p.k_rows)) return -2;
-  if (g.epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c, g.C, g.ldc, g.M, g.N)) return -2;
   if (g2) {
-    m.units2 = one_units(*g2, m.p2);
+    m.units2 = one_units(*g2, m.p);
     m.a_k2 = g2->a_kmajor;
-    if (!encode_map(&m.a2, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, m.p2.a_rows, true, m.p2.k_rows)) return -2;
-    if (!encode_map(&m.b2, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p2.k_rows)) return -2;
-    if (g2->epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c2, g2->C, g2->ldc, g2->M, g2->N)) return -2;
+    if (!encode_map(&m.a, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, m.p.a_rows, true, m.p.k_rows)) return -2;
+    if (!encode_map(&m.b, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p.k_rows)) return -2;
   }
   m.fill = g2 ? two_fill(g, *g2, 190) : 0;
   const int units = m.units + m.units2, n_sm = ppu_sm_count();

@@ -116,7 +116,7 @@ __device__ __forceinline__ PairUnit pair_unit(const TcParams& p, int u, int num_
 template <int PAIR_BN, bool A_K, bool B_K, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-                    const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ OutMap<MODE> mapC,
+                    const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ Second<MODE> two,
                     const __grid_constant__ TcParams p) {
   using PC = PairCfg<PAIR_BN>;
   constexpr int ST = PC::STAGES, PAIR_STAGE_BYTES = PC::STAGE_BYTES, HALF_BYTES = PC::A_HALF, B_SLAB = PC::B_SLAB;
@@ -162,20 +162,20 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   const int k_blocks = (p.K + PAIR_KH * BK - 1) / (PAIR_KH * BK);
   int num_units = p.splits > 1 ? num_tiles * p.splits
                                : num_tiles + (PAIR_BN == 256 && num_tiles > p.tail_from ? num_tiles - p.tail_from : 0);
-  // units of a DRAIN_TWO launch: those of p, then those of mapC.p2
+  // units of a DRAIN_TWO launch: those of p, then those of two.p
   constexpr bool TWO = MODE == DRAIN_TWO, FIT = MODE != DRAIN_COLS;   // FIT: boxes may be smaller than a stage
-  if constexpr (TWO) num_units = mapC.units + mapC.units2;
+  if constexpr (TWO) num_units = two.units + two.units2;
   auto unit_of = [&](int i) {
-    if constexpr (TWO) return two_unit(i, pair, n_pairs, mapC.units, mapC.units2, mapC.fill);
+    if constexpr (TWO) return two_unit(i, pair, n_pairs, two.units, two.units2, two.fill);
     else return pair + i * n_pairs;
   };
-  auto second = [&](int u) { if constexpr (TWO) return u >= mapC.units; else return false; };
-  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &mapC.p2 : &p; else return &p; };
-  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? mapC.a_k2 : mapC.a_k) != 0; else return A_K; };
+  auto second = [&](int u) { if constexpr (TWO) return u >= two.units; else return false; };
+  auto params = [&](bool sec) { if constexpr (TWO) return sec ? &two.p : &p; else return &p; };
+  auto a_kmajor = [&](bool sec) { if constexpr (TWO) return (sec ? two.a_k2 : two.a_k) != 0; else return A_K; };
   auto locate = [&](int u, bool sec) {
     if constexpr (TWO) {
       const TcParams& q = *params(sec);
-      return pair_unit<PAIR_BN>(q, sec ? u - mapC.units : u, q.tiles_m * q.tiles_n, (q.K + PAIR_KH * BK - 1) / (PAIR_KH * BK));
+      return pair_unit<PAIR_BN>(q, sec ? u - two.units : u, q.tiles_m * q.tiles_n, (q.K + PAIR_KH * BK - 1) / (PAIR_KH * BK));
     } else {
       return pair_unit<PAIR_BN>(p, u, num_tiles, k_blocks);
     }
@@ -195,7 +195,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         const bool narrow = w.bn != PAIR_BN;
         const int b_slab = narrow ? B_SLAB / 2 : B_SLAB;          // this CTA's bn/2 rows of B, 64 k
         const CUtensorMap *mA = &mapA, *mB = narrow ? &mapB2 : &mapB;
-        if constexpr (TWO) if (sec) { mA = &mapC.a2; mB = &mapC.b2; }
+        if constexpr (TWO) if (sec) { mA = &two.a; mB = &two.b; }
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.flags);
           if (!ok) break;
@@ -289,15 +289,14 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * PAIR_BN);
       if constexpr (TWO)
-        drain_two(*params(sec), sec ? &mapC.c2 : &mapC.c, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+        drain_two(*params(sec), store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
       else
-        drain_mode<MODE>(p, mapC, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+        drain_mode<MODE>(p, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
-    if (MODE != DRAIN_COLS && lane == 0) tma_store_wait();
   }
 
   // ---------------- common exit ----------------
@@ -353,16 +352,11 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   }
   mapB2 = mapB;
   if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
-  OutMap<MODE> mapC;
-  if constexpr (MODE != DRAIN_COLS) {
-    mapC = {};
-    if (g.C && !encode_out_map(&mapC.c, g.C, g.ldc, g.M, MODE == DRAIN_PIECES ? (int)g.ldc : g.N)) return -2;
-  }
   constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB2, mapC, p) ==
+    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB2, Second<MODE>{}, p) ==
                    cudaSuccess ? 0 : -3;
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, smem, st>>>(mapA, mapB, mapB2, mapC, p);
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, smem, st>>>(mapA, mapB, mapB2, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -402,19 +396,17 @@ int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t 
   auto kernel = gemm_tc_pair_kernel<256, true, false, DRAIN_TWO>;
   if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
   CUtensorMap mapA, mapB;
-  OutMap<DRAIN_TWO> m = {};
+  Second<DRAIN_TWO> m = {};
   TcParams p;
   m.units = two_units(g, p);
   m.a_k = g.a_kmajor;
   if (!encode_map(&mapA, g.A, g.lda, g.a_kmajor, g.M, g.K, 128, true, p.k_rows)) return -2;
   if (!encode_map(&mapB, g.B, g.ldb, false, g.N, g.K, 128, true, p.k_rows)) return -2;
-  if (g.epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c, g.C, g.ldc, g.M, g.N)) return -2;
   if (g2) {
-    m.units2 = two_units(*g2, m.p2);
+    m.units2 = two_units(*g2, m.p);
     m.a_k2 = g2->a_kmajor;
-    if (!encode_map(&m.a2, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, 128, true, m.p2.k_rows)) return -2;
-    if (!encode_map(&m.b2, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p2.k_rows)) return -2;
-    if (g2->epilogue == EPI_OUT_BF16 && !encode_out_map(&m.c2, g2->C, g2->ldc, g2->M, g2->N)) return -2;
+    if (!encode_map(&m.a, g2->A, g2->lda, g2->a_kmajor, g2->M, g2->K, 128, true, m.p.k_rows)) return -2;
+    if (!encode_map(&m.b, g2->B, g2->ldb, false, g2->N, g2->K, 128, true, m.p.k_rows)) return -2;
   }
   const int units = m.units + m.units2, max_pairs = ppu_sm_count() / 2, waves = (units + max_pairs - 1) / max_pairs;
   m.fill = g2 ? two_fill(g, *g2, 330) : 0;
