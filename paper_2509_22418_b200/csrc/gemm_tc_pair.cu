@@ -59,6 +59,13 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// the same without a release at cluster scope, which waits until the warp's global stores have arrived (the
+// largest stall of 256 x 32768 x 2048, whose tiles are mostly stores: ARRIVE_US).  For an accumulator handed back
+// it orders nothing that is needed: its reads from tensor memory are complete (tcgen05.wait::ld), and nobody
+// in the cluster reads the stores.
+__device__ __forceinline__ void mbar_arrive_cluster_cta(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // TMA tile load of a CTA pair: the bytes land in this CTA's shared memory, the completion is
 // counted on the barrier at cluster address `bar` (the leader's)
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
@@ -294,7 +301,10 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
         drain_mode<MODE>(p, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
+      if (lane == 0) {
+        if constexpr (MODE == DRAIN_COLS) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
+        else mbar_arrive_cluster_cta(map_to_rank(tempty_bar(acc), 0));
+      }
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
   }
