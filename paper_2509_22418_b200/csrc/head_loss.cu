@@ -23,7 +23,7 @@
 // Step 2 once rewrote the whole buffer as ds: 27 us per 1024 rows of 32768 (L2-resident), 7 % of the
 // call at 8192 rows; without it GAIN_US.
 // Roundings: u and f X are bf16 (the tensor cores' operand type; each off by at most half a step, 2^-8 of
-// its own value, independently), dX and dE are rounded once from fp32; statistics, losses and running
+// its own value; f is off by as much for all but the entries' places, see there), dX and dE are rounded once from fp32; statistics, losses and running
 // sums are fp32.  (The tensor cores' fp32 sums drop what lies below the last bit, so logits come out low
 // by up to 2^-24 per 16 products: 2e-6 of a logit at d = 2048.)
 #include <algorithm>
@@ -118,10 +118,18 @@ __global__ void __launch_bounds__(256) count_rows_kernel(Targets tg, int T, int 
 }
 // the same by one block, which needs no zeroed count: one launch less
 __global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int T, int V, int* count) {
+  __shared__ int s_n[32];
   pdl_wait(); pdl_trigger();
   int n = 0;
-  for (int64_t t0 = 0; t0 < T; t0 += 1024) n += __syncthreads_count(t0 + threadIdx.x < T && row_counts(tg, t0 + threadIdx.x, V));
-  if (threadIdx.x == 0) *count = n;
+#pragma unroll 4
+  for (int64_t t = threadIdx.x; t < T; t += 1024) n += row_counts(tg, t, V);
+  n = __reduce_add_sync(0xffffffffu, n);
+  if ((threadIdx.x & 31) == 0) s_n[threadIdx.x >> 5] = n;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    n = __reduce_add_sync(0xffffffffu, s_n[threadIdx.x]);
+    if (threadIdx.x == 0) *count = n;
+  }
 }
 
 // scales 64 stored powers
@@ -201,8 +209,8 @@ template <bool GRAD, int W>
 __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const RowArgs a, int rows) {
   constexpr int R = W == 1 ? 4 : 1, THREADS = W == 1 ? 128 : 32 * W, N = 32 * W;     // rows and threads of a block, threads of a row
   __shared__ int s_id[R][MAX_ENTRIES];
-  __shared__ float s_q[R][MAX_ENTRIES], s_l[R][MAX_ENTRIES];
-  __shared__ float s_total[R], s_entropy[R], s_sum[16];
+  __shared__ float s_q[R][MAX_ENTRIES], s_l[R][MAX_ENTRIES], s_v[R][MAX_ENTRIES];
+  __shared__ float s_total[R], s_entropy[R], s_f[R], s_inv[R], s_sum[16];
   __shared__ int s_any[R], s_last, s_count[THREADS / 32];
   __shared__ Piece s_piece[W];
   const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5, tid = W == 1 ? lane : threadIdx.x;   // of the row
@@ -340,7 +348,6 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         w = 1.f / (float)n;
       }
       const float total = s_total[g];
-      const float f = w * a.tg.inv_temp * total * exp2f(ref - lse2);
       if (warp == 0) {
         float x = 0.f;
         for (int j = lane; j < k; j += 32)
@@ -350,10 +357,56 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           const float l = s_entropy[g] + x * LN2;
           if (a.row_loss) a.row_loss[t] = l;
           a.weighted[t] = w * l;
-          if (GRAD) a.factor[row] = f;
+        }
+        if (GRAD) {
+          // what the entries' places are to hold: (p - q / Q) / 2^(ref - lse2).  With p = exp(x): (exp(x) - 1) + (1 - q / Q)
+          // keeps its digits where p is next to 1.  An id given twice: its first entry stands for all.
+          for (int j = lane; j < k; j += 32) {
+            const int id = s_id[g][j];
+            float v = 0.f;
+            if (id >= 0 && total != 0.f && !(j > 0 && s_id[g][j - 1] == id)) {
+              float q = 0.f;
+              for (int i = j; i < k && s_id[g][i] == id; ++i) q += s_q[g][i];
+              v = (expm1f((s_l[g][j] - lse2) * LN2) + (total - q) / total) * exp2f(lse2 - ref);
+            }
+            s_v[g][j] = v;
+          }
+          __syncwarp();
+          // These carry most of the gradient, and rounded to bf16 they would be off by up to 2^-8.  So the row's factor
+          // is moved by as much, to where they round best: a lane tries the factor that makes one of them
+          // exact (the largest of its share; the last lane leaves it), the least sum of squares is taken.
+          // (relative errors at 8192 x 2048 x 32768 against 64 bits, 1.7e-3 of them the results' own rounding: dE 2.9e-3
+          // without, 2.4e-3 with; dX 2.4e-3 and 1.7e-3)
+          float ratio = 1.f;
+          if (lane < 31) {
+            float top = 0.f;
+            for (int j = lane; j < k; j += 31) if (fabsf(s_v[g][j]) > fabsf(top)) top = s_v[g][j];
+            const float r = __bfloat162float(__float2bfloat16_rn(top));
+            if (r != 0.f) ratio = top / r;
+          }
+          const float inv = 1.f / ratio;
+          float err = 0.f;
+          for (int j = 0; j < k; ++j) {
+            const float v = s_v[g][j], e = fmaf(-__bfloat162float(__float2bfloat16_rn(v * inv)), ratio, v);
+            err = fmaf(e, e, err);
+          }
+          if (!(err < INFINITY)) err = INFINITY;
+          float best = err;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
+          const unsigned who = __ballot_sync(0xffffffffu, err == best);
+          const int from = best < INFINITY ? __ffs(who) - 1 : 31;
+          const float use = __shfl_sync(0xffffffffu, ratio, from), use_inv = __shfl_sync(0xffffffffu, inv, from);
+          if (lane == 0) {
+            const float f = w * a.tg.inv_temp * total * exp2f(ref - lse2) * use;
+            s_f[g] = f; s_inv[g] = use_inv;
+            a.factor[row] = f;
+          }
         }
       }
       if (GRAD) {
+        sync();
+        const float f = s_f[g], inv = s_inv[g];
         if (fx)
 #pragma unroll 4
           for (int i = tid; i < n8; i += N) {
@@ -373,13 +426,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         }
         for (int j = tid; j < k; j += N) {          // those stand: overwrite the entries' places
           const int id = s_id[g][j];
-          if (id < 0) continue;
-          if (j > 0 && s_id[g][j - 1] == id) continue;          // an id given twice: its first entry writes for all
-          float q = 0.f;
-          for (int i = j; i < k && s_id[g][i] == id; ++i) q += s_q[g][i];
-          // p - q / Q with p = exp(x): (exp(x) - 1) + (1 - q / Q) keeps its digits where p is next to 1
-          if (total != 0.f)
-            ur[id] = __float2bfloat16_rn((expm1f((s_l[g][j] - lse2) * LN2) + (total - q) / total) * exp2f(lse2 - ref));
+          if (id >= 0 && total != 0.f && !(j > 0 && s_id[g][j - 1] == id)) ur[id] = __float2bfloat16_rn(s_v[g][j] * inv);
         }
       }
     }

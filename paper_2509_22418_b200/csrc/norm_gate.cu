@@ -18,7 +18,7 @@
 // (no atomics).  Rows arrive through a ring of cp.async copies in shared memory: a unit works on one row at a
 // time, two to four sums over its threads one after the other, and loads for it would wait as long again.
 // LANES is a compile-time constant: with the loops over lanes and warps left to run time the same
-// kernel issued 675 instructions per warp and row and took 84 us where it now takes FWD_US (8192 x 2048).
+// kernel issued 675 instructions per warp and row and took 84 us at 8192 x 2048 where it takes 38.
 #include <algorithm>
 #include "../../include/ppu.h"
 #include "common.cuh"
@@ -28,7 +28,11 @@ int ppu_fail(int code, const char* fmt, ...);
 namespace {
 
 constexpr int MAX_D = 4096;
-constexpr int FWD_CH = 4, BWD_CH = 2;         // the backward pass has its running sums beside the row
+// 8 columns a thread, and as many threads on an SM as the registers then allow.  8192 x 2048, inputs and outputs beyond
+// the L2: forward 38.2 us with 768 threads of 80 registers, 42.9 with 1024 of 64 (spilling), 49 with 16 columns
+// a thread (384 threads of 145 registers); backward 55.3 us with 512 threads of 128 registers, 68 with 256, 76 with
+// 4 columns a thread.  Three rows in flight do as well as four.
+constexpr int CH = 2, FWD_THREADS = 768, BWD_THREADS = 512;
 
 struct NormArgs {
   const bf16 *y, *dh;
@@ -135,7 +139,7 @@ template <int LANES> __device__ __forceinline__ int turns_of(const Unit& u) {
 }
 
 // a vector's chunks of this thread
-template <int LANES, int CH>
+template <int LANES>
 __device__ __forceinline__ void load_vector(const float* p, int tid, int d, float (&f)[CH][4]) {
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -146,18 +150,18 @@ __device__ __forceinline__ void load_vector(const float* p, int tid, int d, floa
 
 // A row in flight: per thread and chunk 8 bytes of each bf16 and 16 of each fp32 operand.  A thread
 // copies and reads its own columns alone, so there is no barrier.
-template <bool BWD, int GATE, int CH> struct Ring {
+template <bool BWD, int GATE> struct Ring {
   static constexpr int NB = BWD ? 2 : 1, NF = (BWD ? 2 : 1) + (GATE == 2 ? 1 : 0);
   static constexpr int BYTES = CH * (8 * NB + 16 * NF);      // per thread
-  static constexpr int STAGES = BWD && GATE == 2 ? 3 : 4;
+  static constexpr int STAGES = 3;
 };
 
 // GATE: 0 none, 1 one row for all rows, 2 read with each row
 template <int LANES, int GATE>
-__global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(Layout<LANES>::BLOCK, FWD_THREADS / Layout<LANES>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
   pdl_wait(); pdl_trigger();
-  constexpr int CH = FWD_CH, BLOCK = Layout<LANES>::BLOCK;
-  using R = Ring<false, GATE, CH>;
+  constexpr int BLOCK = Layout<LANES>::BLOCK;
+  using R = Ring<false, GATE>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_sum[Layout<LANES>::UNITS][2 * Layout<LANES>::WARPS];
   const Unit u = my_unit<LANES>(a);
@@ -271,10 +275,10 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_fwd_kernel(con
 
 // GATE: 0 none, 1 one row for all of the unit's rows, 2 read with each row, its gradient written at the end of each group
 template <int LANES, int GATE>
-__global__ void __launch_bounds__(Layout<LANES>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(Layout<LANES>::BLOCK, BWD_THREADS / Layout<LANES>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
   pdl_wait(); pdl_trigger();
-  constexpr int CH = BWD_CH, BLOCK = Layout<LANES>::BLOCK;
-  using R = Ring<true, GATE, CH>;
+  constexpr int BLOCK = Layout<LANES>::BLOCK;
+  using R = Ring<true, GATE>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_sum[Layout<LANES>::UNITS][2 * 2 * Layout<LANES>::WARPS];
   const Unit u = my_unit<LANES>(a);
@@ -471,15 +475,15 @@ constexpr int SMS = 148;                      // work is split for a B200 (also 
 struct Shape { int lanes, units, per_group, gate_mode; size_t partial; };
 
 // threads of a unit: the fewest that hold a row, of the sizes that are compiled
-int lanes_for(int d, int ch) {
-  for (int l : {4, 8, 16, 32, 64, 96, 128, 192, 256}) if (4 * ch * l >= d) return l;
+int lanes_for(int d) {
+  for (int l : {4, 8, 16, 32, 64, 96, 128, 192, 256}) if (4 * CH * l >= d) return l;
   return 512;
 }
-// rows are dealt to about `threads` threads per SM
+// rows are dealt to as many threads per SM as are resident there
 Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
   Shape s;
-  s.lanes = lanes_for(d, backward ? BWD_CH : FWD_CH);
-  const int threads = 512;
+  s.lanes = lanes_for(d);
+  const int threads = backward ? BWD_THREADS : FWD_THREADS;
   const int64_t target = std::min<int64_t>(16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (threads / s.lanes)));
   const int64_t groups = has_gate ? ((int64_t)T + gate_rows - 1) / gate_rows : 1;
   s.per_group = 0;
@@ -521,7 +525,7 @@ bool misaligned(std::initializer_list<const void*> ps) {
 template <int LANES, int GATE, bool BWD>
 int launch_norm(const NormArgs& a, cudaStream_t st) {
   using L = Layout<LANES>;
-  using R = Ring<BWD, GATE, BWD ? BWD_CH : FWD_CH>;
+  using R = Ring<BWD, GATE>;
   constexpr int bytes = R::BYTES * R::STAGES * L::BLOCK;
   static_assert(bytes <= 220 * 1024, "shared memory of a block");
   static PerDeviceFlag attr;
@@ -547,8 +551,7 @@ int dispatch(const NormArgs& a, const Shape& s, cudaStream_t st) {
 #undef LANES_CASE
     default: break;
   }
-  if constexpr (BWD) return launch_gate<512, BWD>(a, s.gate_mode, st);
-  return ppu_fail(PPU_ESHAPE, "row too long");
+  return launch_gate<512, BWD>(a, s.gate_mode, st);
 }
 
 }  // namespace

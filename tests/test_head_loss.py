@@ -6,7 +6,8 @@ Roundings counted (u = 2^-24 for fp32, half a step; bf16 half a step 2^-8):
     addition off by at most a whole step 2^-23 of the sum of magnitudes: (d / 16 + 8) 2^-23 sum |x e|;
   log-sum-exp: the largest logit error, the exponentials' relative error (2^-21 with the rounding of their
     argument: |argument| u / ln 2 more) and the rounding of the result;
-  ds = f u: the stored power u is bf16, 2^-8 of Q p |w| (an entry's place: 2^-8 of its own value), beside the
+  ds = f u: the stored power u is bf16, and the row's factor is moved by up to half a bf16 step so that the
+    entries' places round well: 2 * 2^-8 of Q p |w| (an entry's place: 2^-8 of its own value), beside the
     logits' errors; for dE the factor is multiplied into X, which is rounded to bf16 again: 2^-8 |ds| more;
   dX, dE: the errors of ds times the other operand's magnitudes, the sums' (n / 16 + 8) 2^-23 of the sum of
     magnitudes, and the result's own half step.
@@ -52,7 +53,7 @@ def tolerances(X, E, q, w, temp, R, entropy):
     lse = worst + 2.0 ** -21 + 4 * U * spread + 8 * U
     row = R["Q"] * (lse + worst) + 32 * U * (np.abs(entropy) + (np.abs(q).sum(1)) * (spread + 8))
     both = (s_err + lse[:, None]) * 1.01
-    ds = np.abs(w)[:, None] * R["Q"][:, None] * R["p"] * (BF + 2.0 ** -15 + both) + BF * np.abs(R["ds"]) + np.abs(w)[:, None] * 64 * U
+    ds = np.abs(w)[:, None] * R["Q"][:, None] * R["p"] * (2 * BF + 2.0 ** -14 + both) + BF * np.abs(R["ds"]) + np.abs(w)[:, None] * 64 * U
     ds_e = ds * (1 + BF) + BF * np.abs(R["ds"])
     # (64 U: the entries' own places, 1 - p formed from q and p in fp32)
     sums = lambda n: (n / 16 + 12) * 2 * U  # noqa: E731
@@ -220,7 +221,7 @@ def test_offsets_beyond_32_bits():
         p = torch.exp(s - lse[:, None])
         ds = p * w
         ds[at] -= w
-        err = w * p * (BF + 2.0 ** -15 + 1.01 * (s_err + tol["lse"][b][:, None])) + BF * ds.abs() + w * 64 * U
+        err = w * p * (2 * BF + 2.0 ** -14 + 1.01 * (s_err + tol["lse"][b][:, None])) + BF * ds.abs() + w * 64 * U
         R["dX"][b] = ds @ e
         tol["dX"][b] = (err @ e.abs() + sums(V) * (ds.abs() @ e.abs())) * (1 + BF) + BF * R["dX"][b].abs()
         R["dE"] += ds.T @ x[b]
