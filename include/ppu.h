@@ -340,7 +340,7 @@ int ppu_head_xent(const void* X, int64_t ldx, const void* E, int64_t lde, const 
                   float* lse, void* dX, int64_t lddx, void* dE, int64_t ldde, int chunk_rows,
                   void* workspace, size_t workspace_bytes, int32_t* flags, void* cuda_stream);
 /* ld_ids, ld_logits: row strides of teacher_ids (int32) and teacher_logits (fp32), at least k;
- * 1 <= k <= PPU_MAX_TEACHER_ENTRIES; teacher_lse may be null. */
+ * 1 <= k <= PPU_MAX_TEACHER_ENTRIES; 1e-4 <= temperature <= 1e4; teacher_lse may be null. */
 int ppu_head_distill(const void* X, int64_t ldx, const void* E, int64_t lde,
                      const int32_t* teacher_ids, int64_t ld_ids, const float* teacher_logits,
                      int64_t ld_logits, int k, const float* teacher_lse, float temperature,

@@ -6,6 +6,9 @@
                                                        the 1.3B-class layer shape but only L layers
                                                        (a few GB: the small case for profiler
                                                        captures of the bandwidth-bound kernels)
+  head  --m T --n V --k D [--teacher K] [--no-grad]     head loss of T rows against V ids (cross entropy, or
+                                                       distillation from K teacher entries)
+  norm  --m T --k D [--rms] [--gate-rows R]            gated norm pair, forward and backward
 Times with CUDA events on the launching stream after warm-up; operands are sized by the caller
 (keep them above the 126 MB L2 if DRAM behaviour matters).  Also the target of profiler runs.
 """
@@ -19,7 +22,7 @@ from paper_2509_22418_b200 import build, ppu, synth
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["gemm", "attn", "path"])
+    ap.add_argument("op", choices=["gemm", "attn", "path", "head", "norm"])
     ap.add_argument("--m", type=int, default=8192)
     ap.add_argument("--n", type=int, default=8192)
     ap.add_argument("--k", type=int, default=2048)
@@ -37,6 +40,10 @@ def main():
     ap.add_argument("--replicas", type=int, default=4)
     ap.add_argument("--train-non-mlp", action="store_true")
     ap.add_argument("--head-slices", type=int, default=0, help="path: MLP + head slicing with this many head groups")
+    ap.add_argument("--teacher", type=int, default=0)
+    ap.add_argument("--no-grad", action="store_true")
+    ap.add_argument("--rms", action="store_true")
+    ap.add_argument("--gate-rows", type=int, default=0, help="norm: rows that share a row of the gate (0: all of them)")
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--warmup", type=int, default=3)
     a = ap.parse_args()
@@ -89,6 +96,29 @@ def main():
         fl = 2.0 * a.m * a.n * a.k
         print(f"gemm M={a.m} N={a.n} K={a.k} a_mn={a.a_mn} b_mn={a.b_mn} backend={a.backend}: {ms:.4f} ms "
               f"{fl / ms / 1e9:.1f} TFLOP/s")
+    elif a.op == "head":
+        T, V, d = a.m, a.n, a.k
+        E = (torch.randn((V, d), generator=g) * (3.0 / d ** 0.5)).to(dev).bfloat16()
+        X = torch.randn((T, d), generator=g).to(dev).bfloat16()
+        ids = torch.randint(0, V, (T, max(1, a.teacher)), generator=g, dtype=torch.int32).to(dev)
+        z = torch.randn(ids.shape, generator=g).to(dev)
+        if a.teacher:
+            ms = timed(lambda: ppu.ppu_head_distill(X, E, ids, z, temperature=2.0, grad=not a.no_grad))
+        else:
+            ms = timed(lambda: ppu.ppu_head_xent(X, E, ids[:, 0].contiguous(), grad=not a.no_grad))
+        fl = (2.0 if a.no_grad else 6.0) * T * V * d
+        print(f"head T={T} V={V} d={d} teacher={a.teacher} grad={not a.no_grad}: {ms:.4f} ms {fl / ms / 1e9:.1f} TFLOP/s")
+    elif a.op == "norm":
+        T, d = a.m, a.k
+        rows = a.gate_rows or T
+        y, r = torch.randn((T, d), generator=g).to(dev).bfloat16(), torch.randn((T, d), generator=g).to(dev)
+        one, gate = torch.ones(d, device=dev), torch.ones((-(-T // rows), d), device=dev)
+        kw = dict(gate=gate, gate_rows=rows, kind="rms" if a.rms else "layer")
+        r_out, hh, st = ppu.ppu_norm_gate_fwd(y, r, one, one, **kw)
+        ms = timed(lambda: ppu.ppu_norm_gate_fwd(y, r, one, one, **kw))
+        print(f"norm fwd T={T} d={d}: {ms:.4f} ms {12.0 * T * d / ms / 1e6:.0f} GB/s")
+        ms = timed(lambda: ppu.ppu_norm_gate_bwd(hh, r, y, r_out, st, one, one, **kw))
+        print(f"norm bwd: {ms:.4f} ms {18.0 * T * d / ms / 1e6:.0f} GB/s")
     else:
         B_, S, h, dh = a.batch, a.seq, a.heads, a.dh
         d = h * dh

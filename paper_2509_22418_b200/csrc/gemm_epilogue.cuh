@@ -343,7 +343,7 @@ __device__ __forceinline__ float ex2_fast(float x) {
 // its 4 KB of shared memory, so that a store covers four rows' whole 128-byte lines.  (From the registers, a lane
 // 32 bytes of its own row at a time, a store touches 32 lines: 2304 x 32000 x 768 took 95 us against 70 without
 // the store.  By TMA from the same shared memory it took 90: the buffer is free again only when the copy has
-// read it.  This way STORE_US.)  Row r of the buffer has its 16-byte pieces in the places j ^ (r & 7): no bank conflicts
+// read it.  This way 85; the dE of 256 x 2048 x 32768, all stores, 73 us instead of 111 by TMA.)  Row r of the buffer has its 16-byte pieces in the places j ^ (r & 7): no bank conflicts
 // either way.  rows, cols: of the output, from here on.
 __device__ __forceinline__ void store_group(bf16* out, long long ld, uint32_t buf, const uint32_t* o, int rows, int cols, int lane) {
   __syncwarp();                     // (the group before has been read)

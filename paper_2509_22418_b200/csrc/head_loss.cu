@@ -15,17 +15,18 @@
 //      logits (within 41 nats of 0), else the piece's maximum.  The entries' own x are kept in fp32 (the powers
 //      would be too coarse for the loss and for p - 1 next to p = 1); for that a kernel before it has
 //      sorted each row's entries and counted how many lie before each piece (not needed for one entry a row).
-//   2. a warp or a block per row joins the pieces to the row's log-sum-exp and forms the row loss.  Then ds_tv = f_t u_tv with one factor per
-//      row: the powers stay as they are, but for the entries' places, which are overwritten, and for
-//      pieces (rows) beyond the range of the common reference, which are rescaled.
+//   2. a warp or a block per row joins the pieces to the row's log-sum-exp and forms the row loss.  Then
+//      ds_tv = f_t u_tv with one factor per row: the powers stay as they are, but for the entries'
+//      places, which are overwritten, and for pieces (rows) beyond the range of the common reference,
+//      which are rescaled.
 //   3. dX = f (u E), the factor applied in the product's epilogue, and dE = u^T (f X) with f X formed in
-//      step 2; dE over several chunks is a running fp32 sum, rounded once by the last.
+//      step 2, both in one launch; dE over several chunks is a running fp32 sum, rounded once by the last.
 // Step 2 once rewrote the whole buffer as ds: 27 us per 1024 rows of 32768 (L2-resident), 7 % of the
-// call at 8192 rows; without it GAIN_US.
+// call at 8192 rows of d = 2048.
 // Roundings: u and f X are bf16 (the tensor cores' operand type; each off by at most half a step, 2^-8 of
-// its own value; f is off by as much for all but the entries' places, see there), dX and dE are rounded once from fp32; statistics, losses and running
-// sums are fp32.  (The tensor cores' fp32 sums drop what lies below the last bit, so logits come out low
-// by up to 2^-24 per 16 products: 2e-6 of a logit at d = 2048.)
+// its own value; f is off by as much for all but the entries' places, see there), dX and dE are rounded
+// once from fp32; statistics, losses and running sums are fp32.  (The tensor cores' fp32 sums drop what
+// lies below the last bit, so logits come out low: by 1.2e-6 of the log-sum-exp at d = 2048.)
 #include <algorithm>
 #include <climits>
 #include "../../include/ppu.h"
@@ -484,7 +485,8 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 // Slices of the reductions of dX [rows, d] over V and dE [V, d] over the rows, which one launch works, from a
 // model of its time: units of (k + overhead), 6 ns for each k (an SM pair's 256 x 256 tile; one SM's 128 x 128
 // tile takes the same), shared out evenly or as long as the longest unit; then for a split product its
-// partial sums, read at 3.3 TB/s by a launch of its own (3 us).  Slices are at least 1024 long.
+// partial sums, read at 3.3 TB/s by a launch of its own (3 us).  Slices are at least 1024 long (at 512 the join of 24 rows and
+// of 1001 costs more than it saves: 66 us against 62, 56 against 52).
 void choose_splits(int64_t rows, int64_t d, int64_t V, int want, bool split_e, int* sx, int* se) {
   GemmArgs gx, ge;
   gx.M = (int)rows; gx.N = (int)d; ge.M = (int)V; ge.N = (int)d;
@@ -737,7 +739,7 @@ extern "C" int ppu_head_distill(const void* X, int64_t ldx, const void* E, int64
                                 size_t workspace_bytes, int32_t* flags, void* cuda_stream) {
   if (k < 1 || k > PPU_MAX_TEACHER_ENTRIES)
     return ppu_fail(PPU_ESHAPE, "k must lie in 1..%d (got %d)", PPU_MAX_TEACHER_ENTRIES, k);
-  if (!(temperature > 0.f) || !(temperature < 1e6f)) return ppu_fail(PPU_EINVAL, "temperature must be positive");
+  if (!(temperature >= 1e-4f) || !(temperature <= 1e4f)) return ppu_fail(PPU_EINVAL, "temperature must lie in 1e-4..1e4");
   if (ld_ids < k || ld_logits < k) return ppu_fail(PPU_EINVAL, "teacher row strides must be at least k");
   if (T && !teacher_logits) return ppu_fail(PPU_EINVAL, "null operand");
   HeadCall c;

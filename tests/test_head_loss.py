@@ -587,7 +587,8 @@ def test_cross_entropy_refuses_misaligned_operands(ppu):
 
 @pytest.mark.parametrize("k,ldi,ldz,temp,z,code", [(0, 4, 4, 1.0, True, -2), (129, 200, 200, 1.0, True, -2), (4, 3, 4, 1.0, True, -1), (4, 4, 3, 1.0, True, -1),
                                                    (4, 4, 4, 0.0, True, -1), (4, 4, 4, -1.0, True, -1), (4, 4, 4, math.nan, True, -1),
-                                                   (4, 4, 4, math.inf, True, -1), (4, 4, 4, 1.0, False, -1)])
+                                                   (4, 4, 4, math.inf, True, -1), (4, 4, 4, 1e-5, True, -1), (4, 4, 4, 1e5, True, -1),
+                                                   (4, 4, 4, 1.0, False, -1)])
 def test_distillation_refuses(ppu, k, ldi, ldz, temp, z, code):
     buf = (C.c_uint8 * 4096)()
     base = (C.addressof(buf) + 255) & ~255

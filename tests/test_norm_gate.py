@@ -40,7 +40,8 @@ def hat_error(x, x_err, xh, mean, rstd):
     return own + np.abs(xh) * rel, rel
 
 
-def backward(c, y, r_out, st, dh, dr, v, gate, groups):
+def backward(c, y, r_out, st, dh, dr, v, gate, groups, e_dh=0.0):
+    """The definition's gradients and their tolerances; e_dh: how far the dh that was used may be from this one."""
     m1, s1, m2, s2 = (st[:, i:i + 1] for i in range(4))
     yh, rh = (y - m1) * s1, (r_out - m2) * s2
     dhat = dh * v["g2"]
@@ -66,7 +67,7 @@ def backward(c, y, r_out, st, dh, dr, v, gate, groups):
         dot = mean(a(dx * xh))
         e_dot = mean(e_dx * a(xh) + a(dx) * e_xh) + S * dot
         return s * (e_dx + S * mean(a(dx)) + mean(e_dx) + e_xh * dot + (a(xh) + e_xh) * e_dot) + 6 * U * s * (a(dx) + mean(a(dx)) + a(xh) * dot)
-    e_G = 2 * U * a(dr) + through_error(dhat, 2 * U * a(dhat), rh, e_rh, s2)
+    e_G = 2 * U * a(dr) + through_error(dhat, 2 * U * a(dhat) + a(v["g2"]) * e_dh, rh, e_rh, s2)
     e_q = a(gate * v["g1"]) * e_G + 4 * U * a(q)
     e_dy = through_error(q, e_q, yh, e_yh, s1)
     over = (len(y) + 110) * U
@@ -78,7 +79,8 @@ def backward(c, y, r_out, st, dh, dr, v, gate, groups):
     e_dn = a(gate) * e_G + 2 * U * a(dn)
     tol = dict(dy=e_dy * (1 + BF) + BF * a(dy), dr=c["scale"] * e_G + 2 * U * a(c["scale"] * G),
                dg1=(e_dn * a(yh) + a(dn) * e_yh).sum(0) + over * a(dn * yh).sum(0), db1=e_dn.sum(0) + over * a(dn).sum(0),
-               dg2=(a(dh) * e_rh).sum(0) + over * a(dh * rh).sum(0), db2=over * a(dh).sum(0), dgate=e_gate + over * mag_gate)
+               dg2=(a(dh) * e_rh + e_dh * (a(rh) + e_rh)).sum(0) + over * a(dh * rh).sum(0),
+               db2=(e_dh + over * a(dh)).sum(0), dgate=e_gate + over * mag_gate)
     return R, {n: t + 1e-30 for n, t in tol.items()}
 
 
