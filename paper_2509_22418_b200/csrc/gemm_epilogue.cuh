@@ -89,6 +89,11 @@ struct TcParams {
   PieceEntries entries;
   const float* row_scale; unsigned* zero_word;
   int dependent;   // launched as a programmatic dependent
+  // Epilogue warps.  0: all eight drain each tile, half of its columns each.  1: four drain one accumulator, four the
+  // other, so that one tile is read from tensor memory (600 cycles of latency for 64 columns) while the other
+  // is stored (900 cycles of the load/store pipe): for blocks that work several tiles (dE of
+  // 24 x 32768 x 768: 18.7 -> 16.7 us, of 90 x 6300 x 360: 11 -> 8).
+  int alternate;
 };
 
 // what a kernel's epilogue warps do with an accumulator: the epilogues of drain_cols, or one of

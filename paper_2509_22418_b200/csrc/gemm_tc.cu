@@ -53,7 +53,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI_WARPS); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? EPI_WARPS / 2 : EPI_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -190,15 +190,20 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
+      if (FIT && p.alternate && acc != half) {   // the other four warps' accumulator
+        if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+        continue;
+      }
+      const int c_begin = FIT && p.alternate ? 0 : half * (BN / 2), c_end = FIT && p.alternate ? BN : (half + 1) * (BN / 2);
       const bool sec = second(u);
       const Place w = locate(u, sec);
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * BN);
       if constexpr (TWO)
-        drain_two(*params(sec), store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+        drain_two(*params(sec), store_buf, w.m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
       else
-        drain_mode<MODE>(p, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, half * (BN / 2), (half + 1) * (BN / 2), lane);
+        drain_mode<MODE>(p, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(tempty_bar(acc));
@@ -286,7 +291,7 @@ TcParams make_params(const GemmArgs& g) {
   p.tiles_m = p.tiles_n = 0; p.tail_from = 1 << 30; p.n_fastest = 0; p.splits = 1; p.split_stride = 0;
   p.C3 = g.C3; p.ldc3 = g.ldc3; p.c3_lo = g.c3_lo; p.c3_hi = g.c3_hi;
   p.piece_scale = g.piece_scale; p.piece_stats = g.piece_stats; p.ld_pieces = g.ld_pieces;
-  p.entries = g.entries; p.row_scale = g.row_scale; p.zero_word = g.zero_word; p.dependent = g.transient ? 1 : 0;
+  p.entries = g.entries; p.row_scale = g.row_scale; p.zero_word = g.zero_word; p.dependent = g.transient ? 1 : 0; p.alternate = 0;
   p.rope_S = g.rope_S > 0 ? g.rope_S : 1; p.rope_dh = g.rope_dh > 0 ? g.rope_dh : 2; p.rope_cols = g.rope_cols;
   const bool f32 = g.epilogue == EPI_STORE_F32 || g.epilogue == EPI_RESID_F32;
   const long long out_unit = f32 ? 8 : 16;   // elements per 32 bytes
@@ -321,6 +326,7 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   const int tiles = p.tiles_m * p.tiles_n * p.splits;
   const int n_sm = ppu_sm_count();
   const int grid = tiles < n_sm ? tiles : n_sm;
+  p.alternate = MODE != DRAIN_COLS && tiles >= 2 * grid;
   constexpr int smem = C::SMEM + store_smem<MODE>();
   if (g.transient)
     return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, GEMM_THREADS, smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
@@ -467,5 +473,6 @@ int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   }
   m.fill = g2 ? two_fill(g, *g2, 190) : 0;
   const int units = m.units + m.units2, n_sm = ppu_sm_count();
+  p.alternate = units >= 2 * n_sm;
   return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, GEMM_THREADS, smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
 }

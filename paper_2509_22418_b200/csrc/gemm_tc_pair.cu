@@ -145,7 +145,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < ST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * EPI_WARPS); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? EPI_WARPS : 2 * EPI_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -289,16 +289,21 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * STORE_BYTES;
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_units; u = unit_of(++i)) {
+      if (FIT && p.alternate && acc != half) {   // the other four warps' accumulator
+        if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+        continue;
+      }
       const bool sec = second(u);
       const PairUnit w = locate(u, sec);
+      const int c_begin = FIT && p.alternate ? 0 : half * (w.bn / 2), c_end = FIT && p.alternate ? w.bn : (half + 1) * (w.bn / 2);
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * PAIR_BN);
       if constexpr (TWO)
-        drain_two(*params(sec), store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+        drain_two(*params(sec), store_buf, m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
       else
-        drain_mode<MODE>(p, store_buf, m0, w.n0, w.sp, t_acc, quarter, half * (w.bn / 2), (half + 1) * (w.bn / 2), lane);
+        drain_mode<MODE>(p, store_buf, m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
@@ -360,6 +365,7 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
     p.tail_from = tiles - rem;
     pairs = max_pairs;
   }
+  p.alternate = MODE != DRAIN_COLS && tiles >= 2 * pairs;
   mapB2 = mapB;
   if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
   constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE>();
@@ -420,6 +426,7 @@ int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t 
   }
   const int units = m.units + m.units2, max_pairs = ppu_sm_count() / 2, waves = (units + max_pairs - 1) / max_pairs;
   m.fill = g2 ? two_fill(g, *g2, 330) : 0;
+  p.alternate = units >= 2 * max_pairs;
   // (one product alone: as many pairs as give each the same number of tiles)
   const int pairs = g2 ? (units < max_pairs ? units : max_pairs) : (units + waves - 1) / waves;
   return ppu_launch_dependent(kernel, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
