@@ -454,19 +454,34 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
   }
 }
 
-// out bf16 [rows, 4 n4] = sum of `splits` fp32 partial products, in index order, times the row's factor
+// out bf16 [rows, 4 n4] = sum of `splits` fp32 partial products times the row's factor.  A block takes 32
+// places of 4 values; each of its 8 warps adds an eighth of the partial products in index order, and the 8 sums are
+// added in order (one thread for all of them: 41 us for 148 products of [120, 128], a chain of loads).
 __global__ void __launch_bounds__(256)
 join_partials_kernel(const float* part, int splits, int64_t stride, const float* row_scale, bf16* out, int64_t ldo, int rows, int n4) {
+  __shared__ float4 s_sum[8][32];
   pdl_wait(); pdl_trigger();
-  const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-  if (i >= (int64_t)rows * n4) return;
-  const int64_t r = i / n4;
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int64_t i = blockIdx.x * (int64_t)32 + lane;
+  const bool on = i < (int64_t)rows * n4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int q = 0; q < splits; ++q) {
-    const float4 x = *reinterpret_cast<const float4*>(part + q * stride + i * 4);
+  if (on) {
+    const int q1 = (g + 1) * splits / 8;
+#pragma unroll 4
+    for (int q = g * splits / 8; q < q1; ++q) {
+      const float4 x = *reinterpret_cast<const float4*>(part + q * stride + i * 4);
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+  }
+  s_sum[g][lane] = s;
+  __syncthreads();
+  if (g || !on) return;
+#pragma unroll
+  for (int w = 1; w < 8; ++w) {
+    const float4 x = s_sum[w][lane];
     s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
   }
+  const int64_t r = i / n4;
   const float f = row_scale ? row_scale[r] : 1.f;
   __nv_bfloat162 a = __floats2bfloat162_rn(f * s.x, f * s.y), b = __floats2bfloat162_rn(f * s.z, f * s.w);
   *reinterpret_cast<uint2*>(out + r * ldo + (i - r * n4) * 4) =
@@ -503,7 +518,8 @@ void choose_splits(int64_t rows, int64_t d, int64_t V, int want, bool split_e, i
   };
   *sx = *se = 1;
   double best = ns(1, 1);
-  for (int s = 2; tx && s <= 32 && s <= V / 1024; ++s)
+  const int most = (int)std::max<int64_t>(32, units / std::max<int64_t>(tx, 1));     // (a single tile's reduction goes to all SMs)
+  for (int s = 2; tx && s <= most && s <= V / 1024; ++s)
     if (const double t = ns(s, 1); t < 0.95 * best) { best = t; *sx = s; }
   for (int s = 2; te && split_e && s <= 32 && s <= rows / 1024; ++s)
     if (const double t = ns(*sx, s); t < 0.95 * best) { best = t; *se = s; }
@@ -600,7 +616,7 @@ void split_product(GemmArgs& g, int splits, float* part) {
 }
 cudaError_t join(const GemmArgs& g, void* out, int64_t ldo, cudaStream_t st) {
   const int64_t n = (int64_t)g.M * (g.N / 4);
-  return ppu_launch_dependent(join_partials_kernel, (unsigned)((n + 255) / 256), 256, 0, st, (const float*)g.C, g.splits, g.split_stride, g.row_scale,
+  return ppu_launch_dependent(join_partials_kernel, (unsigned)((n + 31) / 32), 256, 0, st, (const float*)g.C, g.splits, g.split_stride, g.row_scale,
                               (bf16*)out, ldo, g.M, g.N / 4);
 }
 
