@@ -148,8 +148,7 @@ PyObject* head_call(const Head& h, int k, int grads, int chunk_rows, PyObject* w
   at::Tensor out[5] = {make({}, at::kFloat, h.dev), make({h.T}, at::kFloat, h.dev), make({h.T}, at::kFloat, h.dev), at::Tensor(), at::Tensor()};
   if (grads & 1) out[3] = make({h.T, h.d}, at::kBFloat16, h.dev);
   if (grads & 2) out[4] = make({h.V, h.d}, at::kBFloat16, h.dev);
-  void* dX = (grads & 1) ? out[3].data_ptr() : nullptr;
-  // (no rows: torch gives no address, the call wants to know that the gradient is asked for)
+  void* dX = (grads & 1) ? out[3].data_ptr() : nullptr;      // (null without rows)
   void* dE = (grads & 2) ? out[4].data_ptr() : nullptr;
   const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)h.dev);
   int rc;

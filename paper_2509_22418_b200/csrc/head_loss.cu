@@ -651,17 +651,18 @@ int run_head(const HeadCall& c) {
     return PPU_OK;
   }
   // the rows that count, for a mean: up to 2^10 rows by every block of the row kernel for itself (a launch
-  // costs more), up to 2^14 by one block
+  // costs more; its entries have to be those of all rows), up to 2^14 by one block
+  const bool by_rows = c.T <= (1 << 10) && (k == 1 || p.chunks == 1);
   if (!c.weight && c.T > (1 << 14)) {
     CUDA_OK(cudaMemsetAsync(count, 0, 4, c.st));
     CUDA_OK(ppu_launch_dependent(count_rows_kernel, (c.T + 255) / 256, 256, 0, c.st, c.tg, c.T, c.V, count));
-  } else if (!c.weight && c.T > (1 << 10)) {
+  } else if (!c.weight && !by_rows) {
     CUDA_OK(ppu_launch_dependent(count_rows_block_kernel, 1, 1024, 0, c.st, c.tg, c.T, c.V, count));
   }
   RowArgs r;
   r.tg = c.tg; r.u = u; r.ldu = p.ldu; r.ld_pieces = p.n_pieces; r.n_pieces = (int)p.n_pieces; r.stats = stats;
   r.X = (const bf16*)c.X; r.ldx = c.ldx; r.d = c.d; r.V = c.V; r.T = c.T;
-  r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = c.T > (1 << 10) ? count : nullptr;
+  r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = by_rows ? nullptr : count;
   r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
   r.done = done; r.loss = c.loss; r.flags = c.flags;
   float* ex = (float*)(ws + p.off_x);

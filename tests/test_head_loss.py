@@ -300,6 +300,33 @@ def test_distillation_against_its_definition(T, d, V, k, temp, ragged, known):
 
 
 @gpu
+@pytest.mark.parametrize("T,d,V,k", [(700, 72, 1003, 5), (1024, 8, 64, 128), (600, 64, 300, 2), (1300, 40, 500, 3)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_distillation_in_chunks_of_rows(T, d, V, k, weights):
+    """A mean counts the rows of all chunks: loss and row factors as with one chunk."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    rng, Xt, X, Et, E, target = make(T, d, V, seed=T)
+    ids, z = teacher(rng, T, V, k, target, True)
+    ids[256:512] = -1                      # a whole chunk without an entry
+    ii, q, ent, there = soft(ids, z, 1.0, None)
+    w = rng.random(T).astype(np.float32) if weights else None
+    w64 = w.astype(np.float64) * there if weights else mean_weights(there)
+    R = definition(X, E, ii, q, ent, w64, 1.0)
+    args = [Xt, Et, torch.from_numpy(ids).cuda(), torch.from_numpy(z).cuda()]
+    wt = None if w is None else torch.from_numpy(w).cuda()
+    whole = ppu.ppu_head_distill(*args, row_weight=wt)
+    assert abs(float(whole[0]) - (w64 * R["row"]).sum()) <= 1e-3 * (np.abs(w64) * np.abs(R["row"])).sum()
+    # dE: fp32 sums of the same products in another order, 2^-23 a term and side, each rounded once to bf16
+    tol = 2 * BF * whole[4].double().abs().cpu().numpy() * (1 + 2 * BF) + 2 * T * 2 * U * (np.abs(R["ds"]).T @ np.abs(X)) * (1 + 8 * BF)
+    for rows in (1, 512):
+        got = ppu.ppu_head_distill(*args, row_weight=wt, chunk_rows=rows)
+        for j in range(4):
+            assert torch.equal(got[j], whole[j]), j
+        assert ((got[4].double() - whole[4].double()).abs().cpu().numpy() <= tol + 1e-30).all()
+
+
+@gpu
 def test_one_teacher_entry_is_cross_entropy():
     import torch
     from paper_2509_22418_b200 import ppu
