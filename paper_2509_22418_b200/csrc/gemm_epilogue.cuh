@@ -422,14 +422,21 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int j = 0; j < PIECE; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
-    float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.piece_scale;
+    mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    float top = mx[0] * p.piece_scale;
     if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
+    float less = top;
+    if (fabsf(top) > 16777216.f) {         // 2^24: the rounding of top would be an exponent of more than 1 (the largest is taken off first)
+#pragma unroll
+      for (int j = 0; j < PIECE; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - mx[0]);
+      less = 0.f;
+    }
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     uint32_t o[PIECE / 2];
 #pragma unroll
     for (int j = 0; j < PIECE / 2; ++j) {
-      const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -top));
-      const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -top));
+      const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -less));
+      const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -less));
       sum[(2 * j) & 3] += e0;
       sum[(2 * j + 1) & 3] += e1;
       o[j] = pack2_bf16(e0, e1);

@@ -431,6 +431,50 @@ def test_logits_far_from_zero(shift):
 
 
 @gpu
+@pytest.mark.parametrize("size,temp", [(3e3, 1.0), (1e6, 1.0), (1e4, 1e-4), (1e12, 1.0)])
+def test_logits_beyond_the_range_of_whole_numbers(size, temp):
+    """Logits of 1e8 to 1e26: the softmax is the largest logit's, losses are differences of logits."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    rng = np.random.default_rng(5)
+    T, d, V = 260, 64, 500
+    Xt, X = bf16(rng.standard_normal((T, d)) * size)
+    Et, E = bf16(rng.standard_normal((V, d)) * size)
+    target = rng.integers(0, V, T).astype(np.int32)
+    s = X @ E.T / temp
+    order = np.argsort(s, 1)
+    top = order[:, -1]
+    target[::4] = top[::4]
+    mag = (np.abs(X) @ np.abs(E).T).max(1) / temp
+    err = (d / 16 + 12) * 2 * U * mag      # of a logit, its scaling included
+    r = np.arange(T)
+    clear = s[r, top] - s[r, order[:, -2]] > 2 * err + 100
+    assert clear.mean() > 0.9
+    X, target, top, s, err, mag = X[clear], target[clear], top[clear], s[clear], err[clear], mag[clear]
+    T = len(X)
+    r = np.arange(T)
+    tt = torch.from_numpy(target).cuda()
+    Xc, Ec = torch.from_numpy(X).bfloat16().cuda(), Et.cuda()
+    if temp == 1.0:
+        loss, row, lse, dX, dE = ppu.ppu_head_xent(Xc, Ec, tt)
+    else:
+        loss, row, lse, dX, dE = ppu.ppu_head_distill(Xc, Ec, tt[:, None], torch.ones(T, 1, device="cuda"), temperature=temp)
+    assert (np.abs(lse.double().cpu().numpy() - s[r, top]) <= err + 4).all()
+    assert (np.abs(row.double().cpu().numpy() - (s[r, top] - s[r, target])) <= 2 * err + 8).all()
+    assert not row.cpu().numpy()[target == top].any()
+    # two powers, one factor and the result are rounded to bf16
+    want, size_of = (E[top] - E[target]) / T / temp, (np.abs(E[top]) + np.abs(E[target])) / T / temp
+    assert (np.abs(dX.double().cpu().numpy() - want) <= 4 * BF * size_of).all()
+    ds = np.zeros((T, V))
+    ds[r, top] += 1 / T / temp
+    np.add.at(ds, (r, target), -1 / T / temp)
+    one = np.zeros((T, V))
+    one[r, top] = one[r, target] = 1 / T / temp
+    one[target == top] = 0
+    assert (np.abs(dE.double().cpu().numpy() - ds.T @ X) <= 5 * BF * (one.T @ np.abs(X))).all()
+
+
+@gpu
 def test_rows_that_do_not_count_may_hold_anything():
     import torch
     from paper_2509_22418_b200 import ppu
