@@ -48,12 +48,12 @@ enum GemmEpilogue {
   // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_two only)
   EPI_OUT_BF16 = 8
 };
-// the columns of each row whose x is wanted itself (EPI_PIECES): ids [M][ld] ascending, k of them, behind them or
+// the columns of each row whose x is wanted itself, as {x - ref, ref} with the piece's ref (EPI_PIECES): ids [M][ld] ascending, k of them, behind them or
 // elsewhere negative; with k > 1, off [M][ld_off] = how many of a row's ids lie before each piece
 struct PieceEntries {
   const int32_t* ids; int64_t ld; int k;
   const uint8_t* off; int64_t ld_off;
-  float* x;                              // out [M][k]
+  float2* x;                             // out [M][k]
 };
 constexpr int PIECE = 64;               // columns of one softmax piece
 constexpr float PIECE_RANGE = 60.f;

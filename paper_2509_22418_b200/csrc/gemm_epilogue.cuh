@@ -404,16 +404,6 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
       if (id < nb || id >= nb + PIECE) id = -1;
     }
     tmem_ld_wait();
-    for (unsigned any = __ballot_sync(0xffffffffu, id >= 0); any; any = __ballot_sync(0xffffffffu, id >= 0)) {
-      const int col = __shfl_sync(0xffffffffu, id, __ffs(any) - 1);
-      const float x = __uint_as_float(tmem_ld1(t_row + c0 + (col - nb))) * p.piece_scale;
-      while (id == col) {                  // an id may be given several times
-        p.entries.x[(long long)m * p.entries.k + at] = x;
-        ++at;
-        id = at < end ? p.entries.ids[(long long)m * p.entries.ld + at] : -1;
-      }
-      __syncwarp();
-    }
     if (nb + PIECE > p.N) {                // columns past the vocabulary: nothing
 #pragma unroll
       for (int j = 0; j < PIECE; ++j)
@@ -425,11 +415,21 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
     mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     float top = mx[0] * p.piece_scale;
     if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
-    float less = top;
+    float less = top, off = 0.f;
     if (fabsf(top) > 16777216.f) {         // 2^24: the rounding of top would be an exponent of more than 1 (the largest is taken off first)
 #pragma unroll
       for (int j = 0; j < PIECE; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - mx[0]);
-      less = 0.f;
+      less = 0.f; off = mx[0];
+    }
+    for (unsigned any = __ballot_sync(0xffffffffu, id >= 0); any; any = __ballot_sync(0xffffffffu, id >= 0)) {
+      const int col = __shfl_sync(0xffffffffu, id, __ffs(any) - 1);
+      const float x = __uint_as_float(tmem_ld1(t_row + c0 + (col - nb)));
+      while (id == col) {                  // an id may be given several times
+        p.entries.x[(long long)m * p.entries.k + at] = make_float2(fmaf(x - off, p.piece_scale, -less), top);
+        ++at;
+        id = at < end ? p.entries.ids[(long long)m * p.entries.ld + at] : -1;
+      }
+      __syncwarp();
     }
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     uint32_t o[PIECE / 2];

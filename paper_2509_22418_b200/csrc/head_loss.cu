@@ -51,7 +51,7 @@ struct RowArgs {
   bf16* u; int64_t ldu;                  // powers of this chunk's rows; null without gradients
   const float2* stats; int64_t ld_pieces; int n_pieces;
   const bf16* X; int64_t ldx; int d, V;
-  const float* x;                        // the entries' x [rows][k]
+  const float2* x;                       // the entries' {x - ref, ref} [rows][k]
   int sorted;                            // tg is the chunk's own (sorted) copy: its rows are the chunk's
   int64_t row0;                          // first row of the chunk
   int T;
@@ -210,7 +210,8 @@ template <bool GRAD, int W>
 __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const RowArgs a, int rows) {
   constexpr int R = W == 1 ? 4 : 1, THREADS = W == 1 ? 128 : 32 * W, N = 32 * W;     // rows and threads of a block, threads of a row
   __shared__ int s_id[R][MAX_ENTRIES];
-  __shared__ float s_q[R][MAX_ENTRIES], s_l[R][MAX_ENTRIES], s_v[R][MAX_ENTRIES];
+  __shared__ float s_q[R][MAX_ENTRIES], s_v[R][MAX_ENTRIES];
+  __shared__ float2 s_x[R][MAX_ENTRIES];
   __shared__ float s_total[R], s_entropy[R], s_f[R], s_inv[R], s_sum[16];
   __shared__ int s_any[R], s_last, s_count[THREADS / 32];
   __shared__ Piece s_piece[W];
@@ -241,13 +242,13 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
     // the row's entries and their q
     if (warp == 0) {
       constexpr int PER = MAX_ENTRIES / 32;
-      float zs[PER], ex[PER]; int id[PER]; bool in[PER];
+      float zs[PER]; float2 ex[PER]; int id[PER]; bool in[PER];
       float top = -INFINITY;
       bool any = false;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int j = lane + 32 * i;
-        id[i] = -1; zs[i] = ex[i] = 0.f; in[i] = false;
+        id[i] = -1; zs[i] = 0.f; ex[i] = make_float2(0.f, 0.f); in[i] = false;
         if (j < k) {
           id[i] = a.tg.ids[te * a.tg.ld_ids + j];
           ex[i] = a.x[row * k + j];                 // (of an absent entry: whatever is there, and not used)
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           if (q != 0.f) entropy += q * (zs[i] - norm);
           total += q;
         }
-        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; s_l[g][j] = ex[i]; }
+        if (j < k) { s_id[g][j] = in[i] ? id[i] : -1; s_q[g][j] = q; s_x[g][j] = ex[i]; }
       }
       total = warp_sum(total); entropy = warp_sum(entropy);
       if (lane == 0) { s_total[g] = total; s_entropy[g] = entropy; s_any[g] = any; }
@@ -317,11 +318,11 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
     } else {
       __syncwarp();
     }
-    const float lse2 = all.m + log2f(all.s);        // base 2
-    if (tid == 0 && a.lse) a.lse[t] = lse2 * LN2;
-
-    // the reference of the row's powers: 0, or where that is too far from their sum, the sum itself
-    const float ref = fabsf(lse2) <= PIECE_RANGE ? 0.f : lse2;
+    // The row's powers are relative to the largest of its pieces' references (0 for ordinary logits) and add up to
+    // all.s: p = u / all.s.  What follows uses the two apart: far from 0 their sum, the log-sum-exp, is rounded to
+    // more than the powers are (at 2^20 to 2^-4, an error of 4 % of p).
+    const float ref = all.m, log_s = log2f(all.s);       // base 2
+    if (tid == 0 && a.lse) a.lse[t] = (ref + log_s) * LN2;
     bf16* ur = a.u + row * a.ldu;
     uint4* fx = GRAD && a.fx ? reinterpret_cast<uint4*>(a.fx + row * a.d) : nullptr;
     if (!s_any[g]) {                                // the row has no loss and no gradient
@@ -351,8 +352,10 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
       const float total = s_total[g];
       if (warp == 0) {
         float x = 0.f;
-        for (int j = lane; j < k; j += 32)
-          if (s_id[g][j] >= 0 && s_q[g][j] != 0.f) x = fmaf(s_q[g][j], lse2 - s_l[g][j], x);
+        for (int j = lane; j < k; j += 32) {
+          const float2 e = s_x[g][j];
+          if (s_id[g][j] >= 0 && s_q[g][j] != 0.f) x = fmaf(s_q[g][j], ((ref - e.y) - e.x) + log_s, x);
+        }
         x = warp_sum(x);
         if (lane == 0) {
           const float l = s_entropy[g] + x * LN2;
@@ -360,15 +363,16 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           a.weighted[t] = w * l;
         }
         if (GRAD) {
-          // what the entries' places are to hold: (p - q / Q) / 2^(ref - lse2).  With p = exp(x): (exp(x) - 1) + (1 - q / Q)
+          // what the entries' places are to hold: (p - q / Q) all.s.  With p = exp(x): (exp(x) - 1) + (1 - q / Q)
           // keeps its digits where p is next to 1.  An id given twice: its first entry stands for all.
           for (int j = lane; j < k; j += 32) {
             const int id = s_id[g][j];
+            const float2 e = s_x[g][j];
             float v = 0.f;
             if (id >= 0 && total != 0.f && !(j > 0 && s_id[g][j - 1] == id)) {
               float q = 0.f;
               for (int i = j; i < k && s_id[g][i] == id; ++i) q += s_q[g][i];
-              v = (expm1f((s_l[g][j] - lse2) * LN2) + (total - q) / total) * exp2f(lse2 - ref);
+              v = (expm1f(((e.y - ref) + e.x - log_s) * LN2) + (total - q) / total) * all.s;
             }
             s_v[g][j] = v;
           }
@@ -399,7 +403,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           const int from = best < INFINITY ? __ffs(who) - 1 : 31;
           const float use = __shfl_sync(0xffffffffu, ratio, from), use_inv = __shfl_sync(0xffffffffu, inv, from);
           if (lane == 0) {
-            const float f = w * a.tg.inv_temp * total * exp2f(ref - lse2) * use;
+            const float f = w * a.tg.inv_temp * total * exp2f(-log_s) * use;
             s_f[g] = f; s_inv[g] = use_inv;
             a.factor[row] = f;
           }
@@ -418,7 +422,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
             for (int q = 0; q < 8; ++q) v[q] *= f;
             fx[i] = pack8(v);
           }
-        if (!plain || ref != 0.f) {                 // (seldom) powers that are relative to something else
+        if (!plain) {                               // (seldom) powers that are relative to something else
           for (int i = tid; i < a.n_pieces; i += N) {
             const float2 v = st[i];
             if (v.x != ref && v.y != 0.f) scale_piece(ur + (int64_t)i * PIECE, exp2f(v.x - ref));
@@ -549,7 +553,7 @@ Plan make_plan(int T, int d, int V, int want, int chunk_rows, int k) {
   p.off_factor = take(4ll * p.chunk);
   p.off_stats = take(8ll * p.chunk * p.n_pieces);
   p.ld_off = round_up(p.n_pieces + 1, 4);
-  p.off_x = take(4ll * p.chunk * k);
+  p.off_x = take(8ll * p.chunk * k);
   p.off_ids = take(k > 1 ? 4ll * p.chunk * k : 0);
   p.off_z = take(k > 1 ? 4ll * p.chunk * k : 0);
   p.off_before = take(k > 1 ? p.chunk * p.ld_off : 0);
@@ -665,7 +669,7 @@ int run_head(const HeadCall& c) {
   r.scale2 = LOG2E / c.temp; r.weight = c.weight; r.count = by_rows ? nullptr : count;
   r.row_loss = c.row_loss; r.lse = c.lse; r.weighted = (float*)(ws + p.off_weighted); r.factor = factor; r.fx = fx;
   r.done = done; r.loss = c.loss; r.flags = c.flags;
-  float* ex = (float*)(ws + p.off_x);
+  float2* ex = (float2*)(ws + p.off_x);
   int32_t* sorted_ids = (int32_t*)(ws + p.off_ids);
   float* sorted_z = (float*)(ws + p.off_z);
   uint8_t* before = ws + p.off_before;
