@@ -14,9 +14,11 @@
 // bounds them.  A "unit" of LANES threads owns a contiguous range of rows; a thread owns CH chunks of 4
 // columns of all of them (16 bytes of fp32, 8 of bf16: neighbours are adjacent in both).  So gains,
 // shifts and gate stay in registers over the rows, and the parameter sums of the backward pass are
-// running sums in registers, written once per unit and added in a fixed order by a second small kernel
-// (no atomics).  Rows arrive through a ring of cp.async copies in shared memory: a unit works on one row at a
-// time, two to four sums over its threads one after the other, and loads for it would wait as long again.
+// running sums in registers, which the units of a block add up in shared memory and a second small kernel over
+// the blocks, in a fixed order (no atomics).  (With a unit's sums written by itself, 16384 x 64 took 17.7 us where
+// it takes 9.5, and 2041 x 768 with 13 gates 14.1 where it takes 11.6.)
+// Rows arrive through a ring of cp.async copies in shared memory: a unit works on one row at a time, two to four
+// sums over its threads one after the other, and loads for it would wait as long again.
 // LANES is a compile-time constant: with the loops over lanes and warps left to run time the same
 // kernel issued 675 instructions per warp and row and took 84 us at 8192 x 2048 where it takes 38.
 #include <algorithm>
@@ -43,9 +45,10 @@ struct NormArgs {
   float scale, eps;
   int T, d, gate_rows, layer;
   int deal_rows;                     // rows dealt to the units as one (1, or the rows of a group)
-  int units;
+  int units, blocks;
   int per_group;                     // units that share a group of gate rows (0: units own whole groups / plain rows)
-  float* partial;                    // [5][units][d]: dg1, db1, dg2, db2, dgate
+  int join_gate;                     // the units of a block share a group
+  float* partial;                    // [4][blocks][d]: dg1, db1, dg2, db2; then dgate: [blocks or units][d]
   float* dgate;
 };
 
@@ -70,9 +73,11 @@ __device__ __forceinline__ uint2 to_bf4(const float* f) {
 __device__ __forceinline__ void from_f4(const float4& v, float* f) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
 __device__ __forceinline__ float4 to_f4(const float* f) { return make_float4(f[0], f[1], f[2], f[3]); }
 
-// how the threads of a block make up units
-template <int LANES> struct Layout {
-  static constexpr int UNITS = LANES <= 32 ? 128 / LANES : LANES <= 128 ? (LANES == 96 ? 1 : 128 / LANES) : 1;   // units in a block
+// Units of a block: about 128 threads forward, 256 backward, where they share their sums (with 512 throughout 16
+// rows of 2048 take 7.0 us for 5.5), or 480 of 96, five units to an SM.
+constexpr int units_of(int lanes, bool bwd) { return !bwd ? (lanes <= 128 ? 128 / lanes : 1) : lanes == 96 ? 5 : lanes <= 128 ? 256 / lanes : 1; }
+template <int LANES, bool BWD> struct Layout {
+  static constexpr int UNITS = units_of(LANES, BWD);
   static constexpr int BLOCK = LANES * UNITS;
   static constexpr int WARPS = LANES > 32 ? LANES / 32 : 1;
 };
@@ -81,7 +86,7 @@ template <int LANES> struct Layout {
 // memory and the unit's own named barrier.  Two buffers in turn: a thread that is back for the next sum
 // writes the other one, and the one after that lies behind a barrier that all readers of this have passed.
 template <int LANES, int N> struct UnitSum {
-  static constexpr int W = Layout<LANES>::WARPS;
+  static constexpr int W = LANES > 32 ? LANES / 32 : 1;
   float* buf;                       // [2][W][N] of this unit
   int bar, lane, warp, turn;
   __device__ __forceinline__ void operator()(float (&v)[N]) {
@@ -112,11 +117,13 @@ struct Unit {
   int lo, hi;                       // rows
   int group;                        // gate row of all of them (units that share a group)
 };
-template <int LANES>
+template <int LANES, bool BWD>
 __device__ __forceinline__ Unit my_unit(const NormArgs& a) {
   Unit u;
   u.tid = threadIdx.x % LANES;
-  u.unit = blockIdx.x * Layout<LANES>::UNITS + threadIdx.x / LANES;
+  // (rows that are not shared out by groups go to all blocks before a block gets a second unit's)
+  if (BWD && a.per_group == 0) u.unit = blockIdx.x + threadIdx.x / LANES * a.blocks;
+  else u.unit = blockIdx.x * Layout<LANES, BWD>::UNITS + threadIdx.x / LANES;
   u.group = u.lo = u.hi = 0;
   if (u.unit >= a.units) return u;
   if (a.per_group > 0) {            // a share of one group's rows
@@ -158,13 +165,13 @@ template <bool BWD, int GATE> struct Ring {
 
 // GATE: 0 none, 1 one row for all rows, 2 read with each row
 template <int LANES, int GATE>
-__global__ void __launch_bounds__(Layout<LANES>::BLOCK, FWD_THREADS / Layout<LANES>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(Layout<LANES, false>::BLOCK, FWD_THREADS / Layout<LANES, false>::BLOCK) norm_gate_fwd_kernel(const NormArgs a) {
   pdl_wait(); pdl_trigger();
-  constexpr int BLOCK = Layout<LANES>::BLOCK;
+  constexpr int BLOCK = Layout<LANES, false>::BLOCK;
   using R = Ring<false, GATE>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float s_sum[Layout<LANES>::UNITS][2 * Layout<LANES>::WARPS];
-  const Unit u = my_unit<LANES>(a);
+  __shared__ float s_sum[Layout<LANES, false>::UNITS][2 * Layout<LANES, false>::WARPS];
+  const Unit u = my_unit<LANES, false>(a);
   const int slot = threadIdx.x / LANES;
   UnitSum<LANES, 1> sum{s_sum[slot], 1 + slot, (int)threadIdx.x & 31, u.tid >> 5, 0};
   bool on[CH];
@@ -275,13 +282,13 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK, FWD_THREADS / Layout<LAN
 
 // GATE: 0 none, 1 one row for all of the unit's rows, 2 read with each row, its gradient written at the end of each group
 template <int LANES, int GATE>
-__global__ void __launch_bounds__(Layout<LANES>::BLOCK, BWD_THREADS / Layout<LANES>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(Layout<LANES, true>::BLOCK, BWD_THREADS / Layout<LANES, true>::BLOCK) norm_gate_bwd_kernel(const NormArgs a) {
   pdl_wait(); pdl_trigger();
-  constexpr int BLOCK = Layout<LANES>::BLOCK;
+  constexpr int BLOCK = Layout<LANES, true>::BLOCK;
   using R = Ring<true, GATE>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float s_sum[Layout<LANES>::UNITS][2 * 2 * Layout<LANES>::WARPS];
-  const Unit u = my_unit<LANES>(a);
+  __shared__ float s_sum[Layout<LANES, true>::UNITS][2 * 2 * Layout<LANES, true>::WARPS];
+  const Unit u = my_unit<LANES, true>(a);
   const int slot = threadIdx.x / LANES;
   UnitSum<LANES, 2> sum{s_sum[slot], 1 + slot, (int)threadIdx.x & 31, u.tid >> 5, 0};
   bool on[CH];
@@ -408,15 +415,19 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK, BWD_THREADS / Layout<LAN
         }
       }
   }
-  if (u.unit >= a.units) return;
-  const int64_t plane = (int64_t)a.units * a.d;
+  // the sums of the block's units, added up in order: across a warp's by shuffles, then through shared memory
+  constexpr int PLANES = GATE == 1 ? 5 : 4, WIDE = LANES * CH, PARTS = LANES < 32 ? BLOCK / 32 : Layout<LANES, true>::UNITS;
+  static_assert(PLANES * PARTS * WIDE * 16 <= R::BYTES * R::STAGES * BLOCK, "sums in the ring's place");
+  const int part = LANES < 32 ? (int)threadIdx.x >> 5 : slot;
+  const bool writes = LANES >= 32 || (threadIdx.x & 31) < LANES;
+  float4* joined = reinterpret_cast<float4*>(smem);          // [plane][part][column / 4]
+  if (PARTS > 1) __syncthreads();                            // (the ring has been read)
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if (!on[c]) continue;
-    const int col = 4 * (u.tid + LANES * c);
-    float* p = a.partial + (int64_t)u.unit * a.d + col;
-    if (GATE == 1) {
-      float gt[4], g1[4], b1[4] = {}, o[4];
+    float o[4] = {};
+    if (GATE == 1 && on[c]) {
+      const int col = 4 * (u.tid + LANES * c);
+      float gt[4], g1[4], b1[4] = {};
       from_f4(*reinterpret_cast<const float4*>(a.gate + (int64_t)u.group * a.d + col), gt);
       from_f4(*reinterpret_cast<const float4*>(a.g1 + col), g1);
       if (a.b1) from_f4(*reinterpret_cast<const float4*>(a.b1 + col), b1);
@@ -426,20 +437,41 @@ __global__ void __launch_bounds__(Layout<LANES>::BLOCK, BWD_THREADS / Layout<LAN
         A[c][j] *= gt[j];
         B[c][j] *= gt[j];
       }
-      *reinterpret_cast<float4*>(p + 4 * plane) = to_f4(o);
+      if (!a.join_gate && u.unit < a.units) *reinterpret_cast<float4*>(a.partial + ((int64_t)4 * a.blocks + u.unit) * a.d + col) = to_f4(o);
     }
-    *reinterpret_cast<float4*>(p) = to_f4(GATE == 2 ? PA[c] : A[c]);
-    *reinterpret_cast<float4*>(p + plane) = to_f4(GATE == 2 ? PB[c] : B[c]);
-    *reinterpret_cast<float4*>(p + 2 * plane) = to_f4(C[c]);
-    *reinterpret_cast<float4*>(p + 3 * plane) = to_f4(D[c]);
+#pragma unroll
+    for (int q = 0; q < PLANES; ++q) {
+      float (&v)[4] = q == 0 ? (GATE == 2 ? PA[c] : A[c]) : q == 1 ? (GATE == 2 ? PB[c] : B[c]) : q == 2 ? C[c] : q == 3 ? D[c] : o;
+#pragma unroll
+      for (int w = LANES; w < 32; w *= 2)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += __shfl_xor_sync(0xffffffffu, v[j], w);
+      if (PARTS == 1) {                                      // a block is one unit
+        if (on[c] && (q < 4 || a.join_gate))
+          *reinterpret_cast<float4*>(a.partial + ((int64_t)q * a.blocks + blockIdx.x) * a.d + 4 * (u.tid + LANES * c)) = to_f4(v);
+      } else if (writes) joined[(q * PARTS + part) * WIDE + u.tid + LANES * c] = to_f4(v);
+    }
+  }
+  if (PARTS == 1) return;
+  __syncthreads();
+  const int n4 = a.d / 4, planes = GATE == 1 && a.join_gate ? 5 : 4;
+  for (int i = threadIdx.x; i < planes * n4; i += BLOCK) {
+    const int q = i / n4, c4 = i - q * n4;
+    float4 v = joined[q * PARTS * WIDE + c4];
+#pragma unroll
+    for (int w = 1; w < PARTS; ++w) {
+      const float4 x = joined[(q * PARTS + w) * WIDE + c4];
+      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    *reinterpret_cast<float4*>(a.partial + ((int64_t)q * a.blocks + blockIdx.x) * a.d + 4 * c4) = v;
   }
 }
 
-// parameter gradients from the units' partial sums: blockIdx.y = 0..3 the norms' gains and shifts over
-// all units, 4 + g the gate's row g over the units of its group.  A block takes 128 columns (4 to a lane), a warp
-// adds a 32nd of the units in order, and the 32 sums are added in order.
+// parameter gradients from the blocks' partial sums: blockIdx.y = 0..3 the norms' gains and shifts over
+// all blocks, 4 + g the gate's row g over its group's parts.  A block takes 128 columns (4 to a lane), a warp
+// adds a 32nd of the parts in order, and the 32 sums are added in order.
 struct ParamOut { float* out[4]; float* dgate; };
-__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* partial, const ParamOut po, int units, int per_group, int d) {
+__global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* partial, const ParamOut po, int blocks, int group_parts, int d) {
   pdl_wait(); pdl_trigger();
   __shared__ float4 sh[32][32];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -447,8 +479,9 @@ __global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* par
   const int which = min((int)blockIdx.y, 4), g = (int)blockIdx.y - 4;
   float* out = which == 0 ? po.out[0] : which == 1 ? po.out[1] : which == 2 ? po.out[2] : which == 3 ? po.out[3] : po.dgate + (int64_t)g * d;
   if (!out) return;
-  const int n = which < 4 ? units : per_group, first = which < 4 ? 0 : g * per_group;
-  const float* p = partial + ((int64_t)which * units + first) * d + c;
+  const int n = which < 4 ? blocks : group_parts;
+  const int64_t first = which < 4 ? 0 : (int64_t)g * group_parts;
+  const float* p = partial + ((int64_t)which * blocks + first) * d + c;
   const int per = (n + 31) / 32, b0 = w * per, b1 = min(n, b0 + per);
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < d) {
@@ -472,7 +505,7 @@ __global__ void __launch_bounds__(1024) norm_gate_params_kernel(const float* par
 // ---- host ---------------------------------------------------------------------------------------
 constexpr int SMS = 148;                      // work is split for a B200 (also where sizes are asked without a device)
 
-struct Shape { int lanes, units, per_group, gate_mode; size_t partial; };
+struct Shape { int lanes, slots, units, blocks, per_group, join_gate, gate_mode; size_t partial; };
 
 // threads of a unit: the fewest that hold a row, of the sizes that are compiled
 int lanes_for(int d) {
@@ -481,23 +514,30 @@ int lanes_for(int d) {
 }
 // rows are dealt to as many threads per SM as are resident there
 Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
-  Shape s;
+  Shape s = {};
   s.lanes = lanes_for(d);
-  const int threads = backward ? BWD_THREADS : FWD_THREADS;
-  const int64_t target = std::min<int64_t>(16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (threads / s.lanes)));
   const int64_t groups = has_gate ? ((int64_t)T + gate_rows - 1) / gate_rows : 1;
-  s.per_group = 0;
   s.gate_mode = !has_gate ? 0 : groups == 1 ? 1 : 2;
-  if (backward && has_gate && groups < target) {       // several units to a group
-    s.gate_mode = 1;
-    const int64_t rows = std::min<int64_t>(gate_rows, T);
-    s.per_group = (int)std::max<int64_t>(1, std::min<int64_t>(rows, target / groups));
-    s.units = (int)(groups * s.per_group);
-  } else {
-    // whole groups (backward, more groups than units) or plain rows
-    s.units = (int)std::min<int64_t>(target, backward && has_gate ? groups : T);
+  if (!backward) {
+    s.units = (int)std::min<int64_t>({T, 16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (FWD_THREADS / s.lanes))});
+    return s;
   }
-  s.partial = backward ? 5 * (size_t)s.units * d * 4 : 0;
+  const int64_t slots = units_of(s.lanes, true), target = SMS * (BWD_THREADS / s.lanes);     // units of a block, of the machine
+  if (has_gate && groups < target) {                   // several units to a group, whole blocks of them where it has that many
+    s.gate_mode = 1;
+    int64_t per = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(gate_rows, T), target / groups));
+    s.join_gate = per % slots <= per / 8;              // (else too many units would be left without rows)
+    if (s.join_gate) per = per / slots * slots;
+    s.per_group = (int)per;
+    s.units = (int)(groups * per);
+    s.blocks = (int)((s.units + slots - 1) / slots);
+  } else {                                             // whole groups (more groups than units) or plain rows
+    const int64_t n = has_gate ? groups : T;
+    s.blocks = (int)std::min<int64_t>(target / slots, n);
+    s.units = (int)(s.blocks * std::min<int64_t>(slots, (n + s.blocks - 1) / s.blocks));
+  }
+  s.slots = (int)slots;
+  s.partial = (4 * (size_t)s.blocks + (s.gate_mode == 1 ? (s.join_gate ? s.blocks : s.units) : 0)) * d * 4;
   return s;
 }
 
@@ -524,7 +564,7 @@ bool misaligned(std::initializer_list<const void*> ps) {
 
 template <int LANES, int GATE, bool BWD>
 int launch_norm(const NormArgs& a, cudaStream_t st) {
-  using L = Layout<LANES>;
+  using L = Layout<LANES, BWD>;
   using R = Ring<BWD, GATE>;
   constexpr int bytes = R::BYTES * R::STAGES * L::BLOCK;
   static_assert(bytes <= 220 * 1024, "shared memory of a block");
@@ -533,7 +573,7 @@ int launch_norm(const NormArgs& a, cudaStream_t st) {
   if constexpr (BWD) kernel = norm_gate_bwd_kernel<LANES, GATE>;
   else kernel = norm_gate_fwd_kernel<LANES, GATE>;
   if (!ppu_set_smem_once(attr, kernel, bytes)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
-  CUDA_OK(ppu_launch_dependent(kernel, (a.units + L::UNITS - 1) / L::UNITS, L::BLOCK, bytes, st, a));
+  CUDA_OK(ppu_launch_dependent(kernel, BWD ? a.blocks : (a.units + L::UNITS - 1) / L::UNITS, L::BLOCK, bytes, st, a));
   return PPU_OK;
 }
 template <int LANES, bool BWD>
@@ -609,11 +649,12 @@ extern "C" int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void
   a.dh = (const bf16*)dh; a.dr = dr_out; a.y = (const bf16*)y; a.r = r_out; a.stats = (float4*)stats;
   a.gate = gate; a.g1 = post_gain; a.b1 = post_shift; a.g2 = pre_gain; a.dy = (bf16*)dy; a.dr_out = dr;
   a.scale = res_scale; a.T = T; a.d = d; a.gate_rows = gate ? gate_rows : 1; a.layer = kind == PPU_NORM_LAYER; a.units = s.units;
-  a.deal_rows = s.gate_mode == 2 ? gate_rows : 1; a.per_group = s.per_group; a.partial = (float*)workspace; a.dgate = dgate;
+  a.deal_rows = s.gate_mode == 2 ? gate_rows : 1; a.per_group = s.per_group; a.blocks = s.blocks; a.join_gate = s.join_gate; a.partial = (float*)workspace; a.dgate = dgate;
   const int rc2 = dispatch<true>(a, s, st);
   if (rc2) return rc2;
   const int groups = s.gate_mode == 1 ? s.units / s.per_group : 0;      // gate rows still to be summed
+  const int parts = s.join_gate ? s.per_group / s.slots : s.per_group;
   const ParamOut po = {{dpost_gain, dpost_shift, dpre_gain, dpre_shift}, dgate};
-  CUDA_OK(ppu_launch_dependent(norm_gate_params_kernel, dim3((d + 127) / 128, 4 + groups), 1024, 0, st, a.partial, po, s.units, s.per_group, d));
+  CUDA_OK(ppu_launch_dependent(norm_gate_params_kernel, dim3((d + 127) / 128, 4 + groups), 1024, 0, st, a.partial, po, s.blocks, parts, d));
   return PPU_OK;
 }
