@@ -519,7 +519,7 @@ Shape make_shape(int T, int d, int has_gate, int gate_rows, bool backward) {
   const int64_t groups = has_gate ? ((int64_t)T + gate_rows - 1) / gate_rows : 1;
   s.gate_mode = !has_gate ? 0 : groups == 1 ? 1 : 2;
   if (!backward) {
-    s.units = (int)std::min<int64_t>({T, 16 * SMS, std::max<int64_t>(SMS, (int64_t)SMS * (FWD_THREADS / s.lanes))});
+    s.units = (int)std::min<int64_t>(T, (int64_t)SMS * (FWD_THREADS / s.lanes));
     return s;
   }
   const int64_t slots = units_of(s.lanes, true), target = SMS * (BWD_THREADS / s.lanes);     // units of a block, of the machine
