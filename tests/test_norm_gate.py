@@ -128,7 +128,7 @@ CASES = [
     (5000, 8, 3),           # the same, a last group of two rows
     (257, 136, None), (300, 256, 300), (1500, 264, 7),
     (333, 768, 64), (1001, 1032, 1), (130, 2048, 130), (400, 2056, 2), (97, 4096, 10), (1, 4096, None),
-    (20000, 8, 1), (1301, 264, 1), (1640, 256, 10), (3000, 32, None), (1999, 520, 1),
+    (20000, 8, 1), (1301, 264, 1), (1640, 256, 10), (3000, 32, None), (1999, 520, 1), (350, 2104, 90), (161, 2568, None),
 ]
 
 
