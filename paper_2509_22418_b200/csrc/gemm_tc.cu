@@ -200,13 +200,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * BN);
-      if constexpr (TWO)
-        drain_two(*params(sec), store_buf, w.m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
-      else
-        drain_mode<MODE>(p, store_buf, w.m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(tempty_bar(acc));
+      drain<MODE>(*params(sec), store_buf, w.m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane, [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(tempty_bar(acc));
+      });
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
   }

@@ -300,16 +300,14 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(acc * PAIR_BN);
-      if constexpr (TWO)
-        drain_two(*params(sec), store_buf, m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
-      else
-        drain_mode<MODE>(p, store_buf, m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (MODE == DRAIN_COLS) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
-        else mbar_arrive_cluster_cta(map_to_rank(tempty_bar(acc), 0));
-      }
+      drain<MODE>(*params(sec), store_buf, m0, w.n0, w.sp, t_acc, quarter, c_begin, c_end, lane, [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (MODE == DRAIN_COLS) mbar_arrive_cluster(map_to_rank(tempty_bar(acc), 0));
+          else mbar_arrive_cluster_cta(map_to_rank(tempty_bar(acc), 0));
+        }
+      });
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
     }
   }
