@@ -10,7 +10,7 @@ constexpr int BM = 128;
 constexpr int BK = 64;            // 64 bf16 = 128 bytes = one swizzle row
 constexpr int UMMA_K = 16;
 constexpr int EPI_WARPS = 8;      // two per TMEM lane quarter, each draining half the columns
-constexpr int GEMM_THREADS = 64 + 32 * EPI_WARPS;  // warp 0: TMA, warp 1: MMA + TMEM owner, then epilogue
+// (a block: warp 0: TMA, warp 1: MMA + TMEM owner, then epilogue)
 
 // hardware tanh (relative error about 2^-11, below the bf16 rounding of the stored result)
 __device__ __forceinline__ float tanh_fast(float x) {
@@ -89,7 +89,7 @@ struct TcParams {
   PieceEntries entries;
   const float* row_scale; unsigned* zero_word;
   int dependent;   // launched as a programmatic dependent
-  // Epilogue warps.  0: all eight drain each tile, half of its columns each.  1: four drain one accumulator, four the
+  // Epilogue warps.  0: all drain each tile, a part of its columns each.  1: half of them drain one accumulator, half the
   // other, so that one tile is read from tensor memory (600 cycles of latency for 64 columns) while the other
   // is stored (900 cycles of the load/store pipe): for blocks that work several tiles (dE of
   // 24 x 32768 x 768: 18.7 -> 16.7 us, of 90 x 6300 x 360: 11 -> 8).
@@ -100,7 +100,11 @@ struct TcParams {
 // those that have instantiations of their own: drain_cols keeps its registers, and these have 32 KB of
 // shared memory behind the operand stages, through which they store 64-column groups
 enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_TWO = 2 };
-constexpr int STORE_BYTES = 32 * 128;                      // a warp's 32 rows x 64 bf16 columns
+// DRAIN_PIECES has twice the warps: its 64 columns take a warp 1500 cycles, of which the exponentials are 512 of the SM
+// quarter's unit for them (logits of 4096 x 32768 x 64: 110 us with 8 warps, 88 with 16; x 768: 160 and 153).
+constexpr int epi_warps(int mode) { return mode == DRAIN_PIECES ? 2 * EPI_WARPS : EPI_WARPS; }
+constexpr int gemm_threads(int mode) { return 64 + 32 * epi_warps(mode); }
+constexpr int store_bytes(int mode) { return mode == DRAIN_PIECES ? 32 * 64 : 32 * 128; }    // a warp's 32 rows x 32 or 64 bf16 columns
 template <int MODE> struct Second {};
 // DRAIN_TWO: a launch works the units of two products (launch_gemm_tc_two), the one with the longer units
 // first; A's order may differ between the two.  This holds the second product.
@@ -126,7 +130,18 @@ __device__ __forceinline__ int two_unit(int i, int b, int n, int units, int unit
   return v < units2 ? units + v : NONE;
 }
 
-template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : EPI_WARPS * STORE_BYTES; }
+template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : epi_warps(MODE) * store_bytes(MODE); }
+
+// Columns of a tile of bn that a set of four warps (one for each quarter of the rows) drains: an equal part, of the whole
+// tile or, where the sets take turns, of every other tile's; pieces are not divided, so sets may be left without.
+template <int MODE> __device__ __forceinline__ void set_columns(int set, int alternate, int bn, int& begin, int& end) {
+  constexpr int SETS = epi_warps(MODE) / 4;
+  const int sub = alternate ? set % (SETS / 2) : set;
+  int cols = alternate ? bn / (SETS / 2) : bn / SETS;
+  if (MODE == DRAIN_PIECES && cols < PIECE) cols = PIECE;
+  begin = sub * cols;
+  end = begin + cols < bn ? begin + cols : bn;
+}
 
 // host side (gemm_tc.cu / gemm_tc_pair.cu)
 bool encode_map(CUtensorMap* map, const bf16* base, long long ld, bool kmajor, int rows, int K, int box_rows,
@@ -344,26 +359,30 @@ __device__ __forceinline__ float ex2_fast(float x) {
   return y;
 }
 
-// A warp's 32 rows x 64 columns, packed by its lanes (one row each, 32 words), to global memory through
-// its 4 KB of shared memory, so that a store covers four rows' whole 128-byte lines.  (From the registers, a lane
-// 32 bytes of its own row at a time, a store touches 32 lines: 2304 x 32000 x 768 took 95 us against 70 without
-// the store.  By TMA from the same shared memory it took 90: the buffer is free again only when the copy has
-// read it.  This way 85; the dE of 256 x 2048 x 32768, all stores, 73 us instead of 111 by TMA.)  Row r of the buffer has its 16-byte pieces in the places j ^ (r & 7): no bank conflicts
-// either way.  rows, cols: of the output, from here on.
+// A warp's 32 rows x COLS (64 or 32) columns, packed by its lanes (one row each), to global memory through its
+// shared memory, so that a store covers four rows' whole 128-byte lines, or eight rows' halves.  (From the
+// registers, a lane 32 bytes of its own row at a time, a store touches 32 lines: 2304 x 32000 x 768 took 95 us
+// against 70 without the store and 85 this way.  By TMA from the same shared memory it took 90: the buffer is free
+// again only when the copy has read it; the dE of 256 x 2048 x 32768, all stores, 111 us by TMA and 73 this way.)
+// Row r of the buffer has its 16-byte pieces in other places than its neighbours: no bank conflicts either
+// way.  rows, cols: of the output, from here on.
+template <int COLS>
 __device__ __forceinline__ void store_group(bf16* out, long long ld, uint32_t buf, const uint32_t* o, int rows, int cols, int lane) {
+  constexpr int P = COLS / 8, ROWS = 32 / P;     // pieces of a row, rows of a store
+  auto place = [](int r, int j) { return (uint32_t)(r * COLS * 2 + ((j ^ (COLS == 64 ? r & 7 : r >> 1 & 3)) << 4)); };
   __syncwarp();                     // (the group before has been read)
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(o[4 * j]),
-                 "r"(o[4 * j + 1]), "r"(o[4 * j + 2]), "r"(o[4 * j + 3])
+  for (int j = 0; j < P; ++j)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + place(lane, j)), "r"(o[4 * j]), "r"(o[4 * j + 1]), "r"(o[4 * j + 2]),
+                 "r"(o[4 * j + 3])
                  : "memory");
   __syncwarp();
-  const int piece = lane & 7;
+  const int piece = lane % P;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = 4 * i + (lane >> 3);
+  for (int i = 0; i < P; ++i) {
+    const int r = ROWS * i + lane / P;
     uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(buf + r * 128 + ((piece ^ (r & 7)) << 4)) : "memory");
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(buf + place(r, piece)) : "memory");
     if (r < rows && 8 * piece < cols) *reinterpret_cast<uint4*>(out + r * ld + 8 * piece) = v;
   }
 }
@@ -381,19 +400,20 @@ __device__ __forceinline__ void store_group(bf16* out, long long ld, uint32_t bu
 // The entries' own x are taken from tensor memory a column at a time: a warp's 32 rows have two in a
 // piece with 32 entries in 32768 columns.  (As dot products in the row kernel they were a gather of 4 KB of E
 // for each entry: 106 of 1200 us at 4096 x 2048 x 32768.)
+// The registers of 16 warps hold 32 columns at a time: the halves are read for the largest first, the
+// second half then worked and the first read again.
 template <typename F>
 __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, int m0, int n0,
                                              uint32_t t_acc, int quarter, int c_begin, int c_end, int lane, F release) {
   const int mw = m0 + quarter * 32, m = mw + lane;
   const uint32_t t_row = t_acc + ((uint32_t)(quarter * 32) << 16);
-  if (n0 + c_begin >= p.N || mw >= p.M) { release(); return; }
+  if (c_begin >= c_end || n0 + c_begin >= p.N || mw >= p.M) { release(); return; }
 #pragma unroll 1
   for (int c0 = c_begin; c0 < c_end; c0 += PIECE) {
     const int nb = n0 + c0;
     if (nb >= p.N) break;                  // warp-uniform
-    uint32_t r[PIECE];
+    uint32_t r[32];
     tmem_ld32(t_row + c0, r);
-    tmem_ld32(t_row + c0 + 32, r + 32);
     int at = 0, end = 0, id = -1;          // this row's entries in the piece, and the first one's column
     if (m < p.M) {
       if (p.entries.k > 1) {
@@ -405,24 +425,30 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
       if (at < end) id = p.entries.ids[(long long)m * p.entries.ld + at];
       if (id < nb || id >= nb + PIECE) id = -1;
     }
-    tmem_ld_wait();
-    if (nb + PIECE > p.N) {                // columns past the vocabulary: nothing
+    auto arrived = [&](int h) {
+      tmem_ld_wait();
+      if (nb + 32 * h + 32 > p.N) {        // columns past the vocabulary: nothing
 #pragma unroll
-      for (int j = 0; j < PIECE; ++j)
-        if (nb + j >= p.N) r[j] = 0xff800000u;
-    }
+        for (int j = 0; j < 32; ++j)
+          if (nb + 32 * h + j >= p.N) r[j] = 0xff800000u;
+      }
+    };
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    auto largest = [&] {
 #pragma unroll
-    for (int j = 0; j < PIECE; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
+      for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
+    };
+    arrived(0);
+    largest();
+    tmem_ld32(t_row + c0 + 32, r);
+    arrived(1);
+    largest();
     mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     float top = mx[0] * p.piece_scale;
     if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
     float less = top, off = 0.f;
-    if (fabsf(top) > 16777216.f) {         // 2^24: the rounding of top would be an exponent of more than 1 (the largest is taken off first)
-#pragma unroll
-      for (int j = 0; j < PIECE; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - mx[0]);
-      less = 0.f; off = mx[0];
-    }
+    const bool far = fabsf(top) > 16777216.f;
+    if (far) { less = 0.f; off = mx[0]; }  // 2^24: the rounding of top would be an exponent of more than 1 (the largest is taken off first)
     for (unsigned any = __ballot_sync(0xffffffffu, id >= 0); any; any = __ballot_sync(0xffffffffu, id >= 0)) {
       const int col = __shfl_sync(0xffffffffu, id, __ffs(any) - 1);
       const float x = __uint_as_float(tmem_ld1(t_row + c0 + (col - nb)));
@@ -433,21 +459,31 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
       }
       __syncwarp();
     }
-    if (c0 + PIECE >= c_end || nb + PIECE >= p.N) release();
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    uint32_t o[PIECE / 2];
+    auto powers = [&](int h) {
+      if (far) {
 #pragma unroll
-    for (int j = 0; j < PIECE / 2; ++j) {
-      const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -less));
-      const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -less));
-      sum[(2 * j) & 3] += e0;
-      sum[(2 * j + 1) & 3] += e1;
-      o[j] = pack2_bf16(e0, e1);
-    }
+        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - off);
+      }
+      uint32_t o[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -less));
+        const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -less));
+        sum[(2 * j) & 3] += e0;
+        sum[(2 * j + 1) & 3] += e1;
+        o[j] = pack2_bf16(e0, e1);
+      }
+      // (columns up to the next multiple of 64 belong to the row too)
+      if (p.C) store_group<32>((bf16*)p.C + (long long)mw * p.ldc + nb + 32 * h, p.ldc, buf, o, p.M - mw, 32, lane);
+    };
+    powers(1);
+    tmem_ld32(t_row + c0, r);
+    arrived(0);
+    if (c0 + PIECE >= c_end || nb + PIECE >= p.N) release();
+    powers(0);
     if (m < p.M)
       p.piece_stats[(long long)m * p.ld_pieces + nb / PIECE] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
-    // (columns up to the next multiple of 64 belong to the row too)
-    if (p.C) store_group((bf16*)p.C + (long long)mw * p.ldc + nb, p.ldc, buf, o, p.M - mw, PIECE, lane);
   }
 }
 
@@ -487,7 +523,7 @@ __device__ __forceinline__ void drain_out_bf16(const TcParams& p, uint32_t buf, 
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[16 * h + j] = pack2_bf16(f * __uint_as_float(r[2 * j]), f * __uint_as_float(r[2 * j + 1]));
     }
-    store_group((bf16*)p.C + (long long)mw * p.ldc + nb, p.ldc, buf, o, p.M - mw, p.N - nb, lane);
+    store_group<64>((bf16*)p.C + (long long)mw * p.ldc + nb, p.ldc, buf, o, p.M - mw, p.N - nb, lane);
   }
 }
 

@@ -32,7 +32,7 @@ template <int BN> struct Cfg {
 };
 
 template <int BN, bool A_K, bool B_K, int MODE>
-__global__ void __launch_bounds__(GEMM_THREADS, 1)
+__global__ void __launch_bounds__(gemm_threads(MODE), 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const __grid_constant__ Second<MODE> two, const __grid_constant__ TcParams p) {
   using C = Cfg<BN>;
@@ -53,7 +53,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? EPI_WARPS / 2 : EPI_WARPS); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE) / 2 : epi_warps(MODE)); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -186,15 +186,17 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
   } else {
     // ---------------- epilogue warps ----------------
     const int quarter = warp & 3;              // TMEM lanes [32 q, 32 q + 32) belong to this warp
-    const int half = (warp - 2) >> 2;          // which half of the tile's columns
-    const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * STORE_BYTES;
+    const int set = (warp - 2) >> 2;           // four warps that drain the same columns
+    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE) / 8) : -1;
+    const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * store_bytes(MODE);
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
-      if (FIT && p.alternate && acc != half) {   // the other four warps' accumulator
+      if (turn >= 0 && acc != turn) {            // the other warps' accumulator
         if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
         continue;
       }
-      const int c_begin = FIT && p.alternate ? 0 : half * (BN / 2), c_end = FIT && p.alternate ? BN : (half + 1) * (BN / 2);
+      int c_begin, c_end;
+      set_columns<MODE>(set, turn >= 0, BN, c_begin, c_end);
       const bool sec = second(u);
       const Place w = locate(u, sec);
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
@@ -327,8 +329,8 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   p.alternate = MODE != DRAIN_COLS && tiles >= 2 * grid;
   constexpr int smem = C::SMEM + store_smem<MODE>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, GEMM_THREADS, smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
-  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, GEMM_THREADS, smem, st>>>(mapA, mapB, Second<MODE>{}, p);
+    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, gemm_threads(MODE), smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, gemm_threads(MODE), smem, st>>>(mapA, mapB, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -472,5 +474,5 @@ int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   m.fill = g2 ? two_fill(g, *g2, 190) : 0;
   const int units = m.units + m.units2, n_sm = ppu_sm_count();
   p.alternate = units >= 2 * n_sm;
-  return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, GEMM_THREADS, smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
+  return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, gemm_threads(DRAIN_TWO), smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
 }

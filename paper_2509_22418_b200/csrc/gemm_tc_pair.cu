@@ -121,7 +121,7 @@ __device__ __forceinline__ PairUnit pair_unit(const TcParams& p, int u, int num_
 
 // mapB2: B with a box of 64 rows (the narrow units of a K-major B); otherwise a copy of mapB
 template <int PAIR_BN, bool A_K, bool B_K, int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GEMM_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(MODE), 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                     const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ Second<MODE> two,
                     const __grid_constant__ TcParams p) {
@@ -145,7 +145,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < ST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? EPI_WARPS : 2 * EPI_WARPS); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE) : 2 * epi_warps(MODE)); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -285,17 +285,19 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   } else {
     // ---------------- epilogue warps (both CTAs, 128 rows each) ----------------
     const int quarter = warp & 3;
-    const int half = (warp - 2) >> 2;
-    const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * STORE_BYTES;
+    const int set = (warp - 2) >> 2;           // four warps that drain the same columns
+    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE) / 8) : -1;
+    const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * store_bytes(MODE);
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_units; u = unit_of(++i)) {
-      if (FIT && p.alternate && acc != half) {   // the other four warps' accumulator
+      if (turn >= 0 && acc != turn) {            // the other warps' accumulator
         if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
         continue;
       }
       const bool sec = second(u);
       const PairUnit w = locate(u, sec);
-      const int c_begin = FIT && p.alternate ? 0 : half * (w.bn / 2), c_end = FIT && p.alternate ? w.bn : (half + 1) * (w.bn / 2);
+      int c_begin, c_end;
+      set_columns<MODE>(set, turn >= 0, w.bn, c_begin, c_end);
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
@@ -368,9 +370,9 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
   constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB2, Second<MODE>{}, p) ==
+    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, gemm_threads(MODE), smem, st, mapA, mapB, mapB2, Second<MODE>{}, p) ==
                    cudaSuccess ? 0 : -3;
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, GEMM_THREADS, smem, st>>>(mapA, mapB, mapB2, Second<MODE>{}, p);
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, gemm_threads(MODE), smem, st>>>(mapA, mapB, mapB2, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -427,6 +429,6 @@ int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t 
   p.alternate = units >= 2 * max_pairs;
   // (one product alone: as many pairs as give each the same number of tiles)
   const int pairs = g2 ? (units < max_pairs ? units : max_pairs) : (units + waves - 1) / waves;
-  return ppu_launch_dependent(kernel, 2 * pairs, GEMM_THREADS, smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
+  return ppu_launch_dependent(kernel, 2 * pairs, gemm_threads(DRAIN_TWO), smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
 }
 }  // namespace gemm_tc_detail
