@@ -400,8 +400,7 @@ __device__ __forceinline__ void store_group(bf16* out, long long ld, uint32_t bu
 // The entries' own x are taken from tensor memory a column at a time: a warp's 32 rows have two in a
 // piece with 32 entries in 32768 columns.  (As dot products in the row kernel they were a gather of 4 KB of E
 // for each entry: 106 of 1200 us at 4096 x 2048 x 32768.)
-// The registers of 16 warps hold 32 columns at a time: the halves are read for the largest first, the
-// second half then worked and the first read again.
+// (Of 16 warps a thread has 112 registers: 64 logits, and powers of 32 at a time.)
 template <typename F>
 __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, int m0, int n0,
                                              uint32_t t_acc, int quarter, int c_begin, int c_end, int lane, F release) {
@@ -412,8 +411,9 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
   for (int c0 = c_begin; c0 < c_end; c0 += PIECE) {
     const int nb = n0 + c0;
     if (nb >= p.N) break;                  // warp-uniform
-    uint32_t r[32];
+    uint32_t r[PIECE];
     tmem_ld32(t_row + c0, r);
+    tmem_ld32(t_row + c0 + 32, r + 32);
     int at = 0, end = 0, id = -1;          // this row's entries in the piece, and the first one's column
     if (m < p.M) {
       if (p.entries.k > 1) {
@@ -425,24 +425,15 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
       if (at < end) id = p.entries.ids[(long long)m * p.entries.ld + at];
       if (id < nb || id >= nb + PIECE) id = -1;
     }
-    auto arrived = [&](int h) {
-      tmem_ld_wait();
-      if (nb + 32 * h + 32 > p.N) {        // columns past the vocabulary: nothing
+    tmem_ld_wait();
+    if (nb + PIECE > p.N) {                // columns past the vocabulary: nothing
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (nb + 32 * h + j >= p.N) r[j] = 0xff800000u;
-      }
-    };
+      for (int j = 0; j < PIECE; ++j)
+        if (nb + j >= p.N) r[j] = 0xff800000u;
+    }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    auto largest = [&] {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
-    };
-    arrived(0);
-    largest();
-    tmem_ld32(t_row + c0 + 32, r);
-    arrived(1);
-    largest();
+    for (int j = 0; j < PIECE; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(r[j]));
     mx[0] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     float top = mx[0] * p.piece_scale;
     if (fabsf(top) <= PIECE_RANGE || top == -INFINITY) top = 0.f;      // (-inf: all powers are 0)
@@ -459,29 +450,26 @@ __device__ __forceinline__ void drain_pieces(const TcParams& p, uint32_t buf, in
       }
       __syncwarp();
     }
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    auto powers = [&](int h) {
-      if (far) {
+    if (c0 + PIECE >= c_end || nb + PIECE >= p.N) release();
+    if (far) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - off);
-      }
+      for (int j = 0; j < PIECE; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) - off);
+    }
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < PIECE; h += 32) {
       uint32_t o[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float e0 = ex2_fast(fmaf(__uint_as_float(r[2 * j]), p.piece_scale, -less));
-        const float e1 = ex2_fast(fmaf(__uint_as_float(r[2 * j + 1]), p.piece_scale, -less));
+        const float e0 = ex2_fast(fmaf(__uint_as_float(r[h + 2 * j]), p.piece_scale, -less));
+        const float e1 = ex2_fast(fmaf(__uint_as_float(r[h + 2 * j + 1]), p.piece_scale, -less));
         sum[(2 * j) & 3] += e0;
         sum[(2 * j + 1) & 3] += e1;
         o[j] = pack2_bf16(e0, e1);
       }
       // (columns up to the next multiple of 64 belong to the row too)
-      if (p.C) store_group<32>((bf16*)p.C + (long long)mw * p.ldc + nb + 32 * h, p.ldc, buf, o, p.M - mw, 32, lane);
-    };
-    powers(1);
-    tmem_ld32(t_row + c0, r);
-    arrived(0);
-    if (c0 + PIECE >= c_end || nb + PIECE >= p.N) release();
-    powers(0);
+      if (p.C) store_group<32>((bf16*)p.C + (long long)mw * p.ldc + nb + h, p.ldc, buf, o, p.M - mw, 32, lane);
+    }
     if (m < p.M)
       p.piece_stats[(long long)m * p.ld_pieces + nb / PIECE] = make_float2(top, (sum[0] + sum[1]) + (sum[2] + sum[3]));
   }
