@@ -100,10 +100,10 @@ struct TcParams {
 // those that have instantiations of their own: drain_cols keeps its registers, and these have 32 KB of
 // shared memory behind the operand stages, through which they store 64-column groups
 enum DrainMode { DRAIN_COLS = 0, DRAIN_PIECES = 1, DRAIN_TWO = 2 };
-// DRAIN_PIECES has twice the warps: its 64 columns take a warp 1500 cycles, of which the exponentials are 512 of the SM
+// DRAIN_PIECES has twice the warps on 256-wide tiles: its 64 columns take a warp 1500 cycles, of which the exponentials are 512 of the SM
 // quarter's unit for them (logits of 4096 x 32768 x 64: 110 us with 8 warps, 88 with 16; x 768: 160 and 153).
-constexpr int epi_warps(int mode) { return mode == DRAIN_PIECES ? 2 * EPI_WARPS : EPI_WARPS; }
-constexpr int gemm_threads(int mode) { return 64 + 32 * epi_warps(mode); }
+constexpr int epi_warps(int mode, int bn) { return mode == DRAIN_PIECES && bn == 256 ? 2 * EPI_WARPS : EPI_WARPS; }
+constexpr int gemm_threads(int mode, int bn) { return 64 + 32 * epi_warps(mode, bn); }
 constexpr int store_bytes(int mode) { return mode == DRAIN_PIECES ? 32 * 64 : 32 * 128; }    // a warp's 32 rows x 32 or 64 bf16 columns
 template <int MODE> struct Second {};
 // DRAIN_TWO: a launch works the units of two products (launch_gemm_tc_two), the one with the longer units
@@ -130,12 +130,12 @@ __device__ __forceinline__ int two_unit(int i, int b, int n, int units, int unit
   return v < units2 ? units + v : NONE;
 }
 
-template <int MODE> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : epi_warps(MODE) * store_bytes(MODE); }
+template <int MODE, int BN> constexpr int store_smem() { return MODE == DRAIN_COLS ? 0 : epi_warps(MODE, BN) * store_bytes(MODE); }
 
 // Columns of a tile of bn that a set of four warps (one for each quarter of the rows) drains: an equal part, of the whole
 // tile or, where the sets take turns, of every other tile's; pieces are not divided, so sets may be left without.
-template <int MODE> __device__ __forceinline__ void set_columns(int set, int alternate, int bn, int& begin, int& end) {
-  constexpr int SETS = epi_warps(MODE) / 4;
+template <int MODE, int BN> __device__ __forceinline__ void set_columns(int set, int alternate, int bn, int& begin, int& end) {
+  constexpr int SETS = epi_warps(MODE, BN) / 4;
   const int sub = alternate ? set % (SETS / 2) : set;
   int cols = alternate ? bn / (SETS / 2) : bn / SETS;
   if (MODE == DRAIN_PIECES && cols < PIECE) cols = PIECE;

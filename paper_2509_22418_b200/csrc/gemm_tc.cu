@@ -32,14 +32,14 @@ template <int BN> struct Cfg {
 };
 
 template <int BN, bool A_K, bool B_K, int MODE>
-__global__ void __launch_bounds__(gemm_threads(MODE), 1)
+__global__ void __launch_bounds__(gemm_threads(MODE, BN), 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                const __grid_constant__ Second<MODE> two, const __grid_constant__ TcParams p) {
   using C = Cfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE_BYTES + store_smem<MODE>());
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE_BYTES + store_smem<MODE, BN>());
   // bars[0..ST): full, [ST..2ST): empty, [2ST..2ST+2): tmem_full, [2ST+2..2ST+4): tmem_empty
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -53,7 +53,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE) / 2 : epi_warps(MODE)); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE, BN) / 2 : epi_warps(MODE, BN)); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -187,7 +187,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
     // ---------------- epilogue warps ----------------
     const int quarter = warp & 3;              // TMEM lanes [32 q, 32 q + 32) belong to this warp
     const int set = (warp - 2) >> 2;           // four warps that drain the same columns
-    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE) / 8) : -1;
+    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE, BN) / 8) : -1;
     const uint32_t store_buf = smem_u32(smem + C::STAGES * C::STAGE_BYTES) + (warp - 2) * store_bytes(MODE);
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_tiles; u = unit_of(++i)) {
@@ -196,7 +196,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__
         continue;
       }
       int c_begin, c_end;
-      set_columns<MODE>(set, turn >= 0, BN, c_begin, c_end);
+      set_columns<MODE, BN>(set, turn >= 0, BN, c_begin, c_end);
       const bool sec = second(u);
       const Place w = locate(u, sec);
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
@@ -311,7 +311,7 @@ template <int BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_t(const GemmArgs& g, cudaStream_t st) {
   using C = Cfg<BN>;
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM + store_smem<MODE>())) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_kernel<BN, A_K, B_K, MODE>, C::SMEM + store_smem<MODE, BN>())) return -1;
   CUtensorMap mapA, mapB;
   TcParams p = make_params(g);
   if (MODE == DRAIN_COLS) p.k_rows = BK;
@@ -327,10 +327,10 @@ int launch_t(const GemmArgs& g, cudaStream_t st) {
   const int n_sm = ppu_sm_count();
   const int grid = tiles < n_sm ? tiles : n_sm;
   p.alternate = MODE != DRAIN_COLS && tiles >= 2 * grid;
-  constexpr int smem = C::SMEM + store_smem<MODE>();
+  constexpr int smem = C::SMEM + store_smem<MODE, BN>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, gemm_threads(MODE), smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
-  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, gemm_threads(MODE), smem, st>>>(mapA, mapB, Second<MODE>{}, p);
+    return ppu_launch_dependent(gemm_tc_kernel<BN, A_K, B_K, MODE>, grid, gemm_threads(MODE, BN), smem, st, mapA, mapB, Second<MODE>{}, p) == cudaSuccess ? 0 : -3;
+  gemm_tc_kernel<BN, A_K, B_K, MODE><<<grid, gemm_threads(MODE, BN), smem, st>>>(mapA, mapB, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -455,7 +455,7 @@ int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   if (gemm_tc_pairs_two(g, g2)) return launch_gemm_tc_pair_two(g, g2, st);
   using C = Cfg<128>;
   static PerDeviceFlag attr;
-  constexpr int smem = C::SMEM + store_smem<DRAIN_TWO>();
+  constexpr int smem = C::SMEM + store_smem<DRAIN_TWO, 128>();
   auto kernel = gemm_tc_kernel<128, true, false, DRAIN_TWO>;
   if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
   CUtensorMap mapA, mapB;
@@ -474,5 +474,5 @@ int launch_gemm_tc_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   m.fill = g2 ? two_fill(g, *g2, 190) : 0;
   const int units = m.units + m.units2, n_sm = ppu_sm_count();
   p.alternate = units >= 2 * n_sm;
-  return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, gemm_threads(DRAIN_TWO), smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
+  return ppu_launch_dependent(kernel, units < n_sm ? units : n_sm, gemm_threads(DRAIN_TWO, 128), smem, st, mapA, mapB, m, p) == cudaSuccess ? 0 : -3;
 }

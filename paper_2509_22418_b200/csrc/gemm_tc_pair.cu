@@ -121,7 +121,7 @@ __device__ __forceinline__ PairUnit pair_unit(const TcParams& p, int u, int num_
 
 // mapB2: B with a box of 64 rows (the narrow units of a K-major B); otherwise a copy of mapB
 template <int PAIR_BN, bool A_K, bool B_K, int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(MODE), 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_threads(MODE, PAIR_BN), 1)
 gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                     const __grid_constant__ CUtensorMap mapB2, const __grid_constant__ Second<MODE> two,
                     const __grid_constant__ TcParams p) {
@@ -130,7 +130,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
   extern __shared__ uint8_t smem_raw[];
   // the dynamic window starts at the same offset in both CTAs, so aligned offsets match too
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ST * PAIR_STAGE_BYTES + store_smem<MODE>());
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + ST * PAIR_STAGE_BYTES + store_smem<MODE, PAIR_BN>());
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * ST + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -145,7 +145,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < ST; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE) : 2 * epi_warps(MODE)); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), MODE != DRAIN_COLS && p.alternate ? epi_warps(MODE, PAIR_BN) : 2 * epi_warps(MODE, PAIR_BN)); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -286,7 +286,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
     // ---------------- epilogue warps (both CTAs, 128 rows each) ----------------
     const int quarter = warp & 3;
     const int set = (warp - 2) >> 2;           // four warps that drain the same columns
-    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE) / 8) : -1;
+    const int turn = MODE != DRAIN_COLS && p.alternate ? set / (epi_warps(MODE, PAIR_BN) / 8) : -1;
     const uint32_t store_buf = smem_u32(smem + ST * PAIR_STAGE_BYTES) + (warp - 2) * store_bytes(MODE);
     int acc = 0; uint32_t acc_ph = 0;
     for (int i = 0, u = unit_of(0); u < num_units; u = unit_of(++i)) {
@@ -297,7 +297,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
       const bool sec = second(u);
       const PairUnit w = locate(u, sec);
       int c_begin, c_end;
-      set_columns<MODE>(set, turn >= 0, w.bn, c_begin, c_end);
+      set_columns<MODE, PAIR_BN>(set, turn >= 0, w.bn, c_begin, c_end);
       const int m0 = w.m0 + (int)rank * 128;
       if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
       tc_fence_after();
@@ -330,7 +330,7 @@ gemm_tc_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_const
 template <int PAIR_BN, bool A_K, bool B_K, int MODE = DRAIN_COLS>
 int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM + store_smem<MODE>())) return -1;
+  if (!ppu_set_smem_once(attr, gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, PairCfg<PAIR_BN>::SMEM + store_smem<MODE, PAIR_BN>())) return -1;
   CUtensorMap mapA, mapB, mapB2;
   TcParams p = p0;
   if (MODE == DRAIN_COLS) p.k_rows = BK;
@@ -368,11 +368,11 @@ int launch_pair_t(const GemmArgs& g, const TcParams& p0, cudaStream_t st) {
   p.alternate = MODE != DRAIN_COLS && tiles >= 2 * pairs;
   mapB2 = mapB;
   if (B_K && p.tail_from < tiles && !encode_map(&mapB2, g.B, g.ldb, true, g.N, g.K, 64, g.transient)) return -2;
-  constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE>();
+  constexpr int smem = PairCfg<PAIR_BN>::SMEM + store_smem<MODE, PAIR_BN>();
   if (g.transient)
-    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, gemm_threads(MODE), smem, st, mapA, mapB, mapB2, Second<MODE>{}, p) ==
+    return ppu_launch_dependent(gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE>, 2 * pairs, gemm_threads(MODE, PAIR_BN), smem, st, mapA, mapB, mapB2, Second<MODE>{}, p) ==
                    cudaSuccess ? 0 : -3;
-  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, gemm_threads(MODE), smem, st>>>(mapA, mapB, mapB2, Second<MODE>{}, p);
+  gemm_tc_pair_kernel<PAIR_BN, A_K, B_K, MODE><<<2 * pairs, gemm_threads(MODE, PAIR_BN), smem, st>>>(mapA, mapB, mapB2, Second<MODE>{}, p);
   return cudaGetLastError() == cudaSuccess ? 0 : -3;
 }
 
@@ -408,7 +408,7 @@ static int two_units(const GemmArgs& g, TcParams& p) {
 }
 int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t st) {
   static PerDeviceFlag attr;
-  constexpr int smem = PairCfg<256>::SMEM + store_smem<DRAIN_TWO>();
+  constexpr int smem = PairCfg<256>::SMEM + store_smem<DRAIN_TWO, 256>();
   auto kernel = gemm_tc_pair_kernel<256, true, false, DRAIN_TWO>;
   if (!ppu_set_smem_once(attr, kernel, smem)) return -1;
   CUtensorMap mapA, mapB;
@@ -429,6 +429,6 @@ int launch_gemm_tc_pair_two(const GemmArgs& g, const GemmArgs* g2, cudaStream_t 
   p.alternate = units >= 2 * max_pairs;
   // (one product alone: as many pairs as give each the same number of tiles)
   const int pairs = g2 ? (units < max_pairs ? units : max_pairs) : (units + waves - 1) / waves;
-  return ppu_launch_dependent(kernel, 2 * pairs, gemm_threads(DRAIN_TWO), smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
+  return ppu_launch_dependent(kernel, 2 * pairs, gemm_threads(DRAIN_TWO, 256), smem, st, mapA, mapB, mapB, m, p) == cudaSuccess ? 0 : -3;
 }
 }  // namespace gemm_tc_detail
