@@ -173,6 +173,28 @@ def test_chunks_of_rows(T, d, V):
 
 
 @gpu
+@pytest.mark.parametrize("T,d,V", [
+    (1001, 72, 5003),      # a last wave of a few tiles, worked as halves
+    (1100, 40, 9001),      # the same behind more than two tiles a block
+    (100, 64, 40001),      # one row tile, wide tiles
+    (100, 200, 80003),     # the same, three tiles a block
+    (700, 136, 33000),     # five tiles a block
+])
+def test_how_tiles_are_shared_out(T, d, V):
+    import torch
+    from paper_2509_22418_b200 import ppu
+    rng, Xt, X, Et, E, target = make(T, d, V, seed=T + d)
+    target[2::5] = -1
+    ids, q, ent, there = hard(target)
+    w = mean_weights(there)
+    R = definition(X, E, ids, q, ent, w, 1.0)
+    tol = tolerances(X, E, q, w, 1.0, R, ent)
+    R["row"] *= there
+    tol["row"] *= there
+    check(ppu.ppu_head_xent(Xt, Et, torch.from_numpy(target).cuda()), R, tol)
+
+
+@gpu
 def test_large_vocabulary():
     import torch
     from paper_2509_22418_b200 import ppu
