@@ -590,6 +590,36 @@ def test_strided_operands_and_untouched_surroundings():
 
 
 @gpu
+@pytest.mark.parametrize("T,chunk", [(20000, 0), (1500, 256), (0, 0)])
+def test_capture_of_counted_rows_and_chunks(T, chunk):
+    """Rows counted by a kernel of their own (behind a memset for many), several chunks, no rows at all."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X = torch.randn(T, 64, generator=g, device="cuda").bfloat16()
+    E = (torch.randn(300, 64, generator=g, device="cuda") * 0.4).bfloat16()
+    ids = torch.randint(-50, 300, (T, 3), generator=g, device="cuda", dtype=torch.int32)
+    z = torch.randn(T, 3, generator=g, device="cuda")
+    calls = [lambda: ppu.ppu_head_xent(X, E, ids[:, 0].contiguous(), chunk_rows=chunk), lambda: ppu.ppu_head_distill(X, E, ids, z, chunk_rows=chunk)]
+    for call in calls:
+        want = [t.clone() for t in call()]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            call()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                got = call()
+            for t in got:
+                t.fill_(7)
+            for _ in range(2):
+                graph.replay()
+        s.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+@gpu
 def test_captured_streamed_and_repeated_calls_have_the_same_bits():
     import torch
     from paper_2509_22418_b200 import ppu
