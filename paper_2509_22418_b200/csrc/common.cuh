@@ -43,7 +43,7 @@ enum GemmEpilogue {
   EPI_DELTA_BF16 = 6,
   // softmax pieces (launch_gemm_tc_pieces only): per row and 64 columns, C bf16 = 2^(x - ref) with
   // x = acc * piece_scale, and piece_stats = {ref, sum of the unrounded powers}; ref is 0 where the
-  // piece's largest x lies within +-PIECE_RANGE, else that largest x
+  // piece's largest x lies within +-PIECE_RANGE, else that largest x as a whole number
   EPI_PIECES = 7,
   // C bf16 = row_scale[m] * (aux fp32 + acc), scale and aux optional (launch_gemm_tc_two only)
   EPI_OUT_BF16 = 8

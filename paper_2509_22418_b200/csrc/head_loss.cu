@@ -12,7 +12,7 @@
 // the chunk's two gradient products are done: a [rows, V] buffer of bounded size, not [T, V].
 //   1. tcgen05 product of the chunk's rows with E^T.  Its epilogue works the vocabulary in pieces of 64
 //      columns: bf16 powers u = 2^(x - ref), x = s log2(e), and {ref, sum} in fp32; ref is 0 for ordinary
-//      logits (within 41 nats of 0), else the piece's maximum.  The entries' own x are kept in fp32 (the powers
+//      logits (within 41 nats of 0), else the piece's maximum, as a whole number.  The entries' own x are kept in fp32 (the powers
 //      would be too coarse for the loss and for p - 1 next to p = 1); for that a kernel before it has
 //      sorted each row's entries and counted how many lie before each piece (not needed for one entry a row).
 //   2. a warp or a block per row joins the pieces to the row's log-sum-exp and forms the row loss.  Then
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(1024) count_rows_block_kernel(Targets tg, int 
   }
 }
 
-// scales 64 stored powers
+// scales 64 stored powers (by a power of two: no rounding)
 __device__ __forceinline__ void scale_piece(bf16* p, float f) {
 #pragma unroll
   for (int i = 0; i < PIECE / 8; ++i) {
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
         if (!plain) {                               // (seldom) powers that are relative to something else
           for (int i = tid; i < a.n_pieces; i += N) {
             const float2 v = st[i];
-            if (v.x != ref && v.y != 0.f) scale_piece(ur + (int64_t)i * PIECE, exp2f(v.x - ref));
+            if (v.x != ref && v.y != 0.f) scale_piece(ur + (int64_t)i * PIECE, ldexpf(1.f, (int)(v.x - ref)));
           }
           sync();
         }
