@@ -1,5 +1,6 @@
 """Builds libppu.so (sm_100a, nvcc) and _ops.so (the compiled torch binding of the operators, g++) next to this
-file.  No GPU is needed to build."""
+file.  No GPU is needed to build.  The library needs neither torch nor the binding: where torch (with CUDA) is not
+installed it is built alone, and where the binding does not compile the error comes once the library is there."""
 from __future__ import annotations
 
 import importlib.util
@@ -20,9 +21,10 @@ FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-li
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(OPS):
+    built = [LIB, OPS] if _torch_dir() else [LIB]
+    if not all(os.path.exists(p) for p in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(OPS))
+    t = min(os.path.getmtime(p) for p in built)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "ppu.h"))
     return any(os.path.getmtime(p) > t for p in deps)
@@ -31,8 +33,11 @@ def _stale() -> bool:
 OPS_OBJ = os.path.join(HERE, "_build", "bind.o")
 
 
-def _torch_dir() -> str:
-    return os.path.dirname(importlib.util.find_spec("torch").origin)     # without importing it
+def _torch_dir():
+    """Where torch with CUDA is installed (found without importing it), or None."""
+    spec = importlib.util.find_spec("torch")
+    path = os.path.dirname(spec.origin) if spec and spec.origin else None
+    return path if path and os.path.exists(os.path.join(path, "lib", "libtorch_cuda.so")) else None
 
 
 def _ops_compile():
@@ -55,17 +60,25 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose:
             cmd.insert(1, "-Xptxas=-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    procs.append(("bind.cpp", subprocess.Popen(_ops_compile(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    failed = False
+    with_ops = _torch_dir() is not None
+    if with_ops:
+        procs.append(("bind.cpp", subprocess.Popen(_ops_compile(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    failed = []
     for src, p in procs:
         out = p.communicate()[0].decode()
         if p.returncode != 0 or verbose:
             sys.stderr.write(f"--- {src}\n{out}\n")
-        failed |= p.returncode != 0
-    if failed:
-        raise RuntimeError("compilation failed")
+        if p.returncode != 0:
+            failed.append(src)
+    if [src for src in failed if src != "bind.cpp"]:
+        raise RuntimeError(f"compilation failed: {', '.join(failed)}")
     subprocess.check_call([nvcc, "-shared", "-o", LIB, *objs, "-gencode",
                            "arch=compute_100a,code=sm_100a"])
+    if not with_ops:
+        sys.stderr.write("torch with CUDA is not installed: its binding (_ops.so) is not built\n")
+        return LIB
+    if failed:
+        raise RuntimeError("compilation failed: bind.cpp")
     torch_lib = os.path.join(_torch_dir(), "lib")
     subprocess.check_call(["g++", "-shared", "-o", OPS, OPS_OBJ, "-L" + HERE, "-l:libppu.so", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-ltorch_python", "-ltorch",
                            "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
