@@ -24,6 +24,9 @@ def _stale() -> bool:
     built = [LIB, OPS] if _torch_dir() else [LIB]
     if not all(os.path.exists(p) for p in built):
         return True
+    stamp = _stamp()
+    if OPS in built and os.path.exists(stamp) and open(stamp).read() != _built_for():      # (without a note of it, the binding is taken as it is)
+        return True
     t = min(os.path.getmtime(p) for p in built)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "ppu.h"))
@@ -38,6 +41,17 @@ def _torch_dir():
     spec = importlib.util.find_spec("torch")
     path = os.path.dirname(spec.origin) if spec and spec.origin else None
     return path if path and os.path.exists(os.path.join(path, "lib", "libtorch_cuda.so")) else None
+
+
+def _stamp() -> str:
+    return os.path.join(os.path.dirname(OPS_OBJ), "bind.txt")
+
+
+def _built_for() -> str:
+    """The torch and the Python that a binding belongs to: their ABI is not kept from one version to the next."""
+    torch = _torch_dir()
+    with open(os.path.join(torch, "version.py")) as f:
+        return f"{sys.implementation.cache_tag}\n{torch}\n{f.read()}"
 
 
 def _ops_compile():
@@ -82,6 +96,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     torch_lib = os.path.join(_torch_dir(), "lib")
     subprocess.check_call(["g++", "-shared", "-o", OPS, OPS_OBJ, "-L" + HERE, "-l:libppu.so", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib, "-ltorch_python", "-ltorch",
                            "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
+    with open(_stamp(), "w") as f:
+        f.write(_built_for())
     return LIB
 
 

@@ -78,3 +78,14 @@ def test_built_once(tree):
     n = tree.runs()
     tree.build()
     assert tree.runs() == n
+
+
+def test_built_again_for_another_torch(tree):
+    tree.build()
+    n = tree.runs()
+    (tree.torch_dir / "version.py").write_text("__version__ = '2.1'\n")
+    tree.build()
+    assert tree.runs() > n
+    n = tree.runs()
+    tree.build()
+    assert tree.runs() == n
