@@ -6,6 +6,7 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -220,6 +221,11 @@ PyObject* norm_gate_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Norm o = norm_operands(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
     const int kind = int_arg(a[8], "kind"), in_place = PyObject_IsTrue(a[11]);
     const float scale = float_arg(a[9]), eps = float_arg(a[10]);
+    if (in_place) {                          // as torch's own in-place calls: a graph that saved r is told, and one that leads to r is not cut
+      const at::Tensor& r = THPVariable_Unpack(a[1]);
+      if (r.requires_grad() && c10::GradMode::is_enabled()) refuse("in_place: r requires a gradient (call under torch.no_grad, or pass r.detach())");
+      if (!r.is_inference()) r.unsafeGetTensorImpl()->bump_version();
+    }
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)o.dev);
     const at::Tensor out[3] = {in_place ? THPVariable_Unpack(a[1]) : make({o.T, o.d}, at::kFloat, o.dev), make({o.T, o.d}, at::kBFloat16, o.dev),
                                make({o.T, 4}, at::kFloat, o.dev)};

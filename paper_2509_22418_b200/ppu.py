@@ -423,7 +423,8 @@ def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None
                       kind="layer", res_scale=1.0, eps=1e-5, in_place=False):
     """n = N(y) post_gain + post_shift; r_out = res_scale r + gate n; h = N(r_out) pre_gain + pre_shift for
     a block's output y [T, d] (bf16) and the residual stream r [T, d] (fp32); kind "layer" or "rms";
-    gate fp32 [ceil(T / gate_rows), d] (gate_rows 0: one row for all).  in_place: r_out is r.
+    gate fp32 [ceil(T / gate_rows), d] (gate_rows 0: one row for all).  in_place: r_out is r (refused where r requires a
+    gradient and gradients are recorded).
     Returns (r_out fp32, h bf16, stats fp32 [T, 4])."""
     return (_ops or _binding()).norm_gate_fwd(y, r, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, _kind(kind), res_scale, eps, in_place)
 

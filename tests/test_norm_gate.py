@@ -417,3 +417,30 @@ def test_device_tensors_are_checked():
     for args in ((y.float(), r, y, r, s, g, g), (y, r.half(), y, r, s, g, g), (y, r, y, r, s[:, :2], g, g), (y[:3], r, y, r, s, g, g)):
         with pytest.raises(ppu.PpuError):
             ppu.ppu_norm_gate_bwd(*args)
+
+
+@gpu
+def test_writing_in_place_is_seen_by_autograd():
+    """A graph that saved r is told that r has changed; an r of a graph of its own is not overwritten."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    y, g = torch.randn(4, 64, device="cuda").bfloat16(), torch.ones(64, device="cuda")
+    r = torch.randn(4, 64, device="cuda")
+    w = torch.ones(64, device="cuda", requires_grad=True)
+    loss = (r * w).sum()
+    before = r._version
+    out = ppu.ppu_norm_gate_fwd(y, r, g, g, in_place=True)
+    assert out[0] is r and r._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    for own in (r.clone().requires_grad_(), r.clone().requires_grad_() * 2):
+        was = own.detach().clone()
+        with pytest.raises(ppu.PpuError):
+            ppu.ppu_norm_gate_fwd(y, own, g, g, in_place=True)
+        assert torch.equal(own.detach(), was)
+        with torch.no_grad():
+            got = ppu.ppu_norm_gate_fwd(y, own, g, g, in_place=True)
+        assert torch.equal(got[0].detach(), ppu.ppu_norm_gate_fwd(y, was, g, g)[0])
+    with torch.inference_mode():
+        s = r + 0
+    assert ppu.ppu_norm_gate_fwd(y, s, g, g, in_place=True)[0] is s
