@@ -74,6 +74,11 @@ int int_arg(PyObject* o, const char* name) {
   if (v == -1 && PyErr_Occurred()) throw python_error();
   return as_int(v, name);
 }
+bool truth_arg(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v != 0;
+}
 float float_arg(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw python_error();
@@ -219,7 +224,8 @@ Norm norm_operands(PyObject* y, PyObject* r, PyObject* g1, PyObject* g2, PyObjec
 PyObject* norm_gate_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 12, [&] {
     const Norm o = norm_operands(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
-    const int kind = int_arg(a[8], "kind"), in_place = PyObject_IsTrue(a[11]);
+    const int kind = int_arg(a[8], "kind");
+    const bool in_place = truth_arg(a[11]);
     const float scale = float_arg(a[9]), eps = float_arg(a[10]);
     if (in_place) {                          // as torch's own in-place calls: a graph that saved r is told, and one that leads to r is not cut
       const at::Tensor& r = THPVariable_Unpack(a[1]);

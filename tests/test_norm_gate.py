@@ -444,3 +444,15 @@ def test_writing_in_place_is_seen_by_autograd():
     with torch.inference_mode():
         s = r + 0
     assert ppu.ppu_norm_gate_fwd(y, s, g, g, in_place=True)[0] is s
+
+
+@gpu
+def test_in_place_has_to_be_a_truth_value():
+    """One that is neither true nor false is an error before r is written."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    y, r, g = torch.randn(4, 64, device="cuda").bfloat16(), torch.randn(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    was = r.clone()
+    with pytest.raises(ValueError):
+        ppu.ppu_norm_gate_fwd(y, r, g, g, in_place=np.zeros(2))
+    assert torch.equal(r, was)
