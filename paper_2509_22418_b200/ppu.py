@@ -374,9 +374,14 @@ def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0, k=1) -> int:
     return n.value
 
 
+_GRAD_WORDS = {"x": 1, "e": 2, "xe": 3, "ex": 3}
+
+
 def _grads(grad):
     if isinstance(grad, str):
-        return ("x" in grad) + 2 * ("e" in grad)
+        if grad not in _GRAD_WORDS:
+            raise PpuError(-1, f"grad must be True, False or one of {sorted(_GRAD_WORDS)}, got {grad!r}")
+        return _GRAD_WORDS[grad]
     return 3 if grad else 0
 
 

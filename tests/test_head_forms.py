@@ -39,3 +39,16 @@ def test_powers_beyond_the_common_reference_are_rounded_once(T, V):
     rel -= rel.mean(1, keepdims=True)
     one = 2.0 ** -7 / np.sqrt(12) * np.sqrt(3 / 8 / np.log(2))
     assert np.sqrt((rel ** 2).mean()) <= one * (np.sqrt(2) + np.sqrt(3)) / 2
+
+
+# ---- refusals, on the host ----------------------------------------------------------------------
+def test_gradients_are_named_exactly():
+    """A word that is none of those documented is refused, whatever letters it has."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    X, E, t = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(32, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    for word in ("none", "both", "X", "", "x,e", "ee"):
+        for call in (lambda: ppu.ppu_head_xent(X, E, t, grad=word), lambda: ppu.ppu_head_distill(X, E, t[:, None], X[:, :1].float(), grad=word)):
+            with pytest.raises(ppu.PpuError, match="grad"):
+                call()
+    assert [ppu._grads(g) for g in (True, False, "x", "e", "xe", "ex", None)] == [3, 0, 1, 2, 3, 3, 0]
