@@ -367,10 +367,18 @@ def _binding():
     return _ops
 
 
+def _int32(*values):
+    """The values, or an error where one does not fit the C argument (ctypes keeps its low bits)."""
+    for v in values:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise PpuError(-2, f"{v} is too large")
+    return values
+
+
 def ppu_head_query_bytes(T, d, V, grads=3, chunk_rows=0, k=1) -> int:
     """Bytes of workspace of a head loss; grads: 1 (dX) + 2 (dE); k: entries a row (1 for xent)."""
     n = C.c_size_t(0)
-    _check(lib().ppu_head_query_bytes(T, d, V, grads, chunk_rows, k, C.byref(n)))
+    _check(lib().ppu_head_query_bytes(*_int32(T, d, V, grads, chunk_rows, k), C.byref(n)))
     return n.value
 
 
@@ -437,7 +445,7 @@ def ppu_norm_gate_fwd(y, r, post_gain, pre_gain, post_shift=None, pre_shift=None
 def ppu_norm_gate_query_bytes(T, d, gate_rows=0) -> int:
     """Bytes of workspace of ppu_norm_gate_bwd (gate_rows 0: no gate)."""
     n = C.c_size_t(0)
-    _check(lib().ppu_norm_gate_query_bytes(T, d, gate_rows, C.byref(n)))
+    _check(lib().ppu_norm_gate_query_bytes(*_int32(T, d, gate_rows), C.byref(n)))
     return n.value
 
 

@@ -52,3 +52,21 @@ def test_gradients_are_named_exactly():
             with pytest.raises(ppu.PpuError, match="grad"):
                 call()
     assert [ppu._grads(g) for g in (True, False, "x", "e", "xe", "ex", None)] == [3, 0, 1, 2, 3, 3, 0]
+
+
+def test_sizes_that_do_not_fit_are_refused():
+    """Sizes beyond 32 bits: not the workspace of what is left of them."""
+    from paper_2509_22418_b200 import ppu
+    for big in (2 ** 31, 2 ** 32 + 8, -2 ** 32 + 8, 2 ** 64 + 8):
+        for at in range(3):
+            sizes = [8, 64, 100]
+            sizes[at] = big
+            with pytest.raises(ppu.PpuError) as e:
+                ppu.ppu_head_query_bytes(*sizes)
+            assert e.value.code == -2
+        for kw in (dict(grads=big), dict(chunk_rows=big), dict(k=big)):
+            with pytest.raises(ppu.PpuError):
+                ppu.ppu_head_query_bytes(8, 64, 100, **kw)
+        for sizes in ((big, 64), (8, big), (8, 64, big)):
+            with pytest.raises(ppu.PpuError):
+                ppu.ppu_norm_gate_query_bytes(*sizes)
