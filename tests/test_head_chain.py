@@ -85,3 +85,29 @@ def test_eager_calls_beside_a_captured_pass():
         torch.cuda.synchronize()
         for a, b, x, y in zip(ref, cap, eager, more):
             assert torch.equal(a, b) and torch.equal(a, x) and torch.equal(a, y)
+
+
+@pytest.mark.parametrize("kind,gate_rows", [("layer", 300), ("rms", 100), ("layer", 1), ("rms", None)])
+def test_gradients_of_every_parameter_below_the_head(kind, gate_rows):
+    """The same chain with a cross entropy: the first norm's gain and shift and the gate too."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    T, d, V = 300, 136, 1003
+    c, t, n, v, gate, groups = make(T, d, kind, kind == "layer", gate_rows, seed=6)
+    rng = np.random.default_rng(3)
+    Et = torch.from_numpy((rng.standard_normal((V, d)) * 0.25).astype(np.float32)).bfloat16().cuda()
+    E = Et.double().cpu().numpy()
+    target = rng.integers(0, V, T).astype(np.int32)
+    target[::7] = -1
+    tt = torch.from_numpy(target).cuda()
+    got = chain(ppu, c, t, gate_rows, Et, lambda h: ppu.ppu_head_xent(h, Et, tt))
+    r_out, h, stats = got[:3]
+    H = h.double().cpu().numpy()
+    ids, q, ent, there = hard(target)
+    w = mean_weights(there)
+    R = definition(H, E, ids, q, ent, w, 1.0)
+    tol = tolerances(H, E, q, w, 1.0, R, ent)
+    G, gtol = backward(c, n["y"], r_out.double().cpu().numpy(), stats.double().cpu().numpy(), R["dX"], np.zeros((T, d)), v, gate, groups, e_dh=tol["dX"])
+    for name, x in zip(("dy", "dr", "dg1", "db1", "dg2", "db2", "dgate"), got[8:]):
+        if x is not None:
+            near(x, G[name], gtol[name], name)
