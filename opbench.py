@@ -101,11 +101,11 @@ def main():
         E = (torch.randn((V, d), generator=g) * (3.0 / d ** 0.5)).to(dev).bfloat16()
         X = torch.randn((T, d), generator=g).to(dev).bfloat16()
         ids = torch.randint(0, V, (T, max(1, a.teacher)), generator=g, dtype=torch.int32).to(dev)
-        z = torch.randn(ids.shape, generator=g).to(dev)
+        z, target = torch.randn(ids.shape, generator=g).to(dev), ids[:, 0].contiguous()
         if a.teacher:
             ms = timed(lambda: ppu.ppu_head_distill(X, E, ids, z, temperature=2.0, grad=not a.no_grad))
         else:
-            ms = timed(lambda: ppu.ppu_head_xent(X, E, ids[:, 0].contiguous(), grad=not a.no_grad))
+            ms = timed(lambda: ppu.ppu_head_xent(X, E, target, grad=not a.no_grad))
         fl = (2.0 if a.no_grad else 6.0) * T * V * d
         print(f"head T={T} V={V} d={d} teacher={a.teacher} grad={not a.no_grad}: {ms:.4f} ms {fl / ms / 1e9:.1f} TFLOP/s")
     elif a.op == "norm":
