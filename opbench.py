@@ -113,12 +113,13 @@ def main():
         rows = a.gate_rows or T
         y, r = torch.randn((T, d), generator=g).to(dev).bfloat16(), torch.randn((T, d), generator=g).to(dev)
         one, gate = torch.ones(d, device=dev), torch.ones((-(-T // rows), d), device=dev)
+        gate_bytes = 4 * gate.numel()
         kw = dict(gate=gate, gate_rows=rows, kind="rms" if a.rms else "layer")
         r_out, hh, st = ppu.ppu_norm_gate_fwd(y, r, one, one, **kw)
         ms = timed(lambda: ppu.ppu_norm_gate_fwd(y, r, one, one, **kw))
-        print(f"norm fwd T={T} d={d}: {ms:.4f} ms {12.0 * T * d / ms / 1e6:.0f} GB/s")
+        print(f"norm fwd T={T} d={d}: {ms:.4f} ms {(12.0 * T * d + gate_bytes) / ms / 1e6:.0f} GB/s")
         ms = timed(lambda: ppu.ppu_norm_gate_bwd(hh, r, y, r_out, st, one, one, **kw))
-        print(f"norm bwd: {ms:.4f} ms {18.0 * T * d / ms / 1e6:.0f} GB/s")
+        print(f"norm bwd: {ms:.4f} ms {(18.0 * T * d + 2 * gate_bytes) / ms / 1e6:.0f} GB/s")
     else:
         B_, S, h, dh = a.batch, a.seq, a.heads, a.dh
         d = h * dh
