@@ -6,7 +6,7 @@
                                                        the 1.3B-class layer shape but only L layers
                                                        (a few GB: the small case for profiler
                                                        captures of the bandwidth-bound kernels)
-  head  --m T --n V --k D [--teacher K] [--no-grad]     head loss of T rows against V ids (cross entropy, or
+  head  --m T --n V --k D [--teacher K] [--grad xe|x|e|none]  head loss of T rows against V ids (cross entropy, or
                                                        distillation from K teacher entries)
   norm  --m T --k D [--rms] [--gate-rows R]            gated norm pair, forward and backward
 Times with CUDA events on the launching stream after warm-up; operands are sized by the caller
@@ -41,7 +41,8 @@ def main():
     ap.add_argument("--train-non-mlp", action="store_true")
     ap.add_argument("--head-slices", type=int, default=0, help="path: MLP + head slicing with this many head groups")
     ap.add_argument("--teacher", type=int, default=0)
-    ap.add_argument("--no-grad", action="store_true")
+    ap.add_argument("--grad", choices=["xe", "x", "e", "none"], default="xe", help="head: gradients (x: the vocabulary matrix is frozen)")
+    ap.add_argument("--chunk-rows", type=int, default=0, help="head: rows of a chunk")
     ap.add_argument("--rms", action="store_true")
     ap.add_argument("--gate-rows", type=int, default=0, help="norm: rows that share a row of the gate (0: all of them)")
     ap.add_argument("--iters", type=int, default=10)
@@ -102,12 +103,13 @@ def main():
         X = torch.randn((T, d), generator=g).to(dev).bfloat16()
         ids = torch.randint(0, V, (T, max(1, a.teacher)), generator=g, dtype=torch.int32).to(dev)
         z, target = torch.randn(ids.shape, generator=g).to(dev), ids[:, 0].contiguous()
+        kw = dict(grad=False if a.grad == "none" else a.grad, chunk_rows=a.chunk_rows)
         if a.teacher:
-            ms = timed(lambda: ppu.ppu_head_distill(X, E, ids, z, temperature=2.0, grad=not a.no_grad))
+            ms = timed(lambda: ppu.ppu_head_distill(X, E, ids, z, temperature=2.0, **kw))
         else:
-            ms = timed(lambda: ppu.ppu_head_xent(X, E, target, grad=not a.no_grad))
-        fl = (2.0 if a.no_grad else 6.0) * T * V * d
-        print(f"head T={T} V={V} d={d} teacher={a.teacher} grad={not a.no_grad}: {ms:.4f} ms {fl / ms / 1e9:.1f} TFLOP/s")
+            ms = timed(lambda: ppu.ppu_head_xent(X, E, target, **kw))
+        fl = 2.0 * (1 + len(a.grad.replace("none", ""))) * T * V * d
+        print(f"head T={T} V={V} d={d} teacher={a.teacher} grad={a.grad} chunk_rows={a.chunk_rows}: {ms:.4f} ms {fl / ms / 1e9:.1f} TFLOP/s")
     elif a.op == "norm":
         T, d = a.m, a.k
         rows = a.gate_rows or T
