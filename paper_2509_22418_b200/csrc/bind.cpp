@@ -215,8 +215,11 @@ Norm norm_operands(PyObject* y, PyObject* r, PyObject* g1, PyObject* g2, PyObjec
   if (gate != Py_None) {
     o.gate_rows = int_arg(gate_rows, "gate_rows");
     if (o.gate_rows < 0) refuse("gate_rows must not be negative");
-    if (o.gate_rows == 0) o.gate_rows = o.T > 0 ? o.T : 1;
-    o.gate = (const float*)dense(gate, "gate", at::kFloat, {((int64_t)o.T + o.gate_rows - 1) / o.gate_rows, o.d}, o.dev);
+    const bool one = o.gate_rows == 0;       // one row for all rows; without any it may also be left out
+    if (one) o.gate_rows = o.T > 0 ? o.T : 1;
+    int64_t n = ((int64_t)o.T + o.gate_rows - 1) / o.gate_rows;
+    if (one && o.T == 0 && matrix(gate, "gate").size(0) == 1) n = 1;
+    o.gate = (const float*)dense(gate, "gate", at::kFloat, {n, o.d}, o.dev);
   }
   return o;
 }
@@ -263,7 +266,7 @@ PyObject* norm_gate_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                          make({o.d}, at::kFloat, o.dev), at::Tensor(), at::Tensor()};
     if (o.b1) out[3] = make({o.d}, at::kFloat, o.dev);
     if (o.b2) out[5] = make({o.d}, at::kFloat, o.dev);
-    if (o.gate || a[9] != Py_None) out[6] = at::empty_like(THPVariable_Unpack(a[9]));
+    if (o.gate || a[9] != Py_None) out[6] = o.T ? at::empty_like(THPVariable_Unpack(a[9])) : at::zeros_like(THPVariable_Unpack(a[9]));
     auto f = [&](int i) { return out[i].defined() ? (float*)out[i].data_ptr() : nullptr; };
     const c10::cuda::CUDAStream st = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)o.dev);
     int rc;

@@ -456,3 +456,21 @@ def test_in_place_has_to_be_a_truth_value():
     with pytest.raises(ValueError):
         ppu.ppu_norm_gate_fwd(y, r, g, g, in_place=np.zeros(2))
     assert torch.equal(r, was)
+
+
+@gpu
+@pytest.mark.parametrize("gate_rows", [0, 5])
+def test_no_rows_with_a_gate(gate_rows):
+    """One row of the gate for all rows is one row also for none of them; its gradient is a sum over nothing."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    y, r, s, g = (torch.zeros(0, n, device="cuda") for n in (64, 64, 4, 64))
+    g = torch.ones(64, device="cuda")
+    for rows in (0, 1) if gate_rows == 0 else (0,):
+        gate = torch.full((rows, 64), 3.0, device="cuda")
+        r_out, h, stats = ppu.ppu_norm_gate_fwd(y.bfloat16(), r, g, g, gate=gate, gate_rows=gate_rows)
+        assert r_out.shape == h.shape == (0, 64)
+        got = ppu.ppu_norm_gate_bwd(h, r, y.bfloat16(), r_out, stats, g, g, gate=gate, gate_rows=gate_rows)
+        assert got[6].shape == gate.shape and not got[6].any() and not got[2].any() and not got[4].any()
+    with pytest.raises(ppu.PpuError):
+        ppu.ppu_norm_gate_fwd(y.bfloat16(), r, g, g, gate=torch.ones(2, 64, device="cuda"), gate_rows=gate_rows)
