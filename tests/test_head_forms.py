@@ -323,6 +323,25 @@ def test_powers_beyond_the_common_reference_are_rounded_once(T, V):
     assert np.sqrt((rel ** 2).mean()) <= one * (np.sqrt(2) + np.sqrt(3)) / 2
 
 
+@gpu
+@pytest.mark.parametrize("grad", [True, False, "x", "e"])
+@pytest.mark.parametrize("T,d,V,k,chunk", [(300, 72, 1003, 9, 0), (700, 72, 1003, 9, 256), (24, 64, 33000, 64, 0), (3000, 72, 1003, 3, 0), (24, 40, 70000, 128, 0)])
+def test_whatever_the_workspace_held(T, d, V, k, chunk, grad):
+    """Workspaces of all ones (NaN) and of zeros: the same bits."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    rng, Xt, _, Et, _, target = make(T, d, V, seed=T)
+    ids, z = teacher(rng, T, V, k, target, True)
+    target[::3] = -1
+    tt, it, zt = on_device(target, ids, z)
+    grads = ppu._grads(grad)
+    for n, call in ((1, lambda ws: ppu.ppu_head_xent(Xt, Et, tt, grad=grad, chunk_rows=chunk, workspace=ws)),
+                    (k, lambda ws: ppu.ppu_head_distill(Xt, Et, it, zt, grad=grad, chunk_rows=chunk, workspace=ws))):
+        size = ppu.ppu_head_query_bytes(T, d, V, grads=grads, chunk_rows=chunk, k=n)
+        a, b = (call(torch.full((size,), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255))
+        assert all(x is y or torch.equal(x, y) for x, y in zip(a, b))
+
+
 # ---- refusals, on the host ----------------------------------------------------------------------
 def test_gradients_are_named_exactly():
     """A word that is none of those documented is refused, whatever letters it has."""

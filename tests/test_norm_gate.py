@@ -474,3 +474,33 @@ def test_no_rows_with_a_gate(gate_rows):
         assert got[6].shape == gate.shape and not got[6].any() and not got[2].any() and not got[4].any()
     with pytest.raises(ppu.PpuError):
         ppu.ppu_norm_gate_fwd(y.bfloat16(), r, g, g, gate=torch.ones(2, 64, device="cuda"), gate_rows=gate_rows)
+
+
+@gpu
+@pytest.mark.parametrize("T,d,gate_rows", [(300, 256, 300), (777, 64, 100), (1001, 1032, 1), (1500, 264, 7), (97, 4096, None), (350, 2104, 2 ** 31 - 1)])
+def test_whatever_the_workspace_held(T, d, gate_rows):
+    """Workspaces of all ones (NaN) and of zeros; a gate row for more rows than there are."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    c, t, *_ = make(T, d, "layer", True, gate_rows)
+    r_out, _, stats = call_fwd(c, t, gate_rows)
+    n = ppu.ppu_norm_gate_query_bytes(T, d, gate_rows or 0)
+    a, b = (call_bwd(c, t, r_out, stats, gate_rows, workspace=torch.full((n,), fill, dtype=torch.uint8, device="cuda")) for fill in (0, 255))
+    assert all(x is y or torch.equal(x, y) for x, y in zip(a, b))
+
+
+@gpu
+@pytest.mark.parametrize("which", ["b1", "b2"])
+@pytest.mark.parametrize("gate_rows", [None, 257, 1])
+def test_one_shift_alone(which, gate_rows):
+    """A shift of zeros in the place of one that is not there: the same bits, and no gradient for it."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    c, t, *_ = make(257, 264, "layer", True, gate_rows, seed=9)
+    some, zeros = dict(t, **{which: None}), dict(t, **{which: torch.zeros(264, device="cuda")})
+    a, b = call_fwd(c, some, gate_rows), call_fwd(c, zeros, gate_rows)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    a, b = call_bwd(c, some, a[0], a[2], gate_rows), call_bwd(c, zeros, b[0], b[2], gate_rows)
+    left_out = 3 if which == "b1" else 5
+    assert a[left_out] is None and b[left_out] is not None
+    assert all(torch.equal(x, y) for i, (x, y) in enumerate(zip(a, b)) if i != left_out and y is not None)
