@@ -307,8 +307,9 @@ int ppu_attention_bwd_static(const void* qkv, const void* U, const float* lse, c
  *
  * Softmax cross entropy, and distillation from a teacher's top logits, of hidden states X[T,d]
  * (bf16, row stride ldx) against a vocabulary matrix E[V,d] (bf16, row stride lde; the tied
- * embedding of this library's models), without holding the logits [T,V]: rows are worked in chunks
- * of chunk_rows, and a chunk's softmax is kept (bf16) only until its gradients are formed.  With
+ * embedding of this library's models).  Rows are worked in chunks of chunk_rows; a chunk's softmax is
+ * kept (bf16, in the workspace) only until its gradients are formed, so the logits of more rows than
+ * a chunk's never exist.  With
  * s = X E^T / temperature, lse_t = log sum_v exp s_tv and p = softmax(s):
  *   row_loss_t = sum_j q_tj (log q_tj - s_t,id(j) + lse_t),   loss = sum_t w_t row_loss_t
  *   dX = ds E / temperature, dE = ds^T X / temperature, ds_tv = w_t (Q_t p_tv - sum_{id(j)=v} q_tj)
@@ -326,11 +327,14 @@ int ppu_attention_bwd_static(const void* qkv, const void* U, const float* lse, c
  * loss: fp32 [1].  row_loss, lse: fp32 [T] or null.  dX: bf16 [T,d] (row stride lddx) or null; dE: bf16
  * [V,d] (row stride ldde) or null; both are written, not added to, and overlap no input.  d is a
  * multiple of 8 up to 16384, row strides multiples of 8, X, E, dX, dE 16-byte aligned; T <= 2^20,
- * V <= 2^22, any values within.  chunk_rows: 0 = up to 6144, as many as keep 1 GiB of softmax,
- * else the rows of a chunk (rounded up to a multiple of 256); chunks below 4096 rows are slower.  workspace: DEVICE, 256-byte
+ * V <= 2^22, any values within.  chunk_rows: 0 = up to 6144, as many as keep 1 GiB of softmax (256 at
+ * least: 2 GiB for V = 2^22), else the rows of a chunk (rounded up to a multiple of 256); chunks below 4096 rows
+ * are slower (6144 x 2048 x 32768: 4 % in two).  loss, row_loss and lse do not depend on chunk_rows; dX and dE do by the
+ * order of their sums, and by whether the other one is wanted.  workspace: DEVICE, 256-byte
  * aligned, of the size ppu_head_query_bytes gives for the same T, d, V, gradients (1: dX, 2: dE),
  * chunk_rows and k (entries a row; 1 for xent); calls that may overlap on the GPU need one each.  flags: DEVICE int32 [8], zeroed by the
- * caller once, or null (nothing is reported); read by ppu_op_status.  All other pointers DEVICE.
+ * caller once, or null: an id >= V is then left out, and results of an expired wait are returned, without
+ * a word; read by ppu_op_status.  All other pointers DEVICE.
  * Asynchronous on the stream; results do not depend on timing.  Sizes that are not 0 must not exceed
  * the buffers; the calls may be captured. */
 #define PPU_MAX_TEACHER_ENTRIES 128

@@ -1,6 +1,6 @@
-// Losses of hidden states against a large vocabulary that never hold the [T, V] logits: softmax
-// cross entropy and distillation from a teacher's top logits, with the gradients of the hidden
-// states and of the vocabulary matrix.
+// Losses of hidden states against a large vocabulary, worked in chunks of rows: softmax cross entropy and
+// distillation from a teacher's top logits, with the gradients of the hidden states and of the vocabulary
+// matrix.
 //
 //   s = X E^T / temperature,  lse_t = log sum_v exp(s_tv),  p = softmax(s)
 //   row loss = sum_j q_tj (log q_tj - s_t,id(j) + lse_t)        (cross entropy: one entry, q = 1)
@@ -9,7 +9,10 @@
 //
 // Three matrix products cannot be avoided (6 T V d operations), and a backward pass that forms the
 // logits again would make it four.  So rows are worked in chunks, whose softmax is kept only until
-// the chunk's two gradient products are done: a [rows, V] buffer of bounded size, not [T, V].
+// the chunk's two gradient products are done: a [rows, V] buffer of bounded size, not [T, V].  (Where one chunk is all, up
+// to 6144 rows, that is what bf16 logits would take, and with the running dE of two chunks 8192 x 2048 x 32768 takes
+// 571 MB where its logits are 537.  From there on it grows no further than to 726 MB, for 2^20 rows whose logits are 69 GB;
+// without dE 8192 rows take 285 MB, for the loss alone 17.)
 //   1. tcgen05 product of the chunk's rows with E^T.  Its epilogue works the vocabulary in pieces of 64
 //      columns: bf16 powers u = 2^(x - ref), x = s log2(e), and {ref, sum} in fp32; ref is 0 for ordinary
 //      logits (within 41 nats of 0), else the piece's maximum, as a whole number.  The entries' own x are kept in fp32 (the powers
@@ -493,9 +496,12 @@ join_partials_kernel(const float* part, int splits, int64_t stride, const float*
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-// A chunk by default: 6144 rows (8192 are worked as two of 4096), at most 1 GiB of powers.  The gradient
+// A chunk by default: 6144 rows (8192 are worked as two of 4096), at most 1 GiB of powers, but no fewer than 256 rows (2 GiB
+// for 2^22 ids).  The gradient
 // products lose efficiency below 4096 rows: 8192 x 2048 x 131072 takes 13.7 ms in chunks of 1024, 11.4 of
 // 2048, 10.5 of 4096 and of 8192.
+// (A few more than 6144 rows are two chunks of half as many: 3 % of 6400 x 2048 x 32768, 1.67 ms in one chunk and 1.72, and 2 %
+// of 8191 rows; 6144 take 1.60 in one, 1.67 in two.)
 constexpr int64_t USUAL_ROWS = 6144, U_BYTES = 1ll << 30;
 constexpr int SMS = 148;                      // work is split for a B200 (also where sizes are asked without a device)
 
@@ -530,7 +536,10 @@ void choose_splits(int64_t rows, int64_t d, int64_t V, int want, bool split_e, i
 }
 
 struct Plan {
-  int64_t ldu, n_pieces, chunk, usual;         // usual: rows of a chunk by default (decides orders of sums: results do not depend on chunk_rows)
+  // usual: rows of a chunk by default.  They decide the warps to a row, and so the order of a row's and of the loss's sums:
+  // loss, row losses and lse do not depend on chunk_rows.  (The gradients do, by the order of their sums: dE is added
+  // up over chunks, and the slices of dX go by the chunk's rows and by whether dE is wanted too.)
+  int64_t ldu, n_pieces, chunk, usual;
   int chunks, sx, se;                          // split-K factors of dX and dE
   int64_t ld_off;
   size_t off_weighted, off_factor, off_stats, off_x, off_ids, off_z, off_before, off_u, off_fx, off_acc, off_part_x, off_part_e, bytes;

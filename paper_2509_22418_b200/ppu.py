@@ -347,6 +347,8 @@ def ppu_attention_bwd_static(qkv, U, lse, dU, batch, seq, n_head, d_head, backen
 
 
 # ---- losses of hidden states against the vocabulary ------------------------------------------
+# These and the norm pair take their operands as values: where one requires a gradient, outputs carry no graph all the
+# same (a torch.autograd.Function calls the forward and the backward one).
 MAX_TEACHER_ENTRIES = 128
 NORM_LAYER, NORM_RMS = 0, 1
 _ops = None
@@ -395,10 +397,12 @@ def _grads(grad):
 
 def ppu_head_xent(X, E, target, row_weight=None, grad=True, chunk_rows=0, workspace=None, flags=None):
     """Softmax cross entropy of hidden states X [T, d] against the vocabulary matrix E [V, d] (bf16;
-    rows may be strided), without the logits.  target: int32 [T], negative: the row does not
+    rows may be strided), in chunks of rows: the logits of more rows than a chunk's never exist.  target: int32 [T], negative: the row does not
     count.  row_weight: fp32 [T], or None for the mean over the rows that count.  grad: True, False, or "x" /
     "e" for one gradient only (E frozen, X frozen).  workspace: uint8 tensor of ppu_head_query_bytes, or None.
-    Returns (loss, row_loss [T], lse [T], dX, dE).  flags: int32 [8] zeros for ppu_op_status."""
+    Returns (loss, row_loss [T], lse [T], dX, dE).  flags: int32 [8] zeros, which ppu_op_status reads later.  Without flags NOTHING
+    is reported: rows whose id is V or more are left out as if they had none, and results are returned, though not
+    valid, where a bounded wait inside a kernel ran out."""
     return (_ops or _binding()).head_xent(X, E, target, row_weight, _grads(grad), chunk_rows, workspace, flags)
 
 
@@ -408,7 +412,7 @@ def ppu_head_distill(X, E, teacher_ids, teacher_logits, temperature=1.0, teacher
     (negative: absent) and teacher_logits fp32 [T, k]; teacher_lse fp32 [T]: the log-sum-exp of all of the
     teacher's logits / temperature, or None for the softmax over the k entries.  Loss and gradients are those of
     sum_j q_j (log q_j - log p_j); multiply row_weight by temperature ** 2 for gradients of the
-    same size at every temperature.  The rest as ppu_head_xent."""
+    same size at every temperature.  The rest, flags among it, as ppu_head_xent."""
     return (_ops or _binding()).head_distill(X, E, teacher_ids, teacher_logits, temperature, teacher_lse, row_weight, _grads(grad), chunk_rows,
                                              workspace, flags)
 
