@@ -366,8 +366,9 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
           a.weighted[t] = w * l;
         }
         if (GRAD) {
-          // what the entries' places are to hold: (p - q / Q) all.s.  With p = exp(x): (exp(x) - 1) + (1 - q / Q)
-          // keeps its digits where p is next to 1.  An id given twice: its first entry stands for all.
+          // what the entries' places are to hold: (p - q / Q) all.s.  With p = 2^x: (2^x - 1) + (1 - q / Q) keeps its
+          // digits where p is next to 1, the difference itself where p and q are small (formed through 1, it was off by 6e-8 of
+          // the row: more than entries of 1e-7 have).  An id given twice: its first entry stands for all.
           for (int j = lane; j < k; j += 32) {
             const int id = s_id[g][j];
             const float2 e = s_x[g][j];
@@ -375,7 +376,9 @@ __global__ void __launch_bounds__(W == 1 ? 128 : 32 * W) head_rows_kernel(const 
             if (id >= 0 && total != 0.f && !(j > 0 && s_id[g][j - 1] == id)) {
               float q = 0.f;
               for (int i = j; i < k && s_id[g][i] == id; ++i) q += s_q[g][i];
-              v = (expm1f(((e.y - ref) + e.x - log_s) * LN2) + (total - q) / total) * all.s;
+              const float u = (e.y - ref) + e.x, x = u - log_s;
+              if (x < -1.f) v = fmaf(-q / total, all.s, exp2f(u));
+              else v = (expm1f(x * LN2) + (total - q) / total) * all.s;
             }
             s_v[g][j] = v;
           }

@@ -42,6 +42,40 @@ def on_device(*arrays):
     return [torch.from_numpy(a).cuda() for a in arrays]
 
 
+@gpu
+@pytest.mark.parametrize("T,V", [(64, 2048), (24, 33000)])       # one warp to a row, several
+def test_entries_of_little_weight_keep_their_digits(T, V):
+    """Gradients of entries that teacher and student both give 1e-5 to 1e-10: relative to their own size.  E's columns as
+    above, so that dX[t, c] is ds of one id: its place (or power), the row's factor and the result are off by half a step
+    each; where p and q are not within a factor 5 / 3 of one another their difference has at most four times
+    the relative errors of theirs, from logits below 16 ((128 / 16 + 8) 2^-23 16 each, and of their
+    sum) and a handful of roundings of q's logit below 32: 4 (2 * 3.1e-5 + 8 * 32 * 2^-24) < 2^-11."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    d, k = 128, 64
+    rng = np.random.default_rng(V + 1)
+    E = np.zeros((V, d))
+    E[:, 1] = np.clip(3.0 * rng.standard_normal(V), -14, 14)
+    at = rng.permutation(V)[: d - 2]
+    E[at, np.arange(2, d)] = 1.0
+    Et, E = bf16(E)
+    x = np.zeros((T, d))
+    x[:, 1] = rng.uniform(0.9, 1.1, T)
+    Xt, X = bf16(x)
+    ids = np.array([rng.permutation(at)[:k] for _ in range(T)]).astype(np.int32)
+    z = np.clip(5.0 * rng.standard_normal((T, k)), -15, 15).astype(np.float32)
+    ii, q, ent, _ = soft(ids, z, 1.0, None)
+    R = definition(X, E, ii, q, ent, np.ones(T), 1.0)
+    got = ppu.ppu_head_distill(Xt.cuda(), Et.cuda(), *on_device(ids, z), row_weight=torch.ones(T, device="cuda"))
+    full = np.zeros((T, V))
+    np.put_along_axis(full, ii, q, 1)
+    p, full, ds = R["p"][:, at], full[:, at], R["ds"][:, at]
+    clear = np.abs(p - full) >= 0.25 * (p + full)
+    assert (clear & (full > 0) & (p + full < 1e-6)).sum() > 2 * T
+    rel = np.abs(got[3].double().cpu().numpy()[:, 2:] / ds - 1)[clear]
+    assert rel.max() <= 3 * 2.0 ** -8 * (1 + 2.0 ** -7) + 2.0 ** -11
+
+
 # Warps to a row of the row kernel: one up to some 16 thousand ids or for thousands of rows, else 4, or 16 for few rows
 # of more than 64 thousand ids.
 SEVERAL_WARPS = [(24, 33000), (400, 33000), (24, 70000)]
