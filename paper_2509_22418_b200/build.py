@@ -74,10 +74,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose:
             cmd.insert(1, "-Xptxas=-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    with_ops = _torch_dir() is not None
+    with_ops, failed = _torch_dir() is not None, []
     if with_ops:
-        procs.append(("bind.cpp", subprocess.Popen(_ops_compile(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    failed = []
+        try:
+            procs.append(("bind.cpp", subprocess.Popen(_ops_compile(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+        except OSError as e:               # no such compiler
+            sys.stderr.write(f"--- bind.cpp\n{e}\n")
+            failed.append("bind.cpp")
     for src, p in procs:
         out = p.communicate()[0].decode()
         if p.returncode != 0 or verbose:

@@ -89,3 +89,12 @@ def test_built_again_for_another_torch(tree):
     n = tree.runs()
     tree.build()
     assert tree.runs() == n
+
+
+def test_library_without_a_compiler_for_the_binding(tree, monkeypatch):
+    tools = os.path.dirname(os.environ["NVCC"])
+    os.remove(os.path.join(tools, "g++"))
+    monkeypatch.setenv("PATH", tools)
+    with pytest.raises(RuntimeError, match="bind.cpp"):
+        tree.build()
+    assert os.path.exists(tree.LIB) and not os.path.exists(tree.OPS)
