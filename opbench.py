@@ -42,6 +42,7 @@ def main():
     ap.add_argument("--head-slices", type=int, default=0, help="path: MLP + head slicing with this many head groups")
     ap.add_argument("--teacher", type=int, default=0)
     ap.add_argument("--grad", choices=["xe", "x", "e", "none"], default="xe", help="head: gradients (x: the vocabulary matrix is frozen)")
+    ap.add_argument("--no-grad", dest="grad", action="store_const", const="none")
     ap.add_argument("--chunk-rows", type=int, default=0, help="head: rows of a chunk")
     ap.add_argument("--rms", action="store_true")
     ap.add_argument("--gate-rows", type=int, default=0, help="norm: rows that share a row of the gate (0: all of them)")
