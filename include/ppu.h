@@ -387,6 +387,76 @@ int ppu_norm_gate_bwd(const void* dh, const float* dr_out, const void* y, const 
                       float* dpre_shift, float* dgate, int T, int d, void* workspace,
                       size_t workspace_bytes, void* cuda_stream);
 
+/* ---- embedding lookup and the table's gradient -----------------------------------------
+ *
+ *   out[t] = scale E[id_t]          dE[v] = add[v] + scale sum over t with id_t = v of dout[t]
+ * for token ids [T] (int32) and a table E[V,d].  Negative ids are absent: a row of zeros, no gradient.  Ids >= V are left
+ * out in the same way and set flags[0] (flags as for the head losses, may be null: without a word).  E, out, dout, add and
+ * dE are of the ppu_type given (add of dE's), rows may be strided (lde, ldo ...: multiples of 8); sums are fp32, in a fixed order, rounded
+ * once.  add is a gradient that dE is formed on top of, such as the one of a tied head (ppu_head_xent's dE), or null; it may
+ * be dE itself, whose rows without tokens are then not touched.  All rows of out and dE are written; they overlap no other operand.
+ * d is a multiple of 8 up to 16384, T <= 2^20, V <= 2^22, any values within; operands 16-byte aligned.  workspace:
+ * DEVICE, 256-byte aligned, the size ppu_embed_query_bytes gives for the same T, d and V; calls that may overlap on the GPU need one
+ * each.  All pointers DEVICE.  Asynchronous on the stream; the calls may be captured. */
+typedef enum { PPU_BF16 = 0, PPU_F32 = 1 } ppu_type;
+int ppu_embed_fwd(const int32_t* ids, const void* E, int64_t lde, int e_type, float scale, void* out, int64_t ldo,
+                  int out_type, int T, int d, int V, int32_t* flags, void* cuda_stream);
+int ppu_embed_query_bytes(int T, int d, int V, size_t* bytes);
+int ppu_embed_bwd(const int32_t* ids, const void* dout, int64_t ldd, int dout_type, float scale, const void* add,
+                  int64_t ldadd, void* dE, int64_t ldde, int grad_type, int T, int d, int V, void* workspace,
+                  size_t workspace_bytes, int32_t* flags, void* cuda_stream);
+
+/* ---- norms of queries and keys for each head, with the rotation by position --------------
+ *
+ * On rows [n_q query heads | n_k key heads | n_v value heads] of d_head columns each (bf16, the packed operand that
+ * ppu_attention_fwd reads where n_q = n_k = n_v):
+ *   query and key heads x: y = R(position) (N(x) gain);   value heads are copied.
+ * kind: N is LayerNorm or RMSNorm of the head, with eps added to the mean square.  Gains: fp32 [d_head], shared by the heads,
+ * or [n_q, d_head] and [n_k, d_head] with gain_per_head; null: ones.  R turns the pairs of the first rot_dim columns (a multiple of 8, 0:
+ * none) by position * f_i: (a, b) -> (a cos - b sin, a sin + b cos), where pair i is columns (2i, 2i + 1) (PPU_PAIRS_ADJACENT, the
+ * order of this library's models) or (i, i + rot_dim / 2) (PPU_PAIRS_HALVES), and f_i = rope_base^(-2i / rot_dim) or inv_freq[i]
+ * (fp32 [rot_dim / 2]).  positions: int32 [T], or null: t mod seq (seq 0: t).  Angles are formed in 64 bits.
+ * out may be qkv itself (the values then stay where they are).
+ *
+ * Backward: from dout, the gradient of the result, and the qkv that the forward pass was given: dqkv (may be dout itself; the values'
+ * part is copied), and summed over tokens (and over heads that share a gain) dq_gain and dk_gain (fp32, the gains' shapes, or null).
+ * Nothing else is saved.  Sums have a fixed order.  All are written, not added to.
+ * d_head is a multiple of 8 up to 256; at most 4096 heads of a kind, one of them a query or a key; row strides are multiples of 8; bf16 operands
+ * and gains 16-byte aligned.  workspace: DEVICE, 16-byte aligned, the size ppu_qk_norm_query_bytes gives, only read where a gain's gradient is
+ * wanted; calls that may overlap on the GPU need one each.  All pointers DEVICE.  Asynchronous; may be captured. */
+enum { PPU_PAIRS_ADJACENT = 0, PPU_PAIRS_HALVES = 1 };
+int ppu_qk_norm_fwd(const void* qkv, int64_t ldx, const float* q_gain, const float* k_gain, int gain_per_head,
+                    const int32_t* positions, int seq, int kind, float eps, float rope_base, const float* inv_freq,
+                    int rot_dim, int pairs, void* out, int64_t ldo, int T, int n_q, int n_k, int n_v, int d_head,
+                    void* cuda_stream);
+int ppu_qk_norm_query_bytes(int T, int n_q, int n_k, int n_v, int d_head, int gain_per_head, size_t* bytes);
+int ppu_qk_norm_bwd(const void* dout, int64_t ldy, const void* qkv, int64_t ldx, const float* q_gain,
+                    const float* k_gain, int gain_per_head, const int32_t* positions, int seq, int kind, float eps,
+                    float rope_base, const float* inv_freq, int rot_dim, int pairs, void* dqkv, int64_t ldo,
+                    float* dq_gain, float* dk_gain, int T, int n_q, int n_k, int n_v, int d_head, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream);
+
+/* ---- orthogonalised update of matrices ---------------------------------------------------
+ *
+ * For `batch` matrices G[m,n] (ppu_type g_type; strides in elements: ldg of rows, stride_g of matrices, so that the same
+ * matrix of every layer of the canonical vector is one call):
+ *   m' = beta momentum + weight G;  u = nesterov ? weight G + beta m' : m'    (momentum null: u = G)
+ *   X = u / (|u|_F + eps);  steps times, with the step's (a, b, c):  A = X X^T, X = a X + (b A + c A A) X;  O = scale X
+ * (A = X^T X and X = a X + X (b A + c A A) for m > n, which is the same).  With the usual coefficients (3.4445, -4.7750, 2.0315) five
+ * steps bring singular values above 0.003 of |u|_F to between 0.7 and 1.2: the update of the Muon optimiser.
+ * momentum, momentum_out: fp32, strides of their own, momentum_out may be momentum itself.  coef: HOST fp32, n_coef = 1 triple or one for each
+ * step; coefficients that would take singular values above 2.8 are refused.  O: bf16 [batch, m, n] contiguous.
+ * The products' operands are fp16 and X is carried in 22 bits: O's root mean square error, beside its rounding, is below 2.5e-3 of its root mean
+ * square.  Entries of X below 2^-47 are lost.  A matrix of zeros gives zeros; one with a value that is not finite gives NaN throughout.
+ * Sides up to 65536, steps up to 32.  workspace: DEVICE, 256-byte aligned, the size ppu_orthogonalize_query_bytes gives; calls that may overlap
+ * on the GPU need one each.  flags as for the head losses (PPU_ETIMEOUT alone), may be null.  Other pointers DEVICE, O 16-byte aligned.
+ * Asynchronous on the stream; may be captured; the same inputs give the same bits. */
+int ppu_orthogonalize_query_bytes(int batch, int m, int n, int steps, size_t* bytes);
+int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, int g_type, const float* momentum, int64_t ldm,
+                      int64_t stride_m, float* momentum_out, int64_t ldmo, int64_t stride_mo, float beta, float weight,
+                      int nesterov, const float* coef, int n_coef, int steps, float eps, float scale, void* O, int batch,
+                      int m, int n, void* workspace, size_t workspace_bytes, int32_t* flags, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libppu.so")
 OPS = os.path.join(HERE, "_ops.so")
 SOURCES = ["ppu_api.cu", "ppu_step.cu", "elementwise.cu", "optim.cu", "gemm_simt.cu",
            "gemm_tc.cu", "gemm_tc_pair.cu", "attention_simt.cu", "attention_tc.cu", "attention_static.cu", "wait_probe.cu",
-           "head_loss.cu", "norm_gate.cu"]
+           "head_loss.cu", "norm_gate.cu", "embed.cu", "qk_norm.cu", "orthogonalize.cu"]
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
          "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

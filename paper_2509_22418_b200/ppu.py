@@ -347,7 +347,7 @@ def ppu_attention_bwd_static(qkv, U, lse, dU, batch, seq, n_head, d_head, backen
 
 
 # ---- losses of hidden states against the vocabulary ------------------------------------------
-# These and the norm pair take their operands as values: where one requires a gradient, outputs carry no graph all the
+# These and the operators below take their operands as values: where one requires a gradient, outputs carry no graph all the
 # same (a torch.autograd.Function calls the forward and the backward one).
 MAX_TEACHER_ENTRIES = 128
 NORM_LAYER, NORM_RMS = 0, 1
@@ -460,3 +460,96 @@ def ppu_norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shi
     dgate); those of absent operands are None."""
     return (_ops or _binding()).norm_gate_bwd(dh, dr_out, y, r_out, stats, post_gain, pre_gain, post_shift, pre_shift, gate, gate_rows, _kind(kind),
                                               res_scale, workspace)
+
+
+# ---- embedding lookup and the table's gradient -----------------------------------------------
+_TYPES = {"bf16": 0, "fp32": 1}
+
+
+def _dtype(word):
+    if word not in _TYPES:
+        raise PpuError(-1, f"dtype must be one of {sorted(_TYPES)}, got {word!r}")
+    return _TYPES[word]
+
+
+def ppu_embed_fwd(ids, E, scale=1.0, dtype="fp32", flags=None):
+    """out[t] = scale E[ids[t]] for ids [T] (int32) and the table E [V, d] (bf16 or fp32; rows may be strided).  Negative ids
+    are absent and give a row of zeros; ids of V or more as well, which ppu_op_status reports from flags (int32 [8] zeros; without them
+    nothing is reported).  dtype: the result's, "fp32" (the residual stream) or "bf16".  Returns out [T, d]."""
+    return (_ops or _binding()).embed_fwd(ids, E, scale, _dtype(dtype), flags)
+
+
+def ppu_embed_query_bytes(T, d, V) -> int:
+    """Bytes of workspace of ppu_embed_bwd."""
+    n = C.c_size_t(0)
+    _check(lib().ppu_embed_query_bytes(*_int32(T, d, V), C.byref(n)))
+    return n.value
+
+
+def ppu_embed_bwd(ids, dout, V, scale=1.0, dtype=None, add=None, in_place=False, workspace=None, flags=None):
+    """The table's gradient, dE[v] = add[v] + scale sum of dout[t] over the tokens with ids[t] = v, from dout [T, d] (bf16 or fp32; rows may be
+    strided); sums are fp32 in a fixed order.  dtype: dE's, "bf16" (the default) or "fp32".  add [V, d], of that type: a gradient to form it on top
+    of, such as ppu_head_xent's dE of a tied table; in_place: dE is add, whose rows without tokens are not touched (refused where add
+    requires a gradient and gradients are recorded).  workspace: uint8 tensor of ppu_embed_query_bytes, or None.  Ids as ppu_embed_fwd.
+    Returns dE [V, d]."""
+    return (_ops or _binding()).embed_bwd(ids, dout, V, scale, -1 if dtype is None else _dtype(dtype), add, in_place, workspace, flags)
+
+
+# ---- norms of queries and keys for each head, with the rotation by position ------------------
+PAIRS_ADJACENT, PAIRS_HALVES = 0, 1
+_PAIRS = {"adjacent": PAIRS_ADJACENT, "halves": PAIRS_HALVES}
+
+
+def _pairs(pairs):
+    if pairs not in _PAIRS:
+        raise PpuError(-1, f"pairs must be one of {sorted(_PAIRS)}")
+    return _PAIRS[pairs]
+
+
+def ppu_qk_norm_fwd(qkv, n_q, n_k, n_v, q_gain=None, k_gain=None, positions=None, seq=0, kind="rms", eps=1e-6, rope_base=1e4, inv_freq=None,
+                    rot_dim=None, pairs="adjacent", in_place=False):
+    """Norms each query and key head of qkv [T, (n_q + n_k + n_v) d_head] (bf16; rows may be strided), multiplies by its gain and rotates it by
+    position; value heads are copied.  kind "rms" or "layer"; gains fp32 [d_head], shared by the heads, or [heads, d_head], or None (ones).
+    positions int32 [T], or None: t mod seq (seq 0: t).  The first rot_dim columns of a head (None: all) are rotated, "adjacent" pairs (2i, 2i + 1) or
+    "halves" (i, i + rot_dim / 2), by position rope_base ** (-2i / rot_dim), or position inv_freq[i] (fp32 [rot_dim / 2]).  in_place: the
+    result is qkv (refused where it requires a gradient and gradients are recorded).  With n_q = n_k = n_v the result is what
+    ppu_attention_fwd reads."""
+    return (_ops or _binding()).qk_norm_fwd(qkv, n_q, n_k, n_v, q_gain, k_gain, positions, seq, _kind(kind), eps, rope_base, inv_freq, rot_dim, _pairs(pairs), in_place)
+
+
+def ppu_qk_norm_query_bytes(T, n_q, n_k, n_v, d_head, gain_per_head=False) -> int:
+    """Bytes of workspace of ppu_qk_norm_bwd."""
+    n = C.c_size_t(0)
+    _check(lib().ppu_qk_norm_query_bytes(*_int32(T, n_q, n_k, n_v, d_head), int(bool(gain_per_head)), C.byref(n)))
+    return n.value
+
+
+def ppu_qk_norm_bwd(dout, qkv, n_q, n_k, n_v, q_gain=None, k_gain=None, positions=None, seq=0, kind="rms", eps=1e-6, rope_base=1e4, inv_freq=None,
+                    rot_dim=None, pairs="adjacent", in_place=False, workspace=None):
+    """Gradients of ppu_qk_norm_fwd from dout (shape of qkv, bf16; what ppu_attention_bwd returns) and the qkv it was given (not its
+    result).  in_place: dqkv is dout.  Returns (dqkv, dq_gain, dk_gain); those of absent gains are None."""
+    return (_ops or _binding()).qk_norm_bwd(qkv, n_q, n_k, n_v, q_gain, k_gain, positions, seq, _kind(kind), eps, rope_base, inv_freq, rot_dim, _pairs(pairs), dout,
+                                            in_place, workspace)
+
+
+# ---- orthogonalised update of matrices --------------------------------------------------------
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def ppu_orthogonalize_query_bytes(batch, m, n, steps=5) -> int:
+    """Bytes of workspace of ppu_orthogonalize."""
+    k = C.c_size_t(0)
+    _check(lib().ppu_orthogonalize_query_bytes(*_int32(batch, m, n, steps), C.byref(k)))
+    return k.value
+
+
+def ppu_orthogonalize(G, momentum=None, beta=0.95, weight=1.0, nesterov=True, steps=5, coef=NEWTON_SCHULZ, eps=1e-7, scale=1.0, in_place=False, workspace=None,
+                      flags=None):
+    """The update of matrices G [m, n] or [batch, m, n] (bf16 or fp32; rows and matrices may be strided: one matrix of every layer of a parameter
+    vector is a batch) whose singular values are brought to about one: m' = beta momentum + weight G, u = weight G + beta m' (nesterov) or m'
+    (without a momentum u = G); X = u / (|u| + eps); `steps` times A = X X^T, X = a X + (b A + c A A) X; O = scale X.  coef: (a, b, c), or a
+    sequence of one such triple for each step.  momentum fp32, G's shape; in_place: m' is written over it (refused where it requires a gradient
+    and gradients are recorded).  flags: int32 [8] zeros for ppu_op_status, which reports a bounded wait inside a kernel that ran out; without them the
+    result is returned, though not valid.  Returns (O bf16, m' fp32 or None)."""
+    flat = coef if coef is NEWTON_SCHULZ else tuple(float(x) for c in coef for x in (c if hasattr(c, "__len__") else (c,)))
+    return (_ops or _binding()).orthogonalize(G, momentum, beta, weight, nesterov, flat, steps, eps, scale, in_place, workspace, flags)
