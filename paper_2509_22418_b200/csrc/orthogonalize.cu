@@ -7,13 +7,15 @@
 // for matrices with more rows than columns A = X^T X and X = a X + X P, so that A and P are of the shorter side.
 //
 // Numbers.  The products' operands are fp16 (11 bits; bf16 has 8) times powers of two that keep |X| <= 2.8 below the
-// largest and 2^-26 above the smallest normal number; sums are fp32.  X itself is carried as a pair of fp16 (22 bits), and
-// a X is formed from the pair: rounding X leaves noise in directions whose singular values are small, and the polynomial multiplies
+// largest and 2^-26 above the smallest normal number; sums are fp32.  X itself is carried in fp32 beside its fp16 copy, and
+// a X is formed from that: rounding X leaves noise in directions whose singular values are small, and the polynomial multiplies
 // those by a = 3.4 a step, noise included.  Root mean square error of O relative to O's (5 steps, CPU model): bf16
 // operands and X 1e-2 for random matrices, 0.16 to 0.35 for those with a few large directions; fp16 operands and X 1.3e-3
-// and 2e-2 to 4e-2; with the pair 1.4e-3 and 2e-4 to 5e-4.  P X needs no pair: b A + c A A is small where X is.
+// and 2e-2 to 4e-2; with X in fp32 1.4e-3 and 2e-4 to 5e-4.  P X needs no more: b A + c A A is small where X is.
 //
-// A and A A are symmetric: tiles on and below the diagonal are worked and stored on both sides.
+// A and A A are symmetric: only tiles on and below the diagonal are worked and stored; a block above it is read as its
+// mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
+// the columns, a tile of 128 x 128 took 7 us more.)
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>
@@ -29,26 +31,36 @@ using gemm_tc_detail::UMMA_K;
 using gemm_tc_detail::ld_v8;
 using gemm_tc_detail::st_v8;
 
-constexpr int X_EXP = 12, A_EXP = 12, LO_EXP = 11;      // powers of two: X, A as stored; the pair's second number over its first
+constexpr int X_EXP = 12, A_EXP = 12;                 // powers of two of X and A as stored
 constexpr int SMS = 148, MAX_STEPS = 32, MAX_SIDE = 1 << 16;
 enum Mode { GRAM = 0, POLY = 1, UPDATE = 2 };
 
-struct GemmP {
-  int M, N, K, batch;
-  int tiles_m, tiles_n, tiles;       // tiles of a matrix (on and below the diagonal where the product is symmetric)
-  __half* C; int64_t ldc, stride;    // GRAM, POLY: the symmetric result
-  const __half* A; float b, c;       // POLY: C = b A + c acc, factors with the powers of two
-  const __half *hi; __half* lo;      // UPDATE: X as a pair (its second number is replaced in place)
-  float a, f;                        // X' = a X + f acc
-  __half* hi_out;                    // null: the last step, O = scale X'
-  bf16* O; int64_t ldo; float scale;
+constexpr int EPI = 8;                               // epilogue warps (16 of half the registers: 8192 x 2048 852 us for 741)
+constexpr int KH = 2, BOX = 128 * BK * 2;             // 64-k slabs of a stage; bytes of a box of 64 x 128
+constexpr int STAGES = 3, STAGE_BYTES = 2 * KH * BOX; // a CTA's share of a stage: 128 rows of A, 128 of B, 128 k
+constexpr int BUF_WORDS = 32 * 9;                     // an epilogue warp's
+constexpr int SMEM = STAGES * STAGE_BYTES + EPI * BUF_WORDS * 4 + 1024 + 256;
+constexpr int BLOCK = 64 + 32 * EPI;
+constexpr unsigned long long WAIT_NS = 2000000000ull; // a wait gives up after two seconds
+
+struct KernelP {
+  int m, n, side, batch, steps, left;
+  int tiles_s, sym;                  // tiles along the shorter side, on and below the diagonal
+  int tiles_m, tiles_n, n_fast;      // of X
+  int splits[2];                     // slices of the sum of A, of A A
+  int units[3];                      // units of a matrix
+  int tail_from;                     // tiles of X from here on are worked in two halves of their columns
+  int per_step;
+  __half *A, *P, *hi[2]; int64_t ld, lds;      // operands, by rows
+  float* X; __half* A2;              // X and A as their epilogues read and write them again: 32 x 32 blocks (block_at)
+  int rows32, cols32, side32;        // blocks along X's sides, along the shorter one
+  bf16* O; float scale;
+  float gram;                        // A = gram * its accumulator
+  float a[MAX_STEPS], b[MAX_STEPS], c[MAX_STEPS], f[MAX_STEPS];
+  float* partial;                    // slices' sums
+  unsigned *done, *arrived;          // [3][batch] warps that have finished; [2][batch][sym][CTAs][EPI] slices that have left their sums
   int* flags;
 };
-
-// ---- the tile kernel: one CTA, 128 x 128 ----------------------------------------------------------
-constexpr int TM = 128, TN = 128, STAGES = 6, EPI = 8;
-constexpr int A_BYTES = TM * BK * 2, STAGE_BYTES = A_BYTES + TN * BK * 2;
-constexpr int SMEM = STAGES * STAGE_BYTES + 1024 + 256;
 
 __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -56,211 +68,443 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
 }
 __device__ __forceinline__ float2 half2_floats(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 
-// unit -> matrix and tile; symmetric products count (row, column <= row)
-struct Place { int b, i, j; };
-__device__ __forceinline__ Place place(int u, const GemmP& p, bool symmetric) {
-  Place w;
-  w.b = u / p.tiles;
-  const int t = u - w.b * p.tiles;
-  if (symmetric) {
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// waits with a limit in time: until a barrier's phase is over, until a counter has come to a value
+template <typename F>
+__device__ __forceinline__ bool wait_for(volatile int* abort_flag, int* flags, F ready) {
+  if (ready()) return true;
+  const unsigned long long t0 = now_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (ready()) return true;
+    if ((it & 255u) == 0) {
+      if (*abort_flag) return false;
+      if (now_ns() - t0 > WAIT_NS) break;
+    }
+  }
+  *abort_flag = 1;
+  if (flags) atomicExch(flags + PPU_FLAG_TIMEOUT, 1);
+  return false;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t saddr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// (PAIR: the two CTAs of a cluster on one 256 x 256 tile; else a CTA on 128 x 128)
+template <bool PAIR> __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+  if constexpr (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst), "l"(map), "r"(bar),
+                 "r"(x), "r"(y), "r"(z) : "memory");
+  else tma_load_3d(dst, map, bar, x, y, z);
+}
+template <bool PAIR> __device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (PAIR) {
+    const uint32_t z = 0;
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(z)
+                 : "memory");
+  } else {
+    umma_bf16(d, a, b, idesc, accumulate);
+  }
+}
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar) {
+  if constexpr (PAIR) {
+    const uint16_t mask = 3;
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
+  } else {
+    umma_commit(bar);
+  }
+}
+
+// ---- units -----------------------------------------------------------------------------------------
+// A step's units are all matrices' of A, then of P, then of X; CTAs (or pairs) take every n-th of them, step after step.
+// A unit waits for what it reads to be finished: A of the matrix for its X, P for its A, X for its P, each a counter.
+// A unit waits only for units that come before it, and all CTAs are resident (a cooperative launch) and work in order: so
+// there is always one that can go on.  The same waits order what is overwritten: A's tiles are written when X, and so P, of
+// the step before are done, P's when A is, X's other buffer when P is.
+struct Unit { int mode, b, i, j, split, splits, kb0, kb1, K, bn; };
+template <bool PAIR>
+__device__ __forceinline__ Unit unit_at(const KernelP& p, int r) {
+  constexpr int TILE = PAIR ? 256 : 128;
+  Unit w;
+  w.mode = GRAM;
+  if (r >= p.units[GRAM] * p.batch) { r -= p.units[GRAM] * p.batch; w.mode = POLY; }
+  if (w.mode == POLY && r >= p.units[POLY] * p.batch) { r -= p.units[POLY] * p.batch; w.mode = UPDATE; }
+  const int per = w.mode == GRAM ? p.units[GRAM] : w.mode == POLY ? p.units[POLY] : p.units[UPDATE];
+  w.b = r / per;
+  int t = r - w.b * per;
+  w.bn = TILE; w.split = 0; w.splits = 1;
+  w.K = w.mode == GRAM ? (p.left ? p.n : p.m) : p.side;
+  const int k_blocks = (w.K + KH * BK - 1) / (KH * BK);
+  w.kb0 = 0; w.kb1 = k_blocks;
+  if (w.mode != UPDATE) {
+    w.splits = w.mode == GRAM ? p.splits[0] : p.splits[1];
+    w.split = t % w.splits; t /= w.splits;
+    w.kb0 = (int)((int64_t)w.split * k_blocks / w.splits); w.kb1 = (int)((int64_t)(w.split + 1) * k_blocks / w.splits);
     int i = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     while (i * (i + 1) / 2 > t) --i;
-    w.i = i; w.j = t - i * (i + 1) / 2;
+    w.i = i * TILE; w.j = (t - i * (i + 1) / 2) * TILE;
   } else {
-    w.i = t % p.tiles_m; w.j = t / p.tiles_m;
+    int half = 0;
+    if (PAIR && t >= p.tail_from) { const int v = t - p.tail_from; t = p.tail_from + (v >> 1); half = v & 1; w.bn = TILE / 2; }
+    w.i = (p.n_fast ? t / p.tiles_n : t % p.tiles_m) * TILE;
+    w.j = (p.n_fast ? t % p.tiles_n : t / p.tiles_m) * TILE + half * (TILE / 2);
   }
   return w;
 }
+// the counter a unit waits for, and the value of it
+template <bool PAIR>
+__device__ __forceinline__ const unsigned* awaited(const KernelP& p, const Unit& w, int step, unsigned& value) {
+  constexpr unsigned EACH = (PAIR ? 2 : 1) * EPI;
+  const unsigned before = w.mode == GRAM ? (unsigned)step * p.units[UPDATE] : (unsigned)(step + 1) * p.units[w.mode - 1];
+  value = before * EACH;
+  return p.done + (w.mode == GRAM ? UPDATE : w.mode - 1) * p.batch + w.b;
+}
 
-// 32 columns from n on of row m (one to a lane)
-template <int MODE>
-__device__ __forceinline__ void finish(const GemmP& p, int b, int m, int n, bool mirror, const uint32_t* r) {
-  if (m >= p.M) return;
-  if constexpr (MODE != UPDATE) {
-    __half* row = p.C + b * p.stride + m * p.ldc + n;
-    uint32_t o[16];
-    if (MODE == GRAM) {
+// ---- 32 columns from n on of row m (one to a lane) ---------------------------------------------------
+// The 32 x 32 values of a warp in 1024 consecutive places: eight columns of row 0, of row 1, ... of row 31, the next eight columns.  A lane
+// takes 32 bytes at a time and the warp 1 KB (fp16: 16 and 512), where by rows it would touch 32 lines with each instruction: X of a tile
+// read so takes 1 us, by rows 9.
+__device__ __forceinline__ int64_t block_at(int b, int rows32, int cols32, int m, int n) { return (((int64_t)b * rows32 + m / 32) * cols32 + n / 32) * 1024; }
+// what a unit's result is made of beside the accumulator: A for P, X for X
+__device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int m0, int n, int lane, uint32_t* x) {
+  if (w.mode == POLY) {
+    if (m0 >= p.side) return;
+    const __half* src = p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane;
+    ld_v8(x, src); ld_v8(x + 8, src + 512);
+  } else if (w.mode == UPDATE) {
+    if (m0 >= p.m) return;
+    const float* src = p.X + block_at(w.b, p.rows32, p.cols32, m0, n) + 8 * lane;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] = half2_bits(p.c * __uint_as_float(r[2 * j]), p.c * __uint_as_float(r[2 * j + 1]));
+    for (int j = 0; j < 4; ++j) ld_v8(x + 8 * j, src + 256 * j);
+  }
+}
+// buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored 16 columns at a time
+__device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, uint32_t* buf, int lane) {
+  const int m = m0 + lane;
+  if (w.mode != UPDATE) {
+    if (m0 >= p.side) return;
+    uint32_t o[16];
+    if (w.mode == GRAM) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[j] = half2_bits(p.gram * __uint_as_float(r[2 * j]), p.gram * __uint_as_float(r[2 * j + 1]));
+      __half* again = p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane;
+      st_v8(again, o); st_v8(again + 512, o + 8);
     } else {
-      uint32_t x[16];
-      const __half* src = p.A + b * p.stride + m * p.ldc + n;
-      ld_v8(x, src); ld_v8(x + 8, src + 16);
+      const float b = p.b[step], c = p.c[step];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         const float2 v = half2_floats(x[j]);
-        o[j] = half2_bits(fmaf(p.c, __uint_as_float(r[2 * j]), p.b * v.x), fmaf(p.c, __uint_as_float(r[2 * j + 1]), p.b * v.y));
+        o[j] = half2_bits(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
       }
     }
-    st_v8(row, o); st_v8(row + 16, o + 8);
-    if (mirror) {
-      __half* col = p.C + b * p.stride + m;
+    if (m >= p.side) return;
+    __half* C = (w.mode == GRAM ? p.A : p.P) + ((int64_t)w.b * p.side + m) * p.lds + n;
+    st_v8(C, o); st_v8(C + 16, o + 8);
+    return;
+  }
+  if (m0 >= p.m) return;
+  const float a = p.a[step], f = p.f[step];
+  if (step + 1 < p.steps) {
+    uint32_t y[32], h[16];
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (n + j < p.N) col[(int64_t)(n + j) * p.ldc] = __ushort_as_half((unsigned short)(o[j / 2] >> (16 * (j & 1))));
-    }
+    for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(fmaf(f, __uint_as_float(r[j]), a * __uint_as_float(x[j])));
+    float* again = p.X + block_at(w.b, p.rows32, p.cols32, m0, n) + 8 * lane;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) st_v8(again + 256 * j, y + 8 * j);
+    if (m >= p.m) return;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) h[j] = half2_bits(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1]));
+    __half* hi = p.hi[(step + 1) & 1] + ((int64_t)w.b * p.m + m) * p.ld + n;
+    st_v8(hi, h); st_v8(hi + 16, h + 8);
+    return;
+  }
+  float y[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) y[j] = p.scale * fmaf(f, __uint_as_float(r[j]), a * __uint_as_float(x[j]));
+  if (p.n % 8 == 0) {
+    if (m >= p.m) return;
+    bf16* o = p.O + ((int64_t)w.b * p.m + m) * p.n + n;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (n + 8 * j < p.n) *reinterpret_cast<uint4*>(o + 8 * j) = gemm_tc_detail::pack8_bf16(y + 8 * j);
   } else {
-    const int64_t at = b * p.stride + m * p.ldc + n;
-    uint32_t h[16], l[16];
-    ld_v8(h, p.hi + at); ld_v8(h + 8, p.hi + at + 16);
-    ld_v8(l, p.lo + at); ld_v8(l + 8, p.lo + at + 16);
-    float y[32];
+    const int col = lane & 15;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const float2 a = half2_floats(h[j]), d = half2_floats(l[j]);
-      constexpr float s = 1.f / (1 << LO_EXP);
-      y[2 * j] = fmaf(p.f, __uint_as_float(r[2 * j]), p.a * fmaf(s, d.x, a.x));
-      y[2 * j + 1] = fmaf(p.f, __uint_as_float(r[2 * j + 1]), p.a * fmaf(s, d.y, a.y));
-    }
-    if (p.hi_out) {
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        h[j] = half2_bits(y[2 * j], y[2 * j + 1]);
-        const float2 a = half2_floats(h[j]);
-        l[j] = half2_bits((y[2 * j] - a.x) * (1 << LO_EXP), (y[2 * j + 1] - a.y) * (1 << LO_EXP));
-      }
-      st_v8(p.hi_out + at, h); st_v8(p.hi_out + at + 16, h + 8);
-      st_v8(p.lo + at, l); st_v8(p.lo + at + 16, l + 8);
-    } else {
-      bf16* o = p.O + ((int64_t)b * p.M + m) * p.ldo + n;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) y[j] *= p.scale;
-      if (p.N % 8 == 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n + 8 * j < p.N) *reinterpret_cast<uint4*>(o + 8 * j) = gemm_tc_detail::pack8_bf16(y + 8 * j);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) if (n + j < p.N) o[j] = __float2bfloat16_rn(y[j]);
-      }
+      for (int j = 0; j < 8; ++j) buf[lane * 9 + j] = gemm_tc_detail::pack2_bf16(y[16 * h + 2 * j], y[16 * h + 2 * j + 1]);
+      __syncwarp();
+      const int c = n + 16 * h + col;
+      if (c < p.n)
+        for (int i = lane >> 4; i < 32 && m0 + i < p.m; i += 2)
+          reinterpret_cast<unsigned short*>(p.O)[((int64_t)w.b * p.m + m0 + i) * p.n + c] = (unsigned short)(buf[i * 9 + col / 2] >> (16 * (col & 1)));
+      __syncwarp();
     }
   }
 }
 
-template <bool A_K, bool B_K, int MODE>
-__global__ void __launch_bounds__(64 + 32 * EPI, 1)
-ortho_tile_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ GemmP p) {
+// ---- all steps -----------------------------------------------------------------------------------------
+template <bool PAIR>
+__device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const KernelP& p) {
+  constexpr int CTAS = PAIR ? 2 : 1, TILE = 128 * CTAS;
   extern __shared__ uint8_t smem_raw[];
+  // (the window starts at the same offset in both CTAs of a pair, so aligned offsets match too)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
+  uint32_t* bufs = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(bufs + EPI * BUF_WORDS);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = PAIR ? cluster_rank() : 0;
   const uint32_t bar0 = smem_u32(bars);
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
   auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
   auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
+  auto leaders = [&](uint32_t bar) { return PAIR ? map_to_rank(bar, 0) : bar; };
+  auto wait_bar = [&](uint32_t bar, uint32_t parity) { return wait_for(abort_flag, p.flags, [&] { return mbar_try(bar, parity); }); };
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), EPI); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), CTAS * EPI); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 2 * TN);
+  if (warp == 1) {
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tmem_alloc(smem_u32(tmem_slot), 2 * TILE);
+    }
+  }
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();       // the peer's barriers are set up before anything signals them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  pdl_wait(); pdl_trigger();
+  pdl_wait();
 
-  const int units = p.tiles * p.batch, k_blocks = (p.K + BK - 1) / BK;
+  const int workers = gridDim.x / CTAS, worker = blockIdx.x / CTAS;
+  // calls f(step, unit) for this worker's units in order until it returns false
+  auto each_unit = [&](auto f) {
+    int r = worker;
+    for (int step = 0; step < p.steps;) {
+      if (r >= p.per_step) { r -= p.per_step; ++step; continue; }
+      if (!f(step, unit_at<PAIR>(p, r))) return;
+      r += workers;
+    }
+  };
+  // which operand's 128 x 128 blocks from k0 on are read in the order [k][rows]: X in A = X^T X and as the second operand of P X, and
+  // blocks of A and P above the diagonal
+  auto a_mn = [&](const Unit& w, int k0) { return w.mode == GRAM ? !p.left : (w.mode == POLY || p.left) && k0 / TILE > w.i / TILE; };
+  auto b_mn = [&](const Unit& w, int k0) { return w.mode == GRAM ? !p.left : w.mode == UPDATE && p.left ? true : k0 / TILE > w.j / TILE; };
   if (warp == 0) {
     if (lane == 0) {
-      // ---------------- TMA producer ----------------
-      asm volatile("fence.proxy.async.global;" ::: "memory");      // (the operands were written by plain stores)
+      // ---------------- TMA producer (each CTA: 128 rows of A, its half of B's) ----------------
       int s = 0; uint32_t ph = 0;
-      bool ok = true;
-      for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        const Place w = place(u, p, MODE != UPDATE);
-        for (int kb = 0; kb < k_blocks; ++kb) {
-          ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, p.flags);
-          if (!ok) break;
-          const uint32_t a_dst = smem_u32(smem + s * STAGE_BYTES), b_dst = a_dst + A_BYTES;
-          mbar_expect_tx(full_bar(s), STAGE_BYTES);
-          if (A_K) {
-            tma_load_3d(a_dst, &mapA, full_bar(s), kb * BK, w.i * TM, w.b);
-          } else {
+      each_unit([&](int step, const Unit& w) {
+        unsigned value;
+        const unsigned* counter = awaited<PAIR>(p, w, step, value);
+        if (!wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; })) return false;
+        asm volatile("fence.proxy.async.global;" ::: "memory");      // (the operands were written by plain stores)
+        const CUtensorMap* X = maps + (step & 1);
+        const CUtensorMap *mA = w.mode == GRAM ? X : w.mode == POLY ? maps + 2 : p.left ? maps + 3 : X;
+        const CUtensorMap *mB = w.mode == GRAM ? X : w.mode == POLY ? maps + 2 : p.left ? X : maps + 3;
+        const int a0 = w.i + (int)rank * 128, b_rows = w.bn / CTAS, b0 = w.j + (int)rank * b_rows;
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          if (!wait_bar(empty_bar(s), ph ^ 1u)) return false;
+          const uint32_t a_dst = smem_u32(smem + s * STAGE_BYTES), b_dst = a_dst + KH * BOX;
+          const uint32_t fb = leaders(full_bar(s));
+          const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;      // (the second slab may lie past the end of the sum)
+          // blocks [rows][k] come in a box for each slab of 64 k, blocks [k][rows] in one for each 64 rows, of 128 k
+          const bool amn = a_mn(w, k0), bmn = b_mn(w, k0);
+          const int a_boxes = amn ? 2 : slabs, b_boxes = bmn ? b_rows / 64 : slabs;
+          if (rank == 0) mbar_expect_tx(full_bar(s), CTAS * (a_boxes + b_boxes) * BOX);
 #pragma unroll
-            for (int j = 0; j < TM / 64; ++j) tma_load_3d(a_dst + j * 8192, &mapA, full_bar(s), w.i * TM + 64 * j, kb * BK, w.b);
+          for (int j = 0; j < 2; ++j) {
+            if (j >= a_boxes) break;
+            if (amn) load_box<PAIR>(a_dst + j * BOX, mA, fb, a0 + 64 * j, k0, w.b);
+            else load_box<PAIR>(a_dst + j * BOX, mA, fb, k0 + BK * j, a0, w.b);
           }
-          if (B_K) {
-            tma_load_3d(b_dst, &mapB, full_bar(s), kb * BK, w.j * TN, w.b);
-          } else {
 #pragma unroll
-            for (int j = 0; j < TN / 64; ++j) tma_load_3d(b_dst + j * 8192, &mapB, full_bar(s), w.j * TN + 64 * j, kb * BK, w.b);
+          for (int j = 0; j < 2; ++j) {
+            if (j >= b_boxes) break;
+            if (bmn) load_box<PAIR>(b_dst + j * BOX, mB, fb, b0 + 64 * j, k0, w.b);
+            else load_box<PAIR>(b_dst + j * BOX, mB, fb, k0 + BK * j, b0, w.b);
           }
           if (++s == STAGES) { s = 0; ph ^= 1u; }
         }
-      }
+        return true;
+      });
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       // ---------------- MMA issuer: D fp32, A and B fp16 ----------------
-      const uint32_t idesc = (1u << 4) | ((A_K ? 0u : 1u) << 15) | ((B_K ? 0u : 1u) << 16) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
       int s = 0; uint32_t ph = 0;
       int acc = 0; uint32_t acc_ph = 0;
-      for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        if (!mbar_wait(tempty_bar(acc), acc_ph ^ 1u, abort_flag, p.flags)) break;
+      each_unit([&](int, const Unit& w) {
+        const uint32_t idesc0 = (1u << 4) | ((uint32_t)(w.bn >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+        if (!wait_bar(tempty_bar(acc), acc_ph ^ 1u)) return false;
         tc_fence_after();
-        bool ok = true;
-        for (int kb = 0; kb < k_blocks; ++kb) {
-          ok = mbar_wait(full_bar(s), ph, abort_flag, p.flags);
-          if (!ok) break;
+        for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          if (!wait_bar(full_bar(s), ph)) return false;
           tc_fence_after();
-          const uint32_t a_addr = smem_u32(smem + s * STAGE_BYTES), b_addr = a_addr + A_BYTES;
+          const uint32_t a_addr = smem_u32(smem + s * STAGE_BYTES), b_addr = a_addr + KH * BOX;
+          const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;
+          const bool amn = a_mn(w, k0), bmn = b_mn(w, k0);
+          const uint32_t idesc = idesc0 | ((amn ? 1u : 0u) << 15) | ((bmn ? 1u : 0u) << 16);
+          const uint64_t ad = make_desc(a_addr, amn ? BOX : 16, 1024), bd = make_desc(b_addr, bmn ? BOX : 16, 1024);
+          // (steps of the descriptors' addresses, which stay below 2^14: from 16 k to 16 k, from slab to slab)
+          const uint32_t a_step = (amn ? 2048 : 32) >> 4, b_step = (bmn ? 2048 : 32) >> 4, a_slab = (amn ? 8192 : BOX) >> 4, b_slab = (bmn ? 8192 : BOX) >> 4;
 #pragma unroll
-          for (int k = 0; k < BK / UMMA_K; ++k) {
-            const uint64_t adesc = A_K ? make_desc(a_addr + k * 32, 16, 1024) : make_desc(a_addr + k * 2048, 8192, 1024);
-            const uint64_t bdesc = B_K ? make_desc(b_addr + k * 32, 16, 1024) : make_desc(b_addr + k * 2048, 8192, 1024);
-            umma_bf16(tmem_base + acc * TN, adesc, bdesc, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          for (int kh = 0; kh < KH; ++kh) {
+            if (kh >= slabs) break;
+#pragma unroll
+            for (int k = 0; k < BK / UMMA_K; ++k)
+              umma<PAIR>(tmem_base + (uint32_t)(acc * TILE), ad + kh * a_slab + k * a_step, bd + kh * b_slab + k * b_step, idesc, (kb > w.kb0 || kh > 0 || k > 0) ? 1u : 0u);
           }
-          umma_commit(empty_bar(s));
+          commit<PAIR>(empty_bar(s));
           if (++s == STAGES) { s = 0; ph ^= 1u; }
         }
-        if (!ok) break;
-        umma_commit(tfull_bar(acc));
+        commit<PAIR>(tfull_bar(acc));
         if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
-      }
+        return true;
+      });
     }
   } else {
-    // ---------------- epilogue warps: a quarter of the rows, half of the columns each ----------------
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    // ---------------- epilogue warps: a quarter of a CTA's rows, half of the columns each ----------------
+    const int quarter = warp & 3, half = (warp - 2) >> 2, me = warp - 2;
     int acc = 0; uint32_t acc_ph = 0;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-      const Place w = place(u, p, MODE != UPDATE);
-      if (!mbar_wait(tfull_bar(acc), acc_ph, abort_flag, p.flags)) break;
+    uint32_t* buf = bufs + me * BUF_WORDS;
+    each_unit([&](int step, const Unit& w) {
+      const int m0 = w.i + (int)rank * 128 + quarter * 32;
+      const int c0 = half * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
+      uint32_t x[32];
+      if (w.mode != GRAM) {                        // what other CTAs have written is read from here on
+        unsigned value;
+        const unsigned* counter = awaited<PAIR>(p, w, step, value);
+        const bool ok = lane > 0 || wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; });
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        if (w.splits == 1 && c0 < c1) fetch(p, w, m0, w.j + c0, lane, x);
+      }
+      if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       tc_fence_after();
-      const int m = w.i * TM + quarter * 32 + lane;
+      const uint32_t t_row = tmem_base + (uint32_t)(acc * TILE) + ((uint32_t)(quarter * 32) << 16);
+      // A tile in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
+      // up those of its own columns in the order of the slices.  (The slices of a tile are consecutive units, so that they are worked at the same time.)
+      auto mine = [&](int c) { return w.splits == 1 || c / 32 * w.splits / (w.bn / 32) == w.split; };
+      const int tile = w.i / TILE * (w.i / TILE + 1) / 2 + w.j / TILE;
+      const int64_t place = ((int64_t)w.b * p.sym + tile) * CTAS + rank;
+      const int64_t slice = (int64_t)128 * TILE / 4;      // in float4
+      float4* sums = reinterpret_cast<float4*>(p.partial) + place * w.splits * slice + me * (32 * (TILE / 2) / 4) + lane;
+      if (w.splits > 1) {
+        unsigned* arrived = p.arrived + ((w.mode == POLY ? (int64_t)p.batch * p.sym * CTAS : 0) + place) * EPI + me;
+        bool some = false;
 #pragma unroll 1
-      for (int c = half * (TN / 2); c < (half + 1) * (TN / 2); c += 32) {
-        const int n = w.j * TN + c;
-        if (n >= p.N) break;
-        uint32_t r[32];
-        tmem_ld32(tmem_base + acc * TN + c + ((uint32_t)(quarter * 32) << 16), r);
-        tmem_ld_wait();
-        finish<MODE>(p, w.b, m, n, MODE != UPDATE && w.i != w.j, r);
+        for (int c = c0; c < c1; c += 32) {
+          if (mine(c)) { some = true; continue; }
+          uint32_t r[32];
+          tmem_ld32(t_row + c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            sums[w.split * slice + ((c - c0) / 4 + j) * 32] =
+                make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
+        }
         __syncwarp();
+        bool ok = true;
+        if (lane == 0) {
+          asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
+          const unsigned all = (unsigned)(step + 1) * w.splits;
+          if (some) ok = wait_for(abort_flag, p.flags, [&] { return load_acquire(arrived) >= all; });
+        }
+        if (!__all_sync(0xffffffffu, ok)) return false;
+      }
+#pragma unroll 1
+      for (int c = c0; c < c1; c += 32) {
+        if (!mine(c)) continue;
+        const int n = w.j + c;
+        uint32_t r[32], next[32];
+        tmem_ld32(t_row + c, r);
+        if (w.splits > 1) fetch(p, w, m0, n, lane, x);
+        else if (c + 32 < c1) fetch(p, w, m0, n + 32, lane, next);
+        tmem_ld_wait();
+        if (w.splits > 1) {
+          float all[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) all[j] = 0.f;
+#pragma unroll 1
+          for (int q = 0; q < w.splits; ++q) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              float4 v = make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
+              if (q != w.split) v = __ldcg(sums + q * slice + ((c - c0) / 4 + j) * 32);
+              all[4 * j] += v.x; all[4 * j + 1] += v.y; all[4 * j + 2] += v.z; all[4 * j + 3] += v.w;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(all[j]);
+        }
+        finish(p, w, step, m0, n, r, x, buf, lane);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = next[j];
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(tempty_bar(acc));
+      if (lane == 0) {
+        if constexpr (PAIR) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(leaders(tempty_bar(acc))) : "memory");
+        else mbar_arrive(tempty_bar(acc));
+      }
+      asm volatile("fence.proxy.async.global;" ::: "memory");      // (read by copies of other CTAs)
+      __syncwarp();
+      if (lane == 0) {
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + w.mode * p.batch + w.b) : "memory");
+      }
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
-    }
+      return true;
+    });
   }
   // ---------------- common exit ----------------
   if (*abort_flag) {
-    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);      // copies and products in flight
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_sync_all();       // neither CTA leaves while its peer may still signal it
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, 2 * TN);
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    else tmem_dealloc(tmem_base, 2 * TILE);
   }
 }
+
+struct Maps { CUtensorMap m[4]; };                 // X (even steps), X (odd steps), A, P
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BLOCK, 1) ortho_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) {
+  ortho_steps<true>(maps.m, p);
+}
+__global__ void __launch_bounds__(BLOCK, 1) ortho_single_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) { ortho_steps<false>(maps.m, p); }
 
 // ---- momentum, norm and the first X ----------------------------------------------------------------
 struct PrepP {
@@ -270,8 +514,9 @@ struct PrepP {
   int rows, cols, nesterov, f32;
   float beta, w, eps, scale;
   double* partial;                                 // [batch][blocks]
-  __half *hi, *lo; int64_t ld;
+  __half* hi; int64_t ld; float* X; int rows32, cols32;
   bf16* O;                                         // no steps: scale X
+  unsigned* counters; int n_counters;              // set to 0
 };
 
 // four columns of a row from column c on; what lies behind the row's end is 0.  VEC: rows are whole fours, aligned
@@ -291,28 +536,43 @@ __device__ __forceinline__ float4 weigh(float s, const float4 a, float t, const 
   return make_float4(fmaf(s, a.x, t * b.x), fmaf(s, a.y, t * b.y), fmaf(s, a.z, t * b.z), fmaf(s, a.w, t * b.w));
 }
 
+constexpr int AHEAD = 4;                            // fours of a thread in flight
 // the new momentum, and the sum of the squares of u in 64 bits (whose range holds any)
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
   pdl_wait(); pdl_trigger();
   const int b = blockIdx.y;
   const uint32_t chunks = (p.cols + 3) / 4;
-  const uint64_t n = (uint64_t)p.rows * chunks;
+  const uint64_t n = (uint64_t)p.rows * chunks, stride = (uint64_t)gridDim.x * 256;
   double sum = 0.0;
-  for (uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (uint64_t)gridDim.x * 256) {
-    const uint32_t row = n <= 0xffffffffu ? (uint32_t)e / chunks : (uint32_t)(e / chunks), c = 4 * (uint32_t)(e - (uint64_t)row * chunks);
-    const int left = p.cols - c;
-    float4 u = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
-    if (p.m) {
-      const float4 m = load4<VEC>(p.m + b * p.stride_m + row * p.ldm + c, left), g = u;
-      const float4 v = weigh(p.beta, m, p.w, g);
-      float* o = p.m_out + b * p.stride_m_out + row * p.ldm_out + c;
-      if (VEC) *reinterpret_cast<float4*>(o) = v;
-      else { o[0] = v.x; if (left > 1) o[1] = v.y; if (left > 2) o[2] = v.z; if (left > 3) o[3] = v.w; }
-      u = p.nesterov ? weigh(p.beta, v, p.w, g) : v;
+  for (uint64_t e0 = (uint64_t)blockIdx.x * 256 + threadIdx.x; e0 < n; e0 += AHEAD * stride) {
+    float4 u[AHEAD], m[AHEAD];
+    int64_t row[AHEAD]; int c[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const uint64_t e = e0 + i * stride;
+      row[i] = n <= 0xffffffffu ? (uint32_t)e / chunks : e / chunks;
+      c[i] = 4 * (int)(e - (uint64_t)row[i] * chunks);
+      u[i] = m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (e < n) {
+        u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row[i] * p.ldg + c[i], p.cols - c[i]);
+        if (p.m) m[i] = load4<VEC>(p.m + b * p.stride_m + row[i] * p.ldm + c[i], p.cols - c[i]);
+      }
     }
-    sum = fma((double)u.x, (double)u.x, sum); sum = fma((double)u.y, (double)u.y, sum);
-    sum = fma((double)u.z, (double)u.z, sum); sum = fma((double)u.w, (double)u.w, sum);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (e0 + i * stride >= n) break;
+      const int left = p.cols - c[i];
+      if (p.m) {
+        const float4 g = u[i], v = weigh(p.beta, m[i], p.w, g);
+        float* o = p.m_out + b * p.stride_m_out + row[i] * p.ldm_out + c[i];
+        if (VEC) *reinterpret_cast<float4*>(o) = v;
+        else { o[0] = v.x; if (left > 1) o[1] = v.y; if (left > 2) o[2] = v.z; if (left > 3) o[3] = v.w; }
+        u[i] = p.nesterov ? weigh(p.beta, v, p.w, g) : v;
+      }
+      sum = fma((double)u[i].x, (double)u[i].x, sum); sum = fma((double)u[i].y, (double)u[i].y, sum);
+      sum = fma((double)u[i].z, (double)u[i].z, sum); sum = fma((double)u[i].w, (double)u[i].w, sum);
+    }
   }
   __shared__ double s_sum[8];
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -324,11 +584,13 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
   }
 }
 
-// X as a pair of fp16, its rows filled up with zeros
+// X in fp32 by blocks and in fp16 by rows, filled up with zeros
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blocks) {
   pdl_wait(); pdl_trigger();
   const int b = blockIdx.y;
+  if (b == 0)
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < p.n_counters; i += gridDim.x * 256) p.counters[i] = 0;
   __shared__ double s_inv;
   if (threadIdx.x < 32) {
     double s = 0.0;
@@ -339,56 +601,88 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
   }
   __syncthreads();
   const double inv = s_inv;
-  const uint32_t chunks = p.ld / 4;
-  const uint64_t n = (uint64_t)p.rows * chunks;
-  for (uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (uint64_t)gridDim.x * 256) {
-    const uint32_t row = n <= 0xffffffffu ? (uint32_t)e / chunks : (uint32_t)(e / chunks), c = 4 * (uint32_t)(e - (uint64_t)row * chunks);
-    const int left = p.cols - (int)c;
-    float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (left > 0) {
-      u = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
-      if (p.m) {
-        const float4 m = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
-        u = p.nesterov ? weigh(p.beta, m, p.w, u) : m;
+  // a warp takes 32 x 32 blocks, 4 rows of 8 fours at a time
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r0 = lane >> 3, c0 = 4 * (lane & 7);
+  const int n = p.rows32 * p.cols32;
+  for (int e = n - 1 - (blockIdx.x * 8 + warp); e >= 0; e -= gridDim.x * 8) {      // (from the end: what was read last is still in the L2)
+    const int rb = e / p.cols32, cb = e - rb * p.cols32, c = cb * 32 + c0, left = p.cols - c;
+    float4 u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = rb * 32 + 4 * i + r0;
+      u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (left > 0 && row < p.rows) {
+        u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
+        if (p.m) {
+          const float4 m = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
+          u[i] = p.nesterov ? weigh(p.beta, m, p.w, u[i]) : m;
+        }
       }
     }
-    const float x[4] = {(float)(u.x * inv), (float)(u.y * inv), (float)(u.z * inv), (float)(u.w * inv)};
-    if (p.O) {
+    float* block = p.X + ((int64_t)b * n + e) * 1024 + (c0 / 8) * 256 + c0 % 8;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) if (j < left) p.O[((int64_t)b * p.rows + row) * p.cols + c + j] = __float2bfloat16_rn(p.scale * x[j]);
-      continue;
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = rb * 32 + 4 * i + r0;
+      const float s = p.O ? 1.f : 1 << X_EXP;
+      const float4 x = make_float4((float)(u[i].x * inv) * s, (float)(u[i].y * inv) * s, (float)(u[i].z * inv) * s, (float)(u[i].w * inv) * s);
+      if (p.O) {
+        if (row < p.rows) {
+          bf16* o = p.O + ((int64_t)b * p.rows + row) * p.cols + c;
+          if (left > 0) o[0] = __float2bfloat16_rn(p.scale * x.x);
+          if (left > 1) o[1] = __float2bfloat16_rn(p.scale * x.y);
+          if (left > 2) o[2] = __float2bfloat16_rn(p.scale * x.z);
+          if (left > 3) o[3] = __float2bfloat16_rn(p.scale * x.w);
+        }
+        continue;
+      }
+      *reinterpret_cast<float4*>(block + 8 * (4 * i + r0)) = x;
+      if (row < p.rows) *reinterpret_cast<uint2*>(p.hi + ((int64_t)b * p.rows + row) * p.ld + c) = make_uint2(half2_bits(x.x, x.y), half2_bits(x.z, x.w));
     }
-    uint32_t h[2], l[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float s = 1 << X_EXP, y0 = x[2 * j] * s, y1 = x[2 * j + 1] * s;
-      h[j] = half2_bits(y0, y1);
-      const float2 a = half2_floats(h[j]);
-      l[j] = half2_bits((y0 - a.x) * (1 << LO_EXP), (y1 - a.y) * (1 << LO_EXP));
-    }
-    const int64_t at = ((int64_t)b * p.rows + row) * p.ld + c;
-    *reinterpret_cast<uint2*>(p.hi + at) = make_uint2(h[0], h[1]);
-    *reinterpret_cast<uint2*>(p.lo + at) = make_uint2(l[0], l[1]);
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-struct Plan { int side, blocks; int64_t ld, lds; size_t partial, hi[2], lo, a, p, bytes; };
+struct Plan {
+  int side, blocks; int64_t ld, lds;
+  bool pair;
+  int tiles_s, sym, tiles_m, tiles_n, splits[2], workers;
+  size_t partial, hi[2], x, a, a2, p, sums, counters, bytes;
+  int rows32, cols32, side32;
+  int n_counters;
+};
 
 Plan make_plan(int batch, int m, int n, int steps) {
   Plan q = {};
   q.side = std::min(m, n);
   q.ld = ((int64_t)n + 63) / 64 * 64;
   q.lds = ((int64_t)q.side + 63) / 64 * 64;
+  q.rows32 = (m + 31) / 32; q.cols32 = (n + 31) / 32; q.side32 = (q.side + 31) / 32;
   const int64_t chunks = (int64_t)m * ((n + 3) / 4);
   q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 8 / std::min(batch, SMS * 8)));
+  auto tiles = [](int64_t x, int t) { return (int)((x + t - 1) / t); };
+  // SM pairs on 256 x 256 tiles where X has enough of them, else single SMs on 128 x 128
+  q.pair = q.side > 128 && (int64_t)tiles(m, 256) * tiles(n, 256) * batch >= 32;
+  const int t = q.pair ? 256 : 128;
+  q.workers = q.pair ? SMS / 2 : SMS;
+  q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;
+  q.tiles_m = tiles(m, t); q.tiles_n = tiles(n, t);
+  // Sums of A and A A in slices where there are fewer tiles than workers, of 4096 products at least: joining slices takes about 9 us, and 2048
+  // products 10 (8192 x 2048: A in two slices 31 us, in one 48; A A, whose sums are of 2048, 20 and 15).
+  for (int i = 0; i < 2; ++i) {
+    const int64_t k_blocks = ((i == 0 ? std::max(m, n) : q.side) + KH * BK - 1) / (KH * BK);
+    q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / 32}));
+  }
   size_t at = 0;
   auto take = [&](size_t k) { const size_t was = at; at += (k + 255) / 256 * 256; return was; };
   q.partial = take((size_t)batch * q.blocks * 8);
   if (steps > 0) {
     const size_t x = (size_t)batch * m * q.ld * 2, s = (size_t)batch * q.side * q.lds * 2;
-    q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.lo = take(x);
-    q.a = take(s); q.p = take(s);
+    q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.x = take((size_t)batch * q.rows32 * q.cols32 * 4096);
+    q.a = take(s); q.a2 = take((size_t)batch * q.side32 * q.side32 * 2048); q.p = take(s);
+    const int most = std::max(q.splits[0], q.splits[1]), ctas = q.pair ? 2 : 1;
+    q.sums = take(most > 1 ? (size_t)batch * q.sym * most * t * t * 4 : 0);
+    q.n_counters = 3 * batch + (most > 1 ? 2 * batch * q.sym * ctas * EPI : 0);
+    q.counters = take((size_t)q.n_counters * 4);
   }
   q.bytes = at;
   return q;
@@ -398,9 +692,9 @@ int check_ortho(int batch, int m, int n, int steps) {
   if (batch < 0 || m < 0 || n < 0) return ppu_fail(PPU_EINVAL, "negative size");
   if (m > MAX_SIDE || n > MAX_SIDE || batch > 65535) return ppu_fail(PPU_ESHAPE, "at most 65535 matrices of sides up to %d", MAX_SIDE);
   if (steps < 0 || steps > MAX_STEPS) return ppu_fail(PPU_EINVAL, "steps must be 0 to %d", MAX_STEPS);
-  // tiles are counted in 32 bits
+  // (32 warps report each tile in each of 32 steps: counted in 32 bits)
   const int64_t tiles = (((int64_t)m + 127) / 128) * (((int64_t)n + 127) / 128) * batch;
-  if (tiles > (1 << 30)) return ppu_fail(PPU_ESHAPE, "too many matrices of this size");
+  if (tiles > (1 << 20)) return ppu_fail(PPU_ESHAPE, "too many matrices of this size");
   return PPU_OK;
 }
 
@@ -431,26 +725,50 @@ double largest_poly(double b, double c, double top) {
       return ppu_fail(PPU_ECUDA, "%s failed: %s", #call, cudaGetErrorString(e_));        \
   } while (0)
 
-// boxes of 64 x rows over [batch][rows][inner]
-bool encode(CUtensorMap* map, const __half* base, int64_t ld, int inner, int rows, int batch, int box_rows) {
+// boxes of 64 x 128 over [batch][rows][inner]
+bool encode(CUtensorMap* map, const __half* base, int64_t ld, int inner, int rows, int batch) {
   const cuuint64_t dim[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch}, stride[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * rows * 2};
-  const cuuint32_t box[3] = {(cuuint32_t)BK, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)BK, 128, 1}, one[3] = {1, 1, 1};
   return get_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, (void*)base, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-struct Operand { const __half* p; int64_t ld; int rows, inner; };      // as stored: [batch][rows][ld], `inner` columns of it
 
-template <bool A_K, bool B_K, int MODE>
-int product(const Operand& A, const Operand& B, GemmP p, cudaStream_t st) {
-  static PerDeviceFlag attr;
-  if (!ppu_set_smem_once(attr, ortho_tile_kernel<A_K, B_K, MODE>, SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
-  CUtensorMap mapA, mapB;
-  if (!encode(&mapA, A.p, A.ld, A.inner, A.rows, p.batch, A_K ? TM : 64) || !encode(&mapB, B.p, B.ld, B.inner, B.rows, p.batch, B_K ? TN : 64))
-    return ppu_fail(PPU_ECUDA, "tensor map not accepted");
-  p.tiles_m = (p.M + TM - 1) / TM; p.tiles_n = (p.N + TN - 1) / TN;
-  p.tiles = MODE == UPDATE ? p.tiles_m * p.tiles_n : p.tiles_m * (p.tiles_m + 1) / 2;
-  const int64_t units = (int64_t)p.tiles * p.batch;
-  CUDA_OK(ppu_launch_dependent(ortho_tile_kernel<A_K, B_K, MODE>, (unsigned)std::min<int64_t>(units, ppu_sm_count()), 64 + 32 * EPI, SMEM, st, mapA, mapB, p));
+// how many CTAs (or pairs) are resident together on the current device
+int resident(bool pair) {
+  static int known[2][PPU_MAX_DEVICES];
+  int& n = known[pair][ppu_current_device()];
+  if (n > 0) return n;
+  int got = 0;
+  if (pair) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2); cfg.blockDim = dim3(BLOCK); cfg.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&got, ortho_pair_kernel, &cfg) != cudaSuccess) return -1;
+    n = std::min(got, ppu_sm_count() / 2);
+  } else {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&got, ortho_single_kernel, BLOCK, SMEM) != cudaSuccess) return -1;
+    n = got > 0 ? ppu_sm_count() : 0;
+  }
+  return n;
+}
+
+int launch_steps(const Maps& maps, const KernelP& p, bool pair, cudaStream_t st) {
+  static PerDeviceFlag attr_set[2];
+  void (*kernel)(Maps, KernelP) = pair ? ortho_pair_kernel : ortho_single_kernel;
+  if (!ppu_set_smem_once(attr_set[pair], kernel, SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  const int most = resident(pair);
+  if (most < 1) return ppu_fail(PPU_ECUDA, "the kernel does not fit on this device");
+  const int units = p.batch * std::max(p.units[GRAM], std::max(p.units[POLY], p.units[UPDATE]));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((pair ? 2 : 1) * std::min(most, units)); cfg.blockDim = dim3(BLOCK); cfg.dynamicSmemBytes = SMEM; cfg.stream = st;
+  cudaLaunchAttribute attr[1];                     // CTAs wait for one another: all of them are resident
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, maps, p));
   return PPU_OK;
 }
 
@@ -515,36 +833,41 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   if (steps > 0 && gemm_tc_init() != 0) return ppu_fail(PPU_ECUDA, "no tensor-map encoder");
   cudaStream_t st = (cudaStream_t)cuda_stream;
   uint8_t* ws = (uint8_t*)workspace;
-  __half *hi[2] = {(__half*)(ws + q.hi[0]), (__half*)(ws + q.hi[1])}, *lo = (__half*)(ws + q.lo), *A = (__half*)(ws + q.a), *P = (__half*)(ws + q.p);
+  __half *hi[2] = {(__half*)(ws + q.hi[0]), (__half*)(ws + q.hi[1])}, *A = (__half*)(ws + q.a), *P = (__half*)(ws + q.p);
   PrepP pp = {};
   pp.G = G; pp.ldg = ldg; pp.stride_g = stride_g; pp.m = momentum; pp.ldm = ldm; pp.stride_m = stride_m;
   pp.m_out = momentum_out; pp.ldm_out = ldmo; pp.stride_m_out = stride_mo; pp.rows = m; pp.cols = n; pp.nesterov = nesterov != 0;
-  pp.beta = beta; pp.w = weight; pp.eps = eps; pp.scale = scale; pp.partial = (double*)(ws + q.partial); pp.hi = hi[0]; pp.lo = lo; pp.ld = q.ld;
+  pp.beta = beta; pp.w = weight; pp.eps = eps; pp.scale = scale; pp.partial = (double*)(ws + q.partial); pp.hi = hi[0]; pp.ld = q.ld;
+  pp.X = (float*)(ws + q.x); pp.rows32 = q.rows32; pp.cols32 = q.cols32;
   pp.O = steps == 0 ? (bf16*)O : nullptr;
+  pp.counters = (unsigned*)(ws + q.counters); pp.n_counters = q.n_counters;
   const bool vec = n % 4 == 0 && aligned(G, ldg, stride_g, 4 * g_bytes) && aligned(momentum, ldm, stride_m, 16) && aligned(momentum_out, ldmo, stride_mo, 16);
-  int rc2 = g_type == PPU_BF16 ? prepare<bf16>(pp, q, batch, vec, st) : prepare<float>(pp, q, batch, vec, st);
-  const bool left = m <= n;
-  for (int k = 0; k < steps && !rc2; ++k) {
-    const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
-    const Operand X = {hi[k & 1], q.ld, m, n}, SA = {A, q.lds, q.side, q.side}, SP = {P, q.lds, q.side, q.side};
-    GemmP g = {};
-    g.batch = batch; g.flags = flags;
-    // A = X X^T or X^T X
-    g.M = g.N = q.side; g.K = left ? n : m; g.C = A; g.ldc = q.lds; g.stride = q.side * q.lds;
-    g.c = std::ldexp(1.f, A_EXP - 2 * X_EXP);
-    rc2 = left ? product<true, true, GRAM>(X, X, g, st) : product<false, false, GRAM>(X, X, g, st);
-    if (rc2) break;
-    // P = b A + c A A
-    g.K = q.side; g.C = P; g.A = A;
-    g.b = std::ldexp(c[1], p_exp[k] - A_EXP); g.c = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
-    rc2 = product<true, true, POLY>(SA, SA, g, st);
-    if (rc2) break;
-    // X = a X + P X or X P
-    g.M = m; g.N = n; g.K = q.side; g.hi = hi[k & 1]; g.lo = lo; g.hi_out = k + 1 < steps ? hi[(k + 1) & 1] : nullptr;
-    g.ldc = q.ld; g.stride = (int64_t)m * q.ld; g.a = c[0]; g.f = std::ldexp(1.f, -p_exp[k]);
-    g.O = (bf16*)O; g.ldo = n; g.scale = scale;
-    if (k + 1 == steps) { g.a = std::ldexp(c[0], -X_EXP); g.f = std::ldexp(1.f, -p_exp[k] - X_EXP); }
-    rc2 = left ? product<true, false, UPDATE>(SP, X, g, st) : product<true, true, UPDATE>(X, SP, g, st);
+  const int rc2 = g_type == PPU_BF16 ? prepare<bf16>(pp, q, batch, vec, st) : prepare<float>(pp, q, batch, vec, st);
+  if (rc2 || steps == 0) return rc2;
+  Maps maps;
+  if (!encode(&maps.m[0], hi[0], q.ld, n, m, batch) || !encode(&maps.m[1], steps > 1 ? hi[1] : hi[0], q.ld, n, m, batch) ||
+      !encode(&maps.m[2], A, q.lds, q.side, q.side, batch) || !encode(&maps.m[3], P, q.lds, q.side, q.side, batch))
+    return ppu_fail(PPU_ECUDA, "tensor map not accepted");
+  KernelP p = {};
+  p.m = m; p.n = n; p.side = q.side; p.batch = batch; p.steps = steps; p.left = m <= n;
+  p.tiles_s = q.tiles_s; p.sym = q.sym; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n; p.n_fast = m > n;
+  p.splits[0] = q.splits[0]; p.splits[1] = q.splits[1];
+  const int tiles = q.tiles_m * q.tiles_n, rem = tiles % q.workers;
+  p.tail_from = 1 << 30;
+  p.units[GRAM] = q.sym * q.splits[0]; p.units[POLY] = q.sym * q.splits[1]; p.units[UPDATE] = tiles;
+  if (q.pair && batch == 1 && tiles > q.workers && rem > 0 && 2 * rem <= q.workers) {      // a last wave of halves instead of one of few tiles
+    p.tail_from = tiles - rem;
+    p.units[UPDATE] = tiles + rem;
   }
-  return rc2;
+  p.per_step = batch * (p.units[GRAM] + p.units[POLY] + p.units[UPDATE]);
+  p.A = A; p.P = P; p.hi[0] = hi[0]; p.hi[1] = hi[1]; p.X = pp.X; p.A2 = (__half*)(ws + q.a2); p.rows32 = q.rows32; p.cols32 = q.cols32; p.side32 = q.side32; p.ld = q.ld; p.lds = q.lds; p.O = (bf16*)O; p.scale = scale;
+  p.gram = std::ldexp(1.f, A_EXP - 2 * X_EXP);
+  for (int k = 0; k < steps; ++k) {
+    const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
+    const int out = k + 1 < steps ? 0 : -X_EXP;    // O has no power of two
+    p.b[k] = std::ldexp(c[1], p_exp[k] - A_EXP); p.c[k] = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
+    p.a[k] = std::ldexp(c[0], out); p.f[k] = std::ldexp(1.f, out - p_exp[k]);
+  }
+  p.partial = (float*)(ws + q.sums); p.done = pp.counters; p.arrived = p.done + 3 * batch; p.flags = flags;
+  return launch_steps(maps, p, q.pair, st);
 }
