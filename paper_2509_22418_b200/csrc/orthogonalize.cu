@@ -584,60 +584,62 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
   }
 }
 
-// X in fp32 by blocks and in fp16 by rows, filled up with zeros
+// X in fp32 by blocks and in fp16 by rows, filled up with zeros.  A warp takes one 32 x 32 block, 4 rows of 8 fours at a time, and has it in
+// flight while the norm is put together.
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blocks) {
   pdl_wait(); pdl_trigger();
   const int b = blockIdx.y;
   if (b == 0)
     for (int i = blockIdx.x * 256 + threadIdx.x; i < p.n_counters; i += gridDim.x * 256) p.counters[i] = 0;
-  __shared__ double s_inv;
-  if (threadIdx.x < 32) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += 32) s += p.partial[(int64_t)b * blocks + i];
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    const double d = sqrt(s) + (double)p.eps;
-    if (threadIdx.x == 0) s_inv = d > 0.0 ? 1.0 / d : d == 0.0 ? 0.0 : d;      // (a matrix of zeros stays one; NaN stays NaN)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r0 = lane >> 3, c0 = 4 * (lane & 7);
+  const int n = p.rows32 * p.cols32, e = n - 1 - (blockIdx.x * 8 + warp);      // (from the end: what was read last is still in the L2)
+  const int rb = e / p.cols32, cb = e - rb * p.cols32, c = cb * 32 + c0, left = p.cols - c;
+  float4 u[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = rb * 32 + 4 * i + r0;
+    u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (e >= 0 && left > 0 && row < p.rows) {
+      u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
+      if (p.m) {
+        const float4 m = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
+        u[i] = p.nesterov ? weigh(p.beta, m, p.w, u[i]) : m;
+      }
+    }
+  }
+  __shared__ double s_sum[8], s_inv;
+  double sum = 0.0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < blocks; i += 256) sum += p.partial[(int64_t)b * blocks + i];
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) sum += s_sum[w];
+    const double d = sqrt(sum) + (double)p.eps;
+    s_inv = (d > 0.0 ? 1.0 / d : d == 0.0 ? 0.0 : d) * (p.O ? 1.0 : (double)(1 << X_EXP));      // (a matrix of zeros stays one; NaN stays NaN)
   }
   __syncthreads();
+  if (e < 0) return;
   const double inv = s_inv;
-  // a warp takes 32 x 32 blocks, 4 rows of 8 fours at a time
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r0 = lane >> 3, c0 = 4 * (lane & 7);
-  const int n = p.rows32 * p.cols32;
-  for (int e = n - 1 - (blockIdx.x * 8 + warp); e >= 0; e -= gridDim.x * 8) {      // (from the end: what was read last is still in the L2)
-    const int rb = e / p.cols32, cb = e - rb * p.cols32, c = cb * 32 + c0, left = p.cols - c;
-    float4 u[8];
+  float* block = p.X + ((int64_t)b * n + e) * 1024 + (c0 / 8) * 256 + c0 % 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = rb * 32 + 4 * i + r0;
-      u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (left > 0 && row < p.rows) {
-        u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
-        if (p.m) {
-          const float4 m = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
-          u[i] = p.nesterov ? weigh(p.beta, m, p.w, u[i]) : m;
-        }
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = rb * 32 + 4 * i + r0;
+    const float4 x = make_float4((float)(u[i].x * inv), (float)(u[i].y * inv), (float)(u[i].z * inv), (float)(u[i].w * inv));
+    if (p.O) {
+      if (row < p.rows) {
+        bf16* o = p.O + ((int64_t)b * p.rows + row) * p.cols + c;
+        if (left > 0) o[0] = __float2bfloat16_rn(p.scale * x.x);
+        if (left > 1) o[1] = __float2bfloat16_rn(p.scale * x.y);
+        if (left > 2) o[2] = __float2bfloat16_rn(p.scale * x.z);
+        if (left > 3) o[3] = __float2bfloat16_rn(p.scale * x.w);
       }
+      continue;
     }
-    float* block = p.X + ((int64_t)b * n + e) * 1024 + (c0 / 8) * 256 + c0 % 8;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = rb * 32 + 4 * i + r0;
-      const float s = p.O ? 1.f : 1 << X_EXP;
-      const float4 x = make_float4((float)(u[i].x * inv) * s, (float)(u[i].y * inv) * s, (float)(u[i].z * inv) * s, (float)(u[i].w * inv) * s);
-      if (p.O) {
-        if (row < p.rows) {
-          bf16* o = p.O + ((int64_t)b * p.rows + row) * p.cols + c;
-          if (left > 0) o[0] = __float2bfloat16_rn(p.scale * x.x);
-          if (left > 1) o[1] = __float2bfloat16_rn(p.scale * x.y);
-          if (left > 2) o[2] = __float2bfloat16_rn(p.scale * x.z);
-          if (left > 3) o[3] = __float2bfloat16_rn(p.scale * x.w);
-        }
-        continue;
-      }
-      *reinterpret_cast<float4*>(block + 8 * (4 * i + r0)) = x;
-      if (row < p.rows) *reinterpret_cast<uint2*>(p.hi + ((int64_t)b * p.rows + row) * p.ld + c) = make_uint2(half2_bits(x.x, x.y), half2_bits(x.z, x.w));
-    }
+    *reinterpret_cast<float4*>(block + 8 * (4 * i + r0)) = x;
+    if (row < p.rows) *reinterpret_cast<uint2*>(p.hi + ((int64_t)b * p.rows + row) * p.ld + c) = make_uint2(half2_bits(x.x, x.y), half2_bits(x.z, x.w));
   }
 }
 
@@ -666,11 +668,12 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;
   q.tiles_m = tiles(m, t); q.tiles_n = tiles(n, t);
-  // Sums of A and A A in slices where there are fewer tiles than workers, of 4096 products at least: joining slices takes about 9 us, and 2048
-  // products 10 (8192 x 2048: A in two slices 31 us, in one 48; A A, whose sums are of 2048, 20 and 15).
+  // Sums of A and A A in slices where there are fewer tiles than workers.  Pairs: of 4096 products at least, since joining slices takes about 9 us, and
+  // 2048 products 10 (8192 x 2048: A in two slices 31 us, in one 48; A A, whose sums are of 2048, 20 and 15).  Single SMs: of 1024 (8 x 64 x 4096: a
+  // step 25.7 us, in one slice 34.3, in eight 27.8).
   for (int i = 0; i < 2; ++i) {
     const int64_t k_blocks = ((i == 0 ? std::max(m, n) : q.side) + KH * BK - 1) / (KH * BK);
-    q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / 32}));
+    q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / (q.pair ? 32 : 8)}));
   }
   size_t at = 0;
   auto take = [&](size_t k) { const size_t was = at; at += (k + 255) / 256 * 256; return was; };
@@ -774,13 +777,13 @@ int launch_steps(const Maps& maps, const KernelP& p, bool pair, cudaStream_t st)
 
 template <typename TG>
 int prepare(const PrepP& p, const Plan& q, int batch, bool vec, cudaStream_t st) {
-  const dim3 grid(q.blocks, batch);
+  const dim3 grid(q.blocks, batch), blocks32((q.rows32 * q.cols32 + 7) / 8, batch);
   if (vec) {
     CUDA_OK(ppu_launch_dependent(ortho_norm_kernel<TG, 1>, grid, 256, 0, st, p));
-    CUDA_OK(ppu_launch_dependent(ortho_scale_kernel<TG, 1>, grid, 256, 0, st, p, q.blocks));
+    CUDA_OK(ppu_launch_dependent(ortho_scale_kernel<TG, 1>, blocks32, 256, 0, st, p, q.blocks));
   } else {
     CUDA_OK(ppu_launch_dependent(ortho_norm_kernel<TG, 0>, grid, 256, 0, st, p));
-    CUDA_OK(ppu_launch_dependent(ortho_scale_kernel<TG, 0>, grid, 256, 0, st, p, q.blocks));
+    CUDA_OK(ppu_launch_dependent(ortho_scale_kernel<TG, 0>, blocks32, 256, 0, st, p, q.blocks));
   }
   return PPU_OK;
 }
