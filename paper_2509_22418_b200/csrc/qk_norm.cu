@@ -22,8 +22,12 @@ int ppu_fail(int code, const char* fmt, ...);
 namespace {
 
 constexpr int MAX_DH = 256, BLOCK = 256, SMS = 148;
-constexpr int FWD_ROWS = 4, BWD_ROWS = 2;            // tokens of a slot in flight
-constexpr int FWD_BLOCKS = 4, BWD_BLOCKS = 3;        // blocks on an SM
+// Tokens of a slot at a time (and as many on their way), blocks on an SM.  8192 x 48 heads of 128, us: forward 38.1; with 4 blocks (64 registers,
+// spilling) 42.3, with 2 tokens and 4 blocks 40.7, 8 and 2 46.6, without the group on its way 41.9.  Backward 60.2; 1 token and 4 blocks 66, 3 and 2 60.9, 4 and
+// 2 62.0.
+constexpr int FWD_ROWS = 4, BWD_ROWS = 2;
+constexpr int FWD_BLOCKS = 3, BWD_BLOCKS = 3;
+constexpr int MOST_GROUPS = 4;                       // groups of rows whose angles are formed together
 
 struct QkArgs {
   const bf16 *x, *dy;                // forward: x; backward: x and the gradient of the result
@@ -35,21 +39,29 @@ struct QkArgs {
   int per_head, layer;
   float eps;
   int T, slots, tokens;              // slots of a block that hold different heads, tokens at a time
+  int groups_of_rows;                // of ROWS * tokens tokens each whose angles are formed together
   float* partial; int groups;        // backward: [rows][groups][dh]
-  int norm_y;                        // blocks (y) with heads of queries and keys
   double turns[MAX_DH / 2];          // inverse frequencies / (2 pi)
 };
 
-__device__ __forceinline__ void unpack4(const uint2 u, float* f) {
-  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
-  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-  f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+// Two values in one instruction (half of the arithmetic's issue slots: with one value each the forward pass issued 194 instructions for a warp's two
+// heads and took 48 us at 8192 x 48 heads of 128, where memory allows 31).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 ra, rb, rd;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nmul.rn.f32x2 rd, ra, rb;\nmov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
-__device__ __forceinline__ uint2 pack4(const float* f) {
-  __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-  return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 ra, rb, rc, rd;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nmov.b64 rc, {%6, %7};\nfma.rn.f32x2 rd, ra, rb, rc;\nmov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
-// the 8 columns of a thread: at c0 and c1 = c0 + 4 (HALVES 0), or at c0 and c1
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// The 8 columns of a thread are four pairs (a_i, b_i); v[0] = a_0 a_1, v[1] = a_2 a_3, v[2] = b_0 b_1, v[3] = b_2 b_3.
+// HALVES 0: 8 neighbours from c0 on, a_0 b_0 a_1 b_1 ...; 1: the a's from c0 on, the b's from c1 on.
 template <int HALVES> __device__ __forceinline__ uint4 load_row(const bf16* p, int c0, int c1) {
   if (!HALVES) return *reinterpret_cast<const uint4*>(p + c0);
   const uint2 a = *reinterpret_cast<const uint2*>(p + c0), b = *reinterpret_cast<const uint2*>(p + c1);
@@ -60,14 +72,39 @@ template <int HALVES> __device__ __forceinline__ void store_row(bf16* p, int c0,
   *reinterpret_cast<uint2*>(p + c0) = make_uint2(v.x, v.y);
   *reinterpret_cast<uint2*>(p + c1) = make_uint2(v.z, v.w);
 }
-__device__ __forceinline__ void unpack8(const uint4 u, float* f) { unpack4(make_uint2(u.x, u.y), f); unpack4(make_uint2(u.z, u.w), f + 4); }
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  const uint2 a = pack4(f), b = pack4(f + 4);
-  return make_uint4(a.x, a.y, b.x, b.y);
+__device__ __forceinline__ float low(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float high(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+template <int HALVES> __device__ __forceinline__ void unpack(const uint4 u, float2 (&v)[4]) {
+  if (HALVES) {
+    v[0] = make_float2(low(u.x), high(u.x)); v[1] = make_float2(low(u.y), high(u.y)); v[2] = make_float2(low(u.z), high(u.z)); v[3] = make_float2(low(u.w), high(u.w));
+  } else {
+    v[0] = make_float2(low(u.x), low(u.y)); v[1] = make_float2(low(u.z), low(u.w)); v[2] = make_float2(high(u.x), high(u.y)); v[3] = make_float2(high(u.z), high(u.w));
+  }
 }
-// pair j of a thread's columns
-template <int HALVES> __device__ __forceinline__ constexpr int pair_a(int j) { return HALVES ? j : 2 * j; }
-template <int HALVES> __device__ __forceinline__ constexpr int pair_b(int j) { return HALVES ? 4 + j : 2 * j + 1; }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <int HALVES> __device__ __forceinline__ uint4 pack(const float2 (&v)[4]) {
+  if (HALVES) return make_uint4(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y), pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
+  return make_uint4(pack2(v[0].x, v[2].x), pack2(v[0].y, v[2].y), pack2(v[1].x, v[3].x), pack2(v[1].y, v[3].y));
+}
+// column of value j of v[i]
+template <int HALVES> __device__ __forceinline__ int column(int i, int j, int c0, int c1) {
+  const int pr = 2 * (i & 1) + j;
+  return HALVES ? (i < 2 ? c0 : c1) + pr : c0 + 2 * pr + (i < 2 ? 0 : 1);
+}
+// (a, b) -> (a cos - b sin, a sin + b cos); back: by the negative angle
+template <bool BACK> __device__ __forceinline__ void turn(float2 (&v)[4], const float4 c, const float4 s) {
+  const float2 co[2] = {make_float2(c.x, c.y), make_float2(c.z, c.w)}, si[2] = {make_float2(s.x, s.y), make_float2(s.z, s.w)};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = v[i], b = v[2 + i], n = make_float2(-si[i].x, -si[i].y);
+    v[i] = fma2(a, co[i], mul2(b, BACK ? si[i] : n));
+    v[2 + i] = fma2(b, co[i], mul2(a, BACK ? n : si[i]));
+  }
+}
+__device__ __forceinline__ float total(const float2 a) { return a.x + a.y; }
 
 template <int LANES, int N> __device__ __forceinline__ void slot_sum(float (&v)[N]) {
 #pragma unroll
@@ -76,160 +113,169 @@ template <int LANES, int N> __device__ __forceinline__ void slot_sum(float (&v)[
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
-template <int LANES, int HALVES, bool BWD>
+template <int LANES, int HALVES, int LAYER, bool BWD>
 __global__ void __launch_bounds__(BLOCK, BWD ? BWD_BLOCKS : FWD_BLOCKS) qk_norm_kernel(const __grid_constant__ QkArgs a) {
   constexpr int ROWS = BWD ? BWD_ROWS : FWD_ROWS;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_turns[MAX_DH / 2];
-  const int pairs = a.rot / 2, tile = a.tokens * ROWS;
-  float2* angles = reinterpret_cast<float2*>(smem);        // [2][tile][pairs] (cos, sin)
+  const int pairs = a.rot / 2, group = a.tokens * ROWS, tile = group * a.groups_of_rows;
+  float* angles = reinterpret_cast<float*>(smem);          // [2][tile][pairs / 4][4 cosines, 4 sines]
   pdl_wait(); pdl_trigger();
   for (int i = threadIdx.x; i < pairs; i += BLOCK) s_turns[i] = a.inv_freq ? (double)a.inv_freq[i] * 0.15915494309189535 : a.turns[i];
   __syncthreads();
 
   const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  const int head = blockIdx.y * a.slots + slot % a.slots, mine = slot / a.slots;      // this slot's head, its first token of a tile
+  // this slot's head (dealt round to the blocks: each has its share of the values, which are less work), its first token of a group
+  const int head = slot % a.slots * gridDim.y + blockIdx.y, mine = slot / a.slots;
   const bool on = mine < a.tokens && head < a.heads && 8 * lane < a.dh;
-  const bool turned = 8 * lane < a.rot, normed = head < a.n_q + a.n_k;
+  const bool turned = 8 * lane < a.rot, normed = on && head < a.n_q + a.n_k;
+  const bool work = __any_sync(0xffffffffu, normed);       // (a warp of values copies them)
   const int c0 = HALVES ? (turned ? 4 * lane : 8 * lane) : 8 * lane, c1 = HALVES && turned ? pairs + 4 * lane : c0 + 4;
   const int64_t at = (int64_t)head * a.dh;
-  float gain[8], dgain[8];
+  float2 gain[4], dgain[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) { gain[j] = 1.f; dgain[j] = 0.f; }
-  if (on && normed) {
+  for (int i = 0; i < 4; ++i) { gain[i] = both(1.f); dgain[i] = both(0.f); }
+  if (normed) {
     const bool q = head < a.n_q;
     const float* g = q ? a.q_gain : a.k_gain;
     if (g) {
       if (a.per_head) g += (int64_t)(q ? head : head - a.n_q) * a.dh;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) gain[j] = g[j < 4 ? c0 + j : c1 + j - 4];
+      for (int i = 0; i < 4; ++i) gain[i] = make_float2(g[column<HALVES>(i, 0, c0, c1)], g[column<HALVES>(i, 1, c0, c1)]);
     }
   }
   const float inv_dh = 1.f / (float)a.dh;
   const int tiles = (a.T + tile - 1) / tile;
-  int buf = 0;
-  for (int i = blockIdx.x; i < tiles; i += gridDim.x, buf ^= 1) {
-    const int t0 = i * tile;
-    uint4 raw[ROWS], grad[BWD ? ROWS : 1];
+  uint4 next[ROWS], next_grad[BWD ? ROWS : 1];
+  auto load = [&](int first) {                       // the group of rows from token `first` on
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const int t = t0 + r * a.tokens + mine;
-      raw[r] = make_uint4(0, 0, 0, 0);
-      if (BWD) grad[BWD ? r : 0] = make_uint4(0, 0, 0, 0);
+      const int64_t t = (int64_t)first + r * a.tokens + mine;
+      next[r] = make_uint4(0, 0, 0, 0);
+      if (BWD) next_grad[BWD ? r : 0] = make_uint4(0, 0, 0, 0);
       if (on && t < a.T) {
-        raw[r] = load_row<HALVES>(a.x + t * a.ldx + at, c0, c1);
-        if (BWD) grad[BWD ? r : 0] = load_row<HALVES>(a.dy + t * a.ldy + at, c0, c1);
+        if (!BWD || normed) next[r] = load_row<HALVES>(a.x + t * a.ldx + at, c0, c1);
+        if (BWD) next_grad[BWD ? r : 0] = load_row<HALVES>(a.dy + t * a.ldy + at, c0, c1);
       }
     }
-    float2* cs = angles + buf * tile * pairs;
+  };
+  load(blockIdx.x * tile);
+  int buf = 0;
+  for (int it = blockIdx.x; it < tiles; it += gridDim.x, buf ^= 1) {
+    const int t0 = it * tile;
+    float* cs = angles + buf * tile * a.rot;
     const int n = min(tile, a.T - t0) * pairs;
     for (int e = threadIdx.x; e < n; e += BLOCK) {
       const int row = e / pairs, pr = e - row * pairs, t = t0 + row;
       const int pos = a.positions ? a.positions[t] : a.seq > 0 ? t % a.seq : t;
-      const double turn = (double)pos * s_turns[pr];
+      const double turns = (double)pos * s_turns[pr];
       float s, c;
-      sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
-      cs[e] = make_float2(c, s);
+      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+      float* to = cs + row * a.rot + (pr & ~3) * 2 + (pr & 3);
+      to[0] = c; to[4] = s;
     }
     __syncthreads();
+    for (int g0 = 0; g0 < tile && t0 + g0 < a.T; g0 += group) {
+      uint4 raw[ROWS], grad[BWD ? ROWS : 1];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int row = r * a.tokens + mine, t = t0 + row;
-      const bool there = on && t < a.T;
-      float x[8], y[8];
-      unpack8(raw[r], x);
-      float4 w0 = make_float4(1.f, 0.f, 1.f, 0.f), w1 = w0;                   // (cos, sin) of the pairs 4 lane ..
-      if (there && turned) {
-        const float4* p = reinterpret_cast<const float4*>(cs + (int64_t)row * pairs + 4 * lane);
-        w0 = p[0]; w1 = p[1];
-      }
-      const float co[4] = {w0.x, w0.z, w1.x, w1.z}, si[4] = {w0.y, w0.w, w1.y, w1.w};
-      if constexpr (!BWD) {
-        float mean = 0.f;
-        if (a.layer) {
-          float v[1] = {0.f};
+      for (int r = 0; r < ROWS; ++r) { raw[r] = next[r]; if (BWD) grad[BWD ? r : 0] = next_grad[BWD ? r : 0]; }
+      // the next group is on its way while this one is worked
+      load(g0 + group < tile ? t0 + g0 + group : (int)min((int64_t)a.T, ((int64_t)it + gridDim.x) * tile));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[0] += x[j];
-          slot_sum<LANES>(v);
-          mean = v[0] * inv_dh;
+      for (int r = 0; r < ROWS; ++r) {
+        const int row = g0 + r * a.tokens + mine, t = t0 + row;
+        const bool there = on && t < a.T;
+        uint4 out = BWD ? grad[BWD ? r : 0] : raw[r];
+        if (work) {
+          float2 x[4];
+          unpack<HALVES>(raw[r], x);
+          float4 co = make_float4(1.f, 1.f, 1.f, 1.f), si = make_float4(0.f, 0.f, 0.f, 0.f);      // of the pairs 4 lane ..
+          if (there && turned && normed) {
+            const float4* p = reinterpret_cast<const float4*>(cs + row * a.rot + 8 * lane);
+            co = p[0]; si = p[1];
+          }
+          if constexpr (!BWD) {
+            if (LAYER) {
+              float v[1] = {total(x[0]) + total(x[1]) + total(x[2]) + total(x[3])};
+              slot_sum<LANES>(v);
+              const float mean = v[0] * inv_dh;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { x[i].x -= mean; x[i].y -= mean; }
+            }
+            float v[1] = {total(fma2(x[0], x[0], mul2(x[1], x[1]))) + total(fma2(x[2], x[2], mul2(x[3], x[3])))};
+            if (LAYER && 8 * lane >= a.dh) v[0] = 0.f;                       // (threads without columns)
+            slot_sum<LANES>(v);
+            const float2 rstd = both(rsqrtf(fmaf(v[0], inv_dh, a.eps)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = mul2(x[i], mul2(rstd, gain[i]));
+            turn<false>(x, co, si);
+            if (normed) out = pack<HALVES>(x);
+          } else {
+            float2 y[4], w[4];
+            unpack<HALVES>(out, y);
+            turn<true>(y, co, si);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = mul2(y[i], gain[i]);
+            float mean_w = 0.f;
+            if (LAYER) {
+              float v[2] = {total(x[0]) + total(x[1]) + total(x[2]) + total(x[3]), total(w[0]) + total(w[1]) + total(w[2]) + total(w[3])};
+              slot_sum<LANES>(v);
+              const float mean = v[0] * inv_dh;
+              mean_w = v[1] * inv_dh;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { x[i].x -= mean; x[i].y -= mean; }
+            }
+            // sums of (x - mean)^2 and w (x - mean)
+            float v[2] = {total(fma2(x[0], x[0], mul2(x[1], x[1]))) + total(fma2(x[2], x[2], mul2(x[3], x[3]))),
+                          total(fma2(w[0], x[0], mul2(w[1], x[1]))) + total(fma2(w[2], x[2], mul2(w[3], x[3])))};
+            if (LAYER && 8 * lane >= a.dh) v[0] = v[1] = 0.f;
+            slot_sum<LANES>(v);
+            const float rs = rsqrtf(fmaf(v[0], inv_dh, a.eps));
+            const float2 rstd = both(rs), dot = both(-(v[1] * rs * inv_dh)), less = both(-mean_w);      // (minus) the means of w xh and of w
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 xh = mul2(x[i], rstd);
+              if (there) dgain[i] = fma2(y[i], xh, dgain[i]);                // (without eps, the zeros in the place of a row that is not there give NaN)
+              if (LAYER) { w[i].x += less.x; w[i].y += less.y; }
+              x[i] = mul2(rstd, fma2(xh, dot, w[i]));
+            }
+            if (normed) out = pack<HALVES>(x);
+          }
         }
-        float v[1] = {0.f};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { y[j] = x[j] - mean; v[0] = fmaf(y[j], y[j], v[0]); }
-        if (a.layer && 8 * lane >= a.dh) v[0] = 0.f;                         // (threads without columns)
-        slot_sum<LANES>(v);
-        const float rstd = 1.f / sqrtf(fmaf(v[0], inv_dh, a.eps));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= rstd * gain[j];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = y[pair_a<HALVES>(j)], q = y[pair_b<HALVES>(j)];
-          x[pair_a<HALVES>(j)] = p * co[j] - q * si[j];
-          x[pair_b<HALVES>(j)] = p * si[j] + q * co[j];
-        }
-        if (there) store_row<HALVES>(a.out + t * a.ldo + at, c0, c1, normed ? pack8(x) : raw[r]);
-      } else {
-        unpack8(grad[r], y);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {                                        // turned back
-          const float p = y[pair_a<HALVES>(j)], q = y[pair_b<HALVES>(j)];
-          y[pair_a<HALVES>(j)] = p * co[j] + q * si[j];
-          y[pair_b<HALVES>(j)] = q * co[j] - p * si[j];
-        }
-        float mean = 0.f, mean_w = 0.f;
-        if (a.layer) {
-          float v[2] = {0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 8; ++j) { v[0] += x[j]; v[1] = fmaf(y[j], gain[j], v[1]); }
-          slot_sum<LANES>(v);
-          mean = v[0] * inv_dh; mean_w = v[1] * inv_dh;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] -= mean;
-        }
-        float v[2] = {0.f, 0.f};                                             // sums of (x - mean)^2 and w (x - mean)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { v[0] = fmaf(x[j], x[j], v[0]); v[1] = fmaf(y[j] * gain[j], x[j], v[1]); }
-        if (8 * lane >= a.dh) v[0] = v[1] = 0.f;
-        slot_sum<LANES>(v);
-        const float rstd = 1.f / sqrtf(fmaf(v[0], inv_dh, a.eps));
-        const float dot = v[1] * rstd * inv_dh;                              // mean of w xh
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float xh = x[j] * rstd;
-          if (there) dgain[j] = fmaf(y[j], xh, dgain[j]);                     // (without eps, the zeros in the place of a row that is not there give NaN)
-          x[j] = rstd * (fmaf(y[j], gain[j], -mean_w) - xh * dot);
-        }
-        if (there) store_row<HALVES>(a.out + t * a.ldo + at, c0, c1, normed ? pack8(x) : grad[r]);
+        if (there) store_row<HALVES>(a.out + t * a.ldo + at, c0, c1, out);
       }
     }
   }
   if constexpr (BWD) {
-    if (!a.partial || (int)blockIdx.y >= a.norm_y) return;
+    if (!a.partial) return;
     // sums of the block's slots that share a gain, in the order of the slots
     __syncthreads();                                 // (the angles have been read)
     float* sums = reinterpret_cast<float*>(smem);    // [slots of the block][dh]
     if (8 * lane < a.dh)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sums[slot * a.dh + (j < 4 ? c0 + j : c1 + j - 4)] = on && normed ? dgain[j] : 0.f;
+      for (int i = 0; i < 4; ++i) {
+        sums[slot * a.dh + column<HALVES>(i, 0, c0, c1)] = normed ? dgain[i].x : 0.f;
+        sums[slot * a.dh + column<HALVES>(i, 1, c0, c1)] = normed ? dgain[i].y : 0.f;
+      }
     __syncthreads();
     const int all = a.slots * a.tokens;              // slots in use: head slot % slots, token slot / slots
     if (a.per_head) {
-      const int here = min(a.slots, a.n_q + a.n_k - (int)blockIdx.y * a.slots);
-      for (int e = threadIdx.x; e < here * a.dh; e += BLOCK) {
-        const int h = e / a.dh, c = e - h * a.dh;
+      for (int e = threadIdx.x; e < a.slots * a.dh; e += BLOCK) {
+        const int h = e / a.dh, c = e - h * a.dh, hd = h * gridDim.y + blockIdx.y;
+        if (hd >= a.n_q + a.n_k) break;
         float s = 0.f;
         for (int k = h; k < all; k += a.slots) s += sums[k * a.dh + c];
-        a.partial[((int64_t)blockIdx.x * a.groups + blockIdx.y * a.slots + h) * a.dh + c] = s;
+        a.partial[((int64_t)blockIdx.x * a.groups + hd) * a.dh + c] = s;
       }
     } else {
       for (int e = threadIdx.x; e < 2 * a.dh; e += BLOCK) {
         const int g = e / a.dh, c = e - g * a.dh;
         float s = 0.f;
         for (int k = 0; k < all; ++k) {
-          const int h = blockIdx.y * a.slots + k % a.slots;
+          const int h = k % a.slots * gridDim.y + blockIdx.y;
           if (h < a.n_q + a.n_k && (h >= a.n_q) == (g == 1)) s += sums[k * a.dh + c];
         }
-        a.partial[((int64_t)(blockIdx.x * a.norm_y + blockIdx.y) * 2 + g) * a.dh + c] = s;
+        a.partial[((int64_t)(blockIdx.x * gridDim.y + blockIdx.y) * 2 + g) * a.dh + c] = s;
       }
     }
   }
@@ -258,7 +304,7 @@ __global__ void __launch_bounds__(1024) qk_norm_gains_kernel(const float* partia
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-struct Plan { int lanes, slots, tokens, grid_x, grid_y, rows, groups; size_t bytes; };
+struct Plan { int lanes, slots, tokens, many, grid_x, grid_y, rows, groups; size_t bytes; };
 
 Plan make_plan(int T, int heads, int normed, int dh, int per_head, bool backward) {
   Plan p = {};
@@ -268,8 +314,11 @@ Plan make_plan(int T, int heads, int normed, int dh, int per_head, bool backward
   p.grid_y = (heads + all - 1) / all;
   p.slots = (heads + p.grid_y - 1) / p.grid_y;
   p.tokens = all / p.slots;
-  const int tile = p.tokens * (backward ? BWD_ROWS : FWD_ROWS);
-  const int tiles = (T + tile - 1) / tile, resident = SMS * (backward ? BWD_BLOCKS : FWD_BLOCKS);
+  const int group = p.tokens * (backward ? BWD_ROWS : FWD_ROWS), resident = SMS * (backward ? BWD_BLOCKS : FWD_BLOCKS);
+  // several groups of rows between two barriers where every block then still has several turns, and 32 KB hold their angles
+  p.many = 1;
+  while (p.many < MOST_GROUPS && group * p.many * 2 * dh <= 4096 && (int64_t)T * p.grid_y >= (int64_t)group * p.many * 2 * 4 * resident) p.many *= 2;
+  const int tile = group * p.many, tiles = (T + tile - 1) / tile;
   p.grid_x = std::max(1, std::min(tiles, resident / std::min(p.grid_y, resident)));
   p.groups = per_head ? normed : 2;
   p.rows = per_head ? p.grid_x : p.grid_x * p.grid_y;
@@ -314,25 +363,30 @@ int fill_args(QkArgs& a, int kind, int pairs, int rot, float rope_base, const fl
   return PPU_OK;
 }
 
-template <int LANES, int HALVES, bool BWD>
+template <int LANES, int HALVES, int LAYER, bool BWD>
 int launch_qk(const QkArgs& a, const Plan& p, cudaStream_t st) {
   static PerDeviceFlag attr;
-  constexpr int most = 2 * BLOCK / LANES * (BWD ? BWD_ROWS : FWD_ROWS) * LANES * 4 * 8;      // one head to a block, all of it rotated
-  int bytes = 2 * p.tokens * (BWD ? BWD_ROWS : FWD_ROWS) * (a.rot / 2) * 8;
+  constexpr int most = 2 * BLOCK * (BWD ? BWD_ROWS : FWD_ROWS) * 8 * 4;      // one head to a block, all of it rotated: 64 KB forward
+  int bytes = 2 * p.tokens * (BWD ? BWD_ROWS : FWD_ROWS) * p.many * a.rot * 4;
   if (BWD) bytes = std::max(bytes, BLOCK / LANES * a.dh * 4);
-  if (!ppu_set_smem_once(attr, qk_norm_kernel<LANES, HALVES, BWD>, most)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
-  CUDA_OK(ppu_launch_dependent(qk_norm_kernel<LANES, HALVES, BWD>, dim3(p.grid_x, p.grid_y), BLOCK, bytes, st, a));
+  auto kernel = qk_norm_kernel<LANES, HALVES, LAYER, BWD>;
+  if (!ppu_set_smem_once(attr, kernel, most)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  CUDA_OK(ppu_launch_dependent(kernel, dim3(p.grid_x, p.grid_y), BLOCK, bytes, st, a));
   return PPU_OK;
+}
+template <int LANES, bool BWD>
+int launch_form(const QkArgs& a, const Plan& p, int pairs, cudaStream_t st) {
+  if (pairs == PPU_PAIRS_HALVES) return a.layer ? launch_qk<LANES, 1, 1, BWD>(a, p, st) : launch_qk<LANES, 1, 0, BWD>(a, p, st);
+  return a.layer ? launch_qk<LANES, 0, 1, BWD>(a, p, st) : launch_qk<LANES, 0, 0, BWD>(a, p, st);
 }
 template <bool BWD>
 int dispatch(const QkArgs& a, const Plan& p, int pairs, cudaStream_t st) {
-  const bool h = pairs == PPU_PAIRS_HALVES;
   switch (p.lanes) {
-    case 2: return h ? launch_qk<2, 1, BWD>(a, p, st) : launch_qk<2, 0, BWD>(a, p, st);
-    case 4: return h ? launch_qk<4, 1, BWD>(a, p, st) : launch_qk<4, 0, BWD>(a, p, st);
-    case 8: return h ? launch_qk<8, 1, BWD>(a, p, st) : launch_qk<8, 0, BWD>(a, p, st);
-    case 16: return h ? launch_qk<16, 1, BWD>(a, p, st) : launch_qk<16, 0, BWD>(a, p, st);
-    default: return h ? launch_qk<32, 1, BWD>(a, p, st) : launch_qk<32, 0, BWD>(a, p, st);
+    case 2: return launch_form<2, BWD>(a, p, pairs, st);
+    case 4: return launch_form<4, BWD>(a, p, pairs, st);
+    case 8: return launch_form<8, BWD>(a, p, pairs, st);
+    case 16: return launch_form<16, BWD>(a, p, pairs, st);
+    default: return launch_form<32, BWD>(a, p, pairs, st);
   }
 }
 
@@ -354,9 +408,8 @@ extern "C" int ppu_qk_norm_fwd(const void* qkv, int64_t ldx, const float* q_gain
   if (out == qkv && ldo != ldx) return ppu_fail(PPU_EINVAL, "out in the place of qkv needs its row stride");
   a.x = (const bf16*)qkv; a.ldx = ldx; a.out = (bf16*)out; a.ldo = ldo;
   a.heads = n_q + n_k + (out == qkv ? 0 : n_v);
-  Plan p = make_plan(T, n_q + n_k + n_v, n_q + n_k, d_head, a.per_head, false);
-  p.grid_y = (a.heads + p.slots - 1) / p.slots;
-  a.slots = p.slots; a.tokens = p.tokens;
+  const Plan p = make_plan(T, n_q + n_k + n_v, n_q + n_k, d_head, a.per_head, false);
+  a.slots = p.slots; a.tokens = p.tokens; a.groups_of_rows = p.many;
   return dispatch<false>(a, p, pairs, (cudaStream_t)cuda_stream);
 }
 
@@ -394,13 +447,9 @@ extern "C" int ppu_qk_norm_bwd(const void* dout, int64_t ldy, const void* qkv, i
   a.x = (const bf16*)qkv; a.ldx = ldx; a.dy = (const bf16*)dout; a.ldy = ldy; a.out = (bf16*)dqkv; a.ldo = ldo;
   // (the work is split as if the values were copied in any case: the order of the gains' sums does not depend on it)
   a.heads = n_q + n_k + (dqkv == dout ? 0 : n_v);
-  Plan p = make_plan(T, n_q + n_k + n_v, n_q + n_k, d_head, a.per_head, true);
+  const Plan p = make_plan(T, n_q + n_k + n_v, n_q + n_k, d_head, a.per_head, true);
   if (gains && workspace_bytes < p.bytes) return ppu_fail(PPU_ENOMEM, "workspace has %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  p.grid_y = (n_q + n_k + p.slots - 1) / p.slots;      // blocks that hold heads of queries and keys
-  p.rows = a.per_head ? p.grid_x : p.grid_x * p.grid_y;
-  a.norm_y = p.grid_y;
-  p.grid_y = (a.heads + p.slots - 1) / p.slots;
-  a.slots = p.slots; a.tokens = p.tokens; a.partial = gains ? (float*)workspace : nullptr; a.groups = p.groups;
+  a.slots = p.slots; a.tokens = p.tokens; a.groups_of_rows = p.many; a.partial = gains ? (float*)workspace : nullptr; a.groups = p.groups;
   rc = dispatch<true>(a, p, pairs, st);
   if (rc || !gains) return rc;
   const int columns = p.groups * d_head, q_columns = (a.per_head ? n_q : 1) * d_head;
