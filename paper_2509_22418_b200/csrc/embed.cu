@@ -20,8 +20,8 @@ int ppu_fail(int code, const char* fmt, ...);
 namespace {
 
 constexpr int MAX_D = 16384, MAX_T = 1 << 20, MAX_V = 1 << 22;
-constexpr int SORT_THREADS = 1024, SORT_TOKENS = 16384;      // one block, 16 tokens a thread
-constexpr int TILE = 512, TILE_WARPS = 8;                    // longer lists: tokens of a warp, warps of a block
+constexpr int SORT_THREADS = 1024, SORT_TOKENS = 8192;       // one block, 8 tokens a thread (16384 so take 43 us, in tiles 32)
+constexpr int TILE = 256, TILE_WARPS = 8;                    // longer lists: tokens of a warp, warps of a block
 constexpr int MAX_DIGITS = 256;
 constexpr int SMS = 148;                                     // work is split for a B200
 
@@ -72,15 +72,20 @@ __global__ void __launch_bounds__(256) embed_lookup_kernel(const int32_t* ids, c
 
 // ---- sorting tokens by id ------------------------------------------------------------------------
 // Least significant digit first, `bits` bits a pass.  A warp owns consecutive tokens and takes 32 at a time: lanes
-// with the same digit find each other by match, so that a token's rank among its warp's tokens of that digit
+// with the same digit find each other by a vote for each bit, so that a token's rank among its warp's tokens of that digit
 // needs no atomics and the order is kept.  Absent tokens have the key V, which sorts behind all ids.
 __device__ __forceinline__ uint32_t key_of(int id, int V) { return id < 0 || id >= V ? (uint32_t)V : (uint32_t)id; }
 
 // ranks 32 tokens; counter: the warp's own, one for each digit
-__device__ __forceinline__ uint32_t warp_rank(uint32_t digit, bool valid, uint32_t* counter, int lane) {
-  const uint32_t peers = __match_any_sync(0xffffffffu, valid ? digit : 0xffffffffu);
+__device__ __forceinline__ uint32_t warp_rank(uint32_t digit, int bits, bool valid, uint32_t* counter, int lane) {
+  uint32_t peers = __ballot_sync(0xffffffffu, valid);
+  for (int k = 0; k < bits; ++k) {
+    const bool bit = digit >> k & 1;
+    const uint32_t v = __ballot_sync(0xffffffffu, bit);
+    peers &= bit ? v : ~v;
+  }
   uint32_t before = 0;
-  const int leader = __ffs(peers) - 1;
+  const int leader = valid ? __ffs(peers) - 1 : lane;
   if (valid && lane == leader) { before = counter[digit]; counter[digit] = before + __popc(peers); }
   before = __shfl_sync(0xffffffffu, before, leader);
   __syncwarp();
@@ -128,7 +133,7 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_fill_kernel(const int
     __syncthreads();
     uint32_t rank[ITEMS];
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) rank[j] = warp_rank((key[j] >> shift) & (D - 1), true, counter + warp * D, lane);
+    for (int j = 0; j < ITEMS; ++j) rank[j] = warp_rank((key[j] >> shift) & (D - 1), bits, true, counter + warp * D, lane);
     __syncthreads();
     // exclusive sums of the counters in the order (digit, warp): a thread takes a digit's warps (or some of them)
     const int per = 32 * D >= SORT_THREADS ? 32 * D / SORT_THREADS : 1;      // entries a thread (D <= 256: 8 at most)
@@ -189,25 +194,28 @@ __global__ void __launch_bounds__(TILE_WARPS * 32) embed_count_kernel(const int3
   for (int i = lane; i < D; i += 32) counter[warp][i] = 0;
   __syncwarp();
   bool wrong = false;
+  uint32_t key[TILE / 32];
+#pragma unroll
   for (int j = 0; j < TILE / 32; ++j) {
     const int i = tile * TILE + j * 32 + lane;
-    const bool valid = i < T;
-    if (ids && valid) wrong |= ids[i] >= V;
-    const uint32_t digit = valid ? (tile_key(ids, keys, i, V) >> shift) & (D - 1) : 0;
-    warp_rank(digit, valid, counter[warp], lane);
+    key[j] = 0;
+    if (i < T) { key[j] = tile_key(ids, keys, i, V); if (ids) wrong |= ids[i] >= V; }
   }
+#pragma unroll
+  for (int j = 0; j < TILE / 32; ++j) warp_rank((key[j] >> shift) & (D - 1), bits, tile * TILE + j * 32 + lane < T, counter[warp], lane);
   if (wrong && flags) atomicExch(flags + PPU_FLAG_TOKEN, 1);
   if (tile < tiles)
     for (int i = lane; i < D; i += 32) hist[(int64_t)i * tiles + tile] = counter[warp][i];
 }
 
-__global__ void __launch_bounds__(256) embed_offsets_kernel(uint32_t* hist, uint32_t* totals, int tiles) {
+__global__ void __launch_bounds__(1024) embed_offsets_kernel(uint32_t* hist, uint32_t* totals, int tiles) {
   pdl_wait(); pdl_trigger();
-  __shared__ uint32_t s_sum[8];
+  __shared__ uint32_t s_sum[32];
+  const int warps = blockDim.x / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* row = hist + (int64_t)blockIdx.x * tiles;
   uint32_t carry = 0;
-  for (int base = 0; base < tiles; base += 256) {
+  for (int base = 0; base < tiles; base += blockDim.x) {
     const int i = base + threadIdx.x;
     const uint32_t x = i < tiles ? row[i] : 0;
     uint32_t s = x;
@@ -215,7 +223,7 @@ __global__ void __launch_bounds__(256) embed_offsets_kernel(uint32_t* hist, uint
     if (lane == 31) s_sum[warp] = s;
     __syncthreads();
     uint32_t before = carry, all = 0;
-    for (int w = 0; w < 8; ++w) { if (w < warp) before += s_sum[w]; all += s_sum[w]; }
+    for (int w = 0; w < warps; ++w) { if (w < warp) before += s_sum[w]; all += s_sum[w]; }
     if (i < tiles) row[i] = before + s - x;
     carry += all;
     __syncthreads();
@@ -241,14 +249,20 @@ __global__ void __launch_bounds__(TILE_WARPS * 32) embed_place_kernel(const int3
   }
   __syncthreads();
   if (tile >= tiles) return;
-  for (int i = lane; i < D; i += 32) counter[warp][i] = s_base[i] + hist[(int64_t)i * tiles + tile];
-  __syncwarp();
+  uint32_t key[TILE / 32], ord[TILE / 32];
+#pragma unroll
   for (int j = 0; j < TILE / 32; ++j) {
     const int i = tile * TILE + j * 32 + lane;
-    const bool valid = i < T;
-    const uint32_t key = valid ? tile_key(ids, keys, i, V) : 0;
-    const uint32_t to = warp_rank((key >> shift) & (D - 1), valid, counter[warp], lane);
-    if (valid) { keys_out[to] = key; order_out[to] = ids ? (uint32_t)i : order[i]; }
+    key[j] = ord[j] = 0;
+    if (i < T) { key[j] = tile_key(ids, keys, i, V); ord[j] = ids ? (uint32_t)i : order[i]; }
+  }
+  for (int i = lane; i < D; i += 32) counter[warp][i] = s_base[i] + hist[(int64_t)i * tiles + tile];
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < TILE / 32; ++j) {
+    const bool valid = tile * TILE + j * 32 + lane < T;
+    const uint32_t to = warp_rank((key[j] >> shift) & (D - 1), bits, valid, counter[warp], lane);
+    if (valid) { keys_out[to] = key[j]; order_out[to] = ord[j]; }
   }
 }
 
@@ -263,20 +277,20 @@ struct SumArgs {
   int T, d, V, piece, pieces, slices, lanes;       // lanes: of a group, which covers 8 * lanes columns
 };
 
+// dE's row of an id, from its sum and, where there is something to add to, that row's columns `x`
 template <typename TG>
-__device__ __forceinline__ void finish_row(const SumArgs& a, uint32_t id, int col, F8 v) {
+__device__ __forceinline__ void finish_row(const SumArgs& a, uint32_t id, int col, F8 v, const F8& x) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v.f[j] *= a.scale;
-  if (a.add) {
-    const F8 x = load8((const TG*)a.add + (int64_t)id * a.ldadd + col);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v.f[j] += x.f[j];
-  }
+  for (int j = 0; j < 8; ++j) v.f[j] = a.add ? fmaf(a.scale, v.f[j], x.f[j]) : a.scale * v.f[j];
   store8((TG*)a.dE + (int64_t)id * a.ldde + col, v);
 }
+template <typename TG>
+__device__ __forceinline__ F8 add_row(const SumArgs& a, uint32_t id, int col) { return load8((const TG*)a.add + (int64_t)id * a.ldadd + col); }
 
-constexpr int AHEAD = 4;                            // rows in flight of a group
-template <typename TD, typename TG>
+// Rows in flight of a group.  The rows to add to are read with the tokens that end their ids: read when a sum is done, one after another, they made
+// 4099 x 768 onto an fp32 table take 40 us.
+constexpr int AHEAD = 4;
+template <typename TD, typename TG, bool ADD>
 __global__ void __launch_bounds__(256) embed_sum_kernel(const SumArgs a) {
   pdl_wait(); pdl_trigger();
   const int group = (blockIdx.x * 256 + threadIdx.x) / a.lanes;
@@ -284,61 +298,65 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const SumArgs a) {
   const int col = 8 * (slice * a.lanes + (int)threadIdx.x % a.lanes);
   if (p >= a.pieces || col >= a.d) return;
   const int lo = p * a.piece, hi = min(a.T, lo + a.piece);
-  uint32_t cur = a.keys[lo];
-  if (cur >= (uint32_t)a.V) return;                 // absent tokens alone
-  bool begun = lo > 0 && a.keys[lo - 1] == cur;     // the current id began in an earlier piece
+  const uint32_t V = a.V, NONE = 0xffffffffu;
+  bool begun = lo > 0 && a.keys[lo - 1] == a.keys[lo];      // the first id began in an earlier piece
   F8 sum = {};
   const TD* dout = (const TD*)a.dout + col;
+  bool ended = true;
   for (int i0 = lo; i0 < hi; i0 += AHEAD) {
-    F8 x[AHEAD];
-    uint32_t id[AHEAD];
+    F8 x[AHEAD], y[AHEAD];
+    uint32_t id[AHEAD + 1];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      id[j] = i0 + j < hi ? a.keys[i0 + j] : (uint32_t)a.V;
-      if (id[j] < (uint32_t)a.V) x[j] = load8(dout + (int64_t)a.order[i0 + j] * a.ldd);
-    }
+    for (int j = 0; j <= AHEAD; ++j) id[j] = i0 + j < min(hi + 1, a.T) ? a.keys[i0 + j] : NONE;
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) {
-      if (id[j] >= (uint32_t)a.V) break;            // (nothing but absent tokens, or the piece's end, follows)
-      if (id[j] != cur) {
-        if (begun) store8(a.head + (int64_t)p * a.d + col, sum);
-        else finish_row<TG>(a, cur, col, sum);
-        begun = false; cur = id[j]; sum = F8{};
+    for (int j = 0; j < AHEAD; ++j)
+      if (i0 + j < hi && id[j] < V) {
+        x[j] = load8(dout + (int64_t)a.order[i0 + j] * a.ldd);
+        if (ADD && id[j + 1] != id[j]) y[j] = add_row<TG>(a, id[j], col);
       }
 #pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (i0 + j >= hi || id[j] >= V) break;        // (nothing but absent tokens follows)
+#pragma unroll
       for (int e = 0; e < 8; ++e) sum.f[e] += x[j].f[e];
+      ended = id[j + 1] != id[j];
+      if (ended) {
+        if (begun) store8(a.head + (int64_t)p * a.d + col, sum);
+        else finish_row<TG>(a, id[j], col, sum, y[j]);
+        begun = false; sum = F8{};
+      }
     }
   }
-  const bool goes_on = hi < a.T && a.keys[hi] == cur;
-  if (begun) store8(a.head + (int64_t)p * a.d + col, sum);
-  else if (goes_on) store8(a.last + (int64_t)p * a.d + col, sum);
-  else finish_row<TG>(a, cur, col, sum);
+  if (!ended) store8((begun ? a.head : a.last) + (int64_t)p * a.d + col, sum);      // the id goes on in the next piece
 }
 
-// One block for each piece in which an id begins that goes on behind it, and 256 columns: warps add up consecutive shares
-// of the pieces' sums, and the shares are added in order.
+// One block for each piece in which an id begins that goes on behind it, and 256 columns: its warps add up consecutive shares
+// of the pieces' sums, and the shares are added in order.  (A warp for each piece and blocks of 32 or 8 warps for the longest: 3 to 6 us more for up
+// to 8192 tokens.)
+constexpr int JOIN_WARPS = 8;
 template <typename TG>
-__global__ void __launch_bounds__(256) embed_join_kernel(const SumArgs a) {
+__global__ void __launch_bounds__(32 * JOIN_WARPS) embed_join_kernel(const SumArgs a) {
   pdl_wait(); pdl_trigger();
-  __shared__ float s_sum[8][256];
-  const int p = blockIdx.x, lo = p * a.piece, hi = min(a.T, lo + a.piece);
+  __shared__ float s_sum[JOIN_WARPS][256];
+  const int p = blockIdx.x;
+  const int64_t lo = (int64_t)p * a.piece, hi = lo + a.piece;
   if (hi >= a.T) return;
   const uint32_t id = a.keys[hi - 1];
   if (id >= (uint32_t)a.V || a.keys[hi] != id || (a.keys[lo] == id && lo > 0 && a.keys[lo - 1] == id)) return;
-  int q = p + 1, end = a.pieces;                    // pieces p + 1 .. q begin with this id; q + 1 does not
-  while (end - q > 1) {
-    const int mid = (q + end) / 2;
-    if (a.keys[(int64_t)mid * a.piece] == id) q = mid; else end = mid;
+  int n = 0;                                        // pieces p + 1 .. p + n begin with this id (keys are sorted)
+  for (int more = 32 * JOIN_WARPS; more == 32 * JOIN_WARPS; n += more) {
+    const int64_t at = hi + (int64_t)(n + (int)threadIdx.x) * a.piece;
+    more = __syncthreads_count(at < a.T && a.keys[at] == id);
   }
-  const int n = q - p, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int col = blockIdx.y * 256 + 8 * lane;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = blockIdx.y * 256 + 8 * lane;
   F8 sum = {};
   if (col < a.d) {
     if (warp == 0) sum = load8(a.last + (int64_t)p * a.d + col);
-    const int e = (int)((int64_t)n * (warp + 1) / 8);
-#pragma unroll 4
-    for (int i = (int)((int64_t)n * warp / 8); i < e; ++i) {
-      const F8 x = load8(a.head + (int64_t)(p + 1 + i) * a.d + col);
+    const float* head = a.head + (int64_t)(p + 1) * a.d + col;
+    const int end = (int)((int64_t)n * (warp + 1) / JOIN_WARPS);
+#pragma unroll 8
+    for (int i = (int)((int64_t)n * warp / JOIN_WARPS); i < end; ++i) {
+      const F8 x = load8(head + (int64_t)i * a.d);
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum.f[j] += x.f[j];
     }
@@ -347,10 +365,10 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const SumArgs a) {
   for (int j = 0; j < 8; ++j) s_sum[warp][8 * lane + j] = sum.f[j];
   __syncthreads();
   if (warp > 0 || col >= a.d) return;
-  for (int w = 1; w < 8; ++w)
+  for (int w = 1; w < JOIN_WARPS; ++w)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum.f[j] += s_sum[w][8 * lane + j];
-  finish_row<TG>(a, id, col, sum);
+  finish_row<TG>(a, id, col, sum, a.add ? add_row<TG>(a, id, col) : F8{});
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -366,7 +384,12 @@ Plan make_plan(int T, int d, int V) {
   p.lanes = 1;
   while (p.lanes < 32 && p.lanes * 8 < d) p.lanes *= 2;
   p.slices = (d + 8 * p.lanes - 1) / (8 * p.lanes);
-  p.piece = std::max(32, (T + 2047) / 2048);
+  // Pieces of 32 tokens; shorter (4 at least) where they would not give a quarter of the machine's threads something to do, longer where they
+  // would be more than its threads (each leaves up to two sums).
+  const int64_t threads = (int64_t)p.slices * p.lanes;
+  p.piece = 32;
+  while (p.piece > 4 && T / p.piece * threads < (int64_t)SMS * 256) p.piece /= 2;
+  while (T / p.piece * threads > (int64_t)SMS * 2048) p.piece *= 2;
   p.pieces = (T + p.piece - 1) / p.piece;
   size_t at = 0;
   auto take = [&](size_t n) { const size_t was = at; at += (n + 255) / 256 * 256; return was; };
@@ -412,8 +435,10 @@ template <typename TD, typename TG>
 int sums(const SumArgs& a, cudaStream_t st) {
   const int64_t groups = (int64_t)a.pieces * a.slices;
   const int per_block = 256 / a.lanes;
-  CUDA_OK(ppu_launch_dependent(embed_sum_kernel<TD, TG>, (unsigned)((groups + per_block - 1) / per_block), 256, 0, st, a));
-  if (a.pieces > 1) CUDA_OK(ppu_launch_dependent(embed_join_kernel<TG>, dim3(a.pieces, (a.d + 255) / 256), 256, 0, st, a));
+  const unsigned blocks = (unsigned)((groups + per_block - 1) / per_block);
+  if (a.add) CUDA_OK(ppu_launch_dependent(embed_sum_kernel<TD, TG, true>, blocks, 256, 0, st, a));
+  else CUDA_OK(ppu_launch_dependent(embed_sum_kernel<TD, TG, false>, blocks, 256, 0, st, a));
+  if (a.pieces > 1) CUDA_OK(ppu_launch_dependent(embed_join_kernel<TG>, dim3(a.pieces, (a.d + 255) / 256), 32 * JOIN_WARPS, 0, st, a));
   return PPU_OK;
 }
 
@@ -476,8 +501,7 @@ extern "C" int ppu_embed_bwd(const int32_t* ids, const void* dout, int64_t ldd, 
     int rc2 = PPU_OK;
     if (T <= 1024) rc2 = sort_fill<1>(ids, T, V, p, ws, f, fill_blocks, log2, flags, st);
     else if (T <= 4096) rc2 = sort_fill<4>(ids, T, V, p, ws, f, fill_blocks, log2, flags, st);
-    else if (T <= 8192) rc2 = sort_fill<8>(ids, T, V, p, ws, f, fill_blocks, log2, flags, st);
-    else rc2 = sort_fill<16>(ids, T, V, p, ws, f, fill_blocks, log2, flags, st);
+    else rc2 = sort_fill<8>(ids, T, V, p, ws, f, fill_blocks, log2, flags, st);
     if (rc2) return rc2;
   } else {
     uint32_t *hist = (uint32_t*)(ws + p.hist), *totals = (uint32_t*)(ws + p.totals);
@@ -489,7 +513,7 @@ extern "C" int ppu_embed_bwd(const int32_t* ids, const void* dout, int64_t ldd, 
       const int shift = pass * p.bits;
       CUDA_OK(ppu_launch_dependent(embed_count_kernel, blocks + (pass == 0 ? more : 0), TILE_WARPS * 32, 0, st, from, k_in, T, V, shift, p.bits, hist, p.tiles, blocks, f,
                                    log2, pass == 0 ? flags : nullptr));
-      CUDA_OK(ppu_launch_dependent(embed_offsets_kernel, 1 << p.bits, 256, 0, st, hist, totals, p.tiles));
+      CUDA_OK(ppu_launch_dependent(embed_offsets_kernel, 1 << p.bits, std::min(1024, (p.tiles + 31) / 32 * 32), 0, st, hist, totals, p.tiles));
       CUDA_OK(ppu_launch_dependent(embed_place_kernel, blocks, TILE_WARPS * 32, 0, st, from, k_in, o_in, T, V, shift, p.bits, hist, totals, p.tiles, k_out, o_out));
       std::swap(k_in, k_out); std::swap(o_in, o_out);
     }
