@@ -643,10 +643,298 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
   }
 }
 
+// ---- matrices whose shorter side is at most 128: all of it on chip, in one launch ---------------------------
+// A cluster works a matrix, each CTA up to 256 columns of it (of the transpose, where it has more rows): X in tensor memory, its fp16 copy
+// in shared memory, where both products read it.  The CTAs add up their parts of A through each other's shared memory,
+// each a share of its columns, in the order of their ranks; P is formed by each for itself.  The sum X = a X + P X is formed by the tensor
+// cores on X's own accumulator, which holds a X by then.  A step is a chain of short dependent works (a product, a pass over its result, a
+// barrier): 4 us for 100 x 100, 6 for 128 x 256, 12 where eight CTAs join their sums, against 18 and more through global memory (100 x 100 105 -> 33 us).
+// 512 threads: no change.
+constexpr int SMALL_SIDE = 128, SMALL_COLS = 256, SMALL_CTAS = 8;
+constexpr int SMALL_THREADS = 256, SMALL_WARPS = SMALL_THREADS / 32, PARTS = SMALL_WARPS / 4;      // warps of a quarter of the rows
+constexpr int SLAB = 128 * BK * 2;                   // 128 rows x 64 columns of fp16
+constexpr int SMALL_X = 4 * SLAB, SMALL_A = 2 * SLAB, SMALL_SUMS = 128 * 128 * 4;
+constexpr int SMALL_SMEM = SMALL_X + 2 * SMALL_A + SMALL_SUMS + 1024;
+
+struct SmallP {
+  PrepP in;                          // G, momentum, norm
+  int side, length, left, chunk, steps;      // chunk: columns of a CTA, a multiple of 32
+  bf16* O; float scale, gram;
+  float b[MAX_STEPS], c[MAX_STEPS], t[MAX_STEPS], f[MAX_STEPS];      // t: what X is multiplied by to be added to, f: what brings the sum back
+  int* flags;
+};
+
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const bf16* p) { return __bfloat162float(*p); }
+// elements (i, j .. j + 31) of the matrix (of its transpose, where it has more rows than columns); `have` of them are there
+template <typename T> __device__ __forceinline__ void load32(const T* base, int64_t ld, bool left, bool vec, int i, int j, int have, float (&u)[32]) {
+  if (left && vec) {
+    const T* p = base + i * ld + j;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float4 v = 4 * q < have ? load4<1>(p + 4 * q, 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+      u[4 * q] = v.x; u[4 * q + 1] = v.y; u[4 * q + 2] = v.z; u[4 * q + 3] = v.w;
+    }
+  } else {
+    const T* p = left ? base + i * ld + j : base + j * ld + i;
+    const int64_t step = left ? 1 : ld;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) u[q] = q < have ? load1(p + q * step) : 0.f;
+  }
+}
+__device__ __forceinline__ void store32(float* base, int64_t ld, bool left, bool vec, int i, int j, int have, const float (&u)[32]) {
+  if (left && vec) {
+    float* p = base + i * ld + j;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (4 * q < have) *reinterpret_cast<float4*>(p + 4 * q) = make_float4(u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]);
+  } else {
+    float* p = left ? base + i * ld + j : base + j * ld + i;
+    const int64_t step = left ? 1 : ld;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) if (q < have) p[q * step] = u[q];
+  }
+}
+// 8 fp16 of row r from column c (a multiple of 8) on, in slabs of 64 columns with 128-byte swizzle
+__device__ __forceinline__ uint32_t slab_at(int r, int c) { return (c >> 6) * SLAB + r * 128 + ((((c >> 3) & 7) ^ (r & 7)) << 4); }
+__device__ __forceinline__ float4 load_peer(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+
+template <typename TG, int VEC>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __grid_constant__ SmallP p) {
+  extern __shared__ uint8_t smem_raw[];
+  // (the window starts at the same offset in all CTAs of a cluster)
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t *sX = smem, *sA = smem + SMALL_X, *sP = sA + SMALL_A;
+  float4* sums = reinterpret_cast<float4*>(sP + SMALL_A);      // [32 fours of columns][128 rows]
+  __shared__ uint64_t s_bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  __shared__ double s_part[SMALL_WARPS], s_total;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane;
+  uint32_t rank, ctas;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+  const int b = blockIdx.x / ctas;
+  volatile int* abort_flag = &s_abort;
+  const uint32_t bar = smem_u32(&s_bar);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) tmem_alloc(smem_u32(&s_tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tX = s_tmem + ((uint32_t)(quarter * 32) << 16), tAcc = tX + SMALL_COLS;      // X, and the sums of A and of A A
+  pdl_wait(); pdl_trigger();
+
+  const int col0 = (int)rank * p.chunk, own = max(0, min(p.chunk, p.length - col0)), chunks = p.chunk / 32;
+  uint32_t parity = 0;
+  // fn(k) issues one thread's products; all wait for them
+  auto products = [&](auto fn) {
+    asm volatile("fence.proxy.async;" ::: "memory");       // (the operands in shared memory were written by plain stores)
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      tc_fence_after();
+      asm volatile("fence.proxy.async;" ::: "memory");
+      fn();
+      umma_commit(bar);
+    }
+    wait_for(abort_flag, p.flags, [&] { return mbar_try(bar, parity); });      // (where it gives up the results are not valid, and flags say so)
+    parity ^= 1;
+    tc_fence_after();
+  };
+  auto cluster_barrier = [&] { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+
+  // u, the new momentum and the sum of squares
+  double sum = 0.0;
+  for (int c = part; c < chunks; c += PARTS) {
+    const int j = col0 + 32 * c, have = row < p.side ? min(32, col0 + own - j) : 0;
+    float u[32];
+    load32((const TG*)p.in.G + b * p.in.stride_g, p.in.ldg, p.left, VEC, row, j, have, u);
+    if (p.in.m) {
+      float m[32];
+      load32(p.in.m + b * p.in.stride_m, p.in.ldm, p.left, VEC, row, j, have, m);
+#pragma unroll
+      for (int q = 0; q < 32; ++q) m[q] = fmaf(p.in.beta, m[q], p.in.w * u[q]);
+      store32(p.in.m_out + b * p.in.stride_m_out, p.in.ldm_out, p.left, VEC, row, j, have, m);
+#pragma unroll
+      for (int q = 0; q < 32; ++q) u[q] = p.in.nesterov ? fmaf(p.in.beta, m[q], p.in.w * u[q]) : m[q];
+    }
+    uint32_t bits[32];
+#pragma unroll
+    for (int q = 0; q < 32; ++q) { sum = fma((double)u[q], (double)u[q], sum); bits[q] = __float_as_uint(u[q]); }
+    tmem_st32(tX + 32 * c, bits);
+  }
+  tmem_st_wait();
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_part[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < SMALL_WARPS; ++w) sum += s_part[w];
+    s_total = sum;
+  }
+  cluster_barrier();
+  double norm = 0.0;
+  for (uint32_t r = 0; r < ctas; ++r) {
+    double d;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(d) : "r"(map_to_rank(smem_u32(&s_total), r)));
+    norm += d;
+  }
+  norm = sqrt(norm) + (double)p.in.eps;
+  const double inv = (norm > 0.0 ? 1.0 / norm : norm == 0.0 ? 0.0 : norm) * (double)(1 << X_EXP);      // (a matrix of zeros stays one; NaN stays NaN)
+
+  for (int step = 0; step <= p.steps; ++step) {
+    // X (after the last step O): its fp16 copy, and what the next product is added to
+    for (int c = part; c < chunks; c += PARTS) {
+      uint32_t r[32];
+      tmem_ld32(tX + 32 * c, r);
+      tmem_ld_wait();
+      float x[32];
+#pragma unroll
+      for (int q = 0; q < 32; ++q) x[q] = step == 0 ? (float)(__uint_as_float(r[q]) * inv) : __uint_as_float(r[q]) * p.f[step > 0 ? step - 1 : 0];
+      if (step < p.steps) {
+        const float t = p.t[step];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<uint4*>(sX + slab_at(row, 32 * c + 8 * q)) =
+              make_uint4(half2_bits(x[8 * q], x[8 * q + 1]), half2_bits(x[8 * q + 2], x[8 * q + 3]), half2_bits(x[8 * q + 4], x[8 * q + 5]), half2_bits(x[8 * q + 6], x[8 * q + 7]));
+#pragma unroll
+        for (int q = 0; q < 32; ++q) r[q] = __float_as_uint(t * x[q]);
+        tmem_st32(tX + 32 * c, r);
+      } else {
+        const int j = col0 + 32 * c, have = row < p.side ? min(32, col0 + own - j) : 0;
+        const int m = p.left ? p.side : p.length, n = p.left ? p.length : p.side;
+        bf16* O = p.O + (int64_t)b * m * n;
+        if (p.left) {                                // (rows that are not whole 16 bytes go through shared memory)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = p.scale * x[8 * q + e];
+            const uint4 v = gemm_tc_detail::pack8_bf16(y);
+            if (n % 8) *reinterpret_cast<uint4*>(sX + slab_at(row, 32 * c + 8 * q)) = v;
+            else if (8 * q < have) *reinterpret_cast<uint4*>(O + (int64_t)row * n + j + 8 * q) = v;
+          }
+        } else {
+          bf16* o = O + (int64_t)j * n + row;
+#pragma unroll
+          for (int q = 0; q < 32; ++q) if (q < have) o[(int64_t)q * n] = __float2bfloat16_rn(p.scale * x[q]);
+        }
+      }
+    }
+    if (step == p.steps) {
+      if (p.left && p.length % 8) {
+        __syncthreads();
+        for (int r = warp; r < p.side; r += SMALL_WARPS)
+          for (int c = lane; c < own; c += 32)
+            p.O[((int64_t)b * p.side + r) * p.length + col0 + c] = *reinterpret_cast<const bf16*>(sX + slab_at(r, c & ~7) + (c & 7) * 2);
+      }
+      break;
+    }
+    tmem_st_wait();
+    // A = X X^T of this CTA's columns
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 4) << 24);
+    const uint32_t aX = smem_u32(sX), aA = smem_u32(sA), aP = smem_u32(sP), tBase = s_tmem;
+    products([&] {
+      for (int k = 0; k < p.chunk / UMMA_K; ++k) {
+        const uint64_t d = make_desc(aX + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024);
+        umma_bf16(tBase + SMALL_COLS, d, d, idesc | (uint32_t)(128 >> 3) << 17, k > 0);
+      }
+    });
+    // A in fp16, of all CTAs' sums
+#pragma unroll 1
+    for (int c = 128 / PARTS * part; c < 128 / PARTS * (part + 1); c += 32) {
+      uint32_t r[32];
+      tmem_ld32(tAcc + c, r);
+      tmem_ld_wait();
+      if (ctas == 1) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint4 v;
+          uint32_t* o = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = half2_bits(p.gram * __uint_as_float(r[8 * q + 2 * e]), p.gram * __uint_as_float(r[8 * q + 2 * e + 1]));
+          *reinterpret_cast<uint4*>(sA + slab_at(row, c + 8 * q)) = v;
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          sums[(c / 4 + q) * 128 + row] = make_float4(__uint_as_float(r[4 * q]), __uint_as_float(r[4 * q + 1]), __uint_as_float(r[4 * q + 2]), __uint_as_float(r[4 * q + 3]));
+      }
+    }
+    if (ctas > 1) {
+      cluster_barrier();
+      const int share = 32 * 128 / (int)ctas;        // fours of columns x rows
+      for (int e = threadIdx.x; e < share; e += SMALL_THREADS) {
+        const int at = (int)rank * share + e, r = at & 127, c = 4 * (at >> 7);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f), x[SMALL_CTAS];
+        const uint32_t from = smem_u32(sums + at);
+#pragma unroll
+        for (uint32_t q = 0; q < SMALL_CTAS; ++q) x[q] = q < ctas ? load_peer(map_to_rank(from, q)) : v;
+#pragma unroll
+        for (uint32_t q = 0; q < SMALL_CTAS; ++q) { v.x += x[q].x; v.y += x[q].y; v.z += x[q].z; v.w += x[q].w; }
+        const uint32_t h0 = half2_bits(p.gram * v.x, p.gram * v.y), h1 = half2_bits(p.gram * v.z, p.gram * v.w);
+        const uint32_t to = aA + slab_at(r, c & ~7) + (c & 4) * 2;
+        for (uint32_t q = 0; q < ctas; ++q) asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to_rank(to, q)), "r"(h0), "r"(h1) : "memory");
+      }
+      asm volatile("fence.proxy.async;" ::: "memory");
+      cluster_barrier();
+    }
+    // P = b A + c A A
+    products([&] {
+      for (int k = 0; k < 128 / UMMA_K; ++k) {
+        const uint64_t d = make_desc(aA + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024);
+        umma_bf16(tBase + SMALL_COLS, d, d, idesc | (uint32_t)(128 >> 3) << 17, k > 0);
+      }
+    });
+#pragma unroll 1
+    for (int c = 128 / PARTS * part; c < 128 / PARTS * (part + 1); c += 32) {
+      uint32_t r[32];
+      tmem_ld32(tAcc + c, r);
+      tmem_ld_wait();
+      const float fb = p.b[step], fc = p.c[step];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4 a = *reinterpret_cast<const uint4*>(sA + slab_at(row, c + 8 * q));
+        const uint32_t* h = reinterpret_cast<const uint32_t*>(&a);
+        uint4 v;
+        uint32_t* o = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 x = half2_floats(h[e]);
+          o[e] = half2_bits(fmaf(fc, __uint_as_float(r[8 * q + 2 * e]), fb * x.x), fmaf(fc, __uint_as_float(r[8 * q + 2 * e + 1]), fb * x.y));
+        }
+        *reinterpret_cast<uint4*>(sP + slab_at(row, c + 8 * q)) = v;
+      }
+    }
+    // X = a X + P X
+    products([&] {
+      for (int k = 0; k < 128 / UMMA_K; ++k)
+        umma_bf16(tBase, make_desc(aP + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024), make_desc(aX + k * 2048, SLAB, 1024),
+                  idesc | (1u << 16) | (uint32_t)(p.chunk >> 3) << 17, 1u);
+    });
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_barrier();                                 // no CTA leaves while another may still read its shared memory
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(s_tmem, 512);
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------------------
 struct Plan {
   int side, blocks; int64_t ld, lds;
   bool pair;
+  int ctas, chunk;                   // on chip: CTAs of a matrix (0: not so), columns of each
   int tiles_s, sym, tiles_m, tiles_n, splits[2], workers;
   size_t partial, hi[2], x, a, a2, p, sums, counters, bytes;
   int rows32, cols32, side32;
@@ -674,6 +962,15 @@ Plan make_plan(int batch, int m, int n, int steps) {
   for (int i = 0; i < 2; ++i) {
     const int64_t k_blocks = ((i == 0 ? std::max(m, n) : q.side) + KH * BK - 1) / (KH * BK);
     q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / (q.pair ? 32 : 8)}));
+  }
+  // on chip where a cluster of up to 8 CTAs holds the matrix
+  const int length = std::max(m, n);
+  if (steps > 0 && q.side <= SMALL_SIDE && length <= SMALL_COLS * SMALL_CTAS) {
+    q.ctas = 1;
+    while (q.ctas * SMALL_COLS < length) q.ctas *= 2;
+    q.chunk = ((length + q.ctas - 1) / q.ctas + 31) / 32 * 32;
+    q.bytes = 256;                                 // (nothing is kept in it; checked as any workspace)
+    return q;
   }
   size_t at = 0;
   auto take = [&](size_t k) { const size_t was = at; at += (k + 255) / 256 * 256; return was; };
@@ -775,6 +1072,22 @@ int launch_steps(const Maps& maps, const KernelP& p, bool pair, cudaStream_t st)
   return PPU_OK;
 }
 
+int launch_small(const SmallP& p, int batch, int ctas, bool vec, bool f32, cudaStream_t st) {
+  static PerDeviceFlag attr_set[4];
+  void (*kernel)(SmallP) = f32 ? (vec ? ortho_small_kernel<float, 1> : ortho_small_kernel<float, 0>) : vec ? ortho_small_kernel<bf16, 1> : ortho_small_kernel<bf16, 0>;
+  if (!ppu_set_smem_once(attr_set[2 * f32 + vec], kernel, SMALL_SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)batch * ctas); cfg.blockDim = dim3(SMALL_THREADS); cfg.dynamicSmemBytes = SMALL_SMEM; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p));
+  return PPU_OK;
+}
+
 template <typename TG>
 int prepare(const PrepP& p, const Plan& q, int batch, bool vec, cudaStream_t st) {
   const dim3 grid(q.blocks, batch), blocks32((q.rows32 * q.cols32 + 7) / 8, batch);
@@ -845,6 +1158,17 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   pp.O = steps == 0 ? (bf16*)O : nullptr;
   pp.counters = (unsigned*)(ws + q.counters); pp.n_counters = q.n_counters;
   const bool vec = n % 4 == 0 && aligned(G, ldg, stride_g, 4 * g_bytes) && aligned(momentum, ldm, stride_m, 16) && aligned(momentum_out, ldmo, stride_mo, 16);
+  if (q.ctas > 0) {
+    SmallP p = {};
+    p.in = pp; p.side = q.side; p.length = std::max(m, n); p.left = m <= n; p.chunk = q.chunk; p.steps = steps;
+    p.O = (bf16*)O; p.scale = std::ldexp(scale, -X_EXP); p.gram = std::ldexp(1.f, A_EXP - 2 * X_EXP); p.flags = flags;
+    for (int k = 0; k < steps; ++k) {
+      const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
+      p.b[k] = std::ldexp(c[1], p_exp[k] - A_EXP); p.c[k] = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
+      p.t[k] = std::ldexp(c[0], p_exp[k]); p.f[k] = std::ldexp(1.f, -p_exp[k]);
+    }
+    return launch_small(p, batch, q.ctas, vec, g_type == PPU_F32, st);
+  }
   const int rc2 = g_type == PPU_BF16 ? prepare<bf16>(pp, q, batch, vec, st) : prepare<float>(pp, q, batch, vec, st);
   if (rc2 || steps == 0) return rc2;
   Maps maps;
