@@ -9,9 +9,12 @@
 // Numbers.  The products' operands are fp16 (11 bits; bf16 has 8) times powers of two that keep |X| <= 2.8 below the
 // largest and 2^-26 above the smallest normal number; sums are fp32.  X itself is carried in fp32 beside its fp16 copy, and
 // a X is formed from that: rounding X leaves noise in directions whose singular values are small, and the polynomial multiplies
-// those by a = 3.4 a step, noise included.  Root mean square error of O relative to O's (5 steps, CPU model): bf16
-// operands and X 1e-2 for random matrices, 0.16 to 0.35 for those with a few large directions; fp16 operands and X 1.3e-3
-// and 2e-2 to 4e-2; with X in fp32 1.4e-3 and 2e-4 to 5e-4.  P X needs no more: b A + c A A is small where X is.
+// those by a = 3.4 a step, noise included.  For sides below DIAG_SIDE P's diagonal is kept in fp32 and multiplies the same fp16 copy of X as the rest of
+// P (so that what P annuls it annuls as a whole): it comes to -2.7 where singular values come to one, and half a step of fp16 there is 2^-10 of X.
+// Root mean square error of O relative to O's (5 steps, CPU model; the rounding of O to bf16 is 1.66e-3): bf16 operands and X 1e-2 for random matrices, 0.16 to
+// 0.35 for those with a few large directions; fp16 operands and X 1.3e-3 and 2e-2 to 4e-2; with X in fp32 1.4e-3 (sides of 768), 1.7e-3 (256), 2.4e-3 (33)
+// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 7 % more time (8192 x 2048 117 -> 125 us a step, 24 x 256 x 2048 49 ->
+// 53, whose tiles of X are bound by what is done with them).  Sides up to 128 are mostly worked on chip, below.
 //
 // A and A A are symmetric: only tiles on and below the diagonal are worked and stored; a block above it is read as its
 // mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
@@ -32,7 +35,7 @@ using gemm_tc_detail::ld_v8;
 using gemm_tc_detail::st_v8;
 
 constexpr int X_EXP = 12, A_EXP = 12;                 // powers of two of X and A as stored
-constexpr int SMS = 148, MAX_STEPS = 32, MAX_SIDE = 1 << 16;
+constexpr int SMS = 148, MAX_STEPS = 32, MAX_SIDE = 1 << 16, DIAG_SIDE = 256;
 enum Mode { GRAM = 0, POLY = 1, UPDATE = 2 };
 
 constexpr int EPI = 8;                               // epilogue warps (16 of half the registers: 8192 x 2048 852 us for 741)
@@ -56,7 +59,8 @@ struct KernelP {
   int rows32, cols32, side32;        // blocks along X's sides, along the shorter one
   bf16* O; float scale;
   float gram;                        // A = gram * its accumulator
-  float a[MAX_STEPS], b[MAX_STEPS], c[MAX_STEPS], f[MAX_STEPS];
+  float a[MAX_STEPS], b[MAX_STEPS], c[MAX_STEPS], f[MAX_STEPS], d[MAX_STEPS];
+  float* diag;                       // [batch][side] P's diagonal, times d; null: it stays in P
   float* partial;                    // slices' sums
   unsigned *done, *arrived;          // [3][batch] warps that have finished; [2][batch][sym][CTAs][EPI] slices that have left their sums
   int* flags;
@@ -198,8 +202,15 @@ __device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int m0, i
     for (int j = 0; j < 4; ++j) ld_v8(x + 8 * j, src + 256 * j);
   }
 }
+// P's diagonal for this lane's row (left), or for column n + lane
+__device__ __forceinline__ float diagonal(const KernelP& p, const Unit& w, int m0, int n, int lane) {
+  const int i = (p.left ? m0 : n) + lane;
+  return i < p.side ? __ldcg(p.diag + (int64_t)w.b * p.side + i) : 0.f;
+}
 // buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored 16 columns at a time
-__device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, uint32_t* buf, int lane) {
+// pd: P's diagonal of this lane's row (left) or of column n + lane
+template <bool DIAG>
+__device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, float pd, uint32_t* buf, int lane) {
   const int m = m0 + lane;
   if (w.mode != UPDATE) {
     if (m0 >= p.side) return;
@@ -214,7 +225,12 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         const float2 v = half2_floats(x[j]);
-        o[j] = half2_bits(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
+        float2 y = make_float2(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
+        if (DIAG && n == m0 && lane / 2 == j) {     // the diagonal
+          if (m < p.side) p.diag[(int64_t)w.b * p.side + m] = p.d[step] * (lane & 1 ? y.y : y.x);
+          (lane & 1 ? y.y : y.x) = 0.f;
+        }
+        o[j] = half2_bits(y.x, y.y);
       }
     }
     if (m >= p.side) return;
@@ -224,10 +240,17 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
   }
   if (m0 >= p.m) return;
   const float a = p.a[step], f = p.f[step];
+  // a X + (P's diagonal) (X in fp16) + f (the rest of P X)
+  auto result = [&](int j) {
+    const float v = __uint_as_float(x[j]);
+    float ax = a * v;
+    if constexpr (DIAG) ax = fmaf(p.left ? pd : __shfl_sync(0xffffffffu, pd, j), __half2float(__float2half_rn(v)), ax);
+    return fmaf(f, __uint_as_float(r[j]), ax);
+  };
   if (step + 1 < p.steps) {
     uint32_t y[32], h[16];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(fmaf(f, __uint_as_float(r[j]), a * __uint_as_float(x[j])));
+    for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(result(j));
     float* again = p.X + block_at(w.b, p.rows32, p.cols32, m0, n) + 8 * lane;
 #pragma unroll
     for (int j = 0; j < 4; ++j) st_v8(again + 256 * j, y + 8 * j);
@@ -240,7 +263,7 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
   }
   float y[32];
 #pragma unroll
-  for (int j = 0; j < 32; ++j) y[j] = p.scale * fmaf(f, __uint_as_float(r[j]), a * __uint_as_float(x[j]));
+  for (int j = 0; j < 32; ++j) y[j] = p.scale * result(j);
   if (p.n % 8 == 0) {
     if (m >= p.m) return;
     bf16* o = p.O + ((int64_t)w.b * p.m + m) * p.n + n;
@@ -264,7 +287,7 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
 }
 
 // ---- all steps -----------------------------------------------------------------------------------------
-template <bool PAIR>
+template <bool PAIR, bool DIAG>
 __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const KernelP& p) {
   constexpr int CTAS = PAIR ? 2 : 1, TILE = 128 * CTAS;
   extern __shared__ uint8_t smem_raw[];
@@ -401,12 +424,14 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
       const int m0 = w.i + (int)rank * 128 + quarter * 32;
       const int c0 = half * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
       uint32_t x[32];
+      float pd = 0.f;
       if (w.mode != GRAM) {                        // what other CTAs have written is read from here on
         unsigned value;
         const unsigned* counter = awaited<PAIR>(p, w, step, value);
         const bool ok = lane > 0 || wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; });
         if (!__all_sync(0xffffffffu, ok)) return false;
         if (w.splits == 1 && c0 < c1) fetch(p, w, m0, w.j + c0, lane, x);
+        if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
       }
       if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       tc_fence_after();
@@ -446,7 +471,9 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         if (!mine(c)) continue;
         const int n = w.j + c;
         uint32_t r[32], next[32];
+        float next_pd = pd;
         tmem_ld32(t_row + c, r);
+        if (DIAG && w.mode == UPDATE && !p.left && c + 32 < c1) next_pd = diagonal(p, w, m0, n + 32, lane);
         if (w.splits > 1) fetch(p, w, m0, n, lane, x);
         else if (c + 32 < c1) fetch(p, w, m0, n + 32, lane, next);
         tmem_ld_wait();
@@ -466,8 +493,9 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
 #pragma unroll
           for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(all[j]);
         }
-        finish(p, w, step, m0, n, r, x, buf, lane);
+        finish<DIAG>(p, w, step, m0, n, r, x, pd, buf, lane);
         __syncwarp();
+        pd = next_pd;
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = next[j];
       }
@@ -501,10 +529,12 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
 }
 
 struct Maps { CUtensorMap m[4]; };                 // X (even steps), X (odd steps), A, P
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BLOCK, 1) ortho_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) {
-  ortho_steps<true>(maps.m, p);
+template <bool DIAG> __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BLOCK, 1) ortho_pair_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) {
+  ortho_steps<true, DIAG>(maps.m, p);
 }
-__global__ void __launch_bounds__(BLOCK, 1) ortho_single_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) { ortho_steps<false>(maps.m, p); }
+template <bool DIAG> __global__ void __launch_bounds__(BLOCK, 1) ortho_single_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelP p) {
+  ortho_steps<false, DIAG>(maps.m, p);
+}
 
 // ---- momentum, norm and the first X ----------------------------------------------------------------
 struct PrepP {
@@ -646,21 +676,22 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
 // ---- matrices whose shorter side is at most 128: all of it on chip, in one launch ---------------------------
 // A cluster works a matrix, each CTA up to 256 columns of it (of the transpose, where it has more rows): X in tensor memory, its fp16 copy
 // in shared memory, where both products read it.  The CTAs add up their parts of A through each other's shared memory,
-// each a share of its columns, in the order of their ranks; P is formed by each for itself.  The sum X = a X + P X is formed by the tensor
-// cores on X's own accumulator, which holds a X by then.  A step is a chain of short dependent works (a product, a pass over its result, a
+// each a share of its columns, in the order of their ranks; P is formed by each for itself, and multiplies X as a pair of fp16 (the product
+// costs little here, and small random matrices would lose more than others: 20 x 30 2.1e-3, with the pair 1.3e-3).  A step is a chain of short dependent works (a product, a pass over its result, a
 // barrier): 4 us for 100 x 100, 6 for 128 x 256, 12 where eight CTAs join their sums, against 18 and more through global memory (100 x 100 105 -> 33 us).
 // 512 threads: no change.
 constexpr int SMALL_SIDE = 128, SMALL_COLS = 256, SMALL_CTAS = 8;
 constexpr int SMALL_THREADS = 256, SMALL_WARPS = SMALL_THREADS / 32, PARTS = SMALL_WARPS / 4;      // warps of a quarter of the rows
 constexpr int SLAB = 128 * BK * 2;                   // 128 rows x 64 columns of fp16
-constexpr int SMALL_X = 4 * SLAB, SMALL_A = 2 * SLAB, SMALL_SUMS = 128 * 128 * 4;
-constexpr int SMALL_SMEM = SMALL_X + 2 * SMALL_A + SMALL_SUMS + 1024;
+constexpr int SMALL_X = 4 * SLAB, SMALL_A = 2 * SLAB;
+constexpr int SMALL_SMEM = 2 * SMALL_X + 2 * SMALL_A + 1024;
+static_assert(128 * 128 * 4 <= SMALL_X, "the sums of A lie where X's second numbers do later");
 
 struct SmallP {
   PrepP in;                          // G, momentum, norm
   int side, length, left, chunk, steps;      // chunk: columns of a CTA, a multiple of 32
   bf16* O; float scale, gram;
-  float b[MAX_STEPS], c[MAX_STEPS], t[MAX_STEPS], f[MAX_STEPS];      // t: what X is multiplied by to be added to, f: what brings the sum back
+  float a[MAX_STEPS], b[MAX_STEPS], c[MAX_STEPS], f[MAX_STEPS];      // X = (a + f P's diagonal) X + f (P X)
   int* flags;
 };
 
@@ -708,12 +739,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
   extern __shared__ uint8_t smem_raw[];
   // (the window starts at the same offset in all CTAs of a cluster)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t *sX = smem, *sA = smem + SMALL_X, *sP = sA + SMALL_A;
-  float4* sums = reinterpret_cast<float4*>(sP + SMALL_A);      // [32 fours of columns][128 rows]
+  uint8_t *sX = smem, *sL = smem + SMALL_X, *sA = sL + SMALL_X, *sP = sA + SMALL_A;      // X in fp16, what that leaves, A, P
+  float4* sums = reinterpret_cast<float4*>(sL);      // [32 fours of columns][128 rows], before sL is written
   __shared__ uint64_t s_bar;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   __shared__ double s_part[SMALL_WARPS], s_total;
+  __shared__ float s_diag[128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane;
   uint32_t rank, ctas;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -730,13 +762,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tX = s_tmem + ((uint32_t)(quarter * 32) << 16), tAcc = tX + SMALL_COLS;      // X, and the sums of A and of A A
+  const uint32_t tX = s_tmem + ((uint32_t)(quarter * 32) << 16), tAcc = tX + SMALL_COLS;      // X, and the products' sums
   pdl_wait(); pdl_trigger();
 
   const int col0 = (int)rank * p.chunk, own = max(0, min(p.chunk, p.length - col0)), chunks = p.chunk / 32;
   uint32_t parity = 0;
-  // fn(k) issues one thread's products; all wait for them
-  auto products = [&](auto fn) {
+  // fn() issues one thread's products; all do what they can meanwhile and wait for them
+  auto products = [&](auto fn, auto meanwhile) {
     asm volatile("fence.proxy.async;" ::: "memory");       // (the operands in shared memory were written by plain stores)
     tc_fence_before();
     __syncthreads();
@@ -746,6 +778,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
       fn();
       umma_commit(bar);
     }
+    __syncwarp();
+    meanwhile();
     wait_for(abort_flag, p.flags, [&] { return mbar_try(bar, parity); });      // (where it gives up the results are not valid, and flags say so)
     parity ^= 1;
     tc_fence_after();
@@ -791,22 +825,23 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
   const double inv = (norm > 0.0 ? 1.0 / norm : norm == 0.0 ? 0.0 : norm) * (double)(1 << X_EXP);      // (a matrix of zeros stays one; NaN stays NaN)
 
   for (int step = 0; step <= p.steps; ++step) {
-    // X (after the last step O): its fp16 copy, and what the next product is added to
+    // X (after the last step O), and its fp16 copy
     for (int c = part; c < chunks; c += PARTS) {
-      uint32_t r[32];
+      uint32_t r[32], y[32];
       tmem_ld32(tX + 32 * c, r);
+      if (step > 0) tmem_ld32(tAcc + 32 * c, y);
       tmem_ld_wait();
       float x[32];
+      const float f = step > 0 ? p.f[step - 1] : 0.f, a = step > 0 ? fmaf(f, s_diag[row], p.a[step - 1]) : 0.f;
 #pragma unroll
-      for (int q = 0; q < 32; ++q) x[q] = step == 0 ? (float)(__uint_as_float(r[q]) * inv) : __uint_as_float(r[q]) * p.f[step > 0 ? step - 1 : 0];
+      for (int q = 0; q < 32; ++q) x[q] = step == 0 ? (float)(__uint_as_float(r[q]) * inv) : fmaf(f, __uint_as_float(y[q]), a * __uint_as_float(r[q]));
       if (step < p.steps) {
-        const float t = p.t[step];
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *reinterpret_cast<uint4*>(sX + slab_at(row, 32 * c + 8 * q)) =
               make_uint4(half2_bits(x[8 * q], x[8 * q + 1]), half2_bits(x[8 * q + 2], x[8 * q + 3]), half2_bits(x[8 * q + 4], x[8 * q + 5]), half2_bits(x[8 * q + 6], x[8 * q + 7]));
 #pragma unroll
-        for (int q = 0; q < 32; ++q) r[q] = __float_as_uint(t * x[q]);
+        for (int q = 0; q < 32; ++q) r[q] = __float_as_uint(x[q]);
         tmem_st32(tX + 32 * c, r);
       } else {
         const int j = col0 + 32 * c, have = row < p.side ? min(32, col0 + own - j) : 0;
@@ -841,13 +876,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     tmem_st_wait();
     // A = X X^T of this CTA's columns
     const uint32_t idesc = (1u << 4) | ((uint32_t)(128 >> 4) << 24);
-    const uint32_t aX = smem_u32(sX), aA = smem_u32(sA), aP = smem_u32(sP), tBase = s_tmem;
+    const uint32_t aX = smem_u32(sX), aL = smem_u32(sL), aA = smem_u32(sA), aP = smem_u32(sP), tBase = s_tmem;
     products([&] {
       for (int k = 0; k < p.chunk / UMMA_K; ++k) {
         const uint64_t d = make_desc(aX + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024);
         umma_bf16(tBase + SMALL_COLS, d, d, idesc | (uint32_t)(128 >> 3) << 17, k > 0);
       }
-    });
+    }, [] {});
     // A in fp16, of all CTAs' sums
 #pragma unroll 1
     for (int c = 128 / PARTS * part; c < 128 / PARTS * (part + 1); c += 32) {
@@ -893,6 +928,23 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
         const uint64_t d = make_desc(aA + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024);
         umma_bf16(tBase + SMALL_COLS, d, d, idesc | (uint32_t)(128 >> 3) << 17, k > 0);
       }
+    }, [&] {
+      for (int c = part; c < chunks; c += PARTS) {      // what X's fp16 copy leaves of it
+        uint32_t r[32];
+        tmem_ld32(tX + 32 * c, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x0 = __uint_as_float(r[8 * q + 2 * e]), x1 = __uint_as_float(r[8 * q + 2 * e + 1]);
+            const float2 h = half2_floats(half2_bits(x0, x1));
+            o[e] = half2_bits(x0 - h.x, x1 - h.y);
+          }
+          *reinterpret_cast<uint4*>(sL + slab_at(row, 32 * c + 8 * q)) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+      }
     });
 #pragma unroll 1
     for (int c = 128 / PARTS * part; c < 128 / PARTS * (part + 1); c += 32) {
@@ -909,17 +961,24 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 x = half2_floats(h[e]);
-          o[e] = half2_bits(fmaf(fc, __uint_as_float(r[8 * q + 2 * e]), fb * x.x), fmaf(fc, __uint_as_float(r[8 * q + 2 * e + 1]), fb * x.y));
+          float2 y = make_float2(fmaf(fc, __uint_as_float(r[8 * q + 2 * e]), fb * x.x), fmaf(fc, __uint_as_float(r[8 * q + 2 * e + 1]), fb * x.y));
+          if (c == 32 * quarter && lane / 2 == 4 * q + e) {      // the diagonal
+            s_diag[row] = lane & 1 ? y.y : y.x;
+            (lane & 1 ? y.y : y.x) = 0.f;
+          }
+          o[e] = half2_bits(y.x, y.y);
         }
         *reinterpret_cast<uint4*>(sP + slab_at(row, c + 8 * q)) = v;
       }
     }
-    // X = a X + P X
+    // P X
     products([&] {
-      for (int k = 0; k < 128 / UMMA_K; ++k)
-        umma_bf16(tBase, make_desc(aP + (k >> 2) * SLAB + (k & 3) * 32, 16, 1024), make_desc(aX + k * 2048, SLAB, 1024),
-                  idesc | (1u << 16) | (uint32_t)(p.chunk >> 3) << 17, 1u);
-    });
+      for (int k = 0; k < 2 * 128 / UMMA_K; ++k) {
+        const int j = k & 7;                         // (X, then what it leaves)
+        umma_bf16(tBase + SMALL_COLS, make_desc(aP + (j >> 2) * SLAB + (j & 3) * 32, 16, 1024), make_desc((k < 8 ? aX : aL) + j * 2048, SLAB, 1024),
+                  idesc | (1u << 16) | (uint32_t)(p.chunk >> 3) << 17, k > 0);
+      }
+    }, [] {});
   }
   tc_fence_before();
   __syncthreads();
@@ -936,7 +995,7 @@ struct Plan {
   bool pair;
   int ctas, chunk;                   // on chip: CTAs of a matrix (0: not so), columns of each
   int tiles_s, sym, tiles_m, tiles_n, splits[2], workers;
-  size_t partial, hi[2], x, a, a2, p, sums, counters, bytes;
+  size_t partial, hi[2], x, a, a2, p, diag, sums, counters, bytes;
   int rows32, cols32, side32;
   int n_counters;
 };
@@ -979,6 +1038,7 @@ Plan make_plan(int batch, int m, int n, int steps) {
     const size_t x = (size_t)batch * m * q.ld * 2, s = (size_t)batch * q.side * q.lds * 2;
     q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.x = take((size_t)batch * q.rows32 * q.cols32 * 4096);
     q.a = take(s); q.a2 = take((size_t)batch * q.side32 * q.side32 * 2048); q.p = take(s);
+    q.diag = take(q.side < DIAG_SIDE ? (size_t)batch * q.side * 4 : 0);
     const int most = std::max(q.splits[0], q.splits[1]), ctas = q.pair ? 2 : 1;
     q.sums = take(most > 1 ? (size_t)batch * q.sym * most * t * t * 4 : 0);
     q.n_counters = 3 * batch + (most > 1 ? 2 * batch * q.sym * ctas * EPI : 0);
@@ -1046,19 +1106,21 @@ int resident(bool pair) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&got, ortho_pair_kernel, &cfg) != cudaSuccess) return -1;
+    if (cudaOccupancyMaxActiveClusters(&got, ortho_pair_kernel<true>, &cfg) != cudaSuccess) return -1;
     n = std::min(got, ppu_sm_count() / 2);
   } else {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&got, ortho_single_kernel, BLOCK, SMEM) != cudaSuccess) return -1;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&got, ortho_single_kernel<true>, BLOCK, SMEM) != cudaSuccess) return -1;
     n = got > 0 ? ppu_sm_count() : 0;
   }
   return n;
 }
 
 int launch_steps(const Maps& maps, const KernelP& p, bool pair, cudaStream_t st) {
-  static PerDeviceFlag attr_set[2];
-  void (*kernel)(Maps, KernelP) = pair ? ortho_pair_kernel : ortho_single_kernel;
-  if (!ppu_set_smem_once(attr_set[pair], kernel, SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  static PerDeviceFlag attr_set[4];
+  void (*kernels[4])(Maps, KernelP) = {ortho_single_kernel<false>, ortho_single_kernel<true>, ortho_pair_kernel<false>, ortho_pair_kernel<true>};
+  for (int i = 0; i < 4; ++i)
+    if (!ppu_set_smem_once(attr_set[i], kernels[i], SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
+  auto kernel = kernels[2 * pair + (p.diag != nullptr)];
   const int most = resident(pair);
   if (most < 1) return ppu_fail(PPU_ECUDA, "the kernel does not fit on this device");
   const int units = p.batch * std::max(p.units[GRAM], std::max(p.units[POLY], p.units[UPDATE]));
@@ -1165,7 +1227,7 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
     for (int k = 0; k < steps; ++k) {
       const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
       p.b[k] = std::ldexp(c[1], p_exp[k] - A_EXP); p.c[k] = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
-      p.t[k] = std::ldexp(c[0], p_exp[k]); p.f[k] = std::ldexp(1.f, -p_exp[k]);
+      p.a[k] = c[0]; p.f[k] = std::ldexp(1.f, -p_exp[k]);
     }
     return launch_small(p, batch, q.ctas, vec, g_type == PPU_F32, st);
   }
@@ -1187,13 +1249,13 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
     p.units[UPDATE] = tiles + rem;
   }
   p.per_step = batch * (p.units[GRAM] + p.units[POLY] + p.units[UPDATE]);
-  p.A = A; p.P = P; p.hi[0] = hi[0]; p.hi[1] = hi[1]; p.X = pp.X; p.A2 = (__half*)(ws + q.a2); p.rows32 = q.rows32; p.cols32 = q.cols32; p.side32 = q.side32; p.ld = q.ld; p.lds = q.lds; p.O = (bf16*)O; p.scale = scale;
+  p.A = A; p.P = P; p.hi[0] = hi[0]; p.hi[1] = hi[1]; p.X = pp.X; p.A2 = (__half*)(ws + q.a2); p.diag = q.side < DIAG_SIDE ? (float*)(ws + q.diag) : nullptr; p.rows32 = q.rows32; p.cols32 = q.cols32; p.side32 = q.side32; p.ld = q.ld; p.lds = q.lds; p.O = (bf16*)O; p.scale = scale;
   p.gram = std::ldexp(1.f, A_EXP - 2 * X_EXP);
   for (int k = 0; k < steps; ++k) {
     const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
     const int out = k + 1 < steps ? 0 : -X_EXP;    // O has no power of two
     p.b[k] = std::ldexp(c[1], p_exp[k] - A_EXP); p.c[k] = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
-    p.a[k] = std::ldexp(c[0], out); p.f[k] = std::ldexp(1.f, out - p_exp[k]);
+    p.a[k] = std::ldexp(c[0], out); p.f[k] = p.d[k] = std::ldexp(1.f, out - p_exp[k]);
   }
   p.partial = (float*)(ws + q.sums); p.done = pp.counters; p.arrived = p.done + 3 * batch; p.flags = flags;
   return launch_steps(maps, p, q.pair, st);

@@ -1,15 +1,16 @@
 """The orthogonalised update (ppu_orthogonalize) against its definition in 64 bits.
 
 Two references.  `definition` is the formula.  `model` is the same with the kernels' documented roundings and no others: the products' operands in
-fp16 (times 2^12), X carried as a pair of fp16.  How far the model is from the definition is what the arithmetic itself costs; the kernels may be as far, in
+fp16 (times 2^12) but for P's diagonal, which is kept for shorter sides below 256, and X, which is carried beside the fp16 copy that P multiplies; where the shorter side is at
+most 128 and the longer at most 2048 P multiplies a pair of fp16.  How far the model is from the definition is what the arithmetic itself costs; the kernels may be as far, in
 root mean square, plus the result's rounding (uniform within half a step of 2^-8: 2^-8 / sqrt(3) of the value at most) and a quarter for the fp32 sums.
 
 Element by element: a sum whose last bits differ puts one in a hundred of the values that are then rounded to fp16 on the other side, and from there on
 all roundings are others (the model with its sums changed by 1e-7 is as far from itself as from the definition, and its largest error then is 4.6 to 7.4
 times the root mean square).  So the kernels' errors are not the model's but are distributed like them: sums of many roundings, of which those on
 the diagonal of P act on a whole row and make its root mean square up to twice the others'; six deviations cover 10^6 values: 12 times the cost, beside
-half a step of bf16.  One rounding of P's diagonal (b + c = -2.7 where singular values have come to one, half a step 2^-10, against an X' of 0.65 of X) may be
-all there is in a matrix of a few values, where the model may have none by luck: 2^-10 / 0.65 for each of three steps, below 2^-7 of the value."""
+half a step of bf16.  In a matrix of a few values the model may have no error by luck where the kernels round X to fp16 the other way, times a diagonal
+of P up to 2.8 against an X' of 0.65 of X: 2^-12 * 2.8 / 0.65 for each of five steps, below 2^-7 of the value."""
 import ctypes as C
 import math
 
@@ -50,17 +51,23 @@ def h(x, exp=12):
         return np.ldexp(np.ldexp(x, exp).astype(np.float16).astype(np.float64), -exp)
 
 
+def off_diagonal(P):
+    """P without its diagonal, and the diagonal."""
+    k = np.arange(P.shape[1])
+    d = P[:, k, k].copy()
+    P = P.copy()
+    P[:, k, k] = 0.0
+    return h(P), d
+
+
 def model(u, steps=5, coef=COEF, eps=1e-7, scale=1.0):
     X = start(u, eps).astype(np.float32).astype(np.float64)
     for a, b, c in triples(coef, steps):
-        hi = h(X)
-        X = hi + h(X - hi, 23)
-        if u.shape[1] <= u.shape[2]:
-            G = h(hi @ hi.transpose(0, 2, 1))
-            X = a * X + h(b * G + c * G @ G) @ hi
-        else:
-            G = h(hi.transpose(0, 2, 1) @ hi)
-            X = a * X + hi @ h(b * G + c * G @ G)
+        hi, left = h(X), u.shape[1] <= u.shape[2]
+        G = h(hi @ hi.transpose(0, 2, 1)) if left else h(hi.transpose(0, 2, 1) @ hi)
+        P, d = off_diagonal(b * G + c * G @ G) if min(u.shape[1:]) < 256 else (h(b * G + c * G @ G), np.zeros(G.shape[:2]))
+        Z = hi + h(X - hi) if min(u.shape[1:]) <= 128 and max(u.shape[1:]) <= 2048 else hi
+        X = a * X + d[:, :, None] * Z + P @ Z if left else a * X + d[:, None, :] * Z + Z @ P
     return f32(scale) * X
 
 
