@@ -55,7 +55,7 @@ struct KernelP {
   int tail_from;                     // tiles of X from here on are worked in two halves of their columns
   int per_step;
   __half *A, *P, *hi[2]; int64_t ld, lds;      // operands, by rows
-  float* X; __half* A2;              // X and A as their epilogues read and write them again: 32 x 32 blocks (block_at)
+  __half *lo, *A2;                   // what X's fp16 copy leaves of it, and A once more, as their epilogues read and write them: 32 x 32 blocks (block_at)
   int rows32, cols32, side32;        // blocks along X's sides, along the shorter one
   bf16* O; float scale;
   float gram;                        // A = gram * its accumulator
@@ -190,16 +190,19 @@ __device__ __forceinline__ const unsigned* awaited(const KernelP& p, const Unit&
 // read so takes 1 us, by rows 9.
 __device__ __forceinline__ int64_t block_at(int b, int rows32, int cols32, int m, int n) { return (((int64_t)b * rows32 + m / 32) * cols32 + n / 32) * 1024; }
 // what a unit's result is made of beside the accumulator: A for P, X for X
-__device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int m0, int n, int lane, uint32_t* x) {
+__device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int step, int m0, int n, int lane, uint32_t* x) {
   if (w.mode == POLY) {
     if (m0 >= p.side) return;
     const __half* src = p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane;
     ld_v8(x, src); ld_v8(x + 8, src + 512);
   } else if (w.mode == UPDATE) {
     if (m0 >= p.m) return;
-    const float* src = p.X + block_at(w.b, p.rows32, p.cols32, m0, n) + 8 * lane;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) ld_v8(x + 8 * j, src + 256 * j);
+    if (m0 + lane < p.m) {
+      const __half* hi = p.hi[step & 1] + ((int64_t)w.b * p.m + m0 + lane) * p.ld + n;
+      ld_v8(x, hi); ld_v8(x + 8, hi + 16);
+    }
+    const __half* lo = p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane;
+    ld_v8(x + 16, lo); ld_v8(x + 24, lo + 512);
   }
 }
 // P's diagonal for this lane's row (left), or for column n + lane
@@ -241,29 +244,34 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
   if (m0 >= p.m) return;
   const float a = p.a[step], f = p.f[step];
   // a X + (P's diagonal) (X in fp16) + f (the rest of P X)
-  auto result = [&](int j) {
-    const float v = __uint_as_float(x[j]);
-    float ax = a * v;
-    if constexpr (DIAG) ax = fmaf(p.left ? pd : __shfl_sync(0xffffffffu, pd, j), __half2float(__float2half_rn(v)), ax);
-    return fmaf(f, __uint_as_float(r[j]), ax);
-  };
+  float y[32];
+#pragma unroll
+  for (int j = 0; j < 32; j += 2) {
+    const float2 h = half2_floats(x[j / 2]), l = half2_floats(x[16 + j / 2]);
+    float2 ax = make_float2(a * (h.x + l.x), a * (h.y + l.y));
+    if constexpr (DIAG) {
+      const float d0 = p.left ? pd : __shfl_sync(0xffffffffu, pd, j), d1 = p.left ? pd : __shfl_sync(0xffffffffu, pd, j + 1);
+      ax.x = fmaf(d0, h.x, ax.x); ax.y = fmaf(d1, h.y, ax.y);
+    }
+    y[j] = fmaf(f, __uint_as_float(r[j]), ax.x); y[j + 1] = fmaf(f, __uint_as_float(r[j + 1]), ax.y);
+  }
   if (step + 1 < p.steps) {
-    uint32_t y[32], h[16];
+    uint32_t h[16], l[16];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) y[j] = __float_as_uint(result(j));
-    float* again = p.X + block_at(w.b, p.rows32, p.cols32, m0, n) + 8 * lane;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) st_v8(again + 256 * j, y + 8 * j);
+    for (int j = 0; j < 16; ++j) {
+      h[j] = half2_bits(y[2 * j], y[2 * j + 1]);
+      const float2 v = half2_floats(h[j]);
+      l[j] = half2_bits(y[2 * j] - v.x, y[2 * j + 1] - v.y);
+    }
+    __half* lo = p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane;
+    st_v8(lo, l); st_v8(lo + 512, l + 8);
     if (m >= p.m) return;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) h[j] = half2_bits(__uint_as_float(y[2 * j]), __uint_as_float(y[2 * j + 1]));
     __half* hi = p.hi[(step + 1) & 1] + ((int64_t)w.b * p.m + m) * p.ld + n;
     st_v8(hi, h); st_v8(hi + 16, h + 8);
     return;
   }
-  float y[32];
 #pragma unroll
-  for (int j = 0; j < 32; ++j) y[j] = p.scale * result(j);
+  for (int j = 0; j < 32; ++j) y[j] *= p.scale;
   if (p.n % 8 == 0) {
     if (m >= p.m) return;
     bf16* o = p.O + ((int64_t)w.b * p.m + m) * p.n + n;
@@ -430,7 +438,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         const unsigned* counter = awaited<PAIR>(p, w, step, value);
         const bool ok = lane > 0 || wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; });
         if (!__all_sync(0xffffffffu, ok)) return false;
-        if (w.splits == 1 && c0 < c1) fetch(p, w, m0, w.j + c0, lane, x);
+        if (w.splits == 1 && c0 < c1) fetch(p, w, step, m0, w.j + c0, lane, x);
         if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
       }
       if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
@@ -474,8 +482,8 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         float next_pd = pd;
         tmem_ld32(t_row + c, r);
         if (DIAG && w.mode == UPDATE && !p.left && c + 32 < c1) next_pd = diagonal(p, w, m0, n + 32, lane);
-        if (w.splits > 1) fetch(p, w, m0, n, lane, x);
-        else if (c + 32 < c1) fetch(p, w, m0, n + 32, lane, next);
+        if (w.splits > 1) fetch(p, w, step, m0, n, lane, x);
+        else if (c + 32 < c1) fetch(p, w, step, m0, n + 32, lane, next);
         tmem_ld_wait();
         if (w.splits > 1) {
           float all[32];
@@ -544,7 +552,7 @@ struct PrepP {
   int rows, cols, nesterov, f32;
   float beta, w, eps, scale;
   double* partial;                                 // [batch][blocks]
-  __half* hi; int64_t ld; float* X; int rows32, cols32;
+  __half *hi, *lo; int64_t ld; int rows32, cols32;
   bf16* O;                                         // no steps: scale X
   unsigned* counters; int n_counters;              // set to 0
 };
@@ -614,7 +622,7 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
   }
 }
 
-// X in fp32 by blocks and in fp16 by rows, filled up with zeros.  A warp takes one 32 x 32 block, 4 rows of 8 fours at a time, and has it in
+// X in fp16 by rows, and what that leaves of it by blocks, filled up with zeros.  A warp takes one 32 x 32 block, 4 rows of 8 fours at a time, and has it in
 // flight while the norm is put together.
 template <typename TG, int VEC>
 __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blocks) {
@@ -653,7 +661,7 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
   __syncthreads();
   if (e < 0) return;
   const double inv = s_inv;
-  float* block = p.X + ((int64_t)b * n + e) * 1024 + (c0 / 8) * 256 + c0 % 8;
+  __half* block = p.lo + ((int64_t)b * n + e) * 1024 + (c0 / 16) * 512 + c0 % 16;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = rb * 32 + 4 * i + r0;
@@ -668,8 +676,10 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
       }
       continue;
     }
-    *reinterpret_cast<float4*>(block + 8 * (4 * i + r0)) = x;
-    if (row < p.rows) *reinterpret_cast<uint2*>(p.hi + ((int64_t)b * p.rows + row) * p.ld + c) = make_uint2(half2_bits(x.x, x.y), half2_bits(x.z, x.w));
+    const uint2 h = make_uint2(half2_bits(x.x, x.y), half2_bits(x.z, x.w));
+    const float2 v0 = half2_floats(h.x), v1 = half2_floats(h.y);
+    *reinterpret_cast<uint2*>(block + 16 * (4 * i + r0)) = make_uint2(half2_bits(x.x - v0.x, x.y - v0.y), half2_bits(x.z - v1.x, x.w - v1.y));
+    if (row < p.rows) *reinterpret_cast<uint2*>(p.hi + ((int64_t)b * p.rows + row) * p.ld + c) = h;
   }
 }
 
@@ -995,7 +1005,7 @@ struct Plan {
   bool pair;
   int ctas, chunk;                   // on chip: CTAs of a matrix (0: not so), columns of each
   int tiles_s, sym, tiles_m, tiles_n, splits[2], workers;
-  size_t partial, hi[2], x, a, a2, p, diag, sums, counters, bytes;
+  size_t partial, hi[2], lo, a, a2, p, diag, sums, counters, bytes;
   int rows32, cols32, side32;
   int n_counters;
 };
@@ -1036,7 +1046,7 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.partial = take((size_t)batch * q.blocks * 8);
   if (steps > 0) {
     const size_t x = (size_t)batch * m * q.ld * 2, s = (size_t)batch * q.side * q.lds * 2;
-    q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.x = take((size_t)batch * q.rows32 * q.cols32 * 4096);
+    q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.lo = take((size_t)batch * q.rows32 * q.cols32 * 2048);
     q.a = take(s); q.a2 = take((size_t)batch * q.side32 * q.side32 * 2048); q.p = take(s);
     q.diag = take(q.side < DIAG_SIDE ? (size_t)batch * q.side * 4 : 0);
     const int most = std::max(q.splits[0], q.splits[1]), ctas = q.pair ? 2 : 1;
@@ -1216,7 +1226,7 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   pp.G = G; pp.ldg = ldg; pp.stride_g = stride_g; pp.m = momentum; pp.ldm = ldm; pp.stride_m = stride_m;
   pp.m_out = momentum_out; pp.ldm_out = ldmo; pp.stride_m_out = stride_mo; pp.rows = m; pp.cols = n; pp.nesterov = nesterov != 0;
   pp.beta = beta; pp.w = weight; pp.eps = eps; pp.scale = scale; pp.partial = (double*)(ws + q.partial); pp.hi = hi[0]; pp.ld = q.ld;
-  pp.X = (float*)(ws + q.x); pp.rows32 = q.rows32; pp.cols32 = q.cols32;
+  pp.lo = (__half*)(ws + q.lo); pp.rows32 = q.rows32; pp.cols32 = q.cols32;
   pp.O = steps == 0 ? (bf16*)O : nullptr;
   pp.counters = (unsigned*)(ws + q.counters); pp.n_counters = q.n_counters;
   const bool vec = n % 4 == 0 && aligned(G, ldg, stride_g, 4 * g_bytes) && aligned(momentum, ldm, stride_m, 16) && aligned(momentum_out, ldmo, stride_mo, 16);
@@ -1249,7 +1259,7 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
     p.units[UPDATE] = tiles + rem;
   }
   p.per_step = batch * (p.units[GRAM] + p.units[POLY] + p.units[UPDATE]);
-  p.A = A; p.P = P; p.hi[0] = hi[0]; p.hi[1] = hi[1]; p.X = pp.X; p.A2 = (__half*)(ws + q.a2); p.diag = q.side < DIAG_SIDE ? (float*)(ws + q.diag) : nullptr; p.rows32 = q.rows32; p.cols32 = q.cols32; p.side32 = q.side32; p.ld = q.ld; p.lds = q.lds; p.O = (bf16*)O; p.scale = scale;
+  p.A = A; p.P = P; p.hi[0] = hi[0]; p.hi[1] = hi[1]; p.lo = pp.lo; p.A2 = (__half*)(ws + q.a2); p.diag = q.side < DIAG_SIDE ? (float*)(ws + q.diag) : nullptr; p.rows32 = q.rows32; p.cols32 = q.cols32; p.side32 = q.side32; p.ld = q.ld; p.lds = q.lds; p.O = (bf16*)O; p.scale = scale;
   p.gram = std::ldexp(1.f, A_EXP - 2 * X_EXP);
   for (int k = 0; k < steps; ++k) {
     const float* c = coef + (n_coef == 1 ? 0 : 3 * k);
