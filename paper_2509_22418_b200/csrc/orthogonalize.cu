@@ -38,7 +38,7 @@ constexpr int X_EXP = 12, A_EXP = 12;                 // powers of two of X and 
 constexpr int SMS = 148, MAX_STEPS = 32, MAX_SIDE = 1 << 16, DIAG_SIDE = 256;
 enum Mode { GRAM = 0, POLY = 1, UPDATE = 2 };
 
-constexpr int EPI = 8;                               // epilogue warps (16 of half the registers: 8192 x 2048 852 us for 741)
+constexpr int EPI = 8, W = 16;                      // epilogue warps, columns they take at a time
 constexpr int KH = 2, BOX = 128 * BK * 2;             // 64-k slabs of a stage; bytes of a box of 64 x 128
 constexpr int STAGES = 3, STAGE_BYTES = 2 * KH * BOX; // a CTA's share of a stage: 128 rows of A, 128 of B, 128 k
 constexpr int BUF_WORDS = 32 * 9;                     // an epilogue warp's
@@ -184,70 +184,61 @@ __device__ __forceinline__ const unsigned* awaited(const KernelP& p, const Unit&
   return p.done + (w.mode == GRAM ? UPDATE : w.mode - 1) * p.batch + w.b;
 }
 
-// ---- 32 columns from n on of row m (one to a lane) ---------------------------------------------------
-// The 32 x 32 values of a warp in 1024 consecutive places: eight columns of row 0, of row 1, ... of row 31, the next eight columns.  A lane
-// takes 32 bytes at a time and the warp 1 KB (fp16: 16 and 512), where by rows it would touch 32 lines with each instruction: X of a tile
-// read so takes 1 us, by rows 9.
-__device__ __forceinline__ int64_t block_at(int b, int rows32, int cols32, int m, int n) { return (((int64_t)b * rows32 + m / 32) * cols32 + n / 32) * 1024; }
+// ---- 16 columns from n on of row m (one to a lane) ---------------------------------------------------
+// What the epilogues alone read and write again lies in blocks: 32 x 32 values in 1024 consecutive places, sixteen columns of row 0, of row 1, ... of row
+// 31, then the other sixteen.  A lane takes 32 bytes and the warp 1 KB.
+__device__ __forceinline__ int64_t block_at(int b, int rows32, int cols32, int m, int n) {
+  return (((int64_t)b * rows32 + m / 32) * cols32 + n / 32) * 1024 + (n & 16) * 32;
+}
 // what a unit's result is made of beside the accumulator: A for P, X for X
 __device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int step, int m0, int n, int lane, uint32_t* x) {
   if (w.mode == POLY) {
-    if (m0 >= p.side) return;
-    const __half* src = p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane;
-    ld_v8(x, src); ld_v8(x + 8, src + 512);
-  } else if (w.mode == UPDATE) {
-    if (m0 >= p.m) return;
-    if (m0 + lane < p.m) {
-      const __half* hi = p.hi[step & 1] + ((int64_t)w.b * p.m + m0 + lane) * p.ld + n;
-      ld_v8(x, hi); ld_v8(x + 8, hi + 16);
-    }
-    const __half* lo = p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane;
-    ld_v8(x + 16, lo); ld_v8(x + 24, lo + 512);
+    if (m0 < p.side) ld_v8(x, p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane);
+  } else if (w.mode == UPDATE && m0 < p.m) {
+    if (m0 + lane < p.m) ld_v8(x, p.hi[step & 1] + ((int64_t)w.b * p.m + m0 + lane) * p.ld + n);
+    ld_v8(x + 8, p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane);
   }
 }
-// P's diagonal for this lane's row (left), or for column n + lane
+// P's diagonal for this lane's row (left), or for column n + lane % 16
 __device__ __forceinline__ float diagonal(const KernelP& p, const Unit& w, int m0, int n, int lane) {
-  const int i = (p.left ? m0 : n) + lane;
+  const int i = p.left ? m0 + lane : n + (lane & 15);
   return i < p.side ? __ldcg(p.diag + (int64_t)w.b * p.side + i) : 0.f;
 }
-// buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored 16 columns at a time
-// pd: P's diagonal of this lane's row (left) or of column n + lane
+// buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored
+// pd: P's diagonal of this lane's row (left) or of column n + lane % 16
 template <bool DIAG>
 __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, float pd, uint32_t* buf, int lane) {
   const int m = m0 + lane;
   if (w.mode != UPDATE) {
     if (m0 >= p.side) return;
-    uint32_t o[16];
+    uint32_t o[8];
     if (w.mode == GRAM) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] = half2_bits(p.gram * __uint_as_float(r[2 * j]), p.gram * __uint_as_float(r[2 * j + 1]));
-      __half* again = p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane;
-      st_v8(again, o); st_v8(again + 512, o + 8);
+      for (int j = 0; j < 8; ++j) o[j] = half2_bits(p.gram * __uint_as_float(r[2 * j]), p.gram * __uint_as_float(r[2 * j + 1]));
+      st_v8(p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane, o);
     } else {
       const float b = p.b[step], c = p.c[step];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
+      for (int j = 0; j < 8; ++j) {
         const float2 v = half2_floats(x[j]);
         float2 y = make_float2(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
-        if (DIAG && n == m0 && lane / 2 == j) {     // the diagonal
+        if (DIAG && n - m0 == (lane & 16) && (lane & 15) / 2 == j) {      // the diagonal
           if (m < p.side) p.diag[(int64_t)w.b * p.side + m] = p.d[step] * (lane & 1 ? y.y : y.x);
           (lane & 1 ? y.y : y.x) = 0.f;
         }
         o[j] = half2_bits(y.x, y.y);
       }
     }
-    if (m >= p.side) return;
-    __half* C = (w.mode == GRAM ? p.A : p.P) + ((int64_t)w.b * p.side + m) * p.lds + n;
-    st_v8(C, o); st_v8(C + 16, o + 8);
+    if (m < p.side) st_v8((w.mode == GRAM ? p.A : p.P) + ((int64_t)w.b * p.side + m) * p.lds + n, o);
     return;
   }
   if (m0 >= p.m) return;
   const float a = p.a[step], f = p.f[step];
   // a X + (P's diagonal) (X in fp16) + f (the rest of P X)
-  float y[32];
+  float y[W];
 #pragma unroll
-  for (int j = 0; j < 32; j += 2) {
-    const float2 h = half2_floats(x[j / 2]), l = half2_floats(x[16 + j / 2]);
+  for (int j = 0; j < W; j += 2) {
+    const float2 h = half2_floats(x[j / 2]), l = half2_floats(x[8 + j / 2]);
     float2 ax = make_float2(a * (h.x + l.x), a * (h.y + l.y));
     if constexpr (DIAG) {
       const float d0 = p.left ? pd : __shfl_sync(0xffffffffu, pd, j), d1 = p.left ? pd : __shfl_sync(0xffffffffu, pd, j + 1);
@@ -255,43 +246,44 @@ __device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step
     }
     y[j] = fmaf(f, __uint_as_float(r[j]), ax.x); y[j + 1] = fmaf(f, __uint_as_float(r[j + 1]), ax.y);
   }
+  uint32_t o[8];
   if (step + 1 < p.steps) {
-    uint32_t h[16], l[16];
+    uint32_t l[8];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      h[j] = half2_bits(y[2 * j], y[2 * j + 1]);
-      const float2 v = half2_floats(h[j]);
+    for (int j = 0; j < 8; ++j) {
+      o[j] = half2_bits(y[2 * j], y[2 * j + 1]);
+      const float2 v = half2_floats(o[j]);
       l[j] = half2_bits(y[2 * j] - v.x, y[2 * j + 1] - v.y);
     }
-    __half* lo = p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane;
-    st_v8(lo, l); st_v8(lo + 512, l + 8);
-    if (m >= p.m) return;
-    __half* hi = p.hi[(step + 1) & 1] + ((int64_t)w.b * p.m + m) * p.ld + n;
-    st_v8(hi, h); st_v8(hi + 16, h + 8);
+    st_v8(p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane, l);
+    if (m < p.m) st_v8(p.hi[(step + 1) & 1] + ((int64_t)w.b * p.m + m) * p.ld + n, o);
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 32; ++j) y[j] *= p.scale;
+  for (int j = 0; j < 8; ++j) o[j] = gemm_tc_detail::pack2_bf16(p.scale * y[2 * j], p.scale * y[2 * j + 1]);
   if (p.n % 8 == 0) {
     if (m >= p.m) return;
-    bf16* o = p.O + ((int64_t)w.b * p.m + m) * p.n + n;
+    bf16* to = p.O + ((int64_t)w.b * p.m + m) * p.n + n;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n + 8 * j < p.n) *reinterpret_cast<uint4*>(o + 8 * j) = gemm_tc_detail::pack8_bf16(y + 8 * j);
+    for (int j = 0; j < 2; ++j)
+      if (n + 8 * j < p.n) *reinterpret_cast<uint4*>(to + 8 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
   } else {
-    const int col = lane & 15;
+    const int col = lane & 15, c = n + col;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) buf[lane * 9 + j] = gemm_tc_detail::pack2_bf16(y[16 * h + 2 * j], y[16 * h + 2 * j + 1]);
-      __syncwarp();
-      const int c = n + 16 * h + col;
-      if (c < p.n)
-        for (int i = lane >> 4; i < 32 && m0 + i < p.m; i += 2)
-          reinterpret_cast<unsigned short*>(p.O)[((int64_t)w.b * p.m + m0 + i) * p.n + c] = (unsigned short)(buf[i * 9 + col / 2] >> (16 * (col & 1)));
-      __syncwarp();
-    }
+    for (int j = 0; j < 8; ++j) buf[lane * 9 + j] = o[j];
+    __syncwarp();
+    if (c < p.n)
+      for (int i = lane >> 4; i < 32 && m0 + i < p.m; i += 2)
+        reinterpret_cast<unsigned short*>(p.O)[((int64_t)w.b * p.m + m0 + i) * p.n + c] = (unsigned short)(buf[i * 9 + col / 2] >> (16 * (col & 1)));
+    __syncwarp();
   }
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr)
+               : "memory");
 }
 
 // ---- all steps -----------------------------------------------------------------------------------------
@@ -424,24 +416,24 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
       });
     }
   } else {
-    // ---------------- epilogue warps: a quarter of a CTA's rows, half of the columns each ----------------
-    const int quarter = warp & 3, half = (warp - 2) >> 2, me = warp - 2;
+    // ---------------- epilogue warps: a quarter of a CTA's rows, a quarter of the columns each ----------------
+    const int quarter = warp & 3, set = (warp - 2) >> 2, me = warp - 2;
     int acc = 0; uint32_t acc_ph = 0;
     uint32_t* buf = bufs + me * BUF_WORDS;
     each_unit([&](int step, const Unit& w) {
       const int m0 = w.i + (int)rank * 128 + quarter * 32;
-      const int c0 = half * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
-      uint32_t x[32];
+      const int c0 = set * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
+      uint32_t x[W];
       float pd = 0.f;
+      if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       if (w.mode != GRAM) {                        // what other CTAs have written is read from here on
         unsigned value;
         const unsigned* counter = awaited<PAIR>(p, w, step, value);
-        const bool ok = lane > 0 || wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; });
-        if (!__all_sync(0xffffffffu, ok)) return false;
+        if (lane == 0) load_acquire(counter);      // (the producer has seen it at its value)
+        __syncwarp();
         if (w.splits == 1 && c0 < c1) fetch(p, w, step, m0, w.j + c0, lane, x);
         if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
       }
-      if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)(acc * TILE) + ((uint32_t)(quarter * 32) << 16);
       // A tile in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
@@ -455,13 +447,13 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         unsigned* arrived = p.arrived + ((w.mode == POLY ? (int64_t)p.batch * p.sym * CTAS : 0) + place) * EPI + me;
         bool some = false;
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 32) {
+        for (int c = c0; c < c1; c += W) {
           if (mine(c)) { some = true; continue; }
-          uint32_t r[32];
-          tmem_ld32(t_row + c, r);
+          uint32_t r[W];
+          tmem_ld16(t_row + c, r);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < W / 4; ++j)
             sums[w.split * slice + ((c - c0) / 4 + j) * 32] =
                 make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
         }
@@ -475,37 +467,37 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         if (!__all_sync(0xffffffffu, ok)) return false;
       }
 #pragma unroll 1
-      for (int c = c0; c < c1; c += 32) {
+      for (int c = c0; c < c1; c += W) {
         if (!mine(c)) continue;
         const int n = w.j + c;
-        uint32_t r[32], next[32];
+        uint32_t r[W], next[W];
         float next_pd = pd;
-        tmem_ld32(t_row + c, r);
-        if (DIAG && w.mode == UPDATE && !p.left && c + 32 < c1) next_pd = diagonal(p, w, m0, n + 32, lane);
+        tmem_ld16(t_row + c, r);
+        if (DIAG && w.mode == UPDATE && !p.left && c + W < c1) next_pd = diagonal(p, w, m0, n + W, lane);
         if (w.splits > 1) fetch(p, w, step, m0, n, lane, x);
-        else if (c + 32 < c1) fetch(p, w, step, m0, n + 32, lane, next);
+        else if (c + W < c1) fetch(p, w, step, m0, n + W, lane, next);
         tmem_ld_wait();
         if (w.splits > 1) {
-          float all[32];
+          float all[W];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) all[j] = 0.f;
+          for (int j = 0; j < W; ++j) all[j] = 0.f;
 #pragma unroll 1
           for (int q = 0; q < w.splits; ++q) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < W / 4; ++j) {
               float4 v = make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
               if (q != w.split) v = __ldcg(sums + q * slice + ((c - c0) / 4 + j) * 32);
               all[4 * j] += v.x; all[4 * j + 1] += v.y; all[4 * j + 2] += v.z; all[4 * j + 3] += v.w;
             }
           }
 #pragma unroll
-          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(all[j]);
+          for (int j = 0; j < W; ++j) r[j] = __float_as_uint(all[j]);
         }
         finish<DIAG>(p, w, step, m0, n, r, x, pd, buf, lane);
         __syncwarp();
         pd = next_pd;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] = next[j];
+        for (int j = 0; j < W; ++j) x[j] = next[j];
       }
       tc_fence_before();
       __syncwarp();
