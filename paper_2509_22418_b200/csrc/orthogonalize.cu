@@ -554,14 +554,24 @@ template <int VEC> __device__ __forceinline__ float4 load4(const float* p, int l
   if (VEC) return *reinterpret_cast<const float4*>(p);
   return make_float4(p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, left > 3 ? p[3] : 0.f);
 }
-template <int VEC> __device__ __forceinline__ float4 load4(const bf16* p, int left) {
-  if (VEC) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
+// bf16 as they were read: they are converted when all of a thread's loads have been issued (a conversion waits for its load)
+struct Bf4 {
+  uint2 u;
+  __device__ __forceinline__ operator float4() const {
     const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
     return make_float4(a.x, a.y, b.x, b.y);
   }
-  return make_float4(__bfloat162float(p[0]), left > 1 ? __bfloat162float(p[1]) : 0.f, left > 2 ? __bfloat162float(p[2]) : 0.f, left > 3 ? __bfloat162float(p[3]) : 0.f);
+};
+template <int VEC> __device__ __forceinline__ Bf4 load4(const bf16* p, int left) {
+  if (VEC) return {*reinterpret_cast<const uint2*>(p)};
+  const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+  const uint32_t x = h[0], y = left > 1 ? h[1] : 0, z = left > 2 ? h[2] : 0, w = left > 3 ? h[3] : 0;
+  return {make_uint2(x | y << 16, z | w << 16)};
 }
+__device__ __forceinline__ void clear(float4& v) { v = make_float4(0.f, 0.f, 0.f, 0.f); }
+__device__ __forceinline__ void clear(Bf4& v) { v.u = make_uint2(0, 0); }
+template <typename T> struct FourOf { typedef float4 type; };
+template <> struct FourOf<bf16> { typedef Bf4 type; };
 __device__ __forceinline__ float4 weigh(float s, const float4 a, float t, const float4 b) {
   return make_float4(fmaf(s, a.x, t * b.x), fmaf(s, a.y, t * b.y), fmaf(s, a.z, t * b.z), fmaf(s, a.w, t * b.w));
 }
@@ -569,23 +579,24 @@ __device__ __forceinline__ float4 weigh(float s, const float4 a, float t, const 
 constexpr int AHEAD = 4;                            // fours of a thread in flight
 // the new momentum, and the sum of the squares of u in 64 bits (whose range holds any)
 template <typename TG, int VEC>
-__global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
+__global__ void __launch_bounds__(256, 4) ortho_norm_kernel(const PrepP p) {
   pdl_wait(); pdl_trigger();
   const int b = blockIdx.y;
   const uint32_t chunks = (p.cols + 3) / 4;
   const uint64_t n = (uint64_t)p.rows * chunks, stride = (uint64_t)gridDim.x * 256;
   double sum = 0.0;
   for (uint64_t e0 = (uint64_t)blockIdx.x * 256 + threadIdx.x; e0 < n; e0 += AHEAD * stride) {
-    float4 u[AHEAD], m[AHEAD];
+    typename FourOf<TG>::type raw[AHEAD];
+    float4 m[AHEAD];
     int64_t row[AHEAD]; int c[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const uint64_t e = e0 + i * stride;
       row[i] = n <= 0xffffffffu ? (uint32_t)e / chunks : e / chunks;
       c[i] = 4 * (int)(e - (uint64_t)row[i] * chunks);
-      u[i] = m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      clear(raw[i]); clear(m[i]);
       if (e < n) {
-        u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row[i] * p.ldg + c[i], p.cols - c[i]);
+        raw[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row[i] * p.ldg + c[i], p.cols - c[i]);
         if (p.m) m[i] = load4<VEC>(p.m + b * p.stride_m + row[i] * p.ldm + c[i], p.cols - c[i]);
       }
     }
@@ -593,15 +604,16 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(const PrepP p) {
     for (int i = 0; i < AHEAD; ++i) {
       if (e0 + i * stride >= n) break;
       const int left = p.cols - c[i];
+      float4 u = raw[i];
       if (p.m) {
-        const float4 g = u[i], v = weigh(p.beta, m[i], p.w, g);
+        const float4 g = u, v = weigh(p.beta, m[i], p.w, g);
         float* o = p.m_out + b * p.stride_m_out + row[i] * p.ldm_out + c[i];
         if (VEC) *reinterpret_cast<float4*>(o) = v;
         else { o[0] = v.x; if (left > 1) o[1] = v.y; if (left > 2) o[2] = v.z; if (left > 3) o[3] = v.w; }
-        u[i] = p.nesterov ? weigh(p.beta, v, p.w, g) : v;
+        u = p.nesterov ? weigh(p.beta, v, p.w, g) : v;
       }
-      sum = fma((double)u[i].x, (double)u[i].x, sum); sum = fma((double)u[i].y, (double)u[i].y, sum);
-      sum = fma((double)u[i].z, (double)u[i].z, sum); sum = fma((double)u[i].w, (double)u[i].w, sum);
+      sum = fma((double)u.x, (double)u.x, sum); sum = fma((double)u.y, (double)u.y, sum);
+      sum = fma((double)u.z, (double)u.z, sum); sum = fma((double)u.w, (double)u.w, sum);
     }
   }
   __shared__ double s_sum[8];
@@ -625,18 +637,15 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r0 = lane >> 3, c0 = 4 * (lane & 7);
   const int n = p.rows32 * p.cols32, e = n - 1 - (blockIdx.x * 8 + warp);      // (from the end: what was read last is still in the L2)
   const int rb = e / p.cols32, cb = e - rb * p.cols32, c = cb * 32 + c0, left = p.cols - c;
-  float4 u[8];
+  typename FourOf<TG>::type raw[8];
+  float4 m[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = rb * 32 + 4 * i + r0;
-    u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (e >= 0 && left > 0 && row < p.rows) {
-      u[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
-      if (p.m) {
-        const float4 m = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
-        u[i] = p.nesterov ? weigh(p.beta, m, p.w, u[i]) : m;
-      }
-    }
+    const bool there = e >= 0 && left > 0 && row < p.rows;
+    clear(raw[i]); clear(m[i]);
+    if (there) raw[i] = load4<VEC>((const TG*)p.G + b * p.stride_g + row * p.ldg + c, left);
+    if (there && p.m) m[i] = load4<VEC>(p.m_out + b * p.stride_m_out + row * p.ldm_out + c, left);
   }
   __shared__ double s_sum[8], s_inv;
   double sum = 0.0;
@@ -657,7 +666,9 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = rb * 32 + 4 * i + r0;
-    const float4 x = make_float4((float)(u[i].x * inv), (float)(u[i].y * inv), (float)(u[i].z * inv), (float)(u[i].w * inv));
+    float4 u = raw[i];
+    if (p.m) u = p.nesterov ? weigh(p.beta, m[i], p.w, u) : m[i];
+    const float4 x = make_float4((float)(u.x * inv), (float)(u.y * inv), (float)(u.z * inv), (float)(u.w * inv));
     if (p.O) {
       if (row < p.rows) {
         bf16* o = p.O + ((int64_t)b * p.rows + row) * p.cols + c;
@@ -1009,7 +1020,7 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.lds = ((int64_t)q.side + 63) / 64 * 64;
   q.rows32 = (m + 31) / 32; q.cols32 = (n + 31) / 32; q.side32 = (q.side + 31) / 32;
   const int64_t chunks = (int64_t)m * ((n + 3) / 4);
-  q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 8 / std::min(batch, SMS * 8)));
+  q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 4 / std::min(batch, SMS * 4)));
   auto tiles = [](int64_t x, int t) { return (int)((x + t - 1) / t); };
   // SM pairs on 256 x 256 tiles where X has enough of them, else single SMs on 128 x 128
   q.pair = q.side > 128 && (int64_t)tiles(m, 256) * tiles(n, 256) * batch >= 32;
