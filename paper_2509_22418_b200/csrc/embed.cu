@@ -26,18 +26,25 @@ constexpr int MAX_DIGITS = 256;
 constexpr int SMS = 148;                                     // work is split for a B200
 
 struct F8 { float f[8]; };
-__device__ __forceinline__ F8 load8(const float* p) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
-__device__ __forceinline__ F8 load8(const bf16* p) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
-  F8 r;
+// eight values as they were read: they are converted when all of a thread's loads have been issued (a conversion waits for its load)
+template <typename T> struct Raw8;
+template <> struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ F8 get() const { return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}}; }
+};
+template <> struct Raw8<bf16> {
+  uint4 u;
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ F8 get() const {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+    F8 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 x = __bfloat1622float2(h[i]); r.f[2 * i] = x.x; r.f[2 * i + 1] = x.y; }
-  return r;
-}
+    for (int i = 0; i < 4; ++i) { const float2 x = __bfloat1622float2(h[i]); r.f[2 * i] = x.x; r.f[2 * i + 1] = x.y; }
+    return r;
+  }
+};
+template <typename T> __device__ __forceinline__ F8 load8(const T* p) { Raw8<T> r; r.load(p); return r.get(); }
 __device__ __forceinline__ void store8(float* p, const F8& v) {
   *reinterpret_cast<float4*>(p) = make_float4(v.f[0], v.f[1], v.f[2], v.f[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(v.f[4], v.f[5], v.f[6], v.f[7]);
@@ -304,25 +311,27 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const SumArgs a) {
   const TD* dout = (const TD*)a.dout + col;
   bool ended = true;
   for (int i0 = lo; i0 < hi; i0 += AHEAD) {
-    F8 x[AHEAD], y[AHEAD];
+    Raw8<TD> x[AHEAD];
+    Raw8<TG> y[AHEAD];
     uint32_t id[AHEAD + 1];
 #pragma unroll
     for (int j = 0; j <= AHEAD; ++j) id[j] = i0 + j < min(hi + 1, a.T) ? a.keys[i0 + j] : NONE;
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j)
       if (i0 + j < hi && id[j] < V) {
-        x[j] = load8(dout + (int64_t)a.order[i0 + j] * a.ldd);
-        if (ADD && id[j + 1] != id[j]) y[j] = add_row<TG>(a, id[j], col);
+        x[j].load(dout + (int64_t)a.order[i0 + j] * a.ldd);
+        if (ADD && id[j + 1] != id[j]) y[j].load((const TG*)a.add + (int64_t)id[j] * a.ldadd + col);
       }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (i0 + j >= hi || id[j] >= V) break;        // (nothing but absent tokens follows)
+      const F8 v = x[j].get();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum.f[e] += x[j].f[e];
+      for (int e = 0; e < 8; ++e) sum.f[e] += v.f[e];
       ended = id[j + 1] != id[j];
       if (ended) {
         if (begun) store8(a.head + (int64_t)p * a.d + col, sum);
-        else finish_row<TG>(a, id[j], col, sum, y[j]);
+        else finish_row<TG>(a, id[j], col, sum, ADD ? y[j].get() : F8{});
         begun = false; sum = F8{};
       }
     }
