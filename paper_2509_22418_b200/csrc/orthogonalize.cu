@@ -1215,6 +1215,7 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   if (batch > 1 && (stride_g < 0 || (momentum && (stride_m < 0 || stride_mo < (m - 1) * ldmo + n)))) return ppu_fail(PPU_EINVAL, "matrices written must not overlap");
   if (momentum_out == momentum && momentum && (ldm != ldmo || (batch > 1 && stride_m != stride_mo)))
     return ppu_fail(PPU_EINVAL, "momentum_out in the place of momentum needs its strides");
+  if (momentum_out && (const void*)momentum_out == G) return ppu_fail(PPU_EINVAL, "G is read again after momentum_out is written: they must not overlap");
   const int g_bytes = g_type == PPU_BF16 ? 2 : 4;
   if ((reinterpret_cast<uintptr_t>(G) % g_bytes) || (reinterpret_cast<uintptr_t>(momentum) & 3) || (reinterpret_cast<uintptr_t>(momentum_out) & 3) ||
       (reinterpret_cast<uintptr_t>(O) & 15) || (reinterpret_cast<uintptr_t>(workspace) & 255))

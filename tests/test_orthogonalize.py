@@ -313,7 +313,7 @@ def _coef(*v):
     (dict(gt=2), -1), (dict(eps=C.c_float(-1)), -1), (dict(eps=C.c_float(math.nan)), -1), (dict(mom="there"), -1), (dict(out="there"), -1), (dict(ldg=C.c_int64(15)), -1),
     (dict(mom="there", out="else", ldm=C.c_int64(8)), -1), (dict(mom="there", out="else", ldo=C.c_int64(8)), -1), (dict(mom="there", out="else", so=C.c_int64(64)), -1),
     (dict(mom="there", out="there", ldm=C.c_int64(20)), -1), (dict(mom="there", out="there", sm=C.c_int64(130)), -1), (dict(sg=C.c_int64(-4)), -1), (dict(G="odd"), -1),
-    (dict(mom="odd", out="there"), -1), (dict(O="odd"), -1), (dict(ws="odd"), -1),
+    (dict(mom="odd", out="there"), -1), (dict(mom="else", out="there"), -1), (dict(O="odd"), -1), (dict(ws="odd"), -1),
     (dict(coef=_coef(4.0, -4.0, 3.0)), -1), (dict(coef=_coef(math.nan, 0.0, 0.0)), -1), (dict(coef=_coef(math.inf, 0.0, 0.0)), -1), (dict(coef=_coef(1.0, 1e30, -1e30)), -1),
     (dict(coef=_coef(-3.0, 0.0, 0.0)), -1), (dict(coef=_coef(3.4445, -4.775, math.nan)), -1),
 ])
@@ -348,3 +348,53 @@ def test_device_tensors_are_checked():
     for bad in (G.half(), G[0, 0], G.transpose(1, 2), G[None]):
         with pytest.raises(ppu.PpuError):
             ppu.ppu_orthogonalize(bad)
+
+
+# ---- matrices of many tiles (SM pairs), in 64 bits on the GPU ---------------------------------------
+def on_gpu(u, rounded, steps=5):
+    """The definition (rounded False) or the model of u [batch, m, n]."""
+    import torch
+    def h(x):
+        return (x * 4096).half().double() / 4096 if rounded else x
+    left, small = u.shape[1] <= u.shape[2], min(u.shape[1:]) < 256
+    X = u / (u.square().sum((1, 2), keepdim=True).sqrt() + f32(1e-7))
+    for a, b, c in triples(COEF, steps):
+        hi = h(X)
+        G = h(hi @ hi.mT if left else hi.mT @ hi)
+        P = b * G + c * G @ G
+        d = torch.diagonal(P, dim1=1, dim2=2).clone() if small else torch.zeros_like(P[:, 0])
+        P = h(P - torch.diag_embed(d))
+        X = a * X + (d[:, :, None] * hi + P @ hi if left else d[:, None, :] * hi + hi @ P)
+    return X
+
+
+@gpu
+@pytest.mark.parametrize("batch,m,n,momentum", [
+    (1, 1536, 1600, False), (1, 1701, 1404, True),       # one matrix, on either side
+    (9, 300, 520, True), (9, 520, 301, False), (12, 150, 700, False), (40, 200, 190, True),      # batches, without and with P's diagonal apart
+    (1, 2560, 2304, False), (1, 2304, 2567, False),      # a last wave of halves
+    (1, 520, 8200, False), (1, 8200, 520, True), (3, 333, 8193, False),      # A in slices of its sums
+    (2, 17, 4100, False), (1, 128, 2056, False), (1, 2049, 100, True),       # sides up to 128 that are too long for the chip
+])
+def test_matrices_of_many_tiles(batch, m, n, momentum):
+    import torch
+    from paper_2509_22418_b200 import ppu
+    g = torch.Generator(device="cuda").manual_seed(m)
+    G = torch.randn(batch, m, n, generator=g, device="cuda")
+    old = torch.randn(batch, m, n, generator=g, device="cuda") if momentum else None
+    flags = torch.zeros(8, dtype=torch.int32, device="cuda")
+    O, new = ppu.ppu_orthogonalize(G, momentum=old, flags=flags)
+    ppu.ppu_op_status(flags)
+    u = G.double() if old is None else G.double() + f32(0.95) * new.double()
+    if old is not None:
+        assert float((new.double() - (f32(0.95) * old.double() + G.double())).abs().max()) <= 2.0 ** -22 * float(new.abs().max())
+    want, mod = on_gpu(u, False), on_gpu(u, True)
+    size = want.square().mean((1, 2), keepdim=True).sqrt()
+    cost = (mod - want).square().mean((1, 2), keepdim=True).sqrt() / size
+    err = (O.double() - want).abs()
+    off = err.square().mean((1, 2), keepdim=True).sqrt() / size
+    assert bool((off <= 1.25 * cost + BF / math.sqrt(3)).all()), (float(off.max()), float(cost.max()))
+    # (up to 7e6 values: seven deviations where near() has six)
+    assert bool((err <= (BF + 2.0 ** -7) * want.abs() + 14 * cost * size).all()), float((err / size).max())
+    again = ppu.ppu_orthogonalize(G, momentum=old)
+    assert torch.equal(again[0], O)
