@@ -9,6 +9,10 @@
   head  --m T --n V --k D [--teacher K] [--grad xe|x|e|none]  head loss of T rows against V ids (cross entropy, or
                                                        distillation from K teacher entries)
   norm  --m T --k D [--rms] [--gate-rows R]            gated norm pair, forward and backward
+  embed --m T --n V --k D [--f32] [--add]              lookup of T tokens and the table's gradient (--f32: in fp32; --add: on top of
+                                                       another one)
+  qk    --batch B --seq S --heads H [--kv-heads K] --dh D      norms of queries and keys with rotation, forward and backward
+  ortho --batch B --m M --k N [--f32] [--momentum]     orthogonalised update of B matrices M x N (--f32: of fp32 ones)
 Times with CUDA events on the launching stream after warm-up; operands are sized by the caller
 (keep them above the 126 MB L2 if DRAM behaviour matters).  Also the target of profiler runs.
 """
@@ -22,7 +26,7 @@ from paper_2509_22418_b200 import build, ppu, synth
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["gemm", "attn", "path", "head", "norm"])
+    ap.add_argument("op", choices=["gemm", "attn", "path", "head", "norm", "embed", "qk", "ortho"])
     ap.add_argument("--m", type=int, default=8192)
     ap.add_argument("--n", type=int, default=8192)
     ap.add_argument("--k", type=int, default=2048)
@@ -46,6 +50,9 @@ def main():
     ap.add_argument("--chunk-rows", type=int, default=0, help="head: rows of a chunk")
     ap.add_argument("--rms", action="store_true")
     ap.add_argument("--gate-rows", type=int, default=0, help="norm: rows that share a row of the gate (0: all of them)")
+    ap.add_argument("--add", action="store_true", help="embed: the gradient is added to another one")
+    ap.add_argument("--kv-heads", type=int, default=0, help="qk: heads of keys and of values (0: as many as queries)")
+    ap.add_argument("--momentum", action="store_true", help="ortho: with a momentum")
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--warmup", type=int, default=3)
     a = ap.parse_args()
@@ -123,6 +130,32 @@ def main():
         print(f"norm fwd T={T} d={d}: {ms:.4f} ms {(12.0 * T * d + gate_bytes) / ms / 1e6:.0f} GB/s")
         ms = timed(lambda: ppu.ppu_norm_gate_bwd(hh, r, y, r_out, st, one, one, **kw))
         print(f"norm bwd: {ms:.4f} ms {(18.0 * T * d + 2 * gate_bytes) / ms / 1e6:.0f} GB/s")
+    elif a.op == "embed":
+        T, V, d = a.m, a.n, a.k
+        word, size = ("fp32", 4) if a.f32 else ("bf16", 2)
+        ids = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(dev)
+        E, dout = torch.randn((V, d), generator=g).to(dev).bfloat16(), torch.randn((T, d), generator=g).to(dev)
+        add = torch.randn((V, d), generator=g).to(dev).to(torch.float32 if a.f32 else torch.bfloat16) if a.add else None
+        ms = timed(lambda: ppu.ppu_embed_fwd(ids, E))
+        print(f"embed fwd T={T} V={V} d={d}: {ms:.4f} ms {6.0 * T * d / ms / 1e6:.0f} GB/s")
+        ms = timed(lambda: ppu.ppu_embed_bwd(ids, dout, V, dtype=word, add=add))
+        print(f"embed bwd to {word} add={a.add}: {ms:.4f} ms {(4.0 * T * d + (2 if a.add else 1) * size * V * d) / ms / 1e6:.0f} GB/s")
+    elif a.op == "qk":
+        T, kv, dh = a.batch * a.seq, a.kv_heads or a.heads, a.dh
+        x = torch.randn((T, (a.heads + 2 * kv) * dh), generator=g).to(dev).bfloat16()
+        dy, gain = torch.randn(x.shape, generator=g).to(dev).bfloat16(), torch.ones(dh, device=dev)
+        kw = dict(q_gain=gain, k_gain=gain, seq=a.seq)
+        ms = timed(lambda: ppu.ppu_qk_norm_fwd(x, a.heads, kv, kv, **kw))
+        print(f"qk fwd T={T} heads={a.heads}+{kv}+{kv} dh={dh}: {ms:.4f} ms {4.0 * x.numel() / ms / 1e6:.0f} GB/s")
+        ms = timed(lambda: ppu.ppu_qk_norm_bwd(dy, x, a.heads, kv, kv, **kw))
+        print(f"qk bwd: {ms:.4f} ms {(6.0 * T * (a.heads + kv) + 4.0 * T * kv) * dh / ms / 1e6:.0f} GB/s")
+    elif a.op == "ortho":
+        G = torch.randn((a.batch, a.m, a.k), generator=g).to(dev)
+        mom = torch.randn(G.shape, generator=g).to(dev) if a.momentum else None
+        G = G if a.f32 else G.bfloat16()
+        ms = timed(lambda: ppu.ppu_orthogonalize(G, momentum=mom))
+        s, l = min(a.m, a.k), max(a.m, a.k)
+        print(f"ortho {a.batch} x {a.m} x {a.k} momentum={a.momentum}: {ms:.4f} ms {5.0 * a.batch * s * s * (3 * l + s) / ms / 1e9:.1f} TFLOP/s (symmetric products half)")
     else:
         B_, S, h, dh = a.batch, a.seq, a.heads, a.dh
         d = h * dh
