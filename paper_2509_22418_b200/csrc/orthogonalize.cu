@@ -7,18 +7,22 @@
 // for matrices with more rows than columns A = X^T X and X = a X + X P, so that A and P are of the shorter side.
 //
 // Numbers.  The products' operands are fp16 (11 bits; bf16 has 8) times powers of two that keep |X| <= 2.8 below the
-// largest and 2^-26 above the smallest normal number; sums are fp32.  X itself is carried in fp32 beside its fp16 copy, and
-// a X is formed from that: rounding X leaves noise in directions whose singular values are small, and the polynomial multiplies
+// largest and 2^-26 above the smallest normal number; sums are fp32.  X itself is carried as that fp16 copy and a second fp16 number, what the
+// first leaves of it (22 bits; fp32 on chip), and a X is formed from both: rounding X leaves noise in directions whose singular values are small, and the polynomial multiplies
 // those by a = 3.4 a step, noise included.  For sides below DIAG_SIDE P's diagonal is kept in fp32 and multiplies the same fp16 copy of X as the rest of
 // P (so that what P annuls it annuls as a whole): it comes to -2.7 where singular values come to one, and half a step of fp16 there is 2^-10 of X.
 // Root mean square error of O relative to O's (5 steps, CPU model; the rounding of O to bf16 is 1.66e-3): bf16 operands and X 1e-2 for random matrices, 0.16 to
-// 0.35 for those with a few large directions; fp16 operands and X 1.3e-3 and 2e-2 to 4e-2; with X in fp32 1.4e-3 (sides of 768), 1.7e-3 (256), 2.4e-3 (33)
-// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 7 % more time (8192 x 2048 117 -> 125 us a step, 24 x 256 x 2048 49 ->
-// 53, whose tiles of X are bound by what is done with them).  Sides up to 128 are mostly worked on chip, below.
+// 0.35 for those with a few large directions; fp16 operands and X 1.3e-3 and 2e-2 to 4e-2; with X carried so 1.4e-3 (sides of 768), 1.7e-3 (256), 2.4e-3 (33)
+// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 8 to 11 % more time (8192 x 2048 113 -> 122 us a step, 24 x 256 x 2048
+// 45.3 -> 50.3, 12 x 768 x 768 39.4 -> 43.5: tiles of X are bound by what is done with them).  Sides up to 128 are mostly worked on chip, below.
 //
 // A and A A are symmetric: only tiles on and below the diagonal are worked and stored; a block above it is read as its
 // mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
 // the columns, a tile of 128 x 128 took 7 us more.)
+//
+// What bounds it.  8192 x 2048: 117 GFLOP a step in 110 to 113 us (1050 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
+// A on 74 pairs), 12 (36 tiles of A A) and 43 (256 tiles of X, in three waves and a half); the rest is the ends of the parts, each of which reads what the last warps
+// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 45 us a step for 14 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>
@@ -38,7 +42,8 @@ constexpr int X_EXP = 12, A_EXP = 12;                 // powers of two of X and 
 constexpr int SMS = 148, MAX_STEPS = 32, MAX_SIDE = 1 << 16, DIAG_SIDE = 256;
 enum Mode { GRAM = 0, POLY = 1, UPDATE = 2 };
 
-constexpr int EPI = 8, W = 16;                      // epilogue warps, columns they take at a time
+// epilogue warps, columns they take at a time (8192 x 2048, a step: 8 and 16 110 us, 8 and 32 112, 16 and 16 115: more of them delay the copies' and products' own threads)
+constexpr int EPI = 8, W = 16;
 constexpr int KH = 2, BOX = 128 * BK * 2;             // 64-k slabs of a stage; bytes of a box of 64 x 128
 constexpr int STAGES = 3, STAGE_BYTES = 2 * KH * BOX; // a CTA's share of a stage: 128 rows of A, 128 of B, 128 k
 constexpr int BUF_WORDS = 32 * 9;                     // an epilogue warp's
@@ -416,7 +421,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
       });
     }
   } else {
-    // ---------------- epilogue warps: a quarter of a CTA's rows, a quarter of the columns each ----------------
+    // ---------------- epilogue warps: a quarter of a CTA's rows, half of the columns each ----------------
     const int quarter = warp & 3, set = (warp - 2) >> 2, me = warp - 2;
     int acc = 0; uint32_t acc_ph = 0;
     uint32_t* buf = bufs + me * BUF_WORDS;
@@ -1065,7 +1070,7 @@ int check_ortho(int batch, int m, int n, int steps) {
   if (batch < 0 || m < 0 || n < 0) return ppu_fail(PPU_EINVAL, "negative size");
   if (m > MAX_SIDE || n > MAX_SIDE || batch > 65535) return ppu_fail(PPU_ESHAPE, "at most 65535 matrices of sides up to %d", MAX_SIDE);
   if (steps < 0 || steps > MAX_STEPS) return ppu_fail(PPU_EINVAL, "steps must be 0 to %d", MAX_STEPS);
-  // (32 warps report each tile in each of 32 steps: counted in 32 bits)
+  // (16 warps report each tile in each of 32 steps: counted in 32 bits)
   const int64_t tiles = (((int64_t)m + 127) / 128) * (((int64_t)n + 127) / 128) * batch;
   if (tiles > (1 << 20)) return ppu_fail(PPU_ESHAPE, "too many matrices of this size");
   return PPU_OK;
