@@ -46,6 +46,7 @@ enum Mode { GRAM = 0, POLY = 1, UPDATE = 2 };
 constexpr int EPI = 8, W = 16;
 constexpr int KH = 2, BOX = 128 * BK * 2;             // 64-k slabs of a stage; bytes of a box of 64 x 128
 constexpr int STAGES = 3, STAGE_BYTES = 2 * KH * BOX; // a CTA's share of a stage: 128 rows of A, 128 of B, 128 k
+constexpr int GO = 8;                               // barriers that tell the epilogues that what a unit reads is there
 constexpr int BUF_WORDS = 32 * 9;                     // an epilogue warp's
 constexpr int SMEM = STAGES * STAGE_BYTES + EPI * BUF_WORDS * 4 + 1024 + 256;
 constexpr int BLOCK = 64 + 32 * EPI;
@@ -300,7 +301,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint32_t* bufs = reinterpret_cast<uint32_t*>(smem + STAGES * STAGE_BYTES);
   uint64_t* bars = reinterpret_cast<uint64_t*>(bufs + EPI * BUF_WORDS);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4 + GO);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = PAIR ? cluster_rank() : 0;
@@ -309,11 +310,14 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
   auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
   auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
   auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
+  // (the copying thread is up to five units ahead of the epilogues: the one they work on, the next, finished, and one in each stage lie between)
+  auto go_bar = [&](int u) { return bar0 + 8u * (2 * STAGES + 4 + (u & (GO - 1))); };
   auto leaders = [&](uint32_t bar) { return PAIR ? map_to_rank(bar, 0) : bar; };
   auto wait_bar = [&](uint32_t bar, uint32_t parity) { return wait_for(abort_flag, p.flags, [&] { return mbar_try(bar, parity); }); };
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), CTAS * EPI); }
+    for (int u = 0; u < GO; ++u) mbar_init(go_bar(u), 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -350,11 +354,12 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
   if (warp == 0) {
     if (lane == 0) {
       // ---------------- TMA producer (each CTA: 128 rows of A, its half of B's) ----------------
-      int s = 0; uint32_t ph = 0;
+      int s = 0, u = 0; uint32_t ph = 0;
       each_unit([&](int step, const Unit& w) {
         unsigned value;
         const unsigned* counter = awaited<PAIR>(p, w, step, value);
         if (!wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; })) return false;
+        mbar_arrive(go_bar(u++));
         asm volatile("fence.proxy.async.global;" ::: "memory");      // (the operands were written by plain stores)
         const CUtensorMap* X = maps + (step & 1);
         const CUtensorMap *mA = w.mode == GRAM ? X : w.mode == POLY ? maps + 2 : p.left ? maps + 3 : X;
@@ -423,22 +428,19 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
   } else {
     // ---------------- epilogue warps: a quarter of a CTA's rows, half of the columns each ----------------
     const int quarter = warp & 3, set = (warp - 2) >> 2, me = warp - 2;
-    int acc = 0; uint32_t acc_ph = 0;
+    int acc = 0, u = 0; uint32_t acc_ph = 0;
     uint32_t* buf = bufs + me * BUF_WORDS;
     each_unit([&](int step, const Unit& w) {
       const int m0 = w.i + (int)rank * 128 + quarter * 32;
       const int c0 = set * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
       uint32_t x[W];
       float pd = 0.f;
+      // what other CTAs have written is read from here on (the copying thread has seen the counter), while the products run
+      if (!__all_sync(0xffffffffu, wait_bar(go_bar(u), u / GO & 1))) return false;
+      ++u;
+      if (w.splits == 1 && c0 < c1) fetch(p, w, step, m0, w.j + c0, lane, x);
+      if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
       if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
-      if (w.mode != GRAM) {                        // what other CTAs have written is read from here on
-        unsigned value;
-        const unsigned* counter = awaited<PAIR>(p, w, step, value);
-        if (lane == 0) load_acquire(counter);      // (the producer has seen it at its value)
-        __syncwarp();
-        if (w.splits == 1 && c0 < c1) fetch(p, w, step, m0, w.j + c0, lane, x);
-        if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
-      }
       tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)(acc * TILE) + ((uint32_t)(quarter * 32) << 16);
       // A tile in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
