@@ -20,9 +20,9 @@
 // mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
 // the columns, a tile of 128 x 128 took 7 us more.)
 //
-// What bounds it.  8192 x 2048: 117 GFLOP a step in 110 to 113 us (1050 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
+// What bounds it.  8192 x 2048: 117 GFLOP a step in 106 us (1100 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
 // A on 74 pairs), 12 (36 tiles of A A) and 43 (256 tiles of X, in three waves and a half); the rest is the ends of the parts, each of which reads what the last warps
-// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 45 us a step for 14 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
+// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 41.5 us a step for 14 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>
@@ -196,49 +196,40 @@ __device__ __forceinline__ const unsigned* awaited(const KernelP& p, const Unit&
 __device__ __forceinline__ int64_t block_at(int b, int rows32, int cols32, int m, int n) {
   return (((int64_t)b * rows32 + m / 32) * cols32 + n / 32) * 1024 + (n & 16) * 32;
 }
-// what a unit's result is made of beside the accumulator: A for P, X for X
-__device__ __forceinline__ void fetch(const KernelP& p, const Unit& w, int step, int m0, int n, int lane, uint32_t* x) {
-  if (w.mode == POLY) {
-    if (m0 < p.side) ld_v8(x, p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane);
-  } else if (w.mode == UPDATE && m0 < p.m) {
-    if (m0 + lane < p.m) ld_v8(x, p.hi[step & 1] + ((int64_t)w.b * p.m + m0 + lane) * p.ld + n);
-    ld_v8(x + 8, p.lo + block_at(w.b, p.rows32, p.cols32, m0, n) + 16 * lane);
-  }
-}
 // P's diagonal for this lane's row (left), or for column n + lane % 16
 __device__ __forceinline__ float diagonal(const KernelP& p, const Unit& w, int m0, int n, int lane) {
   const int i = p.left ? m0 + lane : n + (lane & 15);
   return i < p.side ? __ldcg(p.diag + (int64_t)w.b * p.side + i) : 0.f;
 }
-// buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored
+// A, or P with x of A
+template <bool DIAG>
+__device__ __forceinline__ void finish_product(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, int lane) {
+  const int m = m0 + lane;
+  uint32_t o[8];
+  if (w.mode == GRAM) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = half2_bits(p.gram * __uint_as_float(r[2 * j]), p.gram * __uint_as_float(r[2 * j + 1]));
+    st_v8(p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane, o);
+  } else {
+    const float b = p.b[step], c = p.c[step];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 v = half2_floats(x[j]);
+      float2 y = make_float2(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
+      if (DIAG && n - m0 == (lane & 16) && (lane & 15) / 2 == j) {      // the diagonal
+        if (m < p.side) p.diag[(int64_t)w.b * p.side + m] = p.d[step] * (lane & 1 ? y.y : y.x);
+        (lane & 1 ? y.y : y.x) = 0.f;
+      }
+      o[j] = half2_bits(y.x, y.y);
+    }
+  }
+  if (m < p.side) st_v8((w.mode == GRAM ? p.A : p.P) + ((int64_t)w.b * p.side + m) * p.lds + n, o);
+}
+// X, with x: X's two numbers of before.  buf: 32 x 9 words of the warp, through which rows of O that are not whole 16 bytes are stored;
 // pd: P's diagonal of this lane's row (left) or of column n + lane % 16
 template <bool DIAG>
-__device__ __forceinline__ void finish(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, float pd, uint32_t* buf, int lane) {
+__device__ __forceinline__ void finish_x(const KernelP& p, const Unit& w, int step, int m0, int n, const uint32_t* r, const uint32_t* x, float pd, uint32_t* buf, int lane) {
   const int m = m0 + lane;
-  if (w.mode != UPDATE) {
-    if (m0 >= p.side) return;
-    uint32_t o[8];
-    if (w.mode == GRAM) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = half2_bits(p.gram * __uint_as_float(r[2 * j]), p.gram * __uint_as_float(r[2 * j + 1]));
-      st_v8(p.A2 + block_at(w.b, p.side32, p.side32, m0, n) + 16 * lane, o);
-    } else {
-      const float b = p.b[step], c = p.c[step];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 v = half2_floats(x[j]);
-        float2 y = make_float2(fmaf(c, __uint_as_float(r[2 * j]), b * v.x), fmaf(c, __uint_as_float(r[2 * j + 1]), b * v.y));
-        if (DIAG && n - m0 == (lane & 16) && (lane & 15) / 2 == j) {      // the diagonal
-          if (m < p.side) p.diag[(int64_t)w.b * p.side + m] = p.d[step] * (lane & 1 ? y.y : y.x);
-          (lane & 1 ? y.y : y.x) = 0.f;
-        }
-        o[j] = half2_bits(y.x, y.y);
-      }
-    }
-    if (m < p.side) st_v8((w.mode == GRAM ? p.A : p.P) + ((int64_t)w.b * p.side + m) * p.lds + n, o);
-    return;
-  }
-  if (m0 >= p.m) return;
   const float a = p.a[step], f = p.f[step];
   // a X + (P's diagonal) (X in fp16) + f (the rest of P X)
   float y[W];
@@ -296,6 +287,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
 template <bool PAIR, bool DIAG>
 __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const KernelP& p) {
   constexpr int CTAS = PAIR ? 2 : 1, TILE = 128 * CTAS;
+  constexpr int PIECES = 4;                     // of W columns, fetched ahead (203 x 333, a step: one 19.7 us, two 18.1, four 17.2; 24 x 256 x 2048: 45, 42.3, 41.6)
   extern __shared__ uint8_t smem_raw[];
   // (the window starts at the same offset in both CTAs of a pair, so aligned offsets match too)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -350,6 +342,8 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
   // which operand's 128 x 128 blocks from k0 on are read in the order [k][rows]: X in A = X^T X and as the second operand of P X, and
   // blocks of A and P above the diagonal
   auto a_mn = [&](const Unit& w, int k0) { return w.mode == GRAM ? !p.left : (w.mode == POLY || p.left) && k0 / TILE > w.i / TILE; };
+  // (a tile on the diagonal of A or A A: both operands are the same)
+  auto same = [&](const Unit& w) { return w.mode != UPDATE && w.i == w.j; };
   auto b_mn = [&](const Unit& w, int k0) { return w.mode == GRAM ? !p.left : w.mode == UPDATE && p.left ? true : k0 / TILE > w.j / TILE; };
   if (warp == 0) {
     if (lane == 0) {
@@ -372,7 +366,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
           const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;      // (the second slab may lie past the end of the sum)
           // blocks [rows][k] come in a box for each slab of 64 k, blocks [k][rows] in one for each 64 rows, of 128 k
           const bool amn = a_mn(w, k0), bmn = b_mn(w, k0);
-          const int a_boxes = amn ? 2 : slabs, b_boxes = bmn ? b_rows / 64 : slabs;
+          const int a_boxes = amn ? 2 : slabs, b_boxes = same(w) ? 0 : bmn ? b_rows / 64 : slabs;
           if (rank == 0) mbar_expect_tx(full_bar(s), CTAS * (a_boxes + b_boxes) * BOX);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
@@ -403,7 +397,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
           if (!wait_bar(full_bar(s), ph)) return false;
           tc_fence_after();
-          const uint32_t a_addr = smem_u32(smem + s * STAGE_BYTES), b_addr = a_addr + KH * BOX;
+          const uint32_t a_addr = smem_u32(smem + s * STAGE_BYTES), b_addr = same(w) ? a_addr : a_addr + KH * BOX;
           const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;
           const bool amn = a_mn(w, k0), bmn = b_mn(w, k0);
           const uint32_t idesc = idesc0 | ((amn ? 1u : 0u) << 15) | ((bmn ? 1u : 0u) << 16);
@@ -433,19 +427,36 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
     each_unit([&](int step, const Unit& w) {
       const int m0 = w.i + (int)rank * 128 + quarter * 32;
       const int c0 = set * (w.bn / 2), c1 = min(c0 + w.bn / 2, (w.mode == UPDATE ? p.n : p.side) - w.j);      // columns of the tile
-      uint32_t x[W];
-      float pd = 0.f;
+      uint32_t x[PIECES][W];
+      float pd[PIECES];
       // what other CTAs have written is read from here on (the copying thread has seen the counter), while the products run
       if (!__all_sync(0xffffffffu, wait_bar(go_bar(u), u / GO & 1))) return false;
       ++u;
-      if (w.splits == 1 && c0 < c1) fetch(p, w, step, m0, w.j + c0, lane, x);
-      if (DIAG && w.mode == UPDATE && c0 < c1) pd = diagonal(p, w, m0, w.j + c0, lane);
+      const bool rows = m0 < (w.mode == UPDATE ? p.m : p.side);
+      const __half* x_hi = p.hi[step & 1] + ((int64_t)w.b * p.m + min(m0 + lane, p.m - 1)) * p.ld;
+      auto fetch_x = [&](int q, int c) {           // (no branches on what is loaded where: values would be moved, and waited for)
+        if (c >= c1) return;
+        ld_v8(x[q], x_hi + w.j + c);
+        ld_v8(x[q] + 8, p.lo + block_at(w.b, p.rows32, p.cols32, m0, w.j + c) + 16 * lane);
+        if (DIAG) pd[q] = diagonal(p, w, m0, w.j + c, lane);
+      };
+      auto fetch_a = [&](int q, int c) {
+        if (c < c1) ld_v8(x[q], p.A2 + block_at(w.b, p.side32, p.side32, m0, w.j + c) + 16 * lane);
+      };
+      if (rows && w.mode == UPDATE) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) fetch_x(q, c0 + q * W);
+      }
+      if (rows && w.mode == POLY && w.splits == 1) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) fetch_a(q, c0 + q * W);
+      }
       if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)(acc * TILE) + ((uint32_t)(quarter * 32) << 16);
       // A tile in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
       // up those of its own columns in the order of the slices.  (The slices of a tile are consecutive units, so that they are worked at the same time.)
-      auto mine = [&](int c) { return w.splits == 1 || c / 32 * w.splits / (w.bn / 32) == w.split; };
+      auto mine = [&](int c) { return w.splits == 1 || (c - c0) / W * w.splits / (w.bn / 2 / W) == w.split; };
       const int tile = w.i / TILE * (w.i / TILE + 1) / 2 + w.j / TILE;
       const int64_t place = ((int64_t)w.b * p.sym + tile) * CTAS + rank;
       const int64_t slice = (int64_t)128 * TILE / 4;      // in float4
@@ -473,38 +484,69 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         }
         if (!__all_sync(0xffffffffu, ok)) return false;
       }
+      // the tile's pieces, q of every PIECES: fn(q, column)
+      auto each_piece = [&](auto fn) {
 #pragma unroll 1
-      for (int c = c0; c < c1; c += W) {
-        if (!mine(c)) continue;
-        const int n = w.j + c;
-        uint32_t r[W], next[W];
-        float next_pd = pd;
-        tmem_ld16(t_row + c, r);
-        if (DIAG && w.mode == UPDATE && !p.left && c + W < c1) next_pd = diagonal(p, w, m0, n + W, lane);
-        if (w.splits > 1) fetch(p, w, step, m0, n, lane, x);
-        else if (c + W < c1) fetch(p, w, step, m0, n + W, lane, next);
-        tmem_ld_wait();
-        if (w.splits > 1) {
-          float all[W];
+        for (int from = c0; from < c1; from += PIECES * W) {
 #pragma unroll
-          for (int j = 0; j < W; ++j) all[j] = 0.f;
-#pragma unroll 1
-          for (int q = 0; q < w.splits; ++q) {
-#pragma unroll
-            for (int j = 0; j < W / 4; ++j) {
-              float4 v = make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
-              if (q != w.split) v = __ldcg(sums + q * slice + ((c - c0) / 4 + j) * 32);
-              all[4 * j] += v.x; all[4 * j + 1] += v.y; all[4 * j + 2] += v.z; all[4 * j + 3] += v.w;
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < W; ++j) r[j] = __float_as_uint(all[j]);
+          for (int q = 0; q < PIECES; ++q)
+            if (from + q * W < c1) fn(q, from + q * W);
         }
-        finish<DIAG>(p, w, step, m0, n, r, x, pd, buf, lane);
-        __syncwarp();
-        pd = next_pd;
+      };
+      if (!rows) {
+      } else if (w.mode == UPDATE) {
+        each_piece([&](int q, int c) {
+          uint32_t r[W];
+          tmem_ld16(t_row + c, r);
+          tmem_ld_wait();
+          finish_x<DIAG>(p, w, step, m0, w.j + c, r, x[q], pd[q], buf, lane);
+          fetch_x(q, c + PIECES * W);
+        });
+      } else if (w.splits == 1) {
+        each_piece([&](int q, int c) {
+          uint32_t r[W];
+          tmem_ld16(t_row + c, r);
+          tmem_ld_wait();
+          finish_product<DIAG>(p, w, step, m0, w.j + c, r, x[q], lane);
+          if (w.mode == POLY) fetch_a(q, c + PIECES * W);
+        });
+      } else {
+        const int first = w.split == 0;            // what this slice has left of a piece is in flight ahead
+        auto fetch_sums = [&](int q, int c) {
+          if (c >= c1 || !mine(c)) return;
 #pragma unroll
-        for (int j = 0; j < W; ++j) x[j] = next[j];
+          for (int j = 0; j < W / 4; ++j) {
+            const float4 v = __ldcg(sums + first * slice + ((c - c0) / 4 + j) * 32);
+            x[q][4 * j] = __float_as_uint(v.x); x[q][4 * j + 1] = __float_as_uint(v.y); x[q][4 * j + 2] = __float_as_uint(v.z); x[q][4 * j + 3] = __float_as_uint(v.w);
+          }
+        };
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) fetch_sums(q, c0 + q * W);
+        each_piece([&](int piece, int c) {
+          if (mine(c)) {
+            uint32_t r[W], a[8];
+            tmem_ld16(t_row + c, r);
+            if (w.mode == POLY) ld_v8(a, p.A2 + block_at(w.b, p.side32, p.side32, m0, w.j + c) + 16 * lane);
+            tmem_ld_wait();
+            float all[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) all[j] = 0.f;
+#pragma unroll 1
+            for (int q = 0; q < w.splits; ++q) {
+#pragma unroll
+              for (int j = 0; j < W / 4; ++j) {
+                float4 v = make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]), __uint_as_float(r[4 * j + 3]));
+                if (q == first) v = make_float4(__uint_as_float(x[piece][4 * j]), __uint_as_float(x[piece][4 * j + 1]), __uint_as_float(x[piece][4 * j + 2]), __uint_as_float(x[piece][4 * j + 3]));
+                else if (q != w.split) v = __ldcg(sums + q * slice + ((c - c0) / 4 + j) * 32);
+                all[4 * j] += v.x; all[4 * j + 1] += v.y; all[4 * j + 2] += v.z; all[4 * j + 3] += v.w;
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < W; ++j) r[j] = __float_as_uint(all[j]);
+            finish_product<DIAG>(p, w, step, m0, w.j + c, r, a, lane);
+          }
+          fetch_sums(piece, c + PIECES * W);
+        });
       }
       tc_fence_before();
       __syncwarp();
@@ -1035,9 +1077,9 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;
   q.tiles_m = tiles(m, t); q.tiles_n = tiles(n, t);
-  // Sums of A and A A in slices where there are fewer tiles than workers.  Pairs: of 4096 products at least, since joining slices takes about 9 us, and
-  // 2048 products 10 (8192 x 2048: A in two slices 31 us, in one 48; A A, whose sums are of 2048, 20 and 15).  Single SMs: of 1024 (8 x 64 x 4096: a
-  // step 25.7 us, in one slice 34.3, in eight 27.8).
+  // Sums of A and A A in slices where there are fewer tiles than workers.  Pairs: of 4096 products at least, since joining slices takes about 7 us, and
+  // 2048 products 10 (8192 x 2048: A in two slices 30 us, in one 48; with A A, whose sums are of 2048, in two as well, 107 us a step both ways).  Single SMs: of 1024
+  // (8 x 64 x 4096: a step 20.9 us, in one slice 34.3, in eight 23.3).
   for (int i = 0; i < 2; ++i) {
     const int64_t k_blocks = ((i == 0 ? std::max(m, n) : q.side) + KH * BK - 1) / (KH * BK);
     q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / (q.pair ? 32 : 8)}));
