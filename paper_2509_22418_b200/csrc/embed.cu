@@ -101,15 +101,30 @@ __device__ __forceinline__ uint32_t warp_rank(uint32_t digit, int bits, bool val
 
 struct Fill { void* dE; int64_t ldde; const void* add; int64_t ldadd; uint32_t rows, chunks; int mode; };   // mode 0: nothing, 1: zeros, 2: copy add; chunks of 16 bytes
 
-__device__ void fill_rows(const Fill& f, uint32_t block, uint32_t blocks, int bytes_log2) {
-  const uint64_t n = (uint64_t)f.rows * f.chunks;
-  for (uint64_t i = (uint64_t)block * blockDim.x + threadIdx.x; i < n; i += (uint64_t)blocks * blockDim.x) {
-    const uint64_t v = n <= 0xffffffffu ? (uint32_t)i / f.chunks : i / f.chunks;
-    const uint32_t c = (uint32_t)(i - v * f.chunks);
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (f.mode == 2) x = *reinterpret_cast<const uint4*>((const uint8_t*)f.add + ((v * f.ldadd) << bytes_log2) + 16 * c);
-    *reinterpret_cast<uint4*>((uint8_t*)f.dE + ((v * f.ldde) << bytes_log2) + 16 * c) = x;
+// AT_ONCE: 16 bytes in flight of a thread
+template <int AT_ONCE, bool COPY> __device__ __forceinline__ void fill_loop(const Fill& f, uint32_t block, uint32_t blocks, int bytes_log2) {
+  const uint64_t n = (uint64_t)f.rows * f.chunks, step = (uint64_t)blocks * blockDim.x;
+  for (uint64_t i0 = (uint64_t)block * blockDim.x + threadIdx.x; i0 < n; i0 += AT_ONCE * step) {
+    uint4 x[AT_ONCE];
+    uint64_t v[AT_ONCE];
+    uint32_t c[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const uint64_t i = i0 + j * step;
+      v[j] = n <= 0xffffffffu ? (uint32_t)i / f.chunks : i / f.chunks;
+      c[j] = (uint32_t)(i - v[j] * f.chunks);
+      x[j] = make_uint4(0, 0, 0, 0);
+      if (COPY && i < n) x[j] = *reinterpret_cast<const uint4*>((const uint8_t*)f.add + ((v[j] * f.ldadd) << bytes_log2) + 16 * c[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (i0 + j * step < n) *reinterpret_cast<uint4*>((uint8_t*)f.dE + ((v[j] * f.ldde) << bytes_log2) + 16 * c[j]) = x[j];
   }
+}
+// (a copy of 32003 x 768 in fp32, with sums of 4099 tokens: 43.6 us with four in flight, 50 with one; zeros, 32768 x 2048 in bf16, 44.5 and 43.5)
+__device__ __forceinline__ void fill_rows(const Fill& f, uint32_t block, uint32_t blocks, int bytes_log2) {
+  if (f.mode == 2) fill_loop<4, true>(f, block, blocks, bytes_log2);
+  else fill_loop<1, false>(f, block, blocks, bytes_log2);
 }
 
 // Block 0 sorts, the others fill.  ITEMS: tokens a thread.
