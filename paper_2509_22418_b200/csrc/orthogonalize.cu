@@ -69,6 +69,7 @@ struct KernelP {
   float* diag;                       // [batch][side] P's diagonal, times d; null: it stays in P
   float* partial;                    // slices' sums
   unsigned *done, *arrived;          // [3][batch] warps that have finished; [2][batch][sym][CTAs][EPI] slices that have left their sums
+  unsigned* along; int tiles_l;      // [batch][tiles_l] and of them, for X, those of each tile along the longer side: 2 each, 1 for half a tile
   int* flags;
 };
 
@@ -349,21 +350,30 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
     if (lane == 0) {
       // ---------------- TMA producer (each CTA: 128 rows of A, its half of B's) ----------------
       int s = 0, u = 0; uint32_t ph = 0;
+      const unsigned tiles_short = p.left ? p.tiles_m : p.tiles_n;
       each_unit([&](int step, const Unit& w) {
         unsigned value;
         const unsigned* counter = awaited<PAIR>(p, w, step, value);
-        if (!wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; })) return false;
-        mbar_arrive(go_bar(u++));
+        // A's products need not wait for all of X: they are over the longer side, whose tiles are finished in that order
+        bool all = w.mode != GRAM;
+        if (all && !wait_for(abort_flag, p.flags, [&] { return load_acquire(counter) >= value; })) return false;
+        if (all) mbar_arrive(go_bar(u));
         asm volatile("fence.proxy.async.global;" ::: "memory");      // (the operands were written by plain stores)
         const CUtensorMap* X = maps + (step & 1);
         const CUtensorMap *mA = w.mode == GRAM ? X : w.mode == POLY ? maps + 2 : p.left ? maps + 3 : X;
         const CUtensorMap *mB = w.mode == GRAM ? X : w.mode == POLY ? maps + 2 : p.left ? X : maps + 3;
         const int a0 = w.i + (int)rank * 128, b_rows = w.bn / CTAS, b0 = w.j + (int)rank * b_rows;
         for (int kb = w.kb0; kb < w.kb1; ++kb) {
+          const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;      // (the second slab may lie past the end of the sum)
+          if (!all && (kb == w.kb0 || k0 % TILE == 0)) {
+            all = load_acquire(counter) >= value;
+            const unsigned *tile = p.along + (int64_t)w.b * p.tiles_l + k0 / TILE, there = 2u * step * tiles_short * CTAS * EPI;
+            if (!all && !wait_for(abort_flag, p.flags, [&] { return load_acquire(tile) >= there; })) return false;
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+          }
           if (!wait_bar(empty_bar(s), ph ^ 1u)) return false;
           const uint32_t a_dst = smem_u32(smem + s * STAGE_BYTES), b_dst = a_dst + KH * BOX;
           const uint32_t fb = leaders(full_bar(s));
-          const int k0 = kb * KH * BK, slabs = k0 + BK < w.K ? KH : 1;      // (the second slab may lie past the end of the sum)
           // blocks [rows][k] come in a box for each slab of 64 k, blocks [k][rows] in one for each 64 rows, of 128 k
           const bool amn = a_mn(w, k0), bmn = b_mn(w, k0);
           const int a_boxes = amn ? 2 : slabs, b_boxes = same(w) ? 0 : bmn ? b_rows / 64 : slabs;
@@ -382,6 +392,8 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
           }
           if (++s == STAGES) { s = 0; ph ^= 1u; }
         }
+        if (w.mode == GRAM) mbar_arrive(go_bar(u));
+        ++u;
         return true;
       });
     }
@@ -557,7 +569,10 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
       asm volatile("fence.proxy.async.global;" ::: "memory");      // (read by copies of other CTAs)
       __syncwarp();
       if (lane == 0) {
-        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + w.mode * p.batch + w.b) : "memory");
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        if (w.mode == UPDATE)
+          asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(p.along + (int64_t)w.b * p.tiles_l + (p.left ? w.j : w.i) / TILE), "r"(w.bn == TILE ? 2 : 1) : "memory");
+        asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + w.mode * p.batch + w.b) : "memory");
       }
       if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
       return true;
@@ -1103,7 +1118,7 @@ Plan make_plan(int batch, int m, int n, int steps) {
     q.diag = take(q.side < DIAG_SIDE ? (size_t)batch * q.side * 4 : 0);
     const int most = std::max(q.splits[0], q.splits[1]), ctas = q.pair ? 2 : 1;
     q.sums = take(most > 1 ? (size_t)batch * q.sym * most * t * t * 4 : 0);
-    q.n_counters = 3 * batch + (most > 1 ? 2 * batch * q.sym * ctas * EPI : 0);
+    q.n_counters = (3 + std::max(q.tiles_m, q.tiles_n)) * batch + (most > 1 ? 2 * batch * q.sym * ctas * EPI : 0);
     q.counters = take((size_t)q.n_counters * 4);
   }
   q.bytes = at;
@@ -1320,6 +1335,6 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
     p.b[k] = std::ldexp(c[1], p_exp[k] - A_EXP); p.c[k] = std::ldexp(c[2], p_exp[k] - 2 * A_EXP);
     p.a[k] = std::ldexp(c[0], out); p.f[k] = p.d[k] = std::ldexp(1.f, out - p_exp[k]);
   }
-  p.partial = (float*)(ws + q.sums); p.done = pp.counters; p.arrived = p.done + 3 * batch; p.flags = flags;
+  p.partial = (float*)(ws + q.sums); p.done = pp.counters; p.tiles_l = p.left ? q.tiles_n : q.tiles_m; p.along = p.done + 3 * batch; p.arrived = p.along + (int64_t)batch * p.tiles_l; p.flags = flags;
   return launch_steps(maps, p, q.pair, st);
 }
