@@ -325,18 +325,26 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const SumArgs a) {
   F8 sum = {};
   const TD* dout = (const TD*)a.dout + col;
   bool ended = true;
+  // ids and tokens of the rows AHEAD further are on their way while rows are
+  uint32_t id[AHEAD + 1], token[AHEAD];
+  auto ids_from = [&](int i, uint32_t (&k)[AHEAD + 1], uint32_t (&o)[AHEAD]) {
+#pragma unroll
+    for (int j = 0; j <= AHEAD; ++j) k[j] = i + j < min(hi + 1, a.T) ? a.keys[i + j] : NONE;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) o[j] = i + j < hi ? a.order[i + j] : 0;
+  };
+  ids_from(lo, id, token);
   for (int i0 = lo; i0 < hi; i0 += AHEAD) {
     Raw8<TD> x[AHEAD];
     Raw8<TG> y[AHEAD];
-    uint32_t id[AHEAD + 1];
-#pragma unroll
-    for (int j = 0; j <= AHEAD; ++j) id[j] = i0 + j < min(hi + 1, a.T) ? a.keys[i0 + j] : NONE;
+    uint32_t next_id[AHEAD + 1], next_token[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j)
       if (i0 + j < hi && id[j] < V) {
-        x[j].load(dout + (int64_t)a.order[i0 + j] * a.ldd);
+        x[j].load(dout + (int64_t)token[j] * a.ldd);
         if (ADD && id[j + 1] != id[j]) y[j].load((const TG*)a.add + (int64_t)id[j] * a.ldadd + col);
       }
+    ids_from(i0 + AHEAD, next_id, next_token);
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (i0 + j >= hi || id[j] >= V) break;        // (nothing but absent tokens follows)
@@ -350,6 +358,10 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(const SumArgs a) {
         begun = false; sum = F8{};
       }
     }
+#pragma unroll
+    for (int j = 0; j <= AHEAD; ++j) id[j] = next_id[j];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) token[j] = next_token[j];
   }
   if (!ended) store8((begun ? a.head : a.last) + (int64_t)p * a.d + col, sum);      // the id goes on in the next piece
 }
