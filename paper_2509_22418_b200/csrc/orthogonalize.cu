@@ -1086,8 +1086,14 @@ Plan make_plan(int batch, int m, int n, int steps) {
   const int64_t chunks = (int64_t)m * ((n + 3) / 4);
   q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 4 / std::min(batch, SMS * 4)));
   auto tiles = [](int64_t x, int t) { return (int)((x + t - 1) / t); };
-  // SM pairs on 256 x 256 tiles where X has enough of them, else single SMs on 128 x 128
-  q.pair = q.side > 128 && (int64_t)tiles(m, 256) * tiles(n, 256) * batch >= 32;
+  // SM pairs on 256 x 256 tiles, or single SMs on 128 x 128.  Pairs read half as much for a product, singles have four times the units to share out and shorter
+  // ones to wait for.  So pairs where the products bound a step, from about 28 GFLOP on, or where there are some waves of full tiles.  A step, us, pairs and singles:
+  // 8192 x 2048 (117 GFLOP) 104 and 144, 2 x 2048 x 2048 60 and 79, 2048 x 2048 (34) 50.1 and 53.0, 4 x 1024 x 2048 (30) 47 and 45, 6 x 1024 x 1024 (26) 38.0 and 37.8,
+  // 24 x 384 x 2048 (23; of its pairs' tiles a quarter is empty) 70 and 55, 1536 x 2048 (18) 44.7 and 42.4, 4096 x 1024 (14) 49 and 40, 24 x 256 x 2048 (10; 192
+  // full tiles) 38.1 and 40.0, 24 x 256 x 1024 (5; 96) 27.4 and 22.5, 2 x 346 x 2239 32.7 and 22.6.
+  const double flop = (double)batch * q.side * q.side * (3.0 * std::max(m, n) + q.side);
+  const int64_t singles = (int64_t)tiles(m, 128) * tiles(n, 128) * batch, pairs = (int64_t)tiles(m, 256) * tiles(n, 256) * batch;
+  q.pair = q.side > 128 && (flop >= 28e9 || (2 * pairs >= 5 * (SMS / 2) && 2 * singles >= 7 * pairs));
   const int t = q.pair ? 256 : 128;
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;

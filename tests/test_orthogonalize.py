@@ -350,7 +350,7 @@ def test_device_tensors_are_checked():
             ppu.ppu_orthogonalize(bad)
 
 
-# ---- matrices of many tiles (SM pairs), in 64 bits on the GPU ---------------------------------------
+# ---- matrices of many tiles, in 64 bits on the GPU ---------------------------------------------------
 def on_gpu(u, rounded, steps=5):
     """The definition (rounded False) or the model of u [batch, m, n]."""
     import torch
@@ -375,6 +375,8 @@ def on_gpu(u, rounded, steps=5):
     (1, 2560, 2304, False), (1, 2304, 2567, False),      # a last wave of halves
     (1, 520, 8200, False), (1, 8200, 520, True), (3, 333, 8193, False),      # A in slices of its sums
     (2, 17, 4100, False), (1, 128, 2056, False), (1, 2049, 100, True),       # sides up to 128 that are too long for the chip
+    (40, 200, 1281, True), (40, 1281, 190, False), (101, 509, 481, False), (96, 400, 1009, True),      # SM pairs: waves of tiles
+    (1, 2048, 8200, False), (1, 8197, 1500, True), (2, 1793, 2047, False),      # SM pairs: large products, A in slices of its sums
 ])
 def test_matrices_of_many_tiles(batch, m, n, momentum):
     import torch
