@@ -13,16 +13,16 @@
 // P (so that what P annuls it annuls as a whole): it comes to -2.7 where singular values come to one, and half a step of fp16 there is 2^-10 of X.
 // Root mean square error of O relative to O's (5 steps, CPU model; the rounding of O to bf16 is 1.66e-3): bf16 operands and X 1e-2 for random matrices, 0.16 to
 // 0.35 for those with a few large directions; fp16 operands and X 1.3e-3 and 2e-2 to 4e-2; with X carried so 1.4e-3 (sides of 768), 1.7e-3 (256), 2.4e-3 (33)
-// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 8 to 11 % more time (8192 x 2048 113 -> 122 us a step, 24 x 256 x 2048
-// 45.3 -> 50.3, 12 x 768 x 768 39.4 -> 43.5: tiles of X are bound by what is done with them).  Sides up to 128 are mostly worked on chip, below.
+// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 2 to 9 % more time (8192 x 2048 106 -> 108 us a step, 24 x 256 x 2048
+// 37.3 -> 39.7, 12 x 768 x 768 35.0 -> 38.2).  Sides up to 128 are mostly worked on chip, below.
 //
 // A and A A are symmetric: only tiles on and below the diagonal are worked and stored; a block above it is read as its
 // mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
 // the columns, a tile of 128 x 128 took 7 us more.)
 //
-// What bounds it.  8192 x 2048: 117 GFLOP a step in 106 us (1100 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
+// What bounds it.  8192 x 2048: 117 GFLOP a step in 104 to 106 us (1110 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
 // A on 74 pairs), 12 (36 tiles of A A) and 43 (256 tiles of X, in three waves and a half); the rest is the ends of the parts, each of which reads what the last warps
-// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 41.5 us a step for 14 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
+// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 38 us a step for 10 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>
@@ -1087,13 +1087,15 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 4 / std::min(batch, SMS * 4)));
   auto tiles = [](int64_t x, int t) { return (int)((x + t - 1) / t); };
   // SM pairs on 256 x 256 tiles, or single SMs on 128 x 128.  Pairs read half as much for a product, singles have four times the units to share out and shorter
-  // ones to wait for.  So pairs where the products bound a step, from about 28 GFLOP on, or where there are some waves of full tiles.  A step, us, pairs and singles:
+  // ones to wait for.  So pairs where the products bound a step, from 20 GFLOP on (28 where a good part of their tiles
+  // is empty), or where there are some waves of full tiles.  A step, us, pairs and singles:
   // 8192 x 2048 (117 GFLOP) 104 and 144, 2 x 2048 x 2048 60 and 79, 2048 x 2048 (34) 50.1 and 53.0, 4 x 1024 x 2048 (30) 47 and 45, 6 x 1024 x 1024 (26) 38.0 and 37.8,
-  // 24 x 384 x 2048 (23; of its pairs' tiles a quarter is empty) 70 and 55, 1536 x 2048 (18) 44.7 and 42.4, 4096 x 1024 (14) 49 and 40, 24 x 256 x 2048 (10; 192
+  // 24 x 384 x 2048 (23; of its pairs' tiles a quarter is empty) 70 and 55, 12 x 768 x 768 (22) 35.0 and 34.7, 1536 x 2048 (18) 44.7 and 42.4, 4096 x 1024 (14) 49 and 40, 24 x 256 x 2048 (10; 192
   // full tiles) 38.1 and 40.0, 24 x 256 x 1024 (5; 96) 27.4 and 22.5, 2 x 346 x 2239 32.7 and 22.6.
   const double flop = (double)batch * q.side * q.side * (3.0 * std::max(m, n) + q.side);
   const int64_t singles = (int64_t)tiles(m, 128) * tiles(n, 128) * batch, pairs = (int64_t)tiles(m, 256) * tiles(n, 256) * batch;
-  q.pair = q.side > 128 && (flop >= 28e9 || (2 * pairs >= 5 * (SMS / 2) && 2 * singles >= 7 * pairs));
+  const bool full = 2 * singles >= 7 * pairs;
+  q.pair = q.side > 128 && (flop >= (full ? 20e9 : 28e9) || (full && 2 * pairs >= 5 * (SMS / 2)));
   const int t = q.pair ? 256 : 128;
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;
