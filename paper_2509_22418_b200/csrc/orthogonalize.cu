@@ -147,10 +147,11 @@ template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar) {
 
 // ---- units -----------------------------------------------------------------------------------------
 // A step's units are all matrices' of A, then of P, then of X; CTAs (or pairs) take every n-th of them, step after step.
-// A unit waits for what it reads to be finished: A of the matrix for its X, P for its A, X for its P, each a counter.
+// A unit waits for what it reads to be finished: P of the matrix for its A, X for its P, each a counter, A for its X, tile by tile
+// along the longer side, over which it sums.
 // A unit waits only for units that come before it, and all CTAs are resident (a cooperative launch) and work in order: so
-// there is always one that can go on.  The same waits order what is overwritten: A's tiles are written when X, and so P, of
-// the step before are done, P's when A is, X's other buffer when P is.
+// there is always one that can go on.  The same waits order what is overwritten: A's tiles are written when X has been begun, and so P of
+// the step before is done, P's when A is, X's other buffer when P is.
 struct Unit { int mode, b, i, j, split, splits, kb0, kb1, K, bn; };
 template <bool PAIR>
 __device__ __forceinline__ Unit unit_at(const KernelP& p, int r) {
