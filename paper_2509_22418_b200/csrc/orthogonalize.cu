@@ -497,13 +497,13 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         }
         if (!__all_sync(0xffffffffu, ok)) return false;
       }
-      // the tile's pieces, q of every PIECES: fn(q, column)
+      // the tile's pieces, q of every PIECES: fn(q, column); the lanes come together before each, which reads tensor memory
       auto each_piece = [&](auto fn) {
 #pragma unroll 1
         for (int from = c0; from < c1; from += PIECES * W) {
 #pragma unroll
           for (int q = 0; q < PIECES; ++q)
-            if (from + q * W < c1) fn(q, from + q * W);
+            if (from + q * W < c1) { __syncwarp(); fn(q, from + q * W); }
         }
       };
       if (!rows) {
@@ -580,6 +580,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
     });
   }
   // ---------------- common exit ----------------
+  __syncwarp();
   if (*abort_flag) {
     for (int i = 0; i < 64; ++i) __nanosleep(2000);      // copies and products in flight
   }
@@ -836,6 +837,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  __syncwarp();
   if (warp == 0) tmem_alloc(smem_u32(&s_tmem), 512);
   tc_fence_before();
   __syncthreads();
@@ -859,10 +861,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     __syncwarp();
     meanwhile();
     wait_for(abort_flag, p.flags, [&] { return mbar_try(bar, parity); });      // (where it gives up the results are not valid, and flags say so)
+    __syncwarp();                                    // (each lane has left the wait by itself)
     parity ^= 1;
     tc_fence_after();
   };
-  auto cluster_barrier = [&] { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+  // All lanes of a warp take part in a barrier of the cluster, and in a copy to or from tensor memory, together: they are joined before, wherever they may
+  // have gone different ways.
+  auto cluster_barrier = [&] { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); };
 
   // u, the new momentum and the sum of squares
   double sum = 0.0;
@@ -882,8 +887,10 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     uint32_t bits[32];
 #pragma unroll
     for (int q = 0; q < 32; ++q) { sum = fma((double)u[q], (double)u[q], sum); bits[q] = __float_as_uint(u[q]); }
+    __syncwarp();
     tmem_st32(tX + 32 * c, bits);
   }
+  __syncwarp();
   tmem_st_wait();
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_part[warp] = sum;
@@ -906,6 +913,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     // X (after the last step O), and its fp16 copy
     for (int c = part; c < chunks; c += PARTS) {
       uint32_t r[32], y[32];
+      __syncwarp();
       tmem_ld32(tX + 32 * c, r);
       if (step > 0) tmem_ld32(tAcc + 32 * c, y);
       tmem_ld_wait();
@@ -1027,6 +1035,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
 #pragma unroll 1
     for (int c = 128 / PARTS * part; c < 128 / PARTS * (part + 1); c += 32) {
       uint32_t r[32];
+      __syncwarp();
       tmem_ld32(tAcc + c, r);
       tmem_ld_wait();
       const float fb = p.b[step], fc = p.c[step];
@@ -1058,6 +1067,9 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
       }
     }, [] {});
   }
+  __syncwarp();
+  if (*abort_flag)
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);  // products in flight
   tc_fence_before();
   __syncthreads();
   cluster_barrier();                                 // no CTA leaves while another may still read its shared memory
