@@ -56,7 +56,7 @@ struct KernelP {
   int m, n, side, batch, steps, left;
   int tiles_s, sym;                  // tiles along the shorter side, on and below the diagonal
   int tiles_m, tiles_n, n_fast;      // of X
-  int splits[2];                     // slices of the sum of A, of A A
+  int splits;                        // slices of the sum of A
   int units[3];                      // units of a matrix
   int tail_from;                     // tiles of X from here on are worked in two halves of their columns
   int per_step;
@@ -68,7 +68,7 @@ struct KernelP {
   float a[MAX_STEPS], b[MAX_STEPS], c[MAX_STEPS], f[MAX_STEPS], d[MAX_STEPS];
   float* diag;                       // [batch][side] P's diagonal, times d; null: it stays in P
   float* partial;                    // slices' sums
-  unsigned *done, *arrived;          // [3][batch] warps that have finished; [2][batch][sym][CTAs][EPI] slices that have left their sums
+  unsigned *done, *arrived;          // [3][batch] warps that have finished; [batch][sym][CTAs][EPI] slices that have left their sums
   unsigned* along; int tiles_l;      // [batch][tiles_l] and of them, for X, those of each tile along the longer side: 2 each, 1 for half a tile
   int* flags;
 };
@@ -149,8 +149,9 @@ template <bool PAIR> __device__ __forceinline__ void commit(uint32_t bar) {
 // A step's units are all matrices' of A, then of P, then of X; CTAs (or pairs) take every n-th of them, step after step.
 // A unit waits for what it reads to be finished: P of the matrix for its A, X for its P, each a counter, A for its X, tile by tile
 // along the longer side, over which it sums.
-// A unit waits only for units that come before it, and all CTAs are resident (a cooperative launch) and work in order: so
-// there is always one that can go on.  The same waits order what is overwritten: A's tiles are written when X has been begun, and so P of
+// A unit waits only for units that come before it (and slices of a tile of A for one another), and all CTAs are resident (a cooperative launch) and work in
+// order: so there is always one that can go on.  (A tile's slices are consecutive units of different workers, and each leaves its sums before it waits: the first
+// unit that has not come so far waits for nothing behind it, and nor does its worker, whose unit before is finished or of a tile all of whose slices have.)  The same waits order what is overwritten: A's tiles are written when X has been begun, and so P of
 // the step before is done, P's when A is, X's other buffer when P is.
 struct Unit { int mode, b, i, j, split, splits, kb0, kb1, K, bn; };
 template <bool PAIR>
@@ -168,9 +169,11 @@ __device__ __forceinline__ Unit unit_at(const KernelP& p, int r) {
   const int k_blocks = (w.K + KH * BK - 1) / (KH * BK);
   w.kb0 = 0; w.kb1 = k_blocks;
   if (w.mode != UPDATE) {
-    w.splits = w.mode == GRAM ? p.splits[0] : p.splits[1];
-    w.split = t % w.splits; t /= w.splits;
-    w.kb0 = (int)((int64_t)w.split * k_blocks / w.splits); w.kb1 = (int)((int64_t)(w.split + 1) * k_blocks / w.splits);
+    if (w.mode == GRAM) {
+      w.splits = p.splits;
+      w.split = t % w.splits; t /= w.splits;
+      w.kb0 = (int)((int64_t)w.split * k_blocks / w.splits); w.kb1 = (int)((int64_t)(w.split + 1) * k_blocks / w.splits);
+    }
     int i = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while ((i + 1) * (i + 2) / 2 <= t) ++i;
     while (i * (i + 1) / 2 > t) --i;
@@ -460,14 +463,14 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) fetch_x(q, c0 + q * W);
       }
-      if (rows && w.mode == POLY && w.splits == 1) {
+      if (rows && w.mode == POLY) {
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) fetch_a(q, c0 + q * W);
       }
       if (!__all_sync(0xffffffffu, wait_bar(tfull_bar(acc), acc_ph))) return false;
       tc_fence_after();
       const uint32_t t_row = tmem_base + (uint32_t)(acc * TILE) + ((uint32_t)(quarter * 32) << 16);
-      // A tile in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
+      // A tile of A in slices: each slice leaves its sums of the columns that are others' to finish, laid out as the lanes read them, and adds
       // up those of its own columns in the order of the slices.  (The slices of a tile are consecutive units, so that they are worked at the same time.)
       auto mine = [&](int c) { return w.splits == 1 || (c - c0) / W * w.splits / (w.bn / 2 / W) == w.split; };
       const int tile = w.i / TILE * (w.i / TILE + 1) / 2 + w.j / TILE;
@@ -475,7 +478,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
       const int64_t slice = (int64_t)128 * TILE / 4;      // in float4
       float4* sums = reinterpret_cast<float4*>(p.partial) + place * w.splits * slice + me * (32 * (TILE / 2) / 4) + lane;
       if (w.splits > 1) {
-        unsigned* arrived = p.arrived + ((w.mode == POLY ? (int64_t)p.batch * p.sym * CTAS : 0) + place) * EPI + me;
+        unsigned* arrived = p.arrived + place * EPI + me;
         bool some = false;
 #pragma unroll 1
         for (int c = c0; c < c1; c += W) {
@@ -537,9 +540,8 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
         for (int q = 0; q < PIECES; ++q) fetch_sums(q, c0 + q * W);
         each_piece([&](int piece, int c) {
           if (mine(c)) {
-            uint32_t r[W], a[8];
+            uint32_t r[W];
             tmem_ld16(t_row + c, r);
-            if (w.mode == POLY) ld_v8(a, p.A2 + block_at(w.b, p.side32, p.side32, m0, w.j + c) + 16 * lane);
             tmem_ld_wait();
             float all[W];
 #pragma unroll
@@ -556,7 +558,7 @@ __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const Kerne
             }
 #pragma unroll
             for (int j = 0; j < W; ++j) r[j] = __float_as_uint(all[j]);
-            finish_product<DIAG>(p, w, step, m0, w.j + c, r, a, lane);
+            finish_product<DIAG>(p, w, step, m0, w.j + c, r, x[piece], lane);      // (of x only a tile of P reads)
           }
           fetch_sums(piece, c + PIECES * W);
         });
@@ -1084,7 +1086,7 @@ struct Plan {
   int side, blocks; int64_t ld, lds;
   bool pair;
   int ctas, chunk;                   // on chip: CTAs of a matrix (0: not so), columns of each
-  int tiles_s, sym, tiles_m, tiles_n, splits[2], workers;
+  int tiles_s, sym, tiles_m, tiles_n, splits, workers;
   size_t partial, hi[2], lo, a, a2, p, diag, sums, counters, bytes;
   int rows32, cols32, side32;
   int n_counters;
@@ -1113,13 +1115,11 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;
   q.tiles_m = tiles(m, t); q.tiles_n = tiles(n, t);
-  // Sums of A and A A in slices where there are fewer tiles than workers.  Pairs: of 4096 products at least, since joining slices takes about 7 us, and
-  // 2048 products 10 (8192 x 2048: A in two slices 30 us, in one 48; with A A, whose sums are of 2048, in two as well, 107 us a step both ways).  Single SMs: of 1024
-  // (8 x 64 x 4096: a step 20.9 us, in one slice 34.3, in eight 23.3).
-  for (int i = 0; i < 2; ++i) {
-    const int64_t k_blocks = ((i == 0 ? std::max(m, n) : q.side) + KH * BK - 1) / (KH * BK);
-    q.splits[i] = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / (q.pair ? 32 : 8)}));
-  }
+  // The sums of A in slices where there are fewer tiles than workers.  Pairs: of 4096 products at least, since joining slices takes about 7 us, and
+  // 2048 products 10 (8192 x 2048: A in two slices 30 us, in one 48).  Single SMs: of 1024 (8 x 64 x 4096: a step 20.9 us, in one slice 34.3, in eight 23.3).
+  // (A A's sums are of the shorter side; by the same rule it has more tiles than workers before they are long enough.)
+  const int64_t k_blocks = ((int64_t)std::max(m, n) + KH * BK - 1) / (KH * BK);
+  q.splits = (int)std::max<int64_t>(1, std::min<int64_t>({8, q.workers / std::max<int64_t>(1, (int64_t)q.sym * batch), k_blocks / (q.pair ? 32 : 8)}));
   // on chip where a cluster of up to 8 CTAs holds the matrix
   const int length = std::max(m, n);
   if (steps > 0 && q.side <= SMALL_SIDE && length <= SMALL_COLS * SMALL_CTAS) {
@@ -1137,9 +1137,9 @@ Plan make_plan(int batch, int m, int n, int steps) {
     q.hi[0] = take(x); q.hi[1] = take(steps > 1 ? x : 0); q.lo = take((size_t)batch * q.rows32 * q.cols32 * 2048);
     q.a = take(s); q.a2 = take((size_t)batch * q.side32 * q.side32 * 2048); q.p = take(s);
     q.diag = take(q.side < DIAG_SIDE ? (size_t)batch * q.side * 4 : 0);
-    const int most = std::max(q.splits[0], q.splits[1]), ctas = q.pair ? 2 : 1;
-    q.sums = take(most > 1 ? (size_t)batch * q.sym * most * t * t * 4 : 0);
-    q.n_counters = (3 + std::max(q.tiles_m, q.tiles_n)) * batch + (most > 1 ? 2 * batch * q.sym * ctas * EPI : 0);
+    const int ctas = q.pair ? 2 : 1;
+    q.sums = take(q.splits > 1 ? (size_t)batch * q.sym * q.splits * t * t * 4 : 0);
+    q.n_counters = (3 + std::max(q.tiles_m, q.tiles_n)) * batch + (q.splits > 1 ? batch * q.sym * ctas * EPI : 0);
     q.counters = take((size_t)q.n_counters * 4);
   }
   q.bytes = at;
@@ -1220,7 +1220,7 @@ int launch_steps(const Maps& maps, const KernelP& p, bool pair, cudaStream_t st)
     if (!ppu_set_smem_once(attr_set[i], kernels[i], SMEM)) return ppu_fail(PPU_ECUDA, "shared memory limit not accepted");
   auto kernel = kernels[2 * pair + (p.diag != nullptr)];
   const int most = resident(pair);
-  if (most < 1) return ppu_fail(PPU_ECUDA, "the kernel does not fit on this device");
+  if (most < p.splits) return ppu_fail(PPU_ECUDA, "the kernel does not fit on this device");
   const int units = p.batch * std::max(p.units[GRAM], std::max(p.units[POLY], p.units[UPDATE]));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((pair ? 2 : 1) * std::min(most, units)); cfg.blockDim = dim3(BLOCK); cfg.dynamicSmemBytes = SMEM; cfg.stream = st;
@@ -1339,10 +1339,10 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   KernelP p = {};
   p.m = m; p.n = n; p.side = q.side; p.batch = batch; p.steps = steps; p.left = m <= n;
   p.tiles_s = q.tiles_s; p.sym = q.sym; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n; p.n_fast = m > n;
-  p.splits[0] = q.splits[0]; p.splits[1] = q.splits[1];
+  p.splits = q.splits;
   const int tiles = q.tiles_m * q.tiles_n, rem = tiles % q.workers;
   p.tail_from = 1 << 30;
-  p.units[GRAM] = q.sym * q.splits[0]; p.units[POLY] = q.sym * q.splits[1]; p.units[UPDATE] = tiles;
+  p.units[GRAM] = q.sym * q.splits; p.units[POLY] = q.sym; p.units[UPDATE] = tiles;
   if (q.pair && batch == 1 && tiles > q.workers && rem > 0 && 2 * rem <= q.workers) {      // a last wave of halves instead of one of few tiles
     p.tail_from = tiles - rem;
     p.units[UPDATE] = tiles + rem;

@@ -32,3 +32,19 @@ def test_on_chip_beside_other_work(batch, m, n):
                 got.append(ppu.ppu_orthogonalize(G)[0])
     torch.cuda.synchronize()
     assert all(torch.equal(g, ref) for g in got)
+
+
+@gpu
+@pytest.mark.parametrize("batch,m,n", [(3, 333, 8193), (2, 520, 4100), (2, 8200, 300)])
+def test_slices_of_several_matrices(batch, m, n):
+    """A in slices of its sums, several matrices at once: their sums lie apart, whatever the workspace held, however often."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    x = matrices(batch, m, n, "large directions")
+    G = cuda(x)
+    ref = ppu.ppu_orthogonalize(G)[0]
+    near(ref, x.astype("float64"))
+    nb = ppu.ppu_orthogonalize_query_bytes(batch, m, n)
+    ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(8):
+        assert torch.equal(ppu.ppu_orthogonalize(G, workspace=ws)[0], ref)
