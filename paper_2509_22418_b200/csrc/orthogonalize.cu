@@ -644,6 +644,13 @@ __device__ __forceinline__ float4 weigh(float s, const float4 a, float t, const 
   return make_float4(fmaf(s, a.x, t * b.x), fmaf(s, a.y, t * b.y), fmaf(s, a.z, t * b.z), fmaf(s, a.w, t * b.w));
 }
 
+// 1 / (|u| + eps) from the sum of u's squares.  A matrix of zeros stays one; one with a value that is not finite becomes NaN throughout (1 / infinity would
+// leave its finite values zeros).  The sum of finite fp32 squares is finite in 64 bits.
+__device__ __forceinline__ double inverse_norm(double squares, float eps) {
+  const double d = sqrt(squares) + (double)eps;
+  return !isfinite(squares) ? nan("") : d > 0.0 ? 1.0 / d : 0.0;
+}
+
 constexpr int AHEAD = 4;                            // fours of a thread in flight
 // the new momentum, and the sum of the squares of u in 64 bits (whose range holds any)
 template <typename TG, int VEC>
@@ -724,8 +731,7 @@ __global__ void __launch_bounds__(256) ortho_scale_kernel(const PrepP p, int blo
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 8; ++w) sum += s_sum[w];
-    const double d = sqrt(sum) + (double)p.eps;
-    s_inv = (d > 0.0 ? 1.0 / d : d == 0.0 ? 0.0 : d) * (p.O ? 1.0 : (double)(1 << X_EXP));      // (a matrix of zeros stays one; NaN stays NaN)
+    s_inv = inverse_norm(sum, p.eps) * (p.O ? 1.0 : (double)(1 << X_EXP));
   }
   __syncthreads();
   if (e < 0) return;
@@ -908,8 +914,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) ortho_small_kernel(const __g
     asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(d) : "r"(map_to_rank(smem_u32(&s_total), r)));
     norm += d;
   }
-  norm = sqrt(norm) + (double)p.in.eps;
-  const double inv = (norm > 0.0 ? 1.0 / norm : norm == 0.0 ? 0.0 : norm) * (double)(1 << X_EXP);      // (a matrix of zeros stays one; NaN stays NaN)
+  const double inv = inverse_norm(norm, p.in.eps) * (double)(1 << X_EXP);
 
   for (int step = 0; step <= p.steps; ++step) {
     // X (after the last step O), and its fp16 copy

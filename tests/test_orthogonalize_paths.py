@@ -48,3 +48,23 @@ def test_slices_of_several_matrices(batch, m, n):
     ws = torch.full((nb,), 255, dtype=torch.uint8, device="cuda")
     for _ in range(8):
         assert torch.equal(ppu.ppu_orthogonalize(G, workspace=ws)[0], ref)
+
+
+@gpu
+@pytest.mark.parametrize("momentum", [False, True])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("m,n", [(48, 80), (130, 200), (200, 131), (40, 2100)])
+def test_values_that_are_not_finite(m, n, steps, momentum):
+    """A matrix with one is NaN throughout, without a step too; the others of its batch are as without it."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    G = cuda(matrices(3, m, n))
+    kw = dict(steps=steps, momentum=0.5 * G if momentum else None)
+    ref = ppu.ppu_orthogonalize(G, **kw)[0]
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        for where in ("G", "momentum") if momentum else ("G",):
+            g, old = G.clone(), kw["momentum"].clone() if momentum else None
+            (g if where == "G" else old)[1, m - 1, 3] = bad
+            got = ppu.ppu_orthogonalize(g, **dict(kw, momentum=old))[0]
+            assert torch.isnan(got[1]).all() and torch.equal(got[0], ref[0]) and torch.equal(got[2], ref[2])
+    assert not ppu.ppu_orthogonalize(0 * G, steps=steps)[0].any() and not ppu.ppu_orthogonalize(G, steps=steps, eps=float("inf"))[0].any()
