@@ -439,7 +439,7 @@ int ppu_qk_norm_bwd(const void* dout, int64_t ldy, const void* qkv, int64_t ldx,
 /* ---- orthogonalised update of matrices ---------------------------------------------------
  *
  * For `batch` matrices G[m,n] (ppu_type g_type; strides in elements: ldg of rows, stride_g of matrices, so that the same
- * matrix of every layer of the canonical vector is one call):
+ * matrix of every layer of the canonical vector is one call, or the heads of one projection, whose rows lie beside one another):
  *   m' = beta momentum + weight G;  u = nesterov ? weight G + beta m' : m'    (momentum null: u = G)
  *   X = u / (|u|_F + eps);  steps times, with the step's (a, b, c):  A = X X^T, X = a X + (b A + c A A) X;  O = scale X
  * (A = X^T X and X = a X + X (b A + c A A) for m > n, which is the same).  With the usual coefficients (3.4445, -4.7750, 2.0315) five

@@ -446,7 +446,9 @@ Matrices matrices(const at::Tensor& t, const char* name, at::ScalarType type, at
   const int64_t m = t.size(k - 2), n = t.size(k - 1), batch = k == 3 ? t.size(0) : 1;
   Matrices r = {t.data_ptr(), m > 1 ? t.stride(k - 2) : n, 0};
   r.stride = batch > 1 ? t.stride(0) : m * r.ld;
-  if ((n > 1 && t.stride(k - 1) != 1) || r.ld < n || (batch > 1 && r.stride < (m - 1) * r.ld + n))
+  // (one matrix behind another, or the rows of all matrices beside one another: the heads of one projection)
+  const bool behind = r.stride >= (m - 1) * r.ld + n, beside = r.stride >= n && r.ld >= (batch - 1) * r.stride + n;
+  if ((n > 1 && t.stride(k - 1) != 1) || r.ld < n || (batch > 1 && !behind && !beside))
     refuse(std::string(name) + ": the values of a row must be adjacent, rows and matrices must not overlap");
   return r;
 }

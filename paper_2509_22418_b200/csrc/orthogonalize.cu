@@ -1302,7 +1302,10 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
   if (batch == 0 || m == 0 || n == 0) return PPU_OK;
   if (!G || !O || !workspace) return ppu_fail(PPU_EINVAL, "null operand");
   if (ldg < n || (momentum && (ldm < n || ldmo < n))) return ppu_fail(PPU_EINVAL, "row strides must be at least n");
-  if (batch > 1 && (stride_g < 0 || (momentum && (stride_m < 0 || stride_mo < (m - 1) * ldmo + n)))) return ppu_fail(PPU_EINVAL, "matrices written must not overlap");
+  if (batch > 1 && (stride_g < 0 || (momentum && stride_m < 0))) return ppu_fail(PPU_EINVAL, "strides must not be negative");
+  // one matrix behind another, or the rows of all matrices beside one another
+  if (batch > 1 && momentum && !(stride_mo >= (m - 1) * ldmo + n || (stride_mo >= n && ldmo >= (batch - 1) * stride_mo + n)))
+    return ppu_fail(PPU_EINVAL, "matrices written must not overlap");
   if (momentum_out == momentum && momentum && (ldm != ldmo || (batch > 1 && stride_m != stride_mo)))
     return ppu_fail(PPU_EINVAL, "momentum_out in the place of momentum needs its strides");
   if (momentum_out && (const void*)momentum_out == G) return ppu_fail(PPU_EINVAL, "G is read again after momentum_out is written: they must not overlap");

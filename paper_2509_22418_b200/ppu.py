@@ -546,7 +546,7 @@ def ppu_orthogonalize_query_bytes(batch, m, n, steps=5) -> int:
 def ppu_orthogonalize(G, momentum=None, beta=0.95, weight=1.0, nesterov=True, steps=5, coef=NEWTON_SCHULZ, eps=1e-7, scale=1.0, in_place=False, workspace=None,
                       flags=None):
     """The update of matrices G [m, n] or [batch, m, n] (bf16 or fp32; rows and matrices may be strided: one matrix of every layer of a parameter
-    vector is a batch) whose singular values are brought to about one: m' = beta momentum + weight G, u = weight G + beta m' (nesterov) or m'
+    vector is a batch, and so are the heads of one projection, whose rows lie beside one another) whose singular values are brought to about one: m' = beta momentum + weight G, u = weight G + beta m' (nesterov) or m'
     (without a momentum u = G); X = u / (|u| + eps); `steps` times A = X X^T, X = a X + (b A + c A A) X; O = scale X.  coef: (a, b, c), or a
     sequence of one such triple for each step.  momentum fp32, G's shape; in_place: m' is written over it (refused where it requires a gradient
     and gradients are recorded).  flags: int32 [8] zeros for ppu_op_status, which reports a bounded wait inside a kernel that ran out; without them the

@@ -68,3 +68,33 @@ def test_values_that_are_not_finite(m, n, steps, momentum):
             got = ppu.ppu_orthogonalize(g, **dict(kw, momentum=old))[0]
             assert torch.isnan(got[1]).all() and torch.equal(got[0], ref[0]) and torch.equal(got[2], ref[2])
     assert not ppu.ppu_orthogonalize(0 * G, steps=steps)[0].any() and not ppu.ppu_orthogonalize(G, steps=steps, eps=float("inf"))[0].any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("m,heads,n", [(96, 5, 40), (300, 4, 136), (70, 3, 33)])
+def test_matrices_whose_rows_lie_beside_one_another(m, heads, n, dtype):
+    """The heads of one projection W [m, heads n]: a batch of [m, n], read and (the momentum) written where it lies."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    G, mom = cuda(matrices(1, m, heads * n)[0], dtype), cuda(matrices(1, m, heads * n + 8, seed=1)[0])
+    view, mv = G.view(m, heads, n).transpose(0, 1), mom[:, : heads * n].unflatten(1, (heads, n)).transpose(0, 1)
+    was = mom.clone()
+    want, wm = ppu.ppu_orthogonalize(view.contiguous(), momentum=mv.contiguous())
+    O, new = ppu.ppu_orthogonalize(view, momentum=mv)
+    assert torch.equal(O, want) and torch.equal(new, wm) and torch.equal(mom, was)
+    O, new = ppu.ppu_orthogonalize(view, momentum=mv, in_place=True)
+    assert torch.equal(O, want) and torch.equal(mv, wm) and torch.equal(mom[:, heads * n:], was[:, heads * n:])
+    for k in (n - 1, 0):                    # rows that overlap in part, or as a whole
+        with pytest.raises(ppu.PpuError):
+            ppu.ppu_orthogonalize(torch.as_strided(G, (heads, m, n), (k, heads * n, 1)))
+
+
+@pytest.mark.parametrize("stride,ld,ok", [(16, 32, True), (128, 16, True), (24, 40, True), (15, 32, False), (16, 31, False), (64, 16, False), (0, 32, False)])
+def test_momentum_written_must_not_overlap(stride, ld, ok):
+    """2 x 8 x 16: accepted strides come as far as the next check (no workspace)."""
+    import ctypes as C
+    import test_orthogonalize as t
+    from paper_2509_22418_b200 import build, ppu
+    build.build()
+    assert t._call(ppu, mom="there", out="else", so=C.c_int64(stride), ldo=C.c_int64(ld), nb=C.c_size_t(100)) == (-4 if ok else -1)
