@@ -1107,15 +1107,17 @@ Plan make_plan(int batch, int m, int n, int steps) {
   q.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((chunks + 1023) / 1024, SMS * 4 / std::min(batch, SMS * 4)));
   auto tiles = [](int64_t x, int t) { return (int)((x + t - 1) / t); };
   // SM pairs on 256 x 256 tiles, or single SMs on 128 x 128.  Pairs read half as much for a product, singles have four times the units to share out and shorter
-  // ones to wait for.  So pairs where the products bound a step, from 20 GFLOP on (28 where a good part of their tiles
-  // is empty), or where there are some waves of full tiles.  A step, us, pairs and singles:
-  // 8192 x 2048 (117 GFLOP) 104 and 144, 2 x 2048 x 2048 60 and 79, 2048 x 2048 (34) 50.1 and 53.0, 4 x 1024 x 2048 (30) 47 and 45, 6 x 1024 x 1024 (26) 38.0 and 37.8,
-  // 24 x 384 x 2048 (23; of its pairs' tiles a quarter is empty) 70 and 55, 12 x 768 x 768 (22) 35.0 and 34.7, 1536 x 2048 (18) 44.7 and 42.4, 4096 x 1024 (14) 49 and 40, 24 x 256 x 2048 (10; 192
-  // full tiles) 38.1 and 40.0, 24 x 256 x 1024 (5; 96) 27.4 and 22.5, 2 x 346 x 2239 32.7 and 22.6.
+  // ones to wait for.  So pairs where the products bound a step, from 28 GFLOP on, unless a good part of their tiles is empty (less than 3.5 tiles of 128 x 128
+  // to one of 256 x 256).  Five steps, us, pairs and singles; in brackets where calls follow one another for half a second (the clock then falls under large products):
+  //   full tiles   8192 x 2048 (112 GFLOP) 590 and 740 (653, 810), 101 x 509 x 481 (47) 702 and 738 (776, 820), 2 x 1700 x 2000 (45) 283 and 354, 4 x 1300 x 1300 (35) 280 and 312,
+  //                2048 x 2048 (34) 269 and 282, 4 x 1024 x 2048 (30) 252 and 255 (267, 281), 7 x 1024 x 1024 (30) 233 and 242, 8 x 900 x 1200 (29) 259 and 303,
+  //                2300 x 1800 (28) 266 and 282;   below: 6 x 1024 x 1024 (26) 222 and 217 (235, 241), 60 x 256 x 2048 (25) 524 and 509 (542, 536), 3 x 1024 x 2048 (23) 240 and 220,
+  //                12 x 768 x 768 (22) 210 and 202 (226, 227), 12 x 512 x 2048 (21) 262 and 264, 48 x 256 x 2048 (20) 435 and 407, 6 x 512 x 4096 (20) 296 and 275, 2 x 1300 x 1300 (18)
+  //                229 and 211, 24 x 256 x 2048 (10) 241 and 239, 24 x 256 x 1024 (5) 167 and 141; but 60 x 200 x 2048 (15) 552 and 591
+  //   others       96 x 384 x 2048 (92) 1532 and 1221, 128 x 260 x 2500 (67) 2443 and 2032, 80 x 300 x 2600 (58) 1497 and 1263, 32 x 384 x 2048 (31) 503 and 421
   const double flop = (double)batch * q.side * q.side * (3.0 * std::max(m, n) + q.side);
   const int64_t singles = (int64_t)tiles(m, 128) * tiles(n, 128) * batch, pairs = (int64_t)tiles(m, 256) * tiles(n, 256) * batch;
-  const bool full = 2 * singles >= 7 * pairs;
-  q.pair = q.side > 128 && (flop >= (full ? 20e9 : 28e9) || (full && 2 * pairs >= 5 * (SMS / 2)));
+  q.pair = q.side > 128 && flop >= 28e9 && 2 * singles >= 7 * pairs;
   const int t = q.pair ? 256 : 128;
   q.workers = q.pair ? SMS / 2 : SMS;
   q.tiles_s = tiles(q.side, t); q.sym = q.tiles_s * (q.tiles_s + 1) / 2;

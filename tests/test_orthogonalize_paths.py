@@ -1,8 +1,10 @@
 """Further calls of the orthogonalised update (ppu_orthogonalize), by the way that their matrices take through the kernels: on chip (sides up to 128, a
 cluster to a matrix), or step by step through memory on single SMs or SM pairs.  References and bounds are those of test_orthogonalize.py."""
+import math
+
 import pytest
 
-from test_orthogonalize import cuda, matrices, near
+from test_orthogonalize import BF, cuda, f32, matrices, near, on_gpu
 
 gpu = pytest.mark.gpu
 
@@ -98,3 +100,35 @@ def test_momentum_written_must_not_overlap(stride, ld, ok):
     from paper_2509_22418_b200 import build, ppu
     build.build()
     assert t._call(ppu, mom="there", out="else", so=C.c_int64(stride), ldo=C.c_int64(ld), nb=C.c_size_t(100)) == (-4 if ok else -1)
+
+
+def against_64_bits(G, old=None):
+    """G [batch, m, n] (and a momentum) by ppu_orthogonalize, within the bounds of test_matrices_of_many_tiles; and the same bits again."""
+    import torch
+    from paper_2509_22418_b200 import ppu
+    flags = torch.zeros(8, dtype=torch.int32, device="cuda")
+    O, new = ppu.ppu_orthogonalize(G, momentum=old, flags=flags)
+    ppu.ppu_op_status(flags)
+    u = G.double() if old is None else G.double() + f32(0.95) * new.double()
+    off, err, limit, most = distances(O.double(), u)
+    assert bool((off <= limit).all()), (float(off.max()), float(limit.min()))
+    assert bool((err <= most).all())
+    assert torch.equal(ppu.ppu_orthogonalize(G, momentum=old)[0], O)
+
+
+def distances(O, u):
+    """Root mean square of O - O in 64 bits, over its size; each value's; and the bounds of both."""
+    want, mod = on_gpu(u, False), on_gpu(u, True)
+    size = want.square().mean((1, 2), keepdim=True).sqrt()
+    cost = (mod - want).square().mean((1, 2), keepdim=True).sqrt() / size
+    err = (O - want).abs()
+    return err.square().mean((1, 2), keepdim=True).sqrt() / size, err, 1.25 * cost + BF / math.sqrt(3), (BF + 2.0 ** -7) * want.abs() + 14 * cost * size
+
+
+@gpu
+@pytest.mark.parametrize("batch,m,n", [(32, 384, 2048), (8, 900, 1200), (7, 1024, 1030), (6, 1024, 1024), (24, 256, 2048), (96, 200, 2400), (13, 2500, 260)])
+def test_either_side_of_the_choice_of_tiles(batch, m, n):
+    """Products of some 30 GFLOP a step, on tiles that are full or not: single SMs and SM pairs."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    against_64_bits(torch.randn(batch, m, n, generator=g, device="cuda"))
