@@ -1299,6 +1299,8 @@ extern "C" int ppu_orthogonalize(const void* G, int64_t ldg, int64_t stride_g, i
     top = 1.01 * largest_value(c[0], c[1], c[2], top);
     if (!(top <= 2.8) || !(poly <= 1024.0) || !(std::fabs((double)c[0]) <= 1024.0))
       return ppu_fail(PPU_EINVAL, "the coefficients of step %d take singular values up to %g, above 2.8", k, top);
+    // (X's second number loses its digits with X: at 2^-10 values of 2^-13 of the norm keep 14 bits; zeros are exact)
+    if (top > 0.0 && top < 0x1p-10) return ppu_fail(PPU_EINVAL, "the coefficients of step %d leave no singular value above %g, below 2^-10", k, top);
     p_exp[k] = std::min(12, (int)std::floor(std::log2(32768.0 / std::max(poly, 1e-30))));
   }
   if (batch == 0 || m == 0 || n == 0) return PPU_OK;

@@ -185,3 +185,26 @@ def test_the_bounds_see_x_second_number(m, n):
     limit = 1.25 * rms(mod - want) / size + BF / math.sqrt(3)
     off = {k: float((rms(carried(u, f) - want) / size).max()) for k, f in (("there", lambda x: x), ("none", np.zeros_like), ("shifted", lambda x: np.roll(x, 32, 2)))}
     assert off["there"] <= float(limit.max()) and off["none"] > 2 * float(limit.max()) and off["shifted"] > 2 * float(limit.max()), (off, float(limit.max()))
+
+
+# ---- coefficients that make X smaller -------------------------------------------------------------------
+HALF = (0.5, 0.0, 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("m,n", [(72, 136), (200, 260)])
+@pytest.mark.parametrize("steps,coef", [(9, HALF), (12, [HALF] * 9 + [(3.0, -3.0, 1.0)] * 3), (2, (0.0, 0.0, 0.0))])
+def test_coefficients_that_make_x_smaller(steps, coef, m, n):
+    from paper_2509_22418_b200 import ppu
+    x = matrices(2, m, n)
+    near(ppu.ppu_orthogonalize(cuda(x), steps=steps, coef=coef, scale=100.0)[0], x.astype(np.float64), steps=steps, coef=coef, scale=100.0)
+
+
+@pytest.mark.parametrize("coef,steps,code", [(HALF, 32, -1), (HALF, 11, -1), (HALF, 9, -4), ((1e-4, 0.0, 0.0), 1, -1), ((1e-20, 0.0, 0.0), 1, -1), ((0.0, 0.0, 0.0), 32, -4)])
+def test_coefficients_that_leave_x_without_digits_are_refused(coef, steps, code):
+    """What was carried of X fell below fp16's range step by step: after 32 halvings the result was zeros.  (-4: accepted, no workspace.)"""
+    import ctypes as C
+    import test_orthogonalize as t
+    from paper_2509_22418_b200 import build, ppu
+    build.build()
+    assert t._call(ppu, coef=t._coef(*coef), steps=steps, nb=C.c_size_t(100)) == code
