@@ -9,8 +9,8 @@
   head  --m T --n V --k D [--teacher K] [--grad xe|x|e|none]  head loss of T rows against V ids (cross entropy, or
                                                        distillation from K teacher entries)
   norm  --m T --k D [--rms] [--gate-rows R]            gated norm pair, forward and backward
-  embed --m T --n V --k D [--f32] [--add]              lookup of T tokens and the table's gradient (--f32: in fp32; --add: on top of
-                                                       another one)
+  embed --m T --n V --k D [--f32] [--add | --in-place] lookup of T tokens and the table's gradient (--f32: in fp32; --add: on top of
+                                                       another one, --in-place: in its place)
   qk    --batch B --seq S --heads H [--kv-heads K] --dh D      norms of queries and keys with rotation, forward and backward
   ortho --batch B --m M --k N [--f32] [--momentum]     orthogonalised update of B matrices M x N (--f32: of fp32 ones)
 Times with CUDA events on the launching stream after warm-up; operands are sized by the caller
@@ -51,6 +51,7 @@ def main():
     ap.add_argument("--rms", action="store_true")
     ap.add_argument("--gate-rows", type=int, default=0, help="norm: rows that share a row of the gate (0: all of them)")
     ap.add_argument("--add", action="store_true", help="embed: the gradient is added to another one")
+    ap.add_argument("--in-place", action="store_true", help="embed: the gradient is formed in the place of another one")
     ap.add_argument("--kv-heads", type=int, default=0, help="qk: heads of keys and of values (0: as many as queries)")
     ap.add_argument("--momentum", action="store_true", help="ortho: with a momentum")
     ap.add_argument("--iters", type=int, default=10)
@@ -135,11 +136,12 @@ def main():
         word, size = ("fp32", 4) if a.f32 else ("bf16", 2)
         ids = torch.randint(0, V, (T,), generator=g, dtype=torch.int32).to(dev)
         E, dout = torch.randn((V, d), generator=g).to(dev).bfloat16(), torch.randn((T, d), generator=g).to(dev)
-        add = torch.randn((V, d), generator=g).to(dev).to(torch.float32 if a.f32 else torch.bfloat16) if a.add else None
+        add = torch.randn((V, d), generator=g).to(dev).to(torch.float32 if a.f32 else torch.bfloat16) if a.add or a.in_place else None
+        moved = 2 * size * ids.unique().numel() * d if a.in_place else (2 if a.add else 1) * size * V * d      # (in place: the rows with tokens)
         ms = timed(lambda: ppu.ppu_embed_fwd(ids, E))
         print(f"embed fwd T={T} V={V} d={d}: {ms:.4f} ms {6.0 * T * d / ms / 1e6:.0f} GB/s")
-        ms = timed(lambda: ppu.ppu_embed_bwd(ids, dout, V, dtype=word, add=add))
-        print(f"embed bwd to {word} add={a.add}: {ms:.4f} ms {(4.0 * T * d + (2 if a.add else 1) * size * V * d) / ms / 1e6:.0f} GB/s")
+        ms = timed(lambda: ppu.ppu_embed_bwd(ids, dout, V, dtype=word, add=add, in_place=a.in_place))
+        print(f"embed bwd to {word} add={a.add} in_place={a.in_place}: {ms:.4f} ms {(4.0 * T * d + moved) / ms / 1e6:.0f} GB/s")
     elif a.op == "qk":
         T, kv, dh = a.batch * a.seq, a.kv_heads or a.heads, a.dh
         x = torch.randn((T, (a.heads + 2 * kv) * dh), generator=g).to(dev).bfloat16()
