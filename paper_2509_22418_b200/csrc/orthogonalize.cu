@@ -13,16 +13,20 @@
 // P (so that what P annuls it annuls as a whole): it comes to -2.7 where singular values come to one, and half a step of fp16 there is 2^-10 of X.
 // Root mean square error of O relative to O's (5 steps, CPU model; the rounding of O to bf16 is 1.66e-3): bf16 operands and X 1e-2 for random matrices, 0.16 to
 // 0.35 for those with a few large directions; fp16 operands and X 1.3e-3 and 2e-2 to 4e-2; with X carried so 1.4e-3 (sides of 768), 1.7e-3 (256), 2.4e-3 (33)
-// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4, for 2 to 9 % more time (8192 x 2048 106 -> 108 us a step, 24 x 256 x 2048
-// 37.3 -> 39.7, 12 x 768 x 768 35.0 -> 38.2).  Sides up to 128 are mostly worked on chip, below.
+// and 2e-4 to 7e-4; with P's diagonal too 1.3e-3 (256), 1.5e-3 (130) and 2e-4 to 6e-4.  Sides up to 128 are mostly worked on chip, below.
+// Measured, O's rounding included, without P's diagonal and with it, and five steps' time: 24 x 33 x 2100 3.3e-3 and 2.4e-3, 131 and 148 us; 24 x 64 x 2100 2.5e-3 and
+// 2.1e-3, 138 and 155; 24 x 255 x 2100 2.4e-3 and 2.1e-3, 268 and 304; 24 x 256 x 2048 2.35e-3 and 2.06e-3, 241 and 271; 40 x 448 x 4096 2.6e-3 and 2.1e-3, 1292 and 1502;
+// 12 x 768 x 768 2.2e-3 and 2.0e-3, 206 and 217; 8192 x 2048 2.1e-3 and 1.9e-3, 586 and 609.  So it pays for short sides, whose error would else be the largest of all;
+// from 256 on the time is left as it is at an error of 2.8e-3 at most (sides of 350 to 450 of random matrices 12000 long).
 //
 // A and A A are symmetric: only tiles on and below the diagonal are worked and stored; a block above it is read as its
 // mirror image, which tensor cores take in the other order of its elements.  (With the tiles stored on both sides, two bytes at a time down
 // the columns, a tile of 128 x 128 took 7 us more.)
 //
-// What bounds it.  8192 x 2048: 117 GFLOP a step in 104 to 106 us (1110 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
+// What bounds it.  8192 x 2048: 112 GFLOP a step in 104 to 107 us (1060 TFLOP/s).  At the rate of one large product the three parts would take 24 us (72 slices of
 // A on 74 pairs), 12 (36 tiles of A A) and 43 (256 tiles of X, in three waves and a half); the rest is the ends of the parts, each of which reads what the last warps
-// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 38 us a step for 10 GFLOP and 12 bytes a value of X (151 MB, through the L2): the pass over X's tiles.
+// of the one before it store (5 to 9 us each).  24 x 256 x 2048: 36 to 43 us a step (by where its buffers lie) for 10 GFLOP and 12 bytes a value of X (151 MB, through the L2): 8 of them, 100 MB, in the
+// pass over X's tiles, which is most of a step, 2 as A's operand and 2 as that of P X.
 #include <algorithm>
 #include <cmath>
 #include <cuda_fp16.h>
@@ -292,7 +296,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
 template <bool PAIR, bool DIAG>
 __device__ __forceinline__ void ortho_steps(const CUtensorMap* maps, const KernelP& p) {
   constexpr int CTAS = PAIR ? 2 : 1, TILE = 128 * CTAS;
-  constexpr int PIECES = 4;                     // of W columns, fetched ahead (203 x 333, a step: one 19.7 us, two 18.1, four 17.2; 24 x 256 x 2048: 45, 42.3, 41.6)
+  constexpr int PIECES = 4;                     // of W columns, fetched ahead (203 x 333, a step, when this was chosen: one 19.7 us, two 18.1, four 17.2; 24 x 256 x 2048 on pairs: 45, 42.3, 41.6)
   extern __shared__ uint8_t smem_raw[];
   // (the window starts at the same offset in both CTAs of a pair, so aligned offsets match too)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
