@@ -448,7 +448,7 @@ int ppu_qk_norm_bwd(const void* dout, int64_t ldy, const void* qkv, int64_t ldx,
  * step; coefficients that would take singular values above 2.8, or all of them below 2^-10 (but not to 0), are refused.  O: bf16 [batch, m, n] contiguous.
  * The products' operands are fp16; X is carried as a pair of fp16 (22 bits; sides up to 128 in fp32): O's root mean square error, beside its rounding
  * to bf16 (1.7e-3), is 0.2e-3 to 1.8e-3 of its root mean square, for sides of 256 to 640 of long random matrices up to 2.3e-3, of matrices of some ten rows up to
- * 2.5e-3.  Where |u| is far below eps, and so O small, it is 1e-8 scale at most.  A matrix of zeros gives zeros; one with a value that is not finite gives NaN throughout.
+ * 2.5e-3, of a few values up to 1e-2.  Where |u| is far below eps, and so O small, it is 1e-8 scale at most.  A matrix of zeros gives zeros; one with a value that is not finite gives NaN throughout.
  * Sides up to 65536, steps up to 32.  workspace: DEVICE, 256-byte aligned, the size ppu_orthogonalize_query_bytes gives; calls that may overlap
  * on the GPU need one each.  flags as for the head losses (PPU_ETIMEOUT alone), may be null.  Other pointers DEVICE, O 16-byte aligned.
  * Asynchronous on the stream; may be captured; the same inputs give the same bits. */
